@@ -23,6 +23,15 @@
  *   flare_verify_commit       restore the state at the accepted offset
  *   flare_block_softmax_attn  with the per-row ROW_TYPE mask modes
  *
+ * and the same attention work for a tree of drafted tokens, with the decision
+ * which of them the target accepts (a chain is a tree with one child per node):
+ *
+ *   flare_tree_softmax_attn   a tree's queries over paged prefix + ancestors
+ *   flare_tree_linear_attn    gated delta rule along every root path
+ *   flare_tree_verify         acceptance from given random numbers, next token
+ *   flare_tree_commit_state   recurrent state after the accepted path
+ *   flare_tree_append_kv      the accepted path's rows into the paged caches
+ *
  * and, for training, the fused two-stream forward of a GDN layer:
  *
  *   flare_two_stream_fwd      noisy blocks seeded from the on-chip clean state
@@ -100,6 +109,18 @@ typedef enum flare_mask_mode {
 #define FLARE_DEV_BAD_VERIFY_LEN 0x20 /* verify_len[r] outside [0, min(max_verify, block_len-1)],
                                          or an accepted offset outside [0, verify_len[r]] */
 
+#define FLARE_DEV_BAD_TREE 0x40 /* node_len[r] outside [0, N], parent[r] no tree in topological
+                                   order, a drafted token outside the vocabulary, or a path entry
+                                   outside [0, N) */
+#define FLARE_DEV_BAD_LOGITS 0x80 /* a logits row that the result needs has a NaN, a +inf, or no
+                                     finite entry */
+
+/* How flare_tree_verify accepts drafted tokens. */
+typedef enum flare_verify_mode {
+  FLARE_VERIFY_GREEDY = 0, /* a draft is accepted when it is the target's most likely token */
+  FLARE_VERIFY_SAMPLE = 1  /* with probability min(1, p / q), against given uniforms */
+} flare_verify_mode;
+
 /* Activation applied after the ShortConv. */
 typedef enum flare_activation { FLARE_ACT_NONE = 0, FLARE_ACT_SILU = 1 } flare_activation;
 
@@ -159,6 +180,19 @@ typedef struct flare_conv_desc {
   flare_dtype act_dtype;
   flare_activation activation;
 } flare_conv_desc;
+
+/* Verification shape.
+ *   num_requests R, num_nodes N (1..64; the tree calls' block_len), vocab_size
+ *   V (1 .. 2^24), logits_dtype, mode, inv_temperature (> 0 and finite; scales
+ *   the logits in SAMPLE mode, ignored in GREEDY mode). */
+typedef struct flare_tree_verify_desc {
+  int32_t num_requests;
+  int32_t num_nodes;
+  int32_t vocab_size;
+  flare_dtype logits_dtype;
+  flare_verify_mode mode;
+  float inv_temperature;
+} flare_tree_verify_desc;
 
 /* Two-stream training layer shape (the noisy stream of a GDN layer).
  *   num_seqs N, seq_len L (a multiple of chunk_len), chunk_len C (64, the
@@ -418,6 +452,174 @@ flare_status flare_append_kv(const flare_softmax_desc* desc, const void* k_blk, 
                              void* k_pool, void* v_pool, const int32_t* page_table,
                              const int32_t* prefix_len, const int32_t* append_len,
                              int32_t* dev_status, void* stream);
+
+/*
+ * Tree-drafted decoding
+ * ---------------------
+ * A round of request r holds a tree of n = node_len[r] <= N tokens (N =
+ * desc->block_len, 1..64).  Node 0 is the anchor: the token sampled last,
+ * which neither the cache nor the recurrent state holds yet.  parent[r][i]
+ * names node i's parent: parent[r][0] = -1 and 0 <= parent[r][i] < i for
+ * 0 < i < n; entries from n on are not read.  A node's path is its ancestors
+ * from the anchor on and itself.  n = 1 is ordinary single-token decoding,
+ * n = 0 a request that sits the round out.  Outputs of nodes n .. N-1 are
+ * written as zero.  A request whose node_len or parent row is wrong is flagged
+ * with FLARE_DEV_BAD_TREE and skipped.
+ *   parent    [R, N] int32
+ *   node_len  [R]    int32
+ */
+
+/* Bytes of device workspace flare_tree_softmax_attn needs for `desc` (the
+ * trees' ancestor sets and the partial outputs of key ranges that several
+ * blocks share).  Host-only, no GPU work. */
+flare_status flare_tree_softmax_workspace_size(const flare_softmax_desc* desc, size_t* bytes);
+
+/*
+ * Softmax attention of a drafted tree over a paged KV prefix (Eq.
+ * softmax-retrieval with a tree in the block's place).  Node i of request r
+ * sees the whole prefix and the keys of its own path:
+ *     out[r][i][h] = sum_j softmax_j(scale * q . k_j) v_j
+ *     lse[r][i][h] = log sum_j exp(scale * q . k_j)       (natural log)
+ * over j in prefix ++ path(i); kv head h / (Hq / Hkv).  Nodes from node_len[r]
+ * on see nothing: out = 0, lse = -inf.  Nothing past a prefix's end, in an
+ * unused page or in an unused node is used, whatever it holds.  Work is
+ * spread over the GPU by key tiles, so that one long prefix or many ragged
+ * ones load every SM alike; results do not depend on timing.
+ * desc->mask_mode and row_type are ignored.
+ *   q              [R, N, Hq, D]                 act_dtype
+ *   k_blk, v_blk   [R, N, Hkv, D]                act_dtype, the nodes' keys and values
+ *   k_pool, v_pool [num_pages, Hkv, p, D]        act_dtype
+ *   page_table     [R, max_pages_per_req]        int32
+ *   prefix_len     [R]                           int32
+ *   parent, node_len                             the trees
+ *   out            [R, N, Hq, D]                 act_dtype
+ *   lse            [R, N, Hq]                    fp32, nullable
+ *   workspace      >= flare_tree_softmax_workspace_size bytes, 256-byte aligned
+ *   dev_status     FLARE_DEV_BAD_PAGE | FLARE_DEV_BAD_PREFIX_LEN | FLARE_DEV_BAD_TREE |
+ *                  FLARE_DEV_WAIT_TIMEOUT
+ */
+flare_status flare_tree_softmax_attn(const flare_softmax_desc* desc, const void* q,
+                                     const void* k_blk, const void* v_blk, const void* k_pool,
+                                     const void* v_pool, const int32_t* page_table,
+                                     const int32_t* prefix_len, const int32_t* parent,
+                                     const int32_t* node_len, void* out, float* lse,
+                                     void* workspace, size_t workspace_bytes,
+                                     int32_t* dev_status, void* stream);
+
+/*
+ * Gated delta rule along every path of a drafted tree (Eq. per-step-fwd with
+ * the parent's state in the place of the previous one).  From the committed
+ * state S0 = state_pool[state_slot[r]][j], node i's state is one step from its
+ * parent's (the anchor's from S0), and node i reads its own:
+ *     S_i = step(S_parent(i); k_i, v_i, g_i, beta_i),   out[r][i][j] = scale * S_i^T q_i
+ * (q/k head j / (Hv / Hk)).  The state pool is read and never written; slots
+ * may repeat.
+ *   q, k [R, N, Hk, dk], v [R, N, Hv, dv]   act_dtype
+ *   log_decay, beta [R, N, Hv]              fp32
+ *   state_pool  [num_state_slots, Hv, dk, dv] fp32
+ *   state_slot  [R]                         int32
+ *   parent, node_len                        the trees
+ *   out         [R, N, Hv, dv]              act_dtype
+ *   dev_status  FLARE_DEV_BAD_SLOT | FLARE_DEV_BAD_TREE | FLARE_DEV_WAIT_TIMEOUT
+ */
+flare_status flare_tree_linear_attn(const flare_linear_desc* desc, const void* q, const void* k,
+                                    const void* v, const float* log_decay, const float* beta,
+                                    const float* state_pool, const int32_t* state_slot,
+                                    const int32_t* parent, const int32_t* node_len, void* out,
+                                    int32_t* dev_status, void* stream);
+
+/* Bytes of device workspace flare_tree_verify needs (row statistics).  Host-only. */
+flare_status flare_tree_verify_workspace_size(const flare_tree_verify_desc* desc, size_t* bytes);
+
+/*
+ * Which drafted tokens the target accepts, and the token after them.  Row i of
+ * logits is the target's output at node i: p_i = softmax(logits[r][i] *
+ * inv_temperature) is the distribution of i's children.  The walk starts at
+ * the anchor; at node c it tries c's children s in index order and moves to
+ * the first one accepted, until none is.
+ *   GREEDY: s is accepted when token[r][s] is the argmax of row c (the lowest
+ *     index among equals); next_token is the argmax of the last node's row.
+ *   SAMPLE with draft_probs (c's children drawn independently from q_c =
+ *     draft_probs[r][c]): w = p_c, m = 1 at first; s is accepted when
+ *     uniform[r][s] * q_c(x) * m < w(x), x = token[r][s]; otherwise the
+ *     rejected draft's distribution is taken off: w <- max(w - m q_c, 0), m <- sum w.
+ *   SAMPLE without draft_probs (NULL: the drafts are a drafter's fixed
+ *     choices): as above with q_c one at the tried token: accepted when
+ *     uniform[r][s] * m < w(x), else w(x) <- 0, m <- sum w.
+ *   SAMPLE: next_token is the lowest x with the greatest w(x) / noise[r][x];
+ *     with noise ~ Exp(1) that samples w.  A w without mass counts as p_c.
+ * The accepted tokens then follow the target's distribution exactly (the
+ * accept rule min(1, p/q) and residual [p - q]_+ of eq. accept-exact, applied
+ * once per sibling).
+ * node_logp[r][i] = log p_parent(i)(token[r][i]) for every drafted node
+ * (unscaled logits in GREEDY mode), 0 for the anchor and unused nodes.
+ * Logits may be -inf (tokens ruled out).  Rows of nodes without children are
+ * read only where the walk ends; a row that is read must have a finite maximum
+ * and no NaN, else FLARE_DEV_BAD_LOGITS and the request's outputs stay
+ * untouched.
+ *   logits      [R, N, V] logits_dtype (any V; rows need no alignment)
+ *   draft_probs [R, N, V] fp32, nullable; read at nodes with children; ignored in GREEDY mode
+ *   token       [R, N]    int32, the drafted tokens (token[r][0] is not read)
+ *   parent, node_len      the trees
+ *   uniform     [R, N]    fp32 in [0, 1), one per node; nullable in GREEDY mode
+ *   noise       [R, V]    fp32 > 0; nullable in GREEDY mode
+ *   path        [R, N]    int32: the accepted nodes, path[r][0] = 0, then -1
+ *   path_len    [R]       int32: how many (0 where node_len[r] = 0)
+ *   next_token  [R]       int32 (-1 where node_len[r] = 0)
+ *   node_logp   [R, N]    fp32
+ *   workspace   >= flare_tree_verify_workspace_size bytes, 256-byte aligned
+ *   dev_status  FLARE_DEV_BAD_TREE | FLARE_DEV_BAD_LOGITS
+ */
+flare_status flare_tree_verify(const flare_tree_verify_desc* desc, const void* logits,
+                               const float* draft_probs, const int32_t* token,
+                               const int32_t* parent, const int32_t* node_len,
+                               const float* uniform, const float* noise, int32_t* path,
+                               int32_t* path_len, int32_t* next_token, float* node_logp,
+                               void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                               void* stream);
+
+/*
+ * State commit of an accepted path: with n = path_len[r] in [0, N] and nodes
+ * path[r][0 .. n-1] of the round's inputs,
+ *     state_pool[dst_slot[r]][j] <- the state after those tokens from
+ *                                   state_pool[src_slot[r]][j].
+ * dst_slot[r] = src_slot[r] commits in place (n = 0 then leaves the slot
+ * untouched); another slot keeps the source and forks it (n = 0 is a copy), and
+ * several requests may share a source.  Exact fp32 recurrence.
+ * Precondition: the dst_slot entries are distinct, and none is another
+ * request's src_slot.
+ *   k [R, N, Hk, dk], v [R, N, Hv, dv]      act_dtype
+ *   log_decay, beta [R, N, Hv]              fp32
+ *   state_pool  [num_state_slots, Hv, dk, dv] fp32, read and written
+ *   src_slot, dst_slot, path_len [R], path [R, N]   int32
+ *   dev_status  FLARE_DEV_BAD_SLOT | FLARE_DEV_BAD_ACCEPT_LEN (path_len) | FLARE_DEV_BAD_TREE
+ *               (a path entry); the request is skipped.
+ */
+flare_status flare_tree_commit_state(const flare_linear_desc* desc, const void* k, const void* v,
+                                     const float* log_decay, const float* beta,
+                                     float* state_pool, const int32_t* src_slot,
+                                     const int32_t* dst_slot, const int32_t* path,
+                                     const int32_t* path_len, int32_t* dev_status, void* stream);
+
+/*
+ * KV append of an accepted path, every softmax layer's caches in one launch:
+ * for layer l, request r and t < n = path_len[r], row path[r][t] of k_blk[l],
+ * v_blk[l] is copied bit for bit to prefix position prefix_len[r] + t of
+ * k_pool[l], v_pool[l] (page table as in flare_append_kv).  Nothing else in the
+ * pools changes.
+ *   num_layers     1 .. 64
+ *   k_blk, v_blk   HOST arrays of num_layers DEVICE pointers, each [R, N, Hkv, D] act_dtype
+ *   k_pool, v_pool HOST arrays of num_layers DEVICE pointers, each [num_pages, Hkv, p, D]
+ *   page_table [R, max_pages_per_req], prefix_len, path_len [R], path [R, N]   int32
+ *   dev_status     FLARE_DEV_BAD_ACCEPT_LEN, FLARE_DEV_BAD_PREFIX_LEN, FLARE_DEV_BAD_PAGE (as in
+ *                  flare_append_kv), FLARE_DEV_BAD_TREE (a path entry); the request is skipped.
+ */
+flare_status flare_tree_append_kv(const flare_softmax_desc* desc, int32_t num_layers,
+                                  const void* const* k_blk, const void* const* v_blk,
+                                  void* const* k_pool, void* const* v_pool,
+                                  const int32_t* page_table, const int32_t* prefix_len,
+                                  const int32_t* path, const int32_t* path_len,
+                                  int32_t* dev_status, void* stream);
 
 /* Size of the library-owned scratch array used by flare_block_softmax_attn_noalloc. */
 #define FLARE_NOALLOC_SCRATCH_BYTES (64u * 1024u * 1024u)

@@ -87,6 +87,40 @@ SoftmaxPlan plan_for(const flare_softmax_desc* d) {
                       d->act_dtype == FLARE_DT_BF16, device_sms());
 }
 
+// The tree calls read no mask fields of a softmax descriptor.
+flare_status check_tree_softmax(const flare_softmax_desc* d) {
+  if (!d) return FLARE_ERR_INVALID_ARGUMENT;
+  flare_softmax_desc t = *d;
+  t.mask_mode = FLARE_MASK_BLOCK_BIDIR;
+  t.row_type = nullptr;
+  return check_softmax(&t);
+}
+
+TreeSoftmaxPlan tree_plan_for(const flare_softmax_desc* d) {
+  return plan_tree_softmax(d->num_requests, d->block_len, d->num_q_heads, d->num_kv_heads,
+                           d->head_dim, d->page_size, d->max_pages_per_req,
+                           d->act_dtype == FLARE_DT_BF16, device_sms());
+}
+
+flare_status check_tree_verify(const flare_tree_verify_desc* d) {
+  if (!d) return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_requests < 0 || d->num_nodes < 1 || d->vocab_size < 1 ||
+      !valid_dtype(d->logits_dtype) ||
+      (d->mode != FLARE_VERIFY_GREEDY && d->mode != FLARE_VERIFY_SAMPLE))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->mode == FLARE_VERIFY_SAMPLE &&
+      (!(d->inv_temperature > 0.f) || !(d->inv_temperature < 3.0e38f)))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_nodes > 64 || d->vocab_size > (1 << 24)) return FLARE_ERR_UNSUPPORTED;
+  return FLARE_OK;
+}
+
+// Bytes of row statistics, with the cut of a row into chunks.
+size_t tree_verify_workspace(const flare_tree_verify_desc* d, int* chunk, int* n_chunks) {
+  plan_tree_verify(d->num_requests, d->num_nodes, d->vocab_size, device_sms(), chunk, n_chunks);
+  return (size_t)d->num_requests * d->num_nodes * *n_chunks * sizeof(float4);
+}
+
 }  // namespace
 
 namespace flare {
@@ -518,6 +552,248 @@ flare_status flare_append_kv(const flare_softmax_desc* d, const void* k_blk, con
   const int elem = d->act_dtype == FLARE_DT_BF16 ? 2 : 4;
   const cudaError_t e = launch_append_kv(p, append_len, k_pool, v_pool, elem,
                                          static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_tree_softmax_workspace_size(const flare_softmax_desc* d, size_t* bytes) {
+  flare_status st = check_tree_softmax(d);
+  if (st != FLARE_OK) return st;
+  if (!bytes) return FLARE_ERR_INVALID_ARGUMENT;
+  *bytes = d->num_requests == 0 ? 0 : tree_plan_for(d).workspace_bytes;
+  return FLARE_OK;
+}
+
+flare_status flare_tree_softmax_attn(const flare_softmax_desc* d, const void* q,
+                                     const void* k_blk, const void* v_blk, const void* k_pool,
+                                     const void* v_pool, const int32_t* page_table,
+                                     const int32_t* prefix_len, const int32_t* parent,
+                                     const int32_t* node_len, void* out, float* lse,
+                                     void* workspace, size_t workspace_bytes,
+                                     int32_t* dev_status, void* stream) {
+  flare_status st = check_tree_softmax(d);
+  if (st != FLARE_OK) return st;
+  if (!q || !k_blk || !v_blk || !prefix_len || !parent || !node_len || !out || !dev_status)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->max_pages_per_req > 0 && (!k_pool || !v_pool || !page_table))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (!aligned16(q) || !aligned16(k_blk) || !aligned16(v_blk) || !aligned16(k_pool) ||
+      !aligned16(v_pool) || !aligned16(out))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_requests == 0) return FLARE_OK;
+  const TreeSoftmaxPlan plan = tree_plan_for(d);
+  if (workspace_bytes < plan.workspace_bytes || !workspace || ((uintptr_t)workspace & 255u))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  TreeSoftmaxParams p;
+  memset(&p, 0, sizeof p);
+  p.R = d->num_requests;
+  p.N = d->block_len;
+  p.Hq = d->num_q_heads;
+  p.Hkv = d->num_kv_heads;
+  p.G = d->num_q_heads / d->num_kv_heads;
+  p.D = d->head_dim;
+  p.page_size = d->page_size;
+  p.num_pages = d->num_pages;
+  p.max_pages = d->max_pages_per_req;
+  p.scale_log2 = d->scale * 1.4426950408889634f;
+  p.q = q;
+  p.k_blk = k_blk;
+  p.v_blk = v_blk;
+  p.k_pool = k_pool;
+  p.v_pool = v_pool;
+  p.page_table = page_table;
+  p.prefix_len = prefix_len;
+  p.parent = parent;
+  p.node_len = node_len;
+  p.out = out;
+  p.lse = lse;
+  p.gangs = plan.gangs;
+  p.row_tiles = plan.row_tiles;
+  p.tile_rows = plan.tile_rows;
+  char* ws = static_cast<char*>(workspace);
+  p.tiles = reinterpret_cast<int32_t*>(ws + plan.tiles_off);
+  p.first = reinterpret_cast<long long*>(ws + plan.first_off);
+  p.anc = reinterpret_cast<uint64_t*>(ws + plan.anc_off);
+  p.part_o = reinterpret_cast<float*>(ws + plan.part_o_off);
+  p.part_lse = reinterpret_cast<float*>(ws + plan.part_lse_off);
+  p.dev_status = dev_status;
+  const cudaError_t e = launch_tree_softmax(p, d->act_dtype == FLARE_DT_BF16,
+                                            static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_tree_linear_attn(const flare_linear_desc* d, const void* q, const void* k,
+                                    const void* v, const float* log_decay, const float* beta,
+                                    const float* state_pool, const int32_t* state_slot,
+                                    const int32_t* parent, const int32_t* node_len, void* out,
+                                    int32_t* dev_status, void* stream) {
+  flare_status st = check_linear(d);
+  if (st != FLARE_OK) return st;
+  if (!q || !k || !v || !log_decay || !beta || !state_pool || !state_slot || !parent ||
+      !node_len || !out || !dev_status)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(state_pool) ||
+      !aligned16(out))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if ((int64_t)d->num_requests * d->num_v_heads > INT32_MAX) return FLARE_ERR_UNSUPPORTED;
+  if (d->num_requests == 0) return FLARE_OK;
+  GdrParams p;
+  memset(&p, 0, sizeof p);
+  p.R = d->num_requests;
+  p.B = d->block_len;
+  p.Hk = d->num_qk_heads;
+  p.Hv = d->num_v_heads;
+  p.dk = d->head_dim_k;
+  p.dv = d->head_dim_v;
+  p.nslots = d->num_state_slots;
+  p.scale = d->scale;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.log_decay = log_decay;
+  p.beta = beta;
+  p.state_pool = const_cast<float*>(state_pool);  // read only
+  p.state_slot = state_slot;
+  p.parent = parent;
+  p.node_len = node_len;
+  p.out_causal = out;
+  p.dev_status = dev_status;
+  const cudaError_t e = launch_tree_linear(p, d->act_dtype == FLARE_DT_BF16,
+                                           static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_tree_verify_workspace_size(const flare_tree_verify_desc* d, size_t* bytes) {
+  flare_status st = check_tree_verify(d);
+  if (st != FLARE_OK) return st;
+  if (!bytes) return FLARE_ERR_INVALID_ARGUMENT;
+  int chunk, n_chunks;
+  *bytes = tree_verify_workspace(d, &chunk, &n_chunks);
+  return FLARE_OK;
+}
+
+flare_status flare_tree_verify(const flare_tree_verify_desc* d, const void* logits,
+                               const float* draft_probs, const int32_t* token,
+                               const int32_t* parent, const int32_t* node_len,
+                               const float* uniform, const float* noise, int32_t* path,
+                               int32_t* path_len, int32_t* next_token, float* node_logp,
+                               void* workspace, size_t workspace_bytes, int32_t* dev_status,
+                               void* stream) {
+  flare_status st = check_tree_verify(d);
+  if (st != FLARE_OK) return st;
+  const bool sample = d->mode == FLARE_VERIFY_SAMPLE;
+  if (!logits || !token || !parent || !node_len || !path || !path_len || !next_token ||
+      !node_logp || !dev_status || (sample && (!uniform || !noise)))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  const size_t elem = d->logits_dtype == FLARE_DT_BF16 ? 2 : 4;
+  if ((uintptr_t)logits % elem || (uintptr_t)draft_probs % 4 || (uintptr_t)noise % 4)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_requests == 0) return FLARE_OK;
+  TreeVerifyParams p;
+  memset(&p, 0, sizeof p);
+  const size_t need = tree_verify_workspace(d, &p.chunk, &p.n_chunks);
+  if (workspace_bytes < need || !workspace || ((uintptr_t)workspace & 255u))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  p.R = d->num_requests;
+  p.N = d->num_nodes;
+  p.V = d->vocab_size;
+  p.greedy = !sample;
+  p.inv_temp = sample ? d->inv_temperature : 1.f;
+  p.logits = logits;
+  p.draft_probs = draft_probs;
+  p.token = token;
+  p.parent = parent;
+  p.node_len = node_len;
+  p.uniform = uniform;
+  p.noise = noise;
+  p.path = path;
+  p.path_len = path_len;
+  p.next_token = next_token;
+  p.node_logp = node_logp;
+  p.stats = static_cast<float4*>(workspace);
+  p.dev_status = dev_status;
+  const cudaError_t e = launch_tree_verify(p, d->logits_dtype == FLARE_DT_BF16,
+                                           static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_tree_commit_state(const flare_linear_desc* d, const void* k, const void* v,
+                                     const float* log_decay, const float* beta,
+                                     float* state_pool, const int32_t* src_slot,
+                                     const int32_t* dst_slot, const int32_t* path,
+                                     const int32_t* path_len, int32_t* dev_status, void* stream) {
+  flare_status st = check_linear(d);
+  if (st != FLARE_OK) return st;
+  if (!k || !v || !log_decay || !beta || !state_pool || !src_slot || !dst_slot || !path ||
+      !path_len || !dev_status)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(state_pool)) return FLARE_ERR_INVALID_ARGUMENT;
+  if ((int64_t)d->num_requests * d->num_v_heads > INT32_MAX) return FLARE_ERR_UNSUPPORTED;
+  if (d->num_requests == 0) return FLARE_OK;
+  GdrParams p;
+  memset(&p, 0, sizeof p);
+  p.R = d->num_requests;
+  p.B = d->block_len;
+  p.Hk = d->num_qk_heads;
+  p.Hv = d->num_v_heads;
+  p.dk = d->head_dim_k;
+  p.dv = d->head_dim_v;
+  p.nslots = d->num_state_slots;
+  p.k = k;
+  p.v = v;
+  p.log_decay = log_decay;
+  p.beta = beta;
+  p.state_pool = state_pool;
+  p.state_slot = src_slot;
+  p.dst_slot = dst_slot;
+  p.accept_len = path_len;
+  p.path = path;
+  p.write_state = 1;
+  p.dev_status = dev_status;
+  const cudaError_t e = launch_tree_commit(p, d->act_dtype == FLARE_DT_BF16,
+                                           static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_tree_append_kv(const flare_softmax_desc* d, int32_t num_layers,
+                                  const void* const* k_blk, const void* const* v_blk,
+                                  void* const* k_pool, void* const* v_pool,
+                                  const int32_t* page_table, const int32_t* prefix_len,
+                                  const int32_t* path, const int32_t* path_len,
+                                  int32_t* dev_status, void* stream) {
+  flare_status st = check_tree_softmax(d);
+  if (st != FLARE_OK) return st;
+  if (num_layers < 1) return FLARE_ERR_INVALID_ARGUMENT;
+  if (num_layers > kMaxAppendLayers) return FLARE_ERR_UNSUPPORTED;
+  if (!k_blk || !v_blk || !k_pool || !v_pool || !page_table || !prefix_len || !path ||
+      !path_len || !dev_status)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  TreeAppendParams p;
+  memset(&p, 0, sizeof p);
+  for (int l = 0; l < num_layers; ++l) {
+    if (!k_blk[l] || !v_blk[l] || !k_pool[l] || !v_pool[l] || !aligned16(k_blk[l]) ||
+        !aligned16(v_blk[l]) || !aligned16(k_pool[l]) || !aligned16(v_pool[l]))
+      return FLARE_ERR_INVALID_ARGUMENT;
+    p.k_blk[l] = k_blk[l];
+    p.v_blk[l] = v_blk[l];
+    p.k_pool[l] = k_pool[l];
+    p.v_pool[l] = v_pool[l];
+  }
+  if (d->num_requests == 0) return FLARE_OK;
+  p.R = d->num_requests;
+  p.N = d->block_len;
+  p.Hkv = d->num_kv_heads;
+  p.D = d->head_dim;
+  p.page_size = d->page_size;
+  p.num_pages = d->num_pages;
+  p.max_pages = d->max_pages_per_req;
+  p.n_layers = num_layers;
+  p.elem_bytes = d->act_dtype == FLARE_DT_BF16 ? 2 : 4;
+  p.page_table = page_table;
+  p.prefix_len = prefix_len;
+  p.path = path;
+  p.path_len = path_len;
+  p.dev_status = dev_status;
+  const cudaError_t e = launch_tree_append(p, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
 }
 

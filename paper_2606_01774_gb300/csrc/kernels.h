@@ -30,6 +30,11 @@ struct GdrParams {
   const int32_t* verify_len;  // [R] or nullptr
   int max_verify;
   float* verify_states;       // [R,max_verify,Hv,dk,dv]
+  // drafted trees (B = nodes per tree)
+  const int32_t* parent;      // [R,B]
+  const int32_t* node_len;    // [R]
+  const int32_t* path;        // [R,B] accepted nodes: commit along a path
+  const int32_t* dst_slot;    // [R] where that commit writes
   int32_t* dev_status;
 };
 
@@ -129,6 +134,79 @@ bool two_stream_chunk_supported(int B, int dk, int dv);
 cudaError_t launch_two_stream_chunk(const TwoStreamParams& p, cudaStream_t stream);
 cudaError_t launch_gdr_denoise_tc(const GdrParams& p, cudaStream_t stream);
 cudaError_t launch_gdr_recurrent(const GdrParams& p, bool bf16, cudaStream_t stream);
+
+// Softmax attention of drafted trees.  Work is cut by key tiles (tree_sched.cuh):
+// `gangs` spans of the batch's tiles, each walked by `row_tiles` CTAs.
+struct TreeSoftmaxParams {
+  int R, N, Hq, Hkv, G, D, page_size, num_pages, max_pages;
+  float scale_log2;           // logit scale * log2(e)
+  const void* q;              // [R,N,Hq,D]
+  const void* k_blk;          // [R,N,Hkv,D]
+  const void* v_blk;
+  const void* k_pool;         // [num_pages,Hkv,page_size,D]
+  const void* v_pool;
+  const int32_t* page_table;  // [R,max_pages]
+  const int32_t* prefix_len;  // [R]
+  const int32_t* parent;      // [R,N]
+  const int32_t* node_len;    // [R]
+  void* out;                  // [R,N,Hq,D]
+  float* lse;                 // [R,N,Hq] or nullptr
+  int gangs, row_tiles, tile_rows;
+  int32_t* tiles;             // [R] key tiles per kv head; 0 nothing to do, -1 a bad request
+  long long* first;           // [R+1] first tile of each request in the batch's tile order
+  uint64_t* anc;              // [R,N] path of each node as a bit set
+  float* part_o;              // [2 gangs row_tiles][tile_rows][D] partial outputs
+  float* part_lse;            // [2 gangs row_tiles][tile_rows]
+  int32_t* dev_status;
+};
+
+struct TreeSoftmaxPlan {
+  int gangs, row_tiles, tile_rows;
+  size_t tiles_off, first_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
+};
+
+TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,
+                                  int max_pages, bool bf16, int num_sms);
+cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream);
+
+cudaError_t launch_tree_linear(const GdrParams& p, bool bf16, cudaStream_t stream);
+cudaError_t launch_tree_commit(const GdrParams& p, bool bf16, cudaStream_t stream);
+
+struct TreeVerifyParams {
+  int R, N, V, greedy;
+  float inv_temp;
+  const void* logits;         // [R,N,V]
+  const float* draft_probs;   // [R,N,V] or nullptr
+  const int32_t* token;       // [R,N]
+  const int32_t* parent;      // [R,N]
+  const int32_t* node_len;    // [R]
+  const float* uniform;       // [R,N]
+  const float* noise;         // [R,V]
+  int32_t* path;              // [R,N]
+  int32_t* path_len;          // [R]
+  int32_t* next_token;        // [R]
+  float* node_logp;           // [R,N]
+  int chunk, n_chunks;        // row statistics: tokens per chunk, chunks per row
+  float4* stats;              // [R,N,n_chunks] {max, sum of exp(x - max), first argmax, -}
+  int32_t* dev_status;
+};
+void plan_tree_verify(int R, int N, int V, int num_sms, int* chunk, int* n_chunks);
+cudaError_t launch_tree_verify(const TreeVerifyParams& p, bool bf16, cudaStream_t stream);
+
+constexpr int kMaxAppendLayers = 64;
+struct TreeAppendParams {
+  int R, N, Hkv, D, page_size, num_pages, max_pages, n_layers, elem_bytes;
+  const void* k_blk[kMaxAppendLayers];  // each [R,N,Hkv,D]
+  const void* v_blk[kMaxAppendLayers];
+  void* k_pool[kMaxAppendLayers];       // each [num_pages,Hkv,page_size,D]
+  void* v_pool[kMaxAppendLayers];
+  const int32_t* page_table;            // [R,max_pages]
+  const int32_t* prefix_len;            // [R]
+  const int32_t* path;                  // [R,N]
+  const int32_t* path_len;              // [R]
+  int32_t* dev_status;
+};
+cudaError_t launch_tree_append(const TreeAppendParams& p, cudaStream_t stream);
 
 SoftmaxPlan plan_softmax(int R, int B, int Hq, int Hkv, int D, int page_size, int max_pages,
                          bool bf16, int num_sms);

@@ -1,0 +1,145 @@
+// How the softmax attention of a batch of drafted trees is spread over the GPU.
+//
+// A request with a prefix of P tokens has n = ceil(P / 64) + 1 key tiles per
+// kv head: its prefix, 64 tokens a tile, and one tile with its nodes' own keys
+// (at most 64).  The tiles of the whole batch, in the order (request, kv head,
+// tile), are cut into `gangs` spans of equal length; a gang has one CTA per
+// tile of query rows, and each walks the gang's span for its own rows, so the
+// row tiles read a key tile at about the same time and it leaves DRAM once.
+// Equal spans load every SM alike whether the batch is one long prefix or many
+// ragged ones.  Where a span ends inside a (request, kv head) item, the item's
+// pieces are merged afterwards from partial outputs in a fixed order.  A CTA
+// has at most two partial pieces: slot 0, one that starts inside an item (its
+// first), and slot 1, one that starts an item without finishing it (its last).
+//
+// Prefix lengths live on the device, so every CTA computes the cut itself
+// from the per-request tile counts.
+#pragma once
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace flare {
+
+constexpr int kTreeTile = 64;  // keys per tile
+
+struct TreeSpanShared {
+  long long warp_sum[32];
+  long long lo, hi, off;  // the span, and the first tile's offset in its request
+  int r;
+};
+
+// A stretch of one item's tiles: j0 .. j1 - 1 of n.
+struct TreePiece {
+  int r, kvh, j0, j1, n;
+  __device__ bool whole() const { return j0 == 0 && j1 == n; }
+  __device__ int slot() const { return j0 == 0 ? 1 : 0; }
+};
+
+struct TreeCursor {
+  int r, kvh, j;
+  long long left;
+
+  // The next piece of the span; false at its end.
+  __device__ __forceinline__ bool next(const TreeSoftmaxParams& p, TreePiece& w) {
+    if (left <= 0) return false;
+    int n = p.tiles[r];
+    while (n <= 0) n = p.tiles[++r];
+    w.r = r;
+    w.kvh = kvh;
+    w.j0 = j;
+    w.j1 = (int)(left < n - j ? j + left : n);
+    w.n = n;
+    left -= w.j1 - w.j0;
+    if (w.j1 == n) {
+      j = 0;
+      if (++kvh == p.Hkv) {
+        kvh = 0;
+        ++r;
+      }
+    } else {
+      j = w.j1;
+    }
+    return true;
+  }
+};
+
+// How many of the plan's gangs have work: each of them at least a tile.
+__device__ __forceinline__ int tree_gangs(const TreeSoftmaxParams& p, long long total) {
+  return total < p.gangs ? (int)total : p.gangs;
+}
+
+__device__ __forceinline__ long long shfl_up_ll(long long x, int o) {
+  return __shfl_up_sync(0xffffffffu, x, o);
+}
+
+// The span of `gang`, found by all threads of the CTA together; CTA 0 also
+// records where each request's tiles start.
+template <int THREADS>
+__device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int gang,
+                                                TreeSpanShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per = (p.R + THREADS - 1) / THREADS;
+  const int r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
+  long long sum = 0;
+  for (int r = r0; r < r1; ++r) sum += (long long)max(p.tiles[r], 0) * p.Hkv;
+  long long incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = shfl_up_ll(incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) sh.warp_sum[warp] = incl;
+  __syncthreads();
+  long long before = incl - sum, total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const long long x = sh.warp_sum[w];
+    if (w < warp) before += x;
+    total += x;
+  }
+  const int gangs = tree_gangs(p, total);
+  const long long lo = gang < gangs ? total * gang / gangs : 0;
+  const long long hi = gang < gangs ? total * (gang + 1) / gangs : 0;
+  if (tid == 0) {
+    sh.lo = lo;
+    sh.hi = hi;
+  }
+  if (lo < hi && before <= lo && lo < before + sum) {  // this thread holds the first request
+    long long at = before;
+    int r = r0;
+    for (;; ++r) {
+      const long long n = (long long)max(p.tiles[r], 0) * p.Hkv;
+      if (lo < at + n) break;
+      at += n;
+    }
+    sh.r = r;
+    sh.off = lo - at;
+  }
+  if (blockIdx.x == 0) {
+    long long at = before;
+    for (int r = r0; r < r1; ++r) {
+      p.first[r] = at;
+      at += (long long)max(p.tiles[r], 0) * p.Hkv;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) p.first[p.R] = total;
+  __syncthreads();
+  TreeCursor c;
+  c.left = sh.hi - sh.lo;
+  c.r = c.kvh = c.j = 0;
+  if (c.left > 0) {
+    c.r = sh.r;
+    const int n = p.tiles[c.r];
+    c.kvh = (int)(sh.off / n);
+    c.j = (int)(sh.off - (long long)c.kvh * n);
+  }
+  return c;
+}
+
+// The gang whose span holds tile x of `total`.
+__device__ __forceinline__ int tree_gang_of(long long x, long long total, int gangs) {
+  return (int)(((x + 1) * gangs - 1) / total);
+}
+
+}  // namespace flare

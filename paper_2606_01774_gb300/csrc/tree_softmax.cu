@@ -1,0 +1,470 @@
+// Softmax attention of drafted trees over a paged KV prefix: the kernels
+// around the attention itself (tree_sched.cuh has how the work is cut), and
+// the fp32 attention kernel on CUDA cores.
+//
+//   tree_plan_kernel    a CTA per request checks its lengths, page ids and
+//                       tree, and writes its tile count and its nodes' paths
+//   attention           bf16: tree_softmax_tc.cu; fp32: tree_softmax_simt_kernel
+//   tree_finish_kernel  merges items that several gangs share, and writes the
+//                       outputs of unused nodes
+//
+// Online softmax in base 2 with the logit scale folded into q; running
+// maximum, sum and output in fp32.
+#include "common.cuh"
+#include "kernels.h"
+#include "tree.cuh"
+#include "tree_sched.cuh"
+
+namespace flare {
+
+namespace {
+
+constexpr int kPlanThreads = 128;
+constexpr int kRowsS = 32;      // query rows per CTA of the fp32 kernel
+constexpr int kThreadsS = 128;
+constexpr float kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float4 load4(const float* x) {
+  return *reinterpret_cast<const float4*>(x);
+}
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* x) {
+  const uint2 b = *reinterpret_cast<const uint2*>(x);
+  const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b.x));
+  const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b.y));
+  return make_float4(lo.x, lo.y, hi.x, hi.y);
+}
+__device__ __forceinline__ void store4(float* x, float4 v) { *reinterpret_cast<float4*>(x) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+  *reinterpret_cast<uint2*>(x) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo),
+                                            *reinterpret_cast<const uint32_t*>(&hi));
+}
+
+}  // namespace
+
+__global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxParams p) {
+  const int r = blockIdx.x, tid = threadIdx.x;
+  const int n = p.node_len[r], P = p.prefix_len[r];
+  int bad = 0;
+  if (n < 0 || n > p.N) bad |= FLARE_DEV_BAD_TREE;
+  if (P < 0 || P > (long long)p.max_pages * p.page_size) bad |= FLARE_DEV_BAD_PREFIX_LEN;
+  if (!bad && n > 0) {
+    const int pages = (P + p.page_size - 1) / p.page_size;
+    for (int i = tid; i < pages; i += kPlanThreads) {
+      const int pg = p.page_table[(size_t)r * p.max_pages + i];
+      if (pg < 0 || pg >= p.num_pages) bad |= FLARE_DEV_BAD_PAGE;
+    }
+    if (tid < 32) {
+      int p0, p1;
+      if (warp_load_tree(p.parent + (size_t)r * p.N, n, p0, p1)) {
+        uint64_t a0, a1;
+        warp_paths(n, p0, p1, a0, a1);
+        if (tid < p.N) p.anc[(size_t)r * p.N + tid] = a0;
+        if (tid + 32 < p.N) p.anc[(size_t)r * p.N + tid + 32] = a1;
+      } else {
+        bad |= FLARE_DEV_BAD_TREE;
+      }
+    }
+  }
+  const int any = __syncthreads_or(bad);
+  if (bad) flag(p.dev_status, bad);
+  if (tid == 0)
+    p.tiles[r] = any ? -1 : (n == 0 ? 0 : (P + kTreeTile - 1) / kTreeTile + 1);
+}
+
+// fp32 attention.  A CTA takes 32 query rows; thread (y, x) of its 8 x 16 holds
+// rows 4y .. 4y+3 against keys x, x+16, x+32, x+48 of a tile, and columns 4x
+// (+ 64 c) of those rows' outputs.  Bound by the fp32 multiply-adds (4 D per
+// row and key against 8 D bytes per key): a row tile of 32 reuses each staged
+// key 32 times, and the 4 x 4 (4 x 4 D/64) register tiles ask shared memory
+// for one 16-byte read per eight multiply-adds.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftmaxParams p) {
+  constexpr int kS = D + 4;  // row stride of staged rows: 16 lanes on 16 rows spread over the banks
+  constexpr int kC = D / 64;
+  extern __shared__ __align__(16) float sm[];
+  __shared__ TreeSpanShared span;
+  float* Qs = sm;                    // [32][kS]
+  float* Ks = Qs + kRowsS * kS;      // [64][kS]
+  float* Vs = Ks + kTreeTile * kS;   // [64][kS]
+  float* Ps = Vs + kTreeTile * kS;   // [32][64 + 4]
+  constexpr int kPS = kTreeTile + 4;
+
+  const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
+  const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
+  const int m0 = mt * kRowsS;
+  const T* q = static_cast<const T*>(p.q);
+  const T* pools[2] = {static_cast<const T*>(p.k_pool), static_cast<const T*>(p.v_pool)};
+  const T* blks[2] = {static_cast<const T*>(p.k_blk), static_cast<const T*>(p.v_blk)};
+  TreeCursor cur = tree_span<kThreadsS>(p, gang, span);
+  TreePiece w;
+  while (cur.next(p, w)) {
+    const int n = p.node_len[w.r], P = p.prefix_len[w.r];
+    const int M = n * p.G;
+    if (m0 >= M) continue;
+    __syncthreads();  // the previous piece's rows are read
+    for (int e = tid; e < kRowsS * (D / 4); e += kThreadsS) {
+      const int i = e / (D / 4), d = e % (D / 4) * 4, m = m0 + i;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (m < M) {
+        const int t = m / p.G, g = m - t * p.G;
+        v = load4(q + (((size_t)w.r * p.N + t) * p.Hq + w.kvh * p.G + g) * D + d);
+      }
+      *reinterpret_cast<float4*>(Qs + i * kS + d) =
+          make_float4(v.x * p.scale_log2, v.y * p.scale_log2, v.z * p.scale_log2, v.w * p.scale_log2);
+    }
+    uint64_t path[4];  // the keys of the tree tile that each row sees
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = m0 + 4 * y + i;
+      path[i] = m < M ? p.anc[(size_t)w.r * p.N + m / p.G] : 0ull;
+    }
+    float acc[4][4 * kC], mrow[4], lrow[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      mrow[i] = -INFINITY;
+      lrow[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4 * kC; ++c) acc[i][c] = 0.f;
+    }
+    for (int j = w.j0; j < w.j1; ++j) {
+      const bool tree = j == w.n - 1;
+      const int valid = tree ? n : min(kTreeTile, P - j * kTreeTile);
+      __syncthreads();
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        float* dst = kv ? Vs : Ks;
+#pragma unroll 8
+        for (int e = tid; e < kTreeTile * (D / 4); e += kThreadsS) {
+          const int i = e / (D / 4), d = e % (D / 4) * 4;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i < valid) {
+            const T* src;
+            if (tree) {
+              src = blks[kv] + (((size_t)w.r * p.N + i) * p.Hkv + w.kvh) * D;
+            } else {
+              const int tok = j * kTreeTile + i;
+              const int page = p.page_table[(size_t)w.r * p.max_pages + tok / p.page_size];
+              src = pools[kv] +
+                    (((size_t)page * p.Hkv + w.kvh) * p.page_size + tok % p.page_size) * D;
+            }
+            v = load4(src + d);
+          }
+          *reinterpret_cast<float4*>(dst + i * kS + d) = v;
+        }
+      }
+      __syncthreads();
+      float s[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
+#pragma unroll 4
+      for (int d = 0; d < D; d += 4) {
+        float4 a[4], b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(Qs + (4 * y + i) * kS + d);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const float4*>(Ks + (x + 16 * c) * kS + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            s[i][c] = fmaf(a[i].x, b[c].x, s[i][c]);
+            s[i][c] = fmaf(a[i].y, b[c].y, s[i][c]);
+            s[i][c] = fmaf(a[i].z, b[c].z, s[i][c]);
+            s[i][c] = fmaf(a[i].w, b[c].w, s[i][c]);
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int key = x + 16 * c;
+          const bool see = tree ? (path[i] >> key) & 1 : key < valid;
+          if (!see) s[i][c] = -INFINITY;
+          mx = fmaxf(mx, s[i][c]);
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float mnew = fmaxf(mrow[i], mx);
+        const float mref = mnew == -INFINITY ? 0.f : mnew;  // a row that sees nothing yet
+        const float corr = exp2f(mrow[i] - mref);
+        float sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const float e = exp2f(s[i][c] - mref);
+          Ps[(4 * y + i) * kPS + x + 16 * c] = e;
+          sum += e;
+        }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        lrow[i] = lrow[i] * corr + sum;
+        mrow[i] = mnew;
+#pragma unroll
+        for (int c = 0; c < 4 * kC; ++c) acc[i][c] *= corr;
+      }
+      __syncwarp();  // a row's 64 probabilities come from the 16 lanes that read them
+#pragma unroll 1
+      for (int k = 0; k < kTreeTile; k += 4) {
+        float4 pr[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          pr[i] = *reinterpret_cast<const float4*>(Ps + (4 * y + i) * kPS + k);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int c = 0; c < kC; ++c) {
+            const float4 v = *reinterpret_cast<const float4*>(Vs + (k + kk) * kS + 4 * x + 64 * c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float pk = kk == 0 ? pr[i].x : kk == 1 ? pr[i].y : kk == 2 ? pr[i].z : pr[i].w;
+              acc[i][4 * c] = fmaf(pk, v.x, acc[i][4 * c]);
+              acc[i][4 * c + 1] = fmaf(pk, v.y, acc[i][4 * c + 1]);
+              acc[i][4 * c + 2] = fmaf(pk, v.z, acc[i][4 * c + 2]);
+              acc[i][4 * c + 3] = fmaf(pk, v.w, acc[i][4 * c + 3]);
+            }
+          }
+      }
+    }
+    const bool whole = w.whole();
+    const size_t part = ((size_t)blockIdx.x * 2 + w.slot()) * kRowsS;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int m = m0 + 4 * y + i;
+      if (m >= M) continue;
+      const float inv = lrow[i] > 0.f ? 1.f / lrow[i] : 0.f;
+      const float l2 = lrow[i] > 0.f ? mrow[i] + log2f(lrow[i]) : -INFINITY;
+      const int t = m / p.G, g = m - t * p.G;
+      const size_t o = ((size_t)w.r * p.N + t) * p.Hq + w.kvh * p.G + g;
+#pragma unroll
+      for (int c = 0; c < kC; ++c) {
+        const float4 a = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv,
+                                     acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
+        if (whole) store4(static_cast<T*>(p.out) + o * D + 4 * x + 64 * c, a);
+        else store4(p.part_o + (part + 4 * y + i) * D + 4 * x + 64 * c, a);
+      }
+      if (x == 0) {
+        if (!whole) p.part_lse[part + 4 * y + i] = l2;
+        else if (p.lse) p.lse[o] = l2 * kLn2;
+      }
+    }
+  }
+}
+
+// Merges the pieces of items that several gangs share, and writes the unused
+// nodes' rows.  A row's pieces are the last piece of the first gang (slot 1)
+// and the first of each later one (slot 0), in gang order, whatever the
+// timing:  out = sum_s 2^(lse_s - lse) out_s.  WARPS warps share a row: one
+// when there are rows enough to fill the GPU, eight, each with every eighth
+// piece, when a few rows have many pieces.
+template <typename T, int D, int WARPS>
+__global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
+  constexpr int kV = D >= 128 ? D / 128 : 1;  // 16-byte groups per lane
+  constexpr int kLanes = D / (4 * kV);        // lanes that hold columns
+  constexpr int kRowsPerCta = 8 / WARPS;
+  __shared__ float red_o[WARPS > 1 ? 8 : 1][D];
+  __shared__ float red_l[WARPS > 1 ? 8 : 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int sub = warp % WARPS;
+  const long long rows = (long long)p.R * p.N * p.Hq;
+  const long long total = p.first[p.R];
+  const int gangs = tree_gangs(p, total);
+  for (long long o0 = (long long)blockIdx.x * kRowsPerCta; o0 < rows;
+       o0 += (long long)gridDim.x * kRowsPerCta) {
+    const long long o = o0 + warp / WARPS;  // row of out: (r, t, query head)
+    int n = -1, live = 0;
+    int r = 0, t = 0, h = 0;
+    if (o < rows) {
+      h = (int)(o % p.Hq);
+      t = (int)(o / p.Hq % p.N);
+      r = (int)(o / ((long long)p.Hq * p.N));
+      n = p.tiles[r];
+      live = n < 0 ? 0 : p.node_len[r];
+    }
+    int g0 = 0, g1 = 0;
+    const int kvh = h / p.G, m = t * p.G + (h - kvh * p.G);
+    if (n > 0 && t < live) {
+      const long long s0 = p.first[r] + (long long)kvh * n;
+      g0 = tree_gang_of(s0, total, gangs);
+      g1 = tree_gang_of(s0 + n - 1, total, gangs);
+    }
+    const bool dead = n >= 0 && t >= live, merge = g1 > g0;
+    T* out = static_cast<T*>(p.out) + o * D;
+    if (dead && sub == 0) {
+#pragma unroll
+      for (int v = 0; v < kV; ++v)
+        if (lane < kLanes) store4(out + 4 * (lane + 32 * v), make_float4(0.f, 0.f, 0.f, 0.f));
+      if (lane == 0 && p.lse) p.lse[o] = -INFINITY;
+    }
+    if (WARPS == 1 && !merge) continue;
+    const int mt = m / p.tile_rows, row = m - mt * p.tile_rows;
+    auto part = [&](int g) {
+      return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows + row;
+    };
+    // this warp's pieces: running maximum, sum of weights, weighted output
+    float mx = -INFINITY, den = 0.f;
+    float4 acc[kV];
+#pragma unroll
+    for (int v = 0; v < kV; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (merge) {
+      constexpr int kIn = 4;  // pieces in flight
+      for (int g = g0 + sub; g <= g1; g += WARPS * kIn) {
+        float l[kIn];
+        float4 x[kIn][kV];
+#pragma unroll
+        for (int u = 0; u < kIn; ++u) {
+          const int gg = g + u * WARPS;
+          l[u] = gg <= g1 ? p.part_lse[part(gg)] : -INFINITY;
+#pragma unroll
+          for (int v = 0; v < kV; ++v)
+            x[u][v] = gg <= g1 && lane < kLanes
+                          ? *reinterpret_cast<const float4*>(p.part_o + part(gg) * D +
+                                                             4 * (lane + 32 * v))
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kIn; ++u) {
+          if (l[u] == -INFINITY) continue;  // a piece that the row sees nothing of
+          const float mn = fmaxf(mx, l[u]);
+          const float corr = exp2f(mx - mn), e = exp2f(l[u] - mn);
+          den = den * corr + e;
+          mx = mn;
+#pragma unroll
+          for (int v = 0; v < kV; ++v) {
+            acc[v].x = fmaf(e, x[u][v].x, acc[v].x * corr);
+            acc[v].y = fmaf(e, x[u][v].y, acc[v].y * corr);
+            acc[v].z = fmaf(e, x[u][v].z, acc[v].z * corr);
+            acc[v].w = fmaf(e, x[u][v].w, acc[v].w * corr);
+          }
+        }
+      }
+    }
+    if constexpr (WARPS > 1) {
+      __shared__ float red_d[8];
+      __syncthreads();
+      if (lane < kLanes)
+#pragma unroll
+        for (int v = 0; v < kV; ++v)
+          *reinterpret_cast<float4*>(&red_o[warp][4 * (lane + 32 * v)]) = acc[v];
+      if (lane == 0) {
+        red_l[warp] = mx;
+        red_d[warp] = den;
+      }
+      __syncthreads();
+      if (sub != 0 || !merge) continue;
+#pragma unroll
+      for (int u = 1; u < WARPS; ++u) {
+        const float l = red_l[u];
+        if (l == -INFINITY) continue;
+        const float mn = fmaxf(mx, l), corr = exp2f(mx - mn), e = exp2f(l - mn);
+        den = den * corr + e * red_d[u];
+        mx = mn;
+        if (lane < kLanes)
+#pragma unroll
+          for (int v = 0; v < kV; ++v) {
+            const float4 y = *reinterpret_cast<const float4*>(&red_o[u][4 * (lane + 32 * v)]);
+            acc[v].x = fmaf(e, y.x, acc[v].x * corr);
+            acc[v].y = fmaf(e, y.y, acc[v].y * corr);
+            acc[v].z = fmaf(e, y.z, acc[v].z * corr);
+            acc[v].w = fmaf(e, y.w, acc[v].w * corr);
+          }
+      }
+    }
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    if (lane < kLanes)
+#pragma unroll
+      for (int v = 0; v < kV; ++v)
+        store4(out + 4 * (lane + 32 * v),
+               make_float4(acc[v].x * inv, acc[v].y * inv, acc[v].z * inv, acc[v].w * inv));
+    if (lane == 0 && p.lse) p.lse[o] = den > 0.f ? (mx + log2f(den)) * kLn2 : -INFINITY;
+  }
+}
+
+TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,
+                                  int max_pages, bool bf16, int num_sms) {
+  TreeSoftmaxPlan pl;
+  const int G = Hq / Hkv;
+  pl.tile_rows = kRowsS;
+  (void)bf16;
+  const long long rows = (long long)N * G;
+  pl.row_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
+  const int per_sm = D == 256 ? 1 : D == 128 ? 2 : 4;
+  // as many gangs as the GPU holds at once, and no more than there can be tiles
+  long long gangs = (long long)num_sms * per_sm / pl.row_tiles;
+  const long long most =
+      (long long)R * Hkv * (((long long)max_pages * page_size + kTreeTile - 1) / kTreeTile + 1);
+  if (gangs > most) gangs = most;
+  if (gangs < 1) gangs = 1;
+  pl.gangs = (int)gangs;
+  const size_t slots = (size_t)2 * pl.gangs * pl.row_tiles * pl.tile_rows;
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  size_t at = 0;
+  pl.tiles_off = at;
+  at += up((size_t)R * sizeof(int32_t));
+  pl.first_off = at;
+  at += up((size_t)(R + 1) * sizeof(long long));
+  pl.anc_off = at;
+  at += up((size_t)R * N * sizeof(uint64_t));
+  pl.part_o_off = at;
+  at += up(slots * D * sizeof(float));
+  pl.part_lse_off = at;
+  at += up(slots * sizeof(float));
+  pl.workspace_bytes = at;
+  return pl;
+}
+
+namespace {
+
+template <typename T, int D>
+cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  const int smem = (int)sizeof(float) *
+                   ((kRowsS + 2 * kTreeTile) * (D + 4) + kRowsS * (kTreeTile + 4));
+  cudaError_t e = cudaFuncSetAttribute(tree_softmax_simt_kernel<T, D>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  tree_softmax_simt_kernel<T, D>
+      <<<(unsigned)(p.gangs * p.row_tiles), kThreadsS, smem, stream>>>(p);
+  note_launches(1);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t launch_finish(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  const long long rows = (long long)p.R * p.N * p.Hq;
+  constexpr long long kMaxCtas = 152 * 8;
+  if (rows <= kMaxCtas) {
+    tree_finish_kernel<T, D, 8><<<(unsigned)rows, 256, 0, stream>>>(p);
+  } else {
+    const long long ctas = (rows + 7) / 8;
+    tree_finish_kernel<T, D, 1>
+        <<<(unsigned)(ctas < kMaxCtas ? ctas : kMaxCtas), 256, 0, stream>>>(p);
+  }
+  note_launches(1);
+  return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_d(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream) {
+  cudaError_t e = bf16 ? launch_simt_d<__nv_bfloat16, D>(p, stream) : launch_simt_d<float, D>(p, stream);
+  if (e != cudaSuccess) return e;
+  return bf16 ? launch_finish<__nv_bfloat16, D>(p, stream) : launch_finish<float, D>(p, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream) {
+  tree_plan_kernel<<<(unsigned)p.R, kPlanThreads, 0, stream>>>(p);
+  note_launches(1);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  switch (p.D) {
+    case 64: return launch_d<64>(p, bf16, stream);
+    case 128: return launch_d<128>(p, bf16, stream);
+    case 256: return launch_d<256>(p, bf16, stream);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace flare

@@ -40,6 +40,11 @@ FLARE_DEV_BAD_PREFIX_LEN = 0x4
 FLARE_DEV_BAD_ACCEPT_LEN = 0x8
 FLARE_DEV_WAIT_TIMEOUT = 0x10
 FLARE_DEV_BAD_VERIFY_LEN = 0x20
+FLARE_DEV_BAD_TREE = 0x40
+FLARE_DEV_BAD_LOGITS = 0x80
+
+FLARE_VERIFY_GREEDY = 0
+FLARE_VERIFY_SAMPLE = 1
 
 
 class FlareError(RuntimeError):
@@ -72,6 +77,12 @@ class flare_two_stream_desc(ctypes.Structure):
                 ("act_dtype", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
+class flare_tree_verify_desc(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("num_nodes", ctypes.c_int32),
+                ("vocab_size", ctypes.c_int32), ("logits_dtype", ctypes.c_int),
+                ("mode", ctypes.c_int), ("inv_temperature", ctypes.c_float)]
+
+
 class flare_softmax_desc(ctypes.Structure):
     _fields_ = [("num_requests", ctypes.c_int32), ("block_len", ctypes.c_int32),
                 ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
@@ -97,6 +108,7 @@ def load() -> ctypes.CDLL:
     smx = ctypes.POINTER(flare_softmax_desc)
     cnv = ctypes.POINTER(flare_conv_desc)
     tsd = ctypes.POINTER(flare_two_stream_desc)
+    tvd = ctypes.POINTER(flare_tree_verify_desc)
     sigs = {
         "flare_short_conv": [cnv] + [P] * 9,
         "flare_two_stream_fwd": [tsd] + [P] * 13,
@@ -108,6 +120,13 @@ def load() -> ctypes.CDLL:
         "flare_block_softmax_attn": [smx] + [P] * 10 + [S, P, P],
         "flare_block_softmax_attn_noalloc": [smx] + [P] * 11,
         "flare_append_kv": [smx] + [P] * 9,
+        "flare_tree_softmax_workspace_size": [smx, ctypes.POINTER(S)],
+        "flare_tree_softmax_attn": [smx] + [P] * 12 + [S, P, P],
+        "flare_tree_linear_attn": [lin] + [P] * 12,
+        "flare_tree_verify_workspace_size": [tvd, ctypes.POINTER(S)],
+        "flare_tree_verify": [tvd] + [P] * 12 + [S, P, P],
+        "flare_tree_commit_state": [lin] + [P] * 11,
+        "flare_tree_append_kv": [smx, I32] + [P] * 10,
         "flare_debug_gather_prefix": [smx, P, P, P, P, I32, P, P, P, P],
         "flare_debug_wait_timeout": [P, ctypes.c_uint64, P],
         "flare_read_status": [P, P, ctypes.POINTER(I32)],
@@ -239,6 +258,78 @@ def flare_block_softmax_attn_noalloc(desc, q, k_blk, v_blk, k_pool, v_pool, page
         _p(prefix_len), _p(out), _p(lse), _p(dev_status), _stream(stream))
 
 
+def _c(t):
+    """Data pointer of a tensor that must be contiguous."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError("the tree calls take contiguous tensors")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def flare_tree_softmax_workspace_size(desc) -> int:
+    n = ctypes.c_size_t(0)
+    check(load().flare_tree_softmax_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+          "flare_tree_softmax_workspace_size")
+    return int(n.value)
+
+
+def flare_tree_softmax_attn(desc, q, k_blk, v_blk, k_pool, v_pool, page_table, prefix_len, parent,
+                            node_len, out, lse, workspace, workspace_bytes, dev_status,
+                            stream=None) -> int:
+    return load().flare_tree_softmax_attn(
+        ctypes.byref(desc), _c(q), _c(k_blk), _c(v_blk), _c(k_pool), _c(v_pool), _c(page_table),
+        _c(prefix_len), _c(parent), _c(node_len), _c(out), _c(lse), _c(workspace),
+        int(workspace_bytes), _c(dev_status), _stream(stream))
+
+
+def flare_tree_linear_attn(desc, q, k, v, log_decay, beta, state_pool, state_slot, parent,
+                           node_len, out, dev_status, stream=None) -> int:
+    return load().flare_tree_linear_attn(
+        ctypes.byref(desc), _c(q), _c(k), _c(v), _c(log_decay), _c(beta), _c(state_pool),
+        _c(state_slot), _c(parent), _c(node_len), _c(out), _c(dev_status), _stream(stream))
+
+
+def flare_tree_verify_workspace_size(desc) -> int:
+    n = ctypes.c_size_t(0)
+    check(load().flare_tree_verify_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+          "flare_tree_verify_workspace_size")
+    return int(n.value)
+
+
+def flare_tree_verify(desc, logits, draft_probs, token, parent, node_len, uniform, noise, path,
+                      path_len, next_token, node_logp, workspace, workspace_bytes, dev_status,
+                      stream=None) -> int:
+    return load().flare_tree_verify(
+        ctypes.byref(desc), _c(logits), _c(draft_probs), _c(token), _c(parent), _c(node_len),
+        _c(uniform), _c(noise), _c(path), _c(path_len), _c(next_token), _c(node_logp),
+        _c(workspace), int(workspace_bytes), _c(dev_status), _stream(stream))
+
+
+def flare_tree_commit_state(desc, k, v, log_decay, beta, state_pool, src_slot, dst_slot, path,
+                            path_len, dev_status, stream=None) -> int:
+    return load().flare_tree_commit_state(
+        ctypes.byref(desc), _c(k), _c(v), _c(log_decay), _c(beta), _c(state_pool), _c(src_slot),
+        _c(dst_slot), _c(path), _c(path_len), _c(dev_status), _stream(stream))
+
+
+def _pointers(tensors):
+    return (ctypes.c_void_p * len(tensors))(*[_c(t).value for t in tensors])
+
+
+def flare_tree_append_kv(desc, k_blk, v_blk, k_pool, v_pool, page_table, prefix_len, path,
+                         path_len, dev_status, stream=None) -> int:
+    """k_blk, v_blk, k_pool, v_pool: sequences of per-layer device tensors, of one length; their
+    data pointers are passed as host arrays."""
+    n = len(k_pool)
+    if not len(k_blk) == len(v_blk) == len(v_pool) == n:
+        raise ValueError("one k_blk, v_blk, k_pool and v_pool per layer")
+    return load().flare_tree_append_kv(
+        ctypes.byref(desc), n, _pointers(k_blk), _pointers(v_blk), _pointers(k_pool),
+        _pointers(v_pool), _c(page_table), _c(prefix_len), _c(path), _c(path_len), _c(dev_status),
+        _stream(stream))
+
+
 def flare_debug_gather_prefix(desc, k_pool, v_pool, page_table, prefix_len, request, k_out,
                               v_out, dev_status, stream=None) -> int:
     return load().flare_debug_gather_prefix(
@@ -276,6 +367,12 @@ def two_stream_desc(num_seqs, seq_len, chunk_len, block_len, num_qk_heads, num_v
                     head_dim_k, head_dim_v, act_dtype, scale) -> flare_two_stream_desc:
     return flare_two_stream_desc(num_seqs, seq_len, chunk_len, block_len, num_qk_heads,
                                  num_v_heads, head_dim_k, head_dim_v, act_dtype, scale)
+
+
+def tree_verify_desc(num_requests, num_nodes, vocab_size, logits_dtype,
+                     mode=FLARE_VERIFY_SAMPLE, inv_temperature=1.0) -> flare_tree_verify_desc:
+    return flare_tree_verify_desc(num_requests, num_nodes, vocab_size, logits_dtype, mode,
+                                  inv_temperature)
 
 
 def softmax_desc(num_requests, block_len, num_q_heads, num_kv_heads, head_dim, page_size,
