@@ -168,6 +168,7 @@ struct TreeSoftmaxPlan {
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,
                                   int max_pages, bool bf16, int num_sms);
 cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream);
+cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, cudaStream_t stream);
 
 cudaError_t launch_tree_linear(const GdrParams& p, bool bf16, cudaStream_t stream);
 cudaError_t launch_tree_commit(const GdrParams& p, bool bf16, cudaStream_t stream);

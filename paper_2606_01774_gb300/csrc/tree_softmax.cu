@@ -24,15 +24,6 @@ constexpr int kRowsS = 32;      // query rows per CTA of the fp32 kernel
 constexpr int kThreadsS = 128;
 constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ float4 load4(const float* x) {
-  return *reinterpret_cast<const float4*>(x);
-}
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* x) {
-  const uint2 b = *reinterpret_cast<const uint2*>(x);
-  const float2 lo = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b.x));
-  const float2 hi = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&b.y));
-  return make_float4(lo.x, lo.y, hi.x, hi.y);
-}
 __device__ __forceinline__ void store4(float* x, float4 v) { *reinterpret_cast<float4*>(x) = v; }
 __device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
   const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
@@ -78,7 +69,7 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
 // row and key against 8 D bytes per key): a row tile of 32 reuses each staged
 // key 32 times, and the 4 x 4 (4 x 4 D/64) register tiles ask shared memory
 // for one 16-byte read per eight multiply-adds.
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftmaxParams p) {
   constexpr int kS = D + 4;  // row stride of staged rows: 16 lanes on 16 rows spread over the banks
   constexpr int kC = D / 64;
@@ -93,9 +84,9 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
   const int m0 = mt * kRowsS;
-  const T* q = static_cast<const T*>(p.q);
-  const T* pools[2] = {static_cast<const T*>(p.k_pool), static_cast<const T*>(p.v_pool)};
-  const T* blks[2] = {static_cast<const T*>(p.k_blk), static_cast<const T*>(p.v_blk)};
+  const float* q = static_cast<const float*>(p.q);
+  const float* pools[2] = {static_cast<const float*>(p.k_pool), static_cast<const float*>(p.v_pool)};
+  const float* blks[2] = {static_cast<const float*>(p.k_blk), static_cast<const float*>(p.v_blk)};
   TreeCursor cur = tree_span<kThreadsS>(p, gang, span);
   TreePiece w;
   while (cur.next(p, w)) {
@@ -108,7 +99,8 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (m < M) {
         const int t = m / p.G, g = m - t * p.G;
-        v = load4(q + (((size_t)w.r * p.N + t) * p.Hq + w.kvh * p.G + g) * D + d);
+        v = *reinterpret_cast<const float4*>(
+            q + (((size_t)w.r * p.N + t) * p.Hq + w.kvh * p.G + g) * D + d);
       }
       *reinterpret_cast<float4*>(Qs + i * kS + d) =
           make_float4(v.x * p.scale_log2, v.y * p.scale_log2, v.z * p.scale_log2, v.w * p.scale_log2);
@@ -139,7 +131,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
           const int i = e / (D / 4), d = e % (D / 4) * 4;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
           if (i < valid) {
-            const T* src;
+            const float* src;
             if (tree) {
               src = blks[kv] + (((size_t)w.r * p.N + i) * p.Hkv + w.kvh) * D;
             } else {
@@ -148,7 +140,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
               src = pools[kv] +
                     (((size_t)page * p.Hkv + w.kvh) * p.page_size + tok % p.page_size) * D;
             }
-            v = load4(src + d);
+            v = *reinterpret_cast<const float4*>(src + d);
           }
           *reinterpret_cast<float4*>(dst + i * kS + d) = v;
         }
@@ -242,8 +234,8 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
       for (int c = 0; c < kC; ++c) {
         const float4 a = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv,
                                      acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
-        if (whole) store4(static_cast<T*>(p.out) + o * D + 4 * x + 64 * c, a);
-        else store4(p.part_o + (part + 4 * y + i) * D + 4 * x + 64 * c, a);
+        float* dst = whole ? static_cast<float*>(p.out) + o * D : p.part_o + (part + 4 * y + i) * D;
+        store4(dst + 4 * x + 64 * c, a);
       }
       if (x == 0) {
         if (!whole) p.part_lse[part + 4 * y + i] = l2;
@@ -386,11 +378,10 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
                                   int max_pages, bool bf16, int num_sms) {
   TreeSoftmaxPlan pl;
   const int G = Hq / Hkv;
-  pl.tile_rows = kRowsS;
-  (void)bf16;
+  pl.tile_rows = bf16 ? 128 : kRowsS;
   const long long rows = (long long)N * G;
   pl.row_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
-  const int per_sm = D == 256 ? 1 : D == 128 ? 2 : 4;
+  const int per_sm = bf16 || D == 256 ? 1 : D == 128 ? 2 : 4;
   // as many gangs as the GPU holds at once, and no more than there can be tiles
   long long gangs = (long long)num_sms * per_sm / pl.row_tiles;
   const long long most =
@@ -417,14 +408,14 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
 
 namespace {
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
   const int smem = (int)sizeof(float) *
                    ((kRowsS + 2 * kTreeTile) * (D + 4) + kRowsS * (kTreeTile + 4));
-  cudaError_t e = cudaFuncSetAttribute(tree_softmax_simt_kernel<T, D>,
+  cudaError_t e = cudaFuncSetAttribute(tree_softmax_simt_kernel<D>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  tree_softmax_simt_kernel<T, D>
+  tree_softmax_simt_kernel<D>
       <<<(unsigned)(p.gangs * p.row_tiles), kThreadsS, smem, stream>>>(p);
   note_launches(1);
   return cudaGetLastError();
@@ -447,7 +438,7 @@ cudaError_t launch_finish(const TreeSoftmaxParams& p, cudaStream_t stream) {
 
 template <int D>
 cudaError_t launch_d(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream) {
-  cudaError_t e = bf16 ? launch_simt_d<__nv_bfloat16, D>(p, stream) : launch_simt_d<float, D>(p, stream);
+  cudaError_t e = bf16 ? launch_tree_softmax_tc(p, stream) : launch_simt_d<D>(p, stream);
   if (e != cudaSuccess) return e;
   return bf16 ? launch_finish<__nv_bfloat16, D>(p, stream) : launch_finish<float, D>(p, stream);
 }

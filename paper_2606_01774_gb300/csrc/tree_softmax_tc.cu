@@ -1,0 +1,599 @@
+// Softmax attention of drafted trees over a paged KV prefix on the
+// 5th-generation tensor cores (tcgen05), bf16 in, fp32 accumulate.
+//
+// tree_sched.cuh has how the work is cut: a CTA walks its gang's span of key
+// tiles for its own 128 query rows (row m = node * G + g of a (request, kv
+// head) item: the G query heads of a kv head share its keys).  A piece is a
+// stretch of one item's tiles: prefix tiles through the page table, 64 tokens
+// each, and the item's last tile, the tree's own keys, masked by the rows' path
+// bits.  A piece that covers its item stores the output; another stores a
+// partial one, which tree_finish_kernel merges.
+//
+// Serving trees are bound by the keys' and values' bytes: a tile of 64 keys is
+// 256 D bytes for 4 x 128 x 64 D operations, which the tensor cores finish in a
+// third of the time that its share of DRAM bandwidth gives it, padded rows and
+// all.  So the kernel is built as a stream: rings of TMA boxes fill shared
+// memory (a tile takes about a microsecond from issue to arrival), queries,
+// scores, probabilities and output live in tensor memory, and a persistent
+// CTA keeps the rings full across pieces.
+//
+// Warp roles (256 threads):
+//   warp 0     K producer, warp 6 V producer: a TMA box per (page, 64-column
+//              chunk), a lane each, page ids read one tile ahead
+//   warp 7     zeroes V rows that no query may see (past the prefix end, unused
+//              nodes), so that what they hold never meets a zero probability;
+//              follows every V tile, so a slot is free once this warp and the
+//              product have both left it
+//   warp 1     tensor-memory owner; one thread issues S_j = Q K_j^T and
+//              O += P_j V_j; both read their A operand from tensor memory
+//   warps 2-5  softmax, a TMEM lane quarter each: a thread per query row;
+//              online base-2 softmax with a lazily moved maximum (O is rescaled
+//              when it grows by more than 2^8); quarters without a used row skip
+//              the arithmetic
+// Every wait is bounded; a timeout sets FLARE_DEV_WAIT_TIMEOUT, the CTA stops
+// issuing work, writes nothing more, waits for its copies in flight, frees its
+// tensor memory and exits.
+#include <cudaTypedefs.h>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "tc.cuh"
+#include "tree.cuh"
+#include "tree_sched.cuh"
+
+namespace flare {
+
+namespace {
+
+constexpr int kRowsT = 128;            // query rows per CTA (TMEM lanes)
+constexpr int kSmThreads = 128;        // warps 2-5
+constexpr int kVWarpT = 6, kFixWarpT = 7;
+constexpr int kThreadsT = 256;
+constexpr float kMoveMax = 8.0f;       // log2 units
+
+struct TreeMaps {
+  CUtensorMap kblk, vblk;    // (D, Hkv, N, R)           box (64, 1, 64, 1)
+  CUtensorMap kpool, vpool;  // (D, p, Hkv, num_pages)   box (64, min(p, 64), 1, 1)
+};
+
+template <int D>
+struct TreeCfg {
+  static constexpr int kChunks = D / 64;
+  static constexpr int kTileBytes = kChunks * kTreeTile * 128;  // one K (or V) tile
+  static constexpr int kKStages = D == 256 ? 3 : (D == 128 ? 6 : 8);
+  static constexpr int kVStages = D == 256 ? 4 : (D == 128 ? 7 : 8);
+  static constexpr int kSmem = (kKStages + kVStages) * kTileBytes + 1024;
+  // tensor memory columns: O [0, D), Q as bf16 pairs, the S / P buffers
+  static constexpr int kQCol = D;
+  static constexpr int kSCol = D + D / 2;
+  static constexpr int kSBuf = kSCol + 3 * kTreeTile <= 512 ? 3 : 2;
+  static constexpr int kTmemCols = kSCol + kSBuf * kTreeTile > 256 ? 512 : 256;
+};
+
+struct TreeShared {
+  uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], v_fix[8];
+  uint64_t s_full[3], p_full[3], pv_done[3];
+  uint64_t q_ready, o_final, o_free;
+  uint64_t drain;  // after a timeout: every MMA issued has completed
+  uint32_t tmem_base;
+  int abort_flag;
+  TreeSpanShared span;
+};
+
+__device__ __forceinline__ bool warp_wait_t(uint64_t* bar, uint32_t parity, const int* abort) {
+  return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort));
+}
+
+__device__ __forceinline__ bool aborted_t(const TreeShared& sh) {
+  return *reinterpret_cast<const volatile int*>(&sh.abort_flag) != 0;
+}
+
+__device__ __forceinline__ void give_up(TreeShared& sh, int32_t* status) {
+  if (!sh.abort_flag) {
+    sh.abort_flag = 1;
+    flag(status, FLARE_DEV_WAIT_TIMEOUT);
+  }
+}
+
+// A piece with what the roles ask of its request.
+struct TreeItem {
+  TreePiece w;
+  int P, nodes, tiles;
+  // tile j of the piece: whether it holds the tree's keys, and how many of its
+  // rows are keys at all
+  __device__ __forceinline__ bool is_tree(int j) const { return w.j0 + j == w.n - 1; }
+  __device__ __forceinline__ int valid(int j) const {
+    return is_tree(j) ? nodes : min(kTreeTile, P - (w.j0 + j) * kTreeTile);
+  }
+};
+
+// The next piece of the span that has rows of this row tile.
+__device__ __forceinline__ bool next_item(const TreeSoftmaxParams& p, TreeCursor& cur, int m0,
+                                          TreeItem& it) {
+  while (cur.next(p, it.w)) {
+    it.nodes = p.node_len[it.w.r];
+    if (m0 >= it.nodes * p.G) continue;
+    it.P = p.prefix_len[it.w.r];
+    it.tiles = it.w.j1 - it.w.j0;
+    return true;
+  }
+  return false;
+}
+
+}  // namespace
+
+template <int D>
+__global__ void __launch_bounds__(kThreadsT, 1)
+    tree_softmax_tc_kernel(const __grid_constant__ TreeMaps maps, TreeSoftmaxParams p) {
+  using C = TreeCfg<D>;
+  constexpr int kSB = C::kSBuf;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ TreeShared sh;
+  uint8_t* Ks = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* Vs = Ks + C::kKStages * C::kTileBytes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
+  const int m0 = mt * kRowsT;
+
+  if (tid == 0) {
+    sh.abort_flag = 0;
+    for (int s = 0; s < C::kKStages; ++s) {
+      tc::mbar_init(&sh.k_full[s], 1);
+      tc::mbar_init(&sh.k_empty[s], 1);
+    }
+    for (int s = 0; s < C::kVStages; ++s) {
+      tc::mbar_init(&sh.v_full[s], 1);
+      tc::mbar_init(&sh.v_empty[s], 2);  // the product and the zeroing warp
+      tc::mbar_init(&sh.v_fix[s], 1);
+    }
+    for (int b = 0; b < 3; ++b) {
+      tc::mbar_init(&sh.s_full[b], 1);
+      tc::mbar_init(&sh.p_full[b], kSmThreads);
+      tc::mbar_init(&sh.pv_done[b], 1);
+    }
+    tc::mbar_init(&sh.q_ready, kSmThreads);
+    tc::mbar_init(&sh.o_final, 1);
+    tc::mbar_init(&sh.o_free, kSmThreads);
+    tc::mbar_init(&sh.drain, 1);
+    tc::fence_mbar_init();
+  }
+  if (warp == 1) tc::tmem_alloc(&sh.tmem_base, C::kTmemCols);
+  const TreeCursor span = tree_span<kThreadsT>(p, gang, sh.span);
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = sh.tmem_base;
+  const uint32_t tmem_o = tmem, tmem_q = tmem + C::kQCol, tmem_s = tmem + C::kSCol;
+  TreeCursor cur = span;
+  TreeItem it;
+
+  if (warp == 0 || warp == kVWarpT) {
+    // ------------------------------------------------------------ producers
+    const int kv = warp == 0 ? 0 : 1;
+    const CUtensorMap* pool_map = kv ? &maps.vpool : &maps.kpool;
+    const CUtensorMap* blk_map = kv ? &maps.vblk : &maps.kblk;
+    if (lane == 0) {
+      tc::prefetch_tmap(pool_map);
+      tc::prefetch_tmap(blk_map);
+    }
+    const int box_rows = p.page_size < kTreeTile ? p.page_size : kTreeTile;
+    const int boxes = kTreeTile / box_rows;  // of a full tile
+    const int ns = kv ? C::kVStages : C::kKStages;
+    uint64_t* fulls = kv ? sh.v_full : sh.k_full;
+    uint64_t* empties = kv ? sh.v_empty : sh.k_empty;
+    uint8_t* ring = kv ? Vs : Ks;
+    const int bx = lane / C::kChunks, ch = lane % C::kChunks;  // this lane's box of a tile
+    bool ok = true;
+    int g = 0;  // running tile count
+    while (ok && next_item(p, cur, m0, it)) {
+      const int32_t* table = p.page_table + (size_t)it.w.r * p.max_pages;
+      // the page of this lane's box in tile j (0 where the tile has no such box)
+      auto page_of = [&](int j) -> int {
+        const int tok = (it.w.j0 + j) * kTreeTile + bx * box_rows;
+        return j < it.tiles && bx < boxes && !it.is_tree(j) && tok < it.P ? table[tok / p.page_size]
+                                                                         : 0;
+      };
+      int page = page_of(0);
+      for (int j = 0; j < it.tiles; ++j, ++g) {
+        const int page_next = page_of(j + 1);
+        const int st = g % ns;
+        const uint32_t ph = (uint32_t)(g / ns) & 1u;
+        uint8_t* dst = ring + st * C::kTileBytes;
+        if (!warp_wait_t(&empties[st], ph ^ 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        if (it.is_tree(j)) {
+          if (lane == 0) {
+            tc::mbar_expect_tx(&fulls[st], C::kTileBytes);
+#pragma unroll
+            for (int c = 0; c < C::kChunks; ++c)
+              tc::tma_load_4d(dst + c * (kTreeTile * 128), blk_map, &fulls[st], c * 64, it.w.kvh,
+                              0, it.w.r);
+          }
+        } else {
+          const int tok0 = (it.w.j0 + j) * kTreeTile;
+          const int nbox = (min(kTreeTile, it.P - tok0) + box_rows - 1) / box_rows;
+          if (lane == 0)
+            tc::mbar_expect_tx(&fulls[st], (uint32_t)(C::kChunks * nbox * box_rows * 128));
+          __syncwarp();
+          if (bx < nbox)
+            tc::tma_load_4d(dst + ch * (kTreeTile * 128) + bx * box_rows * 128, pool_map,
+                            &fulls[st], ch * 64, (tok0 + bx * box_rows) % p.page_size, it.w.kvh,
+                            page);
+        }
+        page = page_next;
+      }
+    }
+    if (!ok && lane == 0) give_up(sh, p.dev_status);
+    // on the way out every copy issued has landed (a consumer that gave up may
+    // have left some in flight)
+    if (aborted_t(sh)) {
+      for (int s = 0; s < ns && s < g; ++s) {
+        const int last = g - 1 - ((g - 1 - s) % ns + ns) % ns;  // last tile issued into slot s
+        if (last >= 0) tc::mbar_wait(&fulls[s], (uint32_t)(last / ns) & 1u, nullptr, 100000000ull);
+      }
+    }
+  } else if (warp == kFixWarpT) {
+    // ------------------------------------------------------------ V rows nobody may see
+    bool ok = true;
+    int g = 0;
+    while (ok && next_item(p, cur, m0, it)) {
+      for (int j = 0; j < it.tiles; ++j, ++g) {
+        const int st = g % C::kVStages;
+        if (!warp_wait_t(&sh.v_full[st], (uint32_t)(g / C::kVStages) & 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        const int valid = it.valid(j);
+        if (valid < kTreeTile) {
+          uint8_t* dst = Vs + st * C::kTileBytes;
+          const int n16 = (kTreeTile - valid) * 8;  // 16-byte pieces per chunk
+          for (int c = 0; c < C::kChunks; ++c)
+            for (int e = lane; e < n16; e += 32)
+              *reinterpret_cast<uint4*>(dst + c * (kTreeTile * 128) + (valid + e / 8) * 128 +
+                                        (e % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          tc::fence_async_smem();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&sh.v_fix[st]);
+        }
+        if (lane == 0) tc::mbar_arrive(&sh.v_empty[st]);
+      }
+    }
+    if (!ok && lane == 0) give_up(sh, p.dev_status);
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ MMA issuer
+    if (lane == 0) {
+      const uint32_t id_s = tc::idesc_bf16(kRowsT, kTreeTile, false, false);
+      const uint32_t id_o = tc::idesc_bf16(kRowsT, D, false, true);
+      const uint64_t kdesc0 = tc::sdesc_sw128(tc::smem_u32(Ks), 16, 1024);
+      const uint64_t vdesc0 = tc::sdesc_sw128(tc::smem_u32(Vs), kTreeTile * 128, 1024);
+      bool ok = true;
+      int g = 0;              // running tile count
+      uint32_t fix_par = 0u;  // per V slot: parity of its next zeroed tile
+      for (int k = 0; ok && next_item(p, cur, m0, it); ++k) {
+        if (!tc::mbar_wait(&sh.q_ready, (uint32_t)k & 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        // S_j = Q K_j^T into S buffer (g + j) % kSB
+        auto issue_s = [&](int j) -> bool {
+          const int gg = g + j, st = gg % C::kKStages, sb = gg % kSB;
+          if (!tc::mbar_wait(&sh.k_full[st], (uint32_t)(gg / C::kKStages) & 1u, &sh.abort_flag))
+            return false;
+          tc::fence_after_sync();
+          const uint64_t kd = kdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            tc::mma_bf16_ts(tmem_s + sb * kTreeTile, tmem_q + kk * 8,
+                            kd + (uint64_t)(((kk >> 2) * (kTreeTile * 128) + (kk & 3) * 32) >> 4),
+                            id_s, kk > 0 ? 1u : 0u);
+          tc::mma_commit(&sh.s_full[sb]);
+          tc::mma_commit(&sh.k_empty[st]);
+          return true;
+        };
+        auto issue_pv = [&](int j) -> bool {
+          const int gg = g + j, st = gg % C::kVStages, pb = gg % kSB;
+          if (!tc::mbar_wait(&sh.p_full[pb], (uint32_t)(gg / kSB) & 1u, &sh.abort_flag))
+            return false;
+          // the first product of a piece overwrites O: the previous one's must be out
+          if (j == 0 && k > 0 &&
+              !tc::mbar_wait(&sh.o_free, (uint32_t)(k - 1) & 1u, &sh.abort_flag))
+            return false;
+          if (!tc::mbar_wait(&sh.v_full[st], (uint32_t)(gg / C::kVStages) & 1u, &sh.abort_flag))
+            return false;
+          if (it.valid(j) < kTreeTile) {
+            if (!tc::mbar_wait(&sh.v_fix[st], (fix_par >> st) & 1u, &sh.abort_flag)) return false;
+            fix_par ^= 1u << st;
+          }
+          tc::fence_after_sync();
+          const uint64_t vd = vdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kTreeTile / 16; ++kk)
+            tc::mma_bf16_ts(tmem_o, tmem_s + pb * kTreeTile + kk * 8,
+                            vd + (uint64_t)(kk * (2048 >> 4)), id_o, (j > 0 || kk > 0) ? 1u : 0u);
+          tc::mma_commit(&sh.pv_done[pb]);
+          tc::mma_commit(&sh.v_empty[st]);
+          return true;
+        };
+        // MMAs of one thread execute in issue order, so an S buffer can be
+        // rewritten once the product that reads its probabilities was issued.
+        // Three buffers: S0 S1 S2 PV0 S3 PV1 ...; two: S0 S1 PV0 S2 PV1 ...
+        const int n = it.tiles;
+        for (int j = 0; j < 2 && j < n && ok; ++j) ok = issue_s(j);
+        for (int j = 0; j < n && ok; ++j) {
+          if (kSB == 3) {
+            if (j + 2 < n) ok = issue_s(j + 2);
+            if (ok) ok = issue_pv(j);
+          } else {
+            ok = issue_pv(j);
+            if (ok && j + 2 < n) ok = issue_s(j + 2);
+          }
+        }
+        if (ok) tc::mma_commit(&sh.o_final);
+        g += n;
+      }
+      if (!ok) give_up(sh, p.dev_status);
+      if (aborted_t(sh)) {
+        tc::mma_commit(&sh.drain);
+        tc::mbar_wait(&sh.drain, 0u, nullptr, 100000000ull);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ softmax warps
+    const int quarter = warp & 3;
+    const int row = quarter * 32 + lane, m = m0 + row;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const int node = m / p.G, head = m - node * p.G;
+
+    // Q row into tensor memory as bf16 pairs; rows past the tree's are zero
+    auto load_q = [&](const TreeItem& w) {
+      const bool live = m < w.nodes * p.G;
+      if (__any_sync(0xffffffffu, live)) {
+        const uint4* qrow = reinterpret_cast<const uint4*>(
+            static_cast<const __nv_bfloat16*>(p.q) +
+            (((size_t)w.w.r * p.N + (live ? node : 0)) * p.Hq + w.w.kvh * p.G + head) * D);
+        constexpr int kWords = D / 2;                      // TMEM columns of a row
+        constexpr int kBatch = kWords < 64 ? kWords : 64;  // columns per batch of loads
+#pragma unroll 1
+        for (int c0 = 0; c0 < kWords; c0 += kBatch) {
+          uint32_t q[kBatch];
+#pragma unroll
+          for (int q4 = 0; q4 < kBatch / 4; ++q4) {
+            const uint4 v = live ? qrow[(c0 / 4) + q4] : make_uint4(0u, 0u, 0u, 0u);
+            q[4 * q4] = v.x;
+            q[4 * q4 + 1] = v.y;
+            q[4 * q4 + 2] = v.z;
+            q[4 * q4 + 3] = v.w;
+          }
+#pragma unroll
+          for (int c = 0; c < kBatch; c += 16)
+            tc::tmem_st16(tmem_q + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&q[c]));
+        }
+        tc::tmem_st_wait();
+      }
+      tc::fence_before_sync();
+      tc::mbar_arrive(&sh.q_ready);
+    };
+
+    bool ok = true;
+    int g = 0;  // running tile count
+    bool have = next_item(p, cur, m0, it);
+    if (have) load_q(it);
+    for (int k = 0; have; ++k) {
+      const bool live = m < it.nodes * p.G;
+      const bool warp_live = __any_sync(0xffffffffu, live);
+      const uint64_t path = live ? p.anc[(size_t)it.w.r * p.N + node] : 0ull;
+      float m_run = -INFINITY, l_run = 0.f;
+      for (int j = 0; j < it.tiles; ++j) {
+        const int gg = g + j, sb = gg % kSB;
+        if (!warp_wait_t(&sh.s_full[sb], (uint32_t)(gg / kSB) & 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        if (!warp_live) {  // nobody reads these rows' output
+          tc::mbar_arrive(&sh.p_full[sb]);
+          continue;
+        }
+        tc::fence_after_sync();
+        const uint32_t sbuf = tmem_s + lane_off + sb * kTreeTile;
+        uint32_t sr[kTreeTile];
+#pragma unroll
+        for (int c = 0; c < kTreeTile; c += 16)
+          tc::tmem_ld16(sbuf + c, *reinterpret_cast<uint32_t(*)[16]>(&sr[c]));
+        tc::tmem_ld_wait();
+        const int valid = it.valid(j);
+        if (it.is_tree(j)) {
+#pragma unroll
+          for (int c = 0; c < kTreeTile; ++c)
+            if (!((path >> c) & 1)) sr[c] = 0xff800000u;  // -inf
+        } else if (valid < kTreeTile) {
+#pragma unroll
+          for (int c = 0; c < kTreeTile; ++c)
+            if (c >= valid) sr[c] = 0xff800000u;
+        }
+        // tile maximum of the raw scores (scale >= 0 keeps the order)
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < kTreeTile; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(sr[c]));
+        const float mt_ = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        const float m_new = fmaxf(m_run, mt_ * p.scale_log2);
+        const bool need = j == 0 || m_new > m_run + kMoveMax;
+        const bool move = __any_sync(0xffffffffu, need);
+        const float m_use = move ? m_new : m_run;
+        const float corr = j == 0 ? 0.f : tc::ex2(m_run - m_use);
+        // a row that sees nothing of its tiles so far: every probability 0
+        const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
+        float sum0 = 0.f, sum1 = 0.f;
+        uint32_t pk[kTreeTile / 2];
+#pragma unroll
+        for (int c = 0; c < kTreeTile; c += 2) {
+          const float p0 = tc::ex2(fmaf(__uint_as_float(sr[c]), p.scale_log2, neg_m));
+          const float p1 = tc::ex2(fmaf(__uint_as_float(sr[c + 1]), p.scale_log2, neg_m));
+          sum0 += p0;
+          sum1 += p1;
+          const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
+          pk[c / 2] = *reinterpret_cast<const uint32_t*>(&h2);
+        }
+        l_run = j == 0 ? sum0 + sum1 : l_run * corr + (sum0 + sum1);
+        if (move && j >= 1) {  // rescale O, the previous tile's product done
+          const int pb = (gg - 1) % kSB;
+          if (!warp_wait_t(&sh.pv_done[pb], (uint32_t)((gg - 1) / kSB) & 1u, &sh.abort_flag)) {
+            ok = false;
+            break;
+          }
+          tc::fence_after_sync();
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tc::tmem_ld16(tmem_o + lane_off + c, o);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+            tc::tmem_st16(tmem_o + lane_off + c, o);
+          }
+        }
+        m_run = m_use;
+#pragma unroll
+        for (int c = 0; c < kTreeTile / 2; c += 16)
+          tc::tmem_st16(sbuf + c, *reinterpret_cast<uint32_t(*)[16]>(&pk[c]));
+        tc::tmem_st_wait();
+        tc::fence_before_sync();
+        tc::mbar_arrive(&sh.p_full[sb]);
+      }
+      g += it.tiles;
+      if (ok && aborted_t(sh)) ok = false;
+      // the next piece's queries: every S product of this one has completed
+      TreeItem nx = it;
+      const bool more = ok && next_item(p, cur, m0, nx);
+      if (more) load_q(nx);
+      if (ok && !warp_wait_t(&sh.o_final, (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
+      if (!ok) break;
+      if (warp_live) {
+        tc::fence_after_sync();
+        const bool whole = it.w.whole();
+        const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+        const float l2 = l_run > 0.f ? m_run + log2f(l_run) : -INFINITY;
+        const size_t orow = ((size_t)it.w.r * p.N + node) * p.Hq + it.w.kvh * p.G + head;
+        const size_t prow = ((size_t)blockIdx.x * 2 + it.w.slot()) * kRowsT + row;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 16) {
+          uint32_t o[16];
+          tc::tmem_ld16(tmem_o + lane_off + c, o);
+          tc::tmem_ld_wait();
+          if (!live) continue;
+          if (whole) {
+            uint32_t h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(o[2 * i]) * inv,
+                                                              __uint_as_float(o[2 * i + 1]) * inv);
+              h[i] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * D + c);
+            dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
+            dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
+          } else {
+            float4* dst = reinterpret_cast<float4*>(p.part_o + prow * D + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              dst[i] = make_float4(
+                  __uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
+                  __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
+          }
+        }
+        if (live) {
+          if (!whole) p.part_lse[prow] = l2;
+          else if (p.lse) p.lse[orow] = l2 * 0.6931471805599453f;
+        }
+      }
+      tc::fence_before_sync();
+      tc::mbar_arrive(&sh.o_free);
+      have = more;
+      it = nx;
+    }
+    if (!ok) give_up(sh, p.dev_status);
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem, C::kTmemCols);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+namespace {
+
+PFN_cuTensorMapEncodeTiled_v12000 tree_encode_fn() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  }();
+  return fn;
+}
+
+bool encode(CUtensorMap* m, const void* ptr, const cuuint64_t (&dims)[4],
+            const cuuint64_t (&strides)[3], cuuint32_t rows, int rows_dim) {
+  auto fn = tree_encode_fn();
+  if (!fn) return false;
+  cuuint32_t box[4] = {64, 1, 1, 1};
+  box[rows_dim] = rows;
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+         CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch_tc_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  using C = TreeCfg<D>;
+  TreeMaps maps;
+  const cuuint64_t row = D * 2;
+  {
+    const cuuint64_t dims[4] = {D, (cuuint64_t)p.Hkv, (cuuint64_t)p.N, (cuuint64_t)p.R};
+    const cuuint64_t str[3] = {row, p.Hkv * row, (cuuint64_t)p.N * p.Hkv * row};
+    if (!encode(&maps.kblk, p.k_blk, dims, str, kTreeTile, 2) ||
+        !encode(&maps.vblk, p.v_blk, dims, str, kTreeTile, 2))
+      return cudaErrorInvalidValue;
+  }
+  {
+    // an empty pool is never read; its maps point at the nodes' tensors
+    const bool none = p.num_pages == 0 || p.max_pages == 0;
+    const cuuint64_t dims[4] = {D, (cuuint64_t)p.page_size, (cuuint64_t)p.Hkv,
+                                (cuuint64_t)(none ? 1 : p.num_pages)};
+    const cuuint64_t str[3] = {row, p.page_size * row, (cuuint64_t)p.Hkv * p.page_size * row};
+    const cuuint32_t rows = p.page_size < kTreeTile ? p.page_size : kTreeTile;
+    if (!encode(&maps.kpool, none ? p.k_blk : p.k_pool, dims, str, rows, 1) ||
+        !encode(&maps.vpool, none ? p.v_blk : p.v_pool, dims, str, rows, 1))
+      return cudaErrorInvalidValue;
+  }
+  cudaError_t e = cudaFuncSetAttribute(tree_softmax_tc_kernel<D>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+  if (e != cudaSuccess) return e;
+  tree_softmax_tc_kernel<D>
+      <<<(unsigned)(p.gangs * p.row_tiles), kThreadsT, C::kSmem, stream>>>(maps, p);
+  note_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  switch (p.D) {
+    case 64: return launch_tc_d<64>(p, stream);
+    case 128: return launch_tc_d<128>(p, stream);
+    case 256: return launch_tc_d<256>(p, stream);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace flare
