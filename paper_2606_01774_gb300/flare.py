@@ -155,11 +155,21 @@ def _p(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
+def _current_stream():
+    """Handle of the current device's current stream."""
+    global _current_stream
+    from torch import _C
+
+    # the raw handle: building a torch.cuda.Stream object costs 3 us a call
+    def _current_stream(device=_C._cuda_getDevice, raw=_C._cuda_getCurrentRawStream):
+        return raw(device())
+
+    return _current_stream()
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-
-        stream = torch.cuda.current_stream()
+        return _current_stream()
     return ctypes.c_void_p(getattr(stream, "cuda_stream", stream))
 
 
@@ -264,7 +274,7 @@ def _c(t):
         return None
     if not t.is_contiguous():
         raise ValueError("the tree calls take contiguous tensors")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def flare_tree_softmax_workspace_size(desc) -> int:
@@ -314,7 +324,7 @@ def flare_tree_commit_state(desc, k, v, log_decay, beta, state_pool, src_slot, d
 
 
 def _pointers(tensors):
-    return (ctypes.c_void_p * len(tensors))(*[_c(t).value for t in tensors])
+    return (ctypes.c_void_p * len(tensors))(*[_c(t) for t in tensors])
 
 
 def flare_tree_append_kv(desc, k_blk, v_blk, k_pool, v_pool, page_table, prefix_len, path,
