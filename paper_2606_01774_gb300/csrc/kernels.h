@@ -171,6 +171,8 @@ cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStrea
 cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, cudaStream_t stream);
 
 cudaError_t launch_tree_linear(const GdrParams& p, bool bf16, cudaStream_t stream);
+bool tree_linear_tc_supported(int dk, int dv);
+cudaError_t launch_tree_linear_tc(const GdrParams& p, cudaStream_t stream);
 cudaError_t launch_tree_commit(const GdrParams& p, bool bf16, cudaStream_t stream);
 
 struct TreeVerifyParams {

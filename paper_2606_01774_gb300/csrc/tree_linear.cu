@@ -178,7 +178,8 @@ cudaError_t launch_t(const GdrParams& p, cudaStream_t stream) {
 
 template <typename T>
 cudaError_t launch_d(const GdrParams& p, cudaStream_t stream) {
-  if (p.dk == 128 && p.dv == 128) return launch_t<T, 128, 128>(p, stream);
+  if constexpr (sizeof(T) == 4)  // in bf16 that state takes the tensor cores
+    if (p.dk == 128 && p.dv == 128) return launch_t<T, 128, 128>(p, stream);
   if (p.dk == 128 && p.dv == 64) return launch_t<T, 128, 64>(p, stream);
   if (p.dk == 64 && p.dv == 128) return launch_t<T, 64, 128>(p, stream);
   if (p.dk == 64 && p.dv == 64) return launch_t<T, 64, 64>(p, stream);
@@ -189,6 +190,7 @@ cudaError_t launch_d(const GdrParams& p, cudaStream_t stream) {
 
 cudaError_t launch_tree_linear(const GdrParams& p, bool bf16, cudaStream_t stream) {
   if (p.R == 0) return cudaSuccess;
+  if (bf16 && tree_linear_tc_supported(p.dk, p.dv)) return launch_tree_linear_tc(p, stream);
   return bf16 ? launch_d<__nv_bfloat16>(p, stream) : launch_d<float>(p, stream);
 }
 

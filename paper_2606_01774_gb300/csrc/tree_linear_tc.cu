@@ -1,0 +1,641 @@
+// Gated delta rule along the paths of a drafted tree on tcgen05 tensor cores:
+// bf16 activations, 128 x 128 states, persistent CTAs.
+//
+// tree_linear.cu has the system that a tree's paths unroll to.  For one
+// (request, value head) item, with BM = 16, 32 or 64 rows for the tree's nodes:
+//   MMA  W^T = S0^T [K; Q]^T   M = 128 (value columns on lanes), N = 2 BM, K = 128
+//        G   = [K; Q] K^T      M = 128 (rows on lanes), N = BM, over S0^T
+//   A[i][j] = beta_i exp(gamma_i - gamma_j) G[i][j]     for j on i's path, j != i
+//   M[i][j] = exp(gamma_i - gamma_j) G[BM + i][j]       for j on i's path
+//   for i = 0, 1, ...   (thread c owns value column c; parents come first)
+//     delta_i = beta_i (v_i - exp(gamma_i) W^T[c][i]) - sum_j A[i][j] delta_j
+//     out_i   = scale (exp(gamma_i) W^T[c][BM + i] + sum_j M[i][j] delta_j)
+// The state is rounded to bf16 for W; G, the tables, the substitution and the
+// readout are fp32.  Substitution and readout run on the CUDA cores in one
+// pass: a tree's rows are short (its depth), and a block of four columns that
+// a node's path does not touch is skipped.
+//
+// Bound by the state's bytes: 64 KiB an item, so a CTA's life is organised
+// around its copies.  Warp 4 runs ahead: it finds the next item, streams its
+// state in 16 KiB pieces through a ring, its keys and queries by TMA, works
+// out its paths and gates (pointer doubling), and issues the MMAs as the
+// pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
+// tensor memory, then tables, substitution and readout.  BM <= 32: 128
+// tensor-memory columns and under 76 KiB, three CTAs per SM; BM = 64: two.
+// Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
+// lets its copies and MMAs land, frees its tensor memory and exits.
+#include <cudaTypedefs.h>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "tc.cuh"
+#include "tree.cuh"
+
+namespace flare {
+
+namespace {
+
+constexpr int kTlD = 128;          // d_k = d_v
+constexpr int kTlCompute = 128;    // warps 0-3: a thread per value column
+constexpr int kTlThreads = 160;    // and the producer warp
+constexpr int kPieceRows = 32;     // state rows per ring piece
+constexpr int kPieceBytes = kPieceRows * kTlD * 4;
+constexpr int kPieces = kTlD / kPieceRows;  // per item
+
+// What the producer warp works out for an item.  Three buffers: the item at
+// work, the next one, whose state is on its way, and the one after, worked out
+// while the first is in its readout.
+template <int BM>
+struct TlMeta {
+  alignas(16) float gam2[BM];  // gamma_i log2(e)
+  float beta[BM];
+  uint64_t anc[BM];
+  int item, n;                 // item < 0: no more
+};
+
+template <int BM>
+struct TlCfg {
+  static constexpr int kCtas = BM == 64 ? 2 : 3;               // per SM
+  static constexpr int kRing = BM == 16 ? 4 : BM == 32 ? 3 : 2;  // state pieces in flight
+  static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
+  static constexpr int kTable = BM * BM * 4;
+  // BM = 64: the tables take the key / query buffer's place, and the deltas,
+  // too many for registers, have a buffer
+  static constexpr bool kOverlay = BM == 64;
+  static constexpr int kDelta = BM == 64 ? BM * kTlD * 4 : 0;
+  static constexpr int oKQ = 0;
+  static constexpr int oRing = kKQ;
+  static constexpr int oTables = kOverlay ? 0 : oRing + kRing * kPieceBytes;
+  static constexpr int oDelta = oRing + kRing * kPieceBytes + (kOverlay ? 0 : 2 * kTable);
+  static constexpr int oShared = oDelta + kDelta;
+  static constexpr int kTmem = 64 + 2 * BM <= 128 ? 128 : 256;
+};
+
+template <int BM>
+struct alignas(16) TlShared {
+  TlMeta<BM> meta[3];
+  uint64_t full[4], empty[4];  // ring pieces
+  uint64_t kq_full, kq_free, mma_done, meta_full[3];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+template <int BM>
+constexpr int tl_smem() {
+  return TlCfg<BM>::oShared + (int)sizeof(TlShared<BM>);
+}
+
+struct TlMaps {
+  CUtensorMap k, q;  // (128, Hk, N, R) box (64, 1, BM, 1), 128-byte swizzle
+};
+
+// Word offset of columns 4 u .. 4 u + 3 of row `row` of a BM x BM table whose
+// 16-byte units are XOR-swizzled by the row (a warp writes a row per lane).
+template <int BM>
+__device__ __forceinline__ int tl_at(int row, int u) {
+  return row * BM + ((u ^ (row & (BM / 4 - 1))) << 2);
+}
+
+__device__ __forceinline__ bool tl_warp_wait(uint64_t* bar, uint32_t parity, const int* abort) {
+  return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity, abort));
+}
+
+// OR of a predicate over the 128 compute threads, with barrier semantics.
+__device__ __forceinline__ bool tl_compute_or(bool x) {
+  int r;
+  asm volatile(
+      "{\n"
+      " .reg .pred p, q;\n"
+      " setp.ne.s32 p, %1, 0;\n"
+      " bar.red.or.pred q, 1, 128, p;\n"
+      " selp.s32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"((int)x)
+      : "memory");
+  return r != 0;
+}
+
+__device__ __forceinline__ uint32_t tl_pack(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ float tl_bf16(unsigned short x) {
+  return __uint_as_float((uint32_t)x << 16);
+}
+
+}  // namespace
+
+template <int BM>
+__global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
+    tree_linear_tc_kernel(const __grid_constant__ TlMaps maps, GdrParams p) {
+  using C = TlCfg<BM>;
+  // no static shared memory: the dynamic window starts 1024-byte aligned, as
+  // the swizzled operands need (checked below)
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  TlShared<BM>& sh = *reinterpret_cast<TlShared<BM>*>(smem_raw + C::oShared);
+  uint8_t* KQ = smem_raw + C::oKQ;
+  uint8_t* ring = smem_raw + C::oRing;
+  float* At = reinterpret_cast<float*>(smem_raw + C::oTables);
+  float* Mt = At + BM * BM;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tc::smem_u32(smem_raw) & 1023u) {
+    if (tid == 0) flag(p.dev_status, FLARE_DEV_WAIT_TIMEOUT);
+    return;
+  }
+  if (tid == 0) {
+    sh.abort_flag = 0;
+    for (int s = 0; s < C::kRing; ++s) {
+      tc::mbar_init(&sh.full[s], 1);
+      tc::mbar_init(&sh.empty[s], kTlCompute);
+    }
+    tc::mbar_init(&sh.kq_full, 1);
+    tc::mbar_init(&sh.kq_free, kTlCompute);
+    tc::mbar_init(&sh.mma_done, 1);
+    for (int b = 0; b < 3; ++b) tc::mbar_init(&sh.meta_full[b], 1);
+    tc::fence_mbar_init();
+  }
+  if (warp == 4) tc::tmem_alloc(&sh.tmem_base, C::kTmem);
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmS = sh.tmem_base;  // S0^T as bf16 pairs (64 columns); then G
+  const uint32_t tmW = tmS + 64;      // W^T: [K part | Q part]
+  const int total = p.R * p.Hv;
+
+  if (warp == 4) {
+    // ------------------------------------------------------------ producer
+    const uint32_t idW = tc::idesc_bf16(128, 2 * BM, false, false);
+    const uint32_t idG = tc::idesc_bf16(128, BM, false, false);
+    if (lane == 0) {
+      tc::prefetch_tmap(&maps.k);
+      tc::prefetch_tmap(&maps.q);
+    }
+    bool ok = true;
+    uint32_t issued = 0;  // ring pieces so far
+    int items = 0;        // items whose meta is written
+    int kq_items = 0;     // items whose keys and queries are requested
+    int mma_items = 0;    // items whose MMAs are committed
+    int it = blockIdx.x;
+
+    // The next item with something to do, from `it` on: its paths and gates
+    // into the next meta buffer.  Returns it (or -1), with its slot.
+    auto next_meta = [&](int& slot) -> int {
+      TlMeta<BM>& m = sh.meta[items % 3];
+      int found = -1;
+      for (; it < total; it += gridDim.x) {
+        const int r = it / p.Hv, j = it - r * p.Hv;
+        const int n = p.node_len[r], s = p.state_slot[r];
+        const size_t g0 = (size_t)r * p.B * p.Hv + j;
+        int bad = 0;
+        if (n < 0 || n > p.B) bad |= FLARE_DEV_BAD_TREE;
+        if (s < 0 || s >= p.nslots) bad |= FLARE_DEV_BAD_SLOT;
+        int p0 = -1, p1 = -1;
+        if (!bad && !warp_load_tree(p.parent + (size_t)r * p.B, n, p0, p1))
+          bad |= FLARE_DEV_BAD_TREE;
+        if (bad) {
+          if (lane == 0) flag(p.dev_status, bad);
+          continue;
+        }
+        if (n == 0) {  // rests this round
+          for (int e = lane; e < p.B * (kTlD / 8); e += 32)
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out_causal) +
+                                      (g0 + (size_t)(e / (kTlD / 8)) * p.Hv) * kTlD +
+                                      (e % (kTlD / 8)) * 8) = make_uint4(0u, 0u, 0u, 0u);
+          continue;
+        }
+        float x0 = lane < n ? p.log_decay[g0 + (size_t)lane * p.Hv] : 0.f;
+        float x1 = lane + 32 < n ? p.log_decay[g0 + (size_t)(lane + 32) * p.Hv] : 0.f;
+        const float b0 = lane < n ? p.beta[g0 + (size_t)lane * p.Hv] : 0.f;
+        const float b1 = lane + 32 < n ? p.beta[g0 + (size_t)(lane + 32) * p.Hv] : 0.f;
+        // pointer doubling: sets and sums over the 2^k nearest path members
+        uint64_t a0 = lane < n ? 1ull << lane : 0ull;
+        uint64_t a1 = lane + 32 < n ? 1ull << (lane + 32) : 0ull;
+        while (__any_sync(0xffffffffu, p0 >= 0 || p1 >= 0)) {
+          const uint64_t l0 = shfl64(a0, p0 & 31), h0 = shfl64(a1, p0 & 31);
+          const float xl0 = __shfl_sync(0xffffffffu, x0, p0 & 31);
+          const float xh0 = __shfl_sync(0xffffffffu, x1, p0 & 31);
+          const int ql0 = __shfl_sync(0xffffffffu, p0, p0 & 31);
+          const int qh0 = __shfl_sync(0xffffffffu, p1, p0 & 31);
+          if constexpr (BM == 64) {
+            const uint64_t l1 = shfl64(a0, p1 & 31), h1 = shfl64(a1, p1 & 31);
+            const float xl1 = __shfl_sync(0xffffffffu, x0, p1 & 31);
+            const float xh1 = __shfl_sync(0xffffffffu, x1, p1 & 31);
+            const int ql1 = __shfl_sync(0xffffffffu, p0, p1 & 31);
+            const int qh1 = __shfl_sync(0xffffffffu, p1, p1 & 31);
+            if (p1 >= 0) {
+              a1 |= p1 < 32 ? l1 : h1;
+              x1 += p1 < 32 ? xl1 : xh1;
+              p1 = p1 < 32 ? ql1 : qh1;
+            }
+          }
+          if (p0 >= 0) {
+            a0 |= p0 < 32 ? l0 : h0;
+            x0 += p0 < 32 ? xl0 : xh0;
+            p0 = p0 < 32 ? ql0 : qh0;
+          }
+        }
+        if (lane < BM) {
+          m.anc[lane] = a0;
+          m.gam2[lane] = x0 * 1.4426950408889634f;
+          m.beta[lane] = b0;
+        }
+        if constexpr (BM == 64) {
+          m.anc[lane + 32] = a1;
+          m.gam2[lane + 32] = x1 * 1.4426950408889634f;
+          m.beta[lane + 32] = b1;
+        }
+        if (lane == 0) m.n = n;
+        slot = s;
+        found = it;
+        it += gridDim.x;
+        break;
+      }
+      if (lane == 0) m.item = found;
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&sh.meta_full[items % 3]);
+      ++items;
+      return found;
+    };
+    auto issue_piece = [&](int item, int slot, int q) {
+      if (lane == 0) {
+        const int s = issued % C::kRing;
+        const float* src = p.state_pool + ((size_t)slot * p.Hv + item % p.Hv) * kTlD * kTlD +
+                           (size_t)q * kPieceRows * kTlD;
+        tc::mbar_expect_tx(&sh.full[s], kPieceBytes);
+        tc::bulk_load(ring + s * kPieceBytes, src, kPieceBytes, &sh.full[s]);
+      }
+      ++issued;
+    };
+    auto issue_kq = [&](int item) {
+      if (lane == 0) {
+        const int r = item / p.Hv, h = (item - r * p.Hv) / (p.Hv / p.Hk);
+        tc::mbar_expect_tx(&sh.kq_full, C::kKQ);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          tc::tma_load_4d(KQ + c * (2 * BM * 128), &maps.k, &sh.kq_full, c * 64, h, 0, r);
+          tc::tma_load_4d(KQ + c * (2 * BM * 128) + BM * 128, &maps.q, &sh.kq_full, c * 64, h, 0,
+                          r);
+        }
+      }
+      ++kq_items;
+    };
+
+    int slot = 0, slot_next = 0;
+    int cur = next_meta(slot), nxt = -1;
+    if (cur >= 0) {
+      issue_kq(cur);
+      for (int q = 0; q < C::kRing; ++q) issue_piece(cur, slot, q);
+      nxt = next_meta(slot_next);
+    }
+    uint32_t used = 0;  // ring pieces consumed
+    while (cur >= 0 && ok) {
+      // this item's pieces become operands in order; each freed slot takes the
+      // piece kRing ahead, this item's or the next one's
+      for (int q = 0; q < kPieces && ok; ++q, ++used) {
+        const int s = used % C::kRing;
+        if (!tl_warp_wait(&sh.empty[s], (used / C::kRing) & 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        if (q + C::kRing < kPieces) issue_piece(cur, slot, q + C::kRing);
+        else if (nxt >= 0) issue_piece(nxt, slot_next, q + C::kRing - kPieces);
+        if (q == 0 && !tl_warp_wait(&sh.kq_full, (uint32_t)(kq_items - 1) & 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        if (lane == 0) {
+          tc::fence_after_sync();
+#pragma unroll
+          for (int kk = 2 * q; kk < 2 * q + 2; ++kk)
+            tc::mma_bf16_ts(tmW, tmS + kk * 8,
+                            tc::sdesc_sw128(tc::smem_u32(KQ + (kk >> 2) * (2 * BM * 128) +
+                                                         (kk & 3) * 32),
+                                            16, 1024),
+                            idW, kk > 0);
+          if (q == kPieces - 1) {
+#pragma unroll
+            for (int kk = 0; kk < kTlD / 16; ++kk) {
+              const uint64_t kd = tc::sdesc_sw128(
+                  tc::smem_u32(KQ + (kk >> 2) * (2 * BM * 128) + (kk & 3) * 32), 16, 1024);
+              tc::mma_bf16_ss(tmS, kd, kd, idG, kk > 0);
+            }
+            tc::mma_commit(&sh.mma_done);
+          }
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      ++mma_items;
+      // every compute thread is past the previous item: its meta buffer takes
+      // the item after the next
+      int slot_after = 0;
+      const int after = nxt >= 0 ? next_meta(slot_after) : -1;
+      // the key / query buffer: free once the products have read it, or, where
+      // the tables take its place, once the readout has
+      if (nxt >= 0) {
+        uint64_t* bar = C::kOverlay ? &sh.kq_free : &sh.mma_done;
+        if (!tl_warp_wait(bar, (uint32_t)(mma_items - 1) & 1u, &sh.abort_flag)) {
+          ok = false;
+          break;
+        }
+        if (C::kOverlay) tc::fence_async_smem();
+        issue_kq(nxt);
+      }
+      cur = nxt;
+      slot = slot_next;
+      nxt = after;
+      slot_next = slot_after;
+    }
+    if (!ok && lane == 0 && !sh.abort_flag) {
+      sh.abort_flag = 1;
+      flag(p.dev_status, FLARE_DEV_WAIT_TIMEOUT);
+    }
+    __syncwarp();
+    if (*reinterpret_cast<volatile int*>(&sh.abort_flag)) {  // let what is in flight land
+      for (uint32_t back = 1; back <= C::kRing && back <= issued; ++back) {
+        const uint32_t x = issued - back;
+        tc::mbar_wait(&sh.full[x % C::kRing], (x / C::kRing) & 1u, nullptr, 100000000ull);
+      }
+      if (kq_items)
+        tc::mbar_wait(&sh.kq_full, (uint32_t)(kq_items - 1) & 1u, nullptr, 100000000ull);
+      if (lane == 0) {
+        tc::mma_commit(&sh.mma_done);
+        tc::mbar_wait(&sh.mma_done, (uint32_t)mma_items & 1u, nullptr, 100000000ull);
+      }
+      __syncwarp();
+    }
+  } else {
+    // ------------------------------------------------------------ compute
+    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    uint32_t used = 0;  // ring pieces consumed
+    bool bad = false;
+#pragma unroll 1
+    for (int k = 0;; ++k) {
+      bad |= !tc::mbar_wait(&sh.meta_full[k % 3], (uint32_t)(k / 3) & 1u, &sh.abort_flag);
+      if (tl_compute_or(bad)) break;  // the same answer on every compute thread
+      const TlMeta<BM>& m = sh.meta[k % 3];
+      const int item = m.item, n = m.n;
+      if (item < 0) break;
+      const int r = item / p.Hv, j = item - r * p.Hv;
+      const size_t row0 = ((size_t)r * p.B * p.Hv + j) * kTlD;
+      const size_t row_stride = (size_t)p.Hv * kTlD;
+      const unsigned short* vg = static_cast<const unsigned short*>(p.v) + row0 + tid;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out_causal) + row0 + (tid & ~1);
+      constexpr int kVr = BM <= 32 ? BM : 1;
+      unsigned short vr[kVr];  // this column's values (BM <= 32)
+      if constexpr (BM <= 32) {
+#pragma unroll
+        for (int i = 0; i < BM; ++i) vr[i] = i < n ? vg[i * row_stride] : (unsigned short)0;
+      }
+      // the state, piece by piece, into tensor memory as bf16 pairs
+#pragma unroll 1
+      for (int q = 0; q < kPieces; ++q, ++used) {
+        const int s = used % C::kRing;
+        bad |= !tc::mbar_wait(&sh.full[s], (used / C::kRing) & 1u, &sh.abort_flag);
+        __syncwarp();
+        const float* S = reinterpret_cast<const float*>(ring + s * kPieceBytes) + tid;
+        uint32_t w[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = tl_pack(S[(2 * e) * kTlD], S[(2 * e + 1) * kTlD]);
+        tc::tmem_st16(tmS + lane_off + 16 * q, w);
+        tc::tmem_st_wait();
+        tc::fence_before_sync();
+        tc::mbar_arrive(&sh.empty[s]);
+      }
+      bad |= !tc::mbar_wait(&sh.mma_done, (uint32_t)k & 1u, &sh.abort_flag);
+      __syncwarp();
+      tc::fence_after_sync();
+      // the tables: lane i < BM of G's rows A's row i, lane BM + i M's row i
+      if (warp * 32 < 2 * BM) {
+        const bool is_m = tid >= BM;
+        const int i = is_m ? tid - BM : tid;
+        const uint64_t path = m.anc[i];  // empty from n on
+        const float gi = m.gam2[i], f = is_m ? 1.f : m.beta[i];
+        const uint64_t see = is_m ? path : path & ~(1ull << i);
+        float* row = is_m ? Mt : At;
+#pragma unroll
+        for (int c0 = 0; c0 < BM; c0 += 16) {
+          uint32_t g[16];
+          tc::tmem_ld16(tmS + lane_off + c0, g);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const float4 gj = *reinterpret_cast<const float4*>(&m.gam2[c0 + 4 * u]);
+            const float gv[4] = {gj.x, gj.y, gj.z, gj.w};
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {  // masked by selects: exp may overflow off the path
+              const float x = f * tc::ex2(gi - gv[e]) * __uint_as_float(g[4 * u + e]);
+              v[e] = (see >> (c0 + 4 * u + e)) & 1 ? x : 0.f;
+            }
+            *reinterpret_cast<float4*>(row + tl_at<BM>(i, c0 / 4 + u)) =
+                make_float4(v[0], v[1], v[2], v[3]);
+          }
+        }
+      }
+      if (tl_compute_or(bad)) break;  // the tables are complete
+
+      // Rows i, i + 1 of this column and its neighbour: adjacent lanes swap a
+      // value, so that each stores a bf16 pair of two columns.
+      const bool odd = lane & 1;
+      auto store2 = [&](int i, float a, float b) {
+        const float recv = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+        const int row = odd ? i + 1 : i;
+        if (row < p.B)
+          *reinterpret_cast<uint32_t*>(out + row * row_stride) =
+              odd ? tl_pack(recv, b) : tl_pack(a, recv);
+      };
+      if constexpr (BM <= 32) {
+        float dl[BM];
+#pragma unroll
+        for (int i0 = 0; i0 < BM; i0 += 16) {
+          if (i0 < n) {
+            uint32_t wk[16], wq[16];
+            tc::tmem_ld16(tmW + lane_off + i0, wk);
+            tc::tmem_ld16(tmW + lane_off + BM + i0, wq);
+            tc::tmem_ld_wait();
+            float o[2];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int i = i0 + e;
+              o[e & 1] = 0.f;
+              dl[i] = 0.f;
+              if (i < n) {
+                const float ga = tc::ex2(m.gam2[i]);
+                float x = m.beta[i] * (tl_bf16(vr[i]) - ga * __uint_as_float(wk[e]));
+                float y = ga * __uint_as_float(wq[e]);
+                const uint32_t path = (uint32_t)m.anc[i];
+#pragma unroll
+                for (int u = 0; u <= i / 4; ++u) {
+                  if (BM == 16 || u == i / 4 || (path >> (4 * u)) & 15u) {
+                    const float4 a = *reinterpret_cast<const float4*>(At + tl_at<BM>(i, u));
+                    const float4 b = *reinterpret_cast<const float4*>(Mt + tl_at<BM>(i, u));
+                    const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+                      if (4 * u + d < i) {
+                        x = fmaf(-av[d], dl[4 * u + d], x);
+                        y = fmaf(bv[d], dl[4 * u + d], y);
+                      }
+                    if (u == i / 4) y = fmaf(bv[i & 3], x, y);
+                  }
+                }
+                dl[i] = x;
+                o[e & 1] = p.scale * y;
+              }
+              if (e & 1) store2(i - 1, o[0], o[1]);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) store2(i0 + e, 0.f, 0.f);
+          }
+        }
+      } else {
+        // deltas in shared memory, four nodes at a time against the four-node
+        // blocks that any of their paths touches
+        float* Dl = reinterpret_cast<float*>(smem_raw + C::oDelta) + tid;
+        unsigned short vn[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vn[e] = e < n ? vg[e * row_stride] : (unsigned short)0;
+#pragma unroll 1
+        for (int i0 = 0; i0 < n; i0 += 4) {
+          uint32_t wk[4], wq[4];
+          asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(wk[0]), "=r"(wk[1]), "=r"(wk[2]), "=r"(wk[3])
+                       : "r"(tmW + lane_off + i0));
+          asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(wq[0]), "=r"(wq[1]), "=r"(wq[2]), "=r"(wq[3])
+                       : "r"(tmW + lane_off + BM + i0));
+          tc::tmem_ld_wait();
+          float x[4], y[4];
+          uint64_t any = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = i0 + e;
+            const float ga = tc::ex2(m.gam2[i]);
+            x[e] = i < n ? m.beta[i] * (tl_bf16(vn[e]) - ga * __uint_as_float(wk[e])) : 0.f;
+            y[e] = i < n ? ga * __uint_as_float(wq[e]) : 0.f;
+            any |= m.anc[i];
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e)  // the next four nodes' values
+            vn[e] = i0 + 4 + e < n ? vg[(i0 + 4 + e) * row_stride] : (unsigned short)0;
+#pragma unroll 1
+          for (int u = 0; u < i0 / 4; ++u) {
+            if (!((any >> (4 * u)) & 15)) continue;
+            float d[4];
+#pragma unroll
+            for (int f = 0; f < 4; ++f) d[f] = Dl[(4 * u + f) * kTlD];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float4 a = *reinterpret_cast<const float4*>(At + tl_at<BM>(i0 + e, u));
+              const float4 b = *reinterpret_cast<const float4*>(Mt + tl_at<BM>(i0 + e, u));
+              x[e] = fmaf(-a.x, d[0], x[e]);
+              x[e] = fmaf(-a.y, d[1], x[e]);
+              x[e] = fmaf(-a.z, d[2], x[e]);
+              x[e] = fmaf(-a.w, d[3], x[e]);
+              y[e] = fmaf(b.x, d[0], y[e]);
+              y[e] = fmaf(b.y, d[1], y[e]);
+              y[e] = fmaf(b.z, d[2], y[e]);
+              y[e] = fmaf(b.w, d[3], y[e]);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {  // the four among themselves
+            const float4 a = *reinterpret_cast<const float4*>(At + tl_at<BM>(i0 + e, i0 / 4));
+            const float4 b = *reinterpret_cast<const float4*>(Mt + tl_at<BM>(i0 + e, i0 / 4));
+            const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int f = 0; f < e; ++f) {
+              x[e] = fmaf(-av[f], x[f], x[e]);
+              y[e] = fmaf(bv[f], x[f], y[e]);
+            }
+            y[e] = p.scale * fmaf(bv[e], x[e], y[e]);
+            Dl[(i0 + e) * kTlD] = x[e];
+          }
+          store2(i0, y[0], y[1]);
+          store2(i0 + 2, y[2], y[3]);
+        }
+#pragma unroll 1
+        for (int i = (n + 3) & ~3; i < p.B; i += 2) store2(i, 0.f, 0.f);
+        tc::mbar_arrive(&sh.kq_free);  // the tables are read
+      }
+    }
+    if (bad && !sh.abort_flag) {
+      sh.abort_flag = 1;
+      flag(p.dev_status, FLARE_DEV_WAIT_TIMEOUT);
+    }
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 4) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmS, C::kTmem);
+  }
+}
+
+// ------------------------------------------------------------------ host side
+
+namespace {
+
+PFN_cuTensorMapEncodeTiled_v12000 tl_encode_fn() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  }();
+  return fn;
+}
+
+// [R, N, Hk, 128] bf16 as a 4-D map (128, Hk, N, R), box (64, 1, rows, 1);
+// rows past N read as zero
+bool tl_map(CUtensorMap* m, const void* x, const GdrParams& p, int rows) {
+  auto fn = tl_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t gd[4] = {(cuuint64_t)kTlD, (cuuint64_t)p.Hk, (cuuint64_t)p.B, (cuuint64_t)p.R};
+  const cuuint64_t gs[3] = {(cuuint64_t)kTlD * 2, (cuuint64_t)p.Hk * kTlD * 2,
+                            (cuuint64_t)p.B * p.Hk * kTlD * 2};
+  const cuuint32_t bx[4] = {64, 1, (cuuint32_t)rows, 1};
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(x), gd, gs, bx, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+         CUDA_SUCCESS;
+}
+
+template <int BM>
+cudaError_t launch_tl(const GdrParams& p, cudaStream_t stream) {
+  TlMaps maps;
+  if (!tl_map(&maps.k, p.k, p, BM) || !tl_map(&maps.q, p.q, p, BM)) return cudaErrorInvalidValue;
+  constexpr int smem = tl_smem<BM>();
+  static_assert(TlCfg<BM>::kCtas * (smem + 1024) <= 228 * 1024, "CTAs per SM");
+  cudaError_t e = cudaFuncSetAttribute(tree_linear_tc_kernel<BM>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  int dev = 0, sms = kNumSMs;
+  if (cudaGetDevice(&dev) == cudaSuccess)
+    cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const long items = (long)p.R * p.Hv, room = (long)TlCfg<BM>::kCtas * sms;
+  tree_linear_tc_kernel<BM>
+      <<<(unsigned)(items < room ? items : room), kTlThreads, smem, stream>>>(maps, p);
+  note_launches(1);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool tree_linear_tc_supported(int dk, int dv) { return dk == kTlD && dv == kTlD; }
+
+cudaError_t launch_tree_linear_tc(const GdrParams& p, cudaStream_t stream) {
+  return p.B <= 16 ? launch_tl<16>(p, stream)
+         : p.B <= 32 ? launch_tl<32>(p, stream)
+                     : launch_tl<64>(p, stream);
+}
+
+}  // namespace flare
