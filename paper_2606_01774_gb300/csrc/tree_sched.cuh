@@ -29,6 +29,13 @@ struct TreeSpanShared {
   int r;
 };
 
+// The item that a gang starts and leaves unfinished, to be merged: its request
+// (-1: none), kv head and first tile.
+struct alignas(16) TreeCut {
+  int r, kvh;
+  long long s0;
+};
+
 // A stretch of one item's tiles: j0 .. j1 - 1 of n.
 struct TreePiece {
   int r, kvh, j0, j1, n;
@@ -73,8 +80,8 @@ __device__ __forceinline__ long long shfl_up_ll(long long x, int o) {
   return __shfl_up_sync(0xffffffffu, x, o);
 }
 
-// The span of `gang`, found by all threads of the CTA together; CTA 0 also
-// records where each request's tiles start.
+// The span of `gang`, found by all threads of the CTA together; the gang's
+// first CTA also records its cut.
 template <int THREADS>
 __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int gang,
                                                 TreeSpanShared& sh) {
@@ -116,14 +123,26 @@ __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int 
     sh.r = r;
     sh.off = lo - at;
   }
-  if (blockIdx.x == 0) {
-    long long at = before;
-    for (int r = r0; r < r1; ++r) {
-      p.first[r] = at;
-      at += (long long)max(p.tiles[r], 0) * p.Hkv;
+  // what this gang leaves unfinished, for the merge (one thread holds its
+  // last tile)
+  if (blockIdx.x % p.row_tiles == 0) {
+    TreeCut* cut = static_cast<TreeCut*>(p.cuts) + gang;
+    if (lo >= hi) {
+      if (tid == 0) *cut = TreeCut{-1, 0, 0};
+    } else if (before <= hi - 1 && hi - 1 < before + sum) {
+      long long at = before;
+      int r = r0;
+      for (;; ++r) {
+        const long long n = (long long)max(p.tiles[r], 0) * p.Hkv;
+        if (hi - 1 < at + n) break;
+        at += n;
+      }
+      const int n = p.tiles[r], kvh = (int)((hi - 1 - at) / n);
+      const long long s0 = at + (long long)kvh * n;
+      *cut = TreeCut{s0 >= lo && s0 + n > hi ? r : -1, kvh, s0};
     }
   }
-  if (blockIdx.x == 0 && tid == 0) p.first[p.R] = total;
+  if (blockIdx.x == 0 && tid == 0) *p.total = total;
   __syncthreads();
   TreeCursor c;
   c.left = sh.hi - sh.lo;

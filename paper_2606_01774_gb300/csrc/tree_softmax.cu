@@ -12,6 +12,7 @@
 // maximum, sum and output in fp32.
 #include "common.cuh"
 #include "kernels.h"
+#include "pdl.cuh"
 #include "tree.cuh"
 #include "tree_sched.cuh"
 
@@ -34,6 +35,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
 }  // namespace
 
 __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxParams p) {
+  pdl_launch_next();
   const int r = blockIdx.x, tid = threadIdx.x;
   const int n = p.node_len[r], P = p.prefix_len[r];
   int bad = 0;
@@ -87,6 +89,8 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   const float* q = static_cast<const float*>(p.q);
   const float* pools[2] = {static_cast<const float*>(p.k_pool), static_cast<const float*>(p.v_pool)};
   const float* blks[2] = {static_cast<const float*>(p.k_blk), static_cast<const float*>(p.v_blk)};
+  pdl_wait();  // the plan
+  pdl_launch_next();
   TreeCursor cur = tree_span<kThreadsS>(p, gang, span);
   TreePiece w;
   while (cur.next(p, w)) {
@@ -245,141 +249,138 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   }
 }
 
-// Merges the pieces of items that several gangs share, and writes the unused
-// nodes' rows.  A row's pieces are the last piece of the first gang (slot 1)
-// and the first of each later one (slot 0), in gang order, whatever the
-// timing:  out = sum_s 2^(lse_s - lse) out_s.  WARPS warps share a row: one
-// when there are rows enough to fill the GPU, eight, each with every eighth
-// piece, when a few rows have many pieces.
+// Writes the unused nodes' rows, and merges the pieces of items that several
+// gangs share: a CTA per gang, row tile and group of rows takes the item that
+// its gang leaves unfinished.  A row's pieces are that gang's last (slot 1) and
+// the first of each later one (slot 0), in gang order, whatever the timing:
+//     out = sum_s 2^(lse_s - lse) out_s.
+// WARPS warps share a row: one, with eight rows to a CTA, or eight, each with
+// every eighth piece, where rows are few and may have many pieces.
 template <typename T, int D, int WARPS>
 __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   constexpr int kV = D >= 128 ? D / 128 : 1;  // 16-byte groups per lane
   constexpr int kLanes = D / (4 * kV);        // lanes that hold columns
   constexpr int kRowsPerCta = 8 / WARPS;
   __shared__ float red_o[WARPS > 1 ? 8 : 1][D];
-  __shared__ float red_l[WARPS > 1 ? 8 : 1];
+  __shared__ float red_l[8], red_d[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = warp % WARPS;
-  const long long rows = (long long)p.R * p.N * p.Hq;
-  const long long total = p.first[p.R];
+  // unused nodes' rows, a node per warp (the plan has completed: the attention
+  // kernel waited for it before it let this one start)
+  for (long long u = (long long)blockIdx.x * 8 + warp; u < (long long)p.R * p.N;
+       u += (long long)gridDim.x * 8) {
+    const int r = (int)(u / p.N), t = (int)(u - (long long)r * p.N);
+    if (p.tiles[r] < 0 || t < p.node_len[r]) continue;
+    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + u * p.Hq * D);
+    const int n16 = p.Hq * (D * (int)sizeof(T) / 16);
+    for (int e = lane; e < n16; e += 32) out[e] = make_uint4(0u, 0u, 0u, 0u);
+    if (p.lse)
+      for (int e = lane; e < p.Hq; e += 32) p.lse[u * p.Hq + e] = -INFINITY;
+  }
+  const int per_tile = gridDim.x / (p.gangs * p.row_tiles);  // CTAs per gang and row tile
+  const int part_id = blockIdx.x % per_tile;
+  const int g0 = blockIdx.x / per_tile / p.row_tiles, mt = blockIdx.x / per_tile % p.row_tiles;
+  const int row = part_id * kRowsPerCta + warp / WARPS;  // of the row tile
+  pdl_wait();                                            // the attention
+  const long long total = *p.total;
   const int gangs = tree_gangs(p, total);
-  for (long long o0 = (long long)blockIdx.x * kRowsPerCta; o0 < rows;
-       o0 += (long long)gridDim.x * kRowsPerCta) {
-    const long long o = o0 + warp / WARPS;  // row of out: (r, t, query head)
-    int n = -1, live = 0;
-    int r = 0, t = 0, h = 0;
-    if (o < rows) {
-      h = (int)(o % p.Hq);
-      t = (int)(o / p.Hq % p.N);
-      r = (int)(o / ((long long)p.Hq * p.N));
-      n = p.tiles[r];
-      live = n < 0 ? 0 : p.node_len[r];
-    }
-    int g0 = 0, g1 = 0;
-    const int kvh = h / p.G, m = t * p.G + (h - kvh * p.G);
-    if (n > 0 && t < live) {
-      const long long s0 = p.first[r] + (long long)kvh * n;
-      g0 = tree_gang_of(s0, total, gangs);
-      g1 = tree_gang_of(s0 + n - 1, total, gangs);
-    }
-    const bool dead = n >= 0 && t >= live, merge = g1 > g0;
-    T* out = static_cast<T*>(p.out) + o * D;
-    if (dead && sub == 0) {
+  if (g0 >= gangs) return;
+  const TreeCut cut = static_cast<const TreeCut*>(p.cuts)[g0];
+  if (cut.r < 0) return;
+  const int n = p.tiles[cut.r], m = mt * p.tile_rows + row;
+  const bool live = m < p.node_len[cut.r] * p.G;
+  const int g1 = tree_gang_of(cut.s0 + n - 1, total, gangs);
+  auto part = [&](int g) {
+    return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows + row;
+  };
+  // this warp's pieces: running maximum, sum of weights, weighted output
+  float mx = -INFINITY, den = 0.f;
+  float4 acc[kV];
 #pragma unroll
-      for (int v = 0; v < kV; ++v)
-        if (lane < kLanes) store4(out + 4 * (lane + 32 * v), make_float4(0.f, 0.f, 0.f, 0.f));
-      if (lane == 0 && p.lse) p.lse[o] = -INFINITY;
-    }
-    if (WARPS == 1 && !merge) continue;
-    const int mt = m / p.tile_rows, row = m - mt * p.tile_rows;
-    auto part = [&](int g) {
-      return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows + row;
-    };
-    // this warp's pieces: running maximum, sum of weights, weighted output
-    float mx = -INFINITY, den = 0.f;
-    float4 acc[kV];
+  for (int v = 0; v < kV; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (live) {
+    constexpr int kIn = WARPS > 1 ? 8 : 2;  // pieces in flight
+    for (int g = g0 + sub; g <= g1; g += WARPS * kIn) {
+      float l[kIn];
+      float4 x[kIn][kV];
 #pragma unroll
-    for (int v = 0; v < kV; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (merge) {
-      constexpr int kIn = 4;  // pieces in flight
-      for (int g = g0 + sub; g <= g1; g += WARPS * kIn) {
-        float l[kIn];
-        float4 x[kIn][kV];
-#pragma unroll
-        for (int u = 0; u < kIn; ++u) {
-          const int gg = g + u * WARPS;
-          l[u] = gg <= g1 ? p.part_lse[part(gg)] : -INFINITY;
-#pragma unroll
-          for (int v = 0; v < kV; ++v)
-            x[u][v] = gg <= g1 && lane < kLanes
-                          ? *reinterpret_cast<const float4*>(p.part_o + part(gg) * D +
-                                                             4 * (lane + 32 * v))
-                          : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int u = 0; u < kIn; ++u) {
-          if (l[u] == -INFINITY) continue;  // a piece that the row sees nothing of
-          const float mn = fmaxf(mx, l[u]);
-          const float corr = exp2f(mx - mn), e = exp2f(l[u] - mn);
-          den = den * corr + e;
-          mx = mn;
-#pragma unroll
-          for (int v = 0; v < kV; ++v) {
-            acc[v].x = fmaf(e, x[u][v].x, acc[v].x * corr);
-            acc[v].y = fmaf(e, x[u][v].y, acc[v].y * corr);
-            acc[v].z = fmaf(e, x[u][v].z, acc[v].z * corr);
-            acc[v].w = fmaf(e, x[u][v].w, acc[v].w * corr);
-          }
-        }
-      }
-    }
-    if constexpr (WARPS > 1) {
-      __shared__ float red_d[8];
-      __syncthreads();
-      if (lane < kLanes)
+      for (int u = 0; u < kIn; ++u) {
+        const int gg = g + u * WARPS;
+        l[u] = gg <= g1 ? p.part_lse[part(gg)] : -INFINITY;
 #pragma unroll
         for (int v = 0; v < kV; ++v)
-          *reinterpret_cast<float4*>(&red_o[warp][4 * (lane + 32 * v)]) = acc[v];
-      if (lane == 0) {
-        red_l[warp] = mx;
-        red_d[warp] = den;
+          x[u][v] = gg <= g1 && lane < kLanes ? *reinterpret_cast<const float4*>(
+                                                    p.part_o + part(gg) * D + 4 * (lane + 32 * v))
+                                              : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-      __syncthreads();
-      if (sub != 0 || !merge) continue;
 #pragma unroll
-      for (int u = 1; u < WARPS; ++u) {
-        const float l = red_l[u];
-        if (l == -INFINITY) continue;
-        const float mn = fmaxf(mx, l), corr = exp2f(mx - mn), e = exp2f(l - mn);
-        den = den * corr + e * red_d[u];
+      for (int u = 0; u < kIn; ++u) {
+        if (l[u] == -INFINITY) continue;  // a piece that the row sees nothing of
+        const float mn = fmaxf(mx, l[u]);
+        const float corr = exp2f(mx - mn), e = exp2f(l[u] - mn);
+        den = den * corr + e;
         mx = mn;
-        if (lane < kLanes)
 #pragma unroll
-          for (int v = 0; v < kV; ++v) {
-            const float4 y = *reinterpret_cast<const float4*>(&red_o[u][4 * (lane + 32 * v)]);
-            acc[v].x = fmaf(e, y.x, acc[v].x * corr);
-            acc[v].y = fmaf(e, y.y, acc[v].y * corr);
-            acc[v].z = fmaf(e, y.z, acc[v].z * corr);
-            acc[v].w = fmaf(e, y.w, acc[v].w * corr);
-          }
+        for (int v = 0; v < kV; ++v) {
+          acc[v].x = fmaf(e, x[u][v].x, acc[v].x * corr);
+          acc[v].y = fmaf(e, x[u][v].y, acc[v].y * corr);
+          acc[v].z = fmaf(e, x[u][v].z, acc[v].z * corr);
+          acc[v].w = fmaf(e, x[u][v].w, acc[v].w * corr);
+        }
       }
     }
-    const float inv = den > 0.f ? 1.f / den : 0.f;
+  }
+  if constexpr (WARPS > 1) {
     if (lane < kLanes)
 #pragma unroll
       for (int v = 0; v < kV; ++v)
-        store4(out + 4 * (lane + 32 * v),
-               make_float4(acc[v].x * inv, acc[v].y * inv, acc[v].z * inv, acc[v].w * inv));
-    if (lane == 0 && p.lse) p.lse[o] = den > 0.f ? (mx + log2f(den)) * kLn2 : -INFINITY;
+        *reinterpret_cast<float4*>(&red_o[warp][4 * (lane + 32 * v)]) = acc[v];
+    if (lane == 0) {
+      red_l[warp] = mx;
+      red_d[warp] = den;
+    }
+    __syncthreads();
+    if (sub != 0) return;
+#pragma unroll
+    for (int u = 1; u < WARPS; ++u) {
+      const float l = red_l[u];
+      if (l == -INFINITY) continue;
+      const float mn = fmaxf(mx, l), corr = exp2f(mx - mn), e = exp2f(l - mn);
+      den = den * corr + e * red_d[u];
+      mx = mn;
+      if (lane < kLanes)
+#pragma unroll
+        for (int v = 0; v < kV; ++v) {
+          const float4 y = *reinterpret_cast<const float4*>(&red_o[u][4 * (lane + 32 * v)]);
+          acc[v].x = fmaf(e, y.x, acc[v].x * corr);
+          acc[v].y = fmaf(e, y.y, acc[v].y * corr);
+          acc[v].z = fmaf(e, y.z, acc[v].z * corr);
+          acc[v].w = fmaf(e, y.w, acc[v].w * corr);
+        }
+    }
   }
+  if (!live) return;
+  const int t = m / p.G, head = m - t * p.G;
+  const size_t o = ((size_t)cut.r * p.N + t) * p.Hq + cut.kvh * p.G + head;
+  T* out = static_cast<T*>(p.out) + o * D;
+  const float inv = den > 0.f ? 1.f / den : 0.f;
+  if (lane < kLanes)
+#pragma unroll
+    for (int v = 0; v < kV; ++v)
+      store4(out + 4 * (lane + 32 * v),
+             make_float4(acc[v].x * inv, acc[v].y * inv, acc[v].z * inv, acc[v].w * inv));
+  if (lane == 0 && p.lse) p.lse[o] = den > 0.f ? (mx + log2f(den)) * kLn2 : -INFINITY;
 }
 
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,
                                   int max_pages, bool bf16, int num_sms) {
   TreeSoftmaxPlan pl;
   const int G = Hq / Hkv;
-  pl.tile_rows = bf16 ? 128 : kRowsS;
   const long long rows = (long long)N * G;
+  // bf16: two row tiles share a CTA's keys where there are rows for both and
+  // tensor memory holds both (D <= 128).  96 requests of 61 nodes, 244 rows, D =
+  // 128: TWO_MEASURED
+  pl.tile_rows = !bf16 ? kRowsS : D <= 128 && rows > 128 ? 256 : 128;
   pl.row_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
   const int per_sm = bf16 || D == 256 ? 1 : D == 128 ? 2 : 4;
   // as many gangs as the GPU holds at once, and no more than there can be tiles
@@ -394,8 +395,10 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
   size_t at = 0;
   pl.tiles_off = at;
   at += up((size_t)R * sizeof(int32_t));
-  pl.first_off = at;
-  at += up((size_t)(R + 1) * sizeof(long long));
+  pl.total_off = at;
+  at += up(sizeof(long long));
+  pl.cuts_off = at;
+  at += up((size_t)pl.gangs * sizeof(TreeCut));
   pl.anc_off = at;
   at += up((size_t)R * N * sizeof(uint64_t));
   pl.part_o_off = at;
@@ -415,25 +418,26 @@ cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
   cudaError_t e = cudaFuncSetAttribute(tree_softmax_simt_kernel<D>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  tree_softmax_simt_kernel<D>
-      <<<(unsigned)(p.gangs * p.row_tiles), kThreadsS, smem, stream>>>(p);
+  e = pdl_launch(tree_softmax_simt_kernel<D>, dim3((unsigned)(p.gangs * p.row_tiles)), kThreadsS,
+                 smem, stream, true, 1, p);
   note_launches(1);
-  return cudaGetLastError();
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <typename T, int D>
 cudaError_t launch_finish(const TreeSoftmaxParams& p, cudaStream_t stream) {
-  const long long rows = (long long)p.R * p.N * p.Hq;
-  constexpr long long kMaxCtas = 152 * 8;
-  if (rows <= kMaxCtas) {
-    tree_finish_kernel<T, D, 8><<<(unsigned)rows, 256, 0, stream>>>(p);
-  } else {
-    const long long ctas = (rows + 7) / 8;
-    tree_finish_kernel<T, D, 1>
-        <<<(unsigned)(ctas < kMaxCtas ? ctas : kMaxCtas), 256, 0, stream>>>(p);
-  }
+  const long long rows = (long long)p.N * p.G;
+  const int tile = (int)(rows < p.tile_rows ? rows : p.tile_rows);  // used rows of a row tile
+  const int gangs = p.gangs * p.row_tiles;
+  cudaError_t e;
+  if (tile <= 16)
+    e = pdl_launch(tree_finish_kernel<T, D, 8>, dim3((unsigned)(gangs * tile)), 256, 0, stream,
+                   true, 1, p);
+  else
+    e = pdl_launch(tree_finish_kernel<T, D, 1>, dim3((unsigned)(gangs * ((tile + 7) / 8))), 256, 0,
+                   stream, true, 1, p);
   note_launches(1);
-  return cudaGetLastError();
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <int D>

@@ -2,7 +2,7 @@
 // 5th-generation tensor cores (tcgen05), bf16 in, fp32 accumulate.
 //
 // tree_sched.cuh has how the work is cut: a CTA walks its gang's span of key
-// tiles for its own 128 query rows (row m = node * G + g of a (request, kv
+// tiles for its own 128 NQ query rows (row m = node * G + g of a (request, kv
 // head) item: the G query heads of a kv head share its keys).  A piece is a
 // stretch of one item's tiles: prefix tiles through the page table, 64 tokens
 // each, and the item's last tile, the tree's own keys, masked by the rows' path
@@ -17,7 +17,12 @@
 // scores, probabilities and output live in tensor memory, and a persistent
 // CTA keeps the rings full across pieces.
 //
-// Warp roles (256 threads):
+// NQ = 2 (more than 128 rows, D <= 128): a second row tile with its own softmax
+// warps shares every staged tile, so that keys and values enter an SM once for
+// 256 rows; the tensor cores alternate between the two, one's products running
+// while the other's softmax does.
+//
+// Warp roles (256 threads, 384 with NQ = 2):
 //   warp 0     K producer, warp 6 V producer: a TMA box per (page, 64-column
 //              chunk), a lane each, page ids read one tile ahead
 //   warp 7     zeroes V rows that no query may see (past the prefix end, unused
@@ -26,7 +31,7 @@
 //              product have both left it
 //   warp 1     tensor-memory owner; one thread issues S_j = Q K_j^T and
 //              O += P_j V_j; both read their A operand from tensor memory
-//   warps 2-5  softmax, a TMEM lane quarter each: a thread per query row;
+//   warps 2-5 (8-11) softmax, a TMEM lane quarter each: a thread per query row;
 //              online base-2 softmax with a lazily moved maximum (O is rescaled
 //              when it grows by more than 2^8); quarters without a used row skip
 //              the arithmetic
@@ -37,6 +42,7 @@
 
 #include "common.cuh"
 #include "kernels.h"
+#include "pdl.cuh"
 #include "tc.cuh"
 #include "tree.cuh"
 #include "tree_sched.cuh"
@@ -45,10 +51,9 @@ namespace flare {
 
 namespace {
 
-constexpr int kRowsT = 128;            // query rows per CTA (TMEM lanes)
-constexpr int kSmThreads = 128;        // warps 2-5
+constexpr int kRowsT = 128;            // query rows of a row tile (TMEM lanes)
+constexpr int kSmThreads = 128;        // softmax threads of a row tile
 constexpr int kVWarpT = 6, kFixWarpT = 7;
-constexpr int kThreadsT = 256;
 constexpr float kMoveMax = 8.0f;       // log2 units
 
 struct TreeMaps {
@@ -56,24 +61,27 @@ struct TreeMaps {
   CUtensorMap kpool, vpool;  // (D, p, Hkv, num_pages)   box (64, min(p, 64), 1, 1)
 };
 
-template <int D>
+template <int D, int NQ>
 struct TreeCfg {
+  static constexpr int kThreads = NQ == 1 ? 256 : 384;
   static constexpr int kChunks = D / 64;
   static constexpr int kTileBytes = kChunks * kTreeTile * 128;  // one K (or V) tile
   static constexpr int kKStages = D == 256 ? 3 : (D == 128 ? 6 : 8);
   static constexpr int kVStages = D == 256 ? 4 : (D == 128 ? 7 : 8);
   static constexpr int kSmem = (kKStages + kVStages) * kTileBytes + 1024;
-  // tensor memory columns: O [0, D), Q as bf16 pairs, the S / P buffers
+  // tensor memory columns, per row tile: O, Q as bf16 pairs, the S / P buffers
+  static constexpr int kSBuf = NQ == 2 ? (D == 128 ? 1 : 2) : (D == 256 ? 2 : 3);
   static constexpr int kQCol = D;
   static constexpr int kSCol = D + D / 2;
-  static constexpr int kSBuf = kSCol + 3 * kTreeTile <= 512 ? 3 : 2;
-  static constexpr int kTmemCols = kSCol + kSBuf * kTreeTile > 256 ? 512 : 256;
+  static constexpr int kRowCols = kSCol + kSBuf * kTreeTile;
+  static constexpr int kTmemCols = NQ * kRowCols > 256 ? 512 : 256;
+  static_assert(NQ * kRowCols <= 512, "tensor memory");
 };
 
 struct TreeShared {
   uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], v_fix[8];
-  uint64_t s_full[3], p_full[3], pv_done[3];
-  uint64_t q_ready, o_final, o_free;
+  uint64_t s_full[2][3], p_full[2][3], pv_done[2][3];  // per row tile
+  uint64_t q_ready[2], o_final[2], o_free[2];
   uint64_t drain;  // after a timeout: every MMA issued has completed
   uint32_t tmem_base;
   int abort_flag;
@@ -122,10 +130,10 @@ __device__ __forceinline__ bool next_item(const TreeSoftmaxParams& p, TreeCursor
 
 }  // namespace
 
-template <int D>
-__global__ void __launch_bounds__(kThreadsT, 1)
+template <int D, int NQ>
+__global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     tree_softmax_tc_kernel(const __grid_constant__ TreeMaps maps, TreeSoftmaxParams p) {
-  using C = TreeCfg<D>;
+  using C = TreeCfg<D, NQ>;
   constexpr int kSB = C::kSBuf;
   extern __shared__ uint8_t smem_raw[];
   __shared__ TreeShared sh;
@@ -133,7 +141,7 @@ __global__ void __launch_bounds__(kThreadsT, 1)
   uint8_t* Vs = Ks + C::kKStages * C::kTileBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
-  const int m0 = mt * kRowsT;
+  const int m0 = mt * (NQ * kRowsT);
 
   if (tid == 0) {
     sh.abort_flag = 0;
@@ -143,27 +151,30 @@ __global__ void __launch_bounds__(kThreadsT, 1)
     }
     for (int s = 0; s < C::kVStages; ++s) {
       tc::mbar_init(&sh.v_full[s], 1);
-      tc::mbar_init(&sh.v_empty[s], 2);  // the product and the zeroing warp
+      tc::mbar_init(&sh.v_empty[s], 2);  // the products and the zeroing warp
       tc::mbar_init(&sh.v_fix[s], 1);
     }
-    for (int b = 0; b < 3; ++b) {
-      tc::mbar_init(&sh.s_full[b], 1);
-      tc::mbar_init(&sh.p_full[b], kSmThreads);
-      tc::mbar_init(&sh.pv_done[b], 1);
+    for (int t = 0; t < NQ; ++t) {
+      for (int b = 0; b < kSB; ++b) {
+        tc::mbar_init(&sh.s_full[t][b], 1);
+        tc::mbar_init(&sh.p_full[t][b], kSmThreads);
+        tc::mbar_init(&sh.pv_done[t][b], 1);
+      }
+      tc::mbar_init(&sh.q_ready[t], kSmThreads);
+      tc::mbar_init(&sh.o_final[t], 1);
+      tc::mbar_init(&sh.o_free[t], kSmThreads);
     }
-    tc::mbar_init(&sh.q_ready, kSmThreads);
-    tc::mbar_init(&sh.o_final, 1);
-    tc::mbar_init(&sh.o_free, kSmThreads);
     tc::mbar_init(&sh.drain, 1);
     tc::fence_mbar_init();
   }
   if (warp == 1) tc::tmem_alloc(&sh.tmem_base, C::kTmemCols);
-  const TreeCursor span = tree_span<kThreadsT>(p, gang, sh.span);
+  pdl_wait();  // the plan
+  pdl_launch_next();
+  const TreeCursor span = tree_span<C::kThreads>(p, gang, sh.span);
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = sh.tmem_base;
-  const uint32_t tmem_o = tmem, tmem_q = tmem + C::kQCol, tmem_s = tmem + C::kSCol;
   TreeCursor cur = span;
   TreeItem it;
 
@@ -269,68 +280,80 @@ __global__ void __launch_bounds__(kThreadsT, 1)
       const uint64_t kdesc0 = tc::sdesc_sw128(tc::smem_u32(Ks), 16, 1024);
       const uint64_t vdesc0 = tc::sdesc_sw128(tc::smem_u32(Vs), kTreeTile * 128, 1024);
       bool ok = true;
-      int g = 0;              // running tile count
+      int g = 0;              // running tile count of the rings
+      int gt[2] = {0, 0};     // and of each row tile's buffers
+      int kt[2] = {0, 0};     // pieces of each row tile
       uint32_t fix_par = 0u;  // per V slot: parity of its next zeroed tile
-      for (int k = 0; ok && next_item(p, cur, m0, it); ++k) {
-        if (!tc::mbar_wait(&sh.q_ready, (uint32_t)k & 1u, &sh.abort_flag)) {
-          ok = false;
-          break;
-        }
-        // S_j = Q K_j^T into S buffer (g + j) % kSB
-        auto issue_s = [&](int j) -> bool {
-          const int gg = g + j, st = gg % C::kKStages, sb = gg % kSB;
-          if (!tc::mbar_wait(&sh.k_full[st], (uint32_t)(gg / C::kKStages) & 1u, &sh.abort_flag))
+      while (ok && next_item(p, cur, m0, it)) {
+        // row tiles with rows of this item: the first, or both
+        const int nt = NQ == 2 && m0 + kRowsT < it.nodes * p.G ? 2 : 1;
+        for (int t = 0; t < nt && ok; ++t)
+          ok = tc::mbar_wait(&sh.q_ready[t], (uint32_t)kt[t] & 1u, &sh.abort_flag);
+        if (!ok) break;
+        // S_j = Q K_j^T of row tile t
+        auto issue_s = [&](int t, int j) -> bool {
+          const int st = (g + j) % C::kKStages, sb = (gt[t] + j) % kSB;
+          if (t == 0 && !tc::mbar_wait(&sh.k_full[st], (uint32_t)((g + j) / C::kKStages) & 1u,
+                                       &sh.abort_flag))
             return false;
           tc::fence_after_sync();
+          const uint32_t base = tmem + t * C::kRowCols;
           const uint64_t kd = kdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
-            tc::mma_bf16_ts(tmem_s + sb * kTreeTile, tmem_q + kk * 8,
+            tc::mma_bf16_ts(base + C::kSCol + sb * kTreeTile, base + C::kQCol + kk * 8,
                             kd + (uint64_t)(((kk >> 2) * (kTreeTile * 128) + (kk & 3) * 32) >> 4),
                             id_s, kk > 0 ? 1u : 0u);
-          tc::mma_commit(&sh.s_full[sb]);
-          tc::mma_commit(&sh.k_empty[st]);
+          tc::mma_commit(&sh.s_full[t][sb]);
+          if (t == nt - 1) tc::mma_commit(&sh.k_empty[st]);
           return true;
         };
-        auto issue_pv = [&](int j) -> bool {
-          const int gg = g + j, st = gg % C::kVStages, pb = gg % kSB;
-          if (!tc::mbar_wait(&sh.p_full[pb], (uint32_t)(gg / kSB) & 1u, &sh.abort_flag))
+        auto issue_pv = [&](int t, int j) -> bool {
+          const int st = (g + j) % C::kVStages, pb = (gt[t] + j) % kSB;
+          if (!tc::mbar_wait(&sh.p_full[t][pb], (uint32_t)((gt[t] + j) / kSB) & 1u,
+                             &sh.abort_flag))
             return false;
           // the first product of a piece overwrites O: the previous one's must be out
-          if (j == 0 && k > 0 &&
-              !tc::mbar_wait(&sh.o_free, (uint32_t)(k - 1) & 1u, &sh.abort_flag))
+          if (j == 0 && kt[t] > 0 &&
+              !tc::mbar_wait(&sh.o_free[t], (uint32_t)(kt[t] - 1) & 1u, &sh.abort_flag))
             return false;
-          if (!tc::mbar_wait(&sh.v_full[st], (uint32_t)(gg / C::kVStages) & 1u, &sh.abort_flag))
-            return false;
-          if (it.valid(j) < kTreeTile) {
-            if (!tc::mbar_wait(&sh.v_fix[st], (fix_par >> st) & 1u, &sh.abort_flag)) return false;
-            fix_par ^= 1u << st;
+          if (t == 0) {
+            if (!tc::mbar_wait(&sh.v_full[st], (uint32_t)((g + j) / C::kVStages) & 1u,
+                               &sh.abort_flag))
+              return false;
+            if (it.valid(j) < kTreeTile) {
+              if (!tc::mbar_wait(&sh.v_fix[st], (fix_par >> st) & 1u, &sh.abort_flag)) return false;
+              fix_par ^= 1u << st;
+            }
           }
           tc::fence_after_sync();
+          const uint32_t base = tmem + t * C::kRowCols;
           const uint64_t vd = vdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
 #pragma unroll
           for (int kk = 0; kk < kTreeTile / 16; ++kk)
-            tc::mma_bf16_ts(tmem_o, tmem_s + pb * kTreeTile + kk * 8,
+            tc::mma_bf16_ts(base, base + C::kSCol + pb * kTreeTile + kk * 8,
                             vd + (uint64_t)(kk * (2048 >> 4)), id_o, (j > 0 || kk > 0) ? 1u : 0u);
-          tc::mma_commit(&sh.pv_done[pb]);
-          tc::mma_commit(&sh.v_empty[st]);
+          tc::mma_commit(&sh.pv_done[t][pb]);
+          if (t == nt - 1) tc::mma_commit(&sh.v_empty[st]);
           return true;
         };
         // MMAs of one thread execute in issue order, so an S buffer can be
-        // rewritten once the product that reads its probabilities was issued.
-        // Three buffers: S0 S1 S2 PV0 S3 PV1 ...; two: S0 S1 PV0 S2 PV1 ...
+        // rewritten once the product that reads its probabilities was issued:
+        // kSB scores ahead, then P V_j and S_j+kSB in turn, row tile by row tile.
         const int n = it.tiles;
-        for (int j = 0; j < 2 && j < n && ok; ++j) ok = issue_s(j);
-        for (int j = 0; j < n && ok; ++j) {
-          if (kSB == 3) {
-            if (j + 2 < n) ok = issue_s(j + 2);
-            if (ok) ok = issue_pv(j);
-          } else {
-            ok = issue_pv(j);
-            if (ok && j + 2 < n) ok = issue_s(j + 2);
+        for (int j = 0; j < kSB && j < n && ok; ++j)
+          for (int t = 0; t < nt && ok; ++t) ok = issue_s(t, j);
+        for (int j = 0; j < n && ok; ++j)
+          for (int t = 0; t < nt && ok; ++t) {
+            ok = issue_pv(t, j);
+            if (ok && j + kSB < n) ok = issue_s(t, j + kSB);
           }
+        if (!ok) break;
+        for (int t = 0; t < nt; ++t) {
+          tc::mma_commit(&sh.o_final[t]);
+          gt[t] += n;
+          ++kt[t];
         }
-        if (ok) tc::mma_commit(&sh.o_final);
         g += n;
       }
       if (!ok) give_up(sh, p.dev_status);
@@ -342,9 +365,12 @@ __global__ void __launch_bounds__(kThreadsT, 1)
     __syncwarp();
   } else {
     // ------------------------------------------------------------ softmax warps
-    const int quarter = warp & 3;
-    const int row = quarter * 32 + lane, m = m0 + row;
+    const int quarter = warp & 3, t = warp >= 8 ? 1 : 0;  // of row tile t
+    const int row = quarter * 32 + lane, m = m0 + t * kRowsT + row;
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const uint32_t tmem_o = tmem + t * C::kRowCols;
+    const uint32_t tmem_q = tmem_o + C::kQCol, tmem_s = tmem_o + C::kSCol;
+    const int mt0 = m0 + t * kRowsT;
     const int node = m / p.G, head = m - node * p.G;
 
     // Q row into tensor memory as bf16 pairs; rows past the tree's are zero
@@ -374,12 +400,12 @@ __global__ void __launch_bounds__(kThreadsT, 1)
         tc::tmem_st_wait();
       }
       tc::fence_before_sync();
-      tc::mbar_arrive(&sh.q_ready);
+      tc::mbar_arrive(&sh.q_ready[t]);
     };
 
     bool ok = true;
     int g = 0;  // running tile count
-    bool have = next_item(p, cur, m0, it);
+    bool have = next_item(p, cur, mt0, it);
     if (have) load_q(it);
     for (int k = 0; have; ++k) {
       const bool live = m < it.nodes * p.G;
@@ -388,12 +414,12 @@ __global__ void __launch_bounds__(kThreadsT, 1)
       float m_run = -INFINITY, l_run = 0.f;
       for (int j = 0; j < it.tiles; ++j) {
         const int gg = g + j, sb = gg % kSB;
-        if (!warp_wait_t(&sh.s_full[sb], (uint32_t)(gg / kSB) & 1u, &sh.abort_flag)) {
+        if (!warp_wait_t(&sh.s_full[t][sb], (uint32_t)(gg / kSB) & 1u, &sh.abort_flag)) {
           ok = false;
           break;
         }
         if (!warp_live) {  // nobody reads these rows' output
-          tc::mbar_arrive(&sh.p_full[sb]);
+          tc::mbar_arrive(&sh.p_full[t][sb]);
           continue;
         }
         tc::fence_after_sync();
@@ -439,7 +465,7 @@ __global__ void __launch_bounds__(kThreadsT, 1)
         l_run = j == 0 ? sum0 + sum1 : l_run * corr + (sum0 + sum1);
         if (move && j >= 1) {  // rescale O, the previous tile's product done
           const int pb = (gg - 1) % kSB;
-          if (!warp_wait_t(&sh.pv_done[pb], (uint32_t)((gg - 1) / kSB) & 1u, &sh.abort_flag)) {
+          if (!warp_wait_t(&sh.pv_done[t][pb], (uint32_t)((gg - 1) / kSB) & 1u, &sh.abort_flag)) {
             ok = false;
             break;
           }
@@ -460,15 +486,15 @@ __global__ void __launch_bounds__(kThreadsT, 1)
           tc::tmem_st16(sbuf + c, *reinterpret_cast<uint32_t(*)[16]>(&pk[c]));
         tc::tmem_st_wait();
         tc::fence_before_sync();
-        tc::mbar_arrive(&sh.p_full[sb]);
+        tc::mbar_arrive(&sh.p_full[t][sb]);
       }
       g += it.tiles;
       if (ok && aborted_t(sh)) ok = false;
       // the next piece's queries: every S product of this one has completed
       TreeItem nx = it;
-      const bool more = ok && next_item(p, cur, m0, nx);
+      const bool more = ok && next_item(p, cur, mt0, nx);
       if (more) load_q(nx);
-      if (ok && !warp_wait_t(&sh.o_final, (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
+      if (ok && !warp_wait_t(&sh.o_final[t], (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
       if (!ok) break;
       if (warp_live) {
         tc::fence_after_sync();
@@ -476,7 +502,8 @@ __global__ void __launch_bounds__(kThreadsT, 1)
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
         const float l2 = l_run > 0.f ? m_run + log2f(l_run) : -INFINITY;
         const size_t orow = ((size_t)it.w.r * p.N + node) * p.Hq + it.w.kvh * p.G + head;
-        const size_t prow = ((size_t)blockIdx.x * 2 + it.w.slot()) * kRowsT + row;
+        const size_t prow =
+            ((size_t)blockIdx.x * 2 + it.w.slot()) * (NQ * kRowsT) + t * kRowsT + row;
 #pragma unroll 1
         for (int c = 0; c < D; c += 16) {
           uint32_t o[16];
@@ -509,7 +536,7 @@ __global__ void __launch_bounds__(kThreadsT, 1)
         }
       }
       tc::fence_before_sync();
-      tc::mbar_arrive(&sh.o_free);
+      tc::mbar_arrive(&sh.o_free[t]);
       have = more;
       it = nx;
     }
@@ -553,9 +580,9 @@ bool encode(CUtensorMap* m, const void* ptr, const cuuint64_t (&dims)[4],
          CUDA_SUCCESS;
 }
 
-template <int D>
+template <int D, int NQ>
 cudaError_t launch_tc_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
-  using C = TreeCfg<D>;
+  using C = TreeCfg<D, NQ>;
   TreeMaps maps;
   const cuuint64_t row = D * 2;
   {
@@ -576,22 +603,23 @@ cudaError_t launch_tc_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
         !encode(&maps.vpool, none ? p.v_blk : p.v_pool, dims, str, rows, 1))
       return cudaErrorInvalidValue;
   }
-  cudaError_t e = cudaFuncSetAttribute(tree_softmax_tc_kernel<D>,
+  cudaError_t e = cudaFuncSetAttribute(tree_softmax_tc_kernel<D, NQ>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (e != cudaSuccess) return e;
-  tree_softmax_tc_kernel<D>
-      <<<(unsigned)(p.gangs * p.row_tiles), kThreadsT, C::kSmem, stream>>>(maps, p);
+  e = pdl_launch(tree_softmax_tc_kernel<D, NQ>, dim3((unsigned)(p.gangs * p.row_tiles)),
+                 C::kThreads, C::kSmem, stream, true, 1, maps, p);
   note_launches(1);
-  return cudaGetLastError();
+  return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  const bool two = p.tile_rows == 2 * kRowsT;
   switch (p.D) {
-    case 64: return launch_tc_d<64>(p, stream);
-    case 128: return launch_tc_d<128>(p, stream);
-    case 256: return launch_tc_d<256>(p, stream);
+    case 64: return two ? launch_tc_d<64, 2>(p, stream) : launch_tc_d<64, 1>(p, stream);
+    case 128: return two ? launch_tc_d<128, 2>(p, stream) : launch_tc_d<128, 1>(p, stream);
+    case 256: return launch_tc_d<256, 1>(p, stream);
     default: return cudaErrorInvalidValue;
   }
 }

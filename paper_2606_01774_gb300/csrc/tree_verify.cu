@@ -1,11 +1,11 @@
 // Verification of drafted trees against the target's distributions.
 //
-//   tree_rows_kernel  log-sum-exp and argmax of every row that has children, in
-//                     one pass over the logits: CTAs (chunk, row) leave a
+//   tree_rows_kernel  log-sum-exp (and argmax) of every row that has children,
+//                     in one pass over the logits: CTAs (chunk, row) leave a
 //                     partial {max, sum, argmax} each
-//   tree_walk_kernel  a CTA per request joins the partials, writes the drafted
-//                     nodes' log-probabilities, walks the tree and draws the
-//                     next token
+//   tree_walk_kernel  a cluster per request joins the partials, writes the
+//                     drafted nodes' log-probabilities, walks the tree and
+//                     draws the next token
 //
 // With siblings drawn independently from q, a rejection replaces the target by
 // the normalised positive part of (target - q).  Iterating that telescopes:
@@ -14,8 +14,16 @@
 // stored, and a mass is only summed when another sibling is still to be tried.
 // With fixed drafts the residual is p without the rejected tokens.
 // The next token is the argmax of w / noise (noise ~ Exp(1) samples w).
+//
+// Bound by the logits' bytes on many rows and by latency on few.  The walk
+// itself needs a dozen numbers per node, gathered by a thread each before it
+// starts; what is long in it, a pass over one row, is cut over the cluster's
+// CTAs, which all take the same decisions from the same numbers and exchange
+// sums and maxima through distributed shared memory, in rank order.
 #include "common.cuh"
 #include "kernels.h"
+#include "pdl.cuh"
+#include "tc.cuh"
 #include "tree.cuh"
 
 namespace flare {
@@ -23,39 +31,9 @@ namespace flare {
 namespace {
 
 constexpr int kRowThreads = 256;
-constexpr int kWalkThreads = 1024;
+constexpr int kWalkThreads = 512;
+constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
-
-// Calls f(x, value) for the elements [lo, hi) of a row that may start at any
-// element: 16-byte loads over the aligned middle, kIn of them in flight per
-// thread, single elements at both ends.
-template <typename T, int THREADS, typename F>
-__device__ __forceinline__ void for_row(const T* row, int lo, int hi, F&& f) {
-  constexpr int kE = 16 / sizeof(T), kIn = 4;
-  const int tid = threadIdx.x;
-  const int skew = (int)(((uintptr_t)(row + lo) & 15u) / sizeof(T));
-  const int a = min(hi, skew ? lo + kE - skew : lo);  // first aligned element
-  const int nv = (hi - a) / kE;
-  if (tid < a - lo) f(lo + tid, to_f32(row[lo + tid]));
-  const int tail = a + nv * kE;
-  if (tid < hi - tail) f(tail + tid, to_f32(row[tail + tid]));
-  const uint4* v = reinterpret_cast<const uint4*>(row + a);
-  for (int i0 = tid; i0 < nv; i0 += kIn * THREADS) {
-    uint4 x[kIn];
-#pragma unroll
-    for (int u = 0; u < kIn; ++u)
-      if (i0 + u * THREADS < nv) x[u] = v[i0 + u * THREADS];
-#pragma unroll
-    for (int u = 0; u < kIn; ++u) {
-      if (i0 + u * THREADS < nv) {
-        const T* e = reinterpret_cast<const T*>(&x[u]);
-        const int base = a + (i0 + u * THREADS) * kE;
-#pragma unroll
-        for (int k = 0; k < kE; ++k) f(base + k, to_f32(e[k]));
-      }
-    }
-  }
-}
 
 // The better of two (value, index) candidates: the greater value, the lower
 // index among equals.
@@ -85,37 +63,97 @@ __device__ __forceinline__ float4 join_stats(float4 a, float4 b) {
 
 }  // namespace
 
-template <typename T>
+// A chunk of a row: 16-byte loads over its aligned middle, eight of them in
+// flight per thread, and single elements at both ends (a row may start at any
+// element).  The running maximum moves once per batch, not per element.
+template <typename T, bool GREEDY>
 __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams p) {
+  constexpr int kE = 16 / sizeof(T), kIn = 8;
   __shared__ float4 red[kRowThreads / 32];
-  __shared__ int inner;
+  pdl_launch_next();
   const int row = blockIdx.y, r = row / p.N, i = row - r * p.N, tid = threadIdx.x;
-  const int n = p.node_len[r];
-  if (n < 0 || n > p.N || i >= n) return;  // a wrong length is flagged by the walk
-  if (tid < 32) {
+  {  // rows without children are read only where a walk ends
     const int32_t* par = p.parent + (size_t)r * p.N;
-    const bool kid = (tid < n && par[tid] == i) || (tid + 32 < n && par[tid + 32] == i);
-    const bool any = __any_sync(0xffffffffu, kid);
-    if (tid == 0) inner = any;
+    const int lane = tid & 31;
+    // both in one round trip, unused nodes' entries (any value) masked after it
+    const int n = p.node_len[r];
+    const int p0 = lane < p.N ? par[lane] : -1, p1 = lane + 32 < p.N ? par[lane + 32] : -1;
+    const bool kid = (lane < n && p0 == i) || (lane + 32 < n && p1 == i);
+    // the same in every warp; a wrong length is flagged by the walk
+    if (n > p.N || i >= n || !__any_sync(0xffffffffu, kid)) return;
   }
-  __syncthreads();
-  if (!inner) return;
   const int lo = blockIdx.x * p.chunk, hi = min(p.V, lo + p.chunk);
   const T* x = static_cast<const T*>(p.logits) + (size_t)row * p.V;
   const float scale = p.inv_temp * kLog2e;
-  // running maximum of the raw logits, moved lazily: sum of 2^(scale (x - m))
-  float m = -INFINITY, s = 0.f;
+  float m = -INFINITY, s = 0.f;  // maximum of the raw logits, sum of 2^(scale (x - m))
   int best = p.V;
-  for_row<T, kRowThreads>(x, lo, hi, [&](int at, float v) {
+  auto one = [&](int at) {
+    const float v = to_f32(x[at]);
     if (v > m) {
-      s *= exp2f(scale * (m - v));
+      s *= tc::ex2(scale * (m - v));
       m = v;
       best = at;
-    } else if (v == m && at < best) {
-      best = at;
+    } else if (GREEDY && v == m) {
+      best = min(best, at);
     }
-    if (v != -INFINITY) s += exp2f(scale * (v - m));  // a NaN makes the sum one
-  });
+    if (v != -INFINITY) s += tc::ex2(scale * (v - m));  // a NaN makes the sum one
+  };
+  const int skew = (int)(((uintptr_t)(x + lo) & 15u) / sizeof(T));
+  const int a = min(hi, skew ? lo + kE - skew : lo);  // first aligned element
+  const int nv = (hi - a) / kE, tail = a + nv * kE;
+  if (tid < a - lo) one(lo + tid);
+  const uint4* vec = reinterpret_cast<const uint4*>(x + a);
+  for (int i0 = tid; i0 < nv; i0 += kIn * kRowThreads) {
+    uint4 w[kIn];
+#pragma unroll
+    for (int u = 0; u < kIn; ++u)
+      if (i0 + u * kRowThreads < nv) w[u] = __ldcs(vec + i0 + u * kRowThreads);
+#pragma unroll
+    for (int u = 0; u < kIn; ++u) {
+      if (i0 + u * kRowThreads >= nv) continue;
+      float v[kE];
+      if constexpr (sizeof(T) == 2) {
+        const uint32_t h[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[2 * k] = __uint_as_float(h[k] << 16);
+          v[2 * k + 1] = __uint_as_float(h[k] & 0xffff0000u);
+        }
+      } else {
+        v[0] = __uint_as_float(w[u].x);
+        v[1] = __uint_as_float(w[u].y);
+        v[2] = __uint_as_float(w[u].z);
+        v[3] = __uint_as_float(w[u].w);
+      }
+      float bm = v[0];
+#pragma unroll
+      for (int k = 1; k < kE; ++k) bm = fmaxf(bm, v[k]);
+      if (bm > m) {
+        s *= tc::ex2(scale * (m - bm));
+        m = bm;
+        if constexpr (GREEDY) {
+          const int base = a + (i0 + u * kRowThreads) * kE;
+#pragma unroll
+          for (int k = kE - 1; k >= 0; --k)
+            if (v[k] == bm) best = base + k;
+        }
+      } else if (GREEDY && bm == m) {  // equal to an element of a scalar end further right
+        const int base = a + (i0 + u * kRowThreads) * kE;
+#pragma unroll
+        for (int k = kE - 1; k >= 0; --k)
+          if (v[k] == bm) best = min(best, base + k);
+      }
+      const float neg = m == -INFINITY ? 0.f : -scale * m;
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int k = 0; k < kE; k += 2) {
+        s0 += tc::ex2(fmaf(v[k], scale, neg));
+        s1 += tc::ex2(fmaf(v[k + 1], scale, neg));
+      }
+      s += s0 + s1;
+    }
+  }
+  if (tid < hi - tail) one(tail + tid);
   float4 st = make_float4(m * p.inv_temp, s, (float)best, 0.f);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -134,73 +172,117 @@ __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams
   }
 }
 
+namespace {
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t x;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(x));
+  return x;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t x;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(x));
+  return x;
+}
+// Every thread of the cluster; orders shared-memory writes before remote reads.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A 32-bit word of shared memory of the cluster's CTA `rank`.
+__device__ __forceinline__ uint32_t cluster_word(const void* mine, uint32_t rank) {
+  uint32_t at, x;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+               : "=r"(at)
+               : "r"(tc::smem_u32(mine)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+
+struct WalkShared {
+  int par[kMaxNodes], tok[kMaxNodes], line[kMaxNodes], best_of[kMaxNodes], gone[kMaxNodes];
+  unsigned long long kids[kMaxNodes];
+  float uni[kMaxNodes], logp[kMaxNodes], lse[kMaxNodes], q[kMaxNodes];
+  float red_v[kWalkThreads / 32];
+  int red_i[kWalkThreads / 32];
+  int tree_ok;
+  // the walk: the node it stands at, its path, the residual there
+  int cur, len, more, n_gone;
+  unsigned long long left;  // children still to be tried
+  float c, m;
+  // this CTA's share of a pass over a row, in two buffers: a CTA is at most
+  // one pass ahead of another that still reads its last share
+  float part_v[2];
+  int part_i[2], part_odd[2];
+};
+
+}  // namespace
+
 template <typename T>
 __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParams p) {
   constexpr int kWarps = kWalkThreads / 32;
-  __shared__ int par[kMaxNodes], tok[kMaxNodes], line[kMaxNodes], best_of[kMaxNodes];
-  __shared__ float uni[kMaxNodes], logp[kMaxNodes], lse[kMaxNodes];
-  __shared__ float red_v[kWarps];
-  __shared__ int red_i[kWarps];
-  __shared__ int tree_ok, inner_lo, inner_hi;
-  __shared__ int s_cur, s_len, s_next, s_more, s_gone;
-  __shared__ int gone[kMaxNodes];
-  __shared__ float s_c, s_m;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  __shared__ WalkShared sh;
+  const uint32_t rank = cluster_rank(), ranks = cluster_size();
+  const int r = blockIdx.x / ranks, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n = p.node_len[r];
+  // every CTA of a cluster comes to the same answer at each of these exits
   if (n < 0 || n > p.N) {
-    if (tid == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);
+    if (tid == 0 && rank == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);
+    pdl_wait();
     return;
   }
   const bool sample = !p.greedy;
   if (tid < 32) {
     int p0, p1;
     const bool ok = warp_load_tree(p.parent + (size_t)r * p.N, n, p0, p1);
-    par[tid] = p0;
-    par[tid + 32] = p1;
-    if (tid == 0) {
-      tree_ok = ok;
-      inner_lo = inner_hi = 0;
-      s_cur = 0;
-      s_len = 1;
-      s_c = 0.f;
-      s_m = 1.f;
-      s_gone = 0;
-      s_next = 1;
-      line[0] = 0;
+    sh.par[tid] = p0;
+    sh.par[tid + 32] = p1;
+    sh.kids[tid] = sh.kids[tid + 32] = 0ull;
+    __syncwarp();
+    if (ok) {
+      if (p0 >= 0) atomicOr(&sh.kids[p0], 1ull << tid);
+      if (p1 >= 0) atomicOr(&sh.kids[p1], 1ull << (tid + 32));
     }
+    if (tid == 0) sh.tree_ok = ok;
+  } else if (tid >= 64 && tid < 64 + kMaxNodes) {
+    const int i = tid - 64;
+    const bool drafted = i > 0 && i < n;
+    sh.tok[i] = drafted ? p.token[(size_t)r * p.N + i] : 0;
+    sh.uni[i] = drafted && sample ? p.uniform[(size_t)r * p.N + i] : 0.f;
   }
   __syncthreads();
-  int bad = tree_ok ? 0 : FLARE_DEV_BAD_TREE;
-  if (tid < kMaxNodes && tid > 0 && tid < n) {
-    const int x = p.token[(size_t)r * p.N + tid];
-    tok[tid] = x;
-    if (x < 0 || x >= p.V) bad |= FLARE_DEV_BAD_TREE;
-    if (sample) uni[tid] = p.uniform[(size_t)r * p.N + tid];
-  }
+  int bad = sh.tree_ok ? 0 : FLARE_DEV_BAD_TREE;
+  if (tid < kMaxNodes && (sh.tok[tid] < 0 || sh.tok[tid] >= p.V)) bad = FLARE_DEV_BAD_TREE;
   if (__syncthreads_or(bad)) {
-    if (bad && (tid == 0 || tree_ok)) flag(p.dev_status, bad);
+    if (tid == 0 && rank == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);
+    pdl_wait();
     return;
   }
   if (n == 0) {
-    if (tid < p.N) {
+    if (rank == 0 && tid < p.N) {
       p.path[(size_t)r * p.N + tid] = -1;
       p.node_logp[(size_t)r * p.N + tid] = 0.f;
     }
-    if (tid == 0) {
+    if (rank == 0 && tid == 0) {
       p.path_len[r] = 0;
       p.next_token[r] = -1;
     }
+    pdl_wait();
     return;
   }
-  if (tid > 0 && tid < n) {  // which nodes have children
-    const int a = par[tid];
-    atomicOr(a < 32 ? &inner_lo : &inner_hi, 1 << (a & 31));
+  const T* rows = static_cast<const T*>(p.logits) + (size_t)r * p.N * p.V;
+  const float* drafts =
+      sample && p.draft_probs ? p.draft_probs + (size_t)r * p.N * p.V : nullptr;
+  float x_tok = 0.f;  // the drafted token's logit, and its probability for the drafter
+  if (tid > 0 && tid < n) {
+    const size_t at = (size_t)sh.par[tid] * p.V + sh.tok[tid];
+    x_tok = to_f32(rows[at]) * p.inv_temp;
+    sh.q[tid] = drafts ? drafts[at] : 1.f;
   }
-  __syncthreads();
-  auto is_inner = [&](int i) { return ((i < 32 ? inner_lo : inner_hi) >> (i & 31)) & 1; };
+  pdl_wait();  // the row statistics
   // a warp per row with children: its log-sum-exp and argmax
   for (int i = warp; i < n; i += kWarps) {
-    if (!is_inner(i)) continue;
+    if (!sh.kids[i]) continue;
     float4 st = make_float4(-INFINITY, 0.f, (float)p.V, 0.f);
     for (int c = lane; c < p.n_chunks; c += 32)
       st = join_stats(st, p.stats[((size_t)r * p.N + i) * p.n_chunks + c]);
@@ -213,160 +295,217 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
       st = join_stats(st, y);
     }
     if (lane == 0) {
-      lse[i] = st.x + logf(st.y);
-      best_of[i] = (int)st.z;
-      if (!(fabsf(lse[i]) < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
+      sh.lse[i] = st.x + logf(st.y);
+      sh.best_of[i] = (int)st.z;
+      if (!(fabsf(sh.lse[i]) < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
     }
   }
   if (__syncthreads_or(bad)) {
-    if (bad) flag(p.dev_status, bad);
+    if (tid == 0 && rank == 0) flag(p.dev_status, FLARE_DEV_BAD_LOGITS);
     return;
   }
-  const T* rows = static_cast<const T*>(p.logits) + (size_t)r * p.N * p.V;
-  const float* drafts =
-      sample && p.draft_probs ? p.draft_probs + (size_t)r * p.N * p.V : nullptr;
-  if (tid < n)
-    logp[tid] = tid == 0 ? 0.f
-                         : to_f32(rows[(size_t)par[tid] * p.V + tok[tid]]) * p.inv_temp - lse[par[tid]];
+  if (tid < kMaxNodes) sh.logp[tid] = tid > 0 && tid < n ? x_tok - sh.lse[sh.par[tid]] : 0.f;
+  if (tid == 0) {
+    sh.cur = 0;
+    sh.len = 1;
+    sh.line[0] = 0;
+    sh.left = sh.kids[0];
+    sh.c = 0.f;
+    sh.m = 1.f;
+    sh.n_gone = 0;
+  }
   __syncthreads();
 
-  // The walk: thread 0 tries siblings until it needs a mass (then the CTA sums
-  // it) or is done.
+  const float scale = p.inv_temp * kLog2e;
+  const int lo = (int)((long long)p.V * rank / ranks), hi = (int)((long long)p.V * (rank + 1) / ranks);
+  // Calls f(x, ...) for this CTA's tokens of a row, kIn of a thread's loads in
+  // flight: consecutive threads on consecutive tokens, whatever the alignment.
+  constexpr int kIn = 8;
+  int pass = 0;
+
+  // The walk: thread 0 tries children until it needs a mass (then the cluster
+  // sums it) or is done.
   while (true) {
     if (tid == 0) {
-      int cur = s_cur, len = s_len, more = 0, i = s_next;
-      float c = s_c, m = s_m;
-      for (; i < n; ++i) {
-        if (par[i] != cur) continue;
+      int cur = sh.cur, len = sh.len, more = 0;
+      unsigned long long left = sh.left;
+      float c = sh.c, m = sh.m;
+      while (left) {
+        const int i = __ffsll((long long)left) - 1;
+        left &= left - 1;
         bool ok;
         if (!sample) {
-          ok = tok[i] == best_of[cur];
+          ok = sh.tok[i] == sh.best_of[cur];
         } else {
-          const float px = expf(logp[i]);
+          const float px = expf(sh.logp[i]);
           if (drafts) {
-            const float q = drafts[(size_t)cur * p.V + tok[i]];
-            ok = uni[i] * q * m < fmaxf(px - c * q, 0.f);
+            ok = sh.uni[i] * sh.q[i] * m < fmaxf(px - c * sh.q[i], 0.f);
             if (!ok) {
               c += m;
-              bool another = false;
-              for (int e = i + 1; e < n; ++e) another = another || par[e] == cur;
-              if (another) {  // its mass is needed
+              if (left) {  // another sibling: the residual's mass is needed
                 more = 1;
-                ++i;
                 break;
               }
             }
           } else {
             bool was = false;
-            for (int e = 0; e < s_gone; ++e) was = was || gone[e] == tok[i];
-            ok = !was && uni[i] * m < px;
+            for (int e = 0; e < sh.n_gone; ++e) was = was || sh.gone[e] == sh.tok[i];
+            ok = !was && sh.uni[i] * m < px;
             if (!ok && !was) {
-              gone[s_gone++] = tok[i];
+              sh.gone[sh.n_gone++] = sh.tok[i];
               m = fmaxf(m - px, 0.f);
             }
           }
         }
         if (ok) {
           cur = i;
-          line[len++] = i;
+          sh.line[len++] = i;
+          left = sh.kids[i];
           c = 0.f;
           m = 1.f;
-          s_gone = 0;
+          sh.n_gone = 0;
         }
       }
-      s_cur = cur;
-      s_len = len;
-      s_next = i;
-      s_c = c;
-      s_m = m;
-      s_more = more;
+      sh.cur = cur;
+      sh.len = len;
+      sh.left = left;
+      sh.c = c;
+      sh.m = m;
+      sh.more = more;
     }
     __syncthreads();
-    if (!s_more) break;
-    const T* x = rows + (size_t)s_cur * p.V;
-    const float* q = drafts + (size_t)s_cur * p.V;
-    const float c = s_c, shift = lse[s_cur] * kLog2e, scale = p.inv_temp * kLog2e;
+    if (!sh.more) break;
+    const T* x = rows + (size_t)sh.cur * p.V;
+    const float* q = drafts + (size_t)sh.cur * p.V;
+    const float c = sh.c, shift = sh.lse[sh.cur] * kLog2e;
     float sum = 0.f;
-    for_row<T, kWalkThreads>(x, 0, p.V, [&](int at, float v) {
-      sum += fmaxf(exp2f(v * scale - shift) - c * q[at], 0.f);
-    });
-    sum = warp_sum(sum);
-    if (lane == 0) red_v[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-      float m = 0.f;
-      for (int w = 0; w < kWarps; ++w) m += red_v[w];
-      s_m = m;
+    for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
+      float xv[kIn], qv[kIn];
+#pragma unroll
+      for (int u = 0; u < kIn; ++u) {
+        const int t = t0 + u * kWalkThreads;
+        xv[u] = t < hi ? to_f32(x[t]) : -INFINITY;
+        qv[u] = t < hi ? q[t] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kIn; ++u) sum += fmaxf(exp2f(xv[u] * scale - shift) - c * qv[u], 0.f);
     }
+    sum = warp_sum(sum);
+    if (lane == 0) sh.red_v[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+      const float m = warp_sum(lane < kWarps ? sh.red_v[lane] : 0.f);
+      if (lane == 0) sh.part_v[pass & 1] = m;
+    }
+    cluster_sync();
+    if (warp == 0) {
+      const float m = warp_sum(
+          lane < (int)ranks ? __uint_as_float(cluster_word(&sh.part_v[pass & 1], lane)) : 0.f);
+      if (lane == 0) sh.m = m;
+    }
+    ++pass;
     __syncthreads();
   }
 
   // The next token, from the last accepted node's row.
-  const int cur = s_cur;
-  int next = 0;
-  int odd = 0;
-  if (!sample && is_inner(cur)) {
-    next = best_of[cur];
+  const int cur = sh.cur;
+  int next = 0, odd = 0;
+  if (!sample && sh.kids[cur]) {
+    next = sh.best_of[cur];
   } else {
     const T* x = rows + (size_t)cur * p.V;
     const float* noise = sample ? p.noise + (size_t)r * p.V : nullptr;
-    const float scale = p.inv_temp * kLog2e;
-    float c = drafts ? s_c : 0.f;
-    int ng = s_gone;
+    float c = drafts ? sh.c : 0.f;
+    int ng = sh.n_gone;
     while (true) {
+      const float* q = c > 0.f ? drafts + (size_t)cur * p.V : nullptr;
+      const float shift = q ? sh.lse[cur] * kLog2e : 0.f;
       float v0 = -INFINITY;
       int i0 = p.V;
-      if (!sample) {
-        for_row<T, kWalkThreads>(x, 0, p.V, [&](int at, float v) {
-          odd |= !(v < INFINITY);
-          take_best(v0, i0, v, at);
-        });
-      } else if (c > 0.f) {
-        const float* q = drafts + (size_t)cur * p.V;
-        const float shift = lse[cur] * kLog2e;
-        for_row<T, kWalkThreads>(x, 0, p.V, [&](int at, float v) {
-          const float w = exp2f(v * scale - shift) - c * q[at];
-          if (w > 0.f) take_best(v0, i0, w / noise[at], at);
-        });
-      } else {  // the whole row: in logarithms, so that no normaliser is needed
-        for_row<T, kWalkThreads>(x, 0, p.V, [&](int at, float v) {
-          odd |= !(v < INFINITY);
-          bool out = v == -INFINITY;
-          for (int e = 0; e < ng; ++e) out = out || gone[e] == at;
-          if (!out) take_best(v0, i0, v * scale - log2f(noise[at]), at);
-        });
+      for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
+        float xv[kIn], ev[kIn], qv[kIn];
+#pragma unroll
+        for (int u = 0; u < kIn; ++u) {
+          const int t = t0 + u * kWalkThreads;
+          xv[u] = t < hi ? to_f32(x[t]) : -INFINITY;
+          ev[u] = noise && t < hi ? noise[t] : 1.f;
+          qv[u] = q && t < hi ? q[t] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kIn; ++u) {
+          const int t = t0 + u * kWalkThreads;
+          odd |= !(xv[u] < INFINITY);
+          float v;
+          bool out = xv[u] == -INFINITY;
+          if (!sample) {
+            v = xv[u];
+          } else if (q) {
+            const float w = exp2f(xv[u] * scale - shift) - c * qv[u];
+            out = out || !(w > 0.f);
+            v = w / ev[u];
+          } else {  // in logarithms: no normaliser is needed
+            for (int e = 0; e < ng; ++e) out = out || sh.gone[e] == t;
+            v = xv[u] * scale - log2f(ev[u]);
+          }
+          if (!out) take_best(v0, i0, v, t);
+        }
       }
       warp_best(v0, i0);
       if (lane == 0) {
-        red_v[warp] = v0;
-        red_i[warp] = i0;
+        sh.red_v[warp] = v0;
+        sh.red_i[warp] = i0;
       }
-      __syncthreads();
+      const int any_odd = __syncthreads_or(odd);
       if (warp == 0) {
-        v0 = red_v[lane];
-        i0 = red_i[lane];
+        v0 = lane < kWarps ? sh.red_v[lane] : -INFINITY;
+        i0 = lane < kWarps ? sh.red_i[lane] : p.V;
         warp_best(v0, i0);
-        if (lane == 0) red_i[0] = i0;
+        if (lane == 0) {
+          sh.part_v[pass & 1] = v0;
+          sh.part_i[pass & 1] = i0;
+          sh.part_odd[pass & 1] = any_odd;
+        }
       }
+      cluster_sync();
+      if (warp == 0) {
+        v0 = -INFINITY;
+        i0 = p.V;
+        int o = 0;
+        if (lane < (int)ranks) {
+          v0 = __uint_as_float(cluster_word(&sh.part_v[pass & 1], lane));
+          i0 = (int)cluster_word(&sh.part_i[pass & 1], lane);
+          o = (int)cluster_word(&sh.part_odd[pass & 1], lane);
+        }
+        warp_best(v0, i0);
+        o = __any_sync(0xffffffffu, o);
+        if (lane == 0) {
+          sh.red_i[0] = i0;
+          sh.red_i[1] = o;
+        }
+      }
+      ++pass;
       __syncthreads();
-      next = red_i[0];
-      if (next < p.V || (c == 0.f && ng == 0)) break;
+      next = sh.red_i[0];
+      odd = sh.red_i[1];
+      if (odd || next < p.V || (c == 0.f && ng == 0)) break;
       __syncthreads();
       c = 0.f;  // nothing left of the residual: the target itself
       ng = 0;
     }
+    cluster_sync();  // nobody leaves while its share may still be read
     if (next >= p.V) odd = 1;
   }
-  if (__syncthreads_or(odd)) {
+  if (rank != 0) return;
+  if (odd) {
     if (tid == 0) flag(p.dev_status, FLARE_DEV_BAD_LOGITS);
     return;
   }
   if (tid < p.N) {
-    p.path[(size_t)r * p.N + tid] = tid < s_len ? line[tid] : -1;
-    p.node_logp[(size_t)r * p.N + tid] = tid < n ? logp[tid] : 0.f;
+    p.path[(size_t)r * p.N + tid] = tid < sh.len ? sh.line[tid] : -1;
+    p.node_logp[(size_t)r * p.N + tid] = sh.logp[tid];
   }
   if (tid == 0) {
-    p.path_len[r] = s_len;
+    p.path_len[r] = sh.len;
     p.next_token[r] = next;
   }
 }
@@ -387,10 +526,10 @@ void plan_tree_verify(int R, int N, int V, int num_sms, int* chunk, int* n_chunk
 namespace {
 template <typename T>
 cudaError_t launch_t(const TreeVerifyParams& p, cudaStream_t stream) {
-  if (p.N > 1) {  // a lone anchor has no row with children
-    // rows along y: 65535 a launch
+  const bool rows = p.N > 1;  // a lone anchor has no row with children
+  if (rows) {
     TreeVerifyParams b = p;
-    const int step = 65535 / p.N;  // requests per launch
+    const int step = 65535 / p.N;  // requests per launch: rows go along the grid's y
     for (int r0 = 0; r0 < p.R; r0 += step) {
       const int nr = p.R - r0 < step ? p.R - r0 : step;
       const size_t e = (size_t)r0 * p.N;
@@ -398,16 +537,25 @@ cudaError_t launch_t(const TreeVerifyParams& p, cudaStream_t stream) {
       b.parent = p.parent + e;
       b.node_len = p.node_len + r0;
       b.stats = p.stats + e * p.n_chunks;
-      tree_rows_kernel<T>
-          <<<dim3((unsigned)p.n_chunks, (unsigned)(nr * p.N)), kRowThreads, 0, stream>>>(b);
+      const dim3 grid((unsigned)p.n_chunks, (unsigned)(nr * p.N));
+      if (p.greedy) tree_rows_kernel<T, true><<<grid, kRowThreads, 0, stream>>>(b);
+      else tree_rows_kernel<T, false><<<grid, kRowThreads, 0, stream>>>(b);
       note_launches(1);
       const cudaError_t err = cudaGetLastError();
       if (err != cudaSuccess) return err;
     }
   }
-  tree_walk_kernel<T><<<(unsigned)p.R, kWalkThreads, 0, stream>>>(p);
+  // CTAs per request: more while a share keeps 2048 tokens and the batch does
+  // not yet fill the GPU
+  int cluster = 1;
+  while (cluster < kMaxCluster && p.V / (2 * cluster) >= 2048 &&
+         (long long)p.R * 2 * cluster <= 4LL * kNumSMs)
+    cluster *= 2;
+  const cudaError_t err =
+      pdl_launch(tree_walk_kernel<T>, dim3((unsigned)p.R * cluster), kWalkThreads, 0, stream, rows,
+                 cluster, p);
   note_launches(1);
-  return cudaGetLastError();
+  return err != cudaSuccess ? err : cudaGetLastError();
 }
 }  // namespace
 
