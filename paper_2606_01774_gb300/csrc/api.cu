@@ -610,8 +610,7 @@ flare_status flare_tree_softmax_attn(const flare_softmax_desc* d, const void* q,
   p.row_tiles = plan.row_tiles;
   p.tile_rows = plan.tile_rows;
   char* ws = static_cast<char*>(workspace);
-  p.tiles = reinterpret_cast<int32_t*>(ws + plan.tiles_off);
-  p.total = reinterpret_cast<long long*>(ws + plan.total_off);
+  p.bad = reinterpret_cast<int32_t*>(ws + plan.bad_off);
   p.cuts = ws + plan.cuts_off;
   p.anc = reinterpret_cast<uint64_t*>(ws + plan.anc_off);
   p.part_o = reinterpret_cast<float*>(ws + plan.part_o_off);

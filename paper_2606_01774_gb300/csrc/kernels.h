@@ -152,8 +152,7 @@ struct TreeSoftmaxParams {
   void* out;                  // [R,N,Hq,D]
   float* lse;                 // [R,N,Hq] or nullptr
   int gangs, row_tiles, tile_rows;
-  int32_t* tiles;             // [R] key tiles per kv head; 0 nothing to do, -1 a bad request
-  long long* total;           // key tiles of the batch
+  int32_t* bad;               // [R] whether a request is skipped
   void* cuts;                 // [gangs] TreeCut: the item that a gang leaves unfinished
   uint64_t* anc;              // [R,N] path of each node as a bit set
   float* part_o;              // [2 gangs row_tiles][tile_rows][D] partial outputs
@@ -163,7 +162,7 @@ struct TreeSoftmaxParams {
 
 struct TreeSoftmaxPlan {
   int gangs, row_tiles, tile_rows;
-  size_t tiles_off, total_off, cuts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
+  size_t bad_off, cuts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
 };
 
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,

@@ -12,8 +12,10 @@
 // has at most two partial pieces: slot 0, one that starts inside an item (its
 // first), and slot 1, one that starts an item without finishing it (its last).
 //
-// Prefix lengths live on the device, so every CTA computes the cut itself
-// from the per-request tile counts.
+// Lengths live on the device, so every CTA computes the cut itself.  Whether a
+// request's pages and tree are sound does not enter it: that is checked beside
+// the attention, and a bad request's pieces are dropped where they would be
+// stored.
 #pragma once
 
 #include "common.cuh"
@@ -30,11 +32,17 @@ struct TreeSpanShared {
 };
 
 // The item that a gang starts and leaves unfinished, to be merged: its request
-// (-1: none), kv head and first tile.
+// (-1: none) and kv head, and the last gang that has a piece of it.
 struct alignas(16) TreeCut {
-  int r, kvh;
-  long long s0;
+  int r, kvh, last, nodes;
 };
+
+// Key tiles per kv head of a request; 0 when it has no nodes or a wrong length.
+__device__ __forceinline__ int tree_tiles(const TreeSoftmaxParams& p, int r) {
+  const int n = p.node_len[r], P = p.prefix_len[r];
+  const bool ok = n > 0 && n <= p.N && P >= 0 && P <= (long long)p.max_pages * p.page_size;
+  return ok ? (P + kTreeTile - 1) / kTreeTile + 1 : 0;
+}
 
 // A stretch of one item's tiles: j0 .. j1 - 1 of n.
 struct TreePiece {
@@ -50,8 +58,8 @@ struct TreeCursor {
   // The next piece of the span; false at its end.
   __device__ __forceinline__ bool next(const TreeSoftmaxParams& p, TreePiece& w) {
     if (left <= 0) return false;
-    int n = p.tiles[r];
-    while (n <= 0) n = p.tiles[++r];
+    int n = tree_tiles(p, r);
+    while (n == 0) n = tree_tiles(p, ++r);
     w.r = r;
     w.kvh = kvh;
     w.j0 = j;
@@ -76,6 +84,11 @@ __device__ __forceinline__ int tree_gangs(const TreeSoftmaxParams& p, long long 
   return total < p.gangs ? (int)total : p.gangs;
 }
 
+// The gang whose span holds tile x of `total`.
+__device__ __forceinline__ int tree_gang_of(long long x, long long total, int gangs) {
+  return (int)(((x + 1) * gangs - 1) / total);
+}
+
 __device__ __forceinline__ long long shfl_up_ll(long long x, int o) {
   return __shfl_up_sync(0xffffffffu, x, o);
 }
@@ -89,7 +102,7 @@ __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int 
   const int per = (p.R + THREADS - 1) / THREADS;
   const int r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
   long long sum = 0;
-  for (int r = r0; r < r1; ++r) sum += (long long)max(p.tiles[r], 0) * p.Hkv;
+  for (int r = r0; r < r1; ++r) sum += (long long)tree_tiles(p, r) * p.Hkv;
   long long incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -116,7 +129,7 @@ __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int 
     long long at = before;
     int r = r0;
     for (;; ++r) {
-      const long long n = (long long)max(p.tiles[r], 0) * p.Hkv;
+      const long long n = (long long)tree_tiles(p, r) * p.Hkv;
       if (lo < at + n) break;
       at += n;
     }
@@ -128,37 +141,32 @@ __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int 
   if (blockIdx.x % p.row_tiles == 0) {
     TreeCut* cut = static_cast<TreeCut*>(p.cuts) + gang;
     if (lo >= hi) {
-      if (tid == 0) *cut = TreeCut{-1, 0, 0};
+      if (tid == 0) *cut = TreeCut{-1, 0, 0, 0};
     } else if (before <= hi - 1 && hi - 1 < before + sum) {
       long long at = before;
       int r = r0;
       for (;; ++r) {
-        const long long n = (long long)max(p.tiles[r], 0) * p.Hkv;
+        const long long n = (long long)tree_tiles(p, r) * p.Hkv;
         if (hi - 1 < at + n) break;
         at += n;
       }
-      const int n = p.tiles[r], kvh = (int)((hi - 1 - at) / n);
+      const int n = tree_tiles(p, r), kvh = (int)((hi - 1 - at) / n);
       const long long s0 = at + (long long)kvh * n;
-      *cut = TreeCut{s0 >= lo && s0 + n > hi ? r : -1, kvh, s0};
+      const bool mine = s0 >= lo && s0 + n > hi;
+      *cut = TreeCut{mine ? r : -1, kvh, tree_gang_of(s0 + n - 1, total, gangs), p.node_len[r]};
     }
   }
-  if (blockIdx.x == 0 && tid == 0) *p.total = total;
   __syncthreads();
   TreeCursor c;
   c.left = sh.hi - sh.lo;
   c.r = c.kvh = c.j = 0;
   if (c.left > 0) {
     c.r = sh.r;
-    const int n = p.tiles[c.r];
+    const int n = tree_tiles(p, c.r);
     c.kvh = (int)(sh.off / n);
     c.j = (int)(sh.off - (long long)c.kvh * n);
   }
   return c;
-}
-
-// The gang whose span holds tile x of `total`.
-__device__ __forceinline__ int tree_gang_of(long long x, long long total, int gangs) {
-  return (int)(((x + 1) * gangs - 1) / total);
 }
 
 }  // namespace flare

@@ -3,10 +3,12 @@
 // the fp32 attention kernel on CUDA cores.
 //
 //   tree_plan_kernel    a CTA per request checks its lengths, page ids and
-//                       tree, and writes its tile count and its nodes' paths
+//                       tree, and writes its nodes' paths
 //   attention           bf16: tree_softmax_tc.cu; fp32: tree_softmax_simt_kernel
 //   tree_finish_kernel  merges items that several gangs share, and writes the
 //                       outputs of unused nodes
+// Each starts while the one before it runs (pdl.cuh) and waits for it where it
+// needs its results.
 //
 // Online softmax in base 2 with the logit scale folded into q; running
 // maximum, sum and output in fp32.
@@ -61,8 +63,7 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
   }
   const int any = __syncthreads_or(bad);
   if (bad) flag(p.dev_status, bad);
-  if (tid == 0)
-    p.tiles[r] = any ? -1 : (n == 0 ? 0 : (P + kTreeTile - 1) / kTreeTile + 1);
+  if (tid == 0) p.bad[r] = any;
 }
 
 // fp32 attention.  A CTA takes 32 query rows; thread (y, x) of its 8 x 16 holds
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   while (cur.next(p, w)) {
     const int n = p.node_len[w.r], P = p.prefix_len[w.r];
     const int M = n * p.G;
-    if (m0 >= M) continue;
+    if (m0 >= M || p.bad[w.r]) continue;
     __syncthreads();  // the previous piece's rows are read
     for (int e = tid; e < kRowsS * (D / 4); e += kThreadsS) {
       const int i = e / (D / 4), d = e % (D / 4) * 4, m = m0 + i;
@@ -265,12 +266,12 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   __shared__ float red_l[8], red_d[8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int sub = warp % WARPS;
-  // unused nodes' rows, a node per warp (the plan has completed: the attention
-  // kernel waited for it before it let this one start)
+  // unused nodes' rows, a node per warp (the attention kernel waited for the
+  // plan before it let this one start)
   for (long long u = (long long)blockIdx.x * 8 + warp; u < (long long)p.R * p.N;
        u += (long long)gridDim.x * 8) {
     const int r = (int)(u / p.N), t = (int)(u - (long long)r * p.N);
-    if (p.tiles[r] < 0 || t < p.node_len[r]) continue;
+    if (p.bad[r] || t < p.node_len[r]) continue;
     uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + u * p.Hq * D);
     const int n16 = p.Hq * (D * (int)sizeof(T) / 16);
     for (int e = lane; e < n16; e += 32) out[e] = make_uint4(0u, 0u, 0u, 0u);
@@ -282,14 +283,10 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   const int g0 = blockIdx.x / per_tile / p.row_tiles, mt = blockIdx.x / per_tile % p.row_tiles;
   const int row = part_id * kRowsPerCta + warp / WARPS;  // of the row tile
   pdl_wait();                                            // the attention
-  const long long total = *p.total;
-  const int gangs = tree_gangs(p, total);
-  if (g0 >= gangs) return;
   const TreeCut cut = static_cast<const TreeCut*>(p.cuts)[g0];
-  if (cut.r < 0) return;
-  const int n = p.tiles[cut.r], m = mt * p.tile_rows + row;
-  const bool live = m < p.node_len[cut.r] * p.G;
-  const int g1 = tree_gang_of(cut.s0 + n - 1, total, gangs);
+  if (cut.r < 0 || p.bad[cut.r]) return;
+  const int m = mt * p.tile_rows + row, g1 = cut.last;
+  const bool live = m < cut.nodes * p.G;
   auto part = [&](int g) {
     return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows + row;
   };
@@ -393,10 +390,8 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
   const size_t slots = (size_t)2 * pl.gangs * pl.row_tiles * pl.tile_rows;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t at = 0;
-  pl.tiles_off = at;
+  pl.bad_off = at;
   at += up((size_t)R * sizeof(int32_t));
-  pl.total_off = at;
-  at += up(sizeof(long long));
   pl.cuts_off = at;
   at += up((size_t)pl.gangs * sizeof(TreeCut));
   pl.anc_off = at;

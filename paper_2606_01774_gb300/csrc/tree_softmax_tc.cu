@@ -20,11 +20,13 @@
 // NQ = 2 (more than 128 rows, D <= 128): a second row tile with its own softmax
 // warps shares every staged tile, so that keys and values enter an SM once for
 // 256 rows; the tensor cores alternate between the two, one's products running
-// while the other's softmax does.
+// while the other's softmax does.  Its queries are read from shared memory, so
+// that tensor memory has room for two score buffers per row tile.
 //
 // Warp roles (256 threads, 384 with NQ = 2):
 //   warp 0     K producer, warp 6 V producer: a TMA box per (page, 64-column
-//              chunk), a lane each, page ids read one tile ahead
+//              chunk), a lane each, page ids read one tile ahead; they start
+//              before the plan is known to be done
 //   warp 7     zeroes V rows that no query may see (past the prefix end, unused
 //              nodes), so that what they hold never meets a zero probability;
 //              follows every V tile, so a slot is free once this warp and the
@@ -66,13 +68,16 @@ struct TreeCfg {
   static constexpr int kThreads = NQ == 1 ? 256 : 384;
   static constexpr int kChunks = D / 64;
   static constexpr int kTileBytes = kChunks * kTreeTile * 128;  // one K (or V) tile
-  static constexpr int kKStages = D == 256 ? 3 : (D == 128 ? 6 : 8);
-  static constexpr int kVStages = D == 256 ? 4 : (D == 128 ? 7 : 8);
-  static constexpr int kSmem = (kKStages + kVStages) * kTileBytes + 1024;
-  // tensor memory columns, per row tile: O, Q as bf16 pairs, the S / P buffers
-  static constexpr int kSBuf = NQ == 2 ? (D == 128 ? 1 : 2) : (D == 256 ? 2 : 3);
+  // NQ = 1: queries in tensor memory; 2: in shared memory, rows of 128 bytes in
+  // 64-column chunks like the keys
+  static constexpr int kQTile = NQ == 2 ? kChunks * kRowsT * 128 : 0;
+  static constexpr int kKStages = NQ == 2 ? (D == 128 ? 5 : 8) : D == 256 ? 3 : (D == 128 ? 6 : 8);
+  static constexpr int kVStages = NQ == 2 ? (D == 128 ? 5 : 8) : D == 256 ? 4 : (D == 128 ? 7 : 8);
+  static constexpr int kSmem = NQ * kQTile + (kKStages + kVStages) * kTileBytes + 1024;
+  // tensor memory columns, per row tile: O, Q as bf16 pairs (NQ = 1), the S / P buffers
+  static constexpr int kSBuf = D == 256 || (NQ == 2 && D == 128) ? 2 : 3;
   static constexpr int kQCol = D;
-  static constexpr int kSCol = D + D / 2;
+  static constexpr int kSCol = NQ == 2 ? D : D + D / 2;
   static constexpr int kRowCols = kSCol + kSBuf * kTreeTile;
   static constexpr int kTmemCols = NQ * kRowCols > 256 ? 512 : 256;
   static_assert(NQ * kRowCols <= 512, "tensor memory");
@@ -137,7 +142,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
   constexpr int kSB = C::kSBuf;
   extern __shared__ uint8_t smem_raw[];
   __shared__ TreeShared sh;
-  uint8_t* Ks = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* Qs = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t* Ks = Qs + NQ * C::kQTile;
   uint8_t* Vs = Ks + C::kKStages * C::kTileBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
@@ -168,8 +174,6 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     tc::fence_mbar_init();
   }
   if (warp == 1) tc::tmem_alloc(&sh.tmem_base, C::kTmemCols);
-  pdl_wait();  // the plan
-  pdl_launch_next();
   const TreeCursor span = tree_span<C::kThreads>(p, gang, sh.span);
   tc::fence_before_sync();
   __syncthreads();
@@ -279,6 +283,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       const uint32_t id_o = tc::idesc_bf16(kRowsT, D, false, true);
       const uint64_t kdesc0 = tc::sdesc_sw128(tc::smem_u32(Ks), 16, 1024);
       const uint64_t vdesc0 = tc::sdesc_sw128(tc::smem_u32(Vs), kTreeTile * 128, 1024);
+      const uint64_t qdesc0 = tc::sdesc_sw128(tc::smem_u32(Qs), 16, 1024);
       bool ok = true;
       int g = 0;              // running tile count of the rings
       int gt[2] = {0, 0};     // and of each row tile's buffers
@@ -300,10 +305,19 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           const uint32_t base = tmem + t * C::kRowCols;
           const uint64_t kd = kdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            tc::mma_bf16_ts(base + C::kSCol + sb * kTreeTile, base + C::kQCol + kk * 8,
-                            kd + (uint64_t)(((kk >> 2) * (kTreeTile * 128) + (kk & 3) * 32) >> 4),
-                            id_s, kk > 0 ? 1u : 0u);
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t kdk =
+                kd + (uint64_t)(((kk >> 2) * (kTreeTile * 128) + (kk & 3) * 32) >> 4);
+            if constexpr (NQ == 2)
+              tc::mma_bf16_ss(base + C::kSCol + sb * kTreeTile,
+                              qdesc0 + (uint64_t)((t * C::kQTile + (kk >> 2) * (kRowsT * 128) +
+                                                   (kk & 3) * 32) >>
+                                                  4),
+                              kdk, id_s, kk > 0 ? 1u : 0u);
+            else
+              tc::mma_bf16_ts(base + C::kSCol + sb * kTreeTile, base + C::kQCol + kk * 8, kdk, id_s,
+                              kk > 0 ? 1u : 0u);
+          }
           tc::mma_commit(&sh.s_full[t][sb]);
           if (t == nt - 1) tc::mma_commit(&sh.k_empty[st]);
           return true;
@@ -373,15 +387,22 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     const int mt0 = m0 + t * kRowsT;
     const int node = m / p.G, head = m - node * p.G;
 
-    // Q row into tensor memory as bf16 pairs; rows past the tree's are zero
+    // this thread's query row of an item (of a used row's warp: the other rows'
+    // outputs are never read)
+    auto q_row = [&](const TreeItem& w) {
+      const bool live = m < w.nodes * p.G;
+      return reinterpret_cast<const uint4*>(
+          static_cast<const __nv_bfloat16*>(p.q) +
+          (((size_t)w.w.r * p.N + (live ? node : 0)) * p.Hq + w.w.kvh * p.G + head) * D);
+    };
+    // Q row where the score product reads it: tensor memory, as bf16 pairs, or
+    // shared memory (128-byte swizzle); unused rows are zero
     auto load_q = [&](const TreeItem& w) {
       const bool live = m < w.nodes * p.G;
       if (__any_sync(0xffffffffu, live)) {
-        const uint4* qrow = reinterpret_cast<const uint4*>(
-            static_cast<const __nv_bfloat16*>(p.q) +
-            (((size_t)w.w.r * p.N + (live ? node : 0)) * p.Hq + w.w.kvh * p.G + head) * D);
-        constexpr int kWords = D / 2;                      // TMEM columns of a row
-        constexpr int kBatch = kWords < 64 ? kWords : 64;  // columns per batch of loads
+        const uint4* qrow = q_row(w);
+        constexpr int kWords = D / 2;                      // 32-bit words of a row
+        constexpr int kBatch = kWords < 64 ? kWords : 64;  // words per batch of loads
 #pragma unroll 1
         for (int c0 = 0; c0 < kWords; c0 += kBatch) {
           uint32_t q[kBatch];
@@ -393,11 +414,23 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
             q[4 * q4 + 2] = v.z;
             q[4 * q4 + 3] = v.w;
           }
+          if constexpr (NQ == 2) {
+            uint8_t* dst = Qs + t * C::kQTile + row * 128;
 #pragma unroll
-          for (int c = 0; c < kBatch; c += 16)
-            tc::tmem_st16(tmem_q + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&q[c]));
+            for (int q4 = 0; q4 < kBatch / 4; ++q4) {
+              const int u = c0 / 4 + q4;  // 16-byte unit of the row
+              *reinterpret_cast<uint4*>(dst + (u >> 3) * (kRowsT * 128) +
+                                        (((u & 7) ^ (row & 7)) << 4)) =
+                  make_uint4(q[4 * q4], q[4 * q4 + 1], q[4 * q4 + 2], q[4 * q4 + 3]);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < kBatch; c += 16)
+              tc::tmem_st16(tmem_q + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&q[c]));
+          }
         }
-        tc::tmem_st_wait();
+        if constexpr (NQ == 2) tc::fence_async_smem();
+        else tc::tmem_st_wait();
       }
       tc::fence_before_sync();
       tc::mbar_arrive(&sh.q_ready[t]);
@@ -407,10 +440,22 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     int g = 0;  // running tile count
     bool have = next_item(p, cur, mt0, it);
     if (have) load_q(it);
+    pdl_wait();  // the plan: paths, and which requests are bad
+    if (tid == 64) pdl_launch_next();
     for (int k = 0; have; ++k) {
       const bool live = m < it.nodes * p.G;
       const bool warp_live = __any_sync(0xffffffffu, live);
       const uint64_t path = live ? p.anc[(size_t)it.w.r * p.N + node] : 0ull;
+      const bool skip = p.bad[it.w.r] != 0;
+      // the next piece, its queries on their way to L2 before they are needed
+      TreeItem nx = it;
+      const bool more = next_item(p, cur, mt0, nx);
+      if (more && m < nx.nodes * p.G) {
+        const char* x = reinterpret_cast<const char*>(q_row(nx));
+#pragma unroll
+        for (int c = 0; c < D * 2; c += 128)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(x + c));
+      }
       float m_run = -INFINITY, l_run = 0.f;
       for (int j = 0; j < it.tiles; ++j) {
         const int gg = g + j, sb = gg % kSB;
@@ -491,9 +536,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       g += it.tiles;
       if (ok && aborted_t(sh)) ok = false;
       // the next piece's queries: every S product of this one has completed
-      TreeItem nx = it;
-      const bool more = ok && next_item(p, cur, mt0, nx);
-      if (more) load_q(nx);
+      if (ok && more) load_q(nx);
       if (ok && !warp_wait_t(&sh.o_final[t], (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
       if (!ok) break;
       if (warp_live) {
@@ -505,32 +548,37 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         const size_t prow =
             ((size_t)blockIdx.x * 2 + it.w.slot()) * (NQ * kRowsT) + t * kRowsT + row;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 16) {
-          uint32_t o[16];
-          tc::tmem_ld16(tmem_o + lane_off + c, o);
+        for (int c0 = 0; c0 < D; c0 += 64) {
+          uint32_t o[64];
+#pragma unroll
+          for (int c = 0; c < 64; c += 16)
+            tc::tmem_ld16(tmem_o + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&o[c]));
           tc::tmem_ld_wait();
-          if (!live) continue;
+          if (!live || skip) continue;
           if (whole) {
-            uint32_t h[8];
+            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * D + c0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const __nv_bfloat162 h2 = __floats2bfloat162_rn(__uint_as_float(o[2 * i]) * inv,
-                                                              __uint_as_float(o[2 * i + 1]) * inv);
-              h[i] = *reinterpret_cast<const uint32_t*>(&h2);
+            for (int c = 0; c < 64; c += 8) {
+              uint32_t h[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 h2 =
+                    __floats2bfloat162_rn(__uint_as_float(o[c + 2 * i]) * inv,
+                                          __uint_as_float(o[c + 2 * i + 1]) * inv);
+                h[i] = *reinterpret_cast<const uint32_t*>(&h2);
+              }
+              dst[c / 8] = make_uint4(h[0], h[1], h[2], h[3]);
             }
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * D + c);
-            dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
-            dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
           } else {
-            float4* dst = reinterpret_cast<float4*>(p.part_o + prow * D + c);
+            float4* dst = reinterpret_cast<float4*>(p.part_o + prow * D + c0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              dst[i] = make_float4(
-                  __uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
-                  __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
+            for (int c = 0; c < 64; c += 4)
+              dst[c / 4] = make_float4(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
+                                       __uint_as_float(o[c + 2]) * inv,
+                                       __uint_as_float(o[c + 3]) * inv);
           }
         }
-        if (live) {
+        if (live && !skip) {
           if (!whole) p.part_lse[prow] = l2;
           else if (p.lse) p.lse[orow] = l2 * 0.6931471805599453f;
         }
@@ -548,6 +596,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, C::kTmemCols);
   }
+  pdl_wait();  // also where the span was empty
 }
 
 // ------------------------------------------------------------------ host side
@@ -593,9 +642,11 @@ cudaError_t launch_tc_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
       return cudaErrorInvalidValue;
   }
   {
-    // an empty pool is never read; its maps point at the nodes' tensors
+    // page ids are checked beside the stream: one outside the pool reads as
+    // zeros.  Without a pool the maps show one row of the nodes' tensors.
     const bool none = p.num_pages == 0 || p.max_pages == 0;
-    const cuuint64_t dims[4] = {D, (cuuint64_t)p.page_size, (cuuint64_t)p.Hkv,
+    const cuuint64_t dims[4] = {D, (cuuint64_t)(none ? 1 : p.page_size),
+                                (cuuint64_t)(none ? 1 : p.Hkv),
                                 (cuuint64_t)(none ? 1 : p.num_pages)};
     const cuuint64_t str[3] = {row, p.page_size * row, (cuuint64_t)p.Hkv * p.page_size * row};
     const cuuint32_t rows = p.page_size < kTreeTile ? p.page_size : kTreeTile;
