@@ -118,6 +118,19 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       : "memory");
 }
 
+// True on one thread of a converged warp, always the same one.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t x;
+  asm volatile(
+      "{\n"
+      " .reg .pred p;\n"
+      " elect.sync _|p, 0xffffffff;\n"
+      " selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(x));
+  return x != 0;
+}
+
 // Makes generic-proxy writes to shared memory visible to the async proxy
 // (tensor core / TMA reads that follow).
 __device__ __forceinline__ void fence_async_smem() {

@@ -23,20 +23,20 @@
 // while the other's softmax does.  Its queries are read from shared memory, so
 // that tensor memory has room for two score buffers per row tile.
 //
-// Warp roles (256 threads, 384 with NQ = 2):
+// Warp roles (8 warps, 12 with NQ = 2):
 //   warp 0     K producer, warp 6 V producer: a TMA box per (page, 64-column
 //              chunk), a lane each, page ids read one tile ahead; they start
 //              before the plan is known to be done
-//   warp 7     zeroes V rows that no query may see (past the prefix end, unused
-//              nodes), so that what they hold never meets a zero probability;
-//              follows every V tile, so a slot is free once this warp and the
-//              product have both left it
-//   warp 1     tensor-memory owner; one thread issues S_j = Q K_j^T and
-//              O += P_j V_j; both read their A operand from tensor memory
+//   warps 1, 7 MMA issuers: S_j = Q K_j^T and O += P_j V_j.  Issuing a tile's
+//              products, commits and waits takes one warp as long as a tile may
+//              take, so two share it: NQ = 1 one the scores and one the values,
+//              NQ = 2 a row tile each.  Warp 1 owns the tensor memory.
 //   warps 2-5 (8-11) softmax, a TMEM lane quarter each: a thread per query row;
 //              online base-2 softmax with a lazily moved maximum (O is rescaled
 //              when it grows by more than 2^8); quarters without a used row skip
-//              the arithmetic
+//              the arithmetic.  Warps 2-5 also zero the V rows that no query may
+//              see (past the prefix end, unused nodes), so that what they hold
+//              never meets a zero probability.
 // Every wait is bounded; a timeout sets FLARE_DEV_WAIT_TIMEOUT, the CTA stops
 // issuing work, writes nothing more, waits for its copies in flight, frees its
 // tensor memory and exits.
@@ -55,7 +55,7 @@ namespace {
 
 constexpr int kRowsT = 128;            // query rows of a row tile (TMEM lanes)
 constexpr int kSmThreads = 128;        // softmax threads of a row tile
-constexpr int kVWarpT = 6, kFixWarpT = 7;
+constexpr int kVWarpT = 6, kMma2WarpT = 7;
 constexpr float kMoveMax = 8.0f;       // log2 units
 
 struct TreeMaps {
@@ -87,7 +87,7 @@ struct TreeShared {
   uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], v_fix[8];
   uint64_t s_full[2][3], p_full[2][3], pv_done[2][3];  // per row tile
   uint64_t q_ready[2], o_final[2], o_free[2];
-  uint64_t drain;  // after a timeout: every MMA issued has completed
+  uint64_t drain[2];  // after a timeout: every MMA issued has completed
   uint32_t tmem_base;
   int abort_flag;
   TreeSpanShared span;
@@ -153,12 +153,12 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     sh.abort_flag = 0;
     for (int s = 0; s < C::kKStages; ++s) {
       tc::mbar_init(&sh.k_full[s], 1);
-      tc::mbar_init(&sh.k_empty[s], 1);
+      tc::mbar_init(&sh.k_empty[s], NQ);  // a product per row tile
     }
     for (int s = 0; s < C::kVStages; ++s) {
       tc::mbar_init(&sh.v_full[s], 1);
-      tc::mbar_init(&sh.v_empty[s], 2);  // the products and the zeroing warp
-      tc::mbar_init(&sh.v_fix[s], 1);
+      tc::mbar_init(&sh.v_empty[s], NQ);
+      tc::mbar_init(&sh.v_fix[s], kSmThreads);
     }
     for (int t = 0; t < NQ; ++t) {
       for (int b = 0; b < kSB; ++b) {
@@ -170,7 +170,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       tc::mbar_init(&sh.o_final[t], 1);
       tc::mbar_init(&sh.o_free[t], kSmThreads);
     }
-    tc::mbar_init(&sh.drain, 1);
+    tc::mbar_init(&sh.drain[0], 1);
+    tc::mbar_init(&sh.drain[1], 1);
     tc::fence_mbar_init();
   }
   if (warp == 1) tc::tmem_alloc(&sh.tmem_base, C::kTmemCols);
@@ -249,137 +250,139 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         if (last >= 0) tc::mbar_wait(&fulls[s], (uint32_t)(last / ns) & 1u, nullptr, 100000000ull);
       }
     }
-  } else if (warp == kFixWarpT) {
-    // ------------------------------------------------------------ V rows nobody may see
+  } else if (warp == 1 || warp == kMma2WarpT) {
+    // ------------------------------------------------------------ MMA issuers
+    // The whole warp walks the loop with the same values and one elected thread
+    // issues, so that descriptors stay in uniform registers: issued from a
+    // branch on one lane, each MMA costs some 60 cycles of moves into them.
+    const int t = NQ == 2 && warp != 1 ? 1 : 0;  // of row tile t
+    const bool scores = NQ == 2 || warp == 1, values = NQ == 2 || warp != 1;
+    const uint32_t base = tmem + t * C::kRowCols;
+    const uint32_t id_s = tc::idesc_bf16(kRowsT, kTreeTile, false, false);
+    const uint32_t id_o = tc::idesc_bf16(kRowsT, D, false, true);
+    const uint64_t kdesc0 = tc::sdesc_sw128(tc::smem_u32(Ks), 16, 1024);
+    const uint64_t vdesc0 = tc::sdesc_sw128(tc::smem_u32(Vs), kTreeTile * 128, 1024);
+    const uint64_t qdesc0 = tc::sdesc_sw128(tc::smem_u32(Qs + t * C::kQTile), 16, 1024);
     bool ok = true;
-    int g = 0;
+    int g = 0;              // running tile count of the rings
+    int gt = 0, kt = 0;     // of this row tile's buffers, and its pieces
+    uint32_t fix_par = 0u;  // per V slot: parity of its next zeroed tile
     while (ok && next_item(p, cur, m0, it)) {
-      for (int j = 0; j < it.tiles; ++j, ++g) {
-        const int st = g % C::kVStages;
-        if (!warp_wait_t(&sh.v_full[st], (uint32_t)(g / C::kVStages) & 1u, &sh.abort_flag)) {
-          ok = false;
-          break;
+      const int n = it.tiles;
+      auto k_tile = [&](int j) {
+        return warp_wait_t(&sh.k_full[(g + j) % C::kKStages],
+                           (uint32_t)((g + j) / C::kKStages) & 1u, &sh.abort_flag);
+      };
+      auto v_tile = [&](int j) {
+        const int st = (g + j) % C::kVStages;
+        if (!warp_wait_t(&sh.v_full[st], (uint32_t)((g + j) / C::kVStages) & 1u, &sh.abort_flag))
+          return false;
+        if (it.valid(j) < kTreeTile) {
+          if (!warp_wait_t(&sh.v_fix[st], (fix_par >> st) & 1u, &sh.abort_flag)) return false;
+          fix_par ^= 1u << st;
         }
-        const int valid = it.valid(j);
-        if (valid < kTreeTile) {
-          uint8_t* dst = Vs + st * C::kTileBytes;
-          const int n16 = (kTreeTile - valid) * 8;  // 16-byte pieces per chunk
-          for (int c = 0; c < C::kChunks; ++c)
-            for (int e = lane; e < n16; e += 32)
-              *reinterpret_cast<uint4*>(dst + c * (kTreeTile * 128) + (valid + e / 8) * 128 +
-                                        (e % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          tc::fence_async_smem();
+        return true;
+      };
+      if (t == 1 && m0 + kRowsT >= it.nodes * p.G) {  // no rows of this item: pass its tiles on
+        for (int j = 0; j < n && ok; ++j) {
+          ok = k_tile(j) && v_tile(j);
+          if (ok && lane == 0) {
+            tc::mbar_arrive(&sh.k_empty[(g + j) % C::kKStages]);
+            tc::mbar_arrive(&sh.v_empty[(g + j) % C::kVStages]);
+          }
           __syncwarp();
-          if (lane == 0) tc::mbar_arrive(&sh.v_fix[st]);
         }
-        if (lane == 0) tc::mbar_arrive(&sh.v_empty[st]);
+        g += n;
+        continue;
       }
-    }
-    if (!ok && lane == 0) give_up(sh, p.dev_status);
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
-      const uint32_t id_s = tc::idesc_bf16(kRowsT, kTreeTile, false, false);
-      const uint32_t id_o = tc::idesc_bf16(kRowsT, D, false, true);
-      const uint64_t kdesc0 = tc::sdesc_sw128(tc::smem_u32(Ks), 16, 1024);
-      const uint64_t vdesc0 = tc::sdesc_sw128(tc::smem_u32(Vs), kTreeTile * 128, 1024);
-      const uint64_t qdesc0 = tc::sdesc_sw128(tc::smem_u32(Qs), 16, 1024);
-      bool ok = true;
-      int g = 0;              // running tile count of the rings
-      int gt[2] = {0, 0};     // and of each row tile's buffers
-      int kt[2] = {0, 0};     // pieces of each row tile
-      uint32_t fix_par = 0u;  // per V slot: parity of its next zeroed tile
-      while (ok && next_item(p, cur, m0, it)) {
-        // row tiles with rows of this item: the first, or both
-        const int nt = NQ == 2 && m0 + kRowsT < it.nodes * p.G ? 2 : 1;
-        for (int t = 0; t < nt && ok; ++t)
-          ok = tc::mbar_wait(&sh.q_ready[t], (uint32_t)kt[t] & 1u, &sh.abort_flag);
-        if (!ok) break;
-        // S_j = Q K_j^T of row tile t
-        auto issue_s = [&](int t, int j) -> bool {
-          const int st = (g + j) % C::kKStages, sb = (gt[t] + j) % kSB;
-          if (t == 0 && !tc::mbar_wait(&sh.k_full[st], (uint32_t)((g + j) / C::kKStages) & 1u,
-                                       &sh.abort_flag))
-            return false;
-          tc::fence_after_sync();
-          const uint32_t base = tmem + t * C::kRowCols;
-          const uint64_t kd = kdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
+      if (scores) ok = warp_wait_t(&sh.q_ready[t], (uint32_t)kt & 1u, &sh.abort_flag);
+      if (!ok) break;
+      auto issue_s = [&](int j) -> bool {  // S_j = Q K_j^T
+        if (!k_tile(j)) return false;
+        tc::fence_after_sync();
+        const int st = (g + j) % C::kKStages, sb = (gt + j) % kSB;
+        const uint64_t kd = kdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
+        if (tc::elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint64_t kdk =
                 kd + (uint64_t)(((kk >> 2) * (kTreeTile * 128) + (kk & 3) * 32) >> 4);
             if constexpr (NQ == 2)
               tc::mma_bf16_ss(base + C::kSCol + sb * kTreeTile,
-                              qdesc0 + (uint64_t)((t * C::kQTile + (kk >> 2) * (kRowsT * 128) +
-                                                   (kk & 3) * 32) >>
-                                                  4),
+                              qdesc0 + (uint64_t)(((kk >> 2) * (kRowsT * 128) + (kk & 3) * 32) >> 4),
                               kdk, id_s, kk > 0 ? 1u : 0u);
             else
               tc::mma_bf16_ts(base + C::kSCol + sb * kTreeTile, base + C::kQCol + kk * 8, kdk, id_s,
                               kk > 0 ? 1u : 0u);
           }
           tc::mma_commit(&sh.s_full[t][sb]);
-          if (t == nt - 1) tc::mma_commit(&sh.k_empty[st]);
-          return true;
-        };
-        auto issue_pv = [&](int t, int j) -> bool {
-          const int st = (g + j) % C::kVStages, pb = (gt[t] + j) % kSB;
-          if (!tc::mbar_wait(&sh.p_full[t][pb], (uint32_t)((gt[t] + j) / kSB) & 1u,
-                             &sh.abort_flag))
-            return false;
-          // the first product of a piece overwrites O: the previous one's must be out
-          if (j == 0 && kt[t] > 0 &&
-              !tc::mbar_wait(&sh.o_free[t], (uint32_t)(kt[t] - 1) & 1u, &sh.abort_flag))
-            return false;
-          if (t == 0) {
-            if (!tc::mbar_wait(&sh.v_full[st], (uint32_t)((g + j) / C::kVStages) & 1u,
-                               &sh.abort_flag))
-              return false;
-            if (it.valid(j) < kTreeTile) {
-              if (!tc::mbar_wait(&sh.v_fix[st], (fix_par >> st) & 1u, &sh.abort_flag)) return false;
-              fix_par ^= 1u << st;
-            }
-          }
-          tc::fence_after_sync();
-          const uint32_t base = tmem + t * C::kRowCols;
-          const uint64_t vd = vdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
+          tc::mma_commit(&sh.k_empty[st]);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto issue_pv = [&](int j) -> bool {  // O += P_j V_j
+        const int st = (g + j) % C::kVStages, pb = (gt + j) % kSB;
+        if (!warp_wait_t(&sh.p_full[t][pb], (uint32_t)((gt + j) / kSB) & 1u, &sh.abort_flag))
+          return false;
+        // the first product of a piece overwrites O: the previous one's must be out
+        if (j == 0 && kt > 0 &&
+            !warp_wait_t(&sh.o_free[t], (uint32_t)(kt - 1) & 1u, &sh.abort_flag))
+          return false;
+        if (!v_tile(j)) return false;
+        tc::fence_after_sync();
+        const uint64_t vd = vdesc0 + (uint64_t)((st * C::kTileBytes) >> 4);
+        if (tc::elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kTreeTile / 16; ++kk)
             tc::mma_bf16_ts(base, base + C::kSCol + pb * kTreeTile + kk * 8,
                             vd + (uint64_t)(kk * (2048 >> 4)), id_o, (j > 0 || kk > 0) ? 1u : 0u);
           tc::mma_commit(&sh.pv_done[t][pb]);
-          if (t == nt - 1) tc::mma_commit(&sh.v_empty[st]);
-          return true;
-        };
+          tc::mma_commit(&sh.v_empty[st]);
+        }
+        __syncwarp();
+        return true;
+      };
+      if constexpr (NQ == 2) {
         // MMAs of one thread execute in issue order, so an S buffer can be
         // rewritten once the product that reads its probabilities was issued:
-        // kSB scores ahead, then P V_j and S_j+kSB in turn, row tile by row tile.
-        const int n = it.tiles;
-        for (int j = 0; j < kSB && j < n && ok; ++j)
-          for (int t = 0; t < nt && ok; ++t) ok = issue_s(t, j);
-        for (int j = 0; j < n && ok; ++j)
-          for (int t = 0; t < nt && ok; ++t) {
-            ok = issue_pv(t, j);
-            if (ok && j + kSB < n) ok = issue_s(t, j + kSB);
-          }
-        if (!ok) break;
-        for (int t = 0; t < nt; ++t) {
-          tc::mma_commit(&sh.o_final[t]);
-          gt[t] += n;
-          ++kt[t];
+        // kSB scores ahead, then P V_j and S_j+kSB in turn.
+        for (int j = 0; j < kSB && j < n && ok; ++j) ok = issue_s(j);
+        for (int j = 0; j < n && ok; ++j) {
+          ok = issue_pv(j);
+          if (ok && j + kSB < n) ok = issue_s(j + kSB);
         }
-        g += n;
+      } else if (scores) {
+        for (int j = 0; j < n && ok; ++j) {
+          const int gg = gt + j;  // the buffer's last probabilities have been read
+          if (gg >= kSB)
+            ok = warp_wait_t(&sh.pv_done[t][gg % kSB], (uint32_t)(gg / kSB - 1) & 1u,
+                             &sh.abort_flag);
+          ok = ok && issue_s(j);
+        }
+      } else {
+        for (int j = 0; j < n && ok; ++j) ok = issue_pv(j);
       }
-      if (!ok) give_up(sh, p.dev_status);
-      if (aborted_t(sh)) {
-        tc::mma_commit(&sh.drain);
-        tc::mbar_wait(&sh.drain, 0u, nullptr, 100000000ull);
-      }
+      if (!ok) break;
+      if (values && tc::elect_one()) tc::mma_commit(&sh.o_final[t]);
+      __syncwarp();
+      gt += n;
+      ++kt;
+      g += n;
     }
+    if (!ok && lane == 0) give_up(sh, p.dev_status);
     __syncwarp();
+    if (aborted_t(sh)) {
+      uint64_t* drain = &sh.drain[warp == 1 ? 0 : 1];
+      if (tc::elect_one()) {
+        tc::mma_commit(drain);
+        tc::mbar_wait(drain, 0u, nullptr, 100000000ull);
+      }
+      __syncwarp();
+    }
   } else {
     // ------------------------------------------------------------ softmax warps
-    const int quarter = warp & 3, t = warp >= 8 ? 1 : 0;  // of row tile t
+    const int quarter = warp & 3, t = NQ == 2 && warp >= 8 ? 1 : 0;  // of row tile t
     const int row = quarter * 32 + lane, m = m0 + t * kRowsT + row;
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const uint32_t tmem_o = tmem + t * C::kRowCols;
@@ -437,7 +440,26 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     };
 
     bool ok = true;
-    int g = 0;  // running tile count
+    int g = 0;  // running tile count (of row tile 0: the rings' too)
+    // V rows of tile j that no query may see.  The slot cannot be refilled
+    // before this tile's product, which waits for these threads, so the parity
+    // wait is exact though not every tile is waited for.
+    auto zero_v = [&](int j) -> bool {
+      const int valid = it.valid(j);
+      if (t != 0 || valid == kTreeTile) return true;
+      const int gg = g + j, st = gg % C::kVStages;
+      if (!warp_wait_t(&sh.v_full[st], (uint32_t)(gg / C::kVStages) & 1u, &sh.abort_flag))
+        return false;
+      uint8_t* dst = Vs + st * C::kTileBytes;
+      const int n16 = (kTreeTile - valid) * 8;  // 16-byte pieces per chunk
+      for (int c = 0; c < C::kChunks; ++c)
+        for (int e = row; e < n16; e += kSmThreads)
+          *reinterpret_cast<uint4*>(dst + c * (kTreeTile * 128) + (valid + e / 8) * 128 +
+                                    (e % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+      tc::fence_async_smem();
+      tc::mbar_arrive(&sh.v_fix[st]);
+      return true;
+    };
     bool have = next_item(p, cur, mt0, it);
     if (have) load_q(it);
     pdl_wait();  // the plan: paths, and which requests are bad
@@ -464,6 +486,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           break;
         }
         if (!warp_live) {  // nobody reads these rows' output
+          ok = zero_v(j);
+          if (!ok) break;
           tc::mbar_arrive(&sh.p_full[t][sb]);
           continue;
         }
@@ -530,6 +554,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         for (int c = 0; c < kTreeTile / 2; c += 16)
           tc::tmem_st16(sbuf + c, *reinterpret_cast<uint32_t(*)[16]>(&pk[c]));
         tc::tmem_st_wait();
+        ok = zero_v(j);
+        if (!ok) break;
         tc::fence_before_sync();
         tc::mbar_arrive(&sh.p_full[t][sb]);
       }
