@@ -608,6 +608,7 @@ flare_status flare_tree_softmax_attn(const flare_softmax_desc* d, const void* q,
   p.lse = lse;
   p.gangs = plan.gangs;
   p.row_tiles = plan.row_tiles;
+  p.tile_base = plan.tile_base;
   p.tile_rows = plan.tile_rows;
   char* ws = static_cast<char*>(workspace);
   p.bad = reinterpret_cast<int32_t*>(ws + plan.bad_off);

@@ -1,6 +1,7 @@
 // Internal launch interface between the C ABI layer and the kernels.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -151,7 +152,8 @@ struct TreeSoftmaxParams {
   const int32_t* node_len;    // [R]
   void* out;                  // [R,N,Hq,D]
   float* lse;                 // [R,N,Hq] or nullptr
-  int gangs, row_tiles, tile_rows;
+  int gangs, row_tiles;       // row_tiles: CTAs per gang
+  int tile_base, tile_rows;   // query rows of a row tile, and of a CTA's one or two
   int32_t* bad;               // [R] whether a request is skipped
   void* cuts;                 // [gangs] TreeCut: the item that a gang leaves unfinished
   uint64_t* anc;              // [R,N] path of each node as a bit set
@@ -161,14 +163,20 @@ struct TreeSoftmaxParams {
 };
 
 struct TreeSoftmaxPlan {
-  int gangs, row_tiles, tile_rows;
+  int gangs, row_tiles, tile_base, tile_rows;
   size_t bad_off, cuts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
 };
 
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,
                                   int max_pages, bool bf16, int num_sms);
 cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream);
-cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, cudaStream_t stream);
+// The bf16 attention's tensor maps (queries, nodes' keys and values, pools).
+struct TreeSoftmaxTc {
+  CUtensorMap q, kblk, vblk, kpool, vpool;
+};
+cudaError_t prepare_tree_softmax_tc(const TreeSoftmaxParams& p, TreeSoftmaxTc* tc);
+cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, const TreeSoftmaxTc& tc,
+                                   cudaStream_t stream);
 
 cudaError_t launch_tree_linear(const GdrParams& p, bool bf16, cudaStream_t stream);
 bool tree_linear_tc_supported(int dk, int dv);

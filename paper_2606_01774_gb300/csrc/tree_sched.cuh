@@ -25,6 +25,29 @@ namespace flare {
 
 constexpr int kTreeTile = 64;  // keys per tile
 
+// The query rows of row tile `tile` of a (request, kv head) item: whole nodes
+// with their G query heads, or, with more heads than a tile has rows, some of
+// one node's heads.  Row i is head head0 + i % heads of node node0 + i / heads.
+struct TreeRows {
+  int node0, nodes, head0, heads;
+  __device__ __forceinline__ int node(int i) const { return node0 + i / heads; }
+  __device__ __forceinline__ int head(int i) const { return head0 + i % heads; }
+  // whether row i is one, of a tree of n nodes
+  __device__ __forceinline__ bool used(int i, int n) const {
+    return i < nodes * heads && node(i) < n;
+  }
+};
+
+__device__ __forceinline__ TreeRows tree_rows(const TreeSoftmaxParams& p, int tile) {
+  if (p.G <= p.tile_base) {
+    const int nodes = p.tile_base / p.G;
+    return TreeRows{tile * nodes, nodes, 0, p.G};
+  }
+  const int per = (p.G + p.tile_base - 1) / p.tile_base;  // tiles per node
+  const int h = tile % per * p.tile_base;
+  return TreeRows{tile / per, 1, h, min(p.tile_base, p.G - h)};
+}
+
 struct TreeSpanShared {
   long long warp_sum[32];
   long long lo, hi, off;  // the span, and the first tile's offset in its request

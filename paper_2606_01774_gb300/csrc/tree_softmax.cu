@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
 
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
-  const int m0 = mt * kRowsS;
+  const TreeRows rows = tree_rows(p, mt);
   const float* q = static_cast<const float*>(p.q);
   const float* pools[2] = {static_cast<const float*>(p.k_pool), static_cast<const float*>(p.v_pool)};
   const float* blks[2] = {static_cast<const float*>(p.k_blk), static_cast<const float*>(p.v_blk)};
@@ -96,25 +96,22 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   TreePiece w;
   while (cur.next(p, w)) {
     const int n = p.node_len[w.r], P = p.prefix_len[w.r];
-    const int M = n * p.G;
-    if (m0 >= M || p.bad[w.r]) continue;
+    if (rows.node0 >= n || p.bad[w.r]) continue;
     __syncthreads();  // the previous piece's rows are read
     for (int e = tid; e < kRowsS * (D / 4); e += kThreadsS) {
-      const int i = e / (D / 4), d = e % (D / 4) * 4, m = m0 + i;
+      const int i = e / (D / 4), d = e % (D / 4) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (m < M) {
-        const int t = m / p.G, g = m - t * p.G;
+      if (rows.used(i, n))
         v = *reinterpret_cast<const float4*>(
-            q + (((size_t)w.r * p.N + t) * p.Hq + w.kvh * p.G + g) * D + d);
-      }
+            q + (((size_t)w.r * p.N + rows.node(i)) * p.Hq + w.kvh * p.G + rows.head(i)) * D + d);
       *reinterpret_cast<float4*>(Qs + i * kS + d) =
           make_float4(v.x * p.scale_log2, v.y * p.scale_log2, v.z * p.scale_log2, v.w * p.scale_log2);
     }
     uint64_t path[4];  // the keys of the tree tile that each row sees
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int m = m0 + 4 * y + i;
-      path[i] = m < M ? p.anc[(size_t)w.r * p.N + m / p.G] : 0ull;
+      const int row = 4 * y + i;
+      path[i] = rows.used(row, n) ? p.anc[(size_t)w.r * p.N + rows.node(row)] : 0ull;
     }
     float acc[4][4 * kC], mrow[4], lrow[4];
 #pragma unroll
@@ -229,21 +226,21 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
     const size_t part = ((size_t)blockIdx.x * 2 + w.slot()) * kRowsS;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int m = m0 + 4 * y + i;
-      if (m >= M) continue;
+      const int row = 4 * y + i;
+      if (!rows.used(row, n)) continue;
       const float inv = lrow[i] > 0.f ? 1.f / lrow[i] : 0.f;
       const float l2 = lrow[i] > 0.f ? mrow[i] + log2f(lrow[i]) : -INFINITY;
-      const int t = m / p.G, g = m - t * p.G;
-      const size_t o = ((size_t)w.r * p.N + t) * p.Hq + w.kvh * p.G + g;
+      const size_t o =
+          ((size_t)w.r * p.N + rows.node(row)) * p.Hq + w.kvh * p.G + rows.head(row);
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
         const float4 a = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv,
                                      acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
-        float* dst = whole ? static_cast<float*>(p.out) + o * D : p.part_o + (part + 4 * y + i) * D;
+        float* dst = whole ? static_cast<float*>(p.out) + o * D : p.part_o + (part + row) * D;
         store4(dst + 4 * x + 64 * c, a);
       }
       if (x == 0) {
-        if (!whole) p.part_lse[part + 4 * y + i] = l2;
+        if (!whole) p.part_lse[part + row] = l2;
         else if (p.lse) p.lse[o] = l2 * kLn2;
       }
     }
@@ -285,8 +282,9 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   pdl_wait();                                            // the attention
   const TreeCut cut = static_cast<const TreeCut*>(p.cuts)[g0];
   if (cut.r < 0 || p.bad[cut.r]) return;
-  const int m = mt * p.tile_rows + row, g1 = cut.last;
-  const bool live = m < cut.nodes * p.G;
+  const TreeRows rows = tree_rows(p, mt * (p.tile_rows / p.tile_base) + row / p.tile_base);
+  const int i = row % p.tile_base, g1 = cut.last;
+  const bool live = rows.used(i, cut.nodes);
   auto part = [&](int g) {
     return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows + row;
   };
@@ -357,8 +355,8 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
     }
   }
   if (!live) return;
-  const int t = m / p.G, head = m - t * p.G;
-  const size_t o = ((size_t)cut.r * p.N + t) * p.Hq + cut.kvh * p.G + head;
+  const size_t o =
+      ((size_t)cut.r * p.N + rows.node(i)) * p.Hq + cut.kvh * p.G + rows.head(i);
   T* out = static_cast<T*>(p.out) + o * D;
   const float inv = den > 0.f ? 1.f / den : 0.f;
   if (lane < kLanes)
@@ -373,12 +371,16 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
                                   int max_pages, bool bf16, int num_sms) {
   TreeSoftmaxPlan pl;
   const int G = Hq / Hkv;
-  const long long rows = (long long)N * G;
-  // bf16: two row tiles share a CTA's keys where there are rows for both and
-  // tensor memory holds both (D <= 128).  96 requests of 61 nodes, 244 rows, D =
-  // 128: TWO_MEASURED
-  pl.tile_rows = !bf16 ? kRowsS : D <= 128 && rows > 128 ? 256 : 128;
-  pl.row_tiles = (int)((rows + pl.tile_rows - 1) / pl.tile_rows);
+  pl.tile_base = bf16 ? 128 : kRowsS;
+  const int per_node = G <= pl.tile_base ? 1 : (G + pl.tile_base - 1) / pl.tile_base;
+  const int nodes = G <= pl.tile_base ? pl.tile_base / G : 1;  // of a row tile
+  const long long tiles = (N + nodes - 1) / nodes * (long long)per_node;
+  // bf16: two row tiles share a CTA's keys where there are two and tensor
+  // memory holds both (D <= 128).  96 requests of 61 nodes, 244 rows, D = 128:
+  // TWO_MEASURED
+  const int per_cta = bf16 && D <= 128 && tiles > 1 ? 2 : 1;
+  pl.tile_rows = per_cta * pl.tile_base;
+  pl.row_tiles = (int)((tiles + per_cta - 1) / per_cta);
   const int per_sm = bf16 || D == 256 ? 1 : D == 128 ? 2 : 4;
   // as many gangs as the GPU holds at once, and no more than there can be tiles
   long long gangs = (long long)num_sms * per_sm / pl.row_tiles;
@@ -422,7 +424,7 @@ cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
 template <typename T, int D>
 cudaError_t launch_finish(const TreeSoftmaxParams& p, cudaStream_t stream) {
   const long long rows = (long long)p.N * p.G;
-  const int tile = (int)(rows < p.tile_rows ? rows : p.tile_rows);  // used rows of a row tile
+  const int tile = rows < p.tile_base ? (int)rows : p.tile_rows;  // rows of a CTA that may be used
   const int gangs = p.gangs * p.row_tiles;
   cudaError_t e;
   if (tile <= 16)
@@ -437,7 +439,17 @@ cudaError_t launch_finish(const TreeSoftmaxParams& p, cudaStream_t stream) {
 
 template <int D>
 cudaError_t launch_d(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream) {
-  cudaError_t e = bf16 ? launch_tree_softmax_tc(p, stream) : launch_simt_d<D>(p, stream);
+  // everything the host has to prepare comes first, the three launches in a row
+  TreeSoftmaxTc tc;
+  if (bf16) {
+    const cudaError_t e = prepare_tree_softmax_tc(p, &tc);
+    if (e != cudaSuccess) return e;
+  }
+  tree_plan_kernel<<<(unsigned)p.R, kPlanThreads, 0, stream>>>(p);
+  note_launches(1);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  e = bf16 ? launch_tree_softmax_tc(p, tc, stream) : launch_simt_d<D>(p, stream);
   if (e != cudaSuccess) return e;
   return bf16 ? launch_finish<__nv_bfloat16, D>(p, stream) : launch_finish<float, D>(p, stream);
 }
@@ -445,10 +457,6 @@ cudaError_t launch_d(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream)
 }  // namespace
 
 cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream) {
-  tree_plan_kernel<<<(unsigned)p.R, kPlanThreads, 0, stream>>>(p);
-  note_launches(1);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
   switch (p.D) {
     case 64: return launch_d<64>(p, bf16, stream);
     case 128: return launch_d<128>(p, bf16, stream);

@@ -2,32 +2,31 @@
 // 5th-generation tensor cores (tcgen05), bf16 in, fp32 accumulate.
 //
 // tree_sched.cuh has how the work is cut: a CTA walks its gang's span of key
-// tiles for its own 128 NQ query rows (row m = node * G + g of a (request, kv
-// head) item: the G query heads of a kv head share its keys).  A piece is a
-// stretch of one item's tiles: prefix tiles through the page table, 64 tokens
-// each, and the item's last tile, the tree's own keys, masked by the rows' path
-// bits.  A piece that covers its item stores the output; another stores a
-// partial one, which tree_finish_kernel merges.
+// tiles for its own row tiles of 128 query rows (the nodes' queries of one kv
+// head's G query heads, which share its keys).  A piece is a stretch of one
+// item's tiles: prefix tiles through the page table, 64 tokens each, and the
+// item's last tile, the tree's own keys, masked by the rows' path bits.  A
+// piece that covers its item stores the output; another stores a partial one,
+// which tree_finish_kernel merges.
 //
 // Serving trees are bound by the keys' and values' bytes: a tile of 64 keys is
 // 256 D bytes for 4 x 128 x 64 D operations, which the tensor cores finish in a
 // third of the time that its share of DRAM bandwidth gives it, padded rows and
-// all.  So the kernel is built as a stream: rings of TMA boxes fill shared
-// memory (a tile takes about a microsecond from issue to arrival), queries,
-// scores, probabilities and output live in tensor memory, and a persistent
-// CTA keeps the rings full across pieces.
+// all.  So the kernel is built as a stream: queries in shared memory, rings of
+// TMA boxes in the rest of it (a tile takes about a microsecond from issue to
+// arrival), scores, probabilities and output in tensor memory, and a persistent
+// CTA that keeps the rings full across pieces.
 //
-// NQ = 2 (more than 128 rows, D <= 128): a second row tile with its own softmax
-// warps shares every staged tile, so that keys and values enter an SM once for
-// 256 rows; the tensor cores alternate between the two, one's products running
-// while the other's softmax does.  Its queries are read from shared memory, so
-// that tensor memory has room for two score buffers per row tile.
+// NQ = 2 (more than one row tile, D <= 128): two row tiles with a softmax group
+// each share every staged tile, so that keys and values enter an SM once for
+// 256 rows.
 //
 // Warp roles (8 warps, 12 with NQ = 2):
 //   warp 0     K producer, warp 6 V producer: a TMA box per (page, 64-column
 //              chunk), a lane each, page ids read one tile ahead; they start
 //              before the plan is known to be done
-//   warps 1, 7 MMA issuers: S_j = Q K_j^T and O += P_j V_j.  Issuing a tile's
+//   warps 1, 7 MMA issuers: S_j = Q K_j^T and O += P_j V_j, and the loads of Q
+//              ahead of a piece's first scores.  Issuing a tile's
 //              products, commits and waits takes one warp as long as a tile may
 //              take, so two share it: NQ = 1 one the scores and one the values,
 //              NQ = 2 a row tile each.  Warp 1 owns the tensor memory.
@@ -58,35 +57,29 @@ constexpr int kSmThreads = 128;        // softmax threads of a row tile
 constexpr int kVWarpT = 6, kMma2WarpT = 7;
 constexpr float kMoveMax = 8.0f;       // log2 units
 
-struct TreeMaps {
-  CUtensorMap kblk, vblk;    // (D, Hkv, N, R)           box (64, 1, 64, 1)
-  CUtensorMap kpool, vpool;  // (D, p, Hkv, num_pages)   box (64, min(p, 64), 1, 1)
-};
-
 template <int D, int NQ>
 struct TreeCfg {
   static constexpr int kThreads = NQ == 1 ? 256 : 384;
   static constexpr int kChunks = D / 64;
   static constexpr int kTileBytes = kChunks * kTreeTile * 128;  // one K (or V) tile
-  // NQ = 1: queries in tensor memory; 2: in shared memory, rows of 128 bytes in
-  // 64-column chunks like the keys
-  static constexpr int kQTile = NQ == 2 ? kChunks * kRowsT * 128 : 0;
-  static constexpr int kKStages = NQ == 2 ? (D == 128 ? 5 : 8) : D == 256 ? 3 : (D == 128 ? 6 : 8);
-  static constexpr int kVStages = NQ == 2 ? (D == 128 ? 5 : 8) : D == 256 ? 4 : (D == 128 ? 7 : 8);
+  static constexpr int kQTile = kChunks * kRowsT * 128;         // one row tile's queries
+  // K and V rings: what the queries leave of shared memory
+  static constexpr int kKStages = D == 256 ? 2 : D == 128 ? (NQ == 2 ? 5 : 6) : 8;
+  static constexpr int kVStages = D == 256 ? 3 : D == 128 ? (NQ == 2 ? 5 : 6) : 8;
   static constexpr int kSmem = NQ * kQTile + (kKStages + kVStages) * kTileBytes + 1024;
-  // tensor memory columns, per row tile: O, Q as bf16 pairs (NQ = 1), the S / P buffers
-  static constexpr int kSBuf = D == 256 || (NQ == 2 && D == 128) ? 2 : 3;
-  static constexpr int kQCol = D;
-  static constexpr int kSCol = NQ == 2 ? D : D + D / 2;
+  // tensor memory columns, per row tile: O, then the S / P buffers
+  static constexpr int kSBuf = D == 256 ? 4 : (NQ == 2 && D == 128 ? 2 : 3);
+  static constexpr int kSCol = D;
   static constexpr int kRowCols = kSCol + kSBuf * kTreeTile;
   static constexpr int kTmemCols = NQ * kRowCols > 256 ? 512 : 256;
   static_assert(NQ * kRowCols <= 512, "tensor memory");
+  static_assert(kSmem + 1024 <= 227 * 1024, "shared memory");
 };
 
 struct TreeShared {
   uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8], v_fix[8];
-  uint64_t s_full[2][3], p_full[2][3], pv_done[2][3];  // per row tile
-  uint64_t q_ready[2], o_final[2], o_free[2];
+  uint64_t s_full[2][4], p_full[2][4], pv_done[2][4];  // per row tile
+  uint64_t q_full[2], o_final[2], o_free[2];
   uint64_t drain[2];  // after a timeout: every MMA issued has completed
   uint32_t tmem_base;
   int abort_flag;
@@ -120,12 +113,12 @@ struct TreeItem {
   }
 };
 
-// The next piece of the span that has rows of this row tile.
-__device__ __forceinline__ bool next_item(const TreeSoftmaxParams& p, TreeCursor& cur, int m0,
+// The next piece of the span whose tree reaches node `node0`, a row tile's first.
+__device__ __forceinline__ bool next_item(const TreeSoftmaxParams& p, TreeCursor& cur, int node0,
                                           TreeItem& it) {
   while (cur.next(p, it.w)) {
     it.nodes = p.node_len[it.w.r];
-    if (m0 >= it.nodes * p.G) continue;
+    if (node0 >= it.nodes) continue;
     it.P = p.prefix_len[it.w.r];
     it.tiles = it.w.j1 - it.w.j0;
     return true;
@@ -137,7 +130,7 @@ __device__ __forceinline__ bool next_item(const TreeSoftmaxParams& p, TreeCursor
 
 template <int D, int NQ>
 __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
-    tree_softmax_tc_kernel(const __grid_constant__ TreeMaps maps, TreeSoftmaxParams p) {
+    tree_softmax_tc_kernel(const __grid_constant__ TreeSoftmaxTc maps, TreeSoftmaxParams p) {
   using C = TreeCfg<D, NQ>;
   constexpr int kSB = C::kSBuf;
   extern __shared__ uint8_t smem_raw[];
@@ -147,7 +140,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
   uint8_t* Vs = Ks + C::kKStages * C::kTileBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
-  const int m0 = mt * (NQ * kRowsT);
+  const int node0 = tree_rows(p, mt * NQ).node0;  // of the CTA's first row tile
 
   if (tid == 0) {
     sh.abort_flag = 0;
@@ -166,7 +159,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         tc::mbar_init(&sh.p_full[t][b], kSmThreads);
         tc::mbar_init(&sh.pv_done[t][b], 1);
       }
-      tc::mbar_init(&sh.q_ready[t], kSmThreads);
+      tc::mbar_init(&sh.q_full[t], 1);
       tc::mbar_init(&sh.o_final[t], 1);
       tc::mbar_init(&sh.o_free[t], kSmThreads);
     }
@@ -201,7 +194,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     const int bx = lane / C::kChunks, ch = lane % C::kChunks;  // this lane's box of a tile
     bool ok = true;
     int g = 0;  // running tile count
-    while (ok && next_item(p, cur, m0, it)) {
+    while (ok && next_item(p, cur, node0, it)) {
       const int32_t* table = p.page_table + (size_t)it.w.r * p.max_pages;
       // the page of this lane's box in tile j (0 where the tile has no such box)
       auto page_of = [&](int j) -> int {
@@ -257,6 +250,9 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     // branch on one lane, each MMA costs some 60 cycles of moves into them.
     const int t = NQ == 2 && warp != 1 ? 1 : 0;  // of row tile t
     const bool scores = NQ == 2 || warp == 1, values = NQ == 2 || warp != 1;
+    const TreeRows rows = tree_rows(p, mt * NQ + t);
+    const int box_heads = min(p.G, kRowsT);
+    const uint32_t q_bytes = (uint32_t)(C::kChunks * 128 * box_heads * rows.nodes);
     const uint32_t base = tmem + t * C::kRowCols;
     const uint32_t id_s = tc::idesc_bf16(kRowsT, kTreeTile, false, false);
     const uint32_t id_o = tc::idesc_bf16(kRowsT, D, false, true);
@@ -267,7 +263,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     int g = 0;              // running tile count of the rings
     int gt = 0, kt = 0;     // of this row tile's buffers, and its pieces
     uint32_t fix_par = 0u;  // per V slot: parity of its next zeroed tile
-    while (ok && next_item(p, cur, m0, it)) {
+    bool q_out = false;     // queries in flight
+    while (ok && next_item(p, cur, node0, it)) {
       const int n = it.tiles;
       auto k_tile = [&](int j) {
         return warp_wait_t(&sh.k_full[(g + j) % C::kKStages],
@@ -283,7 +280,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         }
         return true;
       };
-      if (t == 1 && m0 + kRowsT >= it.nodes * p.G) {  // no rows of this item: pass its tiles on
+      if (rows.node0 >= it.nodes) {  // no rows of this item: pass its tiles on
         for (int j = 0; j < n && ok; ++j) {
           ok = k_tile(j) && v_tile(j);
           if (ok && lane == 0) {
@@ -295,8 +292,26 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         g += n;
         continue;
       }
-      if (scores) ok = warp_wait_t(&sh.q_ready[t], (uint32_t)kt & 1u, &sh.abort_flag);
-      if (!ok) break;
+      if (scores) {
+        // the queries, once the last piece's scores have read theirs
+        if (kt > 0)
+          ok = warp_wait_t(&sh.s_full[t][(gt - 1) % kSB], (uint32_t)((gt - 1) / kSB) & 1u,
+                           &sh.abort_flag);
+        if (!ok) break;
+        if (tc::elect_one()) {
+          uint8_t* dst = Qs + t * C::kQTile;
+          tc::mbar_expect_tx(&sh.q_full[t], q_bytes);
+#pragma unroll
+          for (int c = 0; c < C::kChunks; ++c)
+            tc::tma_load_4d(dst + c * (kRowsT * 128), &maps.q, &sh.q_full[t], c * 64,
+                            it.w.kvh * p.G + rows.head0, rows.node0, it.w.r);
+        }
+        __syncwarp();
+        q_out = true;
+        ok = warp_wait_t(&sh.q_full[t], (uint32_t)kt & 1u, &sh.abort_flag);
+        if (!ok) break;
+        q_out = false;
+      }
       auto issue_s = [&](int j) -> bool {  // S_j = Q K_j^T
         if (!k_tile(j)) return false;
         tc::fence_after_sync();
@@ -307,13 +322,9 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           for (int kk = 0; kk < D / 16; ++kk) {
             const uint64_t kdk =
                 kd + (uint64_t)(((kk >> 2) * (kTreeTile * 128) + (kk & 3) * 32) >> 4);
-            if constexpr (NQ == 2)
-              tc::mma_bf16_ss(base + C::kSCol + sb * kTreeTile,
-                              qdesc0 + (uint64_t)(((kk >> 2) * (kRowsT * 128) + (kk & 3) * 32) >> 4),
-                              kdk, id_s, kk > 0 ? 1u : 0u);
-            else
-              tc::mma_bf16_ts(base + C::kSCol + sb * kTreeTile, base + C::kQCol + kk * 8, kdk, id_s,
-                              kk > 0 ? 1u : 0u);
+            tc::mma_bf16_ss(base + C::kSCol + sb * kTreeTile,
+                            qdesc0 + (uint64_t)(((kk >> 2) * (kRowsT * 128) + (kk & 3) * 32) >> 4),
+                            kdk, id_s, kk > 0 ? 1u : 0u);
           }
           tc::mma_commit(&sh.s_full[t][sb]);
           tc::mma_commit(&sh.k_empty[st]);
@@ -373,6 +384,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     if (!ok && lane == 0) give_up(sh, p.dev_status);
     __syncwarp();
     if (aborted_t(sh)) {
+      if (q_out) tc::mbar_wait(&sh.q_full[t], (uint32_t)kt & 1u, nullptr, 100000000ull);
       uint64_t* drain = &sh.drain[warp == 1 ? 0 : 1];
       if (tc::elect_one()) {
         tc::mma_commit(drain);
@@ -383,61 +395,11 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
   } else {
     // ------------------------------------------------------------ softmax warps
     const int quarter = warp & 3, t = NQ == 2 && warp >= 8 ? 1 : 0;  // of row tile t
-    const int row = quarter * 32 + lane, m = m0 + t * kRowsT + row;
+    const int row = quarter * 32 + lane;
+    const TreeRows rows = tree_rows(p, mt * NQ + t);
+    const int node = rows.node(row), head = rows.head(row);
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-    const uint32_t tmem_o = tmem + t * C::kRowCols;
-    const uint32_t tmem_q = tmem_o + C::kQCol, tmem_s = tmem_o + C::kSCol;
-    const int mt0 = m0 + t * kRowsT;
-    const int node = m / p.G, head = m - node * p.G;
-
-    // this thread's query row of an item (of a used row's warp: the other rows'
-    // outputs are never read)
-    auto q_row = [&](const TreeItem& w) {
-      const bool live = m < w.nodes * p.G;
-      return reinterpret_cast<const uint4*>(
-          static_cast<const __nv_bfloat16*>(p.q) +
-          (((size_t)w.w.r * p.N + (live ? node : 0)) * p.Hq + w.w.kvh * p.G + head) * D);
-    };
-    // Q row where the score product reads it: tensor memory, as bf16 pairs, or
-    // shared memory (128-byte swizzle); unused rows are zero
-    auto load_q = [&](const TreeItem& w) {
-      const bool live = m < w.nodes * p.G;
-      if (__any_sync(0xffffffffu, live)) {
-        const uint4* qrow = q_row(w);
-        constexpr int kWords = D / 2;                      // 32-bit words of a row
-        constexpr int kBatch = kWords < 64 ? kWords : 64;  // words per batch of loads
-#pragma unroll 1
-        for (int c0 = 0; c0 < kWords; c0 += kBatch) {
-          uint32_t q[kBatch];
-#pragma unroll
-          for (int q4 = 0; q4 < kBatch / 4; ++q4) {
-            const uint4 v = live ? qrow[(c0 / 4) + q4] : make_uint4(0u, 0u, 0u, 0u);
-            q[4 * q4] = v.x;
-            q[4 * q4 + 1] = v.y;
-            q[4 * q4 + 2] = v.z;
-            q[4 * q4 + 3] = v.w;
-          }
-          if constexpr (NQ == 2) {
-            uint8_t* dst = Qs + t * C::kQTile + row * 128;
-#pragma unroll
-            for (int q4 = 0; q4 < kBatch / 4; ++q4) {
-              const int u = c0 / 4 + q4;  // 16-byte unit of the row
-              *reinterpret_cast<uint4*>(dst + (u >> 3) * (kRowsT * 128) +
-                                        (((u & 7) ^ (row & 7)) << 4)) =
-                  make_uint4(q[4 * q4], q[4 * q4 + 1], q[4 * q4 + 2], q[4 * q4 + 3]);
-            }
-          } else {
-#pragma unroll
-            for (int c = 0; c < kBatch; c += 16)
-              tc::tmem_st16(tmem_q + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&q[c]));
-          }
-        }
-        if constexpr (NQ == 2) tc::fence_async_smem();
-        else tc::tmem_st_wait();
-      }
-      tc::fence_before_sync();
-      tc::mbar_arrive(&sh.q_ready[t]);
-    };
+    const uint32_t tmem_o = tmem + t * C::kRowCols, tmem_s = tmem_o + C::kSCol;
 
     bool ok = true;
     int g = 0;  // running tile count (of row tile 0: the rings' too)
@@ -460,24 +422,14 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       tc::mbar_arrive(&sh.v_fix[st]);
       return true;
     };
-    bool have = next_item(p, cur, mt0, it);
-    if (have) load_q(it);
+    bool have = next_item(p, cur, rows.node0, it);
     pdl_wait();  // the plan: paths, and which requests are bad
     if (tid == 64) pdl_launch_next();
     for (int k = 0; have; ++k) {
-      const bool live = m < it.nodes * p.G;
+      const bool live = rows.used(row, it.nodes);
       const bool warp_live = __any_sync(0xffffffffu, live);
       const uint64_t path = live ? p.anc[(size_t)it.w.r * p.N + node] : 0ull;
       const bool skip = p.bad[it.w.r] != 0;
-      // the next piece, its queries on their way to L2 before they are needed
-      TreeItem nx = it;
-      const bool more = next_item(p, cur, mt0, nx);
-      if (more && m < nx.nodes * p.G) {
-        const char* x = reinterpret_cast<const char*>(q_row(nx));
-#pragma unroll
-        for (int c = 0; c < D * 2; c += 128)
-          asm volatile("prefetch.global.L2 [%0];" ::"l"(x + c));
-      }
       float m_run = -INFINITY, l_run = 0.f;
       for (int j = 0; j < it.tiles; ++j) {
         const int gg = g + j, sb = gg % kSB;
@@ -561,8 +513,6 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       }
       g += it.tiles;
       if (ok && aborted_t(sh)) ok = false;
-      // the next piece's queries: every S product of this one has completed
-      if (ok && more) load_q(nx);
       if (ok && !warp_wait_t(&sh.o_final[t], (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
       if (!ok) break;
       if (warp_live) {
@@ -611,8 +561,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       }
       tc::fence_before_sync();
       tc::mbar_arrive(&sh.o_free[t]);
-      have = more;
-      it = nx;
+      have = next_item(p, cur, rows.node0, it);
     }
     if (!ok) give_up(sh, p.dev_status);
   }
@@ -643,11 +592,9 @@ PFN_cuTensorMapEncodeTiled_v12000 tree_encode_fn() {
 }
 
 bool encode(CUtensorMap* m, const void* ptr, const cuuint64_t (&dims)[4],
-            const cuuint64_t (&strides)[3], cuuint32_t rows, int rows_dim) {
+            const cuuint64_t (&strides)[3], const cuuint32_t (&box)[4]) {
   auto fn = tree_encode_fn();
   if (!fn) return false;
-  cuuint32_t box[4] = {64, 1, 1, 1};
-  box[rows_dim] = rows;
   const cuuint32_t es[4] = {1, 1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -656,30 +603,9 @@ bool encode(CUtensorMap* m, const void* ptr, const cuuint64_t (&dims)[4],
 }
 
 template <int D, int NQ>
-cudaError_t launch_tc_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
+cudaError_t launch_tc_d(const TreeSoftmaxParams& p, const TreeSoftmaxTc& maps,
+                        cudaStream_t stream) {
   using C = TreeCfg<D, NQ>;
-  TreeMaps maps;
-  const cuuint64_t row = D * 2;
-  {
-    const cuuint64_t dims[4] = {D, (cuuint64_t)p.Hkv, (cuuint64_t)p.N, (cuuint64_t)p.R};
-    const cuuint64_t str[3] = {row, p.Hkv * row, (cuuint64_t)p.N * p.Hkv * row};
-    if (!encode(&maps.kblk, p.k_blk, dims, str, kTreeTile, 2) ||
-        !encode(&maps.vblk, p.v_blk, dims, str, kTreeTile, 2))
-      return cudaErrorInvalidValue;
-  }
-  {
-    // page ids are checked beside the stream: one outside the pool reads as
-    // zeros.  Without a pool the maps show one row of the nodes' tensors.
-    const bool none = p.num_pages == 0 || p.max_pages == 0;
-    const cuuint64_t dims[4] = {D, (cuuint64_t)(none ? 1 : p.page_size),
-                                (cuuint64_t)(none ? 1 : p.Hkv),
-                                (cuuint64_t)(none ? 1 : p.num_pages)};
-    const cuuint64_t str[3] = {row, p.page_size * row, (cuuint64_t)p.Hkv * p.page_size * row};
-    const cuuint32_t rows = p.page_size < kTreeTile ? p.page_size : kTreeTile;
-    if (!encode(&maps.kpool, none ? p.k_blk : p.k_pool, dims, str, rows, 1) ||
-        !encode(&maps.vpool, none ? p.v_blk : p.v_pool, dims, str, rows, 1))
-      return cudaErrorInvalidValue;
-  }
   cudaError_t e = cudaFuncSetAttribute(tree_softmax_tc_kernel<D, NQ>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   if (e != cudaSuccess) return e;
@@ -691,12 +617,45 @@ cudaError_t launch_tc_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, cudaStream_t stream) {
+cudaError_t prepare_tree_softmax_tc(const TreeSoftmaxParams& p, TreeSoftmaxTc* m) {
+  const cuuint64_t D = p.D, row = D * 2;
+  {  // (D, heads, N, R): the nodes' rows; a box is 64 columns of a row tile
+    const cuuint64_t dims[4] = {D, (cuuint64_t)p.Hq, (cuuint64_t)p.N, (cuuint64_t)p.R};
+    const cuuint64_t str[3] = {row, p.Hq * row, (cuuint64_t)p.N * p.Hq * row};
+    const cuuint32_t heads = p.G < kRowsT ? p.G : kRowsT;
+    const cuuint32_t box[4] = {64, heads, p.G < kRowsT ? kRowsT / heads : 1, 1};
+    if (!encode(&m->q, p.q, dims, str, box)) return cudaErrorInvalidValue;
+  }
+  {
+    const cuuint64_t dims[4] = {D, (cuuint64_t)p.Hkv, (cuuint64_t)p.N, (cuuint64_t)p.R};
+    const cuuint64_t str[3] = {row, p.Hkv * row, (cuuint64_t)p.N * p.Hkv * row};
+    const cuuint32_t box[4] = {64, 1, kTreeTile, 1};
+    if (!encode(&m->kblk, p.k_blk, dims, str, box) || !encode(&m->vblk, p.v_blk, dims, str, box))
+      return cudaErrorInvalidValue;
+  }
+  // (D, page rows, kv heads, pages).  Page ids are checked beside the stream: one
+  // outside the pool reads as zeros.  Without a pool the maps show one row of the
+  // nodes' tensors.
+  const bool none = p.num_pages == 0 || p.max_pages == 0;
+  const cuuint64_t dims[4] = {D, (cuuint64_t)(none ? 1 : p.page_size),
+                              (cuuint64_t)(none ? 1 : p.Hkv), (cuuint64_t)(none ? 1 : p.num_pages)};
+  const cuuint64_t str[3] = {row, p.page_size * row, (cuuint64_t)p.Hkv * p.page_size * row};
+  const cuuint32_t box[4] = {64, (cuuint32_t)(p.page_size < kTreeTile ? p.page_size : kTreeTile), 1,
+                             1};
+  if (!encode(&m->kpool, none ? p.k_blk : p.k_pool, dims, str, box) ||
+      !encode(&m->vpool, none ? p.v_blk : p.v_pool, dims, str, box))
+    return cudaErrorInvalidValue;
+  return cudaSuccess;
+}
+
+cudaError_t launch_tree_softmax_tc(const TreeSoftmaxParams& p, const TreeSoftmaxTc& maps,
+                                   cudaStream_t stream) {
   const bool two = p.tile_rows == 2 * kRowsT;
   switch (p.D) {
-    case 64: return two ? launch_tc_d<64, 2>(p, stream) : launch_tc_d<64, 1>(p, stream);
-    case 128: return two ? launch_tc_d<128, 2>(p, stream) : launch_tc_d<128, 1>(p, stream);
-    case 256: return launch_tc_d<256, 1>(p, stream);
+    case 64: return two ? launch_tc_d<64, 2>(p, maps, stream) : launch_tc_d<64, 1>(p, maps, stream);
+    case 128:
+      return two ? launch_tc_d<128, 2>(p, maps, stream) : launch_tc_d<128, 1>(p, maps, stream);
+    case 256: return launch_tc_d<256, 1>(p, maps, stream);
     default: return cudaErrorInvalidValue;
   }
 }

@@ -64,6 +64,11 @@ SOFTMAX_SHAPES = [
     (33, 7, 1, 64, 16, [77, 15, 16, 17]),  # a group that does not divide a row tile
     (5, 40, 1, 128, 64, [200, 333]),
     (7, 3, 3, 256, 128, [1000, 2, 0]),
+    (64, 12, 4, 128, 16, [70, 129]),   # three heads a group, two row tiles of whole nodes
+    (61, 10, 2, 64, 64, [300, 31]),    # five
+    (50, 7, 1, 256, 32, [100]),        # seven, three row tiles
+    (3, 150, 1, 64, 16, [70, 0]),      # more heads than a row tile has rows
+    (5, 260, 2, 128, 64, [65, 300]),
 ]
 
 
