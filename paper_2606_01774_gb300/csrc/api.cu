@@ -613,6 +613,9 @@ flare_status flare_tree_softmax_attn(const flare_softmax_desc* d, const void* q,
   char* ws = static_cast<char*>(workspace);
   p.bad = reinterpret_cast<int32_t*>(ws + plan.bad_off);
   p.cuts = ws + plan.cuts_off;
+  p.counts = reinterpret_cast<int32_t*>(ws + plan.counts_off);
+  p.n_counts = plan.n_counts;
+  p.join = plan.join;
   p.anc = reinterpret_cast<uint64_t*>(ws + plan.anc_off);
   p.part_o = reinterpret_cast<float*>(ws + plan.part_o_off);
   p.part_lse = reinterpret_cast<float*>(ws + plan.part_lse_off);

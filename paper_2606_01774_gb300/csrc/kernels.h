@@ -156,6 +156,9 @@ struct TreeSoftmaxParams {
   int tile_base, tile_rows;   // query rows of a row tile, and of a CTA's one or two
   int32_t* bad;               // [R] whether a request is skipped
   void* cuts;                 // [gangs] TreeCut: the item that a gang leaves unfinished
+  int join;                   // pieces of an item that its last one merges itself
+  int n_counts;
+  int32_t* counts;            // [gangs,row_tiles,1 or 2] stored pieces of the item a gang starts
   uint64_t* anc;              // [R,N] path of each node as a bit set
   float* part_o;              // [2 gangs row_tiles][tile_rows][D] partial outputs
   float* part_lse;            // [2 gangs row_tiles][tile_rows]
@@ -163,8 +166,8 @@ struct TreeSoftmaxParams {
 };
 
 struct TreeSoftmaxPlan {
-  int gangs, row_tiles, tile_base, tile_rows;
-  size_t bad_off, cuts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
+  int gangs, row_tiles, tile_base, tile_rows, n_counts, join;
+  size_t bad_off, cuts_off, counts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
 };
 
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,

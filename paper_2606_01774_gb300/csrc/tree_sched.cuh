@@ -24,6 +24,10 @@
 namespace flare {
 
 constexpr int kTreeTile = 64;  // keys per tile
+// Pieces of an item that its last piece merges itself (bf16).  More of them,
+// or a prefix over the whole GPU, leave few CTAs to read many partials:
+// tree_finish_kernel takes those.
+constexpr int kTreeJoin = 4;
 
 // The query rows of row tile `tile` of a (request, kv head) item: whole nodes
 // with their G query heads, or, with more heads than a tile has rows, some of
@@ -51,7 +55,8 @@ __device__ __forceinline__ TreeRows tree_rows(const TreeSoftmaxParams& p, int ti
 struct TreeSpanShared {
   long long warp_sum[32];
   long long lo, hi, off;  // the span, and the first tile's offset in its request
-  int r;
+  long long total;        // tiles of the batch
+  int gangs, r;
 };
 
 // The item that a gang starts and leaves unfinished, to be merged: its request
@@ -107,6 +112,18 @@ __device__ __forceinline__ int tree_gangs(const TreeSoftmaxParams& p, long long 
   return total < p.gangs ? (int)total : p.gangs;
 }
 
+// First row of a CTA's partial outputs for its piece of an item that gang g0
+// starts: g0's own is its last piece (slot 1), the others' their first.
+__device__ __forceinline__ size_t tree_part(const TreeSoftmaxParams& p, int g, int g0, int mt) {
+  return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows;
+}
+// Columns 4 c4 .. 4 c4 + 3 of row `row` of the partial output whose first row
+// is `part`: rows run fastest, since it is written and read by a thread per row.
+__device__ __forceinline__ float4* tree_part_at(const TreeSoftmaxParams& p, size_t part, int row,
+                                                int c4) {
+  return reinterpret_cast<float4*>(p.part_o + part * p.D) + (size_t)c4 * p.tile_rows + row;
+}
+
 // The gang whose span holds tile x of `total`.
 __device__ __forceinline__ int tree_gang_of(long long x, long long total, int gangs) {
   return (int)(((x + 1) * gangs - 1) / total);
@@ -147,6 +164,8 @@ __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int 
   if (tid == 0) {
     sh.lo = lo;
     sh.hi = hi;
+    sh.total = total;
+    sh.gangs = gangs;
   }
   if (lo < hi && before <= lo && lo < before + sum) {  // this thread holds the first request
     long long at = before;

@@ -26,6 +26,7 @@ constexpr int kPlanThreads = 128;
 constexpr int kRowsS = 32;      // query rows per CTA of the fp32 kernel
 constexpr int kThreadsS = 128;
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kMaxGangs = 1024;
 
 __device__ __forceinline__ void store4(float* x, float4 v) { *reinterpret_cast<float4*>(x) = v; }
 __device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
@@ -39,6 +40,8 @@ __device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
 __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxParams p) {
   pdl_launch_next();
   const int r = blockIdx.x, tid = threadIdx.x;
+  for (int i = r * kPlanThreads + tid; i < p.n_counts; i += gridDim.x * kPlanThreads)
+    p.counts[i] = 0;
   const int n = p.node_len[r], P = p.prefix_len[r];
   int bad = 0;
   if (n < 0 || n > p.N) bad |= FLARE_DEV_BAD_TREE;
@@ -236,8 +239,8 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
       for (int c = 0; c < kC; ++c) {
         const float4 a = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv,
                                      acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
-        float* dst = whole ? static_cast<float*>(p.out) + o * D : p.part_o + (part + row) * D;
-        store4(dst + 4 * x + 64 * c, a);
+        if (whole) store4(static_cast<float*>(p.out) + o * D + 4 * x + 64 * c, a);
+        else *tree_part_at(p, part, row, x + 16 * c) = a;
       }
       if (x == 0) {
         if (!whole) p.part_lse[part + row] = l2;
@@ -247,22 +250,20 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   }
 }
 
-// Writes the unused nodes' rows, and merges the pieces of items that several
-// gangs share: a CTA per gang, row tile and group of rows takes the item that
-// its gang leaves unfinished.  A row's pieces are that gang's last (slot 1) and
-// the first of each later one (slot 0), in gang order, whatever the timing:
+// Writes the unused nodes' rows, and merges the items that the attention left
+// in pieces (more than p.join of them), in gang order, whatever the timing:
 //     out = sum_s 2^(lse_s - lse) out_s.
-// WARPS warps share a row: one, with eight rows to a CTA, or eight, each with
-// every eighth piece, where rows are few and may have many pieces.
-template <typename T, int D, int WARPS>
+// A thread takes four columns of a row; PARTS threads share them, each with
+// every PARTS-th piece: one, or eight, where rows are few and may have many
+// pieces.
+template <typename T, int D, int PARTS>
 __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
-  constexpr int kV = D >= 128 ? D / 128 : 1;  // 16-byte groups per lane
-  constexpr int kLanes = D / (4 * kV);        // lanes that hold columns
-  constexpr int kRowsPerCta = 8 / WARPS;
-  __shared__ float red_o[WARPS > 1 ? 8 : 1][D];
-  __shared__ float red_l[8], red_d[8];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int sub = warp % WARPS;
+  constexpr int kPer = 256 / PARTS;  // (row, column group) elements per CTA and pass
+  constexpr int kIn = PARTS > 1 ? 8 : 4;  // pieces in flight per thread
+  __shared__ int cut_of[kMaxGangs], in_warp[8];
+  __shared__ float4 red_o[PARTS > 1 ? 256 : 1];
+  __shared__ float2 red_l[PARTS > 1 ? 256 : 1];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // unused nodes' rows, a node per warp (the attention kernel waited for the
   // plan before it let this one start)
   for (long long u = (long long)blockIdx.x * 8 + warp; u < (long long)p.R * p.N;
@@ -275,96 +276,86 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
     if (p.lse)
       for (int e = lane; e < p.Hq; e += 32) p.lse[u * p.Hq + e] = -INFINITY;
   }
-  const int per_tile = gridDim.x / (p.gangs * p.row_tiles);  // CTAs per gang and row tile
-  const int part_id = blockIdx.x % per_tile;
-  const int g0 = blockIdx.x / per_tile / p.row_tiles, mt = blockIdx.x / per_tile % p.row_tiles;
-  const int row = part_id * kRowsPerCta + warp / WARPS;  // of the row tile
-  pdl_wait();                                            // the attention
-  const TreeCut cut = static_cast<const TreeCut*>(p.cuts)[g0];
-  if (cut.r < 0 || p.bad[cut.r]) return;
-  const TreeRows rows = tree_rows(p, mt * (p.tile_rows / p.tile_base) + row / p.tile_base);
-  const int i = row % p.tile_base, g1 = cut.last;
-  const bool live = rows.used(i, cut.nodes);
-  auto part = [&](int g) {
-    return (((size_t)g * p.row_tiles + mt) * 2 + (g == g0 ? 1 : 0)) * p.tile_rows + row;
-  };
-  // this warp's pieces: running maximum, sum of weights, weighted output
-  float mx = -INFINITY, den = 0.f;
-  float4 acc[kV];
-#pragma unroll
-  for (int v = 0; v < kV; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (live) {
-    constexpr int kIn = WARPS > 1 ? 8 : 2;  // pieces in flight
-    for (int g = g0 + sub; g <= g1; g += WARPS * kIn) {
-      float l[kIn];
-      float4 x[kIn][kV];
-#pragma unroll
-      for (int u = 0; u < kIn; ++u) {
-        const int gg = g + u * WARPS;
-        l[u] = gg <= g1 ? p.part_lse[part(gg)] : -INFINITY;
-#pragma unroll
-        for (int v = 0; v < kV; ++v)
-          x[u][v] = gg <= g1 && lane < kLanes ? *reinterpret_cast<const float4*>(
-                                                    p.part_o + part(gg) * D + 4 * (lane + 32 * v))
-                                              : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-#pragma unroll
-      for (int u = 0; u < kIn; ++u) {
-        if (l[u] == -INFINITY) continue;  // a piece that the row sees nothing of
-        const float mn = fmaxf(mx, l[u]);
-        const float corr = exp2f(mx - mn), e = exp2f(l[u] - mn);
-        den = den * corr + e;
-        mx = mn;
-#pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          acc[v].x = fmaf(e, x[u][v].x, acc[v].x * corr);
-          acc[v].y = fmaf(e, x[u][v].y, acc[v].y * corr);
-          acc[v].z = fmaf(e, x[u][v].z, acc[v].z * corr);
-          acc[v].w = fmaf(e, x[u][v].w, acc[v].w * corr);
-        }
-      }
+  pdl_wait();  // the attention
+  const TreeCut* cuts = static_cast<const TreeCut*>(p.cuts);
+  int n_cuts = 0;  // in gang order, the same in every CTA
+  for (int base = 0; base < p.gangs; base += 256) {
+    bool has = false;
+    if (base + tid < p.gangs) {
+      const TreeCut c = cuts[base + tid];
+      has = c.r >= 0 && c.last - (base + tid) >= p.join && !p.bad[c.r];
     }
-  }
-  if constexpr (WARPS > 1) {
-    if (lane < kLanes)
-#pragma unroll
-      for (int v = 0; v < kV; ++v)
-        *reinterpret_cast<float4*>(&red_o[warp][4 * (lane + 32 * v)]) = acc[v];
-    if (lane == 0) {
-      red_l[warp] = mx;
-      red_d[warp] = den;
-    }
+    const unsigned mask = __ballot_sync(0xffffffffu, has);
+    if (lane == 0) in_warp[warp] = __popc(mask);
     __syncthreads();
-    if (sub != 0) return;
+    int at = n_cuts;
 #pragma unroll
-    for (int u = 1; u < WARPS; ++u) {
-      const float l = red_l[u];
-      if (l == -INFINITY) continue;
-      const float mn = fmaxf(mx, l), corr = exp2f(mx - mn), e = exp2f(l - mn);
-      den = den * corr + e * red_d[u];
-      mx = mn;
-      if (lane < kLanes)
-#pragma unroll
-        for (int v = 0; v < kV; ++v) {
-          const float4 y = *reinterpret_cast<const float4*>(&red_o[u][4 * (lane + 32 * v)]);
-          acc[v].x = fmaf(e, y.x, acc[v].x * corr);
-          acc[v].y = fmaf(e, y.y, acc[v].y * corr);
-          acc[v].z = fmaf(e, y.z, acc[v].z * corr);
-          acc[v].w = fmaf(e, y.w, acc[v].w * corr);
-        }
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) at += in_warp[w];
+      n_cuts += in_warp[w];
     }
+    if (has) cut_of[at + __popc(mask & ((1u << lane) - 1))] = base + tid;
+    __syncthreads();
   }
-  if (!live) return;
-  const size_t o =
-      ((size_t)cut.r * p.N + rows.node(i)) * p.Hq + cut.kvh * p.G + rows.head(i);
-  T* out = static_cast<T*>(p.out) + o * D;
-  const float inv = den > 0.f ? 1.f / den : 0.f;
-  if (lane < kLanes)
+  // rows that may be used, rounded up so that elements split by shifts
+  const int used = p.N * p.G < p.tile_rows ? p.N * p.G : p.tile_rows;
+  int shift = 0;
+  while ((1 << shift) < used) ++shift;
+  const int passes = ((D / 4 << shift) + kPer - 1) / kPer;
+  const long long units = (long long)n_cuts * p.row_tiles * passes;
+  for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int at = (int)(unit / passes), e = (int)(unit - (long long)at * passes) * kPer + tid % kPer;
+    const int g0 = cut_of[at / p.row_tiles], mt = at % p.row_tiles;
+    const int row = e & ((1 << shift) - 1), c4 = e >> shift, sub = tid / kPer;
+    const TreeCut cut = cuts[g0];
+    const TreeRows rows = tree_rows(p, mt * (p.tile_rows / p.tile_base) + row / p.tile_base);
+    const int i = row % p.tile_base;
+    const bool live = c4 < D / 4 && row < p.tile_rows && rows.used(i, cut.nodes);
+    // this thread's pieces: running maximum, sum of weights, weighted output
+    float mx = -INFINITY, den = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto take = [&](float l, float d, float4 x) {
+      if (l == -INFINITY) return;  // the row sees nothing of it
+      const float mn = fmaxf(mx, l), corr = exp2f(mx - mn), f = exp2f(l - mn);
+      den = den * corr + f * d;
+      mx = mn;
+      acc.x = fmaf(f, x.x, acc.x * corr);
+      acc.y = fmaf(f, x.y, acc.y * corr);
+      acc.z = fmaf(f, x.z, acc.z * corr);
+      acc.w = fmaf(f, x.w, acc.w * corr);
+    };
+    if (live) {
+      for (int g = g0 + sub; g <= cut.last; g += PARTS * kIn) {
+        float l[kIn];
+        float4 x[kIn];
 #pragma unroll
-    for (int v = 0; v < kV; ++v)
-      store4(out + 4 * (lane + 32 * v),
-             make_float4(acc[v].x * inv, acc[v].y * inv, acc[v].z * inv, acc[v].w * inv));
-  if (lane == 0 && p.lse) p.lse[o] = den > 0.f ? (mx + log2f(den)) * kLn2 : -INFINITY;
+        for (int u = 0; u < kIn; ++u) {
+          const int gg = g + u * PARTS;
+          const size_t part = tree_part(p, gg, g0, mt);
+          l[u] = gg <= cut.last ? p.part_lse[part + row] : -INFINITY;
+          x[u] = gg <= cut.last ? *tree_part_at(p, part, row, c4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < kIn; ++u) take(l[u], 1.f, x[u]);
+      }
+    }
+    if constexpr (PARTS > 1) {
+      __syncthreads();  // the previous unit's are read
+      red_o[tid] = acc;
+      red_l[tid] = make_float2(mx, den);
+      __syncthreads();
+      if (sub != 0) continue;
+#pragma unroll
+      for (int u = 1; u < PARTS; ++u)
+        take(red_l[u * kPer + tid].x, red_l[u * kPer + tid].y, red_o[u * kPer + tid]);
+    }
+    if (!live) continue;
+    const size_t o = ((size_t)cut.r * p.N + rows.node(i)) * p.Hq + cut.kvh * p.G + rows.head(i);
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    store4(static_cast<T*>(p.out) + o * D + 4 * c4,
+           make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
+    if (c4 == 0 && p.lse) p.lse[o] = den > 0.f ? (mx + log2f(den)) * kLn2 : -INFINITY;
+  }
 }
 
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,
@@ -387,15 +378,20 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
   const long long most =
       (long long)R * Hkv * (((long long)max_pages * page_size + kTreeTile - 1) / kTreeTile + 1);
   if (gangs > most) gangs = most;
+  if (gangs > kMaxGangs) gangs = kMaxGangs;
   if (gangs < 1) gangs = 1;
   pl.gangs = (int)gangs;
   const size_t slots = (size_t)2 * pl.gangs * pl.row_tiles * pl.tile_rows;
+  pl.join = bf16 ? kTreeJoin : 0;
+  pl.n_counts = bf16 ? pl.gangs * pl.row_tiles * (pl.tile_rows / pl.tile_base) : 0;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t at = 0;
   pl.bad_off = at;
   at += up((size_t)R * sizeof(int32_t));
   pl.cuts_off = at;
   at += up((size_t)pl.gangs * sizeof(TreeCut));
+  pl.counts_off = at;
+  at += up((size_t)pl.n_counts * sizeof(int32_t));
   pl.anc_off = at;
   at += up((size_t)R * N * sizeof(uint64_t));
   pl.part_o_off = at;
@@ -423,16 +419,11 @@ cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
 
 template <typename T, int D>
 cudaError_t launch_finish(const TreeSoftmaxParams& p, cudaStream_t stream) {
-  const long long rows = (long long)p.N * p.G;
-  const int tile = rows < p.tile_base ? (int)rows : p.tile_rows;  // rows of a CTA that may be used
-  const int gangs = p.gangs * p.row_tiles;
-  cudaError_t e;
-  if (tile <= 16)
-    e = pdl_launch(tree_finish_kernel<T, D, 8>, dim3((unsigned)(gangs * tile)), 256, 0, stream,
-                   true, 1, p);
-  else
-    e = pdl_launch(tree_finish_kernel<T, D, 1>, dim3((unsigned)(gangs * ((tile + 7) / 8))), 256, 0,
-                   stream, true, 1, p);
+  const dim3 grid(4 * kNumSMs);
+  const cudaError_t e =
+      (long long)p.N * p.G <= 16
+          ? pdl_launch(tree_finish_kernel<T, D, 8>, grid, 256, 0, stream, true, 1, p)
+          : pdl_launch(tree_finish_kernel<T, D, 1>, grid, 256, 0, stream, true, 1, p);
   note_launches(1);
   return e != cudaSuccess ? e : cudaGetLastError();
 }

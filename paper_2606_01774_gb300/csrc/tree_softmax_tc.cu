@@ -6,8 +6,10 @@
 // head's G query heads, which share its keys).  A piece is a stretch of one
 // item's tiles: prefix tiles through the page table, 64 tokens each, and the
 // item's last tile, the tree's own keys, masked by the rows' path bits.  A
-// piece that covers its item stores the output; another stores a partial one,
-// which tree_finish_kernel merges.
+// piece that covers its item stores the output.  Of an item in up to kTreeJoin
+// pieces the one that ends last takes the others' partial outputs in, its own
+// still in tensor memory (in gang order, whichever it is); the pieces of longer
+// items are merged by tree_finish_kernel, over more of the GPU.
 //
 // Serving trees are bound by the keys' and values' bytes: a tile of 64 keys is
 // 256 D bytes for 4 x 128 x 64 D operations, which the tensor cores finish in a
@@ -83,6 +85,7 @@ struct TreeShared {
   uint64_t drain[2];  // after a timeout: every MMA issued has completed
   uint32_t tmem_base;
   int abort_flag;
+  int last[2];  // whether this CTA's piece of an item ended last
   TreeSpanShared span;
 };
 
@@ -99,6 +102,30 @@ __device__ __forceinline__ void give_up(TreeShared& sh, int32_t* status) {
     sh.abort_flag = 1;
     flag(status, FLARE_DEV_WAIT_TIMEOUT);
   }
+}
+
+// Barrier `id` over a row tile's 128 softmax threads, with an OR.
+__device__ __forceinline__ bool group_or(uint32_t id, bool x) {
+  int r;
+  asm volatile(
+      "{\n"
+      " .reg .pred p, q;\n"
+      " setp.ne.s32 p, %2, 0;\n"
+      " bar.red.or.pred q, %1, 128, p;\n"
+      " selp.s32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"(id), "r"((int)x)
+      : "memory");
+  return r != 0;
+}
+
+// 32 bytes, a memory sector, per thread and instruction: the output's rows are
+// strided across a warp's lanes.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&x)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]),
+               "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+               : "memory");
 }
 
 // A piece with what the roles ask of its request.
@@ -400,6 +427,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     const int node = rows.node(row), head = rows.head(row);
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const uint32_t tmem_o = tmem + t * C::kRowCols, tmem_s = tmem_o + C::kSCol;
+    const bool out32 = ((uintptr_t)p.out & 31u) == 0;  // the caller's tensors: 16 bytes at least
 
     bool ok = true;
     int g = 0;  // running tile count (of row tile 0: the rings' too)
@@ -514,15 +542,35 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       g += it.tiles;
       if (ok && aborted_t(sh)) ok = false;
       if (ok && !warp_wait_t(&sh.o_final[t], (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
-      if (!ok) break;
-      if (warp_live) {
-        tc::fence_after_sync();
-        const bool whole = it.w.whole();
-        const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-        const float l2 = l_run > 0.f ? m_run + log2f(l_run) : -INFINITY;
-        const size_t orow = ((size_t)it.w.r * p.N + node) * p.Hq + it.w.kvh * p.G + head;
-        const size_t prow =
-            ((size_t)blockIdx.x * 2 + it.w.slot()) * (NQ * kRowsT) + t * kRowsT + row;
+      if (group_or(2 + t, !ok)) {  // the row tile's four warps agree
+        ok = false;
+        break;
+      }
+      tc::fence_after_sync();
+      const bool whole = it.w.whole();
+      const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+      const float l2 = l_run > 0.f ? m_run + log2f(l_run) : -INFINITY;
+      // the gangs that share the item: it starts j0 tiles before this span, or
+      // ends j1 tiles before this span's end
+      int g0 = gang, g1 = gang;
+      if (!whole) {
+        const long long s0 = it.w.slot() ? sh.span.hi - it.w.j1 : sh.span.lo - it.w.j0;
+        g0 = tree_gang_of(s0, sh.span.total, sh.span.gangs);
+        g1 = tree_gang_of(s0 + it.w.n - 1, sh.span.total, sh.span.gangs);
+      }
+      const bool joins = !whole && !skip && g1 - g0 < kTreeJoin;
+      bool store = !whole && !skip, merge = false;  // a partial output; the item's
+      int32_t* count = p.counts + ((size_t)g0 * p.row_tiles + mt) * NQ + t;
+      if (joins) {  // with every other piece stored, this one need not be
+        if (row == 0)
+          sh.last[t] = atomicAdd(count, 0) == g1 - g0;
+        tc::named_bar_sync(2 + t, kSmThreads);
+        merge = sh.last[t] != 0;
+        store = !merge;
+      }
+      if (store && warp_live) {
+        const size_t part = tree_part(p, gang, g0, mt);
+        const int trow = t * kRowsT + row;
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += 64) {
           uint32_t o[64];
@@ -530,33 +578,102 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           for (int c = 0; c < 64; c += 16)
             tc::tmem_ld16(tmem_o + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&o[c]));
           tc::tmem_ld_wait();
-          if (!live || skip) continue;
-          if (whole) {
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + orow * D + c0);
+          if (!live) continue;
 #pragma unroll
-            for (int c = 0; c < 64; c += 8) {
-              uint32_t h[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 h2 =
-                    __floats2bfloat162_rn(__uint_as_float(o[c + 2 * i]) * inv,
-                                          __uint_as_float(o[c + 2 * i + 1]) * inv);
-                h[i] = *reinterpret_cast<const uint32_t*>(&h2);
-              }
-              dst[c / 8] = make_uint4(h[0], h[1], h[2], h[3]);
-            }
-          } else {
-            float4* dst = reinterpret_cast<float4*>(p.part_o + prow * D + c0);
-#pragma unroll
-            for (int c = 0; c < 64; c += 4)
-              dst[c / 4] = make_float4(__uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
-                                       __uint_as_float(o[c + 2]) * inv,
-                                       __uint_as_float(o[c + 3]) * inv);
-          }
+          for (int c = 0; c < 64; c += 4)
+            *tree_part_at(p, part, trow, (c0 + c) / 4) = make_float4(
+                __uint_as_float(o[c]) * inv, __uint_as_float(o[c + 1]) * inv,
+                __uint_as_float(o[c + 2]) * inv, __uint_as_float(o[c + 3]) * inv);
         }
-        if (live && !skip) {
-          if (!whole) p.part_lse[prow] = l2;
-          else if (p.lse) p.lse[orow] = l2 * 0.6931471805599453f;
+        if (live) p.part_lse[part + trow] = l2;
+      }
+      if (joins && store) {
+        __threadfence();
+        tc::named_bar_sync(2 + t, kSmThreads);
+        if (row == 0) sh.last[t] = atomicAdd(count, 1) == g1 - g0;
+        tc::named_bar_sync(2 + t, kSmThreads);
+        merge = sh.last[t] != 0;
+      }
+      if ((whole && !skip) || merge) {
+        if (warp_live) {
+          if (merge) __threadfence();
+          // weights of the item's pieces, in gang order
+          float wt[kTreeJoin];
+          float top = -INFINITY, den = 0.f;
+          const int trow = t * kRowsT + row;
+#pragma unroll
+          for (int u = 0; u < kTreeJoin; ++u) {
+            wt[u] = -INFINITY;
+            if (g0 + u <= g1 && live)
+              wt[u] = g0 + u == gang ? l2 : __ldcg(p.part_lse + tree_part(p, g0 + u, g0, mt) + trow);
+            top = fmaxf(top, wt[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kTreeJoin; ++u) {
+            wt[u] = wt[u] == -INFINITY ? 0.f : exp2f(wt[u] - top);
+            den += wt[u];
+          }
+          const float norm = den > 0.f ? 1.f / den : 0.f;
+          const size_t orow = ((size_t)it.w.r * p.N + node) * p.Hq + it.w.kvh * p.G + head;
+          __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + orow * D;
+#pragma unroll 1
+          for (int c0 = 0; c0 < D; c0 += 32) {
+            uint32_t o[32];
+            tc::tmem_ld16(tmem_o + lane_off + c0, *reinterpret_cast<uint32_t(*)[16]>(&o[0]));
+            tc::tmem_ld16(tmem_o + lane_off + c0 + 16, *reinterpret_cast<uint32_t(*)[16]>(&o[16]));
+            tc::tmem_ld_wait();
+            if (!live) continue;
+            if (whole) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * inv);
+            } else {
+              float acc[32];
+#pragma unroll
+              for (int c = 0; c < 32; ++c) acc[c] = 0.f;
+#pragma unroll 1
+              for (int u = 0; u <= g1 - g0; ++u) {
+                const float f = (u == 0 ? wt[0] : u == 1 ? wt[1] : u == 2 ? wt[2] : wt[3]) * norm;
+                if (g0 + u == gang) {
+#pragma unroll
+                  for (int c = 0; c < 32; ++c)
+                    acc[c] = fmaf(f, __uint_as_float(o[c]) * inv, acc[c]);
+                } else if (f > 0.f) {
+                  const float4* src =
+                      tree_part_at(p, tree_part(p, g0 + u, g0, mt), trow, c0 / 4);
+                  float4 x[8];
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) x[c] = __ldcg(src + (size_t)c * p.tile_rows);
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) {
+                    acc[4 * c] = fmaf(f, x[c].x, acc[4 * c]);
+                    acc[4 * c + 1] = fmaf(f, x[c].y, acc[4 * c + 1]);
+                    acc[4 * c + 2] = fmaf(f, x[c].z, acc[4 * c + 2]);
+                    acc[4 * c + 3] = fmaf(f, x[c].w, acc[4 * c + 3]);
+                  }
+                }
+              }
+#pragma unroll
+              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(acc[c]);
+            }
+            uint32_t h[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const __nv_bfloat162 h2 =
+                  __floats2bfloat162_rn(__uint_as_float(o[2 * c]), __uint_as_float(o[2 * c + 1]));
+              h[c] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            if (out32) {
+              store32(out + c0, *reinterpret_cast<uint32_t(*)[8]>(&h[0]));
+              store32(out + c0 + 16, *reinterpret_cast<uint32_t(*)[8]>(&h[8]));
+            } else {
+#pragma unroll
+              for (int c = 0; c < 16; c += 4)
+                *reinterpret_cast<uint4*>(out + c0 + 2 * c) =
+                    make_uint4(h[c], h[c + 1], h[c + 2], h[c + 3]);
+            }
+          }
+          if (live && p.lse)
+            p.lse[orow] = (whole ? l2 : den > 0.f ? top + log2f(den) : -INFINITY) * 0.6931471805599453f;
         }
       }
       tc::fence_before_sync();

@@ -121,6 +121,30 @@ def test_softmax_without_any_cache(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_softmax_tensors_on_16_byte_boundaries(dtype):
+    """Every tensor 16 bytes off a 32-byte boundary."""
+    s = softmax_inputs(12, 3, 20, 8, 2, 128, 32, [500, 33, 0], dtype, [20, 7, 1])
+    for k in ("q", "k_blk", "v_blk", "k_pool", "v_pool"):
+        x = getattr(s, k)
+        pad = 16 // x.element_size()
+        y = torch.empty(x.numel() + pad, dtype=x.dtype, device="cuda")[pad:].view(x.shape)
+        y.copy_(x)
+        setattr(s, k, y)
+    out = torch.empty(s.q.numel() + 16 // s.q.element_size(), dtype=s.q.dtype, device="cuda")
+    out = out[16 // s.q.element_size():].view(s.q.shape)
+    assert out.data_ptr() % 32 == 16
+    check_softmax(s, out=out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prefix", [[9000, 3000, 6100], [2500] * 40, [64 * 150 - 1] * 2])
+def test_softmax_items_in_a_few_pieces(prefix, dtype):
+    """Items that two to four spans share, and more."""
+    R = len(prefix)
+    check_softmax(softmax_inputs(13, R, 17, 8, 2, 64, 64, prefix, dtype, [17 - r % 5 for r in range(R)]))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_softmax_skips_bad_requests_and_no_other(dtype):
     prefix = [300, 100, 64, 65, 0, 129, 500]
     s = softmax_inputs(9, 7, 20, 4, 2, 128, 16, prefix, dtype, [20, 3, 20, 7, 5, 20, 1])
