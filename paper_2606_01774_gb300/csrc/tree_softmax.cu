@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
     bool has = false;
     if (base + tid < p.gangs) {
       const TreeCut c = cuts[base + tid];
-      has = c.r >= 0 && c.last - (base + tid) >= p.join && !p.bad[c.r];
+      has = c.r >= 0 && c.last - (base + tid) >= p.join;
     }
     const unsigned mask = __ballot_sync(0xffffffffu, has);
     if (lane == 0) in_warp[warp] = __popc(mask);
@@ -308,6 +308,7 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
     const int g0 = cut_of[at / p.row_tiles], mt = at % p.row_tiles;
     const int row = e & ((1 << shift) - 1), c4 = e >> shift, sub = tid / kPer;
     const TreeCut cut = cuts[g0];
+    const bool skip = p.bad[cut.r] != 0;
     const TreeRows rows = tree_rows(p, mt * (p.tile_rows / p.tile_base) + row / p.tile_base);
     const int i = row % p.tile_base;
     const bool live = c4 < D / 4 && row < p.tile_rows && rows.used(i, cut.nodes);
@@ -349,7 +350,7 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
       for (int u = 1; u < PARTS; ++u)
         take(red_l[u * kPer + tid].x, red_l[u * kPer + tid].y, red_o[u * kPer + tid]);
     }
-    if (!live) continue;
+    if (!live || skip) continue;
     const size_t o = ((size_t)cut.r * p.N + rows.node(i)) * p.Hq + cut.kvh * p.G + rows.head(i);
     const float inv = den > 0.f ? 1.f / den : 0.f;
     store4(static_cast<T*>(p.out) + o * D + 4 * c4,

@@ -614,37 +614,53 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
             den += wt[u];
           }
           const float norm = den > 0.f ? 1.f / den : 0.f;
+          auto weight = [&](int u) {
+            return (u == 0 ? wt[0] : u == 1 ? wt[1] : u == 2 ? wt[2] : wt[3]) * norm;
+          };
           const size_t orow = ((size_t)it.w.r * p.N + node) * p.Hq + it.w.kvh * p.G + head;
           __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + orow * D;
+          // the other pieces' columns, kCols at a time: every load of a batch in
+          // flight before the first is used
+          constexpr int kCols = NQ == 1 ? 64 : 32;
 #pragma unroll 1
-          for (int c0 = 0; c0 < D; c0 += 32) {
-            uint32_t o[32];
-            tc::tmem_ld16(tmem_o + lane_off + c0, *reinterpret_cast<uint32_t(*)[16]>(&o[0]));
-            tc::tmem_ld16(tmem_o + lane_off + c0 + 16, *reinterpret_cast<uint32_t(*)[16]>(&o[16]));
+          for (int c0 = 0; c0 < D; c0 += kCols) {
+            uint32_t o[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; c += 16)
+              tc::tmem_ld16(tmem_o + lane_off + c0 + c, *reinterpret_cast<uint32_t(*)[16]>(&o[c]));
             tc::tmem_ld_wait();
-            if (!live) continue;
-            if (whole) {
+            float acc[kCols];
 #pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * inv);
-            } else {
-              float acc[32];
+            for (int c = 0; c < kCols; ++c) acc[c] = __uint_as_float(o[c]) * inv;
+            if (!whole) {
+              const float own = weight(gang - g0);
+              if (gang == g0) {
 #pragma unroll
-              for (int c = 0; c < 32; ++c) acc[c] = 0.f;
+                for (int c = 0; c < kCols; ++c) acc[c] *= own;
+              } else {  // its turn comes later: back to tensor memory meanwhile
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
+              }
 #pragma unroll 1
-              for (int u = 0; u <= g1 - g0; ++u) {
-                const float f = (u == 0 ? wt[0] : u == 1 ? wt[1] : u == 2 ? wt[2] : wt[3]) * norm;
+              for (int u = gang == g0 ? 1 : 0; u <= g1 - g0; ++u) {
+                const float f = weight(u);
                 if (g0 + u == gang) {
 #pragma unroll
-                  for (int c = 0; c < 32; ++c)
+                  for (int c = 0; c < kCols; c += 16)
+                    tc::tmem_ld16(tmem_o + lane_off + c0 + c,
+                                  *reinterpret_cast<uint32_t(*)[16]>(&o[c]));
+                  tc::tmem_ld_wait();
+#pragma unroll
+                  for (int c = 0; c < kCols; ++c)
                     acc[c] = fmaf(f, __uint_as_float(o[c]) * inv, acc[c]);
-                } else if (f > 0.f) {
+                } else if (live && f > 0.f) {
                   const float4* src =
                       tree_part_at(p, tree_part(p, g0 + u, g0, mt), trow, c0 / 4);
-                  float4 x[8];
+                  float4 x[kCols / 4];
 #pragma unroll
-                  for (int c = 0; c < 8; ++c) x[c] = __ldcg(src + (size_t)c * p.tile_rows);
+                  for (int c = 0; c < kCols / 4; ++c) x[c] = __ldcg(src + (size_t)c * p.tile_rows);
 #pragma unroll
-                  for (int c = 0; c < 8; ++c) {
+                  for (int c = 0; c < kCols / 4; ++c) {
                     acc[4 * c] = fmaf(f, x[c].x, acc[4 * c]);
                     acc[4 * c + 1] = fmaf(f, x[c].y, acc[4 * c + 1]);
                     acc[4 * c + 2] = fmaf(f, x[c].z, acc[4 * c + 2]);
@@ -652,24 +668,23 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
                   }
                 }
               }
-#pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(acc[c]);
             }
-            uint32_t h[16];
+            if (!live) continue;
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              const __nv_bfloat162 h2 =
-                  __floats2bfloat162_rn(__uint_as_float(o[2 * c]), __uint_as_float(o[2 * c + 1]));
-              h[c] = *reinterpret_cast<const uint32_t*>(&h2);
-            }
-            if (out32) {
-              store32(out + c0, *reinterpret_cast<uint32_t(*)[8]>(&h[0]));
-              store32(out + c0 + 16, *reinterpret_cast<uint32_t(*)[8]>(&h[8]));
-            } else {
+            for (int c = 0; c < kCols; c += 16) {
+              uint32_t h[8];
 #pragma unroll
-              for (int c = 0; c < 16; c += 4)
-                *reinterpret_cast<uint4*>(out + c0 + 2 * c) =
-                    make_uint4(h[c], h[c + 1], h[c + 2], h[c + 3]);
+              for (int i = 0; i < 8; ++i) {
+                const __nv_bfloat162 h2 =
+                    __floats2bfloat162_rn(acc[c + 2 * i], acc[c + 2 * i + 1]);
+                h[i] = *reinterpret_cast<const uint32_t*>(&h2);
+              }
+              if (out32) {
+                store32(out + c0 + c, h);
+              } else {
+                *reinterpret_cast<uint4*>(out + c0 + c) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(out + c0 + c + 8) = make_uint4(h[4], h[5], h[6], h[7]);
+              }
             }
           }
           if (live && p.lse)
