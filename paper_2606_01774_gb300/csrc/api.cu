@@ -612,6 +612,7 @@ flare_status flare_tree_softmax_attn(const flare_softmax_desc* d, const void* q,
   p.tile_rows = plan.tile_rows;
   char* ws = static_cast<char*>(workspace);
   p.bad = reinterpret_cast<int32_t*>(ws + plan.bad_off);
+  p.n_cuts = reinterpret_cast<int32_t*>(ws + plan.n_cuts_off);
   p.cuts = ws + plan.cuts_off;
   p.counts = reinterpret_cast<int32_t*>(ws + plan.counts_off);
   p.n_counts = plan.n_counts;

@@ -155,7 +155,8 @@ struct TreeSoftmaxParams {
   int gangs, row_tiles;       // row_tiles: CTAs per gang
   int tile_base, tile_rows;   // query rows of a row tile, and of a CTA's one or two
   int32_t* bad;               // [R] whether a request is skipped
-  void* cuts;                 // [gangs] TreeCut: the item that a gang leaves unfinished
+  int32_t* n_cuts;
+  void* cuts;                 // [n_cuts <= gangs] TreeCut: items for tree_finish_kernel to merge
   int join;                   // pieces of an item that its last one merges itself
   int n_counts;
   int32_t* counts;            // [gangs,row_tiles,1 or 2] stored pieces of the item a gang starts
@@ -167,7 +168,7 @@ struct TreeSoftmaxParams {
 
 struct TreeSoftmaxPlan {
   int gangs, row_tiles, tile_base, tile_rows, n_counts, join;
-  size_t bad_off, cuts_off, counts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
+  size_t bad_off, n_cuts_off, cuts_off, counts_off, anc_off, part_o_off, part_lse_off, workspace_bytes;
 };
 
 TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page_size,

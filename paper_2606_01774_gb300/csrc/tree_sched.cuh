@@ -52,17 +52,10 @@ __device__ __forceinline__ TreeRows tree_rows(const TreeSoftmaxParams& p, int ti
   return TreeRows{tile / per, 1, h, min(p.tile_base, p.G - h)};
 }
 
-struct TreeSpanShared {
-  long long warp_sum[32];
-  long long lo, hi, off;  // the span, and the first tile's offset in its request
-  long long total;        // tiles of the batch
-  int gangs, r;
-};
-
-// The item that a gang starts and leaves unfinished, to be merged: its request
-// (-1: none) and kv head, and the last gang that has a piece of it.
+// An item that a gang starts and leaves unfinished, for tree_finish_kernel: its
+// request and kv head, and the first and last gang that have a piece of it.
 struct alignas(16) TreeCut {
-  int r, kvh, last, nodes;
+  int r, kvh, nodes, first, last;
 };
 
 // Key tiles per kv head of a request; 0 when it has no nodes or a wrong length.
@@ -138,15 +131,21 @@ __device__ __forceinline__ long long shfl_up_ll(long long x, int o) {
   return __shfl_up_sync(0xffffffffu, x, o);
 }
 
-// The span of `gang`, found by all threads of the CTA together; the gang's
-// first CTA also records its cut.
-template <int THREADS>
-__device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int gang,
-                                                TreeSpanShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (p.R + THREADS - 1) / THREADS;
-  const int r0 = min(p.R, tid * per), r1 = min(p.R, r0 + per);
+// The batch's cut and one gang's span, [lo, hi) of `total` tiles, by a warp on
+// its own (every warp of a CTA works it out for itself: that takes one round
+// trip to memory and no barrier).
+struct TreeSpan {
+  long long lo, hi, total;
+  int gangs;
+  TreeCursor start;
+};
+
+__device__ __forceinline__ TreeSpan tree_span(const TreeSoftmaxParams& p, int gang) {
+  const int lane = threadIdx.x & 31;
+  const int per = (p.R + 31) / 32;
+  const int r0 = min(p.R, lane * per), r1 = min(p.R, r0 + per);
   long long sum = 0;
+#pragma unroll 4
   for (int r = r0; r < r1; ++r) sum += (long long)tree_tiles(p, r) * p.Hkv;
   long long incl = sum;
 #pragma unroll
@@ -154,66 +153,58 @@ __device__ __forceinline__ TreeCursor tree_span(const TreeSoftmaxParams& p, int 
     const long long x = shfl_up_ll(incl, o);
     if (lane >= o) incl += x;
   }
-  if (lane == 31) sh.warp_sum[warp] = incl;
-  __syncthreads();
-  long long before = incl - sum, total = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    const long long x = sh.warp_sum[w];
-    if (w < warp) before += x;
-    total += x;
+  TreeSpan s;
+  s.total = __shfl_sync(0xffffffffu, incl, 31);
+  s.gangs = tree_gangs(p, s.total);
+  s.lo = s.hi = 0;
+  if (gang < s.gangs) {
+    s.lo = tree_div(s.total * gang, s.gangs);
+    s.hi = tree_div(s.total * (gang + 1), s.gangs);
   }
-  const int gangs = tree_gangs(p, total);
-  const long long lo = gang < gangs ? tree_div(total * gang, gangs) : 0;
-  const long long hi = gang < gangs ? tree_div(total * (gang + 1), gangs) : 0;
-  if (tid == 0) {
-    sh.lo = lo;
-    sh.hi = hi;
-    sh.total = total;
-    sh.gangs = gangs;
-  }
-  if (lo < hi && before <= lo && lo < before + sum) {  // this thread holds the first request
-    long long at = before;
-    int r = r0;
-    for (;; ++r) {
-      const long long n = (long long)tree_tiles(p, r) * p.Hkv;
-      if (lo < at + n) break;
-      at += n;
+  s.start.left = s.hi - s.lo;
+  s.start.r = s.start.kvh = s.start.j = 0;
+  if (s.lo == s.hi) return s;
+  // the lane that holds the first request walks to it
+  const bool mine = incl - sum <= s.lo && s.lo < incl;
+  if (mine) {
+    long long at = s.lo - (incl - sum);
+    int r = r0, n = tree_tiles(p, r);
+    while (at >= (long long)n * p.Hkv) {
+      at -= (long long)n * p.Hkv;
+      n = tree_tiles(p, ++r);
     }
-    sh.r = r;
-    sh.off = lo - at;
+    s.start.r = r;
+    s.start.kvh = (int)tree_div(at, n);
+    s.start.j = (int)(at - (long long)s.start.kvh * n);
   }
-  // what this gang leaves unfinished, for the merge (one thread holds its
-  // last tile)
-  if (blockIdx.x % p.row_tiles == 0) {
-    TreeCut* cut = static_cast<TreeCut*>(p.cuts) + gang;
-    if (lo >= hi) {
-      if (tid == 0) *cut = TreeCut{-1, 0, 0, 0};
-    } else if (before <= hi - 1 && hi - 1 < before + sum) {
-      long long at = before;
-      int r = r0;
-      for (;; ++r) {
-        const long long n = (long long)tree_tiles(p, r) * p.Hkv;
-        if (hi - 1 < at + n) break;
-        at += n;
-      }
-      const int n = tree_tiles(p, r), kvh = (int)tree_div(hi - 1 - at, n);
-      const long long s0 = at + (long long)kvh * n;
-      const bool mine = s0 >= lo && s0 + n > hi;
-      *cut = TreeCut{mine ? r : -1, kvh, tree_gang_of(s0 + n - 1, total, gangs), p.node_len[r]};
-    }
-  }
-  __syncthreads();
-  TreeCursor c;
-  c.left = sh.hi - sh.lo;
-  c.r = c.kvh = c.j = 0;
-  if (c.left > 0) {
-    c.r = sh.r;
-    const int n = tree_tiles(p, c.r);
-    c.kvh = (int)tree_div(sh.off, n);
-    c.j = (int)(sh.off - (long long)c.kvh * n);
-  }
-  return c;
+  const int src = __ffs(__ballot_sync(0xffffffffu, mine)) - 1;
+  s.start.r = __shfl_sync(0xffffffffu, s.start.r, src);
+  s.start.kvh = __shfl_sync(0xffffffffu, s.start.kvh, src);
+  s.start.j = __shfl_sync(0xffffffffu, s.start.j, src);
+  return s;
+}
+
+// The first and last gang that have a piece of piece w's item: it starts j0
+// tiles before the span, or ends with it.
+__device__ __forceinline__ void tree_sharers(const TreeSpan& s, const TreePiece& w, int& g0,
+                                             int& g1) {
+  const long long s0 = w.slot() ? s.hi - w.j1 : s.lo - w.j0;
+  g0 = tree_gang_of(s0, s.total, s.gangs);
+  g1 = tree_gang_of(s0 + w.n - 1, s.total, s.gangs);
+}
+
+// Puts the item that a gang starts and does not finish on the list of those
+// that tree_finish_kernel merges (its order does not matter).  One thread of the
+// gang's first CTA, with the gang's last piece, after the plan has emptied the
+// list.
+__device__ __forceinline__ void tree_list_cut(const TreeSoftmaxParams& p, const TreeSpan& s,
+                                              const TreePiece& w) {
+  if (w.whole() || w.slot() == 0) return;
+  int g0, g1;
+  tree_sharers(s, w, g0, g1);
+  if (g1 - g0 < p.join) return;
+  static_cast<TreeCut*>(p.cuts)[atomicAdd(p.n_cuts, 1)] =
+      TreeCut{w.r, w.kvh, p.node_len[w.r], g0, g1};
 }
 
 }  // namespace flare

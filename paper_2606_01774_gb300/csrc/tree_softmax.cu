@@ -26,7 +26,6 @@ constexpr int kPlanThreads = 128;
 constexpr int kRowsS = 32;      // query rows per CTA of the fp32 kernel
 constexpr int kThreadsS = 128;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kMaxGangs = 1024;
 
 __device__ __forceinline__ void store4(float* x, float4 v) { *reinterpret_cast<float4*>(x) = v; }
 __device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
@@ -42,6 +41,7 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
   const int r = blockIdx.x, tid = threadIdx.x;
   for (int i = r * kPlanThreads + tid; i < p.n_counts; i += gridDim.x * kPlanThreads)
     p.counts[i] = 0;
+  if (r == 0 && tid == 0) *p.n_cuts = 0;
   const int n = p.node_len[r], P = p.prefix_len[r];
   int bad = 0;
   if (n < 0 || n > p.N) bad |= FLARE_DEV_BAD_TREE;
@@ -80,7 +80,6 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   constexpr int kS = D + 4;  // row stride of staged rows: 16 lanes on 16 rows spread over the banks
   constexpr int kC = D / 64;
   extern __shared__ __align__(16) float sm[];
-  __shared__ TreeSpanShared span;
   float* Qs = sm;                    // [32][kS]
   float* Ks = Qs + kRowsS * kS;      // [64][kS]
   float* Vs = Ks + kTreeTile * kS;   // [64][kS]
@@ -95,9 +94,11 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   const float* blks[2] = {static_cast<const float*>(p.k_blk), static_cast<const float*>(p.v_blk)};
   pdl_wait();  // the plan
   pdl_launch_next();
-  TreeCursor cur = tree_span<kThreadsS>(p, gang, span);
+  const TreeSpan span = tree_span(p, gang);
+  TreeCursor cur = span.start;
   TreePiece w;
   while (cur.next(p, w)) {
+    if (mt == 0 && tid == 0 && cur.left == 0) tree_list_cut(p, span, w);
     const int n = p.node_len[w.r], P = p.prefix_len[w.r];
     if (rows.node0 >= n || p.bad[w.r]) continue;
     __syncthreads();  // the previous piece's rows are read
@@ -260,7 +261,6 @@ template <typename T, int D, int PARTS>
 __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   constexpr int kPer = 256 / PARTS;  // (row, column group) elements per CTA and pass
   constexpr int kIn = PARTS > 1 ? 8 : 4;  // pieces in flight per thread
-  __shared__ int cut_of[kMaxGangs], in_warp[8];
   __shared__ float4 red_o[PARTS > 1 ? 256 : 1];
   __shared__ float2 red_l[PARTS > 1 ? 256 : 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -277,37 +277,17 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
       for (int e = lane; e < p.Hq; e += 32) p.lse[u * p.Hq + e] = -INFINITY;
   }
   pdl_wait();  // the attention
-  const TreeCut* cuts = static_cast<const TreeCut*>(p.cuts);
-  int n_cuts = 0;  // in gang order, the same in every CTA
-  for (int base = 0; base < p.gangs; base += 256) {
-    bool has = false;
-    if (base + tid < p.gangs) {
-      const TreeCut c = cuts[base + tid];
-      has = c.r >= 0 && c.last - (base + tid) >= p.join;
-    }
-    const unsigned mask = __ballot_sync(0xffffffffu, has);
-    if (lane == 0) in_warp[warp] = __popc(mask);
-    __syncthreads();
-    int at = n_cuts;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      if (w < warp) at += in_warp[w];
-      n_cuts += in_warp[w];
-    }
-    if (has) cut_of[at + __popc(mask & ((1u << lane) - 1))] = base + tid;
-    __syncthreads();
-  }
   // rows that may be used, rounded up so that elements split by shifts
   const int used = p.N * p.G < p.tile_rows ? p.N * p.G : p.tile_rows;
   int shift = 0;
   while ((1 << shift) < used) ++shift;
   const int passes = ((D / 4 << shift) + kPer - 1) / kPer;
-  const long long units = (long long)n_cuts * p.row_tiles * passes;
+  const long long units = (long long)*p.n_cuts * p.row_tiles * passes;
   for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int at = (int)(unit / passes), e = (int)(unit - (long long)at * passes) * kPer + tid % kPer;
-    const int g0 = cut_of[at / p.row_tiles], mt = at % p.row_tiles;
+    const TreeCut cut = static_cast<const TreeCut*>(p.cuts)[at / p.row_tiles];
+    const int g0 = cut.first, mt = at % p.row_tiles;
     const int row = e & ((1 << shift) - 1), c4 = e >> shift, sub = tid / kPer;
-    const TreeCut cut = cuts[g0];
     const bool skip = p.bad[cut.r] != 0;
     const TreeRows rows = tree_rows(p, mt * (p.tile_rows / p.tile_base) + row / p.tile_base);
     const int i = row % p.tile_base;
@@ -379,7 +359,6 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
   const long long most =
       (long long)R * Hkv * (((long long)max_pages * page_size + kTreeTile - 1) / kTreeTile + 1);
   if (gangs > most) gangs = most;
-  if (gangs > kMaxGangs) gangs = kMaxGangs;
   if (gangs < 1) gangs = 1;
   pl.gangs = (int)gangs;
   const size_t slots = (size_t)2 * pl.gangs * pl.row_tiles * pl.tile_rows;
@@ -389,6 +368,8 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
   size_t at = 0;
   pl.bad_off = at;
   at += up((size_t)R * sizeof(int32_t));
+  pl.n_cuts_off = at;
+  at += up(sizeof(int32_t));
   pl.cuts_off = at;
   at += up((size_t)pl.gangs * sizeof(TreeCut));
   pl.counts_off = at;

@@ -86,7 +86,6 @@ struct TreeShared {
   uint32_t tmem_base;
   int abort_flag;
   int last[2];  // whether this CTA's piece of an item ended last
-  TreeSpanShared span;
 };
 
 __device__ __forceinline__ bool warp_wait_t(uint64_t* bar, uint32_t parity, const int* abort) {
@@ -169,38 +168,33 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
   const int node0 = tree_rows(p, mt * NQ).node0;  // of the CTA's first row tile
 
-  if (tid == 0) {
-    sh.abort_flag = 0;
-    for (int s = 0; s < C::kKStages; ++s) {
-      tc::mbar_init(&sh.k_full[s], 1);
-      tc::mbar_init(&sh.k_empty[s], NQ);  // a product per row tile
-    }
-    for (int s = 0; s < C::kVStages; ++s) {
-      tc::mbar_init(&sh.v_full[s], 1);
-      tc::mbar_init(&sh.v_empty[s], NQ);
-      tc::mbar_init(&sh.v_fix[s], kSmThreads);
-    }
-    for (int t = 0; t < NQ; ++t) {
-      for (int b = 0; b < kSB; ++b) {
-        tc::mbar_init(&sh.s_full[t][b], 1);
-        tc::mbar_init(&sh.p_full[t][b], kSmThreads);
-        tc::mbar_init(&sh.pv_done[t][b], 1);
-      }
-      tc::mbar_init(&sh.q_full[t], 1);
-      tc::mbar_init(&sh.o_final[t], 1);
-      tc::mbar_init(&sh.o_free[t], kSmThreads);
-    }
-    tc::mbar_init(&sh.drain[0], 1);
-    tc::mbar_init(&sh.drain[1], 1);
-    tc::fence_mbar_init();
+  // barriers, a thread each: arrivals per phase
+  {
+    auto init = [&](int first, uint64_t* bars, int n, int count) {
+      if (tid >= first && tid < first + n) tc::mbar_init(bars + tid - first, count);
+    };
+    init(0, sh.k_full, C::kKStages, 1);
+    init(8, sh.k_empty, C::kKStages, NQ);  // a product per row tile
+    init(16, sh.v_full, C::kVStages, 1);
+    init(24, sh.v_empty, C::kVStages, NQ);
+    init(32, sh.v_fix, C::kVStages, kSmThreads);
+    init(40, &sh.s_full[0][0], 8, 1);
+    init(48, &sh.p_full[0][0], 8, kSmThreads);
+    init(56, &sh.pv_done[0][0], 8, 1);
+    init(64, sh.q_full, 2, 1);
+    init(66, sh.o_final, 2, 1);
+    init(68, sh.o_free, 2, kSmThreads);
+    init(70, sh.drain, 2, 1);
+    if (tid == 72) sh.abort_flag = 0;
+    if (tid < 96) tc::fence_mbar_init();
   }
   if (warp == 1) tc::tmem_alloc(&sh.tmem_base, C::kTmemCols);
-  const TreeCursor span = tree_span<C::kThreads>(p, gang, sh.span);
+  const TreeSpan span = tree_span(p, gang);
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = sh.tmem_base;
-  TreeCursor cur = span;
+  TreeCursor cur = span.start;
   TreeItem it;
 
   if (warp == 0 || warp == kVWarpT) {
@@ -550,14 +544,9 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       const bool whole = it.w.whole();
       const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
       const float l2 = l_run > 0.f ? m_run + log2f(l_run) : -INFINITY;
-      // the gangs that share the item: it starts j0 tiles before this span, or
-      // ends j1 tiles before this span's end
+      // the gangs that share the item
       int g0 = gang, g1 = gang;
-      if (!whole) {
-        const long long s0 = it.w.slot() ? sh.span.hi - it.w.j1 : sh.span.lo - it.w.j0;
-        g0 = tree_gang_of(s0, sh.span.total, sh.span.gangs);
-        g1 = tree_gang_of(s0 + it.w.n - 1, sh.span.total, sh.span.gangs);
-      }
+      if (!whole) tree_sharers(span, it.w, g0, g1);
       const bool joins = !whole && !skip && g1 - g0 < kTreeJoin;
       bool store = !whole && !skip, merge = false;  // a partial output; the item's
       int32_t* count = p.counts + ((size_t)g0 * p.row_tiles + mt) * NQ + t;
@@ -568,6 +557,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         merge = sh.last[t] != 0;
         store = !merge;
       }
+      if (store && !joins && blockIdx.x % p.row_tiles == 0 && t == 0 && row == 0)
+        tree_list_cut(p, span, it.w);
       if (store && warp_live) {
         const size_t part = tree_part(p, gang, g0, mt);
         const int trow = t * kRowsT + row;
