@@ -195,8 +195,7 @@ __device__ __forceinline__ void tree_sharers(const TreeSpan& s, const TreePiece&
 
 // Puts the item that a gang starts and does not finish on the list of those
 // that tree_finish_kernel merges (its order does not matter).  One thread of the
-// gang's first CTA, with the gang's last piece, after the plan has emptied the
-// list.
+// gang's first CTA, with each of its pieces, after the plan has emptied the list.
 __device__ __forceinline__ void tree_list_cut(const TreeSoftmaxParams& p, const TreeSpan& s,
                                               const TreePiece& w) {
   if (w.whole() || w.slot() == 0) return;

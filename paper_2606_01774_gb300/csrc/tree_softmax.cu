@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   TreeCursor cur = span.start;
   TreePiece w;
   while (cur.next(p, w)) {
-    if (mt == 0 && tid == 0 && cur.left == 0) tree_list_cut(p, span, w);
+    if (mt == 0 && tid == 0) tree_list_cut(p, span, w);
     const int n = p.node_len[w.r], P = p.prefix_len[w.r];
     if (rows.node0 >= n || p.bad[w.r]) continue;
     __syncthreads();  // the previous piece's rows are read
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
 template <typename T, int D, int PARTS>
 __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   constexpr int kPer = 256 / PARTS;  // (row, column group) elements per CTA and pass
-  constexpr int kIn = PARTS > 1 ? 8 : 4;  // pieces in flight per thread
+  constexpr int kIn = PARTS > 1 ? 10 : 4;  // pieces in flight per thread
   __shared__ float4 red_o[PARTS > 1 ? 256 : 1];
   __shared__ float2 red_l[PARTS > 1 ? 256 : 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -282,10 +282,14 @@ __global__ void __launch_bounds__(256) tree_finish_kernel(TreeSoftmaxParams p) {
   int shift = 0;
   while ((1 << shift) < used) ++shift;
   const int passes = ((D / 4 << shift) + kPer - 1) / kPer;
+  // both in one round trip: the list's length, and the first unit's entry (the
+  // list has room for every gang's)
   const long long units = (long long)*p.n_cuts * p.row_tiles * passes;
+  const TreeCut* cuts = static_cast<const TreeCut*>(p.cuts);
+  TreeCut cut = cuts[min(blockIdx.x / (passes * p.row_tiles), p.gangs - 1)];
   for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int at = (int)(unit / passes), e = (int)(unit - (long long)at * passes) * kPer + tid % kPer;
-    const TreeCut cut = static_cast<const TreeCut*>(p.cuts)[at / p.row_tiles];
+    if (unit != blockIdx.x) cut = cuts[at / p.row_tiles];
     const int g0 = cut.first, mt = at % p.row_tiles;
     const int row = e & ((1 << shift) - 1), c4 = e >> shift, sub = tid / kPer;
     const bool skip = p.bad[cut.r] != 0;

@@ -168,6 +168,14 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
   const int node0 = tree_rows(p, mt * NQ).node0;  // of the CTA's first row tile
 
+  // the tensor maps, on their way while the span is worked out
+  if (lane == 0) {
+    if (warp == 0) tc::prefetch_tmap(&maps.kpool);
+    if (warp == 1) tc::prefetch_tmap(&maps.q);
+    if (warp == 2) tc::prefetch_tmap(&maps.kblk);
+    if (warp == 3) tc::prefetch_tmap(&maps.vblk);
+    if (warp == kVWarpT) tc::prefetch_tmap(&maps.vpool);
+  }
   // barriers, a thread each: arrivals per phase
   {
     auto init = [&](int first, uint64_t* bars, int n, int count) {
@@ -202,10 +210,6 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     const int kv = warp == 0 ? 0 : 1;
     const CUtensorMap* pool_map = kv ? &maps.vpool : &maps.kpool;
     const CUtensorMap* blk_map = kv ? &maps.vblk : &maps.kblk;
-    if (lane == 0) {
-      tc::prefetch_tmap(pool_map);
-      tc::prefetch_tmap(blk_map);
-    }
     const int box_rows = p.page_size < kTreeTile ? p.page_size : kTreeTile;
     const int boxes = kTreeTile / box_rows;  // of a full tile
     const int ns = kv ? C::kVStages : C::kKStages;
@@ -452,6 +456,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       const bool warp_live = __any_sync(0xffffffffu, live);
       const uint64_t path = live ? p.anc[(size_t)it.w.r * p.N + node] : 0ull;
       const bool skip = p.bad[it.w.r] != 0;
+      if (tid == 64 && mt == 0 && !skip) tree_list_cut(p, span, it.w);
       float m_run = -INFINITY, l_run = 0.f;
       for (int j = 0; j < it.tiles; ++j) {
         const int gg = g + j, sb = gg % kSB;
@@ -557,8 +562,6 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         merge = sh.last[t] != 0;
         store = !merge;
       }
-      if (store && !joins && blockIdx.x % p.row_tiles == 0 && t == 0 && row == 0)
-        tree_list_cut(p, span, it.w);
       if (store && warp_live) {
         const size_t part = tree_part(p, gang, g0, mt);
         const int trow = t * kRowsT + row;
