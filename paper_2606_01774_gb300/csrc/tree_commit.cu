@@ -9,8 +9,9 @@
 // the 8 row groups of a column sit in one warp and meet in three shuffles.
 // Bound by the state's bytes at serving path lengths (a round accepts a few
 // tokens): the state moves once each way in 16-byte pieces, all of a thread's
-// loads in flight before the path's rows are gathered, and several CTAs per SM
-// overlap one's loads with another's steps.
+// loads in flight together with the path's keys and values (two round trips to
+// memory before the first step), and several CTAs per SM overlap one's loads
+// with another's steps.
 #include "common.cuh"
 #include "kernels.h"
 #include "tree.cuh"
@@ -27,7 +28,6 @@ __global__ void __launch_bounds__(kCommitThreads, 4) tree_commit_kernel(GdrParam
   constexpr int kR = DK / 8;  // state rows per thread
   constexpr int kSplit = DV / kCommitCols;
   extern __shared__ __align__(16) float sm[];
-  __shared__ int row_s[kMaxNodes];
   __shared__ float2 gate_s[kMaxNodes];  // {alpha, beta}
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int item = blockIdx.x / kSplit, part = blockIdx.x % kSplit;
@@ -35,6 +35,15 @@ __global__ void __launch_bounds__(kCommitThreads, 4) tree_commit_kernel(GdrParam
   const int rg = lane >> 2;                     // row group: rows rg*kR ..
   const int c = warp * 16 + (lane & 3) * 4;     // this thread's columns within the CTA's
   const int src = p.state_slot[r], dst = p.dst_slot[r], n = p.accept_len[r];
+  // rows of the path in the same round trip, before their number is known: a
+  // thread's 16-byte pieces of the keys belong to steps tk, tk + kStepK, ..
+  constexpr int kE = 16 / sizeof(T);
+  constexpr int kPk = DK / kE, kStepK = kCommitThreads / kPk;            // key pieces, rows a pass
+  constexpr int kPv = kCommitCols / kE, kStepV = kCommitThreads / kPv;   // value pieces
+  const int tk = tid / kPk, tv = tid / kPv;
+  const int32_t* path = p.path + (size_t)r * p.B;
+  const int row_k = tk < p.B ? path[tk] : 0, row_v = tv < p.B ? path[tv] : 0;
+  const int row_g = tid < p.B ? path[tid] : 0;
   int bad = 0;
   if (src < 0 || src >= p.nslots || dst < 0 || dst >= p.nslots) bad |= FLARE_DEV_BAD_SLOT;
   if (n < 0 || n > p.B) bad |= FLARE_DEV_BAD_ACCEPT_LEN;
@@ -53,30 +62,34 @@ __global__ void __launch_bounds__(kCommitThreads, 4) tree_commit_kernel(GdrParam
     s[m][0] = x.x;
     s[m][1] = x.y;
   }
-  if (tid < n) {
-    const int row = p.path[(size_t)r * p.B + tid];
+  // the path's gates, keys and this CTA's value columns, as fp32
+  float* Ks = sm;            // [n][DK]
+  float* Vs = Ks + n * DK;   // [n][kCommitCols]
+  const T* k = static_cast<const T*>(p.k) + ((size_t)r * p.B * p.Hk + h) * DK + tid % kPk * kE;
+  const T* v = static_cast<const T*>(p.v) + ((size_t)r * p.B * p.Hv + j) * DV +
+               part * kCommitCols + tid % kPv * kE;
+  auto piece = [&](const T* x, int row, size_t stride, float* out) {
     if (row < 0 || row >= p.B) {
       bad = 1;
-    } else {
-      const size_t g = ((size_t)r * p.B + row) * p.Hv + j;
-      row_s[tid] = row;
-      gate_s[tid] = make_float2(expf(p.log_decay[g]), p.beta[g]);
+      return;
     }
+    const uint4 w = *reinterpret_cast<const uint4*>(x + (size_t)row * stride);
+    const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+    for (int i = 0; i < kE; ++i) out[i] = to_f32(e[i]);
+  };
+  for (int t = tk; t < n; t += kStepK)
+    piece(k, t == tk ? row_k : path[t], (size_t)p.Hk * DK, Ks + t * DK + tid % kPk * kE);
+  for (int t = tv; t < n; t += kStepV)
+    piece(v, t == tv ? row_v : path[t], (size_t)p.Hv * DV, Vs + t * kCommitCols + tid % kPv * kE);
+  if (tid < n && row_g >= 0 && row_g < p.B) {
+    const size_t g = ((size_t)r * p.B + row_g) * p.Hv + j;
+    gate_s[tid] = make_float2(expf(p.log_decay[g]), p.beta[g]);
   }
   if (__syncthreads_or(bad)) {
     if (tid == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);
     return;
   }
-  // the path's keys and this CTA's value columns
-  float* Ks = sm;            // [n][DK]
-  float* Vs = Ks + n * DK;   // [n][kCommitCols]
-  const T* k = static_cast<const T*>(p.k) + ((size_t)r * p.B * p.Hk + h) * DK;
-  const T* v = static_cast<const T*>(p.v) + ((size_t)r * p.B * p.Hv + j) * DV + part * kCommitCols;
-  for (int e = tid; e < n * DK; e += kCommitThreads)
-    Ks[e] = to_f32(k[(size_t)row_s[e / DK] * p.Hk * DK + e % DK]);
-  for (int e = tid; e < n * kCommitCols; e += kCommitThreads)
-    Vs[e] = to_f32(v[(size_t)row_s[e / kCommitCols] * p.Hv * DV + e % kCommitCols]);
-  __syncthreads();
 #pragma unroll 1
   for (int t = 0; t < n; ++t) {
     float kv[kR];
