@@ -202,7 +202,7 @@ struct TreeVerifyParams {
   int32_t* next_token;        // [R]
   float* node_logp;           // [R,N]
   int chunk, n_chunks;        // row statistics: tokens per chunk, chunks per row
-  float4* stats;              // [R,N,n_chunks] {max, sum of exp(x - max), first argmax, -}
+  float4* stats;              // [R,N,n_chunks] {max, sum of 2^(x - max), first argmax, -}, x in log2 units
   int32_t* dev_status;
 };
 void plan_tree_verify(int R, int N, int V, int num_sms, int* chunk, int* n_chunks);

@@ -53,12 +53,15 @@ __device__ __forceinline__ void warp_best(float& v, int& i) {
   }
 }
 
-// {max, sum of exp(x - max), argmax} of two disjoint parts of a row
-__device__ __forceinline__ float4 join_stats(float4 a, float4 b) {
-  const float m = fmaxf(a.x, b.x);
-  if (m == -INFINITY) return make_float4(m, a.y + b.y, fminf(a.z, b.z), 0.f);
-  const float s = a.y * expf(a.x - m) + b.y * expf(b.x - m);
-  return make_float4(m, s, a.x > b.x ? a.z : b.x > a.x ? b.z : fminf(a.z, b.z), 0.f);
+// {max, sum of 2^(x - max), argmax} of a row from its parts on a warp's lanes
+// (x in units of log2): the maximum first, then one rescaling per part.
+__device__ __forceinline__ float4 warp_stats(float4 st) {
+  float m = st.x;
+  int best = (int)st.z;
+  warp_best(m, best);
+  float s = st.x == -INFINITY ? st.y : st.y * tc::ex2(st.x - m);  // a NaN sum stays one
+  s = warp_sum(s);
+  return make_float4(m, s, (float)best, 0.f);
 }
 
 }  // namespace
@@ -154,21 +157,13 @@ __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams
     }
   }
   if (tid < hi - tail) one(tail + tid);
-  float4 st = make_float4(m * p.inv_temp, s, (float)best, 0.f);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    float4 y;
-    y.x = __shfl_xor_sync(0xffffffffu, st.x, o);
-    y.y = __shfl_xor_sync(0xffffffffu, st.y, o);
-    y.z = __shfl_xor_sync(0xffffffffu, st.z, o);
-    st = join_stats(st, y);
-  }
+  float4 st = warp_stats(make_float4(m * scale, s, (float)best, 0.f));
   if ((tid & 31) == 0) red[tid >> 5] = st;
   __syncthreads();
-  if (tid == 0) {
-#pragma unroll
-    for (int w = 1; w < kRowThreads / 32; ++w) st = join_stats(st, red[w]);
-    p.stats[(size_t)row * p.n_chunks + blockIdx.x] = st;
+  if (tid < 32) {
+    st = warp_stats(tid < kRowThreads / 32 ? red[tid]
+                                           : make_float4(-INFINITY, 0.f, (float)p.V, 0.f));
+    if (tid == 0) p.stats[(size_t)row * p.n_chunks + blockIdx.x] = st;
   }
 }
 
@@ -202,7 +197,7 @@ __device__ __forceinline__ uint32_t cluster_word(const void* mine, uint32_t rank
 struct WalkShared {
   int par[kMaxNodes], tok[kMaxNodes], line[kMaxNodes], best_of[kMaxNodes], gone[kMaxNodes];
   unsigned long long kids[kMaxNodes];
-  float uni[kMaxNodes], logp[kMaxNodes], lse[kMaxNodes], q[kMaxNodes];
+  float uni[kMaxNodes], logp2[kMaxNodes], lse2[kMaxNodes], q[kMaxNodes], prob[kMaxNodes];
   float red_v[kWalkThreads / 32];
   int red_i[kWalkThreads / 32];
   int tree_ok;
@@ -271,12 +266,13 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     return;
   }
   const T* rows = static_cast<const T*>(p.logits) + (size_t)r * p.N * p.V;
+  const float scale = p.inv_temp * kLog2e;  // logits in units of log2
   const float* drafts =
       sample && p.draft_probs ? p.draft_probs + (size_t)r * p.N * p.V : nullptr;
   float x_tok = 0.f;  // the drafted token's logit, and its probability for the drafter
   if (tid > 0 && tid < n) {
     const size_t at = (size_t)sh.par[tid] * p.V + sh.tok[tid];
-    x_tok = to_f32(rows[at]) * p.inv_temp;
+    x_tok = to_f32(rows[at]) * scale;
     sh.q[tid] = drafts ? drafts[at] : 1.f;
   }
   pdl_wait();  // the row statistics
@@ -284,27 +280,27 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
   for (int i = warp; i < n; i += kWarps) {
     if (!sh.kids[i]) continue;
     float4 st = make_float4(-INFINITY, 0.f, (float)p.V, 0.f);
-    for (int c = lane; c < p.n_chunks; c += 32)
-      st = join_stats(st, p.stats[((size_t)r * p.N + i) * p.n_chunks + c]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      float4 y;
-      y.x = __shfl_xor_sync(0xffffffffu, st.x, o);
-      y.y = __shfl_xor_sync(0xffffffffu, st.y, o);
-      y.z = __shfl_xor_sync(0xffffffffu, st.z, o);
-      st = join_stats(st, y);
+    for (int c0 = 0; c0 < p.n_chunks; c0 += 31) {  // 31 parts and what came before
+      if (lane > 0)
+        st = c0 + lane - 1 < p.n_chunks
+                 ? p.stats[((size_t)r * p.N + i) * p.n_chunks + c0 + lane - 1]
+                 : make_float4(-INFINITY, 0.f, (float)p.V, 0.f);
+      st = warp_stats(st);
     }
     if (lane == 0) {
-      sh.lse[i] = st.x + logf(st.y);
+      sh.lse2[i] = st.x + log2f(st.y);
       sh.best_of[i] = (int)st.z;
-      if (!(fabsf(sh.lse[i]) < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
+      if (!(fabsf(sh.lse2[i]) < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
     }
   }
   if (__syncthreads_or(bad)) {
     if (tid == 0 && rank == 0) flag(p.dev_status, FLARE_DEV_BAD_LOGITS);
     return;
   }
-  if (tid < kMaxNodes) sh.logp[tid] = tid > 0 && tid < n ? x_tok - sh.lse[sh.par[tid]] : 0.f;
+  if (tid < kMaxNodes) {
+    sh.logp2[tid] = tid > 0 && tid < n ? x_tok - sh.lse2[sh.par[tid]] : 0.f;
+    sh.prob[tid] = exp2f(sh.logp2[tid]);
+  }
   if (tid == 0) {
     sh.cur = 0;
     sh.len = 1;
@@ -316,7 +312,6 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
   }
   __syncthreads();
 
-  const float scale = p.inv_temp * kLog2e;
   const int lo = (int)((long long)p.V * rank / ranks), hi = (int)((long long)p.V * (rank + 1) / ranks);
   // Calls f(x, ...) for this CTA's tokens of a row, kIn of a thread's loads in
   // flight: consecutive threads on consecutive tokens, whatever the alignment.
@@ -337,7 +332,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
         if (!sample) {
           ok = sh.tok[i] == sh.best_of[cur];
         } else {
-          const float px = expf(sh.logp[i]);
+          const float px = sh.prob[i];
           if (drafts) {
             ok = sh.uni[i] * sh.q[i] * m < fmaxf(px - c * sh.q[i], 0.f);
             if (!ok) {
@@ -377,7 +372,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     if (!sh.more) break;
     const T* x = rows + (size_t)sh.cur * p.V;
     const float* q = drafts + (size_t)sh.cur * p.V;
-    const float c = sh.c, shift = sh.lse[sh.cur] * kLog2e;
+    const float c = sh.c, shift = sh.lse2[sh.cur];
     float sum = 0.f;
     for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
       float xv[kIn], qv[kIn];
@@ -419,7 +414,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     int ng = sh.n_gone;
     while (true) {
       const float* q = c > 0.f ? drafts + (size_t)cur * p.V : nullptr;
-      const float shift = q ? sh.lse[cur] * kLog2e : 0.f;
+      const float shift = q ? sh.lse2[cur] : 0.f;
       float v0 = -INFINITY;
       int i0 = p.V;
       for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
@@ -502,7 +497,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
   }
   if (tid < p.N) {
     p.path[(size_t)r * p.N + tid] = tid < sh.len ? sh.line[tid] : -1;
-    p.node_logp[(size_t)r * p.N + tid] = sh.logp[tid];
+    p.node_logp[(size_t)r * p.N + tid] = sh.logp2[tid] * 0.6931471805599453f;
   }
   if (tid == 0) {
     p.path_len[r] = sh.len;
@@ -549,7 +544,7 @@ cudaError_t launch_t(const TreeVerifyParams& p, cudaStream_t stream) {
   // not yet fill the GPU
   int cluster = 1;
   while (cluster < kMaxCluster && p.V / (2 * cluster) >= 2048 &&
-         (long long)p.R * 2 * cluster <= 4LL * kNumSMs)
+         (long long)p.R * 2 * cluster <= 2LL * kNumSMs)
     cluster *= 2;
   const cudaError_t err =
       pdl_launch(tree_walk_kernel<T>, dim3((unsigned)p.R * cluster), kWalkThreads, 0, stream, rows,
