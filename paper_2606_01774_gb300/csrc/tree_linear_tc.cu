@@ -17,11 +17,13 @@
 //
 // Bound by the state's bytes: 64 KiB an item, so a CTA's life is organised
 // around its copies.  Warp 4 runs ahead: it finds the next item, streams its
-// state in 16 KiB pieces through a ring, its keys and queries by TMA, works
-// out its paths and gates (pointer doubling), and issues the MMAs as the
+// state in 16 KiB pieces through a ring, its keys, queries and values by TMA,
+// works out its paths and gates (pointer doubling), and issues the MMAs as the
 // pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
-// tensor memory, then tables, substitution and readout.  BM <= 32: 128
-// tensor-memory columns and under 76 KiB, three CTAs per SM; BM = 64: two.
+// tensor memory, then tables, substitution and readout.  A and M lie side by
+// side as pairs (-A, M), so that one packed multiply-add carries a delta into
+// both sums.  BM <= 32: 128 tensor-memory columns and under 76 KiB, three CTAs
+// per SM; BM = 64: two.
 // Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
 // lets its copies and MMAs land, frees its tensor memory and exits.
 #include <cudaTypedefs.h>
@@ -50,24 +52,27 @@ struct TlMeta {
   alignas(16) float gam2[BM];  // gamma_i log2(e)
   float beta[BM];
   uint64_t anc[BM];
-  int item, n;                 // item < 0: no more
+  int item, n;                 // item < 0: no more; n < 0: skipped (a bad tree)
 };
 
 template <int BM>
 struct TlCfg {
   static constexpr int kCtas = BM == 64 ? 2 : 3;               // per SM
-  static constexpr int kRing = BM == 16 ? 4 : BM == 32 ? 3 : 2;  // state pieces in flight
+  static constexpr int kRing = BM == 16 ? 3 : 2;               // state pieces in flight
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
-  static constexpr int kTable = BM * BM * 4;
-  // BM = 64: the tables take the key / query buffer's place, and the deltas,
-  // too many for registers, have a buffer
+  static constexpr int kV = 2 * BM * 128;                      // 2 chunks of value rows x 128 B
+  static constexpr int kTable = BM * BM * 8;                   // pairs (-A, M)
+  // BM = 64: the table takes the key / query buffer's place, and the deltas,
+  // too many for registers, the values', which beta (v - exp(gamma) K S0) in
+  // tensor memory has replaced by then
   static constexpr bool kOverlay = BM == 64;
   static constexpr int kDelta = BM == 64 ? BM * kTlD * 4 : 0;
   static constexpr int oKQ = 0;
   static constexpr int oRing = kKQ;
-  static constexpr int oTables = kOverlay ? 0 : oRing + kRing * kPieceBytes;
-  static constexpr int oDelta = oRing + kRing * kPieceBytes + (kOverlay ? 0 : 2 * kTable);
-  static constexpr int oShared = oDelta + kDelta;
+  static constexpr int oTable = kOverlay ? 0 : oRing + kRing * kPieceBytes;
+  static constexpr int oDelta = oRing + kRing * kPieceBytes;
+  static constexpr int oV = kOverlay ? oDelta + kDelta - kV : oTable + kTable;
+  static constexpr int oShared = oV + kV;
   static constexpr int kTmem = 64 + 2 * BM <= 128 ? 128 : 256;
 };
 
@@ -75,7 +80,7 @@ template <int BM>
 struct alignas(16) TlShared {
   TlMeta<BM> meta[3];
   uint64_t full[4], empty[4];  // ring pieces
-  uint64_t kq_full, kq_free, mma_done, meta_full[3];
+  uint64_t kq_full, v_full, done, mma_done, meta_full[3];  // done: an item's readout
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -87,13 +92,15 @@ constexpr int tl_smem() {
 
 struct TlMaps {
   CUtensorMap k, q;  // (128, Hk, N, R) box (64, 1, BM, 1), 128-byte swizzle
+  CUtensorMap v;     // (128, Hv, N, R) box (64, 1, BM, 1), no swizzle
 };
 
-// Word offset of columns 4 u .. 4 u + 3 of row `row` of a BM x BM table whose
-// 16-byte units are XOR-swizzled by the row (a warp writes a row per lane).
+// Word offset of the pairs of columns 2 u, 2 u + 1 of row `row` of a BM x BM
+// table of pairs whose 16-byte units are XOR-swizzled by the row (a warp writes
+// a row per lane).
 template <int BM>
 __device__ __forceinline__ int tl_at(int row, int u) {
-  return row * BM + ((u ^ (row & (BM / 4 - 1))) << 2);
+  return row * (2 * BM) + ((u ^ (row & (BM / 2 - 1))) << 2);
 }
 
 __device__ __forceinline__ bool tl_warp_wait(uint64_t* bar, uint32_t parity, const int* abort) {
@@ -137,8 +144,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
   TlShared<BM>& sh = *reinterpret_cast<TlShared<BM>*>(smem_raw + C::oShared);
   uint8_t* KQ = smem_raw + C::oKQ;
   uint8_t* ring = smem_raw + C::oRing;
-  float* At = reinterpret_cast<float*>(smem_raw + C::oTables);
-  float* Mt = At + BM * BM;
+  float* Tp = reinterpret_cast<float*>(smem_raw + C::oTable);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tc::smem_u32(smem_raw) & 1023u) {
     if (tid == 0) flag(p.dev_status, FLARE_DEV_WAIT_TIMEOUT);
@@ -151,7 +157,8 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       tc::mbar_init(&sh.empty[s], kTlCompute);
     }
     tc::mbar_init(&sh.kq_full, 1);
-    tc::mbar_init(&sh.kq_free, kTlCompute);
+    tc::mbar_init(&sh.v_full, 1);
+    tc::mbar_init(&sh.done, kTlCompute);
     tc::mbar_init(&sh.mma_done, 1);
     for (int b = 0; b < 3; ++b) tc::mbar_init(&sh.meta_full[b], 1);
     tc::fence_mbar_init();
@@ -171,44 +178,59 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
     if (lane == 0) {
       tc::prefetch_tmap(&maps.k);
       tc::prefetch_tmap(&maps.q);
+      tc::prefetch_tmap(&maps.v);
     }
     bool ok = true;
     uint32_t issued = 0;  // ring pieces so far
     int items = 0;        // items whose meta is written
     int kq_items = 0;     // items whose keys and queries are requested
+    int v_items = 0;      // items whose values are
     int mma_items = 0;    // items whose MMAs are committed
     int it = blockIdx.x;
+    const uint64_t kq_desc = tc::sdesc_sw128(tc::smem_u32(KQ), 16, 1024);
 
-    // The next item with something to do, from `it` on: its paths and gates
-    // into the next meta buffer.  Returns it (or -1), with its slot.
-    auto next_meta = [&](int& slot) -> int {
-      TlMeta<BM>& m = sh.meta[items % 3];
-      int found = -1;
+    // The next item with something to do, from `it` on (-1: none), its number
+    // of nodes and its slot.
+    auto next_item = [&](int& n, int& slot) -> int {
       for (; it < total; it += gridDim.x) {
         const int r = it / p.Hv, j = it - r * p.Hv;
-        const int n = p.node_len[r], s = p.state_slot[r];
-        const size_t g0 = (size_t)r * p.B * p.Hv + j;
+        n = p.node_len[r];
+        slot = p.state_slot[r];
         int bad = 0;
         if (n < 0 || n > p.B) bad |= FLARE_DEV_BAD_TREE;
-        if (s < 0 || s >= p.nslots) bad |= FLARE_DEV_BAD_SLOT;
-        int p0 = -1, p1 = -1;
-        if (!bad && !warp_load_tree(p.parent + (size_t)r * p.B, n, p0, p1))
-          bad |= FLARE_DEV_BAD_TREE;
+        if (slot < 0 || slot >= p.nslots) bad |= FLARE_DEV_BAD_SLOT;
         if (bad) {
           if (lane == 0) flag(p.dev_status, bad);
-          continue;
-        }
-        if (n == 0) {  // rests this round
+        } else if (n == 0) {  // rests this round
           for (int e = lane; e < p.B * (kTlD / 8); e += 32)
-            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out_causal) +
-                                      (g0 + (size_t)(e / (kTlD / 8)) * p.Hv) * kTlD +
-                                      (e % (kTlD / 8)) * 8) = make_uint4(0u, 0u, 0u, 0u);
-          continue;
+            *reinterpret_cast<uint4*>(
+                static_cast<__nv_bfloat16*>(p.out_causal) +
+                (((size_t)r * p.B + e / (kTlD / 8)) * p.Hv + j) * kTlD + (e % (kTlD / 8)) * 8) =
+                make_uint4(0u, 0u, 0u, 0u);
+        } else {
+          const int found = it;
+          it += gridDim.x;
+          return found;
         }
+      }
+      return -1;
+    };
+    // Its paths and gates into the next meta buffer.
+    auto write_meta = [&](int item, int n) {
+      TlMeta<BM>& m = sh.meta[items % 3];
+      if (item >= 0) {
+        const int r = item / p.Hv, j = item - r * p.Hv;
+        const size_t g0 = (size_t)r * p.B * p.Hv + j;
         float x0 = lane < n ? p.log_decay[g0 + (size_t)lane * p.Hv] : 0.f;
         float x1 = lane + 32 < n ? p.log_decay[g0 + (size_t)(lane + 32) * p.Hv] : 0.f;
         const float b0 = lane < n ? p.beta[g0 + (size_t)lane * p.Hv] : 0.f;
         const float b1 = lane + 32 < n ? p.beta[g0 + (size_t)(lane + 32) * p.Hv] : 0.f;
+        int p0, p1;
+        if (!warp_load_tree(p.parent + (size_t)r * p.B, n, p0, p1)) {
+          if (lane == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);
+          n = -1;
+          p0 = p1 = -1;
+        }
         // pointer doubling: sets and sums over the 2^k nearest path members
         uint64_t a0 = lane < n ? 1ull << lane : 0ull;
         uint64_t a1 = lane + 32 < n ? 1ull << (lane + 32) : 0ull;
@@ -247,16 +269,11 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           m.beta[lane + 32] = b1;
         }
         if (lane == 0) m.n = n;
-        slot = s;
-        found = it;
-        it += gridDim.x;
-        break;
       }
-      if (lane == 0) m.item = found;
+      if (lane == 0) m.item = item;
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sh.meta_full[items % 3]);
       ++items;
-      return found;
     };
     auto issue_piece = [&](int item, int slot, int q) {
       if (lane == 0) {
@@ -282,12 +299,29 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       ++kq_items;
     };
 
-    int slot = 0, slot_next = 0;
-    int cur = next_meta(slot), nxt = -1;
+    auto issue_v = [&](int item) {
+      if (lane == 0) {
+        const int r = item / p.Hv, j = item - r * p.Hv;
+        uint8_t* dst = smem_raw + C::oV;
+        tc::mbar_expect_tx(&sh.v_full, C::kV);
+        tc::tma_load_4d(dst, &maps.v, &sh.v_full, 0, j, 0, r);
+        tc::tma_load_4d(dst + BM * 128, &maps.v, &sh.v_full, 64, j, 0, r);
+      }
+      ++v_items;
+    };
+
+    // the item at work, the next one and the one after
+    int slot = 0, slot_next = 0, n = 0, n_next = 0;
+    int cur = next_item(n, slot), nxt = -1;
     if (cur >= 0) {
-      issue_kq(cur);
       for (int q = 0; q < C::kRing; ++q) issue_piece(cur, slot, q);
-      nxt = next_meta(slot_next);
+      issue_kq(cur);
+      issue_v(cur);
+      write_meta(cur, n);
+      nxt = next_item(n_next, slot_next);
+      write_meta(nxt, n_next);
+    } else {
+      write_meta(-1, 0);
     }
     uint32_t used = 0;  // ring pieces consumed
     while (cur >= 0 && ok) {
@@ -305,20 +339,20 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           ok = false;
           break;
         }
-        if (lane == 0) {
-          tc::fence_after_sync();
+        tc::fence_after_sync();
+        if (tc::elect_one()) {
 #pragma unroll
-          for (int kk = 2 * q; kk < 2 * q + 2; ++kk)
-            tc::mma_bf16_ts(tmW, tmS + kk * 8,
-                            tc::sdesc_sw128(tc::smem_u32(KQ + (kk >> 2) * (2 * BM * 128) +
-                                                         (kk & 3) * 32),
-                                            16, 1024),
-                            idW, kk > 0);
+          for (int kk = 0; kk < 2; ++kk)
+            tc::mma_bf16_ts(tmW, tmS + (2 * q + kk) * 8,
+                            kq_desc + (uint64_t)(((q >> 1) * (2 * BM * 128) +
+                                                  ((2 * q + kk) & 3) * 32) >>
+                                                 4),
+                            idW, q + kk > 0);
           if (q == kPieces - 1) {
 #pragma unroll
             for (int kk = 0; kk < kTlD / 16; ++kk) {
-              const uint64_t kd = tc::sdesc_sw128(
-                  tc::smem_u32(KQ + (kk >> 2) * (2 * BM * 128) + (kk & 3) * 32), 16, 1024);
+              const uint64_t kd =
+                  kq_desc + (uint64_t)(((kk >> 2) * (2 * BM * 128) + (kk & 3) * 32) >> 4);
               tc::mma_bf16_ss(tmS, kd, kd, idG, kk > 0);
             }
             tc::mma_commit(&sh.mma_done);
@@ -328,20 +362,25 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       }
       if (!ok) break;
       ++mma_items;
+      // the next keys and queries at once where the products alone read theirs
+      if (!C::kOverlay && nxt >= 0) {
+        ok = tl_warp_wait(&sh.mma_done, (uint32_t)(mma_items - 1) & 1u, &sh.abort_flag);
+        if (!ok) break;
+        issue_kq(nxt);
+      }
       // every compute thread is past the previous item: its meta buffer takes
       // the item after the next
-      int slot_after = 0;
-      const int after = nxt >= 0 ? next_meta(slot_after) : -1;
-      // the key / query buffer: free once the products have read it, or, where
-      // the tables take its place, once the readout has
+      int slot_after = 0, n_after = 0, after = -1;
       if (nxt >= 0) {
-        uint64_t* bar = C::kOverlay ? &sh.kq_free : &sh.mma_done;
-        if (!tl_warp_wait(bar, (uint32_t)(mma_items - 1) & 1u, &sh.abort_flag)) {
-          ok = false;
-          break;
-        }
-        if (C::kOverlay) tc::fence_async_smem();
-        issue_kq(nxt);
+        after = next_item(n_after, slot_after);
+        write_meta(after, n_after);
+        // the values' buffer, and the one that the table shares, once the
+        // readout is done
+        ok = tl_warp_wait(&sh.done, (uint32_t)(mma_items - 1) & 1u, &sh.abort_flag);
+        if (!ok) break;
+        tc::fence_async_smem();
+        if (C::kOverlay) issue_kq(nxt);
+        issue_v(nxt);
       }
       cur = nxt;
       slot = slot_next;
@@ -360,7 +399,9 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       }
       if (kq_items)
         tc::mbar_wait(&sh.kq_full, (uint32_t)(kq_items - 1) & 1u, nullptr, 100000000ull);
-      if (lane == 0) {
+      if (v_items) tc::mbar_wait(&sh.v_full, (uint32_t)(v_items - 1) & 1u, nullptr, 100000000ull);
+      __syncwarp();
+      if (tc::elect_one()) {
         tc::mma_commit(&sh.mma_done);
         tc::mbar_wait(&sh.mma_done, (uint32_t)mma_items & 1u, nullptr, 100000000ull);
       }
@@ -381,14 +422,10 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       const int r = item / p.Hv, j = item - r * p.Hv;
       const size_t row0 = ((size_t)r * p.B * p.Hv + j) * kTlD;
       const size_t row_stride = (size_t)p.Hv * kTlD;
-      const unsigned short* vg = static_cast<const unsigned short*>(p.v) + row0 + tid;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out_causal) + row0 + (tid & ~1);
-      constexpr int kVr = BM <= 32 ? BM : 1;
-      unsigned short vr[kVr];  // this column's values (BM <= 32)
-      if constexpr (BM <= 32) {
-#pragma unroll
-        for (int i = 0; i < BM; ++i) vr[i] = i < n ? vg[i * row_stride] : (unsigned short)0;
-      }
+      const unsigned short* vs =  // this column's values, 64 elements a row
+          reinterpret_cast<const unsigned short*>(smem_raw + C::oV + (tid >> 6) * (BM * 128)) +
+          (tid & 63);
       // the state, piece by piece, into tensor memory as bf16 pairs
 #pragma unroll 1
       for (int q = 0; q < kPieces; ++q, ++used) {
@@ -407,14 +444,31 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       bad |= !tc::mbar_wait(&sh.mma_done, (uint32_t)k & 1u, &sh.abort_flag);
       __syncwarp();
       tc::fence_after_sync();
-      // the tables: lane i < BM of G's rows A's row i, lane BM + i M's row i
+      bad |= !tc::mbar_wait(&sh.v_full, (uint32_t)k & 1u, &sh.abort_flag);
+      __syncwarp();
+      if constexpr (BM == 64) {  // W^T's key part becomes beta (v - exp(gamma) W^T)
+#pragma unroll 1
+        for (int c0 = 0; c0 < BM; c0 += 16) {
+          uint32_t w[16];
+          tc::tmem_ld16(tmW + lane_off + c0, w);
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int i = c0 + e;
+            w[e] = __float_as_uint(m.beta[i] * (tl_bf16(vs[i * 64]) -
+                                                tc::ex2(m.gam2[i]) * __uint_as_float(w[e])));
+          }
+          tc::tmem_st16(tmW + lane_off + c0, w);
+        }
+        tc::tmem_st_wait();
+      }
+      // the table: lane i < BM of G's rows gives -A's row i, lane BM + i M's
       if (warp * 32 < 2 * BM) {
         const bool is_m = tid >= BM;
         const int i = is_m ? tid - BM : tid;
         const uint64_t path = m.anc[i];  // empty from n on
-        const float gi = m.gam2[i], f = is_m ? 1.f : m.beta[i];
+        const float gi = m.gam2[i], f = is_m ? 1.f : -m.beta[i];
         const uint64_t see = is_m ? path : path & ~(1ull << i);
-        float* row = is_m ? Mt : At;
 #pragma unroll
         for (int c0 = 0; c0 < BM; c0 += 16) {
           uint32_t g[16];
@@ -424,18 +478,16 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           for (int u = 0; u < 4; ++u) {
             const float4 gj = *reinterpret_cast<const float4*>(&m.gam2[c0 + 4 * u]);
             const float gv[4] = {gj.x, gj.y, gj.z, gj.w};
-            float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {  // masked by selects: exp may overflow off the path
+              const int c = c0 + 4 * u + e;
               const float x = f * tc::ex2(gi - gv[e]) * __uint_as_float(g[4 * u + e]);
-              v[e] = (see >> (c0 + 4 * u + e)) & 1 ? x : 0.f;
+              Tp[tl_at<BM>(i, c >> 1) + 2 * (c & 1) + (is_m ? 1 : 0)] = (see >> c) & 1 ? x : 0.f;
             }
-            *reinterpret_cast<float4*>(row + tl_at<BM>(i, c0 / 4 + u)) =
-                make_float4(v[0], v[1], v[2], v[3]);
           }
         }
       }
-      if (tl_compute_or(bad)) break;  // the tables are complete
+      if (tl_compute_or(bad)) break;  // the table is complete
 
       // Rows i, i + 1 of this column and its neighbour: adjacent lanes swap a
       // value, so that each stores a bf16 pair of two columns.
@@ -443,12 +495,26 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       auto store2 = [&](int i, float a, float b) {
         const float recv = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
         const int row = odd ? i + 1 : i;
-        if (row < p.B)
+        if (row < p.B && n >= 0)
           *reinterpret_cast<uint32_t*>(out + row * row_stride) =
               odd ? tl_pack(recv, b) : tl_pack(a, recv);
       };
+      // a row's pairs with the deltas of columns 4 u .. 4 u + 3 (as {d, d}): {x, y}
+      // gains {-A d, M d}
+      auto quad = [&](int row, int u, const uint64_t (&d)[4], int count, uint64_t acc) {
+        const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(Tp + tl_at<BM>(row, 2 * u));
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(Tp + tl_at<BM>(row, 2 * u + 1));
+        const uint64_t c[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < count) acc = f2_fma(c[e], d[e], acc);
+        return acc;
+      };
+      auto diag = [&](int i) {  // M[i][i]
+        return Tp[tl_at<BM>(i, i >> 1) + 2 * (i & 1) + 1];
+      };
       if constexpr (BM <= 32) {
-        float dl[BM];
+        uint64_t dl[BM / 4][4];  // the deltas, as {d, d}
 #pragma unroll
         for (int i0 = 0; i0 < BM; i0 += 16) {
           if (i0 < n) {
@@ -461,29 +527,20 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
             for (int e = 0; e < 16; ++e) {
               const int i = i0 + e;
               o[e & 1] = 0.f;
-              dl[i] = 0.f;
+              dl[i / 4][i % 4] = 0ull;
               if (i < n) {
                 const float ga = tc::ex2(m.gam2[i]);
-                float x = m.beta[i] * (tl_bf16(vr[i]) - ga * __uint_as_float(wk[e]));
-                float y = ga * __uint_as_float(wq[e]);
+                uint64_t xy = f2(m.beta[i] * (tl_bf16(vs[i * 64]) - ga * __uint_as_float(wk[e])),
+                                 ga * __uint_as_float(wq[e]));
                 const uint32_t path = (uint32_t)m.anc[i];
 #pragma unroll
-                for (int u = 0; u <= i / 4; ++u) {
-                  if (BM == 16 || u == i / 4 || (path >> (4 * u)) & 15u) {
-                    const float4 a = *reinterpret_cast<const float4*>(At + tl_at<BM>(i, u));
-                    const float4 b = *reinterpret_cast<const float4*>(Mt + tl_at<BM>(i, u));
-                    const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-                      if (4 * u + d < i) {
-                        x = fmaf(-av[d], dl[4 * u + d], x);
-                        y = fmaf(bv[d], dl[4 * u + d], y);
-                      }
-                    if (u == i / 4) y = fmaf(bv[i & 3], x, y);
-                  }
-                }
-                dl[i] = x;
-                o[e & 1] = p.scale * y;
+                for (int u = 0; u < (i + 3) / 4; ++u)
+                  if (BM == 16 || (path >> (4 * u)) & 15u)
+                    xy = quad(i, u, dl[u], i - 4 * u < 4 ? i - 4 * u : 4, xy);
+                float x, y;
+                f2_split(xy, x, y);
+                dl[i / 4][i % 4] = f2_dup(x);
+                o[e & 1] = p.scale * fmaf(diag(i), x, y);
               }
               if (e & 1) store2(i - 1, o[0], o[1]);
             }
@@ -496,9 +553,6 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
         // deltas in shared memory, four nodes at a time against the four-node
         // blocks that any of their paths touches
         float* Dl = reinterpret_cast<float*>(smem_raw + C::oDelta) + tid;
-        unsigned short vn[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) vn[e] = e < n ? vg[e * row_stride] : (unsigned short)0;
 #pragma unroll 1
         for (int i0 = 0; i0 < n; i0 += 4) {
           uint32_t wk[4], wq[4];
@@ -509,59 +563,41 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
                        : "=r"(wq[0]), "=r"(wq[1]), "=r"(wq[2]), "=r"(wq[3])
                        : "r"(tmW + lane_off + BM + i0));
           tc::tmem_ld_wait();
-          float x[4], y[4];
+          uint64_t xy[4];
           uint64_t any = 0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int i = i0 + e;
             const float ga = tc::ex2(m.gam2[i]);
-            x[e] = i < n ? m.beta[i] * (tl_bf16(vn[e]) - ga * __uint_as_float(wk[e])) : 0.f;
-            y[e] = i < n ? ga * __uint_as_float(wq[e]) : 0.f;
+            xy[e] = i < n ? f2(__uint_as_float(wk[e]), ga * __uint_as_float(wq[e])) : 0ull;
             any |= m.anc[i];
           }
-#pragma unroll
-          for (int e = 0; e < 4; ++e)  // the next four nodes' values
-            vn[e] = i0 + 4 + e < n ? vg[(i0 + 4 + e) * row_stride] : (unsigned short)0;
 #pragma unroll 1
           for (int u = 0; u < i0 / 4; ++u) {
             if (!((any >> (4 * u)) & 15)) continue;
-            float d[4];
+            uint64_t d[4];
 #pragma unroll
-            for (int f = 0; f < 4; ++f) d[f] = Dl[(4 * u + f) * kTlD];
+            for (int f = 0; f < 4; ++f) d[f] = f2_dup(Dl[(4 * u + f) * kTlD]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float4 a = *reinterpret_cast<const float4*>(At + tl_at<BM>(i0 + e, u));
-              const float4 b = *reinterpret_cast<const float4*>(Mt + tl_at<BM>(i0 + e, u));
-              x[e] = fmaf(-a.x, d[0], x[e]);
-              x[e] = fmaf(-a.y, d[1], x[e]);
-              x[e] = fmaf(-a.z, d[2], x[e]);
-              x[e] = fmaf(-a.w, d[3], x[e]);
-              y[e] = fmaf(b.x, d[0], y[e]);
-              y[e] = fmaf(b.y, d[1], y[e]);
-              y[e] = fmaf(b.z, d[2], y[e]);
-              y[e] = fmaf(b.w, d[3], y[e]);
-            }
+            for (int e = 0; e < 4; ++e) xy[e] = quad(i0 + e, u, d, 4, xy[e]);
           }
+          float y[4];
+          uint64_t d[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {  // the four among themselves
-            const float4 a = *reinterpret_cast<const float4*>(At + tl_at<BM>(i0 + e, i0 / 4));
-            const float4 b = *reinterpret_cast<const float4*>(Mt + tl_at<BM>(i0 + e, i0 / 4));
-            const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int f = 0; f < e; ++f) {
-              x[e] = fmaf(-av[f], x[f], x[e]);
-              y[e] = fmaf(bv[f], x[f], y[e]);
-            }
-            y[e] = p.scale * fmaf(bv[e], x[e], y[e]);
-            Dl[(i0 + e) * kTlD] = x[e];
+            float x;
+            f2_split(quad(i0 + e, i0 / 4, d, e, xy[e]), x, y[e]);
+            d[e] = f2_dup(x);
+            y[e] = p.scale * fmaf(diag(i0 + e), x, y[e]);
+            Dl[(i0 + e) * kTlD] = x;
           }
           store2(i0, y[0], y[1]);
           store2(i0 + 2, y[2], y[3]);
         }
 #pragma unroll 1
-        for (int i = (n + 3) & ~3; i < p.B; i += 2) store2(i, 0.f, 0.f);
-        tc::mbar_arrive(&sh.kq_free);  // the tables are read
+        for (int i = n < 0 ? p.B : (n + 3) & ~3; i < p.B; i += 2) store2(i, 0.f, 0.f);
       }
+      tc::mbar_arrive(&sh.done);
     }
     if (bad && !sh.abort_flag) {
       sh.abort_flag = 1;
@@ -593,18 +629,19 @@ PFN_cuTensorMapEncodeTiled_v12000 tl_encode_fn() {
   return fn;
 }
 
-// [R, N, Hk, 128] bf16 as a 4-D map (128, Hk, N, R), box (64, 1, rows, 1);
-// rows past N read as zero
-bool tl_map(CUtensorMap* m, const void* x, const GdrParams& p, int rows) {
+// [R, N, H, 128] bf16 as a 4-D map (128, H, N, R), box (64, 1, rows, 1); rows
+// past N read as zero
+bool tl_map(CUtensorMap* m, const void* x, const GdrParams& p, int H, int rows, bool swizzle) {
   auto fn = tl_encode_fn();
   if (!fn) return false;
-  const cuuint64_t gd[4] = {(cuuint64_t)kTlD, (cuuint64_t)p.Hk, (cuuint64_t)p.B, (cuuint64_t)p.R};
-  const cuuint64_t gs[3] = {(cuuint64_t)kTlD * 2, (cuuint64_t)p.Hk * kTlD * 2,
-                            (cuuint64_t)p.B * p.Hk * kTlD * 2};
+  const cuuint64_t gd[4] = {(cuuint64_t)kTlD, (cuuint64_t)H, (cuuint64_t)p.B, (cuuint64_t)p.R};
+  const cuuint64_t gs[3] = {(cuuint64_t)kTlD * 2, (cuuint64_t)H * kTlD * 2,
+                            (cuuint64_t)p.B * H * kTlD * 2};
   const cuuint32_t bx[4] = {64, 1, (cuuint32_t)rows, 1};
   const cuuint32_t es[4] = {1, 1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(x), gd, gs, bx, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
          CUDA_SUCCESS;
 }
@@ -612,7 +649,9 @@ bool tl_map(CUtensorMap* m, const void* x, const GdrParams& p, int rows) {
 template <int BM>
 cudaError_t launch_tl(const GdrParams& p, cudaStream_t stream) {
   TlMaps maps;
-  if (!tl_map(&maps.k, p.k, p, BM) || !tl_map(&maps.q, p.q, p, BM)) return cudaErrorInvalidValue;
+  if (!tl_map(&maps.k, p.k, p, p.Hk, BM, true) || !tl_map(&maps.q, p.q, p, p.Hk, BM, true) ||
+      !tl_map(&maps.v, p.v, p, p.Hv, BM, false))
+    return cudaErrorInvalidValue;
   constexpr int smem = tl_smem<BM>();
   static_assert(TlCfg<BM>::kCtas * (smem + 1024) <= 228 * 1024, "CTAs per SM");
   cudaError_t e = cudaFuncSetAttribute(tree_linear_tc_kernel<BM>,
