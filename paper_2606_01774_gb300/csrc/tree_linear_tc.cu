@@ -7,23 +7,27 @@
 //        G   = [K; Q] K^T      M = 128 (rows on lanes), N = BM, over S0^T
 //   A[i][j] = beta_i exp(gamma_i - gamma_j) G[i][j]     for j on i's path, j != i
 //   M[i][j] = exp(gamma_i - gamma_j) G[BM + i][j]       for j on i's path
+//   X_i = beta_i (v_i - exp(gamma_i) W^T[.][i]),  Y_i = exp(gamma_i) W^T[.][BM + i]
 //   for i = 0, 1, ...   (thread c owns value column c; parents come first)
-//     delta_i = beta_i (v_i - exp(gamma_i) W^T[c][i]) - sum_j A[i][j] delta_j
-//     out_i   = scale (exp(gamma_i) W^T[c][BM + i] + sum_j M[i][j] delta_j)
-// The state is rounded to bf16 for W; G, the tables, the substitution and the
-// readout are fp32.  Substitution and readout run on the CUDA cores in one
-// pass: a tree's rows are short (its depth), and a block of four columns that
-// a node's path does not touch is skipped.
+//     delta_i = X_i - sum_j A[i][j] delta_j,   out_i = scale (Y_i + sum_j M[i][j] delta_j)
+// The nodes go in blocks of 16.  Inside a block substitution and readout run on
+// the CUDA cores in one pass, with A and M side by side as pairs (-A, M), so
+// that one packed multiply-add carries a delta into both sums.  From a finished
+// block to the later ones,
+//   MMA  [X | Y]^T (later) += delta^T [-A | M]^T        M = 128, N = 16 .. 48, K = 16
+// with deltas and tables as bf16 high and low parts, three products each: both
+// sums gather in tensor memory where the first MMA left X and Y.  (All on the
+// CUDA cores, 61 nodes were bound by reading the tables from shared memory,
+// 26 us a call of 192 items against LINEAR_MEASURED.)
+// The state is rounded to bf16 for W; everything else is fp32 or split.
 //
 // Bound by the state's bytes: 64 KiB an item, so a CTA's life is organised
 // around its copies.  Warp 4 runs ahead: it finds the next item, streams its
 // state in 16 KiB pieces through a ring, its keys, queries and values by TMA,
 // works out its paths and gates (pointer doubling), and issues the MMAs as the
 // pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
-// tensor memory, then tables, substitution and readout.  A and M lie side by
-// side as pairs (-A, M), so that one packed multiply-add carries a delta into
-// both sums.  BM <= 32: 128 tensor-memory columns and under 76 KiB, three CTAs
-// per SM; BM = 64: two.
+// tensor memory, then tables, substitution and readout.  BM <= 32: 128
+// tensor-memory columns and under 76 KiB, three CTAs per SM; BM = 64: two.
 // Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
 // lets its copies and MMAs land, frees its tensor memory and exits.
 #include <cudaTypedefs.h>
@@ -58,21 +62,23 @@ struct TlMeta {
 template <int BM>
 struct TlCfg {
   static constexpr int kCtas = BM == 64 ? 2 : 3;               // per SM
-  static constexpr int kRing = BM == 16 ? 3 : 2;               // state pieces in flight
+  static constexpr int kBlocks = BM / 16;
+  static constexpr int kRing = BM == 32 ? 2 : 3;               // state pieces in flight
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
   static constexpr int kV = 2 * BM * 128;                      // 2 chunks of value rows x 128 B
-  static constexpr int kTable = BM * BM * 8;                   // pairs (-A, M)
-  // BM = 64: the table takes the key / query buffer's place, and the deltas,
-  // too many for registers, the values', which beta (v - exp(gamma) K S0) in
-  // tensor memory has replaced by then
+  static constexpr int kDiag = kBlocks * 16 * 16 * 8;          // pairs (-A, M) inside blocks
+  // -A high, low, M high, low between blocks: rows 16 .. BM - 1, K-major SW128
+  static constexpr int kCross = (BM - 16) * 128;
+  // BM = 64: the tables take the key / query buffer's place
   static constexpr bool kOverlay = BM == 64;
-  static constexpr int kDelta = BM == 64 ? BM * kTlD * 4 : 0;
+  static constexpr int kTables = kDiag + 4 * kCross;
   static constexpr int oKQ = 0;
   static constexpr int oRing = kKQ;
-  static constexpr int oTable = kOverlay ? 0 : oRing + kRing * kPieceBytes;
-  static constexpr int oDelta = oRing + kRing * kPieceBytes;
-  static constexpr int oV = kOverlay ? oDelta + kDelta - kV : oTable + kTable;
+  static constexpr int oCross = kOverlay ? 0 : oRing + kRing * kPieceBytes;
+  static constexpr int oDiag = oCross + 4 * kCross;
+  static constexpr int oV = kOverlay ? oRing + kRing * kPieceBytes : oDiag + kDiag;
   static constexpr int oShared = oV + kV;
+  static_assert(!kOverlay || kTables <= kKQ, "tables over keys and queries");
   static constexpr int kTmem = 64 + 2 * BM <= 128 ? 128 : 256;
 };
 
@@ -80,7 +86,7 @@ template <int BM>
 struct alignas(16) TlShared {
   TlMeta<BM> meta[3];
   uint64_t full[4], empty[4];  // ring pieces
-  uint64_t kq_full, v_full, done, mma_done, meta_full[3];  // done: an item's readout
+  uint64_t kq_full, v_full, done, mma_done, upd, meta_full[3];  // done: an item's readout
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -95,12 +101,19 @@ struct TlMaps {
   CUtensorMap v;     // (128, Hv, N, R) box (64, 1, BM, 1), no swizzle
 };
 
-// Word offset of the pairs of columns 2 u, 2 u + 1 of row `row` of a BM x BM
-// table of pairs whose 16-byte units are XOR-swizzled by the row (a warp writes
-// a row per lane).
-template <int BM>
+// Word offset of the pairs of columns 2 u, 2 u + 1 of row `row` of a block's 16 x
+// 16 pairs, whose 16-byte units are XOR-swizzled by the row (a warp writes a row
+// per lane).
 __device__ __forceinline__ int tl_at(int row, int u) {
-  return row * (2 * BM) + ((u ^ (row & (BM / 2 - 1))) << 2);
+  return row * 32 + ((u ^ (row & 7)) << 2);
+}
+
+// x = hi + lo to about 2^-16 relative, each a bf16 pair (a low, b high)
+__device__ __forceinline__ void tl_split(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
 __device__ __forceinline__ bool tl_warp_wait(uint64_t* bar, uint32_t parity, const int* abort) {
@@ -144,7 +157,8 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
   TlShared<BM>& sh = *reinterpret_cast<TlShared<BM>*>(smem_raw + C::oShared);
   uint8_t* KQ = smem_raw + C::oKQ;
   uint8_t* ring = smem_raw + C::oRing;
-  float* Tp = reinterpret_cast<float*>(smem_raw + C::oTable);
+  float* Tp = reinterpret_cast<float*>(smem_raw + C::oDiag);
+  uint8_t* Cross = smem_raw + C::oCross;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tc::smem_u32(smem_raw) & 1023u) {
     if (tid == 0) flag(p.dev_status, FLARE_DEV_WAIT_TIMEOUT);
@@ -160,6 +174,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
     tc::mbar_init(&sh.v_full, 1);
     tc::mbar_init(&sh.done, kTlCompute);
     tc::mbar_init(&sh.mma_done, 1);
+    tc::mbar_init(&sh.upd, 1);
     for (int b = 0; b < 3; ++b) tc::mbar_init(&sh.meta_full[b], 1);
     tc::fence_mbar_init();
   }
@@ -167,8 +182,8 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmS = sh.tmem_base;  // S0^T as bf16 pairs (64 columns); then G
-  const uint32_t tmW = tmS + 64;      // W^T: [K part | Q part]
+  const uint32_t tmS = sh.tmem_base;  // S0^T as bf16 pairs (64 columns); then G, then deltas
+  const uint32_t tmW = tmS + 64;      // W^T: [K part | Q part], then [X | Y]
   const int total = p.R * p.Hv;
 
   if (warp == 4) {
@@ -410,15 +425,18 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
   } else {
     // ------------------------------------------------------------ compute
     const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
-    uint32_t used = 0;  // ring pieces consumed
+    uint32_t used = 0;       // ring pieces consumed
+    uint32_t upd_phase = 0;  // of the updates between blocks
     bool bad = false;
 #pragma unroll 1
     for (int k = 0;; ++k) {
       bad |= !tc::mbar_wait(&sh.meta_full[k % 3], (uint32_t)(k / 3) & 1u, &sh.abort_flag);
-      if (tl_compute_or(bad)) break;  // the same answer on every compute thread
       const TlMeta<BM>& m = sh.meta[k % 3];
-      const int item = m.item, n = m.n;
-      if (item < 0) break;
+      const int item = bad ? -1 : m.item, n = m.n;
+      if (item < 0) {  // a barrier on this way out too: a thread that gave up
+        tl_compute_or(bad);  // meets the others here or at the tables
+        break;
+      }
       const int r = item / p.Hv, j = item - r * p.Hv;
       const size_t row0 = ((size_t)r * p.B * p.Hv + j) * kTlD;
       const size_t row_stride = (size_t)p.Hv * kTlD;
@@ -446,48 +464,77 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       tc::fence_after_sync();
       bad |= !tc::mbar_wait(&sh.v_full, (uint32_t)k & 1u, &sh.abort_flag);
       __syncwarp();
-      if constexpr (BM == 64) {  // W^T's key part becomes beta (v - exp(gamma) W^T)
+      auto x_of = [&](int i, uint32_t w) {
+        return m.beta[i] * (tl_bf16(vs[i * 64]) - tc::ex2(m.gam2[i]) * __uint_as_float(w));
+      };
+      auto y_of = [&](int i, uint32_t w) { return tc::ex2(m.gam2[i]) * __uint_as_float(w); };
+      if constexpr (BM > 16) {  // W^T becomes [X | Y], where the blocks' sums gather
 #pragma unroll 1
         for (int c0 = 0; c0 < BM; c0 += 16) {
-          uint32_t w[16];
-          tc::tmem_ld16(tmW + lane_off + c0, w);
+          uint32_t wk[16], wq[16];
+          tc::tmem_ld16(tmW + lane_off + c0, wk);
+          tc::tmem_ld16(tmW + lane_off + BM + c0, wq);
           tc::tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int i = c0 + e;
-            w[e] = __float_as_uint(m.beta[i] * (tl_bf16(vs[i * 64]) -
-                                                tc::ex2(m.gam2[i]) * __uint_as_float(w[e])));
+            // unused nodes' rows may hold anything: their sums are not read, and
+            // their table rows are zero
+            wk[e] = __float_as_uint(x_of(c0 + e, wk[e]));
+            wq[e] = __float_as_uint(y_of(c0 + e, wq[e]));
           }
-          tc::tmem_st16(tmW + lane_off + c0, w);
+          tc::tmem_st16(tmW + lane_off + c0, wk);
+          tc::tmem_st16(tmW + lane_off + BM + c0, wq);
         }
         tc::tmem_st_wait();
       }
-      // the table: lane i < BM of G's rows gives -A's row i, lane BM + i M's
+      // the tables: lane i < BM of G's rows gives -A's row i, lane BM + i M's
       if (warp * 32 < 2 * BM) {
         const bool is_m = tid >= BM;
-        const int i = is_m ? tid - BM : tid;
+        const int i = is_m ? tid - BM : tid, own = i >> 4;
         const uint64_t path = m.anc[i];  // empty from n on
         const float gi = m.gam2[i], f = is_m ? 1.f : -m.beta[i];
         const uint64_t see = is_m ? path : path & ~(1ull << i);
-#pragma unroll
-        for (int c0 = 0; c0 < BM; c0 += 16) {
+#pragma unroll 1
+        for (int blk = 0; blk < C::kBlocks; ++blk) {
           uint32_t g[16];
-          tc::tmem_ld16(tmS + lane_off + c0, g);
+          tc::tmem_ld16(tmS + lane_off + 16 * blk, g);
           tc::tmem_ld_wait();
+          float v[16];
+          const uint32_t mask = (uint32_t)(see >> (16 * blk));
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const float4 gj = *reinterpret_cast<const float4*>(&m.gam2[c0 + 4 * u]);
+            const float4 gj = *reinterpret_cast<const float4*>(&m.gam2[16 * blk + 4 * u]);
             const float gv[4] = {gj.x, gj.y, gj.z, gj.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {  // masked by selects: exp may overflow off the path
-              const int c = c0 + 4 * u + e;
               const float x = f * tc::ex2(gi - gv[e]) * __uint_as_float(g[4 * u + e]);
-              Tp[tl_at<BM>(i, c >> 1) + 2 * (c & 1) + (is_m ? 1 : 0)] = (see >> c) & 1 ? x : 0.f;
+              v[4 * u + e] = (mask >> (4 * u + e)) & 1 ? x : 0.f;
+            }
+          }
+          if (blk == own) {
+            float* row = Tp + own * 512;
+#pragma unroll
+            for (int c = 0; c < 16; ++c)
+              row[tl_at(i & 15, c >> 1) + 2 * (c & 1) + (is_m ? 1 : 0)] = v[c];
+          } else if (blk < own) {
+            uint32_t hi[8], lo[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) tl_split(v[2 * c], v[2 * c + 1], hi[c], lo[c]);
+            uint8_t* row = Cross + (is_m ? 2 : 0) * C::kCross + (i - 16) * 128;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const int at = ((2 * blk + u) ^ (i & 7)) << 4;
+              *reinterpret_cast<uint4*>(row + at) =
+                  make_uint4(hi[4 * u], hi[4 * u + 1], hi[4 * u + 2], hi[4 * u + 3]);
+              *reinterpret_cast<uint4*>(row + C::kCross + at) =
+                  make_uint4(lo[4 * u], lo[4 * u + 1], lo[4 * u + 2], lo[4 * u + 3]);
             }
           }
         }
+        if (BM > 16) tc::fence_async_smem();  // the cross tables are MMA operands
       }
-      if (tl_compute_or(bad)) break;  // the table is complete
+      tc::fence_before_sync();
+      if (tl_compute_or(bad)) break;  // the tables are complete
 
       // Rows i, i + 1 of this column and its neighbour: adjacent lanes swap a
       // value, so that each stores a bf16 pair of two columns.
@@ -499,104 +546,85 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           *reinterpret_cast<uint32_t*>(out + row * row_stride) =
               odd ? tl_pack(recv, b) : tl_pack(a, recv);
       };
-      // a row's pairs with the deltas of columns 4 u .. 4 u + 3 (as {d, d}): {x, y}
-      // gains {-A d, M d}
-      auto quad = [&](int row, int u, const uint64_t (&d)[4], int count, uint64_t acc) {
-        const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(Tp + tl_at<BM>(row, 2 * u));
-        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(Tp + tl_at<BM>(row, 2 * u + 1));
-        const uint64_t c[4] = {a.x, a.y, b.x, b.y};
+      bool out_of_time = false;
+#pragma unroll 1
+      for (int blk = 0; blk < C::kBlocks; ++blk) {
+        const int i0 = 16 * blk;
+        if (i0 >= n) {  // unused nodes
+          for (int e = 0; e < 16; e += 2) store2(i0 + e, 0.f, 0.f);
+          continue;
+        }
+        const float* T = Tp + blk * 512;
+        uint32_t xr[16], yr[16];
+        tc::tmem_ld16(tmW + lane_off + i0, xr);
+        tc::tmem_ld16(tmW + lane_off + BM + i0, yr);
+        tc::tmem_ld_wait();
+        uint64_t dl[16];  // the deltas, as {d, d}
+        float o[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < count) acc = f2_fma(c[e], d[e], acc);
-        return acc;
-      };
-      auto diag = [&](int i) {  // M[i][i]
-        return Tp[tl_at<BM>(i, i >> 1) + 2 * (i & 1) + 1];
-      };
-      if constexpr (BM <= 32) {
-        uint64_t dl[BM / 4][4];  // the deltas, as {d, d}
+        for (int e = 0; e < 16; ++e) {
+          const int i = i0 + e;
+          o[e & 1] = 0.f;
+          dl[e] = 0ull;
+          if (i < n) {
+            uint64_t xy = BM == 16 ? f2(x_of(i, xr[e]), y_of(i, yr[e]))
+                                   : f2(__uint_as_float(xr[e]), __uint_as_float(yr[e]));
 #pragma unroll
-        for (int i0 = 0; i0 < BM; i0 += 16) {
-          if (i0 < n) {
-            uint32_t wk[16], wq[16];
-            tc::tmem_ld16(tmW + lane_off + i0, wk);
-            tc::tmem_ld16(tmW + lane_off + BM + i0, wq);
-            tc::tmem_ld_wait();
-            float o[2];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int i = i0 + e;
-              o[e & 1] = 0.f;
-              dl[i / 4][i % 4] = 0ull;
-              if (i < n) {
-                const float ga = tc::ex2(m.gam2[i]);
-                uint64_t xy = f2(m.beta[i] * (tl_bf16(vs[i * 64]) - ga * __uint_as_float(wk[e])),
-                                 ga * __uint_as_float(wq[e]));
-                const uint32_t path = (uint32_t)m.anc[i];
-#pragma unroll
-                for (int u = 0; u < (i + 3) / 4; ++u)
-                  if (BM == 16 || (path >> (4 * u)) & 15u)
-                    xy = quad(i, u, dl[u], i - 4 * u < 4 ? i - 4 * u : 4, xy);
-                float x, y;
-                f2_split(xy, x, y);
-                dl[i / 4][i % 4] = f2_dup(x);
-                o[e & 1] = p.scale * fmaf(diag(i), x, y);
-              }
-              if (e & 1) store2(i - 1, o[0], o[1]);
+            for (int u = 0; u < (e + 1) / 2; ++u) {  // columns 2 u, 2 u + 1
+              const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(T + tl_at(e, u));
+              xy = f2_fma(c.x, dl[2 * u], xy);
+              if (2 * u + 1 < e) xy = f2_fma(c.y, dl[2 * u + 1], xy);
             }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) store2(i0 + e, 0.f, 0.f);
+            float x, y;
+            f2_split(xy, x, y);
+            dl[e] = f2_dup(x);
+            o[e & 1] = p.scale * fmaf(T[tl_at(e, e >> 1) + 2 * (e & 1) + 1], x, y);
           }
+          if (e & 1) store2(i - 1, o[0], o[1]);
         }
-      } else {
-        // deltas in shared memory, four nodes at a time against the four-node
-        // blocks that any of their paths touches
-        float* Dl = reinterpret_cast<float*>(smem_raw + C::oDelta) + tid;
-#pragma unroll 1
-        for (int i0 = 0; i0 < n; i0 += 4) {
-          uint32_t wk[4], wq[4];
-          asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
-                       : "=r"(wk[0]), "=r"(wk[1]), "=r"(wk[2]), "=r"(wk[3])
-                       : "r"(tmW + lane_off + i0));
-          asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
-                       : "=r"(wq[0]), "=r"(wq[1]), "=r"(wq[2]), "=r"(wq[3])
-                       : "r"(tmW + lane_off + BM + i0));
-          tc::tmem_ld_wait();
-          uint64_t xy[4];
-          uint64_t any = 0;
+        if (BM > 16 && i0 + 16 < n) {
+          // this block's deltas into the later blocks' sums
+          uint32_t hl[16];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i = i0 + e;
-            const float ga = tc::ex2(m.gam2[i]);
-            xy[e] = i < n ? f2(__uint_as_float(wk[e]), ga * __uint_as_float(wq[e])) : 0ull;
-            any |= m.anc[i];
+          for (int e = 0; e < 8; ++e) {
+            float a, b, unused;
+            f2_split(dl[2 * e], a, unused);
+            f2_split(dl[2 * e + 1], b, unused);
+            tl_split(a, b, hl[e], hl[8 + e]);
           }
-#pragma unroll 1
-          for (int u = 0; u < i0 / 4; ++u) {
-            if (!((any >> (4 * u)) & 15)) continue;
-            uint64_t d[4];
+          tc::tmem_st16(tmS + lane_off, hl);
+          tc::tmem_st_wait();
+          tc::fence_before_sync();
+          tc::named_bar_sync(1, kTlCompute);
+          if (warp == 0) {
+            tc::fence_after_sync();
+            const int rows = BM - 16 - i0;  // of the later blocks
+            const uint32_t id = tc::idesc_bf16(128, rows, false, false);
+            const uint64_t base = tc::sdesc_sw128(tc::smem_u32(Cross), 16, 1024) +
+                                  (uint64_t)((i0 * 128 + blk * 32) >> 4);
+            if (tc::elect_one()) {
 #pragma unroll
-            for (int f = 0; f < 4; ++f) d[f] = f2_dup(Dl[(4 * u + f) * kTlD]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) xy[e] = quad(i0 + e, u, d, 4, xy[e]);
+              for (int part = 0; part < 2; ++part) {  // -A into X, M into Y
+                const uint32_t d = tmW + part * BM + i0 + 16;
+                const uint64_t hi = base + (uint64_t)((2 * part * C::kCross) >> 4);
+                const uint64_t lo = hi + (uint64_t)(C::kCross >> 4);
+                tc::mma_bf16_ts(d, tmS, hi, id, 1);
+                tc::mma_bf16_ts(d, tmS, lo, id, 1);
+                tc::mma_bf16_ts(d, tmS + 8, hi, id, 1);
+              }
+              tc::mma_commit(&sh.upd);
+            }
+            __syncwarp();
           }
-          float y[4];
-          uint64_t d[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {  // the four among themselves
-            float x;
-            f2_split(quad(i0 + e, i0 / 4, d, e, xy[e]), x, y[e]);
-            d[e] = f2_dup(x);
-            y[e] = p.scale * fmaf(diag(i0 + e), x, y[e]);
-            Dl[(i0 + e) * kTlD] = x;
-          }
-          store2(i0, y[0], y[1]);
-          store2(i0 + 2, y[2], y[3]);
+          // after a timeout on: the same barriers, nothing waited for
+          if (!out_of_time) out_of_time = !tc::mbar_wait(&sh.upd, upd_phase, &sh.abort_flag);
+          upd_phase ^= 1u;
+          __syncwarp();
+          tc::fence_after_sync();
         }
-#pragma unroll 1
-        for (int i = n < 0 ? p.B : (n + 3) & ~3; i < p.B; i += 2) store2(i, 0.f, 0.f);
       }
+      bad |= out_of_time;
+      tc::fence_before_sync();
       tc::mbar_arrive(&sh.done);
     }
     if (bad && !sh.abort_flag) {
