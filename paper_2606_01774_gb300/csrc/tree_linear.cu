@@ -10,7 +10,8 @@
 //
 // One CTA per (request, value head).  Thread (part, c) owns value column c;
 // the parts share the nodes in the products with S0, whose rows stream
-// through registers against keys and queries broadcast from shared memory.
+// through registers, 16 ahead of their use, against keys and queries broadcast
+// from shared memory.
 // The Grams are built one (i, j) pair per thread.  Column c's substitution and
 // readout need only its own deltas.
 #include "common.cuh"
@@ -42,6 +43,12 @@ __global__ void __launch_bounds__(kParts * DV) tree_linear_kernel(GdrParams p) {
     if (tid == 0) flag(p.dev_status, bad);
     return;
   }
+  // the state's column c, 16 rows ahead of their use, the first ones from here on
+  constexpr int kAhead = 16;
+  const float* S = p.state_pool + ((size_t)slot * p.Hv + j) * DK * DV + c;
+  float ahead[kAhead];
+#pragma unroll
+  for (int e = 0; e < kAhead; ++e) ahead[e] = S[(size_t)e * DV];
   if (tid < 32) {
     int p0, p1;
     const bool ok = warp_load_tree(p.parent + (size_t)r * p.B, n, p0, p1);
@@ -68,10 +75,16 @@ __global__ void __launch_bounds__(kParts * DV) tree_linear_kernel(GdrParams p) {
   const T* q = static_cast<const T*>(p.q) + ((size_t)r * p.B * p.Hk + h) * DK;
   const T* v = static_cast<const T*>(p.v) + ((size_t)r * p.B * p.Hv + j) * DV;
   T* out = static_cast<T*>(p.out_causal) + ((size_t)r * p.B * p.Hv + j) * DV;
-  for (int e = tid; e < n * DK; e += kThreads) {
-    const int i = e / DK, d = e % DK;
-    Ks[i * kKS + d] = to_f32(k[(size_t)i * p.Hk * DK + d]);
-    Qs[i * kKS + d] = to_f32(q[(size_t)i * p.Hk * DK + d]);
+  constexpr int kE = 16 / sizeof(T);  // staged in 16-byte pieces
+  for (int e = tid; e < n * (DK / kE); e += kThreads) {
+    const int i = e / (DK / kE), d = e % (DK / kE) * kE;
+    const uint4 kw = *reinterpret_cast<const uint4*>(k + (size_t)i * p.Hk * DK + d);
+    const uint4 qw = *reinterpret_cast<const uint4*>(q + (size_t)i * p.Hk * DK + d);
+#pragma unroll
+    for (int x = 0; x < kE; ++x) {
+      Ks[i * kKS + d + x] = to_f32(reinterpret_cast<const T*>(&kw)[x]);
+      Qs[i * kKS + d + x] = to_f32(reinterpret_cast<const T*>(&qw)[x]);
+    }
   }
   __syncthreads();
   if (!tree_ok) {
@@ -106,23 +119,29 @@ __global__ void __launch_bounds__(kParts * DV) tree_linear_kernel(GdrParams p) {
   }
   // K S0 and Q S0: this part's nodes, column c
   {
-    const float* S = p.state_pool + ((size_t)slot * p.Hv + j) * DK * DV + c;
     const int n0 = part * kPer, n1 = min(n, n0 + kPer);
     float wk[kPer], wq[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) wk[i] = wq[i] = 0.f;
     if (n0 < n) {
 #pragma unroll 1
-      for (int d = 0; d < DK; d += 4) {
-        const float s0 = S[(size_t)d * DV], s1 = S[(size_t)(d + 1) * DV];
-        const float s2 = S[(size_t)(d + 2) * DV], s3 = S[(size_t)(d + 3) * DV];
+      for (int d0 = 0; d0 < DK; d0 += kAhead) {
+        float s[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+          s[e] = ahead[e];
+          if (d0 + kAhead < DK) ahead[e] = S[(size_t)(d0 + kAhead + e) * DV];
+        }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           if (n0 + i < n1) {
-            const float4 a = *reinterpret_cast<const float4*>(Ks + (n0 + i) * kKS + d);
-            const float4 b = *reinterpret_cast<const float4*>(Qs + (n0 + i) * kKS + d);
-            wk[i] = fmaf(a.x, s0, fmaf(a.y, s1, fmaf(a.z, s2, fmaf(a.w, s3, wk[i]))));
-            wq[i] = fmaf(b.x, s0, fmaf(b.y, s1, fmaf(b.z, s2, fmaf(b.w, s3, wq[i]))));
+#pragma unroll
+            for (int e = 0; e < kAhead; e += 4) {
+              const float4 a = *reinterpret_cast<const float4*>(Ks + (n0 + i) * kKS + d0 + e);
+              const float4 b = *reinterpret_cast<const float4*>(Qs + (n0 + i) * kKS + d0 + e);
+              wk[i] = fmaf(a.x, s[e], fmaf(a.y, s[e + 1], fmaf(a.z, s[e + 2], fmaf(a.w, s[e + 3], wk[i]))));
+              wq[i] = fmaf(b.x, s[e], fmaf(b.y, s[e + 1], fmaf(b.z, s[e + 2], fmaf(b.w, s[e + 3], wq[i]))));
+            }
           }
         }
       }

@@ -63,9 +63,13 @@ template <int BM>
 struct TlCfg {
   static constexpr int kCtas = BM == 64 ? 2 : 3;               // per SM
   static constexpr int kBlocks = BM / 16;
-  static constexpr int kRing = BM == 32 ? 2 : 3;               // state pieces in flight
+  // state pieces in flight: with a whole item's, BM = 16, CTAs that run in step
+  // keep DRAM busy through their compute phases (3 pieces: 33.4 us, 4: RING_MEASURED
+  // for 64 requests of 16 nodes)
+  static constexpr int kRing = BM == 16 ? 4 : BM == 32 ? 2 : 3;
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
-  static constexpr int kV = 2 * BM * 128;                      // 2 chunks of value rows x 128 B
+  // 2 chunks of value rows x 128 B; BM = 16: in registers, an item ahead
+  static constexpr int kV = BM == 16 ? 0 : 2 * BM * 128;
   static constexpr int kDiag = kBlocks * 16 * 16 * 8;          // pairs (-A, M) inside blocks
   // -A high, low, M high, low between blocks: rows 16 .. BM - 1, K-major SW128
   static constexpr int kCross = (BM - 16) * 128;
@@ -139,10 +143,6 @@ __device__ __forceinline__ bool tl_compute_or(bool x) {
 __device__ __forceinline__ uint32_t tl_pack(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-__device__ __forceinline__ float tl_bf16(unsigned short x) {
-  return __uint_as_float((uint32_t)x << 16);
 }
 
 }  // namespace
@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
     };
 
     auto issue_v = [&](int item) {
+      if (C::kV == 0) return;
       if (lane == 0) {
         const int r = item / p.Hv, j = item - r * p.Hv;
         uint8_t* dst = smem_raw + C::oV;
@@ -428,11 +429,26 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
     uint32_t used = 0;       // ring pieces consumed
     uint32_t upd_phase = 0;  // of the updates between blocks
     bool bad = false;
+    constexpr int kVr = C::kV == 0 ? BM : 1;
+    uint32_t vr[kVr];  // BM = 16: this column's values
+    // the k-th item (-1: no more, or a wait that gave up), its values on their way
+    auto take_item = [&](int k) -> int {
+      bad |= !tc::mbar_wait(&sh.meta_full[k % 3], (uint32_t)(k / 3) & 1u, &sh.abort_flag);
+      const int item = bad ? -1 : sh.meta[k % 3].item;
+      if (C::kV == 0 && item >= 0) {
+        const int r = item / p.Hv, j = item - r * p.Hv;
+        const unsigned short* v = static_cast<const unsigned short*>(p.v) +
+                                  ((size_t)r * p.B * p.Hv + j) * kTlD + tid;
+#pragma unroll
+        for (int i = 0; i < kVr; ++i) vr[i] = __ldg(v + (size_t)min(i, p.B - 1) * p.Hv * kTlD);
+      }
+      return item;
+    };
+    int item = take_item(0);
 #pragma unroll 1
     for (int k = 0;; ++k) {
-      bad |= !tc::mbar_wait(&sh.meta_full[k % 3], (uint32_t)(k / 3) & 1u, &sh.abort_flag);
       const TlMeta<BM>& m = sh.meta[k % 3];
-      const int item = bad ? -1 : m.item, n = m.n;
+      const int n = m.n;
       if (item < 0) {  // a barrier on this way out too: a thread that gave up
         tl_compute_or(bad);  // meets the others here or at the tables
         break;
@@ -462,10 +478,10 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       bad |= !tc::mbar_wait(&sh.mma_done, (uint32_t)k & 1u, &sh.abort_flag);
       __syncwarp();
       tc::fence_after_sync();
-      bad |= !tc::mbar_wait(&sh.v_full, (uint32_t)k & 1u, &sh.abort_flag);
+      if (C::kV != 0) bad |= !tc::mbar_wait(&sh.v_full, (uint32_t)k & 1u, &sh.abort_flag);
       __syncwarp();
-      auto x_of = [&](int i, uint32_t w) {
-        return m.beta[i] * (tl_bf16(vs[i * 64]) - tc::ex2(m.gam2[i]) * __uint_as_float(w));
+      auto x_of = [&](int i, uint32_t v, uint32_t w) {
+        return m.beta[i] * (__uint_as_float(v << 16) - tc::ex2(m.gam2[i]) * __uint_as_float(w));
       };
       auto y_of = [&](int i, uint32_t w) { return tc::ex2(m.gam2[i]) * __uint_as_float(w); };
       if constexpr (BM > 16) {  // W^T becomes [X | Y], where the blocks' sums gather
@@ -479,7 +495,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           for (int e = 0; e < 16; ++e) {
             // unused nodes' rows may hold anything: their sums are not read, and
             // their table rows are zero
-            wk[e] = __float_as_uint(x_of(c0 + e, wk[e]));
+            wk[e] = __float_as_uint(x_of(c0 + e, vs[(c0 + e) * 64], wk[e]));
             wq[e] = __float_as_uint(y_of(c0 + e, wq[e]));
           }
           tc::tmem_st16(tmW + lane_off + c0, wk);
@@ -567,7 +583,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           o[e & 1] = 0.f;
           dl[e] = 0ull;
           if (i < n) {
-            uint64_t xy = BM == 16 ? f2(x_of(i, xr[e]), y_of(i, yr[e]))
+            uint64_t xy = BM == 16 ? f2(x_of(i, vr[e % kVr], xr[e]), y_of(i, yr[e]))
                                    : f2(__uint_as_float(xr[e]), __uint_as_float(yr[e]));
 #pragma unroll
             for (int u = 0; u < (e + 1) / 2; ++u) {  // columns 2 u, 2 u + 1
@@ -626,6 +642,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       bad |= out_of_time;
       tc::fence_before_sync();
       tc::mbar_arrive(&sh.done);
+      item = take_item(k + 1);
     }
     if (bad && !sh.abort_flag) {
       sh.abort_flag = 1;
