@@ -27,28 +27,44 @@ __device__ __forceinline__ bool warp_load_tree(const int32_t* __restrict__ paren
 
 // The paths of nodes lane and lane + 32 as bit sets (itself and its ancestors;
 // empty past n), by pointer doubling: after k rounds a set holds the 2^k
-// nearest members.  The parents must have passed warp_load_tree.
-__device__ __forceinline__ void warp_paths(int n, int p0, int p1, uint64_t& a0, uint64_t& a1) {
+// nearest members.  x0 and x1 become their sums over the paths.  The parents
+// must have passed warp_load_tree.  NODES = 32: no node has an upper half.
+template <int NODES>
+__device__ __forceinline__ void warp_paths(int n, int p0, int p1, uint64_t& a0, uint64_t& a1,
+                                           float& x0, float& x1) {
   const int lane = threadIdx.x & 31;
   a0 = lane < n ? 1ull << lane : 0ull;
   a1 = lane + 32 < n ? 1ull << (lane + 32) : 0ull;
 #pragma unroll 1
   while (__any_sync(0xffffffffu, p0 >= 0 || p1 >= 0)) {
     const uint64_t l0 = shfl64(a0, p0 & 31), h0 = shfl64(a1, p0 & 31);
-    const uint64_t l1 = shfl64(a0, p1 & 31), h1 = shfl64(a1, p1 & 31);
+    const float xl0 = __shfl_sync(0xffffffffu, x0, p0 & 31);
+    const float xh0 = __shfl_sync(0xffffffffu, x1, p0 & 31);
     const int ql0 = __shfl_sync(0xffffffffu, p0, p0 & 31);
     const int qh0 = __shfl_sync(0xffffffffu, p1, p0 & 31);
-    const int ql1 = __shfl_sync(0xffffffffu, p0, p1 & 31);
-    const int qh1 = __shfl_sync(0xffffffffu, p1, p1 & 31);
+    if constexpr (NODES > 32) {
+      const uint64_t l1 = shfl64(a0, p1 & 31), h1 = shfl64(a1, p1 & 31);
+      const float xl1 = __shfl_sync(0xffffffffu, x0, p1 & 31);
+      const float xh1 = __shfl_sync(0xffffffffu, x1, p1 & 31);
+      const int ql1 = __shfl_sync(0xffffffffu, p0, p1 & 31);
+      const int qh1 = __shfl_sync(0xffffffffu, p1, p1 & 31);
+      if (p1 >= 0) {
+        a1 |= p1 < 32 ? l1 : h1;
+        x1 += p1 < 32 ? xl1 : xh1;
+        p1 = p1 < 32 ? ql1 : qh1;
+      }
+    }
     if (p0 >= 0) {
       a0 |= p0 < 32 ? l0 : h0;
+      x0 += p0 < 32 ? xl0 : xh0;
       p0 = p0 < 32 ? ql0 : qh0;
     }
-    if (p1 >= 0) {
-      a1 |= p1 < 32 ? l1 : h1;
-      p1 = p1 < 32 ? ql1 : qh1;
-    }
   }
+}
+
+__device__ __forceinline__ void warp_paths(int n, int p0, int p1, uint64_t& a0, uint64_t& a1) {
+  float x0 = 0.f, x1 = 0.f;
+  warp_paths<kMaxNodes>(n, p0, p1, a0, a1, x0, x1);
 }
 
 }  // namespace flare

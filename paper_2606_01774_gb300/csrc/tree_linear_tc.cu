@@ -18,7 +18,7 @@
 // with deltas and tables as bf16 high and low parts, three products each: both
 // sums gather in tensor memory where the first MMA left X and Y.  (All on the
 // CUDA cores, 61 nodes were bound by reading the tables from shared memory,
-// 26 us a call of 192 items against LINEAR_MEASURED.)
+// 26 us a call of 192 items against 13.5.)
 // The state is rounded to bf16 for W; everything else is fp32 or split.
 //
 // Bound by the state's bytes: 64 KiB an item, so a CTA's life is organised
@@ -64,7 +64,7 @@ struct TlCfg {
   static constexpr int kCtas = BM == 64 ? 2 : 3;               // per SM
   static constexpr int kBlocks = BM / 16;
   // state pieces in flight: with a whole item's, BM = 16, CTAs that run in step
-  // keep DRAM busy through their compute phases (3 pieces: 33.4 us, 4: RING_MEASURED
+  // keep DRAM busy through their compute phases (3 pieces: 33.4 us, 4: 32.9 us
   // for 64 requests of 16 nodes)
   static constexpr int kRing = BM == 16 ? 4 : BM == 32 ? 2 : 3;
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
@@ -246,33 +246,8 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           n = -1;
           p0 = p1 = -1;
         }
-        // pointer doubling: sets and sums over the 2^k nearest path members
-        uint64_t a0 = lane < n ? 1ull << lane : 0ull;
-        uint64_t a1 = lane + 32 < n ? 1ull << (lane + 32) : 0ull;
-        while (__any_sync(0xffffffffu, p0 >= 0 || p1 >= 0)) {
-          const uint64_t l0 = shfl64(a0, p0 & 31), h0 = shfl64(a1, p0 & 31);
-          const float xl0 = __shfl_sync(0xffffffffu, x0, p0 & 31);
-          const float xh0 = __shfl_sync(0xffffffffu, x1, p0 & 31);
-          const int ql0 = __shfl_sync(0xffffffffu, p0, p0 & 31);
-          const int qh0 = __shfl_sync(0xffffffffu, p1, p0 & 31);
-          if constexpr (BM == 64) {
-            const uint64_t l1 = shfl64(a0, p1 & 31), h1 = shfl64(a1, p1 & 31);
-            const float xl1 = __shfl_sync(0xffffffffu, x0, p1 & 31);
-            const float xh1 = __shfl_sync(0xffffffffu, x1, p1 & 31);
-            const int ql1 = __shfl_sync(0xffffffffu, p0, p1 & 31);
-            const int qh1 = __shfl_sync(0xffffffffu, p1, p1 & 31);
-            if (p1 >= 0) {
-              a1 |= p1 < 32 ? l1 : h1;
-              x1 += p1 < 32 ? xl1 : xh1;
-              p1 = p1 < 32 ? ql1 : qh1;
-            }
-          }
-          if (p0 >= 0) {
-            a0 |= p0 < 32 ? l0 : h0;
-            x0 += p0 < 32 ? xl0 : xh0;
-            p0 = p0 < 32 ? ql0 : qh0;
-          }
-        }
+        uint64_t a0, a1;
+        warp_paths<BM>(n, p0, p1, a0, a1, x0, x1);
         if (lane < BM) {
           m.anc[lane] = a0;
           m.gam2[lane] = x0 * 1.4426950408889634f;
