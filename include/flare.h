@@ -465,6 +465,8 @@ flare_status flare_append_kv(const flare_softmax_desc* desc, const void* k_blk, 
  * n = 0 a request that sits the round out.  Outputs of nodes n .. N-1 are
  * written as zero.  A request whose node_len or parent row is wrong is flagged
  * with FLARE_DEV_BAD_TREE and skipped.
+ * What used nodes hold must be finite: nodes of other branches enter a node's
+ * sums with weight zero, which does not silence an infinity or a NaN.
  *   parent    [R, N] int32
  *   node_len  [R]    int32
  */
