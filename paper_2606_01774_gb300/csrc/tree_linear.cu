@@ -15,6 +15,7 @@
 // The FMA pipes and shared memory bound it.  64 requests x 32 heads: 16 nodes of
 // 64 x 64 bf16 39.0 us (1.2 TB/s), of 64 x 64 fp32 39.6 us, of 128 x 128 fp32 124 us
 // (1.5 TB/s); 64 nodes of 64 x 64 bf16 236 us; 8 requests x 16 nodes 19.2 us in fp32.
+#include "async.cuh"
 #include "common.cuh"
 #include "kernels.h"
 #include "tree.cuh"
@@ -27,13 +28,6 @@ constexpr int kParts = 4;  // threads per value column
 // Floats of the staged state, which the two tables of the tree later take over.
 __host__ __device__ constexpr int linear_state(int dk, int dv, int rows) {
   return dk * dv > 2 * rows * (kMaxNodes + 4) ? dk * dv : 2 * rows * (kMaxNodes + 4);
-}
-
-__device__ __forceinline__ void cp_async16(float* dst, const float* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
-                   (uint32_t)__cvta_generic_to_shared(dst)),
-               "l"(src)
-               : "memory");
 }
 }  // namespace
 
@@ -70,7 +64,7 @@ __global__ void __launch_bounds__(kParts * DV, NODES == 16 ? 256 / DV : DV == 64
   float* M = A + rows * kAS;              // [rows][kAS]: e^(..) q.k; over the state, read by then
   const float* state = p.state_pool + ((size_t)slot * p.Hv + j) * DK * DV;
   for (int e = tid; e < DK * DV / 4; e += kThreads) cp_async16(S + 4 * e, state + 4 * e);
-  asm volatile("cp.async.commit_group;" ::: "memory");
+  cp_async_commit();
   if (tid < 32) {
     const size_t g = (size_t)r * p.B * p.Hv + j;
     float x0 = tid < n ? p.log_decay[g + (size_t)tid * p.Hv] : 0.f;
@@ -104,7 +98,7 @@ __global__ void __launch_bounds__(kParts * DV, NODES == 16 ? 256 / DV : DV == 64
       Qs[i * kKS + d + x] = to_f32(reinterpret_cast<const T*>(&qw)[x]);
     }
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  cp_async_wait<0>();
   __syncthreads();
   if (!tree_ok) {
     if (tid == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);

@@ -12,6 +12,7 @@
 //
 // Online softmax in base 2 with the logit scale folded into q; running
 // maximum, sum and output in fp32.
+#include "async.cuh"
 #include "common.cuh"
 #include "kernels.h"
 #include "pdl.cuh"
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
 // key 32 times, and the 4 x 4 (4 x 4 D/64) register tiles ask shared memory
 // for one 16-byte read per eight multiply-adds.
 template <int D>
-__global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftmaxParams p) {
+__global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(TreeSoftmaxParams p) {
   constexpr int kS = D + 4;  // row stride of staged rows: 16 lanes on 16 rows spread over the banks
   constexpr int kC = D / 64;
   extern __shared__ __align__(16) float sm[];
@@ -85,6 +86,7 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   float* Vs = Ks + kTreeTile * kS;   // [64][kS]
   float* Ps = Vs + kTreeTile * kS;   // [32][64 + 4]
   constexpr int kPS = kTreeTile + 4;
+  __shared__ size_t row_at[kTreeTile];
 
   const int tid = threadIdx.x, x = tid & 15, y = tid >> 4;
   const int gang = blockIdx.x / p.row_tiles, mt = blockIdx.x % p.row_tiles;
@@ -92,16 +94,53 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
   const float* q = static_cast<const float*>(p.q);
   const float* pools[2] = {static_cast<const float*>(p.k_pool), static_cast<const float*>(p.v_pool)};
   const float* blks[2] = {static_cast<const float*>(p.k_blk), static_cast<const float*>(p.v_blk)};
-  pdl_wait();  // the plan
-  pdl_launch_next();
   const TreeSpan span = tree_span(p, gang);
   TreeCursor cur = span.start;
-  TreePiece w;
-  while (cur.next(p, w)) {
-    if (mt == 0 && tid == 0) tree_list_cut(p, span, w);
+  auto next_piece = [&](TreePiece& w) {
+    while (cur.next(p, w))
+      if (rows.node0 < p.node_len[w.r]) return true;
+    return false;
+  };
+  // where a tile's rows are: page ids asked for first (find), offsets later
+  // (locate; ~0: none), by a thread per row; then copies, zeros for no row
+  auto find = [&](const TreePiece& w, int j) {
+    const int tok = j * kTreeTile + tid;
+    return tid < kTreeTile && j < w.n - 1 && tok < p.prefix_len[w.r]
+               ? p.page_table[(size_t)w.r * p.max_pages + tok / p.page_size]
+               : -1;
+  };
+  auto locate = [&](const TreePiece& w, int j, int page) {
+    if (tid >= kTreeTile) return;
+    size_t at = ~(size_t)0;
+    if (j == w.n - 1) {
+      if (tid < p.node_len[w.r]) at = (((size_t)w.r * p.N + tid) * p.Hkv + w.kvh) * D;
+    } else if (page >= 0 && page < p.num_pages) {  // the plan may not be through yet
+      at = (((size_t)page * p.Hkv + w.kvh) * p.page_size + (j * kTreeTile + tid) % p.page_size) * D;
+    }
+    row_at[tid] = at;
+  };
+  auto stage = [&](float* dst, int kv, bool tree) {
+    const float* src = (tree ? blks[kv] : pools[kv]) + tid % (D / 4) * 4;
+    dst += tid % (D / 4) * 4;
+#pragma unroll 4
+    for (int i = tid / (D / 4); i < kTreeTile; i += kThreadsS / (D / 4)) {
+      const size_t at = row_at[i];
+      const bool live = at != ~(size_t)0;
+      cp_async16(dst + i * kS, src + (live ? at : 0), live);
+    }
+    cp_async_commit();
+  };
+  TreePiece w, nx;
+  bool more = next_piece(w), planned = false;
+  if (more) {
+    locate(w, w.j0, find(w, w.j0));
+    __syncthreads();
+    stage(Ks, 0, w.j0 == w.n - 1);
+    stage(Vs, 1, w.j0 == w.n - 1);
+  }
+  for (; more; w = nx) {
+    more = next_piece(nx);
     const int n = p.node_len[w.r], P = p.prefix_len[w.r];
-    if (rows.node0 >= n || p.bad[w.r]) continue;
-    __syncthreads();  // the previous piece's rows are read
     for (int e = tid; e < kRowsS * (D / 4); e += kThreadsS) {
       const int i = e / (D / 4), d = e % (D / 4) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -111,6 +150,12 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
       *reinterpret_cast<float4*>(Qs + i * kS + d) =
           make_float4(v.x * p.scale_log2, v.y * p.scale_log2, v.z * p.scale_log2, v.w * p.scale_log2);
     }
+    if (!planned) {
+      pdl_wait();  // the plan
+      pdl_launch_next();
+      planned = true;
+    }
+    if (mt == 0 && tid == 0) tree_list_cut(p, span, w);
     uint64_t path[4];  // the keys of the tree tile that each row sees
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -127,31 +172,12 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
     }
     for (int j = w.j0; j < w.j1; ++j) {
       const bool tree = j == w.n - 1;
-      const int valid = tree ? n : min(kTreeTile, P - j * kTreeTile);
-      __syncthreads();
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        float* dst = kv ? Vs : Ks;
-#pragma unroll 8
-        for (int e = tid; e < kTreeTile * (D / 4); e += kThreadsS) {
-          const int i = e / (D / 4), d = e % (D / 4) * 4;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (i < valid) {
-            const float* src;
-            if (tree) {
-              src = blks[kv] + (((size_t)w.r * p.N + i) * p.Hkv + w.kvh) * D;
-            } else {
-              const int tok = j * kTreeTile + i;
-              const int page = p.page_table[(size_t)w.r * p.max_pages + tok / p.page_size];
-              src = pools[kv] +
-                    (((size_t)page * p.Hkv + w.kvh) * p.page_size + tok % p.page_size) * D;
-            }
-            v = *reinterpret_cast<const float4*>(src + d);
-          }
-          *reinterpret_cast<float4*>(dst + i * kS + d) = v;
-        }
-      }
-      __syncthreads();
+      const int valid = min(kTreeTile, P - j * kTreeTile);  // of a prefix tile
+      const bool last = j + 1 == w.j1, load = !last || more;  // another tile follows
+      const TreePiece& then = last ? nx : w;
+      const int jn = last ? nx.j0 : j + 1, page = load ? find(then, jn) : -1;
+      cp_async_wait<1>();
+      __syncthreads();  // the keys (and a piece's queries)
       float s[4][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -174,6 +200,9 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
             s[i][c] = fmaf(a[i].w, b[c].w, s[i][c]);
           }
       }
+      if (load) locate(then, jn, page);
+      __syncthreads();  // the keys are read
+      if (load) stage(Ks, 0, jn == then.n - 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float mx = -INFINITY;
@@ -203,7 +232,9 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
 #pragma unroll
         for (int c = 0; c < 4 * kC; ++c) acc[i][c] *= corr;
       }
-      __syncwarp();  // a row's 64 probabilities come from the 16 lanes that read them
+      if (load) cp_async_wait<1>();
+      else cp_async_wait<0>();
+      __syncthreads();  // the values (a row's probabilities come from its own warp)
 #pragma unroll 1
       for (int k = 0; k < kTreeTile; k += 4) {
         float4 pr[4];
@@ -225,7 +256,10 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
             }
           }
       }
+      __syncthreads();  // the values are read
+      if (load) stage(Vs, 1, jn == then.n - 1);
     }
+    if (p.bad[w.r]) continue;
     const bool whole = w.whole();
     const size_t part = ((size_t)blockIdx.x * 2 + w.slot()) * kRowsS;
 #pragma unroll
@@ -248,6 +282,10 @@ __global__ void __launch_bounds__(kThreadsS) tree_softmax_simt_kernel(TreeSoftma
         else if (p.lse) p.lse[o] = l2 * kLn2;
       }
     }
+  }
+  if (!planned) {
+    pdl_wait();
+    pdl_launch_next();
   }
 }
 
