@@ -451,12 +451,14 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
     bool have = next_item(p, cur, rows.node0, it);
     pdl_wait();  // the plan: paths, and which requests are bad
     if (tid == 64) pdl_launch_next();
+    auto path_of = [&](const TreeItem& x) {
+      return rows.used(row, x.nodes) ? p.anc[(size_t)x.w.r * p.N + node] : 0ull;
+    };
+    uint64_t path = have ? path_of(it) : 0ull;
+    int bad = have ? p.bad[it.w.r] : 0;
     for (int k = 0; have; ++k) {
       const bool live = rows.used(row, it.nodes);
       const bool warp_live = __any_sync(0xffffffffu, live);
-      const uint64_t path = live ? p.anc[(size_t)it.w.r * p.N + node] : 0ull;
-      const bool skip = p.bad[it.w.r] != 0;
-      if (tid == 64 && mt == 0 && !skip) tree_list_cut(p, span, it.w);
       float m_run = -INFINITY, l_run = 0.f;
       for (int j = 0; j < it.tiles; ++j) {
         const int gg = g + j, sb = gg % kSB;
@@ -539,6 +541,14 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         tc::mbar_arrive(&sh.p_full[t][sb]);
       }
       g += it.tiles;
+      // what the next piece needs first, in flight while this one's output leaves
+      TreeItem nx;
+      const bool more = next_item(p, cur, rows.node0, nx), skip = bad != 0;
+      if (more) {
+        path = path_of(nx);
+        bad = p.bad[nx.w.r];
+      }
+      if (tid == 64 && mt == 0 && !skip) tree_list_cut(p, span, it.w);
       if (ok && aborted_t(sh)) ok = false;
       if (ok && !warp_wait_t(&sh.o_final[t], (uint32_t)k & 1u, &sh.abort_flag)) ok = false;
       if (group_or(2 + t, !ok)) {  // the row tile's four warps agree
@@ -613,9 +623,23 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           };
           const size_t orow = ((size_t)it.w.r * p.N + node) * p.Hq + it.w.kvh * p.G + head;
           __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + orow * D;
+          auto put = [&](int c, const float* x) {  // columns c .. c + 15 of the output
+            uint32_t h[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const __nv_bfloat162 h2 = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+              h[i] = *reinterpret_cast<const uint32_t*>(&h2);
+            }
+            if (out32) {
+              store32(out + c, h);
+            } else {
+              *reinterpret_cast<uint4*>(out + c) = make_uint4(h[0], h[1], h[2], h[3]);
+              *reinterpret_cast<uint4*>(out + c + 8) = make_uint4(h[4], h[5], h[6], h[7]);
+            }
+          };
+          constexpr int kCols = NQ == 1 ? 64 : 32;  // at a time: as registers allow
           // the other pieces' columns, kCols at a time: every load of a batch in
           // flight before the first is used
-          constexpr int kCols = NQ == 1 ? 64 : 32;
 #pragma unroll 1
           for (int c0 = 0; c0 < D; c0 += kCols) {
             uint32_t o[kCols];
@@ -665,21 +689,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
             }
             if (!live) continue;
 #pragma unroll
-            for (int c = 0; c < kCols; c += 16) {
-              uint32_t h[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const __nv_bfloat162 h2 =
-                    __floats2bfloat162_rn(acc[c + 2 * i], acc[c + 2 * i + 1]);
-                h[i] = *reinterpret_cast<const uint32_t*>(&h2);
-              }
-              if (out32) {
-                store32(out + c0 + c, h);
-              } else {
-                *reinterpret_cast<uint4*>(out + c0 + c) = make_uint4(h[0], h[1], h[2], h[3]);
-                *reinterpret_cast<uint4*>(out + c0 + c + 8) = make_uint4(h[4], h[5], h[6], h[7]);
-              }
-            }
+            for (int c = 0; c < kCols; c += 16) put(c0 + c, acc + c);
           }
           if (live && p.lse)
             p.lse[orow] = (whole ? l2 : den > 0.f ? top + log2f(den) : -INFINITY) * 0.6931471805599453f;
@@ -687,7 +697,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       }
       tc::fence_before_sync();
       tc::mbar_arrive(&sh.o_free[t]);
-      have = next_item(p, cur, rows.node0, it);
+      it = nx;
+      have = more;
     }
     if (!ok) give_up(sh, p.dev_status);
   }
