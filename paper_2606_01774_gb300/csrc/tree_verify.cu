@@ -30,7 +30,7 @@ namespace flare {
 
 namespace {
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 128;
 constexpr int kWalkThreads = 512;
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -275,6 +275,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     x_tok = to_f32(rows[at]) * scale;
     sh.q[tid] = drafts ? drafts[at] : 1.f;
   }
+  const int lo = (int)((long long)p.V * rank / ranks), hi = (int)((long long)p.V * (rank + 1) / ranks);
   pdl_wait();  // the row statistics
   // a warp per row with children: its log-sum-exp and argmax
   for (int i = warp; i < n; i += kWarps) {
@@ -312,7 +313,6 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
   }
   __syncthreads();
 
-  const int lo = (int)((long long)p.V * rank / ranks), hi = (int)((long long)p.V * (rank + 1) / ranks);
   // Calls f(x, ...) for this CTA's tokens of a row, kIn of a thread's loads in
   // flight: consecutive threads on consecutive tokens, whatever the alignment.
   constexpr int kIn = 8;
