@@ -564,7 +564,7 @@ flare_status flare_tree_verify_workspace_size(const flare_tree_verify_desc* desc
  *   token       [R, N]    int32, the drafted tokens (token[r][0] is not read)
  *   parent, node_len      the trees
  *   uniform     [R, N]    fp32 in [0, 1), one per node; nullable in GREEDY mode
- *   noise       [R, V]    fp32 > 0; nullable in GREEDY mode
+ *   noise       [R, V]    fp32 in (0, 2^126); nullable in GREEDY mode
  *   path        [R, N]    int32: the accepted nodes, path[r][0] = 0, then -1
  *   path_len    [R]       int32: how many (0 where node_len[r] = 0)
  *   next_token  [R]       int32 (-1 where node_len[r] = 0)
