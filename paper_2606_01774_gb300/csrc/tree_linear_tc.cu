@@ -18,8 +18,10 @@
 // with deltas and tables as bf16 high and low parts, three products each: both
 // sums gather in tensor memory where the first MMA left X and Y.  (All on the
 // CUDA cores, 61 nodes were bound by reading the tables from shared memory,
-// 26 us a call of 192 items against 13.5.)
-// The state is rounded to bf16 for W; everything else is fp32 or split.
+// 26 us a call of 192 items against 13.5, the state then rounded once.)
+// The state, too, enters W as bf16 high and low parts (to about 2^-16, two products
+// a step): rounded once, outputs were off by 2.6e-3 relative where their own
+// rounding to bf16 makes 1.7e-3.
 //
 // Bound by the state's bytes: 64 KiB an item, so a CTA's life is organised
 // around its copies.  Warp 4 runs ahead: it finds the next item, streams its
@@ -28,6 +30,7 @@
 // pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
 // tensor memory, then tables, substitution and readout.  BM <= 32: 128
 // tensor-memory columns and under 76 KiB, three CTAs per SM; BM = 64: two.
+// 64 requests x 16 nodes x 32 heads: 34.0 us, 4.7 TB/s; 6 x 61 nodes: 14.0 us.
 // Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
 // lets its copies and MMAs land, frees its tensor memory and exits.
 #include <cudaTypedefs.h>
@@ -65,7 +68,7 @@ struct TlCfg {
   static constexpr int kBlocks = BM / 16;
   // state pieces in flight: with a whole item's, BM = 16, CTAs that run in step
   // keep DRAM busy through their compute phases (3 pieces: 33.4 us, 4: 32.9 us
-  // for 64 requests of 16 nodes)
+  // for 64 requests of 16 nodes, the state then rounded once)
   static constexpr int kRing = BM == 16 ? 4 : BM == 32 ? 2 : 3;
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
   // 2 chunks of value rows x 128 B; BM = 16: in registers, an item ahead
@@ -83,7 +86,9 @@ struct TlCfg {
   static constexpr int oV = kOverlay ? oRing + kRing * kPieceBytes : oDiag + kDiag;
   static constexpr int oShared = oV + kV;
   static_assert(!kOverlay || kTables <= kKQ, "tables over keys and queries");
-  static constexpr int kTmem = 64 + 2 * BM <= 128 ? 128 : 256;
+  static constexpr int kTmem = BM == 64 ? 256 : 128;
+  // state pieces that tensor memory holds as operands beside W^T, 32 columns each
+  static constexpr int kOps = (kTmem - 2 * BM) / 32 < kPieces ? (kTmem - 2 * BM) / 32 : kPieces;
 };
 
 template <int BM>
@@ -91,6 +96,7 @@ struct alignas(16) TlShared {
   TlMeta<BM> meta[3];
   uint64_t full[4], empty[4];  // ring pieces
   uint64_t kq_full, v_full, done, mma_done, upd, meta_full[3];  // done: an item's readout
+  uint64_t op_free[2];  // the products with the first pieces, whose columns later ones take
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -112,11 +118,13 @@ __device__ __forceinline__ int tl_at(int row, int u) {
   return row * 32 + ((u ^ (row & 7)) << 2);
 }
 
-// x = hi + lo to about 2^-16 relative, each a bf16 pair (a low, b high)
+// x = hi + lo to about 2^-16 relative, each a bf16 pair (a low, b high).  The high
+// parts are cut off, not rounded: one conversion less.
 __device__ __forceinline__ void tl_split(float a, float b, uint32_t& hi, uint32_t& lo) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-  const __nv_bfloat162 l = __floats2bfloat162_rn(a - __low2float(h), b - __high2float(h));
-  hi = *reinterpret_cast<const uint32_t*>(&h);
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  hi = __byte_perm(x, y, 0x7632);
+  const __nv_bfloat162 l = __floats2bfloat162_rn(a - __uint_as_float(x & 0xffff0000u),
+                                                 b - __uint_as_float(y & 0xffff0000u));
   lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 
@@ -175,6 +183,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
     tc::mbar_init(&sh.done, kTlCompute);
     tc::mbar_init(&sh.mma_done, 1);
     tc::mbar_init(&sh.upd, 1);
+    for (int b = 0; b < 2; ++b) tc::mbar_init(&sh.op_free[b], 1);
     for (int b = 0; b < 3; ++b) tc::mbar_init(&sh.meta_full[b], 1);
     tc::fence_mbar_init();
   }
@@ -182,8 +191,9 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  const uint32_t tmS = sh.tmem_base;  // S0^T as bf16 pairs (64 columns); then G, then deltas
-  const uint32_t tmW = tmS + 64;      // W^T: [K part | Q part], then [X | Y]
+  const uint32_t tmS = sh.tmem_base;  // S0^T by pieces, bf16 pairs: 16 columns high, 16 low parts;
+                                      // then G, then deltas
+  const uint32_t tmW = tmS + C::kTmem - 2 * BM;  // W^T: [K part | Q part], then [X | Y]
   const int total = p.R * p.Hv;
 
   if (warp == 4) {
@@ -333,12 +343,15 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
         tc::fence_after_sync();
         if (tc::elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk)
-            tc::mma_bf16_ts(tmW, tmS + (2 * q + kk) * 8,
-                            kq_desc + (uint64_t)(((q >> 1) * (2 * BM * 128) +
-                                                  ((2 * q + kk) & 3) * 32) >>
-                                                 4),
-                            idW, q + kk > 0);
+          for (int kk = 0; kk < 2; ++kk) {
+            const uint64_t kq =
+                kq_desc +
+                (uint64_t)(((q >> 1) * (2 * BM * 128) + ((2 * q + kk) & 3) * 32) >> 4);
+            const uint32_t op = tmS + q % C::kOps * 32 + kk * 8;
+            tc::mma_bf16_ts(tmW, op, kq, idW, q + kk > 0);
+            tc::mma_bf16_ts(tmW, op + 16, kq, idW, 1);
+          }
+          if (q + C::kOps < kPieces) tc::mma_commit(&sh.op_free[q]);
           if (q == kPieces - 1) {
 #pragma unroll
             for (int kk = 0; kk < kTlD / 16; ++kk) {
@@ -435,17 +448,25 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       const unsigned short* vs =  // this column's values, 64 elements a row
           reinterpret_cast<const unsigned short*>(smem_raw + C::oV + (tid >> 6) * (BM * 128)) +
           (tid & 63);
-      // the state, piece by piece, into tensor memory as bf16 pairs
+      // the state, piece by piece, into tensor memory as bf16 high and low parts
 #pragma unroll 1
       for (int q = 0; q < kPieces; ++q, ++used) {
         const int s = used % C::kRing;
         bad |= !tc::mbar_wait(&sh.full[s], (used / C::kRing) & 1u, &sh.abort_flag);
         __syncwarp();
         const float* S = reinterpret_cast<const float*>(ring + s * kPieceBytes) + tid;
-        uint32_t w[16];
+        uint32_t hi[16], lo[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = tl_pack(S[(2 * e) * kTlD], S[(2 * e + 1) * kTlD]);
-        tc::tmem_st16(tmS + lane_off + 16 * q, w);
+        for (int e = 0; e < 16; ++e)
+          tl_split(S[(2 * e) * kTlD], S[(2 * e + 1) * kTlD], hi[e], lo[e]);
+        if (q >= C::kOps) {  // the products with the columns' last piece are through
+          bad |= !tc::mbar_wait(&sh.op_free[q - C::kOps], (uint32_t)k & 1u, &sh.abort_flag);
+          __syncwarp();
+          tc::fence_after_sync();
+        }
+        const uint32_t op = tmS + lane_off + q % C::kOps * 32;
+        tc::tmem_st16(op, hi);
+        tc::tmem_st16(op + 16, lo);
         tc::tmem_st_wait();
         tc::fence_before_sync();
         tc::mbar_arrive(&sh.empty[s]);
