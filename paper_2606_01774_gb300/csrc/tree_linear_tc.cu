@@ -29,8 +29,8 @@
 // works out its paths and gates (pointer doubling), and issues the MMAs as the
 // pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
 // tensor memory, then tables, substitution and readout.  BM <= 32: 128
-// tensor-memory columns and under 76 KiB, three CTAs per SM; BM = 64: two.
-// 64 requests x 16 nodes x 32 heads: 34.0 us, 4.7 TB/s; 6 x 61 nodes: 14.0 us.
+// tensor-memory columns, four (BM = 16) or three CTAs per SM; BM = 64: two.
+// 64 requests x 16 nodes x 32 heads: 33.1 us, 4.8 TB/s; 6 x 61 nodes: 13.9 us.
 // Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
 // lets its copies and MMAs land, frees its tensor memory and exits.
 #include <cudaTypedefs.h>
@@ -64,12 +64,12 @@ struct TlMeta {
 
 template <int BM>
 struct TlCfg {
-  static constexpr int kCtas = BM == 64 ? 2 : 3;               // per SM
+  // CTAs per SM, and state pieces in flight in each.  BM = 16: more CTAs overlap
+  // more compute phases than deeper rings do (64 requests of 16 nodes: 3 CTAs with 4
+  // pieces 34.0 us, 4 with 2 33.1 us)
+  static constexpr int kCtas = BM == 64 ? 2 : BM == 32 ? 3 : 4;
   static constexpr int kBlocks = BM / 16;
-  // state pieces in flight: with a whole item's, BM = 16, CTAs that run in step
-  // keep DRAM busy through their compute phases (3 pieces: 33.4 us, 4: 32.9 us
-  // for 64 requests of 16 nodes, the state then rounded once)
-  static constexpr int kRing = BM == 16 ? 4 : BM == 32 ? 2 : 3;
+  static constexpr int kRing = BM == 64 ? 3 : 2;
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
   // 2 chunks of value rows x 128 B; BM = 16: in registers, an item ahead
   static constexpr int kV = BM == 16 ? 0 : 2 * BM * 128;
