@@ -71,7 +71,7 @@ struct TlCfg {
   static constexpr int kBlocks = BM / 16;
   static constexpr int kRing = BM == 64 ? 3 : 2;
   static constexpr int kKQ = 2 * 2 * BM * 128;                 // 2 chunks of [K; Q] rows x 128 B
-  // 2 chunks of value rows x 128 B; BM = 16: in registers, an item ahead
+  // 2 chunks of value rows x 128 B; BM = 16: in registers
   static constexpr int kV = BM == 16 ? 0 : 2 * BM * 128;
   static constexpr int kDiag = kBlocks * 16 * 16 * 8;          // pairs (-A, M) inside blocks
   // -A high, low, M high, low between blocks: rows 16 .. BM - 1, K-major SW128
@@ -417,19 +417,10 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
     uint32_t used = 0;       // ring pieces consumed
     uint32_t upd_phase = 0;  // of the updates between blocks
     bool bad = false;
-    constexpr int kVr = C::kV == 0 ? BM : 1;
-    uint32_t vr[kVr];  // BM = 16: this column's values
-    // the k-th item (-1: no more, or a wait that gave up), its values on their way
+    // the k-th item (-1: no more, or a wait that gave up)
     auto take_item = [&](int k) -> int {
       bad |= !tc::mbar_wait(&sh.meta_full[k % 3], (uint32_t)(k / 3) & 1u, &sh.abort_flag);
       const int item = bad ? -1 : sh.meta[k % 3].item;
-      if (C::kV == 0 && item >= 0) {
-        const int r = item / p.Hv, j = item - r * p.Hv;
-        const unsigned short* v = static_cast<const unsigned short*>(p.v) +
-                                  ((size_t)r * p.B * p.Hv + j) * kTlD + tid;
-#pragma unroll
-        for (int i = 0; i < kVr; ++i) vr[i] = __ldg(v + (size_t)min(i, p.B - 1) * p.Hv * kTlD);
-      }
       return item;
     };
     int item = take_item(0);
@@ -448,6 +439,13 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       const unsigned short* vs =  // this column's values, 64 elements a row
           reinterpret_cast<const unsigned short*>(smem_raw + C::oV + (tid >> 6) * (BM * 128)) +
           (tid & 63);
+      constexpr int kVr = C::kV == 0 ? BM : 1;
+      uint32_t vr[kVr];  // BM = 16: this column's values, on their way meanwhile
+      if (C::kV == 0) {
+        const unsigned short* v = static_cast<const unsigned short*>(p.v) + row0 + tid;
+#pragma unroll
+        for (int i = 0; i < kVr; ++i) vr[i] = __ldg(v + (size_t)min(i, p.B - 1) * row_stride);
+      }
       // the state, piece by piece, into tensor memory as bf16 high and low parts
 #pragma unroll 1
       for (int q = 0; q < kPieces; ++q, ++used) {
@@ -571,28 +569,37 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
         tc::tmem_ld16(tmW + lane_off + i0, xr);
         tc::tmem_ld16(tmW + lane_off + BM + i0, yr);
         tc::tmem_ld_wait();
-        uint64_t dl[16];  // the deltas, as {d, d}
-        float o[2];
+        uint64_t xy[16];  // {X, Y}, then {delta, the later nodes' share of the readout}
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int i = i0 + e;
-          o[e & 1] = 0.f;
-          dl[e] = 0ull;
-          if (i < n) {
-            uint64_t xy = BM == 16 ? f2(x_of(i, vr[e % kVr], xr[e]), y_of(i, yr[e]))
-                                   : f2(__uint_as_float(xr[e]), __uint_as_float(yr[e]));
+          xy[e] = i >= n     ? 0ull
+                  : BM == 16 ? f2(x_of(i, vr[e % kVr], xr[e]), y_of(i, yr[e]))
+                             : f2(__uint_as_float(xr[e]), __uint_as_float(yr[e]));
+        }
+        // two nodes a step, their deltas at once into all later nodes' sums
 #pragma unroll
-            for (int u = 0; u < (e + 1) / 2; ++u) {  // columns 2 u, 2 u + 1
+        for (int u = 0; u < 8; ++u) {
+          float o0 = 0.f, o1 = 0.f;
+          if (i0 + 2 * u < n) {
+            const float m0 = T[tl_at(2 * u, u) + 1];  // columns 2 u, 2 u + 1 of rows 2 u, ..
+            const ulonglong2 c1 = *reinterpret_cast<const ulonglong2*>(T + tl_at(2 * u + 1, u));
+            float x, y, m1, unused;
+            f2_split(xy[2 * u], x, y);
+            const uint64_t d0 = f2_dup(x);
+            o0 = p.scale * fmaf(m0, x, y);
+            xy[2 * u + 1] = f2_fma(c1.x, d0, xy[2 * u + 1]);
+            f2_split(xy[2 * u + 1], x, y);
+            f2_split(c1.y, unused, m1);
+            const uint64_t d1 = f2_dup(x);
+            o1 = p.scale * fmaf(m1, x, y);
+#pragma unroll
+            for (int e = 2 * u + 2; e < 16; ++e) {
               const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(T + tl_at(e, u));
-              xy = f2_fma(c.x, dl[2 * u], xy);
-              if (2 * u + 1 < e) xy = f2_fma(c.y, dl[2 * u + 1], xy);
+              xy[e] = f2_fma(c.y, d1, f2_fma(c.x, d0, xy[e]));
             }
-            float x, y;
-            f2_split(xy, x, y);
-            dl[e] = f2_dup(x);
-            o[e & 1] = p.scale * fmaf(T[tl_at(e, e >> 1) + 2 * (e & 1) + 1], x, y);
           }
-          if (e & 1) store2(i - 1, o[0], o[1]);
+          store2(i0 + 2 * u, o0, o1);
         }
         if (BM > 16 && i0 + 16 < n) {
           // this block's deltas into the later blocks' sums
@@ -600,8 +607,8 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             float a, b, unused;
-            f2_split(dl[2 * e], a, unused);
-            f2_split(dl[2 * e + 1], b, unused);
+            f2_split(xy[2 * e], a, unused);
+            f2_split(xy[2 * e + 1], b, unused);
             tl_split(a, b, hl[e], hl[8 + e]);
           }
           tc::tmem_st16(tmS + lane_off, hl);
