@@ -30,7 +30,7 @@
 // pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
 // tensor memory, then tables, substitution and readout.  BM <= 32: 128
 // tensor-memory columns, four (BM = 16) or three CTAs per SM; BM = 64: two.
-// 64 requests x 16 nodes x 32 heads: 33.1 us, 4.8 TB/s; 6 x 61 nodes: 13.9 us.
+// 64 requests x 16 nodes x 32 heads: 31.5 us, 5.1 TB/s; 6 x 61 nodes: 13.0 us.
 // Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
 // lets its copies and MMAs land, frees its tensor memory and exits.
 #include <cudaTypedefs.h>
