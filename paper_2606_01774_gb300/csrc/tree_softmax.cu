@@ -24,8 +24,6 @@ namespace flare {
 namespace {
 
 constexpr int kPlanThreads = 128;
-constexpr int kRowsS = 32;      // query rows per CTA of the fp32 kernel
-constexpr int kThreadsS = 128;
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ void store4(float* x, float4 v) { *reinterpret_cast<float4*>(x) = v; }
@@ -33,6 +31,11 @@ __device__ __forceinline__ void store4(__nv_bfloat16* x, float4 v) {
   const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
   *reinterpret_cast<uint2*>(x) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo),
                                             *reinterpret_cast<const uint32_t*>(&hi));
+}
+
+// CTAs per SM of the fp32 kernel: its shared memory, and registers for 16 warps
+__host__ __device__ constexpr int simt_ctas(int D, int rows) {
+  return rows == 32 ? 256 / D : D == 64 ? 2 : 1;
 }
 
 }  // namespace
@@ -70,7 +73,8 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
   if (tid == 0) p.bad[r] = any;
 }
 
-// fp32 attention.  A CTA takes 32 query rows; thread (y, x) of its 8 x 16 holds
+// fp32 attention.  A CTA takes ROWS = 32 or 64 query rows; thread (y, x) of its
+// ROWS / 4 x 16 holds
 // rows 4y .. 4y+3 against keys x, x+16, x+32, x+48 of a tile, and columns 4x
 // (+ 64 c) of those rows' outputs.  Bound by the fp32 multiply-adds (4 D per
 // row and key against 8 D bytes per key): a row tile of 32 reuses each staged
@@ -81,15 +85,17 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
 // whole call: 48 requests x 61 nodes over 1150 tokens, D = 64, 4 x 4 heads 250 us
 // (29 TFLOP/s of 74); 32 x 16 nodes, D = 128 180 us; 12 x 13 nodes, prefixes below
 // 1022, D = 64 24 us, a latency of three launches and one tile.
-template <int D>
-__global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(TreeSoftmaxParams p) {
+template <int D, int ROWS>
+__global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
+    tree_softmax_simt_kernel(TreeSoftmaxParams p) {
+  constexpr int kThreadsS = 4 * ROWS;
   constexpr int kS = D + 4;  // row stride of staged rows: 16 lanes on 16 rows spread over the banks
   constexpr int kC = D / 64;
   extern __shared__ __align__(16) float sm[];
-  float* Qs = sm;                    // [32][kS]
-  float* Ks = Qs + kRowsS * kS;      // [64][kS]
+  float* Qs = sm;                    // [ROWS][kS]
+  float* Ks = Qs + ROWS * kS;      // [64][kS]
   float* Vs = Ks + kTreeTile * kS;   // [64][kS]
-  float* Ps = Vs + kTreeTile * kS;   // [32][64 + 4]
+  float* Ps = Vs + kTreeTile * kS;   // [ROWS][64 + 4]
   constexpr int kPS = kTreeTile + 4;
   __shared__ size_t row_at[kTreeTile];
 
@@ -146,7 +152,7 @@ __global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(T
   for (; more; w = nx) {
     more = next_piece(nx);
     const int n = p.node_len[w.r], P = p.prefix_len[w.r];
-    for (int e = tid; e < kRowsS * (D / 4); e += kThreadsS) {
+    for (int e = tid; e < ROWS * (D / 4); e += kThreadsS) {
       const int i = e / (D / 4), d = e % (D / 4) * 4;
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (rows.used(i, n))
@@ -162,11 +168,15 @@ __global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(T
     }
     if (mt == 0 && tid == 0) tree_list_cut(p, span, w);
     uint64_t path[4];  // the keys of the tree tile that each row sees
+    bool mine = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = 4 * y + i;
-      path[i] = rows.used(row, n) ? p.anc[(size_t)w.r * p.N + rows.node(row)] : 0ull;
+      const bool used = rows.used(row, n);
+      path[i] = used ? p.anc[(size_t)w.r * p.N + rows.node(row)] : 0ull;
+      mine = mine || used;
     }
+    const bool warp_live = __any_sync(0xffffffffu, mine);  // else it copies only
     float acc[4][4 * kC], mrow[4], lrow[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -189,7 +199,7 @@ __global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(T
 #pragma unroll
         for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
 #pragma unroll 4
-      for (int d = 0; d < D; d += 4) {
+      for (int d = 0; d < (warp_live ? D : 0); d += 4) {
         float4 a[4], b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(Qs + (4 * y + i) * kS + d);
@@ -208,40 +218,42 @@ __global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(T
       if (load) locate(then, jn, page);
       __syncthreads();  // the keys are read
       if (load) stage(Ks, 0, jn == then.n - 1);
+      if (warp_live) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float mx = -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          float mx = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int key = x + 16 * c;
-          const bool see = tree ? (path[i] >> key) & 1 : key < valid;
-          if (!see) s[i][c] = -INFINITY;
-          mx = fmaxf(mx, s[i][c]);
+          for (int c = 0; c < 4; ++c) {
+            const int key = x + 16 * c;
+            const bool see = tree ? (path[i] >> key) & 1 : key < valid;
+            if (!see) s[i][c] = -INFINITY;
+            mx = fmaxf(mx, s[i][c]);
+          }
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          const float mnew = fmaxf(mrow[i], mx);
+          const float mref = mnew == -INFINITY ? 0.f : mnew;  // a row that sees nothing yet
+          const float corr = exp2f(mrow[i] - mref);
+          float sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const float e = exp2f(s[i][c] - mref);
+            Ps[(4 * y + i) * kPS + x + 16 * c] = e;
+            sum += e;
+          }
+#pragma unroll
+          for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          lrow[i] = lrow[i] * corr + sum;
+          mrow[i] = mnew;
+#pragma unroll
+          for (int c = 0; c < 4 * kC; ++c) acc[i][c] *= corr;
         }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float mnew = fmaxf(mrow[i], mx);
-        const float mref = mnew == -INFINITY ? 0.f : mnew;  // a row that sees nothing yet
-        const float corr = exp2f(mrow[i] - mref);
-        float sum = 0.f;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const float e = exp2f(s[i][c] - mref);
-          Ps[(4 * y + i) * kPS + x + 16 * c] = e;
-          sum += e;
-        }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        lrow[i] = lrow[i] * corr + sum;
-        mrow[i] = mnew;
-#pragma unroll
-        for (int c = 0; c < 4 * kC; ++c) acc[i][c] *= corr;
       }
       if (load) cp_async_wait<1>();
       else cp_async_wait<0>();
       __syncthreads();  // the values (a row's probabilities come from its own warp)
 #pragma unroll 1
-      for (int k = 0; k < kTreeTile; k += 4) {
+      for (int k = 0; k < (warp_live ? kTreeTile : 0); k += 4) {
         float4 pr[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -266,7 +278,7 @@ __global__ void __launch_bounds__(kThreadsS, 256 / D) tree_softmax_simt_kernel(T
     }
     if (p.bad[w.r]) continue;
     const bool whole = w.whole();
-    const size_t part = ((size_t)blockIdx.x * 2 + w.slot()) * kRowsS;
+    const size_t part = ((size_t)blockIdx.x * 2 + w.slot()) * ROWS;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int row = 4 * y + i;
@@ -390,7 +402,9 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
                                   int max_pages, bool bf16, int num_sms) {
   TreeSoftmaxPlan pl;
   const int G = Hq / Hkv;
-  pl.tile_base = bf16 ? 128 : kRowsS;
+  // fp32: row tiles of 64 where one of 32 does not hold all rows (64 rows over 1150
+  // tokens: 16 requests, D = 256 210 -> 167 us, 32 requests, D = 128 180 -> 172 us)
+  pl.tile_base = bf16 ? 128 : (long long)N * G > 32 ? 64 : 32;
   const int per_node = G <= pl.tile_base ? 1 : (G + pl.tile_base - 1) / pl.tile_base;
   const int nodes = G <= pl.tile_base ? pl.tile_base / G : 1;  // of a row tile
   const long long tiles = (N + nodes - 1) / nodes * (long long)per_node;
@@ -400,7 +414,7 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
   const int per_cta = bf16 && D <= 128 && tiles > 1 ? 2 : 1;
   pl.tile_rows = per_cta * pl.tile_base;
   pl.row_tiles = (int)((tiles + per_cta - 1) / per_cta);
-  const int per_sm = bf16 || D == 256 ? 1 : D == 128 ? 2 : 4;
+  const int per_sm = bf16 ? 1 : simt_ctas(D, pl.tile_base);
   // as many gangs as the GPU holds at once, and no more than there can be tiles
   long long gangs = (long long)num_sms * per_sm / pl.row_tiles;
   const long long most =
@@ -433,17 +447,22 @@ TreeSoftmaxPlan plan_tree_softmax(int R, int N, int Hq, int Hkv, int D, int page
 
 namespace {
 
-template <int D>
-cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
-  const int smem = (int)sizeof(float) *
-                   ((kRowsS + 2 * kTreeTile) * (D + 4) + kRowsS * (kTreeTile + 4));
-  cudaError_t e = cudaFuncSetAttribute(tree_softmax_simt_kernel<D>,
+template <int D, int ROWS>
+cudaError_t launch_simt_rows(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  const int smem =
+      (int)sizeof(float) * ((ROWS + 2 * kTreeTile) * (D + 4) + ROWS * (kTreeTile + 4));
+  cudaError_t e = cudaFuncSetAttribute(tree_softmax_simt_kernel<D, ROWS>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  e = pdl_launch(tree_softmax_simt_kernel<D>, dim3((unsigned)(p.gangs * p.row_tiles)), kThreadsS,
-                 smem, stream, true, 1, p);
+  e = pdl_launch(tree_softmax_simt_kernel<D, ROWS>, dim3((unsigned)(p.gangs * p.row_tiles)),
+                 4 * ROWS, smem, stream, true, 1, p);
   note_launches(1);
   return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_simt_d(const TreeSoftmaxParams& p, cudaStream_t stream) {
+  return p.tile_base == 64 ? launch_simt_rows<D, 64>(p, stream) : launch_simt_rows<D, 32>(p, stream);
 }
 
 template <typename T, int D>
