@@ -74,17 +74,16 @@ __global__ void __launch_bounds__(kPlanThreads) tree_plan_kernel(TreeSoftmaxPara
 }
 
 // fp32 attention.  A CTA takes ROWS = 32 or 64 query rows; thread (y, x) of its
-// ROWS / 4 x 16 holds
-// rows 4y .. 4y+3 against keys x, x+16, x+32, x+48 of a tile, and columns 4x
-// (+ 64 c) of those rows' outputs.  Bound by the fp32 multiply-adds (4 D per
-// row and key against 8 D bytes per key): a row tile of 32 reuses each staged
-// key 32 times, and the 4 x 4 (4 x 4 D/64) register tiles ask shared memory
-// for one 16-byte read per eight multiply-adds.  Copies run a tile ahead, keys
-// while the previous tile's values are at work and values under the next scores
-// (staged between the products, the same calls took about twice as long).  The
-// whole call: 48 requests x 61 nodes over 1150 tokens, D = 64, 4 x 4 heads 250 us
-// (29 TFLOP/s of 74); 32 x 16 nodes, D = 128 180 us; 12 x 13 nodes, prefixes below
-// 1022, D = 64 24 us, a latency of three launches and one tile.
+// ROWS / 4 x 16 holds rows 4y .. 4y+3 against keys x, x+16, x+32, x+48 of a tile,
+// and columns 4x (+ 64 c) of those rows' outputs, in packed pairs: of dimensions in
+// the scores, of columns in the output.  Bound by shared memory's 16-byte reads (one
+// per four packed multiply-adds) and the multiply-adds (4 D per row and key against
+// 8 D bytes per key).  Copies run a tile ahead, keys while the previous tile's values
+// are at work and values under the next scores (staged between the products, the same
+// calls took about twice as long).  The whole call, prefixes of 1150 tokens: 48
+// requests x 61 nodes, D = 64 235 us (31 TFLOP/s of 74); 32 x 16 nodes, D = 128 158
+// us; 16 x 16 nodes, D = 256 160 us; 12 x 13 nodes, prefixes below 1022, D = 64 21 us,
+// a latency of three launches and one tile.
 template <int D, int ROWS>
 __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
     tree_softmax_simt_kernel(TreeSoftmaxParams p) {
@@ -177,13 +176,14 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
       mine = mine || used;
     }
     const bool warp_live = __any_sync(0xffffffffu, mine);  // else it copies only
-    float acc[4][4 * kC], mrow[4], lrow[4];
+    uint64_t acc[4][2 * kC];  // pairs of columns
+    float mrow[4], lrow[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       mrow[i] = -INFINITY;
       lrow[i] = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4 * kC; ++c) acc[i][c] = 0.f;
+      for (int c = 0; c < 2 * kC; ++c) acc[i][c] = 0ull;
     }
     for (int j = w.j0; j < w.j1; ++j) {
       const bool tree = j == w.n - 1;
@@ -193,27 +193,25 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
       const int jn = last ? nx.j0 : j + 1, page = load ? find(then, jn) : -1;
       cp_async_wait<1>();
       __syncthreads();  // the keys (and a piece's queries)
-      float s[4][4];
+      uint64_t s2[4][4];  // even and odd dimensions' sums
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[i][c] = 0.f;
+        for (int c = 0; c < 4; ++c) s2[i][c] = 0ull;
 #pragma unroll 4
       for (int d = 0; d < (warp_live ? D : 0); d += 4) {
-        float4 a[4], b[4];
+        ulonglong2 a[4], b[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(Qs + (4 * y + i) * kS + d);
+        for (int i = 0; i < 4; ++i)
+          a[i] = *reinterpret_cast<const ulonglong2*>(Qs + (4 * y + i) * kS + d);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) b[c] = *reinterpret_cast<const float4*>(Ks + (x + 16 * c) * kS + d);
+        for (int c = 0; c < 4; ++c)
+          b[c] = *reinterpret_cast<const ulonglong2*>(Ks + (x + 16 * c) * kS + d);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            s[i][c] = fmaf(a[i].x, b[c].x, s[i][c]);
-            s[i][c] = fmaf(a[i].y, b[c].y, s[i][c]);
-            s[i][c] = fmaf(a[i].z, b[c].z, s[i][c]);
-            s[i][c] = fmaf(a[i].w, b[c].w, s[i][c]);
-          }
+          for (int c = 0; c < 4; ++c)
+            s2[i][c] = f2_fma(a[i].y, b[c].y, f2_fma(a[i].x, b[c].x, s2[i][c]));
       }
       if (load) locate(then, jn, page);
       __syncthreads();  // the keys are read
@@ -221,13 +219,15 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
       if (warp_live) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float mx = -INFINITY;
+          float s[4], mx = -INFINITY;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
+            float even, odd;
+            f2_split(s2[i][c], even, odd);
             const int key = x + 16 * c;
             const bool see = tree ? (path[i] >> key) & 1 : key < valid;
-            if (!see) s[i][c] = -INFINITY;
-            mx = fmaxf(mx, s[i][c]);
+            s[c] = see ? even + odd : -INFINITY;
+            mx = fmaxf(mx, s[c]);
           }
 #pragma unroll
           for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
           float sum = 0.f;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            const float e = exp2f(s[i][c] - mref);
+            const float e = exp2f(s[c] - mref);
             Ps[(4 * y + i) * kPS + x + 16 * c] = e;
             sum += e;
           }
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
           lrow[i] = lrow[i] * corr + sum;
           mrow[i] = mnew;
 #pragma unroll
-          for (int c = 0; c < 4 * kC; ++c) acc[i][c] *= corr;
+          for (int c = 0; c < 2 * kC; ++c) acc[i][c] = f2_mul(f2_dup(corr), acc[i][c]);
         }
       }
       if (load) cp_async_wait<1>();
@@ -262,14 +262,13 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
         for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
           for (int c = 0; c < kC; ++c) {
-            const float4 v = *reinterpret_cast<const float4*>(Vs + (k + kk) * kS + 4 * x + 64 * c);
+            const ulonglong2 v =
+                *reinterpret_cast<const ulonglong2*>(Vs + (k + kk) * kS + 4 * x + 64 * c);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float pk = kk == 0 ? pr[i].x : kk == 1 ? pr[i].y : kk == 2 ? pr[i].z : pr[i].w;
-              acc[i][4 * c] = fmaf(pk, v.x, acc[i][4 * c]);
-              acc[i][4 * c + 1] = fmaf(pk, v.y, acc[i][4 * c + 1]);
-              acc[i][4 * c + 2] = fmaf(pk, v.z, acc[i][4 * c + 2]);
-              acc[i][4 * c + 3] = fmaf(pk, v.w, acc[i][4 * c + 3]);
+              acc[i][2 * c] = f2_fma(f2_dup(pk), v.x, acc[i][2 * c]);
+              acc[i][2 * c + 1] = f2_fma(f2_dup(pk), v.y, acc[i][2 * c + 1]);
             }
           }
       }
@@ -289,8 +288,9 @@ __global__ void __launch_bounds__(4 * ROWS, simt_ctas(D, ROWS))
           ((size_t)w.r * p.N + rows.node(row)) * p.Hq + w.kvh * p.G + rows.head(row);
 #pragma unroll
       for (int c = 0; c < kC; ++c) {
-        const float4 a = make_float4(acc[i][4 * c] * inv, acc[i][4 * c + 1] * inv,
-                                     acc[i][4 * c + 2] * inv, acc[i][4 * c + 3] * inv);
+        float4 a;
+        f2_split(f2_mul(f2_dup(inv), acc[i][2 * c]), a.x, a.y);
+        f2_split(f2_mul(f2_dup(inv), acc[i][2 * c + 1]), a.z, a.w);
         if (whole) store4(static_cast<float*>(p.out) + o * D + 4 * x + 64 * c, a);
         else *tree_part_at(p, part, row, x + 16 * c) = a;
       }
