@@ -44,8 +44,8 @@
 //
 // The whole call: 64 requests x 16 nodes, prefixes of 512 to 8192, D = 256: 114 us,
 // 5.2 TB/s, bound by the keys' and values' bytes.  96 requests x up to 61 nodes,
-// prefixes of 251 to 2048, D = 128, 16 tokens a page: 87 us, 3.1 TB/s; a tile takes
-// 1.0 us for its two row tiles, 0.67 us of it the MMAs, and the pieces' ends and
+// prefixes of 251 to 2048, D = 128, 16 tokens a page: 85 us, 3.2 TB/s; a tile takes
+// 0.9 us for its two row tiles, 0.67 us of it the MMAs, and the pieces' ends and
 // joins 25 us of the call.  One token over 16384: 18 us, most of it the three
 // launches' chain.
 // Every wait is bounded; a timeout sets FLARE_DEV_WAIT_TIMEOUT, the CTA stops
@@ -127,6 +127,12 @@ __device__ __forceinline__ bool group_or(uint32_t id, bool x) {
       : "r"(id), "r"((int)x)
       : "memory");
   return r != 0;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 
 // 32 bytes, a memory sector, per thread and instruction: the output's rows are
@@ -502,7 +508,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         // tile maximum of the raw scores (scale >= 0 keeps the order)
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < kTreeTile; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(sr[c]));
+        for (int c = 0; c < kTreeTile; c += 2)
+          mx[c / 2 & 3] = max3(mx[c / 2 & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
         const float mt_ = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         const float m_new = fmaxf(m_run, mt_ * p.scale_log2);
         const bool need = j == 0 || m_new > m_run + kMoveMax;
@@ -511,17 +518,22 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
         const float corr = j == 0 ? 0.f : tc::ex2(m_run - m_use);
         // a row that sees nothing of its tiles so far: every probability 0
         const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
-        float sum0 = 0.f, sum1 = 0.f;
+        const uint64_t scale2 = f2_dup(p.scale_log2), neg2 = f2_dup(neg_m);
+        uint64_t sum = 0ull;
         uint32_t pk[kTreeTile / 2];
 #pragma unroll
         for (int c = 0; c < kTreeTile; c += 2) {
-          const float p0 = tc::ex2(fmaf(__uint_as_float(sr[c]), p.scale_log2, neg_m));
-          const float p1 = tc::ex2(fmaf(__uint_as_float(sr[c + 1]), p.scale_log2, neg_m));
-          sum0 += p0;
-          sum1 += p1;
+          float p0, p1;
+          f2_split(f2_fma(f2(__uint_as_float(sr[c]), __uint_as_float(sr[c + 1])), scale2, neg2), p0,
+                   p1);
+          p0 = tc::ex2(p0);
+          p1 = tc::ex2(p1);
+          sum = f2_add(sum, f2(p0, p1));
           const __nv_bfloat162 h2 = __floats2bfloat162_rn(p0, p1);
           pk[c / 2] = *reinterpret_cast<const uint32_t*>(&h2);
         }
+        float sum0, sum1;
+        f2_split(sum, sum0, sum1);
         l_run = j == 0 ? sum0 + sum1 : l_run * corr + (sum0 + sum1);
         if (move && j >= 1) {  // rescale O, the previous tile's product done
           const int pb = (gg - 1) % kSB;
