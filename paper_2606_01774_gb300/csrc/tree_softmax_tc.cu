@@ -445,13 +445,20 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
 
     bool ok = true;
     int g = 0;  // running tile count (of row tile 0: the rings' too)
-    // V rows of tile j that no query may see.  The slot cannot be refilled
-    // before this tile's product, which waits for these threads, so the parity
-    // wait is exact though not every tile is waited for.
+    // V rows of tile j that no query may see.  The slot cannot be refilled before
+    // this tile's product, which waits for these threads, so the parity wait is
+    // exact, though not every tile is waited for, once the slot's last tile has been
+    // read: with more score buffers than V slots these threads may be ahead of that.
     auto zero_v = [&](int j) -> bool {
       const int valid = it.valid(j);
       if (t != 0 || valid == kTreeTile) return true;
       const int gg = g + j, st = gg % C::kVStages;
+      if constexpr (kSB > C::kVStages) {
+        const int last = gg - C::kVStages;
+        if (last >= 0 && !warp_wait_t(&sh.pv_done[t][last % kSB], (uint32_t)(last / kSB) & 1u,
+                                      &sh.abort_flag))
+          return false;
+      }
       if (!warp_wait_t(&sh.v_full[st], (uint32_t)(gg / C::kVStages) & 1u, &sh.abort_flag))
         return false;
       uint8_t* dst = Vs + st * C::kTileBytes;
@@ -512,7 +519,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           mx[c / 2 & 3] = max3(mx[c / 2 & 3], __uint_as_float(sr[c]), __uint_as_float(sr[c + 1]));
         const float mt_ = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         const float m_new = fmaxf(m_run, mt_ * p.scale_log2);
-        const bool need = j == 0 || m_new > m_run + kMoveMax;
+        // (rows in use decide: what the others hold is not defined)
+        const bool need = j == 0 || (live && m_new > m_run + kMoveMax);
         const bool move = __any_sync(0xffffffffu, need);
         const float m_use = move ? m_new : m_run;
         const float corr = j == 0 ? 0.f : tc::ex2(m_run - m_use);
