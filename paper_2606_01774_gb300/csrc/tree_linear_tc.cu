@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
             f2_split(xy[2 * u + 1], x, y);
             f2_split(c1.y, unused, m1);
             const uint64_t d1 = f2_dup(x);
-            o1 = p.scale * fmaf(m1, x, y);
+            if (i0 + 2 * u + 1 < n) o1 = p.scale * fmaf(m1, x, y);
 #pragma unroll
             for (int e = 2 * u + 2; e < 16; ++e) {
               const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(T + tl_at(e, u));

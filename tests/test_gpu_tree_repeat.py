@@ -1,12 +1,12 @@
 """Softmax calls whose pieces, tiles and warps race one another: the same bits every time, and
-the definition's values (tolerances as in test_gpu_tree.py)."""
+the definition's values (tolerances as in test_gpu_tree.py); and unused rows beside a NaN."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import tree as ref
 from test_gpu_tree import SOFTMAX_REL, rel
-from tree_helpers import run_softmax, softmax_inputs
+from tree_helpers import linear_inputs, run_linear, run_softmax, softmax_inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +35,14 @@ def test_softmax_repeats_bit_for_bit(R, N, Hq, Hkv, D, page, longest):
     live = np.arange(N) < s.node_len.cpu().numpy()[sample][:, None]
     got = out[torch.tensor(sample, device="cuda")][torch.from_numpy(live).cuda()]
     assert rel(got, want[live]) <= SOFTMAX_REL["bf16"]
+
+
+@pytest.mark.parametrize("dtype,dk", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("N,n", [(12, 5), (16, 15), (30, 17), (40, 33)])
+def test_linear_unused_rows_are_zero_beside_a_nan(N, n, dtype, dk):
+    """A NaN in the last used node stays out of the rows after it."""
+    s = linear_inputs(80, 2, N, 2, 4, dk, dk, dtype, [n, N])
+    s.v[0, n - 1] = float("nan")
+    out = run_linear(s)
+    assert bool((out[0, n:] == 0).all())
+    assert bool(torch.isfinite(out[1]).all())
