@@ -30,7 +30,7 @@
 // pieces become operands.  Warps 0-3 turn pieces into the bf16 operand S0^T in
 // tensor memory, then tables, substitution and readout.  BM <= 32: 128
 // tensor-memory columns, four (BM = 16) or three CTAs per SM; BM = 64: two.
-// 64 requests x 16 nodes x 32 heads: 31.5 us, 5.1 TB/s; 6 x 61 nodes: 13.0 us.
+// 64 requests x 16 nodes x 32 heads: 32.2 us, 4.9 TB/s; 6 x 61 nodes: 13.3 us.
 // Every wait is bounded; on a timeout the CTA sets FLARE_DEV_WAIT_TIMEOUT,
 // lets its copies and MMAs land, frees its tensor memory and exits.
 #include <cudaTypedefs.h>
@@ -592,14 +592,14 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
             f2_split(xy[2 * u + 1], x, y);
             f2_split(c1.y, unused, m1);
             const uint64_t d1 = f2_dup(x);
-            if (i0 + 2 * u + 1 < n) o1 = p.scale * fmaf(m1, x, y);
+            o1 = p.scale * fmaf(m1, x, y);
 #pragma unroll
             for (int e = 2 * u + 2; e < 16; ++e) {
               const ulonglong2 c = *reinterpret_cast<const ulonglong2*>(T + tl_at(e, u));
               xy[e] = f2_fma(c.y, d1, f2_fma(c.x, d0, xy[e]));
             }
           }
-          store2(i0 + 2 * u, o0, o1);
+          store2(i0 + 2 * u, o0, i0 + 2 * u + 1 < n ? o1 : 0.f);
         }
         if (BM > 16 && i0 + 16 < n) {
           // this block's deltas into the later blocks' sums
