@@ -202,7 +202,9 @@ struct TreeVerifyParams {
   int32_t* next_token;        // [R]
   float* node_logp;           // [R,N]
   int chunk, n_chunks;        // row statistics: tokens per chunk, chunks per row
-  float4* stats;              // [R,N,n_chunks] {max, sum of 2^(x - max), first argmax, -}, x in log2 units
+  // [R,N,n_chunks] {max, sum of 2^(scale (x - max)), first argmax, -} of the logits x,
+  // with scale = inv_temp log2 e
+  float4* stats;
   int32_t* dev_status;
 };
 void plan_tree_verify(int R, int N, int V, int num_sms, int* chunk, int* n_chunks);

@@ -57,13 +57,14 @@ __device__ __forceinline__ void warp_best(float& v, int& i) {
   }
 }
 
-// {max, sum of 2^(x - max), argmax} of a row from its parts on a warp's lanes
-// (x in units of log2): the maximum first, then one rescaling per part.
-__device__ __forceinline__ float4 warp_stats(float4 st) {
+// {max, sum of 2^(scale (x - max)), argmax} of a row from its parts on a warp's
+// lanes: the maximum first, then one rescaling per part.  Maxima are the logits
+// themselves: times the scale, neighbouring floats can round to one value.
+__device__ __forceinline__ float4 warp_stats(float4 st, float scale) {
   float m = st.x;
   int best = (int)st.z;
   warp_best(m, best);
-  float s = st.x == -INFINITY ? st.y : st.y * tc::ex2(st.x - m);  // a NaN sum stays one
+  float s = st.x == -INFINITY ? st.y : st.y * tc::ex2(scale * (st.x - m));  // a NaN sum stays one
   s = warp_sum(s);
   return make_float4(m, s, (float)best, 0.f);
 }
@@ -161,12 +162,13 @@ __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams
     }
   }
   if (tid < hi - tail) one(tail + tid);
-  float4 st = warp_stats(make_float4(m * scale, s, (float)best, 0.f));
+  float4 st = warp_stats(make_float4(m, s, (float)best, 0.f), scale);
   if ((tid & 31) == 0) red[tid >> 5] = st;
   __syncthreads();
   if (tid < 32) {
     st = warp_stats(tid < kRowThreads / 32 ? red[tid]
-                                           : make_float4(-INFINITY, 0.f, (float)p.V, 0.f));
+                                           : make_float4(-INFINITY, 0.f, (float)p.V, 0.f),
+                    scale);
     if (tid == 0) p.stats[(size_t)row * p.n_chunks + blockIdx.x] = st;
   }
 }
@@ -290,10 +292,10 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
         st = c0 + lane - 1 < p.n_chunks
                  ? p.stats[((size_t)r * p.N + i) * p.n_chunks + c0 + lane - 1]
                  : make_float4(-INFINITY, 0.f, (float)p.V, 0.f);
-      st = warp_stats(st);
+      st = warp_stats(st, scale);
     }
     if (lane == 0) {
-      sh.lse2[i] = st.x + log2f(st.y);
+      sh.lse2[i] = fmaf(st.x, scale, log2f(st.y));
       sh.best_of[i] = (int)st.z;
       if (!(fabsf(sh.lse2[i]) < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
     }
