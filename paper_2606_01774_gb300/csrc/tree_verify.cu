@@ -48,6 +48,34 @@ __device__ __forceinline__ void take_best(float& v, int& i, float v2, int i2) {
   }
 }
 
+// The temperature as a factor on differences of logits, for powers of two.
+__device__ __forceinline__ float log2_scale(float inv_temp) {
+  return fminf(inv_temp * kLog2e, 3.402823466e38f);
+}
+
+// The same in a race of candidates of value 2^(scale v) / 2^e: by the difference of
+// two, which keeps its digits where the products with the scale would lose them (a
+// low temperature) or overflow (logits at the end of the type's range).
+__device__ __forceinline__ void take_race(float& v, float& e, int& i, float v2, float e2, int i2,
+                                          float scale) {
+  const float d = fmaf(v2 - v, scale, e - e2);
+  if (d > 0.f || (d == 0.f && i2 < i)) {
+    v = v2;
+    e = e2;
+    i = i2;
+  }
+}
+
+__device__ __forceinline__ void warp_race(float& v, float& e, int& i, float scale) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float v2 = __shfl_xor_sync(0xffffffffu, v, o);
+    const float e2 = __shfl_xor_sync(0xffffffffu, e, o);
+    const int i2 = __shfl_xor_sync(0xffffffffu, i, o);
+    take_race(v, e, i, v2, e2, i2, scale);
+  }
+}
+
 __device__ __forceinline__ void warp_best(float& v, int& i) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -92,7 +120,7 @@ __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams
   }
   const int lo = blockIdx.x * p.chunk, hi = min(p.V, lo + p.chunk);
   const T* x = static_cast<const T*>(p.logits) + (size_t)row * p.V;
-  const float scale = p.inv_temp * kLog2e;
+  const float scale = log2_scale(p.inv_temp);
   float m = -INFINITY, s = 0.f;  // maximum of the raw logits, sum of 2^(scale (x - m))
   int best = p.V;
   auto one = [&](int at) {
@@ -151,12 +179,15 @@ __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams
         for (int k = kE - 1; k >= 0; --k)
           if (v[k] == bm) best = min(best, base + k);
       }
-      const float neg = m == -INFINITY ? 0.f : -scale * m;
+      // differences first: the lowest finite logit times the scale overflows
+      const uint64_t neg = f2_dup(m == -INFINITY ? 0.f : -m), scale2 = f2_dup(scale);
       float s0 = 0.f, s1 = 0.f;
 #pragma unroll
       for (int k = 0; k < kE; k += 2) {
-        s0 += tc::ex2(fmaf(v[k], scale, neg));
-        s1 += tc::ex2(fmaf(v[k + 1], scale, neg));
+        float d0, d1;
+        f2_split(f2_mul(scale2, f2_add(f2(v[k], v[k + 1]), neg)), d0, d1);
+        s0 += tc::ex2(d0);
+        s1 += tc::ex2(d1);
       }
       s += s0 + s1;
     }
@@ -203,8 +234,9 @@ __device__ __forceinline__ uint32_t cluster_word(const void* mine, uint32_t rank
 struct WalkShared {
   int par[kMaxNodes], tok[kMaxNodes], line[kMaxNodes], best_of[kMaxNodes], gone[kMaxNodes];
   unsigned long long kids[kMaxNodes];
-  float uni[kMaxNodes], logp2[kMaxNodes], lse2[kMaxNodes], q[kMaxNodes], prob[kMaxNodes];
-  float red_v[kWalkThreads / 32];
+  float uni[kMaxNodes], logp[kMaxNodes], q[kMaxNodes], prob[kMaxNodes];
+  float mx[kMaxNodes], ls2[kMaxNodes];  // a row's maximum, log2 of its sum
+  float red_v[kWalkThreads / 32], red_e[kWalkThreads / 32];
   int red_i[kWalkThreads / 32];
   int tree_ok;
   // the walk: the node it stands at, its path, the residual there
@@ -213,7 +245,7 @@ struct WalkShared {
   float c, m;
   // this CTA's share of a pass over a row, in two buffers: a CTA is at most
   // one pass ahead of another that still reads its last share
-  float part_v[2];
+  float part_v[2], part_e[2];
   int part_i[2], part_odd[2];
 };
 
@@ -272,13 +304,13 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     return;
   }
   const T* rows = static_cast<const T*>(p.logits) + (size_t)r * p.N * p.V;
-  const float scale = p.inv_temp * kLog2e;  // logits in units of log2
+  const float scale = log2_scale(p.inv_temp);
   const float* drafts =
       sample && p.draft_probs ? p.draft_probs + (size_t)r * p.N * p.V : nullptr;
   float x_tok = 0.f;  // the drafted token's logit, and its probability for the drafter
   if (tid > 0 && tid < n) {
     const size_t at = (size_t)sh.par[tid] * p.V + sh.tok[tid];
-    x_tok = to_f32(rows[at]) * scale;
+    x_tok = to_f32(rows[at]);
     sh.q[tid] = drafts ? drafts[at] : 1.f;
   }
   const int lo = (int)((long long)p.V * rank / ranks), hi = (int)((long long)p.V * (rank + 1) / ranks);
@@ -295,9 +327,10 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
       st = warp_stats(st, scale);
     }
     if (lane == 0) {
-      sh.lse2[i] = fmaf(st.x, scale, log2f(st.y));
+      sh.mx[i] = st.x;
+      sh.ls2[i] = log2f(st.y);
       sh.best_of[i] = (int)st.z;
-      if (!(fabsf(sh.lse2[i]) < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
+      if (!(fabsf(st.x) < INFINITY && st.y < INFINITY)) bad = FLARE_DEV_BAD_LOGITS;
     }
   }
   if (__syncthreads_or(bad)) {
@@ -305,8 +338,11 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     return;
   }
   if (tid < kMaxNodes) {
-    sh.logp2[tid] = tid > 0 && tid < n ? x_tok - sh.lse2[sh.par[tid]] : 0.f;
-    sh.prob[tid] = exp2f(sh.logp2[tid]);
+    const bool drafted = tid > 0 && tid < n;
+    const int at = drafted ? sh.par[tid] : 0;
+    const float d = x_tok - sh.mx[at], ls2 = sh.ls2[at];
+    sh.logp[tid] = drafted ? fmaf(d, p.inv_temp, ls2 * -0.6931471805599453f) : 0.f;
+    sh.prob[tid] = drafted ? exp2f(fmaf(d, scale, -ls2)) : 0.f;
   }
   if (tid == 0) {
     sh.cur = 0;
@@ -378,7 +414,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     if (!sh.more) break;
     const T* x = rows + (size_t)sh.cur * p.V;
     const float* q = drafts + (size_t)sh.cur * p.V;
-    const float c = sh.c, shift = sh.lse2[sh.cur];
+    const float c = sh.c, mx = sh.mx[sh.cur], ls2 = sh.ls2[sh.cur];
     float sum = 0.f;
     for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
       float xv[kIn], qv[kIn];
@@ -389,7 +425,8 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
         qv[u] = t < hi ? q[t] : 0.f;
       }
 #pragma unroll
-      for (int u = 0; u < kIn; ++u) sum += fmaxf(tc::ex2(fmaf(xv[u], scale, -shift)) - c * qv[u], 0.f);
+      for (int u = 0; u < kIn; ++u)
+        sum += fmaxf(tc::ex2(fmaf(xv[u] - mx, scale, -ls2)) - c * qv[u], 0.f);
     }
     sum = warp_sum(sum);
     if (lane == 0) sh.red_v[warp] = sum;
@@ -420,11 +457,14 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     int ng = sh.n_gone;
     while (true) {
       const float* q = c > 0.f ? drafts + (size_t)cur * p.V : nullptr;
-      const float shift = q ? sh.lse2[cur] : 0.f;
-      float v0 = -INFINITY, top = -INFINITY;  // top: a NaN once one was read
+      const float mx = q ? sh.mx[cur] : 0.f, ls2 = q ? sh.ls2[cur] : 0.f;
+      const bool race = sample && !q;  // candidates as {logit, log2 noise}, else as values
+      const float by = race ? scale : 1.f;
+      float v0 = -INFINITY, e0 = 0.f, top = -INFINITY;  // top: a NaN once one was read
       int i0 = p.V;
       // tokens come in ascending order: the first of equals stays.  Quotients and
-      // powers to 2 ulp: only candidates that close to equal can change places.
+      // powers to 2 ulp, and w = p - c q to 2 ulp of p: only candidates that close to
+      // equal can change places.
       auto take = [&](bool ok, float v, int t) {
         if (ok && v > v0) {
           v0 = v;
@@ -449,32 +489,40 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
         } else if (q) {
 #pragma unroll
           for (int u = 0; u < kIn; ++u) {
-            const float w = tc::ex2(fmaf(xv[u], scale, -shift)) - c * qv[u];
+            const float w = tc::ex2(fmaf(xv[u] - mx, scale, -ls2)) - c * qv[u];
             take(w > 0.f, __fdividef(w, ev[u]), t0 + u * kWalkThreads);
           }
-        } else {  // in logarithms: no normaliser is needed
+        } else {  // in logarithms, against the best so far: no normaliser is needed
 #pragma unroll
           for (int u = 0; u < kIn; ++u) {
             const int t = t0 + u * kWalkThreads;
             bool in = true;
             for (int e = 0; e < ng; ++e) in = in && sh.gone[e] != t;
-            take(in, fmaf(xv[u], scale, -log2f(ev[u])), t);
+            const float e = log2f(ev[u]);
+            if (in && fmaf(xv[u] - v0, scale, e0 - e) > 0.f) {
+              v0 = xv[u];
+              e0 = e;
+              i0 = t;
+            }
           }
         }
       }
       odd |= !(top < INFINITY);
-      warp_best(v0, i0);
+      warp_race(v0, e0, i0, by);
       if (lane == 0) {
         sh.red_v[warp] = v0;
+        sh.red_e[warp] = e0;
         sh.red_i[warp] = i0;
       }
       const int any_odd = __syncthreads_or(odd);
       if (warp == 0) {
         v0 = lane < kWarps ? sh.red_v[lane] : -INFINITY;
+        e0 = lane < kWarps ? sh.red_e[lane] : 0.f;
         i0 = lane < kWarps ? sh.red_i[lane] : p.V;
-        warp_best(v0, i0);
+        warp_race(v0, e0, i0, by);
         if (lane == 0) {
           sh.part_v[pass & 1] = v0;
+          sh.part_e[pass & 1] = e0;
           sh.part_i[pass & 1] = i0;
           sh.part_odd[pass & 1] = any_odd;
         }
@@ -482,14 +530,16 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
       cluster_sync();
       if (warp == 0) {
         v0 = -INFINITY;
+        e0 = 0.f;
         i0 = p.V;
         int o = 0;
         if (lane < (int)ranks) {
           v0 = __uint_as_float(cluster_word(&sh.part_v[pass & 1], lane));
+          e0 = __uint_as_float(cluster_word(&sh.part_e[pass & 1], lane));
           i0 = (int)cluster_word(&sh.part_i[pass & 1], lane);
           o = (int)cluster_word(&sh.part_odd[pass & 1], lane);
         }
-        warp_best(v0, i0);
+        warp_race(v0, e0, i0, by);
         o = __any_sync(0xffffffffu, o);
         if (lane == 0) {
           sh.red_i[0] = i0;
@@ -515,7 +565,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
   }
   if (tid < p.N) {
     p.path[(size_t)r * p.N + tid] = tid < sh.len ? sh.line[tid] : -1;
-    p.node_logp[(size_t)r * p.N + tid] = sh.logp2[tid] * 0.6931471805599453f;
+    p.node_logp[(size_t)r * p.N + tid] = sh.logp[tid];
   }
   if (tid == 0) {
     p.path_len[r] = sh.len;

@@ -59,3 +59,78 @@ def test_greedy_tells_maxima_one_ulp_apart(x, low, high):
     got, _ = check_verify(s)
     assert got["path_len"].tolist() == [2, 1, 2]
     assert got["next_token"].tolist() == [high, high, low]
+
+
+LOWEST_RUNS = {"head": [(0, 3001)], "tail": [(5003, 9001)], "chunks": [(2048, 8192)],
+               "all but a few": [(0, 4000), (4003, 8990)], "every second 64": [
+                   (a, a + 64) for a in range(0, 9001, 128)]}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts,greedy", [("sampled", False), ("top", False), ("top", True)])
+@pytest.mark.parametrize("inv_temp", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("run", sorted(LOWEST_RUNS))
+def test_runs_of_the_lowest_finite_logit(run, inv_temp, drafts, greedy, dtype):
+    """Tokens ruled out by the type's lowest value in long runs, as masks leave them."""
+    s = verify_inputs(91, 12, 6, 9001, dtype, drafts, greedy, inv_temp, nodes=[6 - r % 3 for r in
+                                                                              range(12)])
+    for a, b in LOWEST_RUNS[run]:
+        s.logits[:, :, a:b] = torch.finfo(DTYPES[dtype][0]).min
+    check_verify(s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("drafts,greedy", [("sampled", False), ("top", False), ("top", True)])
+def test_rows_of_nothing_but_the_lowest_finite_logit(drafts, greedy, dtype):
+    """Every token alike: the first when greedy, else the uniform distribution."""
+    s = verify_inputs(92, 16, 3, 3001, dtype, drafts, greedy, nodes=[3] * 16, shape="star")
+    s.logits[:, 0] = torch.finfo(DTYPES[dtype][0]).min
+    s.token[:, 1:] = s.token[:, 1:].clamp(min=1)
+    if s.draft_probs is not None:
+        s.uniform.fill_(0.999)  # rejected mostly: the residual of a uniform row decides
+    got, _ = check_verify(s)
+    if greedy:
+        assert got["next_token"].tolist() == [0] * 16
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("inv_temp", [2.0 ** -20, 100.0, 1e4, 2.9e38])
+@pytest.mark.parametrize("drafts", ["sampled", "top"])
+def test_temperatures_far_from_one_on_rows_with_children(drafts, inv_temp, dtype):
+    """Logits near 40 under inverse temperatures whose product with them has no digits left for
+    their differences."""
+    s = verify_inputs(93, 20, 5, 2500, dtype, drafts, False, 1.0, nodes=[5] * 20, shape="star")
+    s.logits += 40.0
+    s.inv_temp = s.desc.inv_temperature = float(np.float32(inv_temp))
+    s.token[:, 1] = s.logits[:, 0].argmax(-1).int()
+    got, want = check_verify(s, allowed=1.0)
+    assert np.array_equal(got["path"].cpu().numpy()[want["margin"] > 1e-4],
+                          want["path"][want["margin"] > 1e-4])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("inv_temp", [1.0, 1e4, 1e7, 2.9e38])
+def test_next_token_among_equal_logits_at_low_temperatures(inv_temp, dtype):
+    """Twenty tokens share the greatest logit: the noise alone chooses among them, on a row without
+    children, however low the temperature."""
+    s = verify_inputs(94, 64, 2, 5003, dtype, "top", False, inv_temp, nodes=[1 + r % 2 for r in
+                                                                           range(64)])
+    s.inv_temp = s.desc.inv_temperature = float(np.float32(inv_temp))
+    s.logits.clamp_(max=10.0)
+    s.logits[:, :, 7::251] = 41.5
+    got, _ = check_verify(s)
+    assert bool((got["next_token"] % 251 == 7).all())
+    assert len(set(got["next_token"].tolist())) > 10
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", ["lowest", "greatest"])
+@pytest.mark.parametrize("inv_temp", [0.5, 1.0, 2.0])
+def test_next_token_from_rows_at_the_ends_of_the_range(inv_temp, value, dtype):
+    """A row without children that holds one finite value throughout is a uniform distribution."""
+    s = verify_inputs(95, 32, 1, 4001, dtype, "top", False, inv_temp, nodes=[1] * 32)
+    info = torch.finfo(DTYPES[dtype][0])
+    s.logits.fill_(info.min if value == "lowest" else info.max)
+    s.logits[:, :, 1::2] = float("-inf")
+    got, _ = check_verify(s)
+    assert bool((got["next_token"] % 2 == 0).all())
