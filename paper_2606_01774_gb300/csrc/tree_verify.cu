@@ -12,7 +12,8 @@
 // after j rejections the unnormalised residual is max(p - c_j q, 0) with
 // c_0 = 0, c_{j+1} = c_j + m_j, m_j its mass (m_0 = 1), so no residual is
 // stored, and a mass is only summed when another sibling is still to be tried.
-// With fixed drafts the residual is p without the rejected tokens.
+// With fixed drafts the residual is p without the rejected tokens: their p comes
+// off the mass, which is summed anew when little of it is left.
 // The next token is the argmax of w / noise (noise ~ Exp(1) samples w).
 //
 // Bound by the logits' bytes on many rows and by latency on few.  The walk
@@ -38,6 +39,9 @@ constexpr int kRowThreads = 128;
 constexpr int kWalkThreads = 512;
 constexpr int kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
+// Fixed drafts: the part of a summed mass down to which differences from it are
+// taken.  They are off by a few 2^-24 of that mass, so the rest by 2^-14 at most.
+constexpr float kResum = 1.f / 256;
 
 // The better of two (value, index) candidates: the greater value, the lower
 // index among equals.
@@ -242,7 +246,7 @@ struct WalkShared {
   // the walk: the node it stands at, its path, the residual there
   int cur, len, more, n_gone;
   unsigned long long left;  // children still to be tried
-  float c, m;
+  float c, m, summed;       // summed: the mass when it was last a sum
   // this CTA's share of a pass over a row, in two buffers: a CTA is at most
   // one pass ahead of another that still reads its last share
   float part_v[2], part_e[2];
@@ -350,7 +354,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     sh.line[0] = 0;
     sh.left = sh.kids[0];
     sh.c = 0.f;
-    sh.m = 1.f;
+    sh.m = sh.summed = 1.f;
     sh.n_gone = 0;
   }
   __syncthreads();
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     if (tid == 0) {
       int cur = sh.cur, len = sh.len, more = 0;
       unsigned long long left = sh.left;
-      float c = sh.c, m = sh.m;
+      float c = sh.c, m = sh.m, summed = sh.summed;
       while (left) {
         const int i = __ffsll((long long)left) - 1;
         left &= left - 1;
@@ -391,6 +395,10 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
             if (!ok && !was) {
               sh.gone[sh.n_gone++] = sh.tok[i];
               m = fmaxf(m - px, 0.f);
+              if (left && m < kResum * summed) {
+                more = 1;
+                break;
+              }
             }
           }
         }
@@ -399,7 +407,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
           sh.line[len++] = i;
           left = sh.kids[i];
           c = 0.f;
-          m = 1.f;
+          m = summed = 1.f;
           sh.n_gone = 0;
         }
       }
@@ -408,25 +416,37 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
       sh.left = left;
       sh.c = c;
       sh.m = m;
+      sh.summed = summed;
       sh.more = more;
     }
     __syncthreads();
     if (!sh.more) break;
     const T* x = rows + (size_t)sh.cur * p.V;
-    const float* q = drafts + (size_t)sh.cur * p.V;
     const float c = sh.c, mx = sh.mx[sh.cur], ls2 = sh.ls2[sh.cur];
     float sum = 0.f;
-    for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
-      float xv[kIn], qv[kIn];
+    if (drafts) {
+      const float* q = drafts + (size_t)sh.cur * p.V;
+      for (int t0 = lo + tid; t0 < hi; t0 += kIn * kWalkThreads) {
+        float xv[kIn], qv[kIn];
 #pragma unroll
-      for (int u = 0; u < kIn; ++u) {
-        const int t = t0 + u * kWalkThreads;
-        xv[u] = t < hi ? to_f32(x[t]) : -INFINITY;
-        qv[u] = t < hi ? q[t] : 0.f;
+        for (int u = 0; u < kIn; ++u) {
+          const int t = t0 + u * kWalkThreads;
+          xv[u] = t < hi ? to_f32(x[t]) : -INFINITY;
+          qv[u] = t < hi ? q[t] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kIn; ++u)
+          sum += fmaxf(tc::ex2(fmaf(xv[u] - mx, scale, -ls2)) - c * qv[u], 0.f);
       }
-#pragma unroll
-      for (int u = 0; u < kIn; ++u)
-        sum += fmaxf(tc::ex2(fmaf(xv[u] - mx, scale, -ls2)) - c * qv[u], 0.f);
+    } else {
+      const int ng = sh.n_gone;
+#pragma unroll 1
+      for (int t = lo + tid; t < hi; t += kWalkThreads) {
+        bool in = true;
+#pragma unroll 1
+        for (int e = 0; e < ng; ++e) in = in && sh.gone[e] != t;
+        if (in) sum += tc::ex2(fmaf(to_f32(x[t]) - mx, scale, -ls2));
+      }
     }
     sum = warp_sum(sum);
     if (lane == 0) sh.red_v[warp] = sum;
@@ -439,7 +459,7 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
     if (warp == 0) {
       const float m = warp_sum(
           lane < (int)ranks ? __uint_as_float(cluster_word(&sh.part_v[pass & 1], lane)) : 0.f);
-      if (lane == 0) sh.m = m;
+      if (lane == 0) sh.m = sh.summed = m;
     }
     ++pass;
     __syncthreads();

@@ -134,3 +134,33 @@ def test_next_token_from_rows_at_the_ends_of_the_range(inv_temp, value, dtype):
     s.logits[:, :, 1::2] = float("-inf")
     got, _ = check_verify(s)
     assert bool((got["next_token"] % 2 == 0).all())
+
+
+@pytest.mark.parametrize("rest", [1e-5, 2e-6, 1e-6, 6e-7, 4e-7])
+@pytest.mark.parametrize("siblings", [2, 3])
+def test_fixed_drafts_that_hold_nearly_all_of_the_mass(siblings, rest):
+    """The first sibling holds all but `rest` of the row and is rejected by the greatest uniform
+    below one; the second is accepted with its share of the rest, to 5 % here.  (With three, the
+    second in turn holds all but `rest` of that.)  1 - p from fp32's p knows the rest to 1e-7.
+    Every decision's fp64 margin exceeds 2.4e-7, twice what an fp32 p near one is off by."""
+    R, V = 64, 1000
+    s = verify_inputs(96, R, 1 + siblings, V, "f32", "top", False, 1.0, nodes=[1 + siblings] * R,
+                      shape="star")
+    s.logits[:] = -1e4
+    x = torch.full((R, V), -1e4, dtype=torch.float64)
+    spread = torch.rand(R, V - 10, dtype=torch.float64, generator=torch.Generator().manual_seed(1))
+    tail = rest * (1 if siblings == 2 else 1e-3)
+    share = 0.5 * tail  # the last sibling's half of the tail, the rest spread over the row
+    x[:, 10:] = torch.log(share * spread / spread.sum(1, keepdim=True))
+    x[:, 0] = np.log1p(-rest)
+    if siblings == 3:
+        x[:, 1] = np.log(rest - tail)
+    x[:, siblings - 1] = np.log(share)
+    s.logits[:, 0] = (x + 80.0 - 0.37 * torch.arange(R, dtype=torch.float64)[:, None]).float().cuda()
+    s.token[:, 1:] = torch.arange(siblings, dtype=torch.int32)
+    s.uniform[:, 1:siblings] = 1.0 - 2.0 ** -24
+    s.uniform[0::2, siblings] = 0.475
+    s.uniform[1::2, siblings] = 0.525
+    got, want = check_verify(s, margin=0.0 if siblings == 3 else 2.4e-7, allowed=0.0)
+    if siblings == 2:
+        assert got["path_len"].tolist() == [2, 1] * (R // 2)
