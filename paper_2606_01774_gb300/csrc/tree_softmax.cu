@@ -12,6 +12,8 @@
 //
 // Online softmax in base 2 with the logit scale folded into q; running
 // maximum, sum and output in fp32.
+#include <limits>
+
 #include "async.cuh"
 #include "common.cuh"
 #include "kernels.h"
@@ -495,7 +497,12 @@ cudaError_t launch_d(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream)
 
 }  // namespace
 
-cudaError_t launch_tree_softmax(const TreeSoftmaxParams& p, bool bf16, cudaStream_t stream) {
+cudaError_t launch_tree_softmax(const TreeSoftmaxParams& params, bool bf16, cudaStream_t stream) {
+  TreeSoftmaxParams p = params;
+  // The bf16 kernel masks scores by -inf before it scales them, which 0 would turn
+  // into a NaN.  The least positive float instead leaves a score below 2^126 less than
+  // 2^-23 of a weight, and -inf as it is.
+  if (bf16 && p.scale_log2 == 0.f) p.scale_log2 = std::numeric_limits<float>::denorm_min();
   switch (p.D) {
     case 64: return launch_d<64>(p, bf16, stream);
     case 128: return launch_d<128>(p, bf16, stream);

@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
           for (int c = 0; c < kTreeTile; ++c)
             if (c >= valid) sr[c] = 0xff800000u;
         }
-        // tile maximum of the raw scores (scale >= 0 keeps the order)
+        // tile maximum of the raw scores (scale > 0 keeps the order, and -inf)
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int c = 0; c < kTreeTile; c += 2)
