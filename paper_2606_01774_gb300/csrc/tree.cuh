@@ -25,6 +25,11 @@ __device__ __forceinline__ bool warp_load_tree(const int32_t* __restrict__ paren
   return __all_sync(0xffffffffu, ok);
 }
 
+// A log-gate as it enters a path's sum.  From -104 down the gate is zero in fp32, and
+// a larger sum would only lose the digits of the other gates: weights along a path
+// are differences of two sums (-1e9 at a reset would leave none).  A NaN stays one.
+__device__ __forceinline__ float tree_log_gate(float g) { return g < -104.f ? -104.f : g; }
+
 // The paths of nodes lane and lane + 32 as bit sets (itself and its ancestors;
 // empty past n), by pointer doubling: after k rounds a set holds the 2^k
 // nearest members.  x0 and x1 become their sums over the paths.  The parents

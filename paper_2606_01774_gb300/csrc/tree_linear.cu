@@ -67,8 +67,8 @@ __global__ void __launch_bounds__(kParts * DV, NODES == 16 ? 256 / DV : DV == 64
   cp_async_commit();
   if (tid < 32) {
     const size_t g = (size_t)r * p.B * p.Hv + j;
-    float x0 = tid < n ? p.log_decay[g + (size_t)tid * p.Hv] : 0.f;
-    float x1 = tid + 32 < n ? p.log_decay[g + (size_t)(tid + 32) * p.Hv] : 0.f;
+    float x0 = tid < n ? tree_log_gate(p.log_decay[g + (size_t)tid * p.Hv]) : 0.f;
+    float x1 = tid + 32 < n ? tree_log_gate(p.log_decay[g + (size_t)(tid + 32) * p.Hv]) : 0.f;
     bet[tid] = tid < n ? p.beta[g + (size_t)tid * p.Hv] : 0.f;
     bet[tid + 32] = tid + 32 < n ? p.beta[g + (size_t)(tid + 32) * p.Hv] : 0.f;
     int p0, p1;

@@ -246,8 +246,9 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
       if (item >= 0) {
         const int r = item / p.Hv, j = item - r * p.Hv;
         const size_t g0 = (size_t)r * p.B * p.Hv + j;
-        float x0 = lane < n ? p.log_decay[g0 + (size_t)lane * p.Hv] : 0.f;
-        float x1 = lane + 32 < n ? p.log_decay[g0 + (size_t)(lane + 32) * p.Hv] : 0.f;
+        float x0 = lane < n ? tree_log_gate(p.log_decay[g0 + (size_t)lane * p.Hv]) : 0.f;
+        float x1 =
+            lane + 32 < n ? tree_log_gate(p.log_decay[g0 + (size_t)(lane + 32) * p.Hv]) : 0.f;
         const float b0 = lane < n ? p.beta[g0 + (size_t)lane * p.Hv] : 0.f;
         const float b1 = lane + 32 < n ? p.beta[g0 + (size_t)(lane + 32) * p.Hv] : 0.f;
         int p0, p1;
