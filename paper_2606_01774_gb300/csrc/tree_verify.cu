@@ -22,9 +22,14 @@
 // CTAs, which all take the same decisions from the same numbers and exchange
 // sums and maxima through distributed shared memory, in rank order.
 //
-// 64 sampled trees of 16 nodes over 32000 tokens: 21.9 us, half of it the row
+// 64 trees of 16 nodes over 32000 tokens: 22.1 us sampled, half of it the row
 // statistics (44 MB, 4 TB/s) and half the walk, which reads 18 MB more in two to
-// four dependent passes per request.  One greedy tree of 9 over 50257: 7.5 us.
+// four dependent passes per request; 23.2 us with fixed drafts, 18.7 greedy.  One
+// greedy tree of 9 over 50257: 7.6 us.
+//
+// Logits enter by their differences alone (to a row's maximum, or to the best
+// candidate so far): their products with the scale may overflow, at a type's lowest
+// value, or leave no digits for a difference, at a low temperature.
 #include "common.cuh"
 #include "kernels.h"
 #include "pdl.cuh"
@@ -209,6 +214,14 @@ __global__ void __launch_bounds__(kRowThreads) tree_rows_kernel(TreeVerifyParams
 }
 
 namespace {
+
+// p - c q of two tokens, p = 2^(scale (x - mx) - ls2).
+__device__ __forceinline__ void residual(float x0, float x1, float q0, float q1, float mx,
+                                         float ls2, float scale, float c, float& w0, float& w1) {
+  float p0, p1;
+  f2_split(f2_fma(f2_add(f2(x0, x1), f2_dup(-mx)), f2_dup(scale), f2_dup(-ls2)), p0, p1);
+  f2_split(f2_fma(f2(q0, q1), f2_dup(-c), f2(tc::ex2(p0), tc::ex2(p1))), w0, w1);
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t x;
@@ -435,8 +448,11 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
           qv[u] = t < hi ? q[t] : 0.f;
         }
 #pragma unroll
-        for (int u = 0; u < kIn; ++u)
-          sum += fmaxf(tc::ex2(fmaf(xv[u] - mx, scale, -ls2)) - c * qv[u], 0.f);
+        for (int u = 0; u < kIn; u += 2) {
+          float w0, w1;
+          residual(xv[u], xv[u + 1], qv[u], qv[u + 1], mx, ls2, scale, c, w0, w1);
+          sum += fmaxf(w0, 0.f) + fmaxf(w1, 0.f);
+        }
       }
     } else {
       const int ng = sh.n_gone;
@@ -508,9 +524,11 @@ __global__ void __launch_bounds__(kWalkThreads) tree_walk_kernel(TreeVerifyParam
           for (int u = 0; u < kIn; ++u) take(true, xv[u], t0 + u * kWalkThreads);
         } else if (q) {
 #pragma unroll
-          for (int u = 0; u < kIn; ++u) {
-            const float w = tc::ex2(fmaf(xv[u] - mx, scale, -ls2)) - c * qv[u];
-            take(w > 0.f, __fdividef(w, ev[u]), t0 + u * kWalkThreads);
+          for (int u = 0; u < kIn; u += 2) {
+            float w0, w1;
+            residual(xv[u], xv[u + 1], qv[u], qv[u + 1], mx, ls2, scale, c, w0, w1);
+            take(w0 > 0.f, __fdividef(w0, ev[u]), t0 + u * kWalkThreads);
+            take(w1 > 0.f, __fdividef(w1, ev[u + 1]), t0 + (u + 1) * kWalkThreads);
           }
         } else {  // in logarithms, against the best so far: no normaliser is needed
 #pragma unroll
