@@ -354,6 +354,8 @@ __global__ void __launch_bounds__(kTlThreads, TlCfg<BM>::kCtas)
           }
           if (q + C::kOps < kPieces) tc::mma_commit(&sh.op_free[q]);
           if (q == kPieces - 1) {
+            // G goes over the first pieces' operands: one thread's MMAs execute in
+            // issue order, whatever their shapes, so W^T has read them by then
 #pragma unroll
             for (int kk = 0; kk < kTlD / 16; ++kk) {
               const uint64_t kd =

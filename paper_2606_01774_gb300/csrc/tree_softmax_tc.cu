@@ -398,7 +398,8 @@ __global__ void __launch_bounds__(TreeCfg<D, NQ>::kThreads, 1)
       if constexpr (NQ == 2) {
         // MMAs of one thread execute in issue order, so an S buffer can be
         // rewritten once the product that reads its probabilities was issued:
-        // kSB scores ahead, then P V_j and S_j+kSB in turn.
+        // kSB scores ahead, then P V_j and S_j+kSB in turn.  No wait stands behind
+        // this, for products of two shapes; the calls' repetitions bit for bit do.
         for (int j = 0; j < kSB && j < n && ok; ++j) ok = issue_s(j);
         for (int j = 0; j < n && ok; ++j) {
           ok = issue_pv(j);
