@@ -32,6 +32,14 @@
  *   flare_tree_commit_state   recurrent state after the accepted path
  *   flare_tree_append_kv      the accepted path's rows into the paged caches
  *
+ * and what stands between these calls and the model's matrix products:
+ *
+ *   flare_rotary              queries and keys rotated to their positions, and back
+ *   flare_rotary_append_kv    the same, keys and values written to the paged cache
+ *   flare_tree_logits         penalties, biases and token masks on the logits
+ *   flare_block_norm, _bwd    the norm, gate and scaled residual after a block
+ *                             and the norm before the next one, with gradients
+ *
  * and, for training, the fused two-stream forward of a GDN layer:
  *
  *   flare_two_stream_fwd      noisy blocks seeded from the on-chip clean state
@@ -115,14 +123,45 @@ typedef enum flare_mask_mode {
 #define FLARE_DEV_BAD_LOGITS 0x80 /* a logits row that the result needs has a NaN, a +inf, or no
                                      finite entry */
 
+#define FLARE_DEV_BAD_HISTORY 0x100 /* history_len[r], output_start[r] or bias_len[r] out of range,
+                                       or a history or bias token outside the vocabulary */
+#define FLARE_DEV_BAD_PENALTY 0x200 /* repetition[r] not positive, normal and finite, or presence[r]
+                                       or frequency[r] not finite */
+
 /* How flare_tree_verify accepts drafted tokens. */
 typedef enum flare_verify_mode {
   FLARE_VERIFY_GREEDY = 0, /* a draft is accepted when it is the target's most likely token */
   FLARE_VERIFY_SAMPLE = 1  /* with probability min(1, p / q), against given uniforms */
 } flare_verify_mode;
 
-/* Activation applied after the ShortConv. */
-typedef enum flare_activation { FLARE_ACT_NONE = 0, FLARE_ACT_SILU = 1 } flare_activation;
+/* Activation applied after the ShortConv (NONE or SILU), or to the gate of flare_block_norm. */
+typedef enum flare_activation {
+  FLARE_ACT_NONE = 0,
+  FLARE_ACT_SILU = 1,   /* u / (1 + e^-u) */
+  FLARE_ACT_SIGMOID = 2 /* 1 / (1 + e^-u) */
+} flare_activation;
+
+/* Which elements of a head are rotated together: j and j + rotary_dim / 2, or 2j and 2j + 1. */
+typedef enum flare_rotary_layout {
+  FLARE_ROTARY_HALF = 0,
+  FLARE_ROTARY_INTERLEAVED = 1
+} flare_rotary_layout;
+
+/* Frequencies f_j of the pairs j < rotary_dim / 2, in radians a position, from
+ * base^(-2j / rotary_dim) (flare_rotary_table):
+ *   PLAIN     as they are
+ *   LINEAR    divided by `factor` (positions interpolated)
+ *   BASE      with base * factor^(rotary_dim / (rotary_dim - 2)) for the base
+ *   BY_PARTS  g f + (1 - g) f / factor: a pair that makes n = original_len f / 2 pi turns
+ *             over the original context keeps its frequency from high_turns turns on
+ *             (g = 1), is interpolated up to low_turns (g = 0), and in between
+ *             g = (n - low_turns) / (high_turns - low_turns) */
+typedef enum flare_rotary_scaling {
+  FLARE_ROTARY_PLAIN = 0,
+  FLARE_ROTARY_LINEAR = 1,
+  FLARE_ROTARY_BASE = 2,
+  FLARE_ROTARY_BY_PARTS = 3
+} flare_rotary_scaling;
 
 /* Gated-delta-rule layer shape.
  *   num_requests R, block_len B (1..64), num_qk_heads Hk, num_v_heads Hv
@@ -193,6 +232,87 @@ typedef struct flare_tree_verify_desc {
   flare_verify_mode mode;
   float inv_temperature;
 } flare_tree_verify_desc;
+
+/* Frequencies of a rotary table.
+ *   rotary_dim (a multiple of 16, 16..256), scaling as above, base (>= 1),
+ *   factor (> 0; not read in PLAIN), original_len (> 0) and 0 <= low_turns <
+ *   high_turns (read in BY_PARTS). */
+typedef struct flare_rotary_freq_desc {
+  int32_t rotary_dim;
+  flare_rotary_scaling scaling;
+  double base;
+  double factor;
+  double original_len;
+  double low_turns;
+  double high_turns;
+} flare_rotary_freq_desc;
+
+/* Shape of a rotation.
+ *   num_requests R; block_len B (>= 1, rows of a request when rows are padded)
+ *   or num_tokens T (rows in all when they are packed, see flare_rotary);
+ *   num_q_heads Hq, num_kv_heads Hkv, head_dim D (64, 128 or 256), rotary_dim
+ *   (a multiple of 16, 16..D: the first elements of each head; the others are
+ *   passed on), layout, inverse (1: by the negative angles, which is the
+ *   gradient of the rotation), act_dtype, amplitude (finite; multiplies the
+ *   rotated elements), q_stride, k_stride, v_stride (elements from one row of
+ *   the inputs to the next, 0 = Hq D or Hkv D; multiples of 16 bytes, so that
+ *   slices of a fused projection are read in place), and for the append
+ *   page_size (16, 32, 64 or 128), num_pages and max_pages_per_req. */
+typedef struct flare_rotary_desc {
+  int32_t num_requests;
+  int32_t block_len;
+  int32_t num_tokens;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t rotary_dim;
+  flare_rotary_layout layout;
+  int32_t inverse;
+  flare_dtype act_dtype;
+  float amplitude;
+  int64_t q_stride;
+  int64_t k_stride;
+  int64_t v_stride;
+  int32_t page_size;
+  int32_t num_pages;
+  int32_t max_pages_per_req;
+} flare_rotary_desc;
+
+/* Shape of flare_tree_logits.
+ *   num_requests R, num_nodes N (1..64), vocab_size V (1 .. 2^24),
+ *   logits_dtype, max_history H (columns of history, 0 .. 2^24), max_bias
+ *   (columns of the bias lists, 0 .. 65536). */
+typedef struct flare_tree_logits_desc {
+  int32_t num_requests;
+  int32_t num_nodes;
+  int32_t vocab_size;
+  flare_dtype logits_dtype;
+  int32_t max_history;
+  int32_t max_bias;
+} flare_tree_logits_desc;
+
+/* Shape of a block's norms.
+ *   num_tokens T, width W (a multiple of 8, 8..16384), group G of the norm after
+ *   the block (0 = W, or 64, 128 or 256 dividing W: a norm per head),
+ *   shared_weight (1: its weight has G entries for all groups, 0: W entries),
+ *   post_norm and pre_norm (0 or 1: whether there is a norm after the block and
+ *   before the next), gate_act, act_dtype, eps (> 0 and finite), residual_scale
+ *   (finite), x_stride and gate_stride (elements from one row to the next, 0 =
+ *   W; multiples of 16 bytes). */
+typedef struct flare_block_norm_desc {
+  int32_t num_tokens;
+  int32_t width;
+  int32_t group;
+  int32_t shared_weight;
+  int32_t post_norm;
+  int32_t pre_norm;
+  flare_activation gate_act;
+  flare_dtype act_dtype;
+  float eps;
+  float residual_scale;
+  int64_t x_stride;
+  int64_t gate_stride;
+} flare_block_norm_desc;
 
 /* Two-stream training layer shape (the noisy stream of a GDN layer).
  *   num_seqs N, seq_len L (a multiple of chunk_len), chunk_len C (64, the
@@ -622,6 +742,168 @@ flare_status flare_tree_append_kv(const flare_softmax_desc* desc, int32_t num_la
                                   const int32_t* page_table, const int32_t* prefix_len,
                                   const int32_t* path, const int32_t* path_len,
                                   int32_t* dev_status, void* stream);
+
+/*
+ * Between the matrix products and the attention, state and verification calls
+ * ---------------------------------------------------------------------------
+ */
+
+/*
+ * The frequencies of a rotation, once per model: table[j] is f_j / 2 pi, the
+ * fraction of a turn that pair j makes a position, as a 64-bit fixed-point
+ * number (2^64 times it rounded down, whole turns dropped).  The product with a
+ * position modulo 2^64 is then the angle without its whole turns: far positions
+ * lose no digits, only the table's own error (fp64's, below 2^-52 turns) grows
+ * with them.  A program may fill a table of its own.
+ *   table   [rotary_dim / 2] uint64 (device), 8-byte aligned
+ */
+flare_status flare_rotary_table(const flare_rotary_freq_desc* desc, uint64_t* table,
+                                void* stream);
+
+/*
+ * Rotary positions: in every head of a row at position m, pair (a, b) number j becomes
+ *     (amplitude (a cos m f_j - b sin m f_j), amplitude (b cos m f_j + a sin m f_j)),
+ * (with -m f_j when desc->inverse) and the elements from rotary_dim on are
+ * copied.  fp32 arithmetic, one rounding.
+ * Rows are padded or packed.  Padded (token_start = NULL): row r B + t is token
+ * t of request r, t < n = token_len[r] (B when token_len is NULL).  Packed:
+ * rows token_start[r] .. token_start[r+1]-1 are request r's (none may be);
+ * token_len and parent must be NULL.  Rows that are no request's token (t >= n,
+ * or from token_start[R] on) are neither used nor written.
+ * A row's position is position[row] if position is given, else prefix_len[r]
+ * (0 when NULL) + t, or + the depth of node t when the rows are drafted trees
+ * (parent given, padded rows with B <= 64; token_len is node_len).
+ *   q, k           [rows, Hq, D], [rows, Hkv, D] act_dtype, rows q_stride and
+ *                  k_stride apart; either may be NULL
+ *   table          [rotary_dim / 2] as flare_rotary_table fills it
+ *   position       [rows] int32, nullable
+ *   prefix_len, token_len [R] int32, nullable
+ *   parent         [R, B] int32, nullable
+ *   token_start    [R + 1] int32, not decreasing, within [0, T]; nullable
+ *   q_out, k_out   act_dtype, dense, or the input's own pointer: in place, with
+ *                  its stride (any other overlap with the input is rejected)
+ *   dev_status     FLARE_DEV_BAD_PREFIX_LEN (negative), FLARE_DEV_BAD_ACCEPT_LEN
+ *                  (token_len outside [0, B]), FLARE_DEV_BAD_TREE: the request is skipped;
+ *                  FLARE_DEV_BAD_ACCEPT_LEN also for a wrong token_start, whose rows
+ *                  may or may not be written.
+ */
+flare_status flare_rotary(const flare_rotary_desc* desc, const void* q, const void* k,
+                          const uint64_t* table, const int32_t* position,
+                          const int32_t* prefix_len, const int32_t* token_len,
+                          const int32_t* parent, const int32_t* token_start, void* q_out,
+                          void* k_out, int32_t* dev_status, void* stream);
+
+/*
+ * KV append with the rotation on the way: flare_rotary on q and k, and token t of
+ * request r enters the cache at prefix position prefix_len[r] + t (page table
+ * and pools as in flare_append_kv): its key as rotated, its value bit for bit.
+ * Whether the rows also go to k_out is the caller's choice (an attention call on the same tokens
+ * takes them as k_blk).  prefix_len is not updated; nothing else in the pools
+ * changes.  Precondition: no two tokens of the call share a cache position.
+ *   q (nullable), k, table, position, token_len, token_start, q_out: as above
+ *   v              [rows, Hkv, D] act_dtype, rows v_stride apart
+ *   prefix_len     [R] int32
+ *   page_table     [R, max_pages_per_req] int32
+ *   k_out          nullable
+ *   k_pool, v_pool [num_pages, Hkv, p, D] act_dtype, written in place
+ *   dev_status     as above; FLARE_DEV_BAD_PREFIX_LEN also for prefix_len[r] + n
+ *                  beyond the table (the request is skipped); FLARE_DEV_BAD_PAGE: the
+ *                  tokens of that page are skipped.
+ */
+flare_status flare_rotary_append_kv(const flare_rotary_desc* desc, const void* q, const void* k,
+                                    const void* v, const uint64_t* table,
+                                    const int32_t* position, const int32_t* prefix_len,
+                                    const int32_t* token_len, const int32_t* token_start,
+                                    const int32_t* page_table, void* q_out, void* k_out,
+                                    void* k_pool, void* v_pool, int32_t* dev_status,
+                                    void* stream);
+
+/*
+ * Penalties for repeated tokens, biases and token masks on the logits of a tree's
+ * nodes, ahead of flare_tree_verify.  Row i of request r is the target's output
+ * at node i, so its context is the request's history and the tokens of node i's
+ * path (all of them output).  With seen(x) whether token x is in the context, c(x)
+ * how often it is in the context's output (history from output_start[r] on, and
+ * the path), and b(x) the sum of the request's biases for x:
+ *     y = seen(x) ? (l > 0 ? l / repetition : l * repetition) : l
+ *     out = y - frequency c(x) - presence [c(x) > 0] + b(x)
+ * and -inf where the mask rules x out, whatever the logit is.  A row whose mask
+ * leaves nothing becomes -inf throughout.  fp32 arithmetic, one rounding.
+ * Rows of nodes from node_len[r] on are neither used nor written.  Ordinary
+ * decoding is N = 1.
+ *   logits       [R, N, V] logits_dtype (any V; rows need no alignment)
+ *   history      [R, H] int32, nullable (no history)
+ *   history_len  [R] int32 in [0, H] (needed with history)
+ *   output_start [R] int32 in [0, H], nullable (0: the whole history is output)
+ *   token        [R, N] int32, the nodes' tokens; nullable: paths add nothing
+ *   parent       [R, N] int32, the trees; read when token is given
+ *   node_len     [R] int32, nullable (N; needed with token)
+ *   repetition, presence, frequency [R] fp32, each nullable (1, 0, 0)
+ *   bias_token, bias_value [R, max_bias] int32 and fp32, bias_len [R] int32; all or none
+ *   mask         [R, N, ceil(V / 32)] uint32, bit x % 32 of word x / 32 set where token
+ *                x is allowed; nullable
+ *   out          as logits; the same pointer (in place: only what changes is
+ *                written) or one that does not overlap it
+ *   dev_status   FLARE_DEV_BAD_TREE | FLARE_DEV_BAD_HISTORY | FLARE_DEV_BAD_PENALTY (the request
+ *                is skipped)
+ */
+flare_status flare_tree_logits(const flare_tree_logits_desc* desc, const void* logits,
+                               const int32_t* history, const int32_t* history_len,
+                               const int32_t* output_start, const int32_t* token,
+                               const int32_t* parent, const int32_t* node_len,
+                               const float* repetition, const float* presence,
+                               const float* frequency, const int32_t* bias_token,
+                               const float* bias_value, const int32_t* bias_len,
+                               const uint32_t* mask, void* out, int32_t* dev_status,
+                               void* stream);
+
+/*
+ * The norm, gate and scaled residual after a block and the norm before the next
+ * one, row by row:
+ *     n = x / sqrt(mean_G x^2 + eps) * post_weight        (x itself without post_norm)
+ *     y = residual + residual_scale * n * act(gate)       (no residual: 0; no gate: 1)
+ *     h = y / sqrt(mean y^2 + eps) * pre_weight           (from y before it is rounded)
+ * With post_norm per head and a SiLU gate this is the output stage of a linear
+ * layer; with post_norm = 0 and no gate the residual and norm between two
+ * blocks.  fp32 arithmetic, one rounding per output; the squares' sums must be fp32
+ * numbers.
+ *   x            [T, W] act_dtype, rows x_stride apart
+ *   gate         [T, W] act_dtype, rows gate_stride apart; nullable
+ *   residual     [T, W] act_dtype, dense; nullable
+ *   post_weight  [W] or [G] fp32; nullable (1)
+ *   pre_weight   [W] fp32; nullable (1)
+ *   y            [T, W] act_dtype, dense, nullable; may be `residual` (in place) or a
+ *                dense x
+ *   h            [T, W] act_dtype, dense; with pre_norm only; may be a dense x
+ */
+flare_status flare_block_norm(const flare_block_norm_desc* desc, const void* x, const void* gate,
+                              const void* residual, const float* post_weight,
+                              const float* pre_weight, void* y, void* h, void* stream);
+
+/* Bytes of device workspace flare_block_norm_bwd needs (partial weight gradients).  Host-only. */
+flare_status flare_block_norm_bwd_workspace_size(const flare_block_norm_desc* desc,
+                                                 size_t* bytes);
+
+/*
+ * Gradients of flare_block_norm from the gradients of its outputs, its inputs
+ * read again and its statistics formed again.  Sums over rows are taken in a fixed
+ * order: the same call gives the same bits.
+ *   x, gate, residual, post_weight, pre_weight: as given to flare_block_norm
+ *   dy         [T, W] act_dtype, dense; nullable (no gradient arrives at y)
+ *   dh         [T, W] act_dtype, dense; with pre_norm only
+ *   dx         as x (same stride)
+ *   dgate      as gate (same stride); with a gate only
+ *   dresidual  [T, W] act_dtype, dense; nullable; may be dy (in place)
+ *   dpost_weight, dpre_weight  fp32 as the weights; nullable; written, not added to
+ *   workspace  >= flare_block_norm_bwd_workspace_size bytes, 256-byte aligned (may be
+ *              NULL when neither weight gradient is asked for)
+ */
+flare_status flare_block_norm_bwd(const flare_block_norm_desc* desc, const void* x,
+                                  const void* gate, const void* residual,
+                                  const float* post_weight, const float* pre_weight,
+                                  const void* dy, const void* dh, void* dx, void* dgate,
+                                  void* dresidual, float* dpost_weight, float* dpre_weight,
+                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /* Size of the library-owned scratch array used by flare_block_softmax_attn_noalloc. */
 #define FLARE_NOALLOC_SCRATCH_BYTES (64u * 1024u * 1024u)

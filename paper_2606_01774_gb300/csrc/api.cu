@@ -115,6 +115,153 @@ flare_status check_tree_verify(const flare_tree_verify_desc* d) {
   return FLARE_OK;
 }
 
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+
+// Whether the byte ranges of two arrays share a byte.
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + b_bytes && y < x + a_bytes;
+}
+
+size_t elem_bytes(flare_dtype d) { return d == FLARE_DT_BF16 ? 2 : 4; }
+
+// Bytes from the first row of an array to the end of its last.
+size_t span_bytes(int64_t rows, int64_t stride, int64_t width, size_t elem) {
+  return rows > 0 ? (size_t)((rows - 1) * stride + width) * elem : 0;
+}
+
+flare_status check_rotary(const flare_rotary_desc* d, bool packed, bool append) {
+  if (!d) return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_requests < 0 || (packed ? d->num_tokens < 0 : d->block_len < 1) ||
+      d->num_q_heads < 1 || d->num_kv_heads < 1 || !valid_dtype(d->act_dtype) ||
+      (d->layout != FLARE_ROTARY_HALF && d->layout != FLARE_ROTARY_INTERLEAVED) ||
+      (d->inverse != 0 && d->inverse != 1) ||
+      !(d->amplitude > -3.0e38f && d->amplitude < 3.0e38f))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256) return FLARE_ERR_UNSUPPORTED;
+  if (d->rotary_dim < 16 || d->rotary_dim > d->head_dim || d->rotary_dim % 16)
+    return FLARE_ERR_UNSUPPORTED;
+  if (d->num_q_heads > 65536 || d->num_kv_heads > 65536) return FLARE_ERR_UNSUPPORTED;
+  if (!packed && (int64_t)d->num_requests * d->block_len > INT32_MAX) return FLARE_ERR_UNSUPPORTED;
+  const int64_t strides[3] = {d->q_stride, d->k_stride, d->v_stride};
+  for (int i = 0; i < 3; ++i) {
+    const int64_t width = (int64_t)(i ? d->num_kv_heads : d->num_q_heads) * d->head_dim;
+    if (strides[i] && (strides[i] < width || strides[i] * elem_bytes(d->act_dtype) % 16))
+      return FLARE_ERR_INVALID_ARGUMENT;
+    if (strides[i] > ((int64_t)1 << 31)) return FLARE_ERR_UNSUPPORTED;
+  }
+  if (append) {
+    if (d->page_size < 1 || d->num_pages < 0 || d->max_pages_per_req < 0)
+      return FLARE_ERR_INVALID_ARGUMENT;
+    if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128)
+      return FLARE_ERR_UNSUPPORTED;
+    if ((int64_t)d->max_pages_per_req * d->page_size > (1 << 24)) return FLARE_ERR_UNSUPPORTED;
+  }
+  return FLARE_OK;
+}
+
+// The rotation of both calls; k_pool is null without an append.
+flare_status rotary(const flare_rotary_desc* d, const void* q, const void* k, const void* v,
+                    const uint64_t* table, const int32_t* position, const int32_t* prefix_len,
+                    const int32_t* token_len, const int32_t* parent, const int32_t* token_start,
+                    const int32_t* page_table, void* q_out, void* k_out, void* k_pool,
+                    void* v_pool, int32_t* dev_status, void* stream) {
+  const int64_t rows =
+      token_start ? d->num_tokens : (int64_t)d->num_requests * d->block_len;
+  RotaryParams p;
+  memset(&p, 0, sizeof p);
+  p.R = d->num_requests;
+  p.B = d->block_len;
+  p.rows = (int)rows;
+  p.Hq = d->num_q_heads;
+  p.Hkv = d->num_kv_heads;
+  p.D = d->head_dim;
+  p.rd = d->rotary_dim;
+  p.interleaved = d->layout == FLARE_ROTARY_INTERLEAVED;
+  p.inverse = d->inverse;
+  p.page_size = d->page_size;
+  p.num_pages = d->num_pages;
+  p.max_pages = d->max_pages_per_req;
+  p.amplitude = d->amplitude;
+  const int64_t q_width = (int64_t)p.Hq * p.D, k_width = (int64_t)p.Hkv * p.D;
+  p.q_stride = d->q_stride ? d->q_stride : q_width;
+  p.k_stride = d->k_stride ? d->k_stride : k_width;
+  p.v_stride = d->v_stride ? d->v_stride : k_width;
+  p.q_out_stride = q_out == q ? p.q_stride : q_width;
+  p.k_out_stride = k_out == k ? p.k_stride : k_width;
+  const size_t e = elem_bytes(d->act_dtype);
+  if ((q && q_out != q && overlap(q, span_bytes(rows, p.q_stride, q_width, e), q_out,
+                                  span_bytes(rows, q_width, q_width, e))) ||
+      (k && k_out && k_out != k && overlap(k, span_bytes(rows, p.k_stride, k_width, e), k_out,
+                                           span_bytes(rows, k_width, k_width, e))))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.table = table;
+  p.position = position;
+  p.prefix_len = prefix_len;
+  p.token_len = token_len;
+  p.parent = parent;
+  p.token_start = token_start;
+  p.page_table = page_table;
+  p.q_out = q_out;
+  p.k_out = k_out;
+  p.k_pool = k_pool;
+  p.v_pool = v_pool;
+  p.dev_status = dev_status;
+  const cudaError_t err = launch_rotary(p, d->act_dtype == FLARE_DT_BF16, device_sms(),
+                                        static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status check_block_norm(const flare_block_norm_desc* d) {
+  if (!d) return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_tokens < 0 || d->width < 1 || d->group < 0 || !valid_dtype(d->act_dtype) ||
+      (d->shared_weight != 0 && d->shared_weight != 1) ||
+      (d->post_norm != 0 && d->post_norm != 1) || (d->pre_norm != 0 && d->pre_norm != 1) ||
+      (d->gate_act != FLARE_ACT_NONE && d->gate_act != FLARE_ACT_SILU &&
+       d->gate_act != FLARE_ACT_SIGMOID) ||
+      !(d->eps > 0.f && d->eps < 3.0e38f) ||
+      !(d->residual_scale > -3.0e38f && d->residual_scale < 3.0e38f))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  const int64_t strides[2] = {d->x_stride, d->gate_stride};
+  for (int64_t s : strides) {
+    if (s && (s < d->width || s * elem_bytes(d->act_dtype) % 16)) return FLARE_ERR_INVALID_ARGUMENT;
+    if (s > ((int64_t)1 << 31)) return FLARE_ERR_UNSUPPORTED;
+  }
+  if (d->width % 8 || d->width > 16384) return FLARE_ERR_UNSUPPORTED;
+  if (d->group && d->group != d->width) {
+    if (d->group != 64 && d->group != 128 && d->group != 256) return FLARE_ERR_UNSUPPORTED;
+    if (d->width % d->group) return FLARE_ERR_INVALID_ARGUMENT;
+  }
+  return FLARE_OK;
+}
+
+BlockNormParams block_norm_params(const flare_block_norm_desc* d, const void* x, const void* gate,
+                                  const void* residual, const float* post_weight,
+                                  const float* pre_weight) {
+  BlockNormParams p;
+  memset(&p, 0, sizeof p);
+  p.T = d->num_tokens;
+  p.W = d->width;
+  p.G = d->group ? d->group : d->width;
+  p.shared = d->shared_weight;
+  p.post = d->post_norm;
+  p.pre = d->pre_norm;
+  p.act = d->gate_act;
+  p.eps = d->eps;
+  p.alpha = d->residual_scale;
+  p.x_stride = d->x_stride ? d->x_stride : d->width;
+  p.gate_stride = d->gate_stride ? d->gate_stride : d->width;
+  p.x = x;
+  p.gate = gate;
+  p.residual = residual;
+  p.wpost = d->post_norm ? post_weight : nullptr;
+  p.wpre = d->pre_norm ? pre_weight : nullptr;
+  return p;
+}
+
 // Bytes of row statistics, with the cut of a row into chunks.
 size_t tree_verify_workspace(const flare_tree_verify_desc* d, int* chunk, int* n_chunks) {
   plan_tree_verify(d->num_requests, d->num_nodes, d->vocab_size, device_sms(), chunk, n_chunks);
@@ -799,6 +946,179 @@ flare_status flare_tree_append_kv(const flare_softmax_desc* d, int32_t num_layer
   p.path_len = path_len;
   p.dev_status = dev_status;
   const cudaError_t e = launch_tree_append(p, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_rotary_table(const flare_rotary_freq_desc* d, uint64_t* table, void* stream) {
+  if (!d || !table || !aligned(table, 8)) return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->scaling != FLARE_ROTARY_PLAIN && d->scaling != FLARE_ROTARY_LINEAR &&
+      d->scaling != FLARE_ROTARY_BASE && d->scaling != FLARE_ROTARY_BY_PARTS)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (!(d->base >= 1.0 && d->base < 1e300) ||
+      (d->scaling != FLARE_ROTARY_PLAIN && !(d->factor > 0.0 && d->factor < 1e100)))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->scaling == FLARE_ROTARY_BY_PARTS &&
+      !(d->original_len > 0.0 && d->original_len < 1e100 && d->low_turns >= 0.0 &&
+        d->low_turns < d->high_turns && d->high_turns < 1e100))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->rotary_dim < 16 || d->rotary_dim > 256 || d->rotary_dim % 16) return FLARE_ERR_UNSUPPORTED;
+  const cudaError_t e = launch_rotary_table(*d, table, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_rotary(const flare_rotary_desc* d, const void* q, const void* k,
+                          const uint64_t* table, const int32_t* position,
+                          const int32_t* prefix_len, const int32_t* token_len,
+                          const int32_t* parent, const int32_t* token_start, void* q_out,
+                          void* k_out, int32_t* dev_status, void* stream) {
+  flare_status st = check_rotary(d, token_start != nullptr, false);
+  if (st != FLARE_OK) return st;
+  if ((!q && !k) || !q != !q_out || !k != !k_out || !table || !dev_status)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (token_start && (token_len || parent)) return FLARE_ERR_INVALID_ARGUMENT;
+  if (parent && d->block_len > kMaxTreeNodes) return FLARE_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) ||
+      !aligned(table, 8))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  return rotary(d, q, k, nullptr, table, position, prefix_len, token_len, parent, token_start,
+                nullptr, q_out, k_out, nullptr, nullptr, dev_status, stream);
+}
+
+flare_status flare_rotary_append_kv(const flare_rotary_desc* d, const void* q, const void* k,
+                                    const void* v, const uint64_t* table,
+                                    const int32_t* position, const int32_t* prefix_len,
+                                    const int32_t* token_len, const int32_t* token_start,
+                                    const int32_t* page_table, void* q_out, void* k_out,
+                                    void* k_pool, void* v_pool, int32_t* dev_status,
+                                    void* stream) {
+  flare_status st = check_rotary(d, token_start != nullptr, true);
+  if (st != FLARE_OK) return st;
+  if (!k || !v || !q != !q_out || !table || !prefix_len || !page_table || !k_pool || !v_pool ||
+      !dev_status)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (token_start && token_len) return FLARE_ERR_INVALID_ARGUMENT;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out) ||
+      !aligned16(k_pool) || !aligned16(v_pool) || !aligned(table, 8))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  return rotary(d, q, k, v, table, position, prefix_len, token_len, nullptr, token_start,
+                page_table, q_out, k_out, k_pool, v_pool, dev_status, stream);
+}
+
+flare_status flare_tree_logits(const flare_tree_logits_desc* d, const void* logits,
+                               const int32_t* history, const int32_t* history_len,
+                               const int32_t* output_start, const int32_t* token,
+                               const int32_t* parent, const int32_t* node_len,
+                               const float* repetition, const float* presence,
+                               const float* frequency, const int32_t* bias_token,
+                               const float* bias_value, const int32_t* bias_len,
+                               const uint32_t* mask, void* out, int32_t* dev_status,
+                               void* stream) {
+  if (!d) return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_requests < 0 || d->num_nodes < 1 || d->vocab_size < 1 || d->max_history < 0 ||
+      d->max_bias < 0 || !valid_dtype(d->logits_dtype))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (d->num_nodes > kMaxTreeNodes || d->vocab_size > (1 << 24) || d->max_history > (1 << 24) ||
+      d->max_bias > 65536)
+    return FLARE_ERR_UNSUPPORTED;
+  if (!logits || !out || !dev_status || (history && !history_len) ||
+      (token && (!parent || !node_len)) || !bias_token != !bias_value || !bias_token != !bias_len)
+    return FLARE_ERR_INVALID_ARGUMENT;
+  const size_t e = elem_bytes(d->logits_dtype);
+  const size_t bytes = (size_t)d->num_requests * d->num_nodes * d->vocab_size * e;
+  if (!aligned(logits, e) || !aligned(out, e) ||
+      (out != logits && overlap(logits, bytes, out, bytes)))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  TreeLogitsParams p;
+  memset(&p, 0, sizeof p);
+  p.R = d->num_requests;
+  p.N = d->num_nodes;
+  p.V = d->vocab_size;
+  p.H = d->max_history;
+  p.max_bias = d->max_bias;
+  p.logits = logits;
+  p.history = history;
+  p.history_len = history_len;
+  p.output_start = output_start;
+  p.token = token;
+  p.parent = parent;
+  p.node_len = node_len;
+  p.repetition = repetition;
+  p.presence = presence;
+  p.frequency = frequency;
+  p.bias_token = bias_token;
+  p.bias_value = bias_value;
+  p.bias_len = bias_len;
+  p.mask = mask;
+  p.out = out;
+  p.dev_status = dev_status;
+  const cudaError_t err = launch_tree_logits(p, d->logits_dtype == FLARE_DT_BF16, device_sms(),
+                                             static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? FLARE_OK
+                            : err == cudaErrorInvalidConfiguration ? FLARE_ERR_UNSUPPORTED
+                                                                   : FLARE_ERR_CUDA;
+}
+
+flare_status flare_block_norm(const flare_block_norm_desc* d, const void* x, const void* gate,
+                              const void* residual, const float* post_weight,
+                              const float* pre_weight, void* y, void* h, void* stream) {
+  flare_status st = check_block_norm(d);
+  if (st != FLARE_OK) return st;
+  if (!x || (!y && !h) || !h != !d->pre_norm) return FLARE_ERR_INVALID_ARGUMENT;
+  if (!aligned16(x) || !aligned16(gate) || !aligned16(residual) || !aligned16(post_weight) ||
+      !aligned16(pre_weight) || !aligned16(y) || !aligned16(h))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  BlockNormParams p = block_norm_params(d, x, gate, residual, post_weight, pre_weight);
+  if (y == h || ((y == x || h == x) && p.x_stride != p.W)) return FLARE_ERR_INVALID_ARGUMENT;
+  p.y = y;
+  p.h = h;
+  const cudaError_t e = launch_block_norm(p, d->act_dtype == FLARE_DT_BF16, device_sms(),
+                                          static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
+}
+
+flare_status flare_block_norm_bwd_workspace_size(const flare_block_norm_desc* d, size_t* bytes) {
+  flare_status st = check_block_norm(d);
+  if (st != FLARE_OK) return st;
+  if (!bytes) return FLARE_ERR_INVALID_ARGUMENT;
+  *bytes = (size_t)block_norm_bwd_ctas(d->num_tokens, d->width, d->act_dtype == FLARE_DT_BF16,
+                                       device_sms()) * 2 * d->width * sizeof(float);
+  return FLARE_OK;
+}
+
+flare_status flare_block_norm_bwd(const flare_block_norm_desc* d, const void* x,
+                                  const void* gate, const void* residual,
+                                  const float* post_weight, const float* pre_weight,
+                                  const void* dy, const void* dh, void* dx, void* dgate,
+                                  void* dresidual, float* dpost_weight, float* dpre_weight,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  flare_status st = check_block_norm(d);
+  if (st != FLARE_OK) return st;
+  if (!x || !dx || !gate != !dgate || (dresidual && !residual) || !dh != !d->pre_norm ||
+      (!dy && !dh) || (dpost_weight && !d->post_norm) || (dpre_weight && !d->pre_norm))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  if (!aligned16(x) || !aligned16(gate) || !aligned16(residual) || !aligned16(post_weight) ||
+      !aligned16(pre_weight) || !aligned16(dy) || !aligned16(dh) || !aligned16(dx) ||
+      !aligned16(dgate) || !aligned16(dresidual) || !aligned(dpost_weight, 4) ||
+      !aligned(dpre_weight, 4))
+    return FLARE_ERR_INVALID_ARGUMENT;
+  BlockNormParams p = block_norm_params(d, x, gate, residual, post_weight, pre_weight);
+  const bool weights = dpost_weight || dpre_weight;
+  if (weights) {
+    size_t need;
+    flare_block_norm_bwd_workspace_size(d, &need);
+    if (workspace_bytes < need || (need && !workspace) || !aligned(workspace, 256))
+      return FLARE_ERR_INVALID_ARGUMENT;
+  }
+  p.dy = dy;
+  p.dh = dh;
+  p.dx = dx;
+  p.dgate = dgate;
+  p.dres = dresidual;
+  p.dwpost = dpost_weight;
+  p.dwpre = dpre_weight;
+  p.part = weights ? static_cast<float*>(workspace) : nullptr;
+  const cudaError_t e = launch_block_norm_bwd(p, d->act_dtype == FLARE_DT_BF16, device_sms(),
+                                              static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? FLARE_OK : FLARE_ERR_CUDA;
 }
 

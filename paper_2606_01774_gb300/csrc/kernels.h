@@ -225,6 +225,84 @@ struct TreeAppendParams {
 };
 cudaError_t launch_tree_append(const TreeAppendParams& p, cudaStream_t stream);
 
+constexpr int kMaxTreeNodes = 64;
+
+// Rotation of queries and keys, with or without the append.  Rows r B + t when token_start is
+// null, else packed.
+struct RotaryParams {
+  int R, B, rows, Hq, Hkv, D, rd, interleaved, inverse;
+  int page_size, num_pages, max_pages;
+  float amplitude;
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;  // elements between rows
+  const void* q;               // nullptr: no queries
+  const void* k;               // nullptr: no keys
+  const void* v;               // append only
+  const uint64_t* table;       // [rd / 2] turns a position, 2^64 to a turn
+  const int32_t* position;     // [rows] or nullptr
+  const int32_t* prefix_len;   // [R] or nullptr
+  const int32_t* token_len;    // [R] or nullptr
+  const int32_t* parent;       // [R,B] or nullptr
+  const int32_t* token_start;  // [R+1] or nullptr
+  const int32_t* page_table;   // [R,max_pages], append only
+  void* q_out;
+  void* k_out;                 // may be nullptr in an append
+  void* k_pool;                // nullptr: no append
+  void* v_pool;
+  int32_t* dev_status;
+};
+cudaError_t launch_rotary_table(const flare_rotary_freq_desc& d, uint64_t* table,
+                                cudaStream_t stream);
+cudaError_t launch_rotary(const RotaryParams& p, bool bf16, int num_sms, cudaStream_t stream);
+
+struct TreeLogitsParams {
+  int R, N, V, H, max_bias;
+  const void* logits;           // [R,N,V]
+  const int32_t* history;       // [R,H] or nullptr
+  const int32_t* history_len;   // [R]
+  const int32_t* output_start;  // [R] or nullptr
+  const int32_t* token;         // [R,N] or nullptr
+  const int32_t* parent;        // [R,N], with token
+  const int32_t* node_len;      // [R] or nullptr
+  const float* repetition;      // [R] or nullptr, as the next two
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_token;    // [R,max_bias] or nullptr
+  const float* bias_value;
+  const int32_t* bias_len;      // [R]
+  const uint32_t* mask;         // [R,N,ceil(V/32)] or nullptr
+  void* out;
+  int32_t* dev_status;
+};
+cudaError_t launch_tree_logits(const TreeLogitsParams& p, bool bf16, int num_sms,
+                               cudaStream_t stream);
+
+struct BlockNormParams {
+  int T, W, G, shared, post, pre, act;
+  float eps, alpha;
+  int64_t x_stride, gate_stride;
+  const void* x;
+  const void* gate;      // or nullptr, as the next three
+  const void* residual;
+  const float* wpost;
+  const float* wpre;
+  void* y;               // forward: y, h
+  void* h;
+  const void* dy;        // backward
+  const void* dh;
+  void* dx;
+  void* dgate;
+  void* dres;
+  float* dwpost;
+  float* dwpre;
+  float* part;           // [CTAs][2][W] partial weight gradients
+};
+cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
+                              cudaStream_t stream);
+// CTAs of the backward pass: each leaves one partial weight gradient.
+int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms);
+cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
+                                  cudaStream_t stream);
+
 SoftmaxPlan plan_softmax(int R, int B, int Hq, int Hkv, int D, int page_size, int max_pages,
                          bool bf16, int num_sms);
 cudaError_t launch_softmax(const SoftmaxParams& p, const SoftmaxPlan& plan, bool bf16,

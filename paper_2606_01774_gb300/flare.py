@@ -34,6 +34,13 @@ FLARE_ROW_CAUSAL = 0
 FLARE_ROW_BIDIR = 1
 FLARE_ACT_NONE = 0
 FLARE_ACT_SILU = 1
+FLARE_ACT_SIGMOID = 2
+FLARE_ROTARY_HALF = 0
+FLARE_ROTARY_INTERLEAVED = 1
+FLARE_ROTARY_PLAIN = 0
+FLARE_ROTARY_LINEAR = 1
+FLARE_ROTARY_BASE = 2
+FLARE_ROTARY_BY_PARTS = 3
 
 FLARE_DEV_BAD_SLOT = 0x1
 FLARE_DEV_BAD_PAGE = 0x2
@@ -43,6 +50,8 @@ FLARE_DEV_WAIT_TIMEOUT = 0x10
 FLARE_DEV_BAD_VERIFY_LEN = 0x20
 FLARE_DEV_BAD_TREE = 0x40
 FLARE_DEV_BAD_LOGITS = 0x80
+FLARE_DEV_BAD_HISTORY = 0x100
+FLARE_DEV_BAD_PENALTY = 0x200
 
 FLARE_VERIFY_GREEDY = 0
 FLARE_VERIFY_SAMPLE = 1
@@ -84,6 +93,40 @@ class flare_tree_verify_desc(ctypes.Structure):
                 ("mode", ctypes.c_int), ("inv_temperature", ctypes.c_float)]
 
 
+class flare_rotary_freq_desc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("low_turns", ctypes.c_double),
+                ("high_turns", ctypes.c_double)]
+
+
+class flare_rotary_desc(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("block_len", ctypes.c_int32),
+                ("num_tokens", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int),
+                ("inverse", ctypes.c_int32), ("act_dtype", ctypes.c_int),
+                ("amplitude", ctypes.c_float), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("max_pages_per_req", ctypes.c_int32)]
+
+
+class flare_tree_logits_desc(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("num_nodes", ctypes.c_int32),
+                ("vocab_size", ctypes.c_int32), ("logits_dtype", ctypes.c_int),
+                ("max_history", ctypes.c_int32), ("max_bias", ctypes.c_int32)]
+
+
+class flare_block_norm_desc(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("group", ctypes.c_int32), ("shared_weight", ctypes.c_int32),
+                ("post_norm", ctypes.c_int32), ("pre_norm", ctypes.c_int32),
+                ("gate_act", ctypes.c_int), ("act_dtype", ctypes.c_int),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float),
+                ("x_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64)]
+
+
 class flare_softmax_desc(ctypes.Structure):
     _fields_ = [("num_requests", ctypes.c_int32), ("block_len", ctypes.c_int32),
                 ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
@@ -110,6 +153,10 @@ def load() -> ctypes.CDLL:
     cnv = ctypes.POINTER(flare_conv_desc)
     tsd = ctypes.POINTER(flare_two_stream_desc)
     tvd = ctypes.POINTER(flare_tree_verify_desc)
+    frq = ctypes.POINTER(flare_rotary_freq_desc)
+    rot = ctypes.POINTER(flare_rotary_desc)
+    tld = ctypes.POINTER(flare_tree_logits_desc)
+    bnd = ctypes.POINTER(flare_block_norm_desc)
     sigs = {
         "flare_short_conv": [cnv] + [P] * 9,
         "flare_two_stream_fwd": [tsd] + [P] * 13,
@@ -128,6 +175,13 @@ def load() -> ctypes.CDLL:
         "flare_tree_verify": [tvd] + [P] * 12 + [S, P, P],
         "flare_tree_commit_state": [lin] + [P] * 11,
         "flare_tree_append_kv": [smx, I32] + [P] * 10,
+        "flare_rotary_table": [frq, P, P],
+        "flare_rotary": [rot] + [P] * 12,
+        "flare_rotary_append_kv": [rot] + [P] * 15,
+        "flare_tree_logits": [tld] + [P] * 17,
+        "flare_block_norm": [bnd] + [P] * 8,
+        "flare_block_norm_bwd_workspace_size": [bnd, ctypes.POINTER(S)],
+        "flare_block_norm_bwd": [bnd] + [P] * 13 + [S, P],
         "flare_debug_gather_prefix": [smx, P, P, P, P, I32, P, P, P, P],
         "flare_debug_wait_timeout": [P, ctypes.c_uint64, P],
         "flare_read_status": [P, P, ctypes.POINTER(I32)],
@@ -347,6 +401,124 @@ def flare_tree_append_kv(desc, k_blk, v_blk, k_pool, v_pool, page_table, prefix_
         _c(prefix_len), _c(path), _c(path_len), _c(dev_status), _stream(stream))
 
 
+def _device():
+    """Index of the current device."""
+    global _device
+    from torch import _C
+
+    _device = _C._cuda_getDevice
+    return _device()
+
+
+def _d(t, device):
+    """Data pointer of a contiguous tensor on the current device."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError("tensors must be on the current device")
+    if not t.is_contiguous():
+        raise ValueError("only the rows of q, k, v, x, gate and their gradients may be strided")
+    return t.data_ptr()
+
+
+def _rows(t, step, inner, device):
+    """Data pointer of rows `step` elements apart (0: dense), a row's elements contiguous.
+
+    The rows are all leading dimensions but the last `inner`."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError("tensors must be on the current device")
+    if step and t.dim() == inner + 1 and t.stride(0) == step and (
+            t.stride(-1) == 1 and (inner == 1 or t.stride(-2) == t.shape[-1])):
+        return t.data_ptr()
+    dense = 1
+    for i in range(t.dim() - 1, -1, -1):
+        if i == t.dim() - inner - 1:
+            dense = step or dense
+        if t.shape[i] > 1 and t.stride(i) != dense:
+            raise ValueError("strides other than the descriptor's")
+        dense *= t.shape[i]
+    return t.data_ptr()
+
+
+def flare_rotary_table(desc, table, stream=None) -> int:
+    return load().flare_rotary_table(ctypes.byref(desc), _d(table, _device()), _stream(stream))
+
+
+def flare_rotary(desc, q, k, table, position, prefix_len, token_len, parent, token_start, q_out,
+                 k_out, dev_status, stream=None) -> int:
+    """q, k (and the outputs written in place) have rows q_stride and k_stride apart."""
+    dev = _device()
+    qs, ks = desc.q_stride, desc.k_stride
+    return load().flare_rotary(
+        ctypes.byref(desc), _rows(q, qs, 2, dev), _rows(k, ks, 2, dev), _d(table, dev),
+        _d(position, dev), _d(prefix_len, dev), _d(token_len, dev), _d(parent, dev),
+        _d(token_start, dev), _out_rows(q_out, q, qs, dev), _out_rows(k_out, k, ks, dev),
+        _d(dev_status, dev), _stream(stream))
+
+
+def _out_rows(out, source, step, device):
+    """An output is dense, or its input's own rows."""
+    if out is not None and source is not None and out.data_ptr() == source.data_ptr():
+        return _rows(out, step, 2, device)
+    return _d(out, device)
+
+
+def flare_rotary_append_kv(desc, q, k, v, table, position, prefix_len, token_len, token_start,
+                           page_table, q_out, k_out, k_pool, v_pool, dev_status,
+                           stream=None) -> int:
+    dev = _device()
+    qs, ks = desc.q_stride, desc.k_stride
+    return load().flare_rotary_append_kv(
+        ctypes.byref(desc), _rows(q, qs, 2, dev), _rows(k, ks, 2, dev),
+        _rows(v, desc.v_stride, 2, dev), _d(table, dev), _d(position, dev), _d(prefix_len, dev),
+        _d(token_len, dev), _d(token_start, dev), _d(page_table, dev),
+        _out_rows(q_out, q, qs, dev), _out_rows(k_out, k, ks, dev), _d(k_pool, dev),
+        _d(v_pool, dev), _d(dev_status, dev), _stream(stream))
+
+
+def flare_tree_logits(desc, logits, history, history_len, output_start, token, parent, node_len,
+                      repetition, presence, frequency, bias_token, bias_value, bias_len, mask,
+                      out, dev_status, stream=None) -> int:
+    dev = _device()
+    return load().flare_tree_logits(
+        ctypes.byref(desc), _d(logits, dev), _d(history, dev), _d(history_len, dev),
+        _d(output_start, dev), _d(token, dev), _d(parent, dev), _d(node_len, dev),
+        _d(repetition, dev), _d(presence, dev), _d(frequency, dev), _d(bias_token, dev),
+        _d(bias_value, dev), _d(bias_len, dev), _d(mask, dev), _d(out, dev), _d(dev_status, dev),
+        _stream(stream))
+
+
+def flare_block_norm(desc, x, gate, residual, post_weight, pre_weight, y, h, stream=None) -> int:
+    dev = _device()
+    return load().flare_block_norm(
+        ctypes.byref(desc), _rows(x, desc.x_stride, 1, dev), _rows(gate, desc.gate_stride, 1, dev),
+        _d(residual, dev), _d(post_weight, dev), _d(pre_weight, dev), _d(y, dev), _d(h, dev),
+        _stream(stream))
+
+
+def flare_block_norm_bwd_workspace_size(desc) -> int:
+    n = ctypes.c_size_t(0)
+    check(load().flare_block_norm_bwd_workspace_size(ctypes.byref(desc), ctypes.byref(n)),
+          "flare_block_norm_bwd_workspace_size")
+    return int(n.value)
+
+
+def flare_block_norm_bwd(desc, x, gate, residual, post_weight, pre_weight, dy, dh, dx, dgate,
+                         dresidual, dpost_weight, dpre_weight, workspace, workspace_bytes,
+                         stream=None) -> int:
+    """dx and dgate have their inputs' strides."""
+    dev = _device()
+    xs, gs = desc.x_stride, desc.gate_stride
+    return load().flare_block_norm_bwd(
+        ctypes.byref(desc), _rows(x, xs, 1, dev), _rows(gate, gs, 1, dev), _d(residual, dev),
+        _d(post_weight, dev), _d(pre_weight, dev), _d(dy, dev), _d(dh, dev),
+        _rows(dx, xs, 1, dev), _rows(dgate, gs, 1, dev), _d(dresidual, dev),
+        _d(dpost_weight, dev), _d(dpre_weight, dev), _d(workspace, dev), int(workspace_bytes),
+        _stream(stream))
+
+
 def flare_debug_gather_prefix(desc, k_pool, v_pool, page_table, prefix_len, request, k_out,
                               v_out, dev_status, stream=None) -> int:
     return load().flare_debug_gather_prefix(
@@ -390,6 +562,35 @@ def tree_verify_desc(num_requests, num_nodes, vocab_size, logits_dtype,
                      mode=FLARE_VERIFY_SAMPLE, inv_temperature=1.0) -> flare_tree_verify_desc:
     return flare_tree_verify_desc(num_requests, num_nodes, vocab_size, logits_dtype, mode,
                                   inv_temperature)
+
+
+def rotary_freq_desc(rotary_dim, base=10000.0, scaling=FLARE_ROTARY_PLAIN, factor=1.0,
+                     original_len=0.0, low_turns=1.0, high_turns=32.0) -> flare_rotary_freq_desc:
+    return flare_rotary_freq_desc(rotary_dim, scaling, base, factor, original_len, low_turns,
+                                  high_turns)
+
+
+def rotary_desc(num_requests, block_len, num_tokens, num_q_heads, num_kv_heads, head_dim,
+                rotary_dim, act_dtype, layout=FLARE_ROTARY_HALF, inverse=0, amplitude=1.0,
+                q_stride=0, k_stride=0, v_stride=0, page_size=0, num_pages=0,
+                max_pages_per_req=0) -> flare_rotary_desc:
+    """Padded rows read block_len, packed ones num_tokens; the page fields are the append's."""
+    return flare_rotary_desc(num_requests, block_len, num_tokens, num_q_heads, num_kv_heads,
+                             head_dim, rotary_dim, layout, inverse, act_dtype, amplitude, q_stride,
+                             k_stride, v_stride, page_size, num_pages, max_pages_per_req)
+
+
+def tree_logits_desc(num_requests, num_nodes, vocab_size, logits_dtype, max_history=0,
+                     max_bias=0) -> flare_tree_logits_desc:
+    return flare_tree_logits_desc(num_requests, num_nodes, vocab_size, logits_dtype, max_history,
+                                  max_bias)
+
+
+def block_norm_desc(num_tokens, width, act_dtype, group=0, shared_weight=0, post_norm=1,
+                    pre_norm=1, gate_act=FLARE_ACT_NONE, eps=1e-6, residual_scale=1.0, x_stride=0,
+                    gate_stride=0) -> flare_block_norm_desc:
+    return flare_block_norm_desc(num_tokens, width, group, shared_weight, post_norm, pre_norm,
+                                 gate_act, act_dtype, eps, residual_scale, x_stride, gate_stride)
 
 
 def softmax_desc(num_requests, block_len, num_q_heads, num_kv_heads, head_dim, page_size,
