@@ -746,6 +746,7 @@ flare_status flare_tree_append_kv(const flare_softmax_desc* desc, int32_t num_la
 /*
  * Between the matrix products and the attention, state and verification calls
  * ---------------------------------------------------------------------------
+ * Arrays of no rows may be null pointers.
  */
 
 /*

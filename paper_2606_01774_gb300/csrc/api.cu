@@ -160,6 +160,10 @@ flare_status check_rotary(const flare_rotary_desc* d, bool packed, bool append) 
   return FLARE_OK;
 }
 
+bool no_rows(const flare_rotary_desc* d, bool packed) {
+  return d->num_requests == 0 || (packed && d->num_tokens == 0);
+}
+
 // The rotation of both calls; k_pool is null without an append.
 flare_status rotary(const flare_rotary_desc* d, const void* q, const void* k, const void* v,
                     const uint64_t* table, const int32_t* position, const int32_t* prefix_len,
@@ -972,7 +976,7 @@ flare_status flare_rotary(const flare_rotary_desc* d, const void* q, const void*
                           const int32_t* parent, const int32_t* token_start, void* q_out,
                           void* k_out, int32_t* dev_status, void* stream) {
   flare_status st = check_rotary(d, token_start != nullptr, false);
-  if (st != FLARE_OK) return st;
+  if (st != FLARE_OK || no_rows(d, token_start != nullptr)) return st;
   if ((!q && !k) || !q != !q_out || !k != !k_out || !table || !dev_status)
     return FLARE_ERR_INVALID_ARGUMENT;
   if (token_start && (token_len || parent)) return FLARE_ERR_INVALID_ARGUMENT;
@@ -992,7 +996,7 @@ flare_status flare_rotary_append_kv(const flare_rotary_desc* d, const void* q, c
                                     void* k_pool, void* v_pool, int32_t* dev_status,
                                     void* stream) {
   flare_status st = check_rotary(d, token_start != nullptr, true);
-  if (st != FLARE_OK) return st;
+  if (st != FLARE_OK || no_rows(d, token_start != nullptr)) return st;
   if (!k || !v || !q != !q_out || !table || !prefix_len || !page_table || !k_pool || !v_pool ||
       !dev_status)
     return FLARE_ERR_INVALID_ARGUMENT;
@@ -1020,6 +1024,7 @@ flare_status flare_tree_logits(const flare_tree_logits_desc* d, const void* logi
   if (d->num_nodes > kMaxTreeNodes || d->vocab_size > (1 << 24) || d->max_history > (1 << 24) ||
       d->max_bias > 65536)
     return FLARE_ERR_UNSUPPORTED;
+  if (d->num_requests == 0) return FLARE_OK;
   if (!logits || !out || !dev_status || (history && !history_len) ||
       (token && (!parent || !node_len)) || !bias_token != !bias_value || !bias_token != !bias_len)
     return FLARE_ERR_INVALID_ARGUMENT;
@@ -1062,7 +1067,7 @@ flare_status flare_block_norm(const flare_block_norm_desc* d, const void* x, con
                               const void* residual, const float* post_weight,
                               const float* pre_weight, void* y, void* h, void* stream) {
   flare_status st = check_block_norm(d);
-  if (st != FLARE_OK) return st;
+  if (st != FLARE_OK || d->num_tokens == 0) return st;
   if (!x || (!y && !h) || !h != !d->pre_norm) return FLARE_ERR_INVALID_ARGUMENT;
   if (!aligned16(x) || !aligned16(gate) || !aligned16(residual) || !aligned16(post_weight) ||
       !aligned16(pre_weight) || !aligned16(y) || !aligned16(h))
@@ -1093,8 +1098,10 @@ flare_status flare_block_norm_bwd(const flare_block_norm_desc* d, const void* x,
                                   void* workspace, size_t workspace_bytes, void* stream) {
   flare_status st = check_block_norm(d);
   if (st != FLARE_OK) return st;
-  if (!x || !dx || !gate != !dgate || (dresidual && !residual) || !dh != !d->pre_norm ||
-      (!dy && !dh) || (dpost_weight && !d->post_norm) || (dpre_weight && !d->pre_norm))
+  if ((dpost_weight && !d->post_norm) || (dpre_weight && !d->pre_norm) ||
+      (d->num_tokens > 0 &&
+       (!x || !dx || !gate != !dgate || (dresidual && !residual) || !dh != !d->pre_norm ||
+        (!dy && !dh))))
     return FLARE_ERR_INVALID_ARGUMENT;
   if (!aligned16(x) || !aligned16(gate) || !aligned16(residual) || !aligned16(post_weight) ||
       !aligned16(pre_weight) || !aligned16(dy) || !aligned16(dh) || !aligned16(dx) ||

@@ -74,7 +74,7 @@ __device__ __forceinline__ float act(int kind, float z, float& slope) {
     slope = 1.f;
     return z;
   }
-  const float a = 1.f / (1.f + __expf(-z));
+  const float a = 1.f / (1.f + expf(-z));
   if (kind == FLARE_ACT_SIGMOID) {
     slope = a * (1.f - a);
     return a;
@@ -403,12 +403,14 @@ int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms) {
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
                                   cudaStream_t stream) {
   const int ctas = block_norm_bwd_ctas(p.T, p.W, bf16, num_sms);
+  const bool weights = p.dwpost || p.dwpre;
+  if (ctas == 0 && !weights) return cudaSuccess;
   if (ctas > 0) {
     if (bf16) run<__nv_bfloat16>(p, true, ctas, stream);
     else run<float>(p, true, ctas, stream);
     note_launches(1);
   }
-  if (p.part) {
+  if (weights) {  // of no rows: zeros
     block_norm_weights_kernel<<<dim3((unsigned)(p.W + 31) / 32, 2), 256, 0, stream>>>(p, ctas);
     note_launches(1);
   }
