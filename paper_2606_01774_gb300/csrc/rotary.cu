@@ -102,22 +102,25 @@ __device__ __forceinline__ bool resolve(const RotaryParams& p, int64_t row, int6
 
 }  // namespace
 
-// Units of a row: heads x (D / 2 Piece::N), the queries', then the keys', then the values'.
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
-    rotary_kernel(const __grid_constant__ RotaryParams p, int tile, int log2_units, int heads) {
+// A head is units of 32 bytes, D / 2N of them (N elements to a piece).  A thread has one unit number
+// of every head_slots'th head of a row, so its cosines and sines stay in registers
+// from the first head to the last; 256 threads take 256 / (units head_slots) rows at a time.
+template <typename T, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads, 3)
+    rotary_kernel(const __grid_constant__ RotaryParams p, int tile, int log2_units,
+                  int log2_slots) {
   constexpr int N = Piece<T>::N;
-  extern __shared__ char smem[];
-  float2* turn = reinterpret_cast<float2*>(smem);  // [tile][rd / 2]
-  int64_t* pos = reinterpret_cast<int64_t*>(turn + tile * (p.rd / 2));
+  extern __shared__ __align__(16) char smem[];
+  const int pairs = p.rd / 2, turning = p.rd / (2 * N);
+  // [tile][N / 2][turning] {cos, sin, cos, sin}: a unit's pairs two by two, neighbouring units
+  // next to each other
+  float4* turn = reinterpret_cast<float4*>(smem);
+  int64_t* pos = reinterpret_cast<int64_t*>(turn + tile * (pairs / 2));
   int64_t* slot = pos + tile;
   int* live = reinterpret_cast<int*>(slot + tile);
   const int tid = threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * tile;
   const int rows = (int)min((int64_t)tile, p.rows - row0);
-  const int units = 1 << log2_units, u = tid & (units - 1);
-  const int n_q = p.q ? p.Hq : 0, n_k = p.k ? p.Hkv : 0;
-  const int pairs = p.rd / 2, turning = p.rd / (2 * N);
 
   if (blockIdx.x == 0 && p.token_start) {
     int bad = 0;
@@ -129,77 +132,84 @@ __global__ void __launch_bounds__(kThreads)
   if (tid < rows) live[tid] = resolve(p, row0 + tid, pos[tid], slot[tid]);
   __syncthreads();
   for (int i = tid; i < rows * pairs; i += kThreads) {
-    const int t = i / pairs;
+    const int t = i / pairs, j = i - t * pairs, unit = j / N, e = j - unit * N;
     if (live[t]) {
-      float2 cs = cos_sin((uint64_t)pos[t] * p.table[i - t * pairs]);
+      float2 cs = cos_sin((uint64_t)pos[t] * p.table[j]);
       cs.x *= p.amplitude;
       cs.y *= p.inverse ? -p.amplitude : p.amplitude;
-      turn[i] = cs;
+      reinterpret_cast<float2*>(turn + (t * (N / 2) + e / 2) * turning + unit)[e & 1] = cs;
     }
   }
   __syncthreads();
 
-  // this thread's pieces of a head, in elements, and its pairs
+  const int u = tid & ((1 << log2_units) - 1), row_threads = log2_units + log2_slots;
+  const int first = (tid >> log2_units) & ((1 << log2_slots) - 1), slots = 1 << log2_slots;
+  const int n_q = p.q ? p.Hq : 0, n_k = n_q + (p.k ? p.Hkv : 0);
+  const int heads = n_k + (p.k_pool ? p.Hkv : 0);
+  // this thread's pieces of a head, in elements
   const bool turns = u < turning;
-  const int e0 = !turns || p.interleaved ? 2 * N * u : N * u;
-  const int e1 = turns && !p.interleaved ? p.rd / 2 + N * u : e0 + N;
-  const int step = kThreads >> log2_units;
-  const int total = rows * heads;
-  for (int i0 = tid >> log2_units; i0 < total; i0 += step * kUnroll) {
-    uint4 a[kUnroll], b[kUnroll];
-    int t[kUnroll], h[kUnroll];
+  const int e0 = !turns || INTERLEAVED ? 2 * N * u : N * u;
+  const int e1 = turns && !INTERLEAVED ? pairs + N * u : e0 + N;
+  for (int t = tid >> row_threads; t < rows; t += kThreads >> row_threads) {
+    if (!live[t]) continue;
+    float c[N], s[N];
+    if (turns) {
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      const int i = i0 + j * step;
-      t[j] = i / heads;
-      h[j] = i - t[j] * heads;
-      if (i >= total || !live[t[j]]) {
-        t[j] = -1;
-        continue;
+      for (int k = 0; k < N / 2; ++k) {
+        const float4 f = turn[(t * (N / 2) + k) * turning + u];
+        c[2 * k] = f.x, s[2 * k] = f.y, c[2 * k + 1] = f.z, s[2 * k + 1] = f.w;
       }
-      const int64_t row = row0 + t[j];
-      const T* src;
-      if (h[j] < n_q) src = static_cast<const T*>(p.q) + row * p.q_stride + h[j] * p.D;
-      else if (h[j] < n_q + n_k)
-        src = static_cast<const T*>(p.k) + row * p.k_stride + (h[j] - n_q) * p.D;
-      else src = static_cast<const T*>(p.v) + row * p.v_stride + (h[j] - n_q - n_k) * p.D;
-      a[j] = *reinterpret_cast<const uint4*>(src + e0);
-      b[j] = *reinterpret_cast<const uint4*>(src + e1);
     }
+    const int64_t row = row0 + t;
+    const T* q = static_cast<const T*>(p.q) + row * p.q_stride;
+    const T* k = static_cast<const T*>(p.k) + row * p.k_stride - n_q * p.D;
+    const T* v = static_cast<const T*>(p.v) + row * p.v_stride - n_k * p.D;
+    T* q_out = static_cast<T*>(p.q_out) + row * p.q_out_stride;
+    T* k_out = static_cast<T*>(p.k_out) + row * p.k_out_stride - n_q * p.D;
+    const int64_t pool_head = (int64_t)p.page_size * p.D;
+    for (int h0 = first; h0 < heads; h0 += slots * kUnroll) {
+      uint4 a[kUnroll], b[kUnroll];
 #pragma unroll
-    for (int j = 0; j < kUnroll; ++j) {
-      if (t[j] < 0) continue;
-      const int64_t row = row0 + t[j];
-      if (turns && h[j] < n_q + n_k) {
-        float x[2 * N];
-        Piece<T>::load(a[j], x);
-        Piece<T>::load(b[j], x + N);
-        const float2* cs = turn + t[j] * pairs + N * u;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float2 c = cs[e];
-          float& lo = p.interleaved ? x[2 * e] : x[e];
-          float& hi = p.interleaved ? x[2 * e + 1] : x[N + e];
-          const float y = lo * c.x - hi * c.y;
-          hi = hi * c.x + lo * c.y;
-          lo = y;
+      for (int j = 0; j < kUnroll; ++j) {
+        const int h = h0 + j * slots;
+        if (h < heads) {
+          const T* src = (h < n_q ? q : h < n_k ? k : v) + h * p.D;
+          a[j] = *reinterpret_cast<const uint4*>(src + e0);
+          b[j] = *reinterpret_cast<const uint4*>(src + e1);
         }
-        a[j] = Piece<T>::store(x);
-        b[j] = Piece<T>::store(x + N);
       }
-      const auto put = [&](void* to, int64_t at) {
-        T* dst = static_cast<T*>(to) + at;
-        *reinterpret_cast<uint4*>(dst + e0) = a[j];
-        *reinterpret_cast<uint4*>(dst + e1) = b[j];
-      };
-      if (h[j] < n_q) {
-        put(p.q_out, row * p.q_out_stride + h[j] * p.D);
-      } else if (h[j] < n_q + n_k) {
-        const int hk = h[j] - n_q;
-        if (p.k_out) put(p.k_out, row * p.k_out_stride + hk * p.D);
-        if (p.k_pool) put(p.k_pool, (slot[t[j]] + (int64_t)hk * p.page_size) * p.D);
-      } else {
-        put(p.v_pool, (slot[t[j]] + (int64_t)(h[j] - n_q - n_k) * p.page_size) * p.D);
+#pragma unroll
+      for (int j = 0; j < kUnroll; ++j) {
+        const int h = h0 + j * slots;
+        if (h >= heads) continue;
+        if (turns && h < n_k) {
+          float x[2 * N];
+          Piece<T>::load(a[j], x);
+          Piece<T>::load(b[j], x + N);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            float& lo = x[INTERLEAVED ? 2 * e : e];
+            float& hi = x[INTERLEAVED ? 2 * e + 1 : N + e];
+            const float y = lo * c[e] - hi * s[e];
+            hi = hi * c[e] + lo * s[e];
+            lo = y;
+          }
+          a[j] = Piece<T>::store(x);
+          b[j] = Piece<T>::store(x + N);
+        }
+        const auto put = [&](T* dst) {
+          *reinterpret_cast<uint4*>(dst + e0) = a[j];
+          *reinterpret_cast<uint4*>(dst + e1) = b[j];
+        };
+        if (h < n_q) {
+          put(q_out + h * p.D);
+        } else if (h < n_k) {
+          if (p.k_out) put(k_out + h * p.D);
+          if (p.k_pool)
+            put(static_cast<T*>(p.k_pool) + slot[t] * p.D + (h - n_q) * pool_head);
+        } else {
+          put(static_cast<T*>(p.v_pool) + slot[t] * p.D + (h - n_k) * pool_head);
+        }
       }
     }
   }
@@ -238,10 +248,18 @@ static cudaError_t launch(const RotaryParams& p, int num_sms, cudaStream_t strea
   const int heads = (p.q ? p.Hq : 0) + (p.k ? p.Hkv : 0) + (p.k_pool ? p.Hkv : 0);
   int tile = 16;
   while (tile > 1 && (p.rows + tile - 1) / tile < 2 * num_sms) tile /= 2;
-  const int smem = tile * (p.rd / 2 * (int)sizeof(float2) + 2 * (int)sizeof(int64_t) +
+  // as many rows at a time as the tile has, or four heads in flight per thread
+  int log2_slots = 0;
+  while (log2_units + log2_slots < 8 && (tile << (log2_units + log2_slots) < kThreads ||
+                                         heads >> log2_slots > kUnroll))
+    ++log2_slots;
+  const int smem = tile * (p.rd / 4 * (int)sizeof(float4) + 2 * (int)sizeof(int64_t) +
                            (int)sizeof(int));
   const unsigned grid = (unsigned)((p.rows + tile - 1) / tile);
-  rotary_kernel<T><<<grid, kThreads, smem, stream>>>(p, tile, log2_units, heads);
+  if (p.interleaved)
+    rotary_kernel<T, true><<<grid, kThreads, smem, stream>>>(p, tile, log2_units, log2_slots);
+  else
+    rotary_kernel<T, false><<<grid, kThreads, smem, stream>>>(p, tile, log2_units, log2_slots);
   note_launches(1);
   return cudaGetLastError();
 }
