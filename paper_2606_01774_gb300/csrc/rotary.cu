@@ -19,7 +19,9 @@ namespace flare {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
+constexpr int kCtas = 6;     // of an SM
+constexpr int kTileBytes = 48 << 10;
 constexpr int kUnroll = 4;  // units in flight per thread
 
 // cos and sin of `phase` / 2^64 turns.
@@ -104,9 +106,9 @@ __device__ __forceinline__ bool resolve(const RotaryParams& p, int64_t row, int6
 
 // A head is units of 32 bytes, D / 2N of them (N elements to a piece).  A thread has one unit number
 // of every head_slots'th head of a row, so its cosines and sines stay in registers
-// from the first head to the last; 256 threads take 256 / (units head_slots) rows at a time.
+// from the first head to the last; the CTA takes 128 / (units head_slots) rows at a time.
 template <typename T, bool INTERLEAVED>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, kCtas)
     rotary_kernel(const __grid_constant__ RotaryParams p, int tile, int log2_units,
                   int log2_slots) {
   constexpr int N = Piece<T>::N;
@@ -246,11 +248,16 @@ static cudaError_t launch(const RotaryParams& p, int num_sms, cudaStream_t strea
   int log2_units = 0;
   while ((2 * Piece<T>::N << log2_units) < p.D) ++log2_units;
   const int heads = (p.q ? p.Hq : 0) + (p.k ? p.Hkv : 0) + (p.k_pool ? p.Hkv : 0);
+  // tiles of up to 48 KiB: larger ones leave a CTA's memory idle while it works out its next angles
+  // (32768 rows of 9 KiB: 117 us with 32 rows, 110 with 16, 105 with 8, 99 with 4, 101 with
+  // 2), smaller ones work out few at a time (of 6 KiB: 63, 61, 61, 62, 67)
   int tile = 16;
-  while (tile > 1 && (p.rows + tile - 1) / tile < 2 * num_sms) tile /= 2;
+  while (tile > 1 && ((int64_t)tile * heads * p.D * (int)sizeof(T) > kTileBytes ||
+                      (p.rows + tile - 1) / tile < 2 * num_sms))
+    tile /= 2;
   // as many rows at a time as the tile has, or four heads in flight per thread
   int log2_slots = 0;
-  while (log2_units + log2_slots < 8 && (tile << (log2_units + log2_slots) < kThreads ||
+  while (log2_units + log2_slots < 7 && (tile << (log2_units + log2_slots) < kThreads ||
                                          heads >> log2_slots > kUnroll))
     ++log2_slots;
   const int smem = tile * (p.rd / 4 * (int)sizeof(float4) + 2 * (int)sizeof(int64_t) +
