@@ -8,59 +8,84 @@
 //   du = alpha g         dgate = du n act'(gate)                  dresidual = g
 //   dn = du act(gate)    dx = q (w dn - x q^2 mean_G(x w dn))     dw = sum_rows dn x q
 //
-// A CTA takes a row at a time and keeps it in registers, eight elements of a thread next to
-// each other, from the one time it is read to the outputs: bound by bytes.  The gradient of a weight
-// is summed over a CTA's rows in registers, the CTAs' sums in a fixed order by a second kernel.
+// Bound by bytes: every row is read once and written once.  A team of threads takes a row,
+// eight elements next to each other per thread; a team is a warp for rows of up to 256 elements
+// (eight teams to a CTA), a CTA for rows of up to 4096, a cluster of two or four CTAs for longer
+// ones.  Teams walk their rows; a thread copies its own elements of the next rows to
+// its own places in shared memory meanwhile (cp.async), so loads need no barrier, and
+// only the sums over a row meet other threads.  The gradient of a weight is summed over a team's
+// rows in registers, then over the CTA, and the CTAs' sums in a fixed order by a second kernel.
+#include "async.cuh"
 #include "common.cuh"
 #include "kernels.h"
+#include "pdl.cuh"
 #include "piece.cuh"
 
 namespace flare {
 
 namespace {
 
-template <typename T>
-struct Eight {  // eight elements as they lie in memory
-  static constexpr int M = 8 / Piece<T>::N;
-  uint4 u[M];
-  __device__ __forceinline__ void read(const T* p) {
+constexpr int kMaxTeam = 512;                // threads of a CTA, eight elements each
+constexpr int kMaxCols = 8 * kMaxTeam;       // columns of a CTA
+constexpr int kMaxCluster = 4;
+
+__device__ __forceinline__ float exp2f_fast(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Sums over a row, the same in every thread of it.  Calls alternate between two buffers, so that
+// one is written again only after a barrier that follows its last reader.
+struct RowSum {
+  float (*buf)[2][16];           // [2][values][warps]
+  float (*far)[2][kMaxCluster];  // [2][values][CTAs of the cluster]
+  int cluster, rank, turn;
+
+  template <int K>
+  __device__ __forceinline__ void operator()(float (&v)[K]) {
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < M; ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
-  }
-  __device__ __forceinline__ void values(float* x) const {
+    for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
+    if (warps == 1) return;  // a row of up to 256
+    turn ^= 1;
+    if (lane == 0) {
 #pragma unroll
-    for (int i = 0; i < M; ++i) Piece<T>::load(u[i], x + i * Piece<T>::N);
+      for (int k = 0; k < K; ++k) buf[turn][k][threadIdx.x >> 5] = v[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = (lane & 15) < warps ? buf[turn][k][lane & 15] : 0.f;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
+    if (cluster == 1) return;
+    if (threadIdx.x < cluster) {  // to every CTA of the cluster
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        uint32_t at;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                     : "=r"(at)
+                     : "r"((uint32_t)__cvta_generic_to_shared(&far[turn][k][rank])),
+                       "r"(threadIdx.x));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v[k]) : "memory");
+      }
+    }
+    __syncwarp();
+    cluster_sync();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = 0.f;
+      for (int i = 0; i < cluster; ++i) v[k] += far[turn][k][i];
+    }
   }
 };
-
-template <typename T>
-__device__ __forceinline__ void write8(T* p, const float* x) {
-#pragma unroll
-  for (int i = 0; i < Eight<T>::M; ++i)
-    reinterpret_cast<uint4*>(p)[i] = Piece<T>::store(x + i * Piece<T>::N);
-}
-
-__device__ __forceinline__ void weight8(const float* w, int at, float* out) {
-  const float4 a = *reinterpret_cast<const float4*>(w + at);
-  const float4 b = *reinterpret_cast<const float4*>(w + at + 4);
-  out[0] = a.x, out[1] = a.y, out[2] = a.z, out[3] = a.w;
-  out[4] = b.x, out[5] = b.y, out[6] = b.z, out[7] = b.w;
-}
-
-// Sums over the CTA, the same in every thread; `slot` alternates between calls.
-template <int K>
-__device__ __forceinline__ void cta_sum(float (&v)[K], float (*buf)[K][32]) {
-  const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
-  if (warps == 1) return;
-  if (lane == 0)
-#pragma unroll
-    for (int k = 0; k < K; ++k) (*buf)[k][threadIdx.x >> 5] = v[k];
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = warp_sum(lane < warps ? (*buf)[k][lane] : 0.f);
-}
 
 // Sum over `lanes` neighbouring lanes.
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
@@ -68,319 +93,463 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
   return v;
 }
 
-// The gate's activation and its derivative.
-__device__ __forceinline__ float act(int kind, float z, float& slope) {
-  if (kind == FLARE_ACT_NONE) {
-    slope = 1.f;
-    return z;
-  }
-  const float a = 1.f / (1.f + expf(-z));
-  if (kind == FLARE_ACT_SIGMOID) {
-    slope = a * (1.f - a);
-    return a;
-  }
-  slope = a * (1.f + z * (1.f - a));
-  return z * a;
+// 1 / (1 + e^-z).  The exponent z log2 e in two parts (its rounding would be a relative error
+// of |z| 2^-24), the quotient by the fast reciprocal: 2^-22 in all.  Zero from z = -87.3 down,
+// where the quotient leaves the normal numbers.
+__device__ __forceinline__ float sigmoid(float z) {
+  constexpr float kLog2e = 1.44269504089f, kRest = 1.92596300e-8f;
+  const float t = z * -kLog2e, hi = t > 127.f ? 127.f : t;  // a NaN stays one
+  const float lo = fmaf(z, -kLog2e, -hi) - z * kRest;
+  const float e = exp2f_fast(hi);
+  return __fdividef(1.f, 1.f + (fabsf(hi) < 127.f ? fmaf(e, lo * 0.693147181f, e) : e));
 }
+
+// Sigmoids of eight gates (nothing for a gate that is taken as it is).
+__device__ __forceinline__ void sigmoid8(int kind, const uint64_t (&z)[4], uint64_t (&s)[4]) {
+  if (kind == FLARE_ACT_NONE) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float z0, z1;
+    f2_split(z[i], z0, z1);
+    s[i] = f2(sigmoid(z0), sigmoid(z1));
+  }
+}
+
+// The gate's activation from the gate and its sigmoid.
+__device__ __forceinline__ uint64_t activation(int kind, uint64_t z, uint64_t s) {
+  return kind == FLARE_ACT_NONE ? z : kind == FLARE_ACT_SIGMOID ? s : f2_mul(z, s);
+}
+
+// Its derivative: 1, s (1 - s) or s (1 + z (1 - s)).
+__device__ __forceinline__ uint64_t activation_slope(int kind, uint64_t z, uint64_t s) {
+  const uint64_t one = f2_dup(1.f);
+  if (kind == FLARE_ACT_NONE) return one;
+  const uint64_t rest = f2_fma(s, f2_dup(-1.f), one);
+  return f2_mul(s, kind == FLARE_ACT_SIGMOID ? rest : f2_fma(z, rest, one));
+}
+
+__device__ __forceinline__ float pair_sum(uint64_t v) {
+  float a, b;
+  f2_split(v, a, b);
+  return a + b;
+}
+
+// sum of a_i b_i
+__device__ __forceinline__ float dot8(const uint64_t (&a)[4], const uint64_t (&b)[4]) {
+  uint64_t s = f2_mul(a[0], b[0]), t = f2_mul(a[1], b[1]);
+  s = f2_fma(a[2], b[2], s);
+  t = f2_fma(a[3], b[3], t);
+  return pair_sum(f2_add(s, t));
+}
+
+// A thread's own places in shared memory: its eight elements of each input of a row.
+template <typename T>
+struct Slots {
+  static constexpr int M = 8 / Piece<T>::N;
+  uint4* at;   // of this thread, piece 0
+  int pieces;  // from one piece to the next: threads of the CTA
+
+  __device__ __forceinline__ void fetch(int array, const T* src) const {
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      cp_async16(at + (array * M + i) * pieces, reinterpret_cast<const uint4*>(src) + i);
+  }
+  __device__ __forceinline__ void read(int array, uint64_t (&x)[4]) const {
+    uint4 u[M];
+#pragma unroll
+    for (int i = 0; i < M; ++i) u[i] = at[(array * M + i) * pieces];
+    load_pairs<T>(u, x);
+  }
+};
+
+// Eight fp32 values of a thread's own.
+struct Scratch {
+  uint4* at;
+  int pieces;
+
+  __device__ __forceinline__ void write(int kind, const uint64_t (&x)[4]) const {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f2_split(x[i], f[2 * i], f[2 * i + 1]);
+    at[2 * kind * pieces] = Piece<float>::store(f);
+    at[(2 * kind + 1) * pieces] = Piece<float>::store(f + 4);
+  }
+  __device__ __forceinline__ void read(int kind, uint64_t (&x)[4]) const {
+    const uint4 u[2] = {at[2 * kind * pieces], at[(2 * kind + 1) * pieces]};
+    load_pairs<float>(u, x);
+  }
+};
+
+// A thread's own weights in shared memory: after the block (times alpha), before the next.
+struct Weights : Scratch {
+  __device__ __forceinline__ void fill(const BlockNormParams& p, int c) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float4 w = make_float4(1.f, 1.f, 1.f, 1.f);
+      if (p.wpost) w = reinterpret_cast<const float4*>(p.wpost + (p.shared ? c % p.G : c))[i];
+      w.x *= p.alpha, w.y *= p.alpha, w.z *= p.alpha, w.w *= p.alpha;
+      reinterpret_cast<float4*>(at)[i * pieces] = w;
+      w = make_float4(1.f, 1.f, 1.f, 1.f);
+      if (p.wpre) w = reinterpret_cast<const float4*>(p.wpre + c)[i];
+      reinterpret_cast<float4*>(at)[(2 + i) * pieces] = w;
+    }
+  }
+};
+
+__device__ __forceinline__ void wait_rows(int later) {
+  if (later >= 3) cp_async_wait<3>();
+  else if (later == 2) cp_async_wait<2>();
+  else cp_async_wait<1>();
+}
+
+// Shared memory of a CTA: weights (eight of each kind per thread), backward with a gate its
+// sigmoids, then stages x inputs.
+struct Shape {
+  int team, teams, cluster, ctas;  // threads of a CTA's team, teams of a CTA, CTAs of a cluster
+  int cols;                        // columns of a CTA
+  int arrays, stages;
+  int smem;
+};
 
 }  // namespace
 
-template <typename T, int V>
-__global__ void __launch_bounds__(512) block_norm_kernel(const __grid_constant__ BlockNormParams p) {
-  __shared__ float buf[2][1][32];
-  const int tid = threadIdx.x, W = p.W;
-  const bool heads = p.post && p.G != W;
-  const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)W;
-  for (int row = blockIdx.x; row < p.T; row += gridDim.x) {
-    const T* x_row = static_cast<const T*>(p.x) + (int64_t)row * p.x_stride;
-    const T* g_row = static_cast<const T*>(p.gate) + (int64_t)row * p.gate_stride;
-    const T* r_row = static_cast<const T*>(p.residual) + (int64_t)row * W;
-    Eight<T> xin[V], gin[V], rin[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * blockDim.x + tid) * 8;
-      if (c < W) {
-        xin[j].read(x_row + c);
-        if (p.gate) gin[j].read(g_row + c);
-        if (p.residual) rin[j].read(r_row + c);
-      }
+template <typename T, bool GATE>
+__global__ void __launch_bounds__(kMaxTeam, 2)
+    block_norm_kernel(const __grid_constant__ BlockNormParams p, const __grid_constant__ Shape s) {
+  extern __shared__ __align__(16) char smem[];
+  __shared__ float buf[2][2][16], far[2][2][kMaxCluster];
+  const int thread = threadIdx.y * blockDim.x + threadIdx.x;
+  const int threads = blockDim.x * blockDim.y;
+  const int rank = blockIdx.x % s.cluster;
+  RowSum row_sum{buf, far, s.cluster, rank, 0};
+  const int c = rank * s.cols + threadIdx.x * 8;
+  const bool mine = threadIdx.x * 8 < s.cols && c < p.W;
+  const bool heads = p.post && p.G != p.W;
+  const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
+  const Weights weights{{reinterpret_cast<uint4*>(smem) + thread, threads}};
+  uint4* ring = reinterpret_cast<uint4*>(smem) + 4 * threads + thread;
+  const int stage = s.arrays * Slots<T>::M * threads;
+  constexpr int kGate = 1, kRes = 1 + GATE;
+
+  if (mine) weights.fill(p, c);
+  if (s.cluster > 1) cluster_sync();  // every CTA runs before another writes to its memory
+  const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
+  const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
+  const auto fetch = [&](int64_t row, int at) {
+    if (mine && row < p.T) {
+      const Slots<T> to{ring + at * stage, threads};
+      to.fetch(0, static_cast<const T*>(p.x) + row * p.x_stride + c);
+      if (GATE) to.fetch(kGate, static_cast<const T*>(p.gate) + row * p.gate_stride + c);
+      if (p.residual) to.fetch(kRes, static_cast<const T*>(p.residual) + row * p.W + c);
     }
-    float q[V], y[V][8];
+    cp_async_commit();
+  };
+  for (int i = 0; i < s.stages - 1; ++i) fetch(first + i * step, i);
+  int at = 0;
+  for (int64_t row = first; row < p.T; row += step) {
+    const int last = at == 0 ? s.stages - 1 : at - 1;
+    fetch(row + (s.stages - 1) * step, last);
+    wait_rows(s.stages - 1);
+    const Slots<T> in{ring + at * stage, threads};
+    at = at + 1 == s.stages ? 0 : at + 1;
+
+    uint64_t y[4] = {}, t[4] = {}, w[4] = {};
+    if (mine) {
+      in.read(0, y);
+      weights.read(0, w);
+    }
     if (p.post) {
-      float all[1] = {0.f};
+      float sum[1] = {dot8(y, y)};
+      if (heads) sum[0] = lanes_sum(sum[0], p.G / 8);
+      else row_sum(sum);
+      const uint64_t q = f2_dup(rsqrtf(sum[0] * per_group + p.eps));
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        float x[8], s = 0.f;
-        if ((j * blockDim.x + tid) * 8 < W) {
-          xin[j].values(x);
+      for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], q);
+    }
+    if (GATE) {
+      uint64_t sig[4] = {};
+      if (mine) in.read(kGate, t);
+      sigmoid8(p.act, t, sig);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) s += x[e] * x[e];
-        }
-        if (heads) q[j] = rsqrtf(lanes_sum(s, p.G / 8) * per_group + p.eps);
-        else all[0] += s;
-      }
-      if (!heads) {
-        cta_sum<1>(all, &buf[0]);
-#pragma unroll
-        for (int j = 0; j < V; ++j) q[j] = rsqrtf(all[0] * per_group + p.eps);
+      for (int i = 0; i < 4; ++i) {
+        w[i] = f2_mul(w[i], activation(p.act, t[i], sig[i]));
+        t[i] = 0;
       }
     }
-    float squares[1] = {0.f};
+    if (p.residual && mine) in.read(kRes, t);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * blockDim.x + tid) * 8;
-      if (c >= W) continue;
-      xin[j].values(y[j]);
-      if (p.post) {
-        float w[8];
-        if (p.wpost) weight8(p.wpost, p.shared ? c % p.G : c, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] *= p.wpost ? q[j] * w[e] : q[j];
-      }
-      if (p.gate) {
-        float z[8], slope;
-        gin[j].values(z);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] *= act(p.act, z[e], slope);
-      }
-      float res[8];
-      if (p.residual) rin[j].values(res);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[j][e] = p.alpha * y[j][e] + (p.residual ? res[e] : 0.f);
-        squares[0] += y[j][e] * y[j][e];
-      }
-      if (p.y) write8<T>(static_cast<T*>(p.y) + (int64_t)row * W + c, y[j]);
-    }
+    for (int i = 0; i < 4; ++i) y[i] = f2_fma(y[i], w[i], t[i]);
+    if (p.y && mine) store_pairs<T>(static_cast<T*>(p.y) + row * p.W + c, y);
     if (p.pre) {
-      cta_sum<1>(squares, &buf[1]);
-      const float r = rsqrtf(squares[0] * per_row + p.eps);
+      float squares[1] = {dot8(y, y)};
+      row_sum(squares);
+      const uint64_t r = f2_dup(rsqrtf(squares[0] * per_row + p.eps));
+      if (mine) {
+        weights.read(1, w);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = (j * blockDim.x + tid) * 8;
-        if (c >= W) continue;
-        float w[8];
-        if (p.wpre) weight8(p.wpre, c, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] *= p.wpre ? r * w[e] : r;
-        write8<T>(static_cast<T*>(p.h) + (int64_t)row * W + c, y[j]);
+        for (int i = 0; i < 4; ++i) y[i] = f2_mul(y[i], f2_mul(w[i], r));
+        store_pairs<T>(static_cast<T*>(p.h) + row * p.W + c, y);
       }
     }
-    if (blockDim.x > 32) __syncthreads();  // the sums' buffers before the next row's
   }
+  if (s.cluster > 1) cluster_sync();  // none leaves while another may write to its memory
 }
 
-template <typename T, int V>
-__global__ void __launch_bounds__(512)
-    block_norm_bwd_kernel(const __grid_constant__ BlockNormParams p) {
-  __shared__ float buf1[1][32], buf2[2][32], buf3[1][32];
-  const int tid = threadIdx.x, W = p.W;
-  const bool heads = p.post && p.G != W;
-  const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)W;
-  float dwpost[V][8], dwpre[V][8];
-#pragma unroll
-  for (int j = 0; j < V; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) dwpost[j][e] = dwpre[j][e] = 0.f;
+template <typename T, bool GATE>
+__global__ void __launch_bounds__(kMaxTeam, 2)
+    block_norm_bwd_kernel(const __grid_constant__ BlockNormParams p,
+                          const __grid_constant__ Shape s) {
+  extern __shared__ __align__(16) char smem[];
+  __shared__ float buf[2][2][16], far[2][2][kMaxCluster];
+  const int thread = threadIdx.y * blockDim.x + threadIdx.x;
+  const int threads = blockDim.x * blockDim.y;
+  const int rank = blockIdx.x % s.cluster;
+  RowSum row_sum{buf, far, s.cluster, rank, 0};
+  const int c = rank * s.cols + threadIdx.x * 8;
+  const bool mine = threadIdx.x * 8 < s.cols && c < p.W;
+  const bool heads = p.post && p.G != p.W;
+  const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
+  const Weights weights{{reinterpret_cast<uint4*>(smem) + thread, threads}};
+  const Scratch scratch{reinterpret_cast<uint4*>(smem) + 4 * threads + thread, threads};
+  uint4* ring = reinterpret_cast<uint4*>(smem) + (GATE ? 6 : 4) * threads + thread;
+  const int stage = s.arrays * Slots<T>::M * threads;
+  const bool use_res = p.pre && p.residual;  // y itself is needed by its norm alone
+  constexpr int kGate = 1, kRes = 1 + GATE;
+  const int i_dy = kRes + use_res, i_dh = i_dy + (p.dy != nullptr);
 
-  for (int row = blockIdx.x; row < p.T; row += gridDim.x) {
-    Eight<T> xin[V], gin[V], rin[V], yin[V], hin[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * blockDim.x + tid) * 8;
-      if (c < W) {
-        const int64_t at = (int64_t)row * W + c;
-        xin[j].read(static_cast<const T*>(p.x) + (int64_t)row * p.x_stride + c);
-        if (p.gate) gin[j].read(static_cast<const T*>(p.gate) + (int64_t)row * p.gate_stride + c);
-        if (p.pre && p.residual) rin[j].read(static_cast<const T*>(p.residual) + at);
-        if (p.dy) yin[j].read(static_cast<const T*>(p.dy) + at);
-        if (p.pre) hin[j].read(static_cast<const T*>(p.dh) + at);
-      }
+  if (mine) weights.fill(p, c);
+  if (s.cluster > 1) cluster_sync();
+  const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
+  const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
+  const auto fetch = [&](int64_t row, int at) {
+    if (mine && row < p.T) {
+      const Slots<T> to{ring + at * stage, threads};
+      to.fetch(0, static_cast<const T*>(p.x) + row * p.x_stride + c);
+      if (GATE) to.fetch(kGate, static_cast<const T*>(p.gate) + row * p.gate_stride + c);
+      if (use_res) to.fetch(kRes, static_cast<const T*>(p.residual) + row * p.W + c);
+      if (p.dy) to.fetch(i_dy, static_cast<const T*>(p.dy) + row * p.W + c);
+      if (p.pre) to.fetch(i_dh, static_cast<const T*>(p.dh) + row * p.W + c);
     }
-    float q[V];
+    cp_async_commit();
+  };
+  uint64_t dwpost[4] = {}, dwpre[4] = {};
+
+  for (int i = 0; i < s.stages - 1; ++i) fetch(first + i * step, i);
+  int at = 0;
+  for (int64_t row = first; row < p.T; row += step) {
+    const int last = at == 0 ? s.stages - 1 : at - 1;
+    fetch(row + (s.stages - 1) * step, last);
+    wait_rows(s.stages - 1);
+    const Slots<T> in{ring + at * stage, threads};
+    at = at + 1 == s.stages ? 0 : at + 1;
+
+    // What a sum separates is read again after it, rather than held: 64 registers a thread let an
+    // SM hold two rows of 4096.  Columns past the row's stay zero throughout.
+    float q = 1.f;
     if (p.post) {
-      float all[1] = {0.f};
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        float x[8], s = 0.f;
-        if ((j * blockDim.x + tid) * 8 < W) {
-          xin[j].values(x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s += x[e] * x[e];
-        }
-        if (heads) q[j] = rsqrtf(lanes_sum(s, p.G / 8) * per_group + p.eps);
-        else all[0] += s;
-      }
-      if (!heads) {
-        cta_sum<1>(all, &buf1);
-#pragma unroll
-        for (int j = 0; j < V; ++j) q[j] = rsqrtf(all[0] * per_group + p.eps);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) q[j] = 1.f;
+      uint64_t x[4] = {};
+      if (mine) in.read(0, x);
+      float sum[1] = {dot8(x, x)};
+      if (heads) sum[0] = lanes_sum(sum[0], p.G / 8);
+      else row_sum(sum);
+      q = rsqrtf(sum[0] * per_group + p.eps);
     }
-
-    float g[V][8];  // the gradient at y
-    float sums[2] = {0.f, 0.f};
+    const uint64_t qq = f2_dup(q);
+    if (GATE && mine) {
+      uint64_t z[4], sig[4] = {};
+      in.read(kGate, z);
+      sigmoid8(p.act, z, sig);
+      scratch.write(0, sig);
+    }
+    uint64_t g[4] = {};
     if (p.pre) {
-      float y[V][8];
+      uint64_t y[4] = {};
+      float sums[2] = {0.f, 0.f};
+      if (mine) {
+        uint64_t x[4], w[4], t[4];
+        if (use_res) in.read(kRes, y);
+        in.read(0, x);
+        weights.read(0, w);
+        if (GATE) {
+          uint64_t sig[4];
+          in.read(kGate, t);
+          scratch.read(0, sig);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = (j * blockDim.x + tid) * 8;
-        if (c >= W) continue;
-        float w[8], t[8], slope;
-        xin[j].values(y[j]);
-        if (p.post) {
-          if (p.wpost) weight8(p.wpost, p.shared ? c % p.G : c, w);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[j][e] *= p.wpost ? q[j] * w[e] : q[j];
+          for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], activation(p.act, t[i], sig[i]));
         }
-        if (p.gate) {
-          gin[j].values(t);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[j][e] *= act(p.act, t[e], slope);
-        }
-        if (p.residual) rin[j].values(t);
-        hin[j].values(g[j]);
-        if (p.wpre) weight8(p.wpre, c, w);
+        for (int i = 0; i < 4; ++i) y[i] = f2_fma(x[i], f2_mul(w[i], qq), y[i]);
+        in.read(i_dh, t);
+        weights.read(1, w);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          y[j][e] = p.alpha * y[j][e] + (p.residual ? t[e] : 0.f);
-          sums[0] += y[j][e] * y[j][e];
-          sums[1] += y[j][e] * (p.wpre ? g[j][e] * w[e] : g[j][e]);
-        }
+        for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], t[i]);
+        sums[0] = dot8(y, y);
+        sums[1] = dot8(y, w);
       }
-      cta_sum<2>(sums, &buf2);
+      row_sum(sums);
       const float r = rsqrtf(sums[0] * per_row + p.eps);
-      const float back = sums[1] * per_row * r * r;
+      const uint64_t rr = f2_dup(r), back = f2_dup(-(sums[1] * per_row * r * r * r));
+      if (mine) {
+        uint64_t dh[4], w[4];
+        in.read(i_dh, dh);
+        if (p.dy) in.read(i_dy, g);
+        weights.read(1, w);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = (j * blockDim.x + tid) * 8;
-        if (c >= W) continue;
-        float w[8], t[8];
-        if (p.wpre) weight8(p.wpre, c, w);
-        if (p.dy) yin[j].values(t);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          dwpre[j][e] += g[j][e] * y[j][e] * r;
-          g[j][e] = r * ((p.wpre ? g[j][e] * w[e] : g[j][e]) - y[j][e] * back);
-          if (p.dy) g[j][e] += t[e];
+        for (int i = 0; i < 4; ++i) {
+          const uint64_t d = f2_mul(dh[i], rr);
+          dwpre[i] = f2_fma(d, y[i], dwpre[i]);
+          g[i] = f2_fma(y[i], back, f2_fma(d, w[i], g[i]));
         }
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j)
-        if ((j * blockDim.x + tid) * 8 < W) yin[j].values(g[j]);
+    } else if (mine) {
+      in.read(i_dy, g);
     }
-
-    float dot[V], all[1] = {0.f};
+    float dot[1] = {0.f};
+    if (mine) {
+      if (p.dres) store_pairs<T>(static_cast<T*>(p.dres) + row * p.W + c, g);
+      uint64_t x[4], w[4];
+      in.read(0, x);
+      weights.read(0, w);
+      if (GATE) {
+        uint64_t z[4], sig[4];
+        in.read(kGate, z);
+        scratch.read(0, sig);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * blockDim.x + tid) * 8;
-      dot[j] = 0.f;
-      if (c < W) {
-        if (p.dres) write8<T>(static_cast<T*>(p.dres) + (int64_t)row * W + c, g[j]);
-        float x[8], w[8], z[8], slope, dz[8];
-        xin[j].values(x);
-        if (p.post && p.wpost) weight8(p.wpost, p.shared ? c % p.G : c, w);
-        if (p.gate) gin[j].values(z);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float d = p.alpha * g[j][e];
-          const float xq = x[e] * q[j];
-          if (p.gate) {
-            const float a = act(p.act, z[e], slope);
-            dz[e] = d * (p.post && p.wpost ? xq * w[e] : xq) * slope;
-            d *= a;
-          }
-          if (p.post) {
-            dwpost[j][e] += d * xq;
-            if (p.wpost) d *= w[e];
-            dot[j] += x[e] * d;
-          }
-          g[j][e] = d;
+        for (int i = 0; i < 4; ++i) {
+          const uint64_t n = f2_mul(x[i], f2_mul(w[i], qq));
+          const uint64_t a = activation(p.act, z[i], sig[i]);
+          z[i] = f2_mul(activation_slope(p.act, z[i], sig[i]), f2_mul(g[i], n));
+          g[i] = f2_mul(g[i], a);
         }
-        if (p.gate)
-          write8<T>(static_cast<T*>(p.dgate) + (int64_t)row * p.gate_stride + c, dz);
+        store_pairs<T>(static_cast<T*>(p.dgate) + row * p.gate_stride + c, z);
       }
-      if (heads) dot[j] = lanes_sum(dot[j], p.G / 8);
-      else all[0] += dot[j];
-    }
-    if (p.post && !heads) {
-      cta_sum<1>(all, &buf3);
 #pragma unroll
-      for (int j = 0; j < V; ++j) dot[j] = all[0];
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = (j * blockDim.x + tid) * 8;
-      if (c >= W) continue;
-      if (p.post) {
-        float x[8];
-        xin[j].values(x);
-        const float back = dot[j] * per_group * q[j] * q[j];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[j][e] = q[j] * (g[j][e] - x[e] * back);
+      for (int i = 0; i < 4; ++i) {
+        dwpost[i] = f2_fma(g[i], f2_mul(x[i], qq), dwpost[i]);
+        g[i] = f2_mul(g[i], w[i]);
       }
-      write8<T>(static_cast<T*>(p.dx) + (int64_t)row * p.x_stride + c, g[j]);
+      dot[0] = dot8(x, g);
     }
-    if (blockDim.x > 32) __syncthreads();
+    if (p.post) {
+      if (heads) dot[0] = lanes_sum(dot[0], p.G / 8);
+      else row_sum(dot);
+      const uint64_t back = f2_dup(-(dot[0] * per_group * q * q * q));
+      uint64_t x[4] = {};
+      if (mine) in.read(0, x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = f2_fma(x[i], back, f2_mul(g[i], qq));
+    }
+    if (mine) store_pairs<T>(static_cast<T*>(p.dx) + row * p.x_stride + c, g);
   }
-
+  if (s.cluster > 1) cluster_sync();
+  pdl_launch_next();
   if (!p.part) return;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int c = (j * blockDim.x + tid) * 8;
-    if (c >= W) continue;
-    float* at = p.part + (int64_t)blockIdx.x * 2 * W + c;
-    write8<float>(at, dwpost[j]);
-    write8<float>(at + W, dwpre[j]);
+  for (int i = 0; i < 4; ++i) dwpost[i] = f2_mul(dwpost[i], f2_dup(p.alpha));
+
+  // the CTA's sums: [CTAs][post columns], then [CTAs][W] before the next block
+  const int wide = p.shared ? p.G : p.W;
+  float* post = p.part + (int64_t)(p.shared ? blockIdx.x : blockIdx.x / s.cluster) * wide;
+  float* pre = p.part + (int64_t)gridDim.x * wide + (int64_t)(blockIdx.x / s.cluster) * p.W;
+  if (!p.shared && blockDim.y == 1) {
+    if (mine) {
+      store_pairs<float>(post + c, dwpost);
+      store_pairs<float>(pre + c, dwpre);
+    }
+    return;
+  }
+  float* sums = reinterpret_cast<float*>(smem);  // [teams][columns]
+  const int cols = blockDim.x * 8, from = rank * s.cols;
+  const int used = min(min(cols, s.cols), p.W - from);
+  for (int kind = 0; kind < 2; ++kind) {
+    __syncthreads();
+    store_pairs<float>(sums + thread * 8, kind ? dwpre : dwpost);
+    __syncthreads();
+    const bool by_group = p.shared && !kind;
+    const int n = by_group ? p.G : used;
+    for (int i = thread; i < n; i += threads) {
+      float total = 0.f;
+      for (int team = 0; team < blockDim.y; ++team)
+        for (int k = i; k < used; k += n) total += sums[team * cols + k];
+      if (by_group) post[i] = total;
+      else (kind ? pre : post)[from + i] = total;
+    }
   }
 }
 
-// The CTAs' partial weight gradients joined: 32 columns a CTA, eight warps that take every eighth
-// CTA (and group) and are then added in order.
-__global__ void __launch_bounds__(256)
-    block_norm_weights_kernel(const __grid_constant__ BlockNormParams p, int ctas) {
-  __shared__ float buf[8][33];
+// The CTAs' weight gradients joined: 32 columns a CTA, its warps one partial sum in 32 each,
+// added in order at the end.
+__global__ void __launch_bounds__(1024)
+    block_norm_weights_kernel(const __grid_constant__ BlockNormParams p, int ctas, int cluster) {
+  __shared__ float buf[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int wide_post = p.shared ? p.G : p.W;
   const bool post = blockIdx.y == 0;
   float* out = post ? p.dwpost : p.dwpre;
-  const int wide = post && p.shared ? p.G : p.W, c = blockIdx.x * 32 + lane;
+  const int wide = post ? wide_post : p.W, c = blockIdx.x * 32 + lane;
+  pdl_wait();
   if (!out || blockIdx.x * 32 >= wide) return;
-  const int groups = p.W / wide;
+  const int n = post && p.shared ? ctas : ctas / cluster;
   float sum = 0.f;
   if (c < wide) {
-    const float* at = p.part + (post ? 0 : p.W) + c;
-    for (int i = warp; i < ctas * groups; i += 8) {
-      const int cta = i / groups;
-      sum += at[(int64_t)cta * 2 * p.W + (i - cta * groups) * wide];
-    }
+    const float* at = p.part + (post ? 0 : (int64_t)ctas * wide_post) + c;
+#pragma unroll 4
+    for (int i = warp; i < n; i += 32) sum += at[(int64_t)i * wide];
   }
   buf[warp][lane] = sum;
   __syncthreads();
-  if (warp == 0 && c < wide) {
-    for (int k = 1; k < 8; ++k) sum += buf[k][lane];
-    out[c] = sum;
-  }
+  sum = warp_sum(buf[lane][warp]);
+  if (lane == 0 && blockIdx.x * 32 + warp < wide) out[blockIdx.x * 32 + warp] = sum;
 }
 
 namespace {
 
-int row_threads(int W, int V) { return (W + 8 * V * 32 - 1) / (8 * V * 32) * 32; }
-int vectors(int W) { return W <= 2048 ? 1 : W <= 8192 ? 2 : 4; }
+// The teams of a call on T rows of W elements, `arrays` inputs of `elem` bytes.
+Shape shape_for(int T, int W, int arrays, int elem, bool sigmoids, int num_sms) {
+  Shape s = {};
+  s.cluster = W <= kMaxCols ? 1 : W <= 2 * kMaxCols ? 2 : 4;
+  // whole groups of up to 256 columns to a CTA
+  s.cols = s.cluster == 1 ? W : (W / s.cluster + 255) / 256 * 256;
+  s.team = (s.cols + 255) / 256 * 32;
+  s.teams = s.team == 32 ? 8 : 1;
+  s.arrays = arrays;
+  const int threads = s.team * s.teams;
+  const int per_sm = threads > 256 ? 2 : threads > 128 ? 4 : 8;
+  const int most = (220 << 10) / per_sm - 2048;
+  const int weights = threads * (sigmoids ? 96 : 64), row = threads * 8 * elem * arrays;
+  s.stages = 2;
+  while (s.stages < 4 && weights + row * (s.stages + 1) <= most) ++s.stages;
+  s.smem = weights + row * s.stages;
+  const int rows = (T + s.teams - 1) / s.teams;  // of a CTA or cluster at a time
+  const int clusters = per_sm * num_sms / s.cluster;
+  s.ctas = (rows < clusters ? rows : clusters) * s.cluster;
+  return s;
+}
+
+int arrays_of(const BlockNormParams& p, bool bwd) {
+  return 1 + (p.gate != nullptr) + (p.residual && (!bwd || p.pre)) +
+         (bwd ? (p.dy != nullptr) + p.pre : 0);
+}
 
 template <typename T>
-void run(const BlockNormParams& p, bool bwd, int ctas, cudaStream_t stream) {
-  const int v = vectors(p.W), threads = row_threads(p.W, v);
-  const auto go = [&](auto* fwd_kernel, auto* bwd_kernel) {
-    if (bwd) bwd_kernel<<<ctas, threads, 0, stream>>>(p);
-    else fwd_kernel<<<ctas, threads, 0, stream>>>(p);
-  };
-  if (v == 1) go(block_norm_kernel<T, 1>, block_norm_bwd_kernel<T, 1>);
-  else if (v == 2) go(block_norm_kernel<T, 2>, block_norm_bwd_kernel<T, 2>);
-  else go(block_norm_kernel<T, 4>, block_norm_bwd_kernel<T, 4>);
+cudaError_t run(const BlockNormParams& p, const Shape& s, bool bwd, cudaStream_t stream) {
+  const auto kernel = bwd ? p.gate ? block_norm_bwd_kernel<T, true> : block_norm_bwd_kernel<T, false>
+                          : p.gate ? block_norm_kernel<T, true> : block_norm_kernel<T, false>;
+  cudaError_t e =
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)s.ctas);
+  cfg.blockDim = dim3((unsigned)s.team, (unsigned)s.teams);
+  cfg.dynamicSmemBytes = (size_t)s.smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)s.cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = s.cluster > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, p, s);
 }
 
 }  // namespace
@@ -388,33 +557,34 @@ void run(const BlockNormParams& p, bool bwd, int ctas, cudaStream_t stream) {
 cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
                               cudaStream_t stream) {
   if (p.T == 0) return cudaSuccess;
-  const int ctas = p.T < 8 * num_sms ? p.T : 8 * num_sms;
-  if (bf16) run<__nv_bfloat16>(p, false, ctas, stream);
-  else run<float>(p, false, ctas, stream);
+  const Shape s = shape_for(p.T, p.W, arrays_of(p, false), bf16 ? 2 : 4, false, num_sms);
   note_launches(1);
-  return cudaGetLastError();
+  return bf16 ? run<__nv_bfloat16>(p, s, false, stream) : run<float>(p, s, false, stream);
 }
 
 int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms) {
-  const int most = (W <= 2048 ? 4 : 2) * num_sms;
-  return T < most ? T : most;
+  return T ? shape_for(T, W, 1, bf16 ? 2 : 4, true, num_sms).ctas : 0;
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
                                   cudaStream_t stream) {
-  const int ctas = block_norm_bwd_ctas(p.T, p.W, bf16, num_sms);
   const bool weights = p.dwpost || p.dwpre;
-  if (ctas == 0 && !weights) return cudaSuccess;
-  if (ctas > 0) {
-    if (bf16) run<__nv_bfloat16>(p, true, ctas, stream);
-    else run<float>(p, true, ctas, stream);
+  if (p.T == 0 && !weights) return cudaSuccess;
+  Shape s = {};
+  s.cluster = 1;
+  if (p.T > 0) {
+    s = shape_for(p.T, p.W, arrays_of(p, true), bf16 ? 2 : 4, p.gate, num_sms);
     note_launches(1);
+    const cudaError_t e =
+        bf16 ? run<__nv_bfloat16>(p, s, true, stream) : run<float>(p, s, true, stream);
+    if (e != cudaSuccess) return e;
   }
   if (weights) {  // of no rows: zeros
-    block_norm_weights_kernel<<<dim3((unsigned)(p.W + 31) / 32, 2), 256, 0, stream>>>(p, ctas);
     note_launches(1);
+    return pdl_launch(block_norm_weights_kernel, dim3((unsigned)(p.W + 31) / 32, 2), 1024, 0,
+                      stream, p.T > 0, 1, p, s.ctas, s.cluster);
   }
-  return cudaGetLastError();
+  return cudaSuccess;
 }
 
 }  // namespace flare

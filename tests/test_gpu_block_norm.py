@@ -117,6 +117,8 @@ def test_far_gates_and_zero_rows():
     sig.gate[0], sig.gate[1] = float("inf"), float("-inf")
     y, _ = run_norm(sig)
     assert bool(torch.isfinite(y[keep[:2]]).all()) and bool((y[1] == 0).all())
+    sig.gate[0] = float("nan")
+    assert bool(run_norm(sig)[0][0].isnan().all())
 
 
 def test_no_rows():
