@@ -26,6 +26,8 @@ namespace flare {
 namespace {
 
 constexpr int kMaxTeam = 512;                // threads of a CTA, eight elements each
+constexpr int kBwdVectors = 2;               // of eight elements per thread, backward
+constexpr int kMaxBwdTeam = kMaxTeam / kBwdVectors;
 constexpr int kMaxCols = 8 * kMaxTeam;       // columns of a CTA
 constexpr int kMaxCluster = 4;
 
@@ -47,23 +49,31 @@ struct RowSum {
   float (*far)[2][kMaxCluster];  // [2][values][CTAs of the cluster]
   int cluster, rank, turn;
 
+  // A warp's two sums go down one tree: its halves swap one value each, so that the lower
+  // half holds the first and the upper half the second.
   template <int K>
   __device__ __forceinline__ void operator()(float (&v)[K]) {
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    const bool upper = K == 2 && lane >= 16;
+    float x = v[0];
+    if (K == 2) x = (upper ? v[K - 1] : v[0]) + __shfl_xor_sync(~0u, upper ? v[0] : v[K - 1], 16);
+    else x += __shfl_xor_sync(~0u, x, 16);
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = warp_sum(v[k]);
-    if (warps == 1) return;  // a row of up to 256
-    turn ^= 1;
-    if (lane == 0) {
+    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+    if (warps > 1) {  // a row of more than a warp
+      turn ^= 1;
+      if (K == 2 ? (lane & 15) == 0 : lane == 0) buf[turn][upper][threadIdx.x >> 5] = x;
+      __syncthreads();
+      x = (lane & 15) < warps ? buf[turn][upper][lane & 15] : 0.f;
 #pragma unroll
-      for (int k = 0; k < K; ++k) buf[turn][k][threadIdx.x >> 5] = v[k];
+      for (int o = 8; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
     }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      v[k] = (lane & 15) < warps ? buf[turn][k][lane & 15] : 0.f;
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    if (K == 2) {
+      const float other = __shfl_xor_sync(~0u, x, 16);
+      v[0] = upper ? other : x;
+      v[K - 1] = upper ? x : other;
+    } else {
+      v[0] = x;
     }
     if (cluster == 1) return;
     if (threadIdx.x < cluster) {  // to every CTA of the cluster
@@ -174,6 +184,10 @@ struct Scratch {
     at[2 * kind * pieces] = Piece<float>::store(f);
     at[(2 * kind + 1) * pieces] = Piece<float>::store(f + 4);
   }
+  // of the thread's j-th vector
+  __device__ __forceinline__ Scratch at_vector(int j) const {
+    return {at + j * 2 * pieces, pieces};
+  }
   __device__ __forceinline__ void read(int kind, uint64_t (&x)[4]) const {
     const uint4 u[2] = {at[2 * kind * pieces], at[(2 * kind + 1) * pieces]};
     load_pairs<float>(u, x);
@@ -182,6 +196,10 @@ struct Scratch {
 
 // A thread's own weights in shared memory: after the block (times alpha), before the next.
 struct Weights : Scratch {
+  __device__ __forceinline__ Weights at_vector(int j) const {
+    return {{at + j * 4 * pieces, pieces}};
+  }
+
   __device__ __forceinline__ void fill(const BlockNormParams& p, int c) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -295,175 +313,255 @@ __global__ void __launch_bounds__(kMaxTeam, 2)
   if (s.cluster > 1) cluster_sync();  // none leaves while another may write to its memory
 }
 
+// Sixteen elements of a row per thread, in two vectors of eight.  The sum of the next row's squares
+// goes along with this row's last sum, so x arrives a row ahead of the other inputs.
 template <typename T, bool GATE>
-__global__ void __launch_bounds__(kMaxTeam, 2)
+__global__ void __launch_bounds__(kMaxBwdTeam, 2)
     block_norm_bwd_kernel(const __grid_constant__ BlockNormParams p,
                           const __grid_constant__ Shape s) {
+  constexpr int V = kBwdVectors;
   extern __shared__ __align__(16) char smem[];
   __shared__ float buf[2][2][16], far[2][2][kMaxCluster];
   const int thread = threadIdx.y * blockDim.x + threadIdx.x;
   const int threads = blockDim.x * blockDim.y;
   const int rank = blockIdx.x % s.cluster;
   RowSum row_sum{buf, far, s.cluster, rank, 0};
-  const int c = rank * s.cols + threadIdx.x * 8;
-  const bool mine = threadIdx.x * 8 < s.cols && c < p.W;
+  int c[V];
+  bool mine[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int at = (j * blockDim.x + threadIdx.x) * 8;
+    c[j] = rank * s.cols + at;
+    mine[j] = at < s.cols && c[j] < p.W;
+  }
   const bool heads = p.post && p.G != p.W;
   const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
-  const Weights weights{{reinterpret_cast<uint4*>(smem) + thread, threads}};
-  const Scratch scratch{reinterpret_cast<uint4*>(smem) + 4 * threads + thread, threads};
-  uint4* ring = reinterpret_cast<uint4*>(smem) + (GATE ? 6 : 4) * threads + thread;
-  const int stage = s.arrays * Slots<T>::M * threads;
   const bool use_res = p.pre && p.residual;  // y itself is needed by its norm alone
-  constexpr int kGate = 1, kRes = 1 + GATE;
+  // x in three stages, the others in two; a thread's vectors next to each other in an array
+  constexpr int M = Slots<T>::M;
+  const Weights weights{{reinterpret_cast<uint4*>(smem) + thread, threads}};
+  const Scratch scratch{reinterpret_cast<uint4*>(smem) + 4 * V * threads + thread, threads};
+  uint4* x_ring = reinterpret_cast<uint4*>(smem) + (GATE ? 6 : 4) * V * threads + thread;
+  const int vector = M * threads;  // uint4 of a vector of all threads
+  uint4* ring = x_ring + 3 * V * vector;
+  const int stage = (s.arrays - 1) * V * vector;
+  constexpr int kGate = 0, kRes = GATE;
   const int i_dy = kRes + use_res, i_dh = i_dy + (p.dy != nullptr);
 
-  if (mine) weights.fill(p, c);
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (mine[j]) weights.at_vector(j).fill(p, c[j]);
   if (s.cluster > 1) cluster_sync();
   const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
   const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
-  const auto fetch = [&](int64_t row, int at) {
-    if (mine && row < p.T) {
-      const Slots<T> to{ring + at * stage, threads};
-      to.fetch(0, static_cast<const T*>(p.x) + row * p.x_stride + c);
-      if (GATE) to.fetch(kGate, static_cast<const T*>(p.gate) + row * p.gate_stride + c);
-      if (use_res) to.fetch(kRes, static_cast<const T*>(p.residual) + row * p.W + c);
-      if (p.dy) to.fetch(i_dy, static_cast<const T*>(p.dy) + row * p.W + c);
-      if (p.pre) to.fetch(i_dh, static_cast<const T*>(p.dh) + row * p.W + c);
-    }
-    cp_async_commit();
+  const auto fetch_x = [&](int64_t row, int at) {
+    if (row >= p.T) return;
+    const T* src = static_cast<const T*>(p.x) + row * p.x_stride;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (mine[j]) Slots<T>{x_ring + (at * V + j) * vector, threads}.fetch(0, src + c[j]);
   };
-  uint64_t dwpost[4] = {}, dwpre[4] = {};
+  const auto fetch = [&](int64_t row, int at) {
+    if (row >= p.T) return;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (!mine[j]) continue;
+      uint4* to = ring + at * stage + j * vector;
+      const int64_t dense = row * p.W + c[j];
+      const auto copy = [&](int array, const void* src, int64_t from) {
+        Slots<T>{to + array * V * vector, threads}.fetch(0, static_cast<const T*>(src) + from);
+      };
+      if (GATE) copy(kGate, p.gate, row * p.gate_stride + c[j]);
+      if (use_res) copy(kRes, p.residual, dense);
+      if (p.dy) copy(i_dy, p.dy, dense);
+      if (p.pre) copy(i_dh, p.dh, dense);
+    }
+  };
+  uint64_t dwpost[V][4] = {}, dwpre[V][4] = {};
 
-  for (int i = 0; i < s.stages - 1; ++i) fetch(first + i * step, i);
-  int at = 0;
+  fetch_x(first, 0);
+  fetch(first, 0);
+  fetch_x(first + step, 1);
+  cp_async_commit();
+  cp_async_wait<0>();
+  float q[V];
+  const auto squares = [&](int at, int j) {  // of a vector, over its group where it has one
+    float sum = 0.f;
+    if (mine[j]) {
+      uint64_t x[4];
+      Slots<T>{x_ring + (at * V + j) * vector, threads}.read(0, x);
+      sum = dot8(x, x);
+    }
+    return heads ? lanes_sum(sum, p.G / 8) : sum;
+  };
+#pragma unroll
+  for (int j = 0; j < V; ++j) q[j] = 1.f;
+  if (p.post) {
+    float sum[1] = {0.f}, by[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum[0] += by[j] = squares(0, j);
+    if (!heads) row_sum(sum);
+#pragma unroll
+    for (int j = 0; j < V; ++j) q[j] = rsqrtf((heads ? by[j] : sum[0]) * per_group + p.eps);
+  }
+  int at = 0, x_at = 0;
   for (int64_t row = first; row < p.T; row += step) {
-    const int last = at == 0 ? s.stages - 1 : at - 1;
-    fetch(row + (s.stages - 1) * step, last);
-    wait_rows(s.stages - 1);
-    const Slots<T> in{ring + at * stage, threads};
-    at = at + 1 == s.stages ? 0 : at + 1;
+    const int x_next = x_at == 2 ? 0 : x_at + 1;
+    fetch(row + step, at ^ 1);
+    fetch_x(row + 2 * step, x_at == 0 ? 2 : x_at - 1);
+    cp_async_commit();
+    cp_async_wait<1>();  // this row, and the next one's x
+    const auto in = [&](int array, int j) {
+      return Slots<T>{ring + at * stage + (array * V + j) * vector, threads};
+    };
+    const auto x_in = [&](int j) { return Slots<T>{x_ring + (x_at * V + j) * vector, threads}; };
 
-    // What a sum separates is read again after it, rather than held: 64 registers a thread let an
-    // SM hold two rows of 4096.  Columns past the row's stay zero throughout.
-    float q = 1.f;
-    if (p.post) {
-      uint64_t x[4] = {};
-      if (mine) in.read(0, x);
-      float sum[1] = {dot8(x, x)};
-      if (heads) sum[0] = lanes_sum(sum[0], p.G / 8);
-      else row_sum(sum);
-      q = rsqrtf(sum[0] * per_group + p.eps);
-    }
-    const uint64_t qq = f2_dup(q);
-    if (GATE && mine) {
-      uint64_t z[4], sig[4] = {};
-      in.read(kGate, z);
-      sigmoid8(p.act, z, sig);
-      scratch.write(0, sig);
-    }
-    uint64_t g[4] = {};
+    // columns past the row's stay zero throughout
+    uint64_t g[V][4] = {};
     if (p.pre) {
-      uint64_t y[4] = {};
+      uint64_t y[V][4] = {};
       float sums[2] = {0.f, 0.f};
-      if (mine) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (!mine[j]) continue;
         uint64_t x[4], w[4], t[4];
-        if (use_res) in.read(kRes, y);
-        in.read(0, x);
-        weights.read(0, w);
+        if (use_res) in(kRes, j).read(0, y[j]);
+        x_in(j).read(0, x);
+        weights.at_vector(j).read(0, w);
         if (GATE) {
-          uint64_t sig[4];
-          in.read(kGate, t);
-          scratch.read(0, sig);
+          uint64_t sig[4] = {};
+          in(kGate, j).read(0, t);
+          sigmoid8(p.act, t, sig);
+          scratch.at_vector(j).write(0, sig);
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], activation(p.act, t[i], sig[i]));
         }
+        const uint64_t qq = f2_dup(q[j]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = f2_fma(x[i], f2_mul(w[i], qq), y[i]);
-        in.read(i_dh, t);
-        weights.read(1, w);
+        for (int i = 0; i < 4; ++i) y[j][i] = f2_fma(x[i], f2_mul(w[i], qq), y[j][i]);
+        in(i_dh, j).read(0, t);
+        weights.at_vector(j).read(1, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], t[i]);
-        sums[0] = dot8(y, y);
-        sums[1] = dot8(y, w);
+        sums[0] += dot8(y[j], y[j]);
+        sums[1] += dot8(y[j], w);
       }
       row_sum(sums);
       const float r = rsqrtf(sums[0] * per_row + p.eps);
       const uint64_t rr = f2_dup(r), back = f2_dup(-(sums[1] * per_row * r * r * r));
-      if (mine) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (!mine[j]) continue;
         uint64_t dh[4], w[4];
-        in.read(i_dh, dh);
-        if (p.dy) in.read(i_dy, g);
-        weights.read(1, w);
+        in(i_dh, j).read(0, dh);
+        if (p.dy) in(i_dy, j).read(0, g[j]);
+        weights.at_vector(j).read(1, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint64_t d = f2_mul(dh[i], rr);
-          dwpre[i] = f2_fma(d, y[i], dwpre[i]);
-          g[i] = f2_fma(y[i], back, f2_fma(d, w[i], g[i]));
+          dwpre[j][i] = f2_fma(d, y[j][i], dwpre[j][i]);
+          g[j][i] = f2_fma(y[j][i], back, f2_fma(d, w[i], g[j][i]));
         }
       }
-    } else if (mine) {
-      in.read(i_dy, g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (!mine[j]) continue;
+        in(i_dy, j).read(0, g[j]);
+        if (GATE) {
+          uint64_t z[4], sig[4] = {};
+          in(kGate, j).read(0, z);
+          sigmoid8(p.act, z, sig);
+          scratch.at_vector(j).write(0, sig);
+        }
+      }
     }
-    float dot[1] = {0.f};
-    if (mine) {
-      if (p.dres) store_pairs<T>(static_cast<T*>(p.dres) + row * p.W + c, g);
-      uint64_t x[4], w[4];
-      in.read(0, x);
-      weights.read(0, w);
-      if (GATE) {
-        uint64_t z[4], sig[4];
-        in.read(kGate, z);
-        scratch.read(0, sig);
+    float sums[2] = {0.f, 0.f}, dot[V], next[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      dot[j] = 0.f;
+      if (mine[j]) {
+        if (p.dres) store_pairs<T>(static_cast<T*>(p.dres) + row * p.W + c[j], g[j]);
+        uint64_t x[4], w[4];
+        x_in(j).read(0, x);
+        weights.at_vector(j).read(0, w);
+        const uint64_t qq = f2_dup(q[j]);
+        if (GATE) {
+          uint64_t z[4], sig[4];
+          in(kGate, j).read(0, z);
+          scratch.at_vector(j).read(0, sig);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint64_t n = f2_mul(x[i], f2_mul(w[i], qq));
+            const uint64_t a = activation(p.act, z[i], sig[i]);
+            z[i] = f2_mul(activation_slope(p.act, z[i], sig[i]), f2_mul(g[j][i], n));
+            g[j][i] = f2_mul(g[j][i], a);
+          }
+          store_pairs<T>(static_cast<T*>(p.dgate) + row * p.gate_stride + c[j], z);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint64_t n = f2_mul(x[i], f2_mul(w[i], qq));
-          const uint64_t a = activation(p.act, z[i], sig[i]);
-          z[i] = f2_mul(activation_slope(p.act, z[i], sig[i]), f2_mul(g[i], n));
-          g[i] = f2_mul(g[i], a);
+          dwpost[j][i] = f2_fma(g[j][i], f2_mul(x[i], qq), dwpost[j][i]);
+          g[j][i] = f2_mul(g[j][i], w[i]);
         }
-        store_pairs<T>(static_cast<T*>(p.dgate) + row * p.gate_stride + c, z);
+        if (p.post) dot[j] = dot8(x, g[j]);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        dwpost[i] = f2_fma(g[i], f2_mul(x[i], qq), dwpost[i]);
-        g[i] = f2_mul(g[i], w[i]);
+      if (p.post) {
+        if (heads) dot[j] = lanes_sum(dot[j], p.G / 8);
+        next[j] = row + step < p.T ? squares(x_next, j) : 0.f;
+        sums[0] += dot[j];
+        sums[1] += next[j];
       }
-      dot[0] = dot8(x, g);
     }
-    if (p.post) {
-      if (heads) dot[0] = lanes_sum(dot[0], p.G / 8);
-      else row_sum(dot);
-      const uint64_t back = f2_dup(-(dot[0] * per_group * q * q * q));
-      uint64_t x[4] = {};
-      if (mine) in.read(0, x);
+    if (p.post && !heads) row_sum(sums);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] = f2_fma(x[i], back, f2_mul(g[i], qq));
+    for (int j = 0; j < V; ++j) {
+      if (p.post) {
+        const float inner = heads ? dot[j] : sums[0];
+        const uint64_t qq = f2_dup(q[j]);
+        const uint64_t back = f2_dup(-(inner * per_group * q[j] * q[j] * q[j]));
+        uint64_t x[4] = {};
+        if (mine[j]) x_in(j).read(0, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[j][i] = f2_fma(x[i], back, f2_mul(g[j][i], qq));
+        q[j] = rsqrtf((heads ? next[j] : sums[1]) * per_group + p.eps);
+      }
+      if (mine[j]) store_pairs<T>(static_cast<T*>(p.dx) + row * p.x_stride + c[j], g[j]);
     }
-    if (mine) store_pairs<T>(static_cast<T*>(p.dx) + row * p.x_stride + c, g);
+    at ^= 1;
+    x_at = x_next;
   }
   if (s.cluster > 1) cluster_sync();
   pdl_launch_next();
   if (!p.part) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) dwpost[i] = f2_mul(dwpost[i], f2_dup(p.alpha));
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dwpost[j][i] = f2_mul(dwpost[j][i], f2_dup(p.alpha));
 
   // the CTA's sums: [CTAs][post columns], then [CTAs][W] before the next block
   const int wide = p.shared ? p.G : p.W;
   float* post = p.part + (int64_t)(p.shared ? blockIdx.x : blockIdx.x / s.cluster) * wide;
   float* pre = p.part + (int64_t)gridDim.x * wide + (int64_t)(blockIdx.x / s.cluster) * p.W;
   if (!p.shared && blockDim.y == 1) {
-    if (mine) {
-      store_pairs<float>(post + c, dwpost);
-      store_pairs<float>(pre + c, dwpre);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (mine[j]) {
+        store_pairs<float>(post + c[j], dwpost[j]);
+        store_pairs<float>(pre + c[j], dwpre[j]);
+      }
     }
     return;
   }
   float* sums = reinterpret_cast<float*>(smem);  // [teams][columns]
-  const int cols = blockDim.x * 8, from = rank * s.cols;
+  const int cols = blockDim.x * 8 * V, from = rank * s.cols;
   const int used = min(min(cols, s.cols), p.W - from);
   for (int kind = 0; kind < 2; ++kind) {
     __syncthreads();
-    store_pairs<float>(sums + thread * 8, kind ? dwpre : dwpost);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      store_pairs<float>(sums + threadIdx.y * cols + (j * blockDim.x + threadIdx.x) * 8,
+                         kind ? dwpre[j] : dwpost[j]);
     __syncthreads();
     const bool by_group = p.shared && !kind;
     const int n = by_group ? p.G : used;
@@ -505,23 +603,29 @@ __global__ void __launch_bounds__(1024)
 namespace {
 
 // The teams of a call on T rows of W elements, `arrays` inputs of `elem` bytes.
-Shape shape_for(int T, int W, int arrays, int elem, bool sigmoids, int num_sms) {
+Shape shape_for(int T, int W, int arrays, int elem, bool bwd, bool sigmoids, int num_sms) {
   Shape s = {};
   s.cluster = W <= kMaxCols ? 1 : W <= 2 * kMaxCols ? 2 : 4;
   // whole groups of up to 256 columns to a CTA
   s.cols = s.cluster == 1 ? W : (W / s.cluster + 255) / 256 * 256;
-  s.team = (s.cols + 255) / 256 * 32;
-  s.teams = s.team == 32 ? 8 : 1;
+  const int vectors = bwd ? kBwdVectors : 1;
+  s.team = (s.cols + 256 * vectors - 1) / (256 * vectors) * 32;
+  s.teams = s.team == 32 ? 8 / vectors : 1;
   s.arrays = arrays;
   const int threads = s.team * s.teams;
-  const int per_sm = threads > 256 ? 2 : threads > 128 ? 4 : 8;
-  const int most = (220 << 10) / per_sm - 2048;
-  const int weights = threads * (sigmoids ? 96 : 64), row = threads * 8 * elem * arrays;
-  s.stages = 2;
-  while (s.stages < 4 && weights + row * (s.stages + 1) <= most) ++s.stages;
-  s.smem = weights + row * s.stages;
+  const int per_sm = threads * vectors > 256 ? 2 : threads * vectors > 128 ? 4 : 8;
+  const int own = threads * vectors * (sigmoids ? 96 : 64), row = threads * vectors * 8 * elem;
+  if (bwd) {
+    s.smem = own + row * (3 + 2 * (arrays - 1));
+  } else {
+    const int most = (220 << 10) / per_sm - 2048;
+    s.stages = 2;
+    while (s.stages < 4 && own + row * arrays * (s.stages + 1) <= most) ++s.stages;
+    s.smem = own + row * arrays * s.stages;
+  }
+  const int fit = (226 << 10) / (s.smem + 2048);
   const int rows = (T + s.teams - 1) / s.teams;  // of a CTA or cluster at a time
-  const int clusters = per_sm * num_sms / s.cluster;
+  const int clusters = (fit < per_sm ? fit < 1 ? 1 : fit : per_sm) * num_sms / s.cluster;
   s.ctas = (rows < clusters ? rows : clusters) * s.cluster;
   return s;
 }
@@ -557,13 +661,13 @@ cudaError_t run(const BlockNormParams& p, const Shape& s, bool bwd, cudaStream_t
 cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
                               cudaStream_t stream) {
   if (p.T == 0) return cudaSuccess;
-  const Shape s = shape_for(p.T, p.W, arrays_of(p, false), bf16 ? 2 : 4, false, num_sms);
+  const Shape s = shape_for(p.T, p.W, arrays_of(p, false), bf16 ? 2 : 4, false, false, num_sms);
   note_launches(1);
   return bf16 ? run<__nv_bfloat16>(p, s, false, stream) : run<float>(p, s, false, stream);
 }
 
 int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms) {
-  return T ? shape_for(T, W, 1, bf16 ? 2 : 4, true, num_sms).ctas : 0;
+  return T ? shape_for(T, W, 1, bf16 ? 2 : 4, true, false, num_sms).ctas : 0;
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
@@ -573,7 +677,7 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_s
   Shape s = {};
   s.cluster = 1;
   if (p.T > 0) {
-    s = shape_for(p.T, p.W, arrays_of(p, true), bf16 ? 2 : 4, p.gate, num_sms);
+    s = shape_for(p.T, p.W, arrays_of(p, true), bf16 ? 2 : 4, true, p.gate, num_sms);
     note_launches(1);
     const cudaError_t e =
         bf16 ? run<__nv_bfloat16>(p, s, true, stream) : run<float>(p, s, true, stream);
