@@ -13,6 +13,11 @@ __device__ __forceinline__ void cp_async16(void* dst, const void* src, bool live
                : "memory");
 }
 
+// To a shared address.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 __device__ __forceinline__ void cp_async_commit() {
   asm volatile("cp.async.commit_group;" ::: "memory");
 }

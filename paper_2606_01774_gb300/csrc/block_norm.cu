@@ -27,7 +27,6 @@ namespace {
 
 constexpr int kMaxTeam = 512;                // threads of a CTA, eight elements each
 constexpr int kBwdVectors = 2;               // of eight elements per thread, backward
-constexpr int kMaxBwdTeam = kMaxTeam / kBwdVectors;
 constexpr int kMaxCols = 8 * kMaxTeam;       // columns of a CTA
 constexpr int kMaxCluster = 4;
 
@@ -172,33 +171,10 @@ struct Slots {
   }
 };
 
-// Eight fp32 values of a thread's own.
-struct Scratch {
+// A thread's own weights in shared memory: after the block (times alpha), before the next.
+struct Weights {
   uint4* at;
   int pieces;
-
-  __device__ __forceinline__ void write(int kind, const uint64_t (&x)[4]) const {
-    float f[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f2_split(x[i], f[2 * i], f[2 * i + 1]);
-    at[2 * kind * pieces] = Piece<float>::store(f);
-    at[(2 * kind + 1) * pieces] = Piece<float>::store(f + 4);
-  }
-  // of the thread's j-th vector
-  __device__ __forceinline__ Scratch at_vector(int j) const {
-    return {at + j * 2 * pieces, pieces};
-  }
-  __device__ __forceinline__ void read(int kind, uint64_t (&x)[4]) const {
-    const uint4 u[2] = {at[2 * kind * pieces], at[(2 * kind + 1) * pieces]};
-    load_pairs<float>(u, x);
-  }
-};
-
-// A thread's own weights in shared memory: after the block (times alpha), before the next.
-struct Weights : Scratch {
-  __device__ __forceinline__ Weights at_vector(int j) const {
-    return {{at + j * 4 * pieces, pieces}};
-  }
 
   __device__ __forceinline__ void fill(const BlockNormParams& p, int c) const {
 #pragma unroll
@@ -212,6 +188,10 @@ struct Weights : Scratch {
       reinterpret_cast<float4*>(at)[(2 + i) * pieces] = w;
     }
   }
+  __device__ __forceinline__ void read(int kind, uint64_t (&x)[4]) const {
+    const uint4 u[2] = {at[2 * kind * pieces], at[(2 * kind + 1) * pieces]};
+    load_pairs<float>(u, x);
+  }
 };
 
 __device__ __forceinline__ void wait_rows(int later) {
@@ -220,12 +200,10 @@ __device__ __forceinline__ void wait_rows(int later) {
   else cp_async_wait<1>();
 }
 
-// Shared memory of a CTA: weights (eight of each kind per thread), backward with a gate its
-// sigmoids, then stages x inputs.
 struct Shape {
   int team, teams, cluster, ctas;  // threads of a CTA's team, teams of a CTA, CTAs of a cluster
   int cols;                        // columns of a CTA
-  int arrays, stages;
+  int arrays, stages;              // forward: inputs, and rows in flight
   int smem;
 };
 
@@ -244,7 +222,7 @@ __global__ void __launch_bounds__(kMaxTeam, 2)
   const bool mine = threadIdx.x * 8 < s.cols && c < p.W;
   const bool heads = p.post && p.G != p.W;
   const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
-  const Weights weights{{reinterpret_cast<uint4*>(smem) + thread, threads}};
+  const Weights weights{reinterpret_cast<uint4*>(smem) + thread, threads};
   uint4* ring = reinterpret_cast<uint4*>(smem) + 4 * threads + thread;
   const int stage = s.arrays * Slots<T>::M * threads;
   constexpr int kGate = 1, kRes = 1 + GATE;
@@ -313,12 +291,54 @@ __global__ void __launch_bounds__(kMaxTeam, 2)
   if (s.cluster > 1) cluster_sync();  // none leaves while another may write to its memory
 }
 
+// The shared memory of a backward thread, in 16-byte units: its weights, x of three rows, the other
+// inputs of two.  Units lie THREADS apart, so that copies and reads of neighbouring threads
+// meet neighbouring units, at distances known to the compiler.
+template <typename T, bool GATE, int THREADS>
+struct Own {
+  static constexpr int V = kBwdVectors, M = Slots<T>::M;
+  static constexpr int kGate = 0, kRes = GATE, kDy = kRes + 1, kDh = kRes + 2, kInputs = kRes + 3;
+  static constexpr int kX = 4 * V, kRow = kX + 3 * V * M, kUnits = kRow + 2 * kInputs * V * M;
+  static constexpr int kUnit = 16 * THREADS;  // bytes from unit to unit
+
+  // after the block (kind 0), before the next (1)
+  static __device__ __forceinline__ uint32_t weight(uint32_t own, int kind, int j) {
+    return own + (kind * V + j) * 2 * kUnit;
+  }
+  static __device__ __forceinline__ uint32_t x(uint32_t own, int row, int j) {
+    return own + (kX + (row * V + j) * M) * kUnit;
+  }
+  static __device__ __forceinline__ uint32_t input(uint32_t own, int row, int array, int j) {
+    return own + (kRow + ((row * kInputs + array) * V + j) * M) * kUnit;
+  }
+  static __device__ __forceinline__ void fetch(uint32_t to, const T* src) {
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+      cp_async16(to + i * kUnit, reinterpret_cast<const uint4*>(src) + i);
+  }
+  template <typename U = T>
+  static __device__ __forceinline__ void read(uint32_t at, uint64_t (&v)[4]) {
+    constexpr int K = 8 / Piece<U>::N;
+    uint4 u[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(u[i].x), "=r"(u[i].y), "=r"(u[i].z), "=r"(u[i].w)
+                   : "r"(at + i * kUnit)
+                   : "memory");
+    load_pairs<U>(u, v);
+  }
+};
+
 // Sixteen elements of a row per thread, in two vectors of eight.  The sum of the next row's squares
-// goes along with this row's last sum, so x arrives a row ahead of the other inputs.
-template <typename T, bool GATE>
-__global__ void __launch_bounds__(kMaxBwdTeam, 2)
+// goes along with this row's last sum, so x arrives a row ahead of the other inputs.  What a sum
+// separates is read again after it, rather than held.  alpha enters by the rows' factors alone.
+// FULL: both norms over whole rows, a residual, and gradients at and of it (a block's end).
+template <typename T, bool GATE, bool FULL, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS)
     block_norm_bwd_kernel(const __grid_constant__ BlockNormParams p,
                           const __grid_constant__ Shape s) {
+  using O = Own<T, GATE, THREADS>;
   constexpr int V = kBwdVectors;
   extern __shared__ __align__(16) char smem[];
   __shared__ float buf[2][2][16], far[2][2][kMaxCluster];
@@ -326,6 +346,11 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
   const int threads = blockDim.x * blockDim.y;
   const int rank = blockIdx.x % s.cluster;
   RowSum row_sum{buf, far, s.cluster, rank, 0};
+  const uint32_t own = (uint32_t)__cvta_generic_to_shared(smem) + thread * 16;
+  // columns past the row's hold zeros throughout
+  uint4* units = reinterpret_cast<uint4*>(smem) + thread;
+#pragma unroll 1
+  for (int i = 0; i < O::kUnits; ++i) units[i * THREADS] = make_uint4(0, 0, 0, 0);
   int c[V];
   bool mine[V];
 #pragma unroll
@@ -333,24 +358,20 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
     const int at = (j * blockDim.x + threadIdx.x) * 8;
     c[j] = rank * s.cols + at;
     mine[j] = at < s.cols && c[j] < p.W;
+    if (!mine[j]) continue;
+    for (int i = 0; i < 2; ++i) {
+      float4* to = reinterpret_cast<float4*>(units + (2 * j + i) * THREADS);
+      const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
+      to[0] = p.wpost
+                  ? reinterpret_cast<const float4*>(p.wpost + (p.shared ? c[j] % p.G : c[j]))[i]
+                  : one;
+      to[2 * V * THREADS] = p.wpre ? reinterpret_cast<const float4*>(p.wpre + c[j])[i] : one;
+    }
   }
-  const bool heads = p.post && p.G != p.W;
+  const bool post_norm = FULL || p.post, pre_norm = FULL || p.pre;
+  const bool heads = !FULL && p.post && p.G != p.W;
   const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
-  const bool use_res = p.pre && p.residual;  // y itself is needed by its norm alone
-  // x in three stages, the others in two; a thread's vectors next to each other in an array
-  constexpr int M = Slots<T>::M;
-  const Weights weights{{reinterpret_cast<uint4*>(smem) + thread, threads}};
-  const Scratch scratch{reinterpret_cast<uint4*>(smem) + 4 * V * threads + thread, threads};
-  uint4* x_ring = reinterpret_cast<uint4*>(smem) + (GATE ? 6 : 4) * V * threads + thread;
-  const int vector = M * threads;  // uint4 of a vector of all threads
-  uint4* ring = x_ring + 3 * V * vector;
-  const int stage = (s.arrays - 1) * V * vector;
-  constexpr int kGate = 0, kRes = GATE;
-  const int i_dy = kRes + use_res, i_dh = i_dy + (p.dy != nullptr);
-
-#pragma unroll
-  for (int j = 0; j < V; ++j)
-    if (mine[j]) weights.at_vector(j).fill(p, c[j]);
+  const bool use_res = FULL || (p.pre && p.residual);  // y itself is needed by its norm alone
   if (s.cluster > 1) cluster_sync();
   const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
   const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
@@ -359,22 +380,21 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
     const T* src = static_cast<const T*>(p.x) + row * p.x_stride;
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (mine[j]) Slots<T>{x_ring + (at * V + j) * vector, threads}.fetch(0, src + c[j]);
+      if (mine[j]) O::fetch(O::x(own, at, j), src + c[j]);
   };
   const auto fetch = [&](int64_t row, int at) {
     if (row >= p.T) return;
+    const int64_t dense = row * p.W;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       if (!mine[j]) continue;
-      uint4* to = ring + at * stage + j * vector;
-      const int64_t dense = row * p.W + c[j];
       const auto copy = [&](int array, const void* src, int64_t from) {
-        Slots<T>{to + array * V * vector, threads}.fetch(0, static_cast<const T*>(src) + from);
+        O::fetch(O::input(own, at, array, j), static_cast<const T*>(src) + (from + c[j]));
       };
-      if (GATE) copy(kGate, p.gate, row * p.gate_stride + c[j]);
-      if (use_res) copy(kRes, p.residual, dense);
-      if (p.dy) copy(i_dy, p.dy, dense);
-      if (p.pre) copy(i_dh, p.dh, dense);
+      if (GATE) copy(O::kGate, p.gate, row * p.gate_stride);
+      if (use_res) copy(O::kRes, p.residual, dense);
+      if (FULL || p.dy) copy(O::kDy, p.dy, dense);
+      if (pre_norm) copy(O::kDh, p.dh, dense);
     }
   };
   uint64_t dwpost[V][4] = {}, dwpre[V][4] = {};
@@ -384,19 +404,16 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
   fetch_x(first + step, 1);
   cp_async_commit();
   cp_async_wait<0>();
-  float q[V];
   const auto squares = [&](int at, int j) {  // of a vector, over its group where it has one
-    float sum = 0.f;
-    if (mine[j]) {
-      uint64_t x[4];
-      Slots<T>{x_ring + (at * V + j) * vector, threads}.read(0, x);
-      sum = dot8(x, x);
-    }
+    uint64_t x[4];
+    O::read(O::x(own, at, j), x);
+    const float sum = dot8(x, x);
     return heads ? lanes_sum(sum, p.G / 8) : sum;
   };
+  float q[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) q[j] = 1.f;
-  if (p.post) {
+  if (post_norm) {
     float sum[1] = {0.f}, by[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) sum[0] += by[j] = squares(0, j);
@@ -411,36 +428,29 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
     fetch_x(row + 2 * step, x_at == 0 ? 2 : x_at - 1);
     cp_async_commit();
     cp_async_wait<1>();  // this row, and the next one's x
-    const auto in = [&](int array, int j) {
-      return Slots<T>{ring + at * stage + (array * V + j) * vector, threads};
-    };
-    const auto x_in = [&](int j) { return Slots<T>{x_ring + (x_at * V + j) * vector, threads}; };
 
-    // columns past the row's stay zero throughout
-    uint64_t g[V][4] = {};
-    if (p.pre) {
-      uint64_t y[V][4] = {};
+    uint64_t g[V][4];
+    if (pre_norm) {
+      uint64_t y[V][4];
       float sums[2] = {0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        if (!mine[j]) continue;
         uint64_t x[4], w[4], t[4];
-        if (use_res) in(kRes, j).read(0, y[j]);
-        x_in(j).read(0, x);
-        weights.at_vector(j).read(0, w);
+        O::read(O::input(own, at, O::kRes, j), y[j]);  // zeros where there is none
+        O::read(O::x(own, x_at, j), x);
+        O::template read<float>(O::weight(own, 0, j), w);
         if (GATE) {
-          uint64_t sig[4] = {};
-          in(kGate, j).read(0, t);
+          uint64_t sig[4];
+          O::read(O::input(own, at, O::kGate, j), t);
           sigmoid8(p.act, t, sig);
-          scratch.at_vector(j).write(0, sig);
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], activation(p.act, t[i], sig[i]));
         }
-        const uint64_t qq = f2_dup(q[j]);
+        const uint64_t qa = f2_dup(q[j] * p.alpha);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[j][i] = f2_fma(x[i], f2_mul(w[i], qq), y[j][i]);
-        in(i_dh, j).read(0, t);
-        weights.at_vector(j).read(1, w);
+        for (int i = 0; i < 4; ++i) y[j][i] = f2_fma(x[i], f2_mul(w[i], qa), y[j][i]);
+        O::read(O::input(own, at, O::kDh, j), t);
+        O::template read<float>(O::weight(own, 1, j), w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], t[i]);
         sums[0] += dot8(y[j], y[j]);
@@ -451,11 +461,10 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
       const uint64_t rr = f2_dup(r), back = f2_dup(-(sums[1] * per_row * r * r * r));
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        if (!mine[j]) continue;
         uint64_t dh[4], w[4];
-        in(i_dh, j).read(0, dh);
-        if (p.dy) in(i_dy, j).read(0, g[j]);
-        weights.at_vector(j).read(1, w);
+        O::read(O::input(own, at, O::kDh, j), dh);
+        O::read(O::input(own, at, O::kDy, j), g[j]);
+        O::template read<float>(O::weight(own, 1, j), w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint64_t d = f2_mul(dh[i], rr);
@@ -465,68 +474,61 @@ __global__ void __launch_bounds__(kMaxBwdTeam, 2)
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (!mine[j]) continue;
-        in(i_dy, j).read(0, g[j]);
-        if (GATE) {
-          uint64_t z[4], sig[4] = {};
-          in(kGate, j).read(0, z);
-          sigmoid8(p.act, z, sig);
-          scratch.at_vector(j).write(0, sig);
-        }
-      }
+      for (int j = 0; j < V; ++j) O::read(O::input(own, at, O::kDy, j), g[j]);
     }
     float sums[2] = {0.f, 0.f}, dot[V], next[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      dot[j] = 0.f;
-      if (mine[j]) {
-        if (p.dres) store_pairs<T>(static_cast<T*>(p.dres) + row * p.W + c[j], g[j]);
-        uint64_t x[4], w[4];
-        x_in(j).read(0, x);
-        weights.at_vector(j).read(0, w);
-        const uint64_t qq = f2_dup(q[j]);
-        if (GATE) {
-          uint64_t z[4], sig[4];
-          in(kGate, j).read(0, z);
-          scratch.at_vector(j).read(0, sig);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint64_t n = f2_mul(x[i], f2_mul(w[i], qq));
-            const uint64_t a = activation(p.act, z[i], sig[i]);
-            z[i] = f2_mul(activation_slope(p.act, z[i], sig[i]), f2_mul(g[j][i], n));
-            g[j][i] = f2_mul(g[j][i], a);
-          }
-          store_pairs<T>(static_cast<T*>(p.dgate) + row * p.gate_stride + c[j], z);
-        }
+      if ((FULL || p.dres) && mine[j]) store_pairs<T>(static_cast<T*>(p.dres) + (row * p.W + c[j]), g[j]);
+      uint64_t x[4], w[4];
+      O::read(O::x(own, x_at, j), x);
+      O::template read<float>(O::weight(own, 0, j), w);
+      const uint64_t qq = f2_dup(q[j]);
+      if (GATE) {
+        uint64_t z[4], sig[4];
+        O::read(O::input(own, at, O::kGate, j), z);
+        sigmoid8(p.act, z, sig);
+        const uint64_t qa = f2_dup(q[j] * p.alpha);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          dwpost[j][i] = f2_fma(g[j][i], f2_mul(x[i], qq), dwpost[j][i]);
-          g[j][i] = f2_mul(g[j][i], w[i]);
+          const uint64_t n = f2_mul(x[i], f2_mul(w[i], qa));
+          const uint64_t a = activation(p.act, z[i], sig[i]);
+          z[i] = f2_mul(activation_slope(p.act, z[i], sig[i]), f2_mul(g[j][i], n));
+          g[j][i] = f2_mul(g[j][i], a);
         }
-        if (p.post) dot[j] = dot8(x, g[j]);
+        if (mine[j])
+          store_pairs<T>(static_cast<T*>(p.dgate) + (row * p.gate_stride + c[j]), z);
       }
-      if (p.post) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        dwpost[j][i] = f2_fma(g[j][i], f2_mul(x[i], qq), dwpost[j][i]);
+        g[j][i] = f2_mul(g[j][i], w[i]);
+      }
+      if (post_norm) {
+        dot[j] = dot8(x, g[j]);
         if (heads) dot[j] = lanes_sum(dot[j], p.G / 8);
         next[j] = row + step < p.T ? squares(x_next, j) : 0.f;
         sums[0] += dot[j];
         sums[1] += next[j];
       }
     }
-    if (p.post && !heads) row_sum(sums);
+    if (post_norm && !heads) row_sum(sums);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (p.post) {
+      const float qa = q[j] * p.alpha;
+      if (post_norm) {
         const float inner = heads ? dot[j] : sums[0];
-        const uint64_t qq = f2_dup(q[j]);
-        const uint64_t back = f2_dup(-(inner * per_group * q[j] * q[j] * q[j]));
-        uint64_t x[4] = {};
-        if (mine[j]) x_in(j).read(0, x);
+        const uint64_t back = f2_dup(-(inner * per_group * qa * q[j] * q[j]));
+        uint64_t x[4];
+        O::read(O::x(own, x_at, j), x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[j][i] = f2_fma(x[i], back, f2_mul(g[j][i], qq));
+        for (int i = 0; i < 4; ++i) g[j][i] = f2_fma(x[i], back, f2_mul(g[j][i], f2_dup(qa)));
         q[j] = rsqrtf((heads ? next[j] : sums[1]) * per_group + p.eps);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[j][i] = f2_mul(g[j][i], f2_dup(qa));
       }
-      if (mine[j]) store_pairs<T>(static_cast<T*>(p.dx) + row * p.x_stride + c[j], g[j]);
+      if (mine[j]) store_pairs<T>(static_cast<T*>(p.dx) + (row * p.x_stride + c[j]), g[j]);
     }
     at ^= 1;
     x_at = x_next;
@@ -602,43 +604,55 @@ __global__ void __launch_bounds__(1024)
 
 namespace {
 
-// The teams of a call on T rows of W elements, `arrays` inputs of `elem` bytes.
-Shape shape_for(int T, int W, int arrays, int elem, bool bwd, bool sigmoids, int num_sms) {
+// The teams of a call on T rows of W elements.
+Shape teams_for(int W, int vectors) {
   Shape s = {};
   s.cluster = W <= kMaxCols ? 1 : W <= 2 * kMaxCols ? 2 : 4;
   // whole groups of up to 256 columns to a CTA
   s.cols = s.cluster == 1 ? W : (W / s.cluster + 255) / 256 * 256;
-  const int vectors = bwd ? kBwdVectors : 1;
   s.team = (s.cols + 256 * vectors - 1) / (256 * vectors) * 32;
   s.teams = s.team == 32 ? 8 / vectors : 1;
-  s.arrays = arrays;
-  const int threads = s.team * s.teams;
-  const int per_sm = threads * vectors > 256 ? 2 : threads * vectors > 128 ? 4 : 8;
-  const int own = threads * vectors * (sigmoids ? 96 : 64), row = threads * vectors * 8 * elem;
-  if (bwd) {
-    s.smem = own + row * (3 + 2 * (arrays - 1));
-  } else {
-    const int most = (220 << 10) / per_sm - 2048;
-    s.stages = 2;
-    while (s.stages < 4 && own + row * arrays * (s.stages + 1) <= most) ++s.stages;
-    s.smem = own + row * arrays * s.stages;
-  }
-  const int fit = (226 << 10) / (s.smem + 2048);
-  const int rows = (T + s.teams - 1) / s.teams;  // of a CTA or cluster at a time
-  const int clusters = (fit < per_sm ? fit < 1 ? 1 : fit : per_sm) * num_sms / s.cluster;
-  s.ctas = (rows < clusters ? rows : clusters) * s.cluster;
   return s;
 }
 
-int arrays_of(const BlockNormParams& p, bool bwd) {
-  return 1 + (p.gate != nullptr) + (p.residual && (!bwd || p.pre)) +
-         (bwd ? (p.dy != nullptr) + p.pre : 0);
+// One CTA or cluster per row until every SM has as many as it holds.
+void set_ctas(Shape& s, int T, int per_sm, int num_sms) {
+  const int fit = (226 << 10) / (s.smem + 2048);
+  per_sm = fit < 1 ? 1 : fit < per_sm ? fit : per_sm;
+  const int rows = (T + s.teams - 1) / s.teams, clusters = per_sm * num_sms / s.cluster;
+  s.ctas = (rows < clusters ? rows : clusters) * s.cluster;
 }
 
-template <typename T>
-cudaError_t run(const BlockNormParams& p, const Shape& s, bool bwd, cudaStream_t stream) {
-  const auto kernel = bwd ? p.gate ? block_norm_bwd_kernel<T, true> : block_norm_bwd_kernel<T, false>
-                          : p.gate ? block_norm_kernel<T, true> : block_norm_kernel<T, false>;
+Shape forward_shape(const BlockNormParams& p, bool bf16, int num_sms) {
+  Shape s = teams_for(p.W, 1);
+  const int threads = s.team * s.teams;
+  const int per_sm = threads > 256 ? 2 : threads > 128 ? 4 : 8;
+  s.arrays = 1 + (p.gate != nullptr) + (p.residual != nullptr);
+  // weights, and as many rows as there is room for
+  const int own = threads * 64, row = threads * (bf16 ? 16 : 32) * s.arrays;
+  const int most = (220 << 10) / per_sm - 2048;
+  s.stages = 2;
+  while (s.stages < 4 && own + row * (s.stages + 1) <= most) ++s.stages;
+  s.smem = own + row * s.stages;
+  set_ctas(s, p.T, per_sm, num_sms);
+  return s;
+}
+
+// Threads whose shared memory a backward CTA has room for.
+int backward_threads(const Shape& s) { return s.team * s.teams <= 128 ? 128 : 256; }
+
+Shape backward_shape(int T, int W, bool gate, bool bf16, int num_sms) {
+  Shape s = teams_for(W, kBwdVectors);
+  const int units =
+      bf16 ? gate ? Own<__nv_bfloat16, true, 1>::kUnits : Own<__nv_bfloat16, false, 1>::kUnits
+           : gate ? Own<float, true, 1>::kUnits : Own<float, false, 1>::kUnits;
+  s.smem = backward_threads(s) * 16 * units;
+  set_ctas(s, T, 512 / backward_threads(s), num_sms);
+  return s;
+}
+
+cudaError_t run(void (*kernel)(BlockNormParams, Shape), const BlockNormParams& p, const Shape& s,
+                cudaStream_t stream) {
   cudaError_t e =
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
   if (e != cudaSuccess) return e;
@@ -656,18 +670,40 @@ cudaError_t run(const BlockNormParams& p, const Shape& s, bool bwd, cudaStream_t
   return cudaLaunchKernelEx(&cfg, kernel, p, s);
 }
 
+template <typename T>
+cudaError_t run_forward(const BlockNormParams& p, const Shape& s, cudaStream_t stream) {
+  return run(p.gate ? block_norm_kernel<T, true> : block_norm_kernel<T, false>, p, s, stream);
+}
+
+template <typename T, bool GATE, bool FULL>
+cudaError_t run_backward(const BlockNormParams& p, const Shape& s, cudaStream_t stream) {
+  return run(backward_threads(s) == 128 ? block_norm_bwd_kernel<T, GATE, FULL, 128>
+                                        : block_norm_bwd_kernel<T, GATE, FULL, 256>,
+             p, s, stream);
+}
+
+template <typename T>
+cudaError_t run_backward(const BlockNormParams& p, const Shape& s, cudaStream_t stream) {
+  const bool full = p.post && p.pre && p.G == p.W && p.residual && p.dy && p.dres;
+  if (p.gate)
+    return full ? run_backward<T, true, true>(p, s, stream)
+                : run_backward<T, true, false>(p, s, stream);
+  return full ? run_backward<T, false, true>(p, s, stream)
+              : run_backward<T, false, false>(p, s, stream);
+}
+
 }  // namespace
 
 cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
                               cudaStream_t stream) {
   if (p.T == 0) return cudaSuccess;
-  const Shape s = shape_for(p.T, p.W, arrays_of(p, false), bf16 ? 2 : 4, false, false, num_sms);
+  const Shape s = forward_shape(p, bf16, num_sms);
   note_launches(1);
-  return bf16 ? run<__nv_bfloat16>(p, s, false, stream) : run<float>(p, s, false, stream);
+  return bf16 ? run_forward<__nv_bfloat16>(p, s, stream) : run_forward<float>(p, s, stream);
 }
 
 int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms) {
-  return T ? shape_for(T, W, 1, bf16 ? 2 : 4, true, false, num_sms).ctas : 0;
+  return T ? backward_shape(T, W, false, bf16, num_sms).ctas : 0;  // a gate only makes it fewer
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
@@ -677,10 +713,10 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_s
   Shape s = {};
   s.cluster = 1;
   if (p.T > 0) {
-    s = shape_for(p.T, p.W, arrays_of(p, true), bf16 ? 2 : 4, true, p.gate, num_sms);
+    s = backward_shape(p.T, p.W, p.gate != nullptr, bf16, num_sms);
     note_launches(1);
     const cudaError_t e =
-        bf16 ? run<__nv_bfloat16>(p, s, true, stream) : run<float>(p, s, true, stream);
+        bf16 ? run_backward<__nv_bfloat16>(p, s, stream) : run_backward<float>(p, s, stream);
     if (e != cudaSuccess) return e;
   }
   if (weights) {  // of no rows: zeros
