@@ -1085,8 +1085,8 @@ flare_status flare_block_norm_bwd_workspace_size(const flare_block_norm_desc* d,
   flare_status st = check_block_norm(d);
   if (st != FLARE_OK) return st;
   if (!bytes) return FLARE_ERR_INVALID_ARGUMENT;
-  *bytes = (size_t)block_norm_bwd_ctas(d->num_tokens, d->width, d->act_dtype == FLARE_DT_BF16,
-                                       device_sms()) * 2 * d->width * sizeof(float);
+  *bytes = (size_t)block_norm_bwd_ctas(d->num_tokens, d->width, d->pre_norm,
+                                       d->act_dtype == FLARE_DT_BF16, device_sms()) * 2 * d->width * sizeof(float);
   return FLARE_OK;
 }
 

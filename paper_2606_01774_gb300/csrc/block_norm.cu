@@ -294,10 +294,11 @@ __global__ void __launch_bounds__(kMaxTeam, 2)
 // The shared memory of a backward thread, in 16-byte units: its weights, x of three rows, the other
 // inputs of two.  Units lie THREADS apart, so that copies and reads of neighbouring threads
 // meet neighbouring units, at distances known to the compiler.
-template <typename T, bool GATE, int THREADS>
+template <typename T, bool GATE, bool PRE, int THREADS>
 struct Own {
   static constexpr int V = kBwdVectors, M = Slots<T>::M;
-  static constexpr int kGate = 0, kRes = GATE, kDy = kRes + 1, kDh = kRes + 2, kInputs = kRes + 3;
+  static constexpr int kGate = 0, kDy = GATE, kRes = kDy + 1, kDh = kDy + 2;
+  static constexpr int kInputs = kDy + (PRE ? 3 : 1);
   static constexpr int kX = 4 * V, kRow = kX + 3 * V * M, kUnits = kRow + 2 * kInputs * V * M;
   static constexpr int kUnit = 16 * THREADS;  // bytes from unit to unit
 
@@ -333,12 +334,19 @@ struct Own {
 // Sixteen elements of a row per thread, in two vectors of eight.  The sum of the next row's squares
 // goes along with this row's last sum, so x arrives a row ahead of the other inputs.  What a sum
 // separates is read again after it, rather than held.  alpha enters by the rows' factors alone.
-// FULL: both norms over whole rows, a residual, and gradients at and of it (a block's end).
-template <typename T, bool GATE, bool FULL, int THREADS>
+// What a call has, where the compiler knows it.
+enum Form {
+  kAny,
+  kBlock,  // both norms over whole rows, a residual, and gradients at and of it: a block's end
+  kOutput  // no norm before the next block: a layer's output stage
+};
+
+template <typename T, bool GATE, int FORM, int THREADS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS)
     block_norm_bwd_kernel(const __grid_constant__ BlockNormParams p,
                           const __grid_constant__ Shape s) {
-  using O = Own<T, GATE, THREADS>;
+  constexpr bool FULL = FORM == kBlock;
+  using O = Own<T, GATE, FORM != kOutput, THREADS>;
   constexpr int V = kBwdVectors;
   extern __shared__ __align__(16) char smem[];
   __shared__ float buf[2][2][16], far[2][2][kMaxCluster];
@@ -368,10 +376,10 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
       to[2 * V * THREADS] = p.wpre ? reinterpret_cast<const float4*>(p.wpre + c[j])[i] : one;
     }
   }
-  const bool post_norm = FULL || p.post, pre_norm = FULL || p.pre;
+  const bool post_norm = FULL || p.post, pre_norm = FULL || (FORM == kAny && p.pre);
   const bool heads = !FULL && p.post && p.G != p.W;
   const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
-  const bool use_res = FULL || (p.pre && p.residual);  // y itself is needed by its norm alone
+  const bool use_res = FULL || (pre_norm && p.residual);  // y itself is needed by its norm alone
   if (s.cluster > 1) cluster_sync();
   const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
   const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
@@ -641,11 +649,19 @@ Shape forward_shape(const BlockNormParams& p, bool bf16, int num_sms) {
 // Threads whose shared memory a backward CTA has room for.
 int backward_threads(const Shape& s) { return s.team * s.teams <= 128 ? 128 : 256; }
 
-Shape backward_shape(int T, int W, bool gate, bool bf16, int num_sms) {
+template <typename T, bool GATE, bool PRE>
+constexpr int units_of() {
+  return Own<T, GATE, PRE, 1>::kUnits;
+}
+
+Shape backward_shape(int T, int W, bool gate, bool pre, bool bf16, int num_sms) {
+  using B = __nv_bfloat16;
   Shape s = teams_for(W, kBwdVectors);
-  const int units =
-      bf16 ? gate ? Own<__nv_bfloat16, true, 1>::kUnits : Own<__nv_bfloat16, false, 1>::kUnits
-           : gate ? Own<float, true, 1>::kUnits : Own<float, false, 1>::kUnits;
+  const int units = bf16 ? pre ? gate ? units_of<B, true, true>() : units_of<B, false, true>()
+                               : gate ? units_of<B, true, false>() : units_of<B, false, false>()
+                         : pre ? gate ? units_of<float, true, true>() : units_of<float, false, true>()
+                               : gate ? units_of<float, true, false>()
+                                      : units_of<float, false, false>();
   s.smem = backward_threads(s) * 16 * units;
   set_ctas(s, T, 512 / backward_threads(s), num_sms);
   return s;
@@ -675,21 +691,24 @@ cudaError_t run_forward(const BlockNormParams& p, const Shape& s, cudaStream_t s
   return run(p.gate ? block_norm_kernel<T, true> : block_norm_kernel<T, false>, p, s, stream);
 }
 
-template <typename T, bool GATE, bool FULL>
+template <typename T, bool GATE, int FORM>
 cudaError_t run_backward(const BlockNormParams& p, const Shape& s, cudaStream_t stream) {
-  return run(backward_threads(s) == 128 ? block_norm_bwd_kernel<T, GATE, FULL, 128>
-                                        : block_norm_bwd_kernel<T, GATE, FULL, 256>,
+  return run(backward_threads(s) == 128 ? block_norm_bwd_kernel<T, GATE, FORM, 128>
+                                        : block_norm_bwd_kernel<T, GATE, FORM, 256>,
              p, s, stream);
+}
+
+template <typename T, bool GATE>
+cudaError_t run_backward(const BlockNormParams& p, const Shape& s, cudaStream_t stream) {
+  if (!p.pre) return run_backward<T, GATE, kOutput>(p, s, stream);
+  if (p.post && p.G == p.W && p.residual && p.dy && p.dres)
+    return run_backward<T, GATE, kBlock>(p, s, stream);
+  return run_backward<T, GATE, kAny>(p, s, stream);
 }
 
 template <typename T>
 cudaError_t run_backward(const BlockNormParams& p, const Shape& s, cudaStream_t stream) {
-  const bool full = p.post && p.pre && p.G == p.W && p.residual && p.dy && p.dres;
-  if (p.gate)
-    return full ? run_backward<T, true, true>(p, s, stream)
-                : run_backward<T, true, false>(p, s, stream);
-  return full ? run_backward<T, false, true>(p, s, stream)
-              : run_backward<T, false, false>(p, s, stream);
+  return p.gate ? run_backward<T, true>(p, s, stream) : run_backward<T, false>(p, s, stream);
 }
 
 }  // namespace
@@ -702,8 +721,9 @@ cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
   return bf16 ? run_forward<__nv_bfloat16>(p, s, stream) : run_forward<float>(p, s, stream);
 }
 
-int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms) {
-  return T ? backward_shape(T, W, false, bf16, num_sms).ctas : 0;  // a gate only makes it fewer
+int block_norm_bwd_ctas(int T, int W, bool pre, bool bf16, int num_sms) {
+  // a gate only makes it fewer
+  return T ? backward_shape(T, W, false, pre, bf16, num_sms).ctas : 0;
 }
 
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
@@ -713,7 +733,7 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_s
   Shape s = {};
   s.cluster = 1;
   if (p.T > 0) {
-    s = backward_shape(p.T, p.W, p.gate != nullptr, bf16, num_sms);
+    s = backward_shape(p.T, p.W, p.gate != nullptr, p.pre, bf16, num_sms);
     note_launches(1);
     const cudaError_t e =
         bf16 ? run_backward<__nv_bfloat16>(p, s, stream) : run_backward<float>(p, s, stream);

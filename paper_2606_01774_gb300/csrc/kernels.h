@@ -299,7 +299,7 @@ struct BlockNormParams {
 cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
                               cudaStream_t stream);
 // CTAs of the backward pass: each leaves one partial weight gradient.
-int block_norm_bwd_ctas(int T, int W, bool bf16, int num_sms);
+int block_norm_bwd_ctas(int T, int W, bool pre, bool bf16, int num_sms);
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
                                   cudaStream_t stream);
 
