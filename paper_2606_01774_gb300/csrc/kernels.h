@@ -298,7 +298,13 @@ struct BlockNormParams {
 };
 cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
                               cudaStream_t stream);
-// CTAs of the backward pass: each leaves one partial weight gradient.
+// The backward pass over rows (T of bf16 or fp32) and how many CTAs it takes at most: each
+// leaves one partial weight gradient.
+template <typename T>
+cudaError_t launch_block_norm_rows(const BlockNormParams& p, int num_sms, int* ctas, int* cluster,
+                                   cudaStream_t stream);
+template <typename T>
+int block_norm_rows_ctas(int T_rows, int W, bool pre, int num_sms);
 int block_norm_bwd_ctas(int T, int W, bool pre, bool bf16, int num_sms);
 cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_sms,
                                   cudaStream_t stream);
