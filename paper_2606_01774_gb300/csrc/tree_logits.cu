@@ -17,33 +17,145 @@ namespace flare {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr uint32_t kPrompt = 1u << 31;  // seen in the history ahead of the output; below: count
+constexpr int kCtas = 3;                 // of an SM
+constexpr int kRows = 3;                 // rows in flight per thread
+constexpr int kScan = 8;                 // pieces of the history in flight per thread, four tokens each
+constexpr uint32_t kPrompt = 1u << 31;   // seen in the history ahead of the output; below: count
 
 // Index of chunk token i: the eight tokens of a thread's piece, eight threads on, lie in
 // banks of their own.
-__device__ __forceinline__ int at(int i) { return i + (i >> 5); }
-
-__device__ __forceinline__ float penalised(float x, bool seen, float rep, float rep_inv) {
-  return seen ? (x > 0.f ? x * rep_inv : x * rep) : x;
-}
+__host__ __device__ __forceinline__ int at(int i) { return i + (i >> 5); }
 
 __device__ __forceinline__ float minus_inf() { return __int_as_float(0xff800000); }
 
+// Bits i .. i + 31 of a bit array (which ends with a word to spare).
+__device__ __forceinline__ uint32_t bits_at(const uint32_t* bits, int i) {
+  return __funnelshift_r(bits[i >> 5], bits[(i >> 5) + 1], i & 31);
+}
+
+// A piece's words where its tokens are allowed, by their bits: ones, else zeros.
+template <typename T>
+__device__ __forceinline__ uint4 keep_words(uint32_t allowed) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (sizeof(T) == 2)
+      w[i] = (allowed >> (2 * i) & 1 ? 0xffffu : 0u) | (allowed >> (2 * i) & 2 ? 0xffff0000u : 0u);
+    else
+      w[i] = allowed >> i & 1 ? ~0u : 0u;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// `raw` with -inf where `keep` is zeros.
+template <typename T>
+__device__ __forceinline__ uint4 ruled_out(const uint4& raw, const uint4& keep) {
+  const uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+  return make_uint4((raw.x & keep.x) | (none & ~keep.x), (raw.y & keep.y) | (none & ~keep.y),
+                    (raw.z & keep.z) | (none & ~keep.z), (raw.w & keep.w) | (none & ~keep.w));
+}
+
+// What a piece's tokens get: y = x (x > 0 ? up : down) + add, which leaves what is neither seen
+// nor has a summand as it is (x + -0 is x, for both zeros).
+template <int E>
+struct Change {
+  float up[E], down[E], add[E];
+};
+
+// A request's penalties, and its history's counts and biases over a chunk of the vocabulary.
+struct Tables {
+  float rep, rep_inv, pres, freq;
+  const uint32_t* word;    // [at(chunk)] counts
+  const uint32_t* biased;  // [chunk / 32] bits: tokens with a bias
+  const uint32_t* before;  // [chunk / 32] how many bits are set in the words before
+  const float* bias;       // of the tokens with one, in order
+
+  __device__ __forceinline__ float bias_of(int e) const {
+    const uint32_t w = biased[e >> 5], bit = 1u << (e & 31);
+    return w & bit ? bias[before[e >> 5] + __popc(w & (bit - 1))] : 0.f;
+  }
+
+  // Of token e of the chunk.
+  __device__ __forceinline__ void one(int e, float& up, float& down, float& add) const {
+    const uint32_t w = word[at(e)], c = w & ~kPrompt;
+    up = w ? rep_inv : 1.f;
+    down = w ? rep : 1.f;
+    add = c ? -freq * (float)c - pres : -0.f;
+    if (biased[e >> 5] >> (e & 31) & 1) add += bias_of(e);
+  }
+  template <int E>
+  __device__ __forceinline__ void piece(int e, uint32_t touched, Change<E>& ch) const {
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      ch.up[k] = ch.down[k] = 1.f;
+      ch.add[k] = -0.f;
+      if (touched >> k & 1) one(e + k, ch.up[k], ch.down[k], ch.add[k]);
+    }
+  }
+};
+
+template <typename T, int E>
+__device__ __forceinline__ uint4 changed(const uint4& raw, const Change<E>& ch) {
+  float x[E];
+  Piece<T>::load(raw, x);
+#pragma unroll
+  for (int k = 0; k < E; ++k) x[k] = fmaf(x[k], x[k] > 0.f ? ch.up[k] : ch.down[k], ch.add[k]);
+  return Piece<T>::store(x);
+}
+
+// A piece of ROWS rows: taken in, then changed, ruled out and put back.
+template <typename T, int ROWS, bool MASK, bool IN_PLACE>
+struct Batch {
+  static constexpr int E = Piece<T>::N;
+  static constexpr uint32_t kAll = (1u << E) - 1;
+  uint4 raw[ROWS];
+  uint32_t allowed[ROWS];
+
+  // `bits`: the mask's byte of the piece in the first row, `nibble` where in it the bits start.
+  __device__ __forceinline__ void load(const T* src, size_t V, const uint8_t* bits,
+                                       size_t mask_bytes, int nibble, uint32_t touched) {
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      allowed[u] = MASK ? bits[u * mask_bytes] : kAll;
+      if (MASK && E == 4) allowed[u] = allowed[u] >> nibble & kAll;
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u)  // in place what stays as it is stays there
+      if (!IN_PLACE || touched || allowed[u] != kAll)
+        raw[u] = *reinterpret_cast<const uint4*>(src + u * V);
+  }
+  __device__ __forceinline__ void store(T* dst, size_t V, const uint4* keep_of, uint32_t touched,
+                                        const Change<E>& ch) {
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      if (IN_PLACE && !touched && allowed[u] == kAll) continue;
+      if (touched & allowed[u]) raw[u] = changed<T>(raw[u], ch);
+      if (MASK) raw[u] = ruled_out<T>(raw[u], keep_of[allowed[u]]);
+      *reinterpret_cast<uint4*>(dst + u * V) = raw[u];
+    }
+  }
+};
+
 }  // namespace
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads)
+// ALIGNED: every row starts on a 16-byte boundary, so that pieces are the same tokens in all.
+template <typename T, bool ALIGNED, bool MASK, bool IN_PLACE>
+__global__ void __launch_bounds__(kThreads, kCtas)
     tree_logits_kernel(const __grid_constant__ TreeLogitsParams p, int chunk, int chunks,
                        int row_parts) {
-  constexpr int E = 16 / sizeof(T);  // elements of a piece
-  extern __shared__ char smem[];
-  float* add = reinterpret_cast<float*>(smem);                     // [at(chunk)]
-  uint32_t* word = reinterpret_cast<uint32_t*>(smem);              // the same, while counting
-  uint32_t* seen = reinterpret_cast<uint32_t*>(add + at(chunk));   // [chunk / 32] bits
-  uint32_t* touched = seen + chunk / 32 + 1;  // seen, or with a summand (a word past the end: 0)
+  constexpr int E = Piece<T>::N;  // elements of a piece
+  constexpr uint32_t kAll = (1u << E) - 1;
+  extern __shared__ __align__(16) char smem[];
+  uint32_t* word = reinterpret_cast<uint32_t*>(smem);  // [at(chunk)] the history's counts
+  const int bit_words = chunk / 32 + 1;                // a word to spare
+  uint32_t* touched = word + at(chunk);  // bits: seen in the history or with a bias
+  uint32_t* held = touched + bit_words;  // the tree's own tokens, which come last
+  uint32_t* biased = held + bit_words;
+  uint32_t* before = biased + bit_words;  // see Tables
+  float* bias = reinterpret_cast<float*>(before + bit_words);  // [min(chunk, max_bias)]
   __shared__ uint64_t path[kMaxNodes];
   __shared__ int tok[kMaxNodes];
-  __shared__ uint32_t base[kMaxNodes];  // a node token's word
+  __shared__ uint4 keep_of[1 << E];  // keep_words
   __shared__ int tree_bad;
 
   const int tid = threadIdx.x, lane = tid & 31;
@@ -68,11 +180,39 @@ __global__ void __launch_bounds__(kThreads)
     return;
   }
   const bool tree = p.token != nullptr;
+  const int row_first = (int)((long long)n * part / row_parts);
+  const int row_last = (int)((long long)n * (part + 1) / row_parts);
+  const T* logits = static_cast<const T*>(p.logits) + (size_t)r * p.N * p.V + c0;
+  T* out = static_cast<T*>(p.out) + (size_t)r * p.N * p.V + c0;
 
-  for (int i = tid; i < at(chunk); i += kThreads) word[i] = 0;
+  // The history's first pieces are asked for ahead of the rows, which keep the memory busy.
+  const int32_t* hist = p.history ? p.history + (size_t)r * p.H : nullptr;
+  const bool quads = ((uintptr_t)hist & 15) == 0;
+  int4 text[kScan];
+  const auto take = [&](int i0) {  // a thread's tokens i0 .. i0 + 3, and so on a round further
+#pragma unroll
+    for (int j = 0; j < kScan; ++j) {
+      const int i = i0 + j * 4 * kThreads;
+      if (quads && i + 4 <= H) {
+        text[j] = *reinterpret_cast<const int4*>(hist + i);
+      } else {
+        text[j].x = i < H ? hist[i] : 0;
+        text[j].y = i + 1 < H ? hist[i + 1] : 0;
+        text[j].z = i + 2 < H ? hist[i + 2] : 0;
+        text[j].w = i + 3 < H ? hist[i + 3] : 0;
+      }
+    }
+  };
+  take(4 * tid);
+  for (int i = tid; i < (at(chunk) + 4 * bit_words + 3) / 4; i += kThreads)  // room for all of it
+    reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+  if (tid < 1 << E) keep_of[tid] = keep_words<T>(tid);
+
   if (tid < 32) {  // the tree's paths and tokens
     bool ok = true;
     if (tree) {
+      const int32_t* token = p.token + (size_t)r * p.N;
+      const int x0 = lane < n ? token[lane] : 0, x1 = lane + 32 < n ? token[lane + 32] : 0;
       int p0, p1;
       uint64_t a0, a1;
       ok = warp_load_tree(p.parent + (size_t)r * p.N, n, p0, p1);
@@ -81,11 +221,9 @@ __global__ void __launch_bounds__(kThreads)
         path[lane] = a0;
         path[lane + 32] = a1;
       }
-      for (int i = lane; i < n; i += 32) {
-        const int x = p.token[(size_t)r * p.N + i];
-        tok[i] = x;
-        ok = ok && x >= 0 && x < p.V;
-      }
+      tok[lane] = x0;
+      tok[lane + 32] = x1;
+      ok = ok && (uint32_t)x0 < (uint32_t)p.V && (uint32_t)x1 < (uint32_t)p.V;
     }
     ok = __all_sync(0xffffffffu, ok);
     if (lane == 0) tree_bad = !ok;
@@ -95,123 +233,217 @@ __global__ void __launch_bounds__(kThreads)
     if (tid == 0) flag(p.dev_status, FLARE_DEV_BAD_TREE);
     return;
   }
-  const int32_t* hist = p.history ? p.history + (size_t)r * p.H : nullptr;
-  int wrong = 0;
-  for (int i = tid; i < H; i += kThreads) {
-    const int x = hist[i];
-    wrong |= x < 0 || x >= p.V;
-    if (x >= c0 && x < c1) {
-      if (i >= out_from) atomicAdd(&word[at(x - c0)], 1u);
-      else atomicOr(&word[at(x - c0)], kPrompt);
+  if (!IN_PLACE || MASK) {
+    // the rows, on their way to L2 while the history is counted (ahead of the loads above they would
+    // only hold those up)
+    for (int i = row_first + tid; i < row_last; i += kThreads) {
+      const uintptr_t row = (uintptr_t)(logits + (size_t)i * p.V), from = row & ~(uintptr_t)15;
+      const uint32_t bytes = (uint32_t)(row + len * sizeof(T) - from) & ~15u;
+      if (bytes)
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"(bytes)
+                     : "memory");
     }
   }
-  const int32_t* bias_token = p.bias_token ? p.bias_token + (size_t)r * p.max_bias : nullptr;
-  const float* bias_value = p.bias_token ? p.bias_value + (size_t)r * p.max_bias : nullptr;
-  for (int i = tid; i < n_bias; i += kThreads)
-    wrong |= bias_token[i] < 0 || bias_token[i] >= p.V;
+  int wrong = 0;
+  const auto count = [&](int i, int x) {
+    wrong |= (uint32_t)x >= (uint32_t)p.V;
+    const int e = x - c0;
+    if ((uint32_t)e >= (uint32_t)len) return;
+    if (i >= out_from) atomicAdd(&word[at(e)], 1u);
+    else atomicOr(&word[at(e)], kPrompt);
+    atomicOr(&touched[e >> 5], 1u << (e & 31));
+  };
+  for (int i0 = 4 * tid; i0 < H; i0 += 4 * kThreads * kScan) {
+    if (i0 >= 4 * kThreads * kScan) take(i0);
+#pragma unroll
+    for (int j = 0; j < kScan; ++j) {
+      const int i = i0 + j * 4 * kThreads;
+      if (i >= H) break;
+      count(i, text[j].x);
+      if (i + 1 < H) count(i + 1, text[j].y);
+      if (i + 2 < H) count(i + 2, text[j].z);
+      if (i + 3 < H) count(i + 3, text[j].w);
+    }
+  }
+  if (tree && tid < n && tok[tid] >= c0 && tok[tid] < c1)
+    atomicOr(&held[(tok[tid] - c0) >> 5], 1u << ((tok[tid] - c0) & 31));
+  if (tid >= kThreads - 32) {
+    // biases by one warp: which tokens have one, and then the list in its order, a token's repetitions
+    // one after another
+    const int32_t* bias_token = p.bias_token + (size_t)r * p.max_bias;
+    const float* bias_value = p.bias_value + (size_t)r * p.max_bias;
+    bool any = false;
+    for (int i = lane; i < n_bias; i += 32) {
+      const int x = bias_token[i], e = x - c0;
+      wrong |= (uint32_t)x >= (uint32_t)p.V;
+      if ((uint32_t)e >= (uint32_t)len) continue;
+      any = true;
+      atomicOr(&biased[e >> 5], 1u << (e & 31));
+    }
+    if (__any_sync(0xffffffffu, any)) {
+      uint32_t total = 0;
+      for (int i0 = 0; i0 < bit_words; i0 += 32) {
+        const uint32_t own = i0 + lane < bit_words ? __popc(biased[i0 + lane]) : 0;
+        uint32_t sum = own;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+          const uint32_t up = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += up;
+        }
+        if (i0 + lane < bit_words) before[i0 + lane] = total + sum - own;
+        total += __shfl_sync(0xffffffffu, sum, 31);
+      }
+      for (uint32_t i = lane; i < total; i += 32) bias[i] = 0.f;
+      __syncwarp();
+      for (int i0 = 0; i0 < n_bias; i0 += 32) {
+        const int e = i0 + lane < n_bias ? bias_token[i0 + lane] - c0 : -1;
+        const bool mine = (uint32_t)e < (uint32_t)len;
+        const float b = mine ? bias_value[i0 + lane] : 0.f;
+        const uint32_t w = mine ? biased[e >> 5] : 0, bit = 1u << (e & 31);
+        float* const sum = bias + (mine ? before[e >> 5] + __popc(w & (bit - 1)) : 0);
+        float value = mine ? *sum : 0.f;
+        const uint32_t same = __match_any_sync(0xffffffffu, mine ? e : -1 - lane);
+        if (__all_sync(0xffffffffu, same == 1u << lane)) {
+          value += b;
+        } else {
+          for (int src = 0; src < 32; ++src) {
+            const float other = __shfl_sync(0xffffffffu, b, src);
+            if (same >> src & 1) value += other;
+          }
+        }
+        if (mine && lane == __ffs(same) - 1) *sum = value;
+        __syncwarp();
+      }
+    }
+  }
   if (__syncthreads_or(wrong)) {
     if (tid == 0) flag(p.dev_status, FLARE_DEV_BAD_HISTORY);
     return;
   }
-  // the tree's tokens pass the rows below as they are: no count, no summand but the bias
-  const bool held = tree && tid < n && tok[tid] >= c0 && tok[tid] < c1;
-  if (held) base[tid] = word[at(tok[tid] - c0)];
-  __syncthreads();
-  if (held) word[at(tok[tid] - c0)] = 0;
-  __syncthreads();
-  for (int i0 = 0; i0 < chunk; i0 += kThreads) {  // counts to summands, in place
-    const int i = i0 + tid;
-    const uint32_t w = word[at(i)];
-    const uint32_t c = w & ~kPrompt;
-    const float s = c ? -freq * (float)c - pres : 0.f;
-    add[at(i)] = s;
-    const uint32_t any = __ballot_sync(0xffffffffu, w != 0);
-    if (lane == 0) seen[i >> 5] = touched[i >> 5] = any;
-  }
-  if (tid == 0) touched[chunk / 32] = 0;
-  __syncthreads();
-  if (tid < 32) {  // biases in the list's order, a token's repetitions one after another
-    for (int i0 = 0; i0 < n_bias; i0 += 32) {
-      const int x = i0 + lane < n_bias ? bias_token[i0 + lane] : -1;
-      const bool mine = x >= c0 && x < c1;
-      const float b = mine ? bias_value[i0 + lane] : 0.f;
-      const uint32_t same = __match_any_sync(0xffffffffu, mine ? x : -1 - lane);
-      float sum = mine ? add[at(x - c0)] : 0.f;
-      if (__all_sync(0xffffffffu, same == 1u << lane)) {
-        sum += b;
-      } else {
-        for (int src = 0; src < 32; ++src) {
-          const float other = __shfl_sync(0xffffffffu, b, src);
-          if (same >> src & 1) sum += other;
-        }
-      }
-      if (mine && lane == __ffs(same) - 1) {
-        add[at(x - c0)] = sum;
-        atomicOr(&touched[(x - c0) >> 5], 1u << ((x - c0) & 31));
-      }
-      __syncwarp();
-    }
-  }
-  __syncthreads();
-  if (held) atomicAnd(&touched[(tok[tid] - c0) >> 5], ~(1u << ((tok[tid] - c0) & 31)));
+  for (int i = tid; i < bit_words; i += kThreads) touched[i] = (touched[i] | biased[i]) & ~held[i];
   __syncthreads();
 
-  const float rep_inv = 1.f / rep;
-  const float none = minus_inf();
+  const Tables tables{rep, 1.f / rep, pres, freq, word, biased, before, bias};
   const int mask_words = (p.V + 31) / 32;
-  const bool in_place = p.logits == p.out;
-  const int row_first = (int)((long long)n * part / row_parts);
-  const int row_last = (int)((long long)n * (part + 1) / row_parts);
-  for (int i = row_first; i < row_last; ++i) {
-    const size_t row = (size_t)r * p.N + i;
-    const T* src = static_cast<const T*>(p.logits) + row * p.V + c0;
-    T* dst = static_cast<T*>(p.out) + row * p.V + c0;
-    const uint32_t* mask = p.mask ? p.mask + row * mask_words : nullptr;
-    const bool together = ((uintptr_t)src & 15) == ((uintptr_t)dst & 15);
-    // elements ahead of the first whole piece: all of them where the rows' 16-byte grids differ
-    const int ahead = (int)((16 - ((uintptr_t)src & 15)) & 15) / (int)sizeof(T);
-    const int head = together ? min(len, ahead) : len;
-    const int pieces = (len - head) / E;
-    for (int j = tid; j < pieces; j += kThreads) {
-      const int e = head + j * E;
-      uint32_t m = (1u << E) - 1;  // allowed
-      if (mask) {
-        const int b = c0 + e, w = b >> 5;
-        const uint32_t next = w + 1 < mask_words ? mask[w + 1] : 0;
-        m &= __funnelshift_r(mask[w], next, b & 31);
+  const uint32_t* mask = p.mask ? p.mask + (size_t)r * p.N * mask_words : nullptr;
+  const auto allowed_at = [&](int row, int e) -> uint32_t {
+    if (!MASK) return kAll;
+    const uint32_t* w = mask + (size_t)row * mask_words + ((c0 + e) >> 5);
+    const uint32_t next = ((c0 + e) >> 5) + 1 < mask_words ? w[1] : 0;
+    return __funnelshift_r(w[0], next, (c0 + e) & 31) & kAll;
+  };
+  // Threads side by side take a row's pieces, kRows rows at a time; where a row has fewer pieces than
+  // there are threads, several groups of rows at once.
+  const bool together = ALIGNED || ((uintptr_t)logits & 15) == ((uintptr_t)out & 15);
+  int side = kThreads;  // threads of a row
+  while (side > 32 && side / 2 * E >= len) side /= 2;
+  const int j0 = tid % side;
+  const int group = tid / side;
+  if constexpr (ALIGNED) {
+    for (int e = j0 * E; e + E <= len; e += side * E) {
+      const uint32_t t = bits_at(touched, e) & kAll;
+      Change<E> ch;
+      if (t) tables.piece<E>(e, t, ch);
+      const size_t V = p.V, mask_bytes = (size_t)mask_words * 4;
+      const int nibble = e & 4;
+      const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + (c0 + e) / 8;
+      const auto load = [&](auto& batch, int i) {
+        batch.load(logits + i * V + e, V, bits + i * mask_bytes, mask_bytes, nibble, t);
+      };
+      const auto store = [&](auto& batch, int i) {
+        batch.store(out + i * V + e, V, keep_of, t, ch);
+      };
+      // kRows rows at a time, the next ones on their way meanwhile
+      const int step = kThreads / side * kRows;
+      int i = row_first + group * kRows;
+      Batch<T, kRows, MASK, IN_PLACE> one, two;
+      if (i + kRows <= row_last) load(one, i);
+      while (i + kRows <= row_last) {
+        if (i + step + kRows <= row_last) load(two, i + step);
+        store(one, i);
+        i += step;
+        if (i + kRows > row_last) break;
+        if (i + step + kRows <= row_last) load(one, i + step);
+        store(two, i);
+        i += step;
       }
-      const uint32_t t =
-          __funnelshift_r(touched[e >> 5], touched[(e >> 5) + 1], e & 31) & ((1u << E) - 1);
-      if (in_place && m == (1u << E) - 1 && !t) continue;
-      uint4 raw;
-      if (m) raw = *reinterpret_cast<const uint4*>(src + e);
-      if (t || m != (1u << E) - 1) {
-        float x[E];
-        Piece<T>::load(raw, x);
-        const uint32_t sn = __funnelshift_r(seen[e >> 5], seen[(e >> 5) + 1], e & 31);
-#pragma unroll
-        for (int k = 0; k < E; ++k) {
-          if (t >> k & 1) x[k] = penalised(x[k], sn >> k & 1, rep, rep_inv) + add[at(e + k)];
-          if (!(m >> k & 1)) x[k] = none;
-        }
-        raw = Piece<T>::store(x);
+      for (int last = min(i + kRows, row_last); i < last; ++i) {
+        Batch<T, 1, MASK, IN_PLACE> rest;
+        load(rest, i);
+        store(rest, i);
       }
-      *reinterpret_cast<uint4*>(dst + e) = raw;
     }
-    // the ends that are no whole piece
-    const int rest = len - pieces * E;
+  } else {
+    // every row its own grid: the pieces start at its first 16-byte boundary
+    const auto ahead = [&](int i) {
+      const uintptr_t first = (uintptr_t)(logits + (size_t)i * p.V) & 15;
+      return together ? min(len, (int)((16 - first) & 15) / (int)sizeof(T)) : len;
+    };
+    struct {
+      uint4 raw[kRows];
+      uint32_t allowed[kRows], touched[kRows];
+    } one, two;
+    const auto load = [&](auto& batch, int i, int j) {
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        const int e = i + u < row_last ? ahead(i + u) + j * E : len;
+        const bool live = e + E <= len;
+        batch.allowed[u] = live ? allowed_at(i + u, e) : 0;
+        batch.touched[u] = live ? bits_at(touched, e) & kAll : 0;
+        if (live && !(IN_PLACE && batch.allowed[u] == kAll && !batch.touched[u]))
+          batch.raw[u] = *reinterpret_cast<const uint4*>(logits + (size_t)(i + u) * p.V + e);
+      }
+    };
+    const auto store = [&](auto& batch, int i, int j) {
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        const int e = i + u < row_last ? ahead(i + u) + j * E : len;
+        const uint32_t m = batch.allowed[u], t = batch.touched[u];
+        if (e + E > len || (IN_PLACE && m == kAll && !t)) continue;
+        if (t & m) {
+          Change<E> ch;
+          tables.piece<E>(e, t & m, ch);
+          batch.raw[u] = changed<T>(batch.raw[u], ch);
+        }
+        if (MASK) batch.raw[u] = ruled_out<T>(batch.raw[u], keep_of[m]);
+        *reinterpret_cast<uint4*>(out + (size_t)(i + u) * p.V + e) = batch.raw[u];
+      }
+    };
+    const int step = kThreads / side * kRows;
+    for (int j = j0; together && j * E + E <= len; j += side) {
+      int i = row_first + group * kRows;
+      if (i < row_last) load(one, i, j);
+      while (i < row_last) {
+        if (i + step < row_last) load(two, i + step, j);
+        store(one, i, j);
+        i += step;
+        if (i >= row_last) break;
+        if (i + step < row_last) load(one, i + step, j);
+        store(two, i, j);
+        i += step;
+      }
+    }
+  }
+  // the ends that are no whole piece
+  for (int i = row_first; i < row_last; ++i) {
+    const T* src = logits + (size_t)i * p.V;
+    const int ahead = (int)((16 - ((uintptr_t)src & 15)) & 15) / (int)sizeof(T);
+    const int head = ALIGNED ? 0 : together ? min(len, ahead) : len;
+    const int pieces = (len - head) / E, rest = len - pieces * E;
     for (int j = tid; j < rest; j += kThreads) {
       const int e = j < head ? j : j + pieces * E;
-      const bool ok = !mask || mask[(c0 + e) >> 5] >> ((c0 + e) & 31) & 1;
-      const bool change = touched[e >> 5] >> (e & 31) & 1;
-      if (in_place && ok && !change) continue;
-      float x = none;
+      const bool ok = allowed_at(i, e) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
+      if (IN_PLACE && ok && !changes) continue;
+      float x = minus_inf();
       if (ok) {
         x = to_f32(src[e]);
-        if (change)
-          x = penalised(x, seen[e >> 5] >> (e & 31) & 1, rep, rep_inv) + add[at(e)];
+        if (changes) {
+          float up, down, add;
+          tables.one(e, up, down, add);
+          x = fmaf(x, x > 0.f ? up : down, add);
+        }
       }
-      dst[e] = from_f32<T>(x);
+      out[(size_t)i * p.V + e] = from_f32<T>(x);
     }
   }
   if (!tree) return;
@@ -225,33 +457,62 @@ __global__ void __launch_bounds__(kThreads)
     uint64_t same = 0;
     for (int k = 0; k < n; ++k) same |= (uint64_t)(tok[k] == x) << k;
     if (m != __ffsll(same) - 1) continue;  // once
-    const size_t row = (size_t)r * p.N + i;
-    if (p.mask && !(p.mask[row * mask_words + (x >> 5)] >> (x & 31) & 1)) continue;
+    float y = to_f32(logits[(size_t)i * p.V + x - c0]);
+    if (!(allowed_at(i, x - c0) & 1)) continue;
+    const uint32_t base = word[at(x - c0)];
     const int mine = __popcll(same & path[i]);
-    const uint32_t c = (base[m] & ~kPrompt) + mine;
-    float y = to_f32(static_cast<const T*>(p.logits)[row * p.V + x]);
-    y = penalised(y, base[m] != 0 || mine, rep, rep_inv);
+    const uint32_t c = (base & ~kPrompt) + mine;
+    if (base != 0 || mine) y *= y > 0.f ? tables.rep_inv : rep;
     if (c) y -= freq * (float)c + pres;
-    static_cast<T*>(p.out)[row * p.V + x] = from_f32<T>(y + add[at(x - c0)]);
+    out[(size_t)i * p.V + x - c0] = from_f32<T>(y + tables.bias_of(x - c0));
   }
 }
+
+namespace {
+
+using Kernel = void (*)(TreeLogitsParams, int, int, int);
+
+template <typename T, bool ALIGNED>
+Kernel kernel_of(const TreeLogitsParams& p) {
+  const bool in_place = p.logits == p.out;
+  return p.mask ? in_place ? tree_logits_kernel<T, ALIGNED, true, true>
+                           : tree_logits_kernel<T, ALIGNED, true, false>
+                : in_place ? tree_logits_kernel<T, ALIGNED, false, true>
+                           : tree_logits_kernel<T, ALIGNED, false, false>;
+}
+
+template <typename T>
+Kernel kernel_of(const TreeLogitsParams& p, bool aligned) {
+  return aligned ? kernel_of<T, true>(p) : kernel_of<T, false>(p);
+}
+
+}  // namespace
 
 cudaError_t launch_tree_logits(const TreeLogitsParams& p, bool bf16, int num_sms,
                                cudaStream_t stream) {
   if (p.R == 0) return cudaSuccess;
-  // the largest chunk that still gives every SM several CTAs
-  int chunk = 4096;
-  while (chunk > 512 && (int64_t)p.R * ((p.V + chunk - 1) / chunk) < 3 * num_sms) chunk /= 2;
-  const int chunks = (p.V + chunk - 1) / chunk;
+  // one wave of CTAs where that leaves chunks of 512 to 16384 tokens, whose history is counted once
+  const int slots = kCtas * num_sms, most = (p.V + 511) / 512;
+  int chunks = slots / p.R;
+  chunks = chunks < 1 ? 1 : chunks > most ? most : chunks;
+  if (chunks < (p.V + 16383) / 16384) chunks = (p.V + 16383) / 16384;
+  const int chunk = ((p.V + chunks - 1) / chunks + 255) / 256 * 256;
+  chunks = (p.V + chunk - 1) / chunk;
   int parts = 1;
-  while (parts * 2 <= p.N && (int64_t)p.R * chunks * parts < 2 * num_sms) parts *= 2;
+  while (parts * 2 * kRows <= p.N && (int64_t)p.R * chunks * parts * 2 <= slots) parts *= 2;
   if ((int64_t)p.R * parts * chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  const int smem = (chunk + chunk / 32 + 2 * (chunk / 32 + 1)) * 4;
+  const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
+  const int smem = (at(chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
   const unsigned grid = (unsigned)p.R * parts * chunks;
-  if (bf16)
-    tree_logits_kernel<__nv_bfloat16><<<grid, kThreads, smem, stream>>>(p, chunk, chunks, parts);
-  else
-    tree_logits_kernel<float><<<grid, kThreads, smem, stream>>>(p, chunk, chunks, parts);
+  const bool aligned = ((uintptr_t)p.logits & 15) == 0 && ((uintptr_t)p.out & 15) == 0 &&
+                       (size_t)p.V * (bf16 ? 2 : 4) % 16 == 0;
+  const auto kernel = bf16 ? kernel_of<__nv_bfloat16>(p, aligned) : kernel_of<float>(p, aligned);
+  if (smem > (48 << 10)) {
+    const cudaError_t e =
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<grid, kThreads, smem, stream>>>(p, chunk, chunks, parts);
   note_launches(1);
   return cudaGetLastError();
 }
