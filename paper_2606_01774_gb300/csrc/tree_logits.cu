@@ -18,7 +18,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCtas = 3;                 // of an SM
-constexpr int kRows = 3;                 // rows in flight per thread
 constexpr int kScan = 8;                 // pieces of the history in flight per thread, four tokens each
 constexpr uint32_t kPrompt = 1u << 31;   // seen in the history ahead of the output; below: count
 
@@ -83,13 +82,15 @@ struct Tables {
     add = c ? -freq * (float)c - pres : -0.f;
     if (biased[e >> 5] >> (e & 31) & 1) add += bias_of(e);
   }
-  template <int E>
+  // Of a piece whose element k is token e + k / S * 32 S + k % S.
+  template <int E, int S>
   __device__ __forceinline__ void piece(int e, uint32_t touched, Change<E>& ch) const {
 #pragma unroll
     for (int k = 0; k < E; ++k) {
       ch.up[k] = ch.down[k] = 1.f;
       ch.add[k] = -0.f;
-      if (touched >> k & 1) one(e + k, ch.up[k], ch.down[k], ch.add[k]);
+      if (touched >> k & 1)
+        one(e + k / S * 32 * S + k % S, ch.up[k], ch.down[k], ch.add[k]);
     }
   }
 };
@@ -103,48 +104,96 @@ __device__ __forceinline__ uint4 changed(const uint4& raw, const Change<E>& ch) 
   return Piece<T>::store(x);
 }
 
-// A piece of ROWS rows: taken in, then changed, ruled out and put back.
-template <typename T, int ROWS, bool MASK, bool IN_PLACE>
+// W consecutive bytes of a row, a part of a piece.
+template <int W>
+struct Part;
+template <>
+struct Part<16> {
+  using Type = uint4;
+};
+template <>
+struct Part<8> {
+  using Type = uint2;
+};
+template <>
+struct Part<4> {
+  using Type = uint32_t;
+};
+
+template <int W>
+__device__ __forceinline__ void get_part(uint4& raw, int k, const void* from) {
+  uint32_t* w = reinterpret_cast<uint32_t*>(&raw);
+  const auto v = *static_cast<const typename Part<W>::Type*>(from);
+  if constexpr (W == 16) raw = v;
+  if constexpr (W == 8) w[2 * k] = v.x, w[2 * k + 1] = v.y;
+  if constexpr (W == 4) w[k] = v;
+}
+
+template <int W>
+__device__ __forceinline__ void put_part(const uint4& raw, int k, void* to) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(&raw);
+  if constexpr (W == 16) *static_cast<uint4*>(to) = raw;
+  if constexpr (W == 8) *static_cast<uint2*>(to) = make_uint2(w[2 * k], w[2 * k + 1]);
+  if constexpr (W == 4) *static_cast<uint32_t*>(to) = w[k];
+}
+
+// The pieces of a warp's lanes in ROWS rows: taken in, then changed, ruled out and put back.
+// `live`: the piece's elements inside the chunk, a whole number of parts.
+template <typename T, int W, int ROWS, bool MASK, bool IN_PLACE>
 struct Batch {
-  static constexpr int E = Piece<T>::N;
-  static constexpr uint32_t kAll = (1u << E) - 1;
+  static constexpr int E = Piece<T>::N, S = W / (int)sizeof(T), K = E / S;
   uint4 raw[ROWS];
   uint32_t allowed[ROWS];
 
-  // `bits`: the mask's byte of the piece in the first row, `nibble` where in it the bits start.
-  __device__ __forceinline__ void load(const T* src, size_t V, const uint8_t* bits,
-                                       size_t mask_bytes, int nibble, uint32_t touched) {
+  // src: the lane's first element, bits: the mask's byte with it, both of the first row.
+  __device__ __forceinline__ void load(const T* src, size_t V, const uint8_t* bits, int bit,
+                                       size_t mask_bytes, uint32_t live, bool kept) {
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-      allowed[u] = MASK ? bits[u * mask_bytes] : kAll;
-      if (MASK && E == 4) allowed[u] = allowed[u] >> nibble & kAll;
+      allowed[u] = live;
+      if (MASK) {
+        allowed[u] = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (live >> (k * S) & 1)
+            allowed[u] |= (bits[u * mask_bytes + k * 4 * S] >> bit & ((1u << S) - 1)) << (k * S);
+      }
     }
 #pragma unroll
-    for (int u = 0; u < ROWS; ++u)  // in place what stays as it is stays there
-      if (!IN_PLACE || touched || allowed[u] != kAll)
-        raw[u] = *reinterpret_cast<const uint4*>(src + u * V);
+    for (int u = 0; u < ROWS; ++u) {
+      if (IN_PLACE && kept && allowed[u] == live) continue;  // what stays as it is, stays
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (live >> (k * S) & 1) get_part<W>(raw[u], k, src + u * V + k * 32 * S);
+    }
   }
   __device__ __forceinline__ void store(T* dst, size_t V, const uint4* keep_of, uint32_t touched,
-                                        const Change<E>& ch) {
+                                        const Change<E>& ch, uint32_t live, bool kept) {
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-      if (IN_PLACE && !touched && allowed[u] == kAll) continue;
+      if (IN_PLACE && kept && allowed[u] == live) continue;
       if (touched & allowed[u]) raw[u] = changed<T>(raw[u], ch);
       if (MASK) raw[u] = ruled_out<T>(raw[u], keep_of[allowed[u]]);
-      *reinterpret_cast<uint4*>(dst + u * V) = raw[u];
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (live >> (k * S) & 1) put_part<W>(raw[u], k, dst + u * V + k * 32 * S);
     }
   }
 };
 
 }  // namespace
 
-// ALIGNED: every row starts on a 16-byte boundary, so that pieces are the same tokens in all.
-template <typename T, bool ALIGNED, bool MASK, bool IN_PLACE>
+// W: bytes on whose boundaries all rows start, up to 16.  A lane's piece is 16 bytes in parts of W, a
+// warp's parts next to each other: the same tokens in every row, whatever V is.  W = 0, for parts
+// that would be small: pieces start at each row's own 16-byte boundaries.
+template <typename T, int W, bool MASK, bool IN_PLACE>
 __global__ void __launch_bounds__(kThreads, kCtas)
     tree_logits_kernel(const __grid_constant__ TreeLogitsParams p, int chunk, int chunks,
                        int row_parts) {
-  constexpr int E = Piece<T>::N;  // elements of a piece
-  constexpr uint32_t kAll = (1u << E) - 1;
+  constexpr int E = Piece<T>::N;               // elements of a piece
+  constexpr int kRows = sizeof(T) == 2 ? 3 : 2;  // in flight per thread, twice
+  constexpr uint32_t kFull = (1u << E) - 1;
+  constexpr int S = W ? W / (int)sizeof(T) : E;  // of a part
   extern __shared__ __align__(16) char smem[];
   uint32_t* word = reinterpret_cast<uint32_t*>(smem);  // [at(chunk)] the history's counts
   const int bit_words = chunk / 32 + 1;                // a word to spare
@@ -326,54 +375,20 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   const Tables tables{rep, 1.f / rep, pres, freq, word, biased, before, bias};
   const int mask_words = (p.V + 31) / 32;
   const uint32_t* mask = p.mask ? p.mask + (size_t)r * p.N * mask_words : nullptr;
-  const auto allowed_at = [&](int row, int e) -> uint32_t {
-    if (!MASK) return kAll;
-    const uint32_t* w = mask + (size_t)row * mask_words + ((c0 + e) >> 5);
-    const uint32_t next = ((c0 + e) >> 5) + 1 < mask_words ? w[1] : 0;
-    return __funnelshift_r(w[0], next, (c0 + e) & 31) & kAll;
-  };
-  // Threads side by side take a row's pieces, kRows rows at a time; where a row has fewer pieces than
-  // there are threads, several groups of rows at once.
-  const bool together = ALIGNED || ((uintptr_t)logits & 15) == ((uintptr_t)out & 15);
-  int side = kThreads;  // threads of a row
-  while (side > 32 && side / 2 * E >= len) side /= 2;
-  const int j0 = tid % side;
-  const int group = tid / side;
-  if constexpr (ALIGNED) {
-    for (int e = j0 * E; e + E <= len; e += side * E) {
-      const uint32_t t = bits_at(touched, e) & kAll;
-      Change<E> ch;
-      if (t) tables.piece<E>(e, t, ch);
-      const size_t V = p.V, mask_bytes = (size_t)mask_words * 4;
-      const int nibble = e & 4;
-      const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + (c0 + e) / 8;
-      const auto load = [&](auto& batch, int i) {
-        batch.load(logits + i * V + e, V, bits + i * mask_bytes, mask_bytes, nibble, t);
-      };
-      const auto store = [&](auto& batch, int i) {
-        batch.store(out + i * V + e, V, keep_of, t, ch);
-      };
-      // kRows rows at a time, the next ones on their way meanwhile
-      const int step = kThreads / side * kRows;
-      int i = row_first + group * kRows;
-      Batch<T, kRows, MASK, IN_PLACE> one, two;
-      if (i + kRows <= row_last) load(one, i);
-      while (i + kRows <= row_last) {
-        if (i + step + kRows <= row_last) load(two, i + step);
-        store(one, i);
-        i += step;
-        if (i + kRows > row_last) break;
-        if (i + step + kRows <= row_last) load(one, i + step);
-        store(two, i);
-        i += step;
-      }
-      for (int last = min(i + kRows, row_last); i < last; ++i) {
-        Batch<T, 1, MASK, IN_PLACE> rest;
-        load(rest, i);
-        store(rest, i);
-      }
-    }
-  } else {
+  // Warps side by side take a row's pieces, kRows rows at a time; where a row has pieces for
+  // fewer warps, several groups of rows at once.
+  int side = kThreads / 32;  // warps of a row
+  while (side > 1 && side / 2 * 32 * E >= len) side /= 2;
+  const int group = tid / 32 / side, step = kThreads / 32 / side * kRows;
+  const size_t V = p.V, mask_bytes = (size_t)mask_words * 4;
+  if constexpr (W == 0) {
+    const bool together = ((uintptr_t)logits & 15) == ((uintptr_t)out & 15);
+    const auto allowed_at = [&](int row, int e) -> uint32_t {
+      if (!MASK) return kFull;
+      const uint32_t* w = mask + (size_t)row * mask_words + ((c0 + e) >> 5);
+      const uint32_t next = ((c0 + e) >> 5) + 1 < mask_words ? w[1] : 0;
+      return __funnelshift_r(w[0], next, (c0 + e) & 31) & kFull;
+    };
     // every row its own grid: the pieces start at its first 16-byte boundary
     const auto ahead = [&](int i) {
       const uintptr_t first = (uintptr_t)(logits + (size_t)i * p.V) & 15;
@@ -389,8 +404,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         const int e = i + u < row_last ? ahead(i + u) + j * E : len;
         const bool live = e + E <= len;
         batch.allowed[u] = live ? allowed_at(i + u, e) : 0;
-        batch.touched[u] = live ? bits_at(touched, e) & kAll : 0;
-        if (live && !(IN_PLACE && batch.allowed[u] == kAll && !batch.touched[u]))
+        batch.touched[u] = live ? bits_at(touched, e) & kFull : 0;
+        if (live && !(IN_PLACE && batch.allowed[u] == kFull && !batch.touched[u]))
           batch.raw[u] = *reinterpret_cast<const uint4*>(logits + (size_t)(i + u) * p.V + e);
       }
     };
@@ -399,18 +414,17 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       for (int u = 0; u < kRows; ++u) {
         const int e = i + u < row_last ? ahead(i + u) + j * E : len;
         const uint32_t m = batch.allowed[u], t = batch.touched[u];
-        if (e + E > len || (IN_PLACE && m == kAll && !t)) continue;
+        if (e + E > len || (IN_PLACE && m == kFull && !t)) continue;
         if (t & m) {
           Change<E> ch;
-          tables.piece<E>(e, t & m, ch);
+          tables.piece<E, E>(e, t & m, ch);
           batch.raw[u] = changed<T>(batch.raw[u], ch);
         }
         if (MASK) batch.raw[u] = ruled_out<T>(batch.raw[u], keep_of[m]);
         *reinterpret_cast<uint4*>(out + (size_t)(i + u) * p.V + e) = batch.raw[u];
       }
     };
-    const int step = kThreads / side * kRows;
-    for (int j = j0; together && j * E + E <= len; j += side) {
+    for (int j = tid % (32 * side); together && j * E + E <= len; j += 32 * side) {
       int i = row_first + group * kRows;
       if (i < row_last) load(one, i, j);
       while (i < row_last) {
@@ -423,27 +437,71 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         i += step;
       }
     }
-  }
-  // the ends that are no whole piece
-  for (int i = row_first; i < row_last; ++i) {
-    const T* src = logits + (size_t)i * p.V;
-    const int ahead = (int)((16 - ((uintptr_t)src & 15)) & 15) / (int)sizeof(T);
-    const int head = ALIGNED ? 0 : together ? min(len, ahead) : len;
-    const int pieces = (len - head) / E, rest = len - pieces * E;
-    for (int j = tid; j < rest; j += kThreads) {
-      const int e = j < head ? j : j + pieces * E;
-      const bool ok = allowed_at(i, e) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
-      if (IN_PLACE && ok && !changes) continue;
-      float x = minus_inf();
-      if (ok) {
-        x = to_f32(src[e]);
-        if (changes) {
-          float up, down, add;
-          tables.one(e, up, down, add);
-          x = fmaf(x, x > 0.f ? up : down, add);
+    // the ends that are no whole piece
+    for (int i = row_first; i < row_last; ++i) {
+      const T* src = logits + (size_t)i * p.V;
+      const int ahead = (int)((16 - ((uintptr_t)src & 15)) & 15) / (int)sizeof(T);
+      const int head = together ? min(len, ahead) : len;
+      const int pieces = (len - head) / E, rest = len - pieces * E;
+      for (int j = tid; j < rest; j += kThreads) {
+        const int e = j < head ? j : j + pieces * E;
+        const bool ok = allowed_at(i, e) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
+        if (IN_PLACE && ok && !changes) continue;
+        float x = minus_inf();
+        if (ok) {
+          x = to_f32(src[e]);
+          if (changes) {
+            float up, down, add;
+            tables.one(e, up, down, add);
+            x = fmaf(x, x > 0.f ? up : down, add);
+          }
         }
+        out[(size_t)i * p.V + e] = from_f32<T>(x);
       }
-      out[(size_t)i * p.V + e] = from_f32<T>(x);
+    }
+  } else {
+    for (int block = tid / 32 % side * 32 * E; block < len; block += side * 32 * E) {
+      const int e = block + lane * S;
+      uint32_t live = 0, t = 0;
+  #pragma unroll
+      for (int k = 0; k < E; k += S) {
+        const int x = e + k * 32;
+        if (x >= len) continue;  // V is a whole number of parts
+        live |= ((1u << S) - 1) << k;
+        t |= (touched[x >> 5] >> (x & 31) & ((1u << S) - 1)) << k;
+      }
+      if (S == E) {
+        if (!live) continue;
+        live = kFull;
+      }
+      Change<E> ch;
+      if (t) tables.piece<E, S>(e, t, ch);
+      const bool kept = !t;
+      const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + (c0 + e) / 8;
+      const auto load = [&](auto& batch, int i) {
+        batch.load(logits + i * V + e, V, bits + i * mask_bytes, e & 7, mask_bytes, live, kept);
+      };
+      const auto store = [&](auto& batch, int i) {
+        batch.store(out + i * V + e, V, keep_of, t, ch, live, kept);
+      };
+      // the next rows are on their way while these are worked on
+      int i = row_first + group * kRows;
+      Batch<T, W, kRows, MASK, IN_PLACE> one, two;
+      if (i + kRows <= row_last) load(one, i);
+      while (i + kRows <= row_last) {
+        if (i + step + kRows <= row_last) load(two, i + step);
+        store(one, i);
+        i += step;
+        if (i + kRows > row_last) break;
+        if (i + step + kRows <= row_last) load(one, i + step);
+        store(two, i);
+        i += step;
+      }
+      for (const int last = min(i + kRows, row_last); i < last; ++i) {
+        Batch<T, W, 1, MASK, IN_PLACE> rest;
+        load(rest, i);
+        store(rest, i);
+      }
     }
   }
   if (!tree) return;
@@ -458,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     for (int k = 0; k < n; ++k) same |= (uint64_t)(tok[k] == x) << k;
     if (m != __ffsll(same) - 1) continue;  // once
     float y = to_f32(logits[(size_t)i * p.V + x - c0]);
-    if (!(allowed_at(i, x - c0) & 1)) continue;
+    if (MASK && !(mask[(size_t)i * mask_words + (x >> 5)] >> (x & 31) & 1)) continue;
     const uint32_t base = word[at(x - c0)];
     const int mine = __popcll(same & path[i]);
     const uint32_t c = (base & ~kPrompt) + mine;
@@ -472,18 +530,21 @@ namespace {
 
 using Kernel = void (*)(TreeLogitsParams, int, int, int);
 
-template <typename T, bool ALIGNED>
+template <typename T, int W>
 Kernel kernel_of(const TreeLogitsParams& p) {
   const bool in_place = p.logits == p.out;
-  return p.mask ? in_place ? tree_logits_kernel<T, ALIGNED, true, true>
-                           : tree_logits_kernel<T, ALIGNED, true, false>
-                : in_place ? tree_logits_kernel<T, ALIGNED, false, true>
-                           : tree_logits_kernel<T, ALIGNED, false, false>;
+  return p.mask ? in_place ? tree_logits_kernel<T, W, true, true>
+                           : tree_logits_kernel<T, W, true, false>
+                : in_place ? tree_logits_kernel<T, W, false, true>
+                           : tree_logits_kernel<T, W, false, false>;
 }
 
 template <typename T>
-Kernel kernel_of(const TreeLogitsParams& p, bool aligned) {
-  return aligned ? kernel_of<T, true>(p) : kernel_of<T, false>(p);
+Kernel kernel_of(const TreeLogitsParams& p) {
+  const uintptr_t all = (uintptr_t)p.logits | (uintptr_t)p.out | (uintptr_t)p.V * sizeof(T);
+  if (all % 16 == 0) return kernel_of<T, 16>(p);
+  if (all % 8 == 0) return kernel_of<T, 8>(p);
+  return kernel_of<T, sizeof(T) == 2 ? 0 : 4>(p);
 }
 
 }  // namespace
@@ -499,14 +560,12 @@ cudaError_t launch_tree_logits(const TreeLogitsParams& p, bool bf16, int num_sms
   const int chunk = ((p.V + chunks - 1) / chunks + 255) / 256 * 256;
   chunks = (p.V + chunk - 1) / chunk;
   int parts = 1;
-  while (parts * 2 * kRows <= p.N && (int64_t)p.R * chunks * parts * 2 <= slots) parts *= 2;
+  while (parts * 8 <= p.N && (int64_t)p.R * chunks * parts * 2 <= slots) parts *= 2;
   if ((int64_t)p.R * parts * chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
   const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
   const int smem = (at(chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
   const unsigned grid = (unsigned)p.R * parts * chunks;
-  const bool aligned = ((uintptr_t)p.logits & 15) == 0 && ((uintptr_t)p.out & 15) == 0 &&
-                       (size_t)p.V * (bf16 ? 2 : 4) % 16 == 0;
-  const auto kernel = bf16 ? kernel_of<__nv_bfloat16>(p, aligned) : kernel_of<float>(p, aligned);
+  const auto kernel = bf16 ? kernel_of<__nv_bfloat16>(p) : kernel_of<float>(p);
   if (smem > (48 << 10)) {
     const cudaError_t e =
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
