@@ -392,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     // every row its own grid: the pieces start at its first 16-byte boundary
     const auto ahead = [&](int i) {
       const uintptr_t first = (uintptr_t)(logits + (size_t)i * p.V) & 15;
-      return together ? min(len, (int)((16 - first) & 15) / (int)sizeof(T)) : len;
+      return min(len, (int)((16 - first) & 15) / (int)sizeof(T));
     };
     struct {
       uint4 raw[kRows];
@@ -437,27 +437,27 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         i += step;
       }
     }
-    // the ends that are no whole piece
-    for (int i = row_first; i < row_last; ++i) {
-      const T* src = logits + (size_t)i * p.V;
-      const int ahead = (int)((16 - ((uintptr_t)src & 15)) & 15) / (int)sizeof(T);
-      const int head = together ? min(len, ahead) : len;
-      const int pieces = (len - head) / E, rest = len - pieces * E;
-      for (int j = tid; j < rest; j += kThreads) {
-        const int e = j < head ? j : j + pieces * E;
-        const bool ok = allowed_at(i, e) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
-        if (IN_PLACE && ok && !changes) continue;
-        float x = minus_inf();
-        if (ok) {
-          x = to_f32(src[e]);
-          if (changes) {
-            float up, down, add;
-            tables.one(e, up, down, add);
-            x = fmaf(x, x > 0.f ? up : down, add);
-          }
-        }
-        out[(size_t)i * p.V + e] = from_f32<T>(x);
+    const auto element = [&](int i, int e) {
+      const T x_in = logits[(size_t)i * p.V + e];
+      const bool ok = allowed_at(i, e) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
+      if (IN_PLACE && ok && !changes) return;
+      float x = ok ? to_f32(x_in) : minus_inf();
+      if (ok && changes) {
+        float up, down, add;
+        tables.one(e, up, down, add);
+        x = fmaf(x, x > 0.f ? up : down, add);
       }
+      out[(size_t)i * p.V + e] = from_f32<T>(x);
+    };
+    if (together) {  // the ends that are no whole piece, fewer than E on each side
+      for (int k = tid; k < (row_last - row_first) * 2 * E; k += kThreads) {
+        const int i = row_first + k / (2 * E), j = k % (2 * E);
+        const int head = ahead(i), pieces = (len - head) / E, rest = len - pieces * E;
+        if (j < rest) element(i, j < head ? j : j + pieces * E);
+      }
+    } else {
+      for (int i = row_first; i < row_last; ++i)
+        for (int e = tid; e < len; e += kThreads) element(i, e);
     }
   } else {
     for (int block = tid / 32 % side * 32 * E; block < len; block += side * 32 * E) {
