@@ -273,6 +273,8 @@ struct TreeLogitsParams {
   void* out;
   int32_t* dev_status;
 };
+template <typename T>
+cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaStream_t stream);
 cudaError_t launch_tree_logits(const TreeLogitsParams& p, bool bf16, int num_sms,
                                cudaStream_t stream);
 

@@ -7,6 +7,8 @@
 // shared memory, turns counts and biases into one summand per token, and streams
 // its rows through.  The tree's own tokens are put right at the end, each by its
 // count on every node's path.  Bound by bytes: logits in and out once.
+#pragma once
+
 #include "common.cuh"
 #include "kernels.h"
 #include "piece.cuh"
@@ -18,8 +20,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCtas = 3;                 // of an SM
+template <typename T>
+constexpr int kRowsOf = sizeof(T) == 2 ? 3 : 2;
 constexpr int kScan = 8;                 // pieces of the history in flight per thread, four tokens each
 constexpr uint32_t kPrompt = 1u << 31;   // seen in the history ahead of the output; below: count
+constexpr int kNarrow = 32767;           // the longest history whose counts have 16 bits each
 
 // Index of chunk token i: the eight tokens of a thread's piece, eight threads on, lie in
 // banks of their own.
@@ -54,6 +59,25 @@ __device__ __forceinline__ uint4 ruled_out(const uint4& raw, const uint4& keep) 
                     (raw.z & keep.z) | (none & ~keep.z), (raw.w & keep.w) | (none & ~keep.w));
 }
 
+// How often the history holds each token of a chunk: in the output, with kPrompt where the prompt has
+// it too.  Two tokens to a word where the history is short.
+struct Counts {
+  uint32_t* word;
+  bool narrow;
+
+  __device__ __forceinline__ uint32_t operator[](int e) const {
+    if (!narrow) return word[at(e)];
+    const uint32_t half = word[at(e >> 1)] >> (e & 1) * 16;
+    return (half & 0x7fffu) | (half & 0x8000u) << 16;
+  }
+  __device__ __forceinline__ void add(int e, bool output) const {
+    uint32_t* w = &word[at(narrow ? e >> 1 : e)];
+    const int shift = narrow ? (e & 1) * 16 : 0;
+    if (output) atomicAdd(w, 1u << shift);
+    else atomicOr(w, narrow ? 0x8000u << shift : kPrompt);
+  }
+};
+
 // What a piece's tokens get: y = x (x > 0 ? up : down) + add, which leaves what is neither seen
 // nor has a summand as it is (x + -0 is x, for both zeros).
 template <int E>
@@ -64,7 +88,7 @@ struct Change {
 // A request's penalties, and its history's counts and biases over a chunk of the vocabulary.
 struct Tables {
   float rep, rep_inv, pres, freq;
-  const uint32_t* word;    // [at(chunk)] counts
+  Counts counts;
   const uint32_t* biased;  // [chunk / 32] bits: tokens with a bias
   const uint32_t* before;  // [chunk / 32] how many bits are set in the words before
   const float* bias;       // of the tokens with one, in order
@@ -76,7 +100,7 @@ struct Tables {
 
   // Of token e of the chunk.
   __device__ __forceinline__ void one(int e, float& up, float& down, float& add) const {
-    const uint32_t w = word[at(e)], c = w & ~kPrompt;
+    const uint32_t w = counts[e], c = w & ~kPrompt;
     up = w ? rep_inv : 1.f;
     down = w ? rep : 1.f;
     add = c ? -freq * (float)c - pres : -0.f;
@@ -185,19 +209,21 @@ struct Batch {
 
 // W: bytes on whose boundaries all rows start, up to 16.  A lane's piece is 16 bytes in parts of W, a
 // warp's parts next to each other: the same tokens in every row, whatever V is.  W = 0, for parts
-// that would be small: pieces start at each row's own 16-byte boundaries.
-template <typename T, int W, bool MASK, bool IN_PLACE>
+// that would be small: pieces start at each row's own 16-byte boundaries.  FEW: rows too few to keep
+// a batch under way.
+template <typename T, int W, bool MASK, bool IN_PLACE, bool FEW>
 __global__ void __launch_bounds__(kThreads, kCtas)
     tree_logits_kernel(const __grid_constant__ TreeLogitsParams p, int chunk, int chunks,
-                       int row_parts) {
+                       int row_parts, bool narrow) {
   constexpr int E = Piece<T>::N;               // elements of a piece
-  constexpr int kRows = sizeof(T) == 2 ? 3 : 2;  // in flight per thread, twice
+  constexpr int kRows = kRowsOf<T>;            // in flight per thread, twice
   constexpr uint32_t kFull = (1u << E) - 1;
   constexpr int S = W ? W / (int)sizeof(T) : E;  // of a part
   extern __shared__ __align__(16) char smem[];
-  uint32_t* word = reinterpret_cast<uint32_t*>(smem);  // [at(chunk)] the history's counts
+  const Counts counts{reinterpret_cast<uint32_t*>(smem), narrow};
+  const int count_words = at(narrow ? chunk / 2 : chunk);
   const int bit_words = chunk / 32 + 1;                // a word to spare
-  uint32_t* touched = word + at(chunk);  // bits: seen in the history or with a bias
+  uint32_t* touched = counts.word + count_words;  // bits: seen in the history or with a bias
   uint32_t* held = touched + bit_words;  // the tree's own tokens, which come last
   uint32_t* biased = held + bit_words;
   uint32_t* before = biased + bit_words;  // see Tables
@@ -253,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     }
   };
   take(4 * tid);
-  for (int i = tid; i < (at(chunk) + 4 * bit_words + 3) / 4; i += kThreads)  // room for all of it
+  for (int i = tid; i < (count_words + 4 * bit_words + 3) / 4; i += kThreads)  // room for all of it
     reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   if (tid < 1 << E) keep_of[tid] = keep_words<T>(tid);
 
@@ -298,8 +324,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     wrong |= (uint32_t)x >= (uint32_t)p.V;
     const int e = x - c0;
     if ((uint32_t)e >= (uint32_t)len) return;
-    if (i >= out_from) atomicAdd(&word[at(e)], 1u);
-    else atomicOr(&word[at(e)], kPrompt);
+    counts.add(e, i >= out_from);
     atomicOr(&touched[e >> 5], 1u << (e & 31));
   };
   for (int i0 = 4 * tid; i0 < H; i0 += 4 * kThreads * kScan) {
@@ -372,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   for (int i = tid; i < bit_words; i += kThreads) touched[i] = (touched[i] | biased[i]) & ~held[i];
   __syncthreads();
 
-  const Tables tables{rep, 1.f / rep, pres, freq, word, biased, before, bias};
+  const Tables tables{rep, 1.f / rep, pres, freq, counts, biased, before, bias};
   const int mask_words = (p.V + 31) / 32;
   const uint32_t* mask = p.mask ? p.mask + (size_t)r * p.N * mask_words : nullptr;
   // Warps side by side take a row's pieces, kRows rows at a time; where a row has pieces for
@@ -460,47 +485,85 @@ __global__ void __launch_bounds__(kThreads, kCtas)
         for (int e = tid; e < len; e += kThreads) element(i, e);
     }
   } else {
-    for (int block = tid / 32 % side * 32 * E; block < len; block += side * 32 * E) {
-      const int e = block + lane * S;
-      uint32_t live = 0, t = 0;
-  #pragma unroll
+    // of a lane's piece: the elements in the chunk (V is a whole number of parts), and those to change
+    const auto bits_of = [&](int e, uint32_t& live, uint32_t& t) {
+      live = t = 0;
+#pragma unroll
       for (int k = 0; k < E; k += S) {
         const int x = e + k * 32;
-        if (x >= len) continue;  // V is a whole number of parts
+        if (x >= len) continue;
         live |= ((1u << S) - 1) << k;
         t |= (touched[x >> 5] >> (x & 31) & ((1u << S) - 1)) << k;
       }
-      if (S == E) {
-        if (!live) continue;
-        live = kFull;
+    };
+    if constexpr (FEW) {  // several blocks of a row under way together
+      constexpr int kBlocks = 4;
+      const int stride = kThreads * E;
+      for (int i = row_first; i < row_last; ++i) {
+        for (int block = tid / 32 * 32 * E; block < len; block += kBlocks * stride) {
+          Batch<T, W, 1, MASK, IN_PLACE> batch[kBlocks];
+          uint32_t live[kBlocks], t[kBlocks];
+          const T* src = logits + i * V + block + lane * S;
+          T* dst = out + i * V + block + lane * S;
+          const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + i * mask_bytes +
+                                (c0 + block + lane * S) / 8;
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u) {
+            bits_of(block + u * stride + lane * S, live[u], t[u]);
+            batch[u].load(src + u * stride, V, bits + u * stride / 8, lane * S & 7, mask_bytes,
+                          live[u], !t[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < kBlocks; ++u) {
+            Change<E> ch;
+            if (t[u]) tables.piece<E, S>(block + u * stride + lane * S, t[u], ch);
+            batch[u].store(dst + u * stride, V, keep_of, t[u], ch, live[u], !t[u]);
+          }
+        }
       }
-      Change<E> ch;
-      if (t) tables.piece<E, S>(e, t, ch);
-      const bool kept = !t;
-      const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + (c0 + e) / 8;
-      const auto load = [&](auto& batch, int i) {
-        batch.load(logits + i * V + e, V, bits + i * mask_bytes, e & 7, mask_bytes, live, kept);
-      };
-      const auto store = [&](auto& batch, int i) {
-        batch.store(out + i * V + e, V, keep_of, t, ch, live, kept);
-      };
-      // the next rows are on their way while these are worked on
-      int i = row_first + group * kRows;
-      Batch<T, W, kRows, MASK, IN_PLACE> one, two;
-      if (i + kRows <= row_last) load(one, i);
-      while (i + kRows <= row_last) {
-        if (i + step + kRows <= row_last) load(two, i + step);
-        store(one, i);
-        i += step;
-        if (i + kRows > row_last) break;
-        if (i + step + kRows <= row_last) load(one, i + step);
-        store(two, i);
-        i += step;
-      }
-      for (const int last = min(i + kRows, row_last); i < last; ++i) {
-        Batch<T, W, 1, MASK, IN_PLACE> rest;
-        load(rest, i);
-        store(rest, i);
+    } else {
+      for (int block = tid / 32 % side * 32 * E; block < len; block += side * 32 * E) {
+        const int e = block + lane * S;
+        uint32_t live = 0, t = 0;
+    #pragma unroll
+        for (int k = 0; k < E; k += S) {
+          const int x = e + k * 32;
+          if (x >= len) continue;  // V is a whole number of parts
+          live |= ((1u << S) - 1) << k;
+          t |= (touched[x >> 5] >> (x & 31) & ((1u << S) - 1)) << k;
+        }
+        if (S == E) {
+          if (!live) continue;
+          live = kFull;
+        }
+        Change<E> ch;
+        if (t) tables.piece<E, S>(e, t, ch);
+        const bool kept = !t;
+        const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + (c0 + e) / 8;
+        const auto load = [&](auto& batch, int i) {
+          batch.load(logits + i * V + e, V, bits + i * mask_bytes, e & 7, mask_bytes, live, kept);
+        };
+        const auto store = [&](auto& batch, int i) {
+          batch.store(out + i * V + e, V, keep_of, t, ch, live, kept);
+        };
+        // the next rows are on their way while these are worked on
+        int i = row_first + group * kRows;
+        Batch<T, W, kRows, MASK, IN_PLACE> one, two;
+        if (i + kRows <= row_last) load(one, i);
+        while (i + kRows <= row_last) {
+          if (i + step + kRows <= row_last) load(two, i + step);
+          store(one, i);
+          i += step;
+          if (i + kRows > row_last) break;
+          if (i + step + kRows <= row_last) load(one, i + step);
+          store(two, i);
+          i += step;
+        }
+        for (const int last = min(i + kRows, row_last); i < last; ++i) {
+          Batch<T, W, 1, MASK, IN_PLACE> rest;
+          load(rest, i);
+          store(rest, i);
+        }
       }
     }
   }
@@ -517,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     if (m != __ffsll(same) - 1) continue;  // once
     float y = to_f32(logits[(size_t)i * p.V + x - c0]);
     if (MASK && !(mask[(size_t)i * mask_words + (x >> 5)] >> (x & 31) & 1)) continue;
-    const uint32_t base = word[at(x - c0)];
+    const uint32_t base = counts[x - c0];
     const int mine = __popcll(same & path[i]);
     const uint32_t c = (base & ~kPrompt) + mine;
     if (base != 0 || mine) y *= y > 0.f ? tables.rep_inv : rep;
@@ -528,50 +591,69 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 
 namespace {
 
-using Kernel = void (*)(TreeLogitsParams, int, int, int);
+using Kernel = void (*)(TreeLogitsParams, int, int, int, bool);
+
+template <typename T, int W, bool MASK, bool IN_PLACE>
+Kernel kernel_of(const TreeLogitsParams& p) {
+  if constexpr (W > 0) {
+    if (p.N < kRowsOf<T>) return tree_logits_kernel<T, W, MASK, IN_PLACE, true>;
+  }
+  return tree_logits_kernel<T, W, MASK, IN_PLACE, false>;
+}
 
 template <typename T, int W>
 Kernel kernel_of(const TreeLogitsParams& p) {
-  const bool in_place = p.logits == p.out;
-  return p.mask ? in_place ? tree_logits_kernel<T, W, true, true>
-                           : tree_logits_kernel<T, W, true, false>
-                : in_place ? tree_logits_kernel<T, W, false, true>
-                           : tree_logits_kernel<T, W, false, false>;
+  if (p.logits == p.out)
+    return p.mask ? kernel_of<T, W, true, true>(p) : kernel_of<T, W, false, true>(p);
+  return p.mask ? kernel_of<T, W, true, false>(p) : kernel_of<T, W, false, false>(p);
 }
 
 template <typename T>
 Kernel kernel_of(const TreeLogitsParams& p) {
   const uintptr_t all = (uintptr_t)p.logits | (uintptr_t)p.out | (uintptr_t)p.V * sizeof(T);
   if (all % 16 == 0) return kernel_of<T, 16>(p);
-  if (all % 8 == 0) return kernel_of<T, 8>(p);
-  return kernel_of<T, sizeof(T) == 2 ? 0 : 4>(p);
+  if constexpr (sizeof(T) == 4) return kernel_of<T, 4>(p);
+  else return all % 8 == 0 ? kernel_of<T, 8>(p) : kernel_of<T, 0>(p);
 }
 
 }  // namespace
 
-cudaError_t launch_tree_logits(const TreeLogitsParams& p, bool bf16, int num_sms,
-                               cudaStream_t stream) {
-  if (p.R == 0) return cudaSuccess;
-  // one wave of CTAs where that leaves chunks of 512 to 16384 tokens, whose history is counted once
-  const int slots = kCtas * num_sms, most = (p.V + 511) / 512;
-  int chunks = slots / p.R;
-  chunks = chunks < 1 ? 1 : chunks > most ? most : chunks;
-  if (chunks < (p.V + 16383) / 16384) chunks = (p.V + 16383) / 16384;
-  const int chunk = ((p.V + chunks - 1) / chunks + 255) / 256 * 256;
+template <typename T>
+cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaStream_t stream) {
+  // One wave of CTAs, if chunks of 512 to 32768 tokens allow it: a history is counted once per chunk.
+  // Counts of 16 bits only where those of 32 need more memory than the wave leaves.
+  const auto smem_of = [&](int chunk, bool narrow) {
+    const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
+    return (at(narrow ? chunk / 2 : chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
+  };
+  constexpr int kOwn = 6144;  // static shared memory and what the system keeps
+  int chunks = 0, chunk = 0, slots = 0;
+  bool narrow = false;
+  for (int per_sm = kCtas; per_sm > 0; --per_sm) {
+    slots = per_sm * num_sms;
+    chunks = slots / p.R < 1 ? 1 : slots / p.R;
+    const int most = (p.V + 511) / 512;
+    chunks = chunks > most ? most : chunks;
+    chunk = ((p.V + chunks - 1) / chunks + 255) / 256 * 256;
+    chunk = chunk > 32768 ? 32768 : chunk;
+    const int room = (228 << 10) / per_sm - kOwn;
+    narrow = smem_of(chunk, false) > room && p.H <= kNarrow;
+    if (smem_of(chunk, narrow) <= room) break;
+  }
+  while (smem_of(chunk, narrow) > (220 << 10)) chunk /= 2;
   chunks = (p.V + chunk - 1) / chunk;
   int parts = 1;
   while (parts * 8 <= p.N && (int64_t)p.R * chunks * parts * 2 <= slots) parts *= 2;
   if ((int64_t)p.R * parts * chunks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
-  const int smem = (at(chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
+  const int smem = smem_of(chunk, narrow);
   const unsigned grid = (unsigned)p.R * parts * chunks;
-  const auto kernel = bf16 ? kernel_of<__nv_bfloat16>(p) : kernel_of<float>(p);
-  if (smem > (48 << 10)) {
+  const Kernel kernel = kernel_of<T>(p);
+  if (smem > (40 << 10)) {  // with the static part, more than a launch has by itself
     const cudaError_t e =
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
   }
-  kernel<<<grid, kThreads, smem, stream>>>(p, chunk, chunks, parts);
+  kernel<<<grid, kThreads, smem, stream>>>(p, chunk, chunks, parts, narrow);
   note_launches(1);
   return cudaGetLastError();
 }
