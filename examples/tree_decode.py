@@ -14,7 +14,13 @@ with no host synchronisation between rounds.  A prompt enters as a chain whose w
 committed, and ordinary decoding is a tree of one node: `--plain` decodes that way, and in
 fp32 both give the same tokens.
 
-    python examples/tree_decode.py [--requests 8] [--tokens 64] [--dtype f32] [--plain]
+With `--stages` all that is left to PyTorch are the matrix products: keys and queries turn by
+their positions (flare_rotary; flare_rotary_append_kv where the tokens are known to stay), linear
+layers end in a norm per head and a gate, the residual stream is added up and normed
+between layers (flare_block_norm), and repeated tokens are penalised ahead of the choice, each
+node by its own path (flare_tree_logits).
+
+    python examples/tree_decode.py [--requests 8] [--tokens 64] [--dtype f32] [--plain] [--stages]
 """
 from __future__ import annotations
 
@@ -41,8 +47,9 @@ class HybridDecoder:
     """A stack of layers ("l" linear, "s" softmax) with the state of `requests` sequences."""
 
     def __init__(self, requests, max_nodes=16, max_tokens=512, layers="llsl", vocab=512, width=256,
-                 dtype="f32", seed=0, device="cuda"):
+                 dtype="f32", seed=0, device="cuda", stages=False, repetition=1.3):
         self.R, self.N, self.V = requests, max_nodes, vocab
+        self.stages, self.width, self.code = stages, width, TYPES[dtype][1]
         self.dt, code = TYPES[dtype]
         self.layers, self.device = layers, device
         Hk, Hv, d, Hq, Hkv, D, page = 2, 4, 64, 4, 2, 64, 16
@@ -79,19 +86,36 @@ class HybridDecoder:
             for n in range(1, max_nodes + 1)), dtype=torch.uint8, device=device)
         self.path = torch.empty(requests, max_nodes, **i32)
         self.path_len, self.next_token = (torch.empty(requests, **i32) for _ in range(2))
+        if stages:
+            cols = {"l": Hv * d, "s": 0}  # the linear layers' gates
+            self.w_gate = [normal(width, cols[c], scale=width ** -0.5) for c in layers]
+            self.head_norm = [1 + normal(d, scale=0.1) for _ in layers]
+            self.norm = [1 + normal(width, scale=0.1) for _ in range(len(layers) + 1)]
+            self.turns = torch.empty(D // 4, dtype=torch.int64, device=device)  # half of a head
+            flare.check(flare.flare_rotary_table(flare.rotary_freq_desc(D // 2), self.turns))
+            self.text = torch.zeros(requests, max_tokens + max_nodes, **i32)
+            self.text_len = torch.zeros(requests, **i32)
+            self.repetition = torch.full((requests,), repetition, device=device)
+            self.presence = torch.full((requests,), 0.1, device=device)
         # the drafter: followers by the head on the bare embedding
         self.followers = (_norm(self.embed) @ self.head).topk(3, dim=1).indices.to(torch.int32)
 
-    def forward(self, token, parent, node_len):
-        """Logits [R, n, V] of every node; keeps what a commit of the round will need."""
+    def forward(self, token, parent, node_len, known=False):
+        """Logits [R, n, V] of every node; keeps what a commit of the round will need.
+
+        known: the tokens are a chain that stays, its keys and values may enter the caches."""
         R, n = token.shape
         Hk, Hv, d, Hq, Hkv, D = self.heads
         x = self.embed[token.long()]
-        self.kept, states, caches = [], iter(self.state), iter(self.cache)
-        for c, w_in, w_out in zip(self.layers, self.w_in, self.w_out):
-            y = _norm(x) @ w_in
+        y = self.add_and_norm(x, None, 0) if self.stages else _norm(x)
+        if self.stages:
+            y, x = y[1], x.contiguous()
+        self.kept, self.appended = [], known and self.stages
+        states, caches = iter(self.state), iter(self.cache)
+        for i, (c, w_in, w_out) in enumerate(zip(self.layers, self.w_in, self.w_out)):
+            z = y @ w_in
             if c == "l":
-                q, k, v, g, b = y.split([Hk * d, Hk * d, Hv * d, Hv, Hv], dim=-1)
+                q, k, v, g, b = z.split([Hk * d, Hk * d, Hv * d, Hv, Hv], dim=-1)
                 q, k = (torch.nn.functional.normalize(t.reshape(R, n, Hk, d), dim=-1)
                         .to(self.dt).contiguous() for t in (q, k))
                 v = v.reshape(R, n, Hv, d).to(self.dt).contiguous()
@@ -102,16 +126,76 @@ class HybridDecoder:
                     self.lin(n), q, k, v, g, b, next(states), self.slot, parent, node_len, out,
                     self.status))
                 self.kept.append((k, v, g, b))
+                if self.stages:
+                    out = self.gated(out, (y @ self.w_gate[i]).to(self.dt), self.head_norm[i])
             else:
-                q, k, v = (t.reshape(R, n, -1, D).to(self.dt).contiguous()
-                           for t in y.split([Hq * D, Hkv * D, Hkv * D], dim=-1))
-                out, cache = torch.empty_like(q), next(caches)
+                cache = next(caches)
+                if self.stages:
+                    q, k, v = self.turned(z, parent, node_len, cache, known)
+                else:
+                    q, k, v = (t.reshape(R, n, -1, D).to(self.dt).contiguous()
+                               for t in z.split([Hq * D, Hkv * D, Hkv * D], dim=-1))
+                out = torch.empty_like(q)
                 flare.check(flare.flare_tree_softmax_attn(
                     self.soft(n), q, k, v, cache[0], cache[1], self.page_table, self.prefix_len,
                     parent, node_len, out, None, self.work, self.work.numel(), self.status))
                 self.kept.append((k, v))
-            x = x + out.float().reshape(R, n, -1) @ w_out
-        return (_norm(x) @ self.head).contiguous()
+            new = out.float().reshape(R, n, -1) @ w_out
+            if self.stages:
+                x, y = self.add_and_norm(new, x, i + 1)
+            else:
+                x = x + new
+                y = _norm(x)
+        logits = (y @ self.head).contiguous()
+        return self.penalised(logits, token, parent, node_len) if self.stages else logits
+
+    def turned(self, z, parent, node_len, cache, known):
+        """Queries and keys at their nodes' positions, and the values; known tokens into the cache."""
+        R, n, _ = z.shape
+        Hk, Hv, d, Hq, Hkv, D = self.heads
+        rows = z.to(self.dt).reshape(R * n, -1)  # the projections' rows are read where they lie
+        q, k, v = (t.unflatten(1, (-1, D)) for t in rows.split([Hq * D, Hkv * D, Hkv * D], dim=1))
+        step = rows.stride(0)
+        desc = flare.rotary_desc(R, n, 0, Hq, Hkv, D, D // 2, self.code, q_stride=step,
+                                 k_stride=step, v_stride=step, page_size=cache.shape[3],
+                                 num_pages=cache.shape[1],
+                                 max_pages_per_req=self.page_table.shape[1])
+        q_out, k_out = (torch.empty(R, n, h, D, dtype=self.dt, device=self.device)
+                        for h in (Hq, Hkv))
+        if known:
+            flare.check(flare.flare_rotary_append_kv(
+                desc, q, k, v, self.turns, None, self.prefix_len, node_len, None, self.page_table,
+                q_out, k_out, cache[0], cache[1], self.status))
+        else:
+            flare.check(flare.flare_rotary(desc, q, k, self.turns, None, self.prefix_len, node_len,
+                                           parent, None, q_out, k_out, self.status))
+        return q_out, k_out, v.reshape(R, n, Hkv, D).contiguous()
+
+    def gated(self, out, gate, weight):
+        """A linear layer's output: normed per head, times SiLU of the gate."""
+        R, n, Hv, d = out.shape
+        desc = flare.block_norm_desc(R * n, Hv * d, self.code, group=d, shared_weight=1, pre_norm=0,
+                                     gate_act=flare.FLARE_ACT_SILU)
+        y = torch.empty_like(out)
+        flare.check(flare.flare_block_norm(desc, out, gate, None, weight, None, y, None))
+        return y
+
+    def add_and_norm(self, new, stream, i):
+        """The residual stream with what a layer adds, and its norm for the next layer."""
+        rows = new.shape[0] * new.shape[1]
+        desc = flare.block_norm_desc(rows, self.width, flare.FLARE_DT_F32, post_norm=0)
+        y, h = torch.empty_like(new), torch.empty_like(new)
+        flare.check(flare.flare_block_norm(desc, new.contiguous(), None, stream, None,
+                                           self.norm[i], y, h))
+        return y, h
+
+    def penalised(self, logits, token, parent, node_len):
+        R, n, V = logits.shape
+        desc = flare.tree_logits_desc(R, n, V, flare.FLARE_DT_F32, self.text.shape[1])
+        flare.check(flare.flare_tree_logits(
+            desc, logits, self.text, self.text_len, None, token, parent, node_len, self.repetition,
+            self.presence, None, None, None, None, None, logits, self.status))
+        return logits
 
     def verify(self, logits, token, parent, node_len):
         """Accepted path, its length and the next token (in self.path, path_len, next_token)."""
@@ -123,16 +207,23 @@ class HybridDecoder:
             self.path_len, self.next_token, logp, self.work, self.work.numel(), self.status))
         return path, self.path_len, self.next_token
 
-    def commit(self, path, path_len):
-        """The accepted nodes into every layer's state or cache."""
+    def commit(self, path, path_len, token=None):
+        """The accepted nodes into every layer's state or cache, their tokens into the text."""
         n, states = path.shape[1], iter(self.state)
+        if self.stages:
+            at = self.text_len[:, None] + torch.arange(n, device=self.device)
+            there = torch.arange(n, device=self.device) < path_len[:, None]
+            new = torch.where(there, token.gather(1, path.clamp(0, n - 1).long()),
+                              self.text.gather(1, at.long()))
+            self.text.scatter_(1, at.long(), new)
+            self.text_len += path_len
         for c, kept in zip(self.layers, self.kept):
             if c == "l":
                 flare.check(flare.flare_tree_commit_state(
                     self.lin(n), *kept, next(states), self.slot, self.slot, path, path_len,
                     self.status))
         soft = [kept for c, kept in zip(self.layers, self.kept) if c == "s"]
-        if soft:
+        if soft and not self.appended:
             flare.check(flare.flare_tree_append_kv(
                 self.soft(n), [k for k, _ in soft], [v for _, v in soft],
                 [c[0] for c in self.cache], [c[1] for c in self.cache], self.page_table,
@@ -147,8 +238,8 @@ class HybridDecoder:
             m = part.shape[1]
             line = torch.arange(m, dtype=torch.int32, device=self.device).repeat(self.R, 1)
             full = torch.full((self.R,), m, dtype=torch.int32, device=self.device)
-            self.forward(part, line - 1, full)
-            self.commit(line, full)
+            self.forward(part, line - 1, full, known=True)
+            self.commit(line, full, part)
         return tokens[:, -1].contiguous()
 
     def draft(self, anchor, plain):
@@ -169,9 +260,9 @@ class HybridDecoder:
             n = len(tree)
             parent = torch.tensor(tree, dtype=torch.int32, device=self.device).repeat(self.R, 1)
             node_len = torch.full((self.R,), n, dtype=torch.int32, device=self.device)
-            logits = self.forward(token, parent, node_len)
+            logits = self.forward(token, parent, node_len, known=plain)
             path, path_len, anchor = self.verify(logits, token, parent, node_len)
-            self.commit(path, path_len)
+            self.commit(path, path_len, token)
             # the drafted tokens on the path, then the target's own
             drafted = token.gather(1, path.clamp(min=0).long())
             drafted = torch.where(path >= 0, drafted, -1)[:, 1:]
@@ -191,10 +282,13 @@ def main():
     ap.add_argument("--tokens", type=int, default=64)
     ap.add_argument("--dtype", choices=sorted(TYPES), default="f32")
     ap.add_argument("--plain", action="store_true", help="one token a round")
+    ap.add_argument("--stages", action="store_true",
+                    help="positions, norms, gates and penalties by the library too")
     a = ap.parse_args()
     prompt = torch.randint(0, 512, (a.requests, 21), dtype=torch.int32, device="cuda",
                            generator=torch.Generator(device="cuda").manual_seed(1))
-    model = HybridDecoder(a.requests, max_tokens=21 + 4 * a.tokens, dtype=a.dtype)
+    model = HybridDecoder(a.requests, max_tokens=21 + 4 * a.tokens, dtype=a.dtype,
+                          stages=a.stages)
     start = time.perf_counter()
     new, rate = model.decode(prompt, a.tokens if a.plain else -(-a.tokens // 2), a.plain)
     print(f"{rate:.2f} tokens per round and request, {time.perf_counter() - start:.2f} s")
