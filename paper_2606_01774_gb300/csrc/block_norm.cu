@@ -16,10 +16,10 @@ struct Slots {
   uint4* at;   // of this thread, piece 0
   int pieces;  // from one piece to the next: threads of the CTA
 
-  __device__ __forceinline__ void fetch(int array, const T* src) const {
+  __device__ __forceinline__ void fetch(int array, const T* src, const bool (&mine)[M]) const {
 #pragma unroll
     for (int i = 0; i < M; ++i)
-      cp_async16(at + (array * M + i) * pieces, reinterpret_cast<const uint4*>(src) + i);
+      if (mine[i]) cp_async16(at + (array * M + i) * pieces, src + i * kFar);
   }
   __device__ __forceinline__ void read(int array, uint64_t (&x)[4]) const {
     uint4 u[M];
@@ -34,15 +34,19 @@ struct Weights {
   uint4* at;
   int pieces;
 
-  __device__ __forceinline__ void fill(const BlockNormParams& p, int c) const {
+  template <typename T>
+  __device__ __forceinline__ void fill(const BlockNormParams& p, int c,
+                                       const bool (&mine)[kHalves<T>]) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+      if (!mine[i % kHalves<T>]) continue;
+      const int at_w = c + weight_column<T>(i);
       float4 w = make_float4(1.f, 1.f, 1.f, 1.f);
-      if (p.wpost) w = reinterpret_cast<const float4*>(p.wpost + (p.shared ? c % p.G : c))[i];
+      if (p.wpost) w = *reinterpret_cast<const float4*>(p.wpost + (p.shared ? at_w % p.G : at_w));
       w.x *= p.alpha, w.y *= p.alpha, w.z *= p.alpha, w.w *= p.alpha;
       reinterpret_cast<float4*>(at)[i * pieces] = w;
       w = make_float4(1.f, 1.f, 1.f, 1.f);
-      if (p.wpre) w = reinterpret_cast<const float4*>(p.wpre + c)[i];
+      if (p.wpre) w = *reinterpret_cast<const float4*>(p.wpre + at_w);
       reinterpret_cast<float4*>(at)[(2 + i) * pieces] = w;
     }
   }
@@ -69,8 +73,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int threads = blockDim.x * blockDim.y;
   const int rank = blockIdx.x % s.cluster;
   RowSum<SIMPLE> row_sum{buf, far, s.cluster, rank, 0};
-  const int c = rank * s.cols + threadIdx.x * 8;
-  const bool mine = threadIdx.x * 8 < s.cols && c < p.W;
+  const int at_row = first_column<T>(0), c = rank * s.cols + at_row;
+  bool mine[kHalves<T>];
+#pragma unroll
+  for (int i = 0; i < kHalves<T>; ++i)
+    mine[i] = at_row + i * kFar < s.cols && c + i * kFar < p.W;
   const bool heads = p.post && p.G != p.W;
   const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
   const Weights weights{reinterpret_cast<uint4*>(smem) + thread, threads};
@@ -78,16 +85,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int stage = s.arrays * Slots<T>::M * threads;
   constexpr int kGate = 1, kRes = 1 + GATE;
 
-  if (mine) weights.fill(p, c);
+  if (!mine[kHalves<T> - 1]) {  // columns past the row's hold zeros throughout
+#pragma unroll 1
+    for (int i = 0; i < 4 + s.stages * s.arrays * Slots<T>::M; ++i)
+      weights.at[i * threads] = make_uint4(0, 0, 0, 0);
+  }
+  weights.fill<T>(p, c, mine);
   if (s.cluster > 1) cluster_sync();  // every CTA runs before another writes to its memory
   const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
   const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
   const auto fetch = [&](int64_t row, int at) {
-    if (mine && row < p.T) {
+    if (row < p.T) {
       const Slots<T> to{ring + at * stage, threads};
-      to.fetch(0, static_cast<const T*>(p.x) + row * p.x_stride + c);
-      if (GATE) to.fetch(kGate, static_cast<const T*>(p.gate) + row * p.gate_stride + c);
-      if (p.residual) to.fetch(kRes, static_cast<const T*>(p.residual) + row * p.W + c);
+      to.fetch(0, static_cast<const T*>(p.x) + row * p.x_stride + c, mine);
+      if (GATE) to.fetch(kGate, static_cast<const T*>(p.gate) + row * p.gate_stride + c, mine);
+      if (p.residual) to.fetch(kRes, static_cast<const T*>(p.residual) + row * p.W + c, mine);
     }
     cp_async_commit();
   };
@@ -100,22 +112,25 @@ __global__ void __launch_bounds__(kThreads, 1)
     const Slots<T> in{ring + at * stage, threads};
     at = at + 1 == s.stages ? 0 : at + 1;
 
-    uint64_t y[4] = {}, t[4] = {}, w[4] = {};
-    if (mine) {
-      in.read(0, y);
-      weights.read(0, w);
-    }
+    uint64_t y[4], t[4] = {}, w[4];
+    in.read(0, y);
+    weights.read(0, w);
     if (p.post) {
-      float sum[1] = {dot8(y, y)};
-      if (heads) sum[0] = lanes_sum(sum[0], p.G / 8);
-      else row_sum(sum);
-      const uint64_t q = f2_dup(rsqrtf(sum[0] * per_group + p.eps));
+      float sum[2];
+      if (heads) {
+        group_sums<T>(y, y, p.G, sum);
+      } else {
+        float all[1] = {dot8(y, y)};
+        row_sum(all);
+        sum[0] = sum[1] = all[0];
+      }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], q);
+      for (int i = 0; i < 4; ++i)
+        w[i] = f2_mul(w[i], f2_dup(rsqrtf(sum[i / 2] * per_group + p.eps)));
     }
     if (GATE) {
       uint64_t sig[4] = {};
-      if (mine) in.read(kGate, t);
+      in.read(kGate, t);
       sigmoid8<T>(p.act, t, sig);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -123,20 +138,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         t[i] = 0;
       }
     }
-    if (p.residual && mine) in.read(kRes, t);
+    if (p.residual) in.read(kRes, t);
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = f2_fma(y[i], w[i], t[i]);
-    if (p.y && mine) store_pairs<T>(static_cast<T*>(p.y) + row * p.W + c, y);
+    if (p.y) store_row<T>(static_cast<T*>(p.y) + row * p.W + c, y, mine);
     if (p.pre) {
       float squares[1] = {dot8(y, y)};
       row_sum(squares);
       const uint64_t r = f2_dup(rsqrtf(squares[0] * per_row + p.eps));
-      if (mine) {
-        weights.read(1, w);
+      weights.read(1, w);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = f2_mul(y[i], f2_mul(w[i], r));
-        store_pairs<T>(static_cast<T*>(p.h) + row * p.W + c, y);
-      }
+      for (int i = 0; i < 4; ++i) y[i] = f2_mul(y[i], f2_mul(w[i], r));
+      store_row<T>(static_cast<T*>(p.h) + row * p.W + c, y, mine);
     }
   }
   if (s.cluster > 1) cluster_sync();  // none leaves while another may write to its memory
@@ -146,6 +159,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // added in order at the end.
 __global__ void __launch_bounds__(1024)
     block_norm_weights_kernel(const __grid_constant__ BlockNormParams p, int ctas, int cluster) {
+  constexpr int kInFlight = 16;
   __shared__ float buf[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int wide_post = p.shared ? p.G : p.W;
@@ -158,8 +172,14 @@ __global__ void __launch_bounds__(1024)
   float sum = 0.f;
   if (c < wide) {
     const float* at = p.part + (post ? 0 : (int64_t)ctas * wide_post) + c;
-#pragma unroll 4
-    for (int i = warp; i < n; i += 32) sum += at[(int64_t)i * wide];
+    for (int i0 = warp; i0 < n; i0 += 32 * kInFlight) {
+      float part[kInFlight];
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k)
+        part[k] = i0 + 32 * k < n ? at[(int64_t)(i0 + 32 * k) * wide] : 0.f;
+#pragma unroll
+      for (int k = 0; k < kInFlight; ++k) sum += part[k];
+    }
   }
   buf[warp][lane] = sum;
   __syncthreads();

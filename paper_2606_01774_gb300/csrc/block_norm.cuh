@@ -166,6 +166,57 @@ __device__ __forceinline__ float dot8(const uint64_t (&a)[4], const uint64_t (&b
   return pair_sum(f2_add(s, t));
 }
 
+// Where a thread's eight elements of a row lie.  In bf16 next to each other, sixteen bytes; in fp32
+// half of them, and the other half 128 elements on, so that a warp's accesses are whole
+// lines.  A warp has 256 elements either way.
+template <typename T>
+constexpr int kHalves = sizeof(T) == 4 ? 2 : 1;
+constexpr int kFar = 128;
+
+template <typename T>
+__device__ __forceinline__ int first_column(int vector) {
+  const int warp = (vector * blockDim.x + threadIdx.x) & ~31, lane = threadIdx.x & 31;
+  return warp * 8 + lane * (8 / kHalves<T>);
+}
+
+// Four weights of the eight: the i-th column they start at.
+template <typename T>
+__device__ __forceinline__ int weight_column(int i) {
+  return i * (kHalves<T> == 1 ? 4 : kFar);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(T* p, const uint64_t (&x)[4],
+                                          const bool (&mine)[kHalves<T>]) {
+  if constexpr (kHalves<T> == 1) {
+    if (mine[0]) store_pairs<T>(p, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float f[4];
+      f2_split(x[2 * i], f[0], f[1]);
+      f2_split(x[2 * i + 1], f[2], f[3]);
+      if (mine[i]) *reinterpret_cast<uint4*>(p + i * kFar) = Piece<float>::store(f);
+    }
+  }
+}
+
+// Sums of a_i b_i over the groups of the first four elements and of the other four.
+template <typename T>
+__device__ __forceinline__ void group_sums(const uint64_t (&a)[4], const uint64_t (&b)[4], int G,
+                                           float (&s)[2]) {
+  s[0] = pair_sum(f2_fma(a[1], b[1], f2_mul(a[0], b[0])));
+  s[1] = pair_sum(f2_fma(a[3], b[3], f2_mul(a[2], b[2])));
+  if (kHalves<T> == 1) {
+    s[0] = s[1] = lanes_sum(s[0] + s[1], G / 8);
+  } else if (G == 2 * kFar) {
+    s[0] = s[1] = lanes_sum(s[0] + s[1], 32);
+  } else {
+    s[0] = lanes_sum(s[0], G / 4);
+    s[1] = lanes_sum(s[1], G / 4);
+  }
+}
+
 // The teams of a call.
 struct Shape {
   int team, teams, cluster, ctas;  // threads of a CTA's team, teams of a CTA, CTAs of a cluster

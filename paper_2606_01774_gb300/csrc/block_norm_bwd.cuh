@@ -32,10 +32,10 @@ struct Own {
   static __device__ __forceinline__ uint32_t input(uint32_t own, int row, int array, int j) {
     return own + (kRow + ((row * kInputs + array) * V + j) * M) * kUnit;
   }
-  static __device__ __forceinline__ void fetch(uint32_t to, const T* src) {
+  static __device__ __forceinline__ void fetch(uint32_t to, const T* src, const bool (&mine)[M]) {
 #pragma unroll
     for (int i = 0; i < M; ++i)
-      cp_async16(to + i * kUnit, reinterpret_cast<const uint4*>(src) + i);
+      if (mine[i]) cp_async16(to + i * kUnit, src + i * kFar);
   }
   template <typename U = T>
   static __device__ __forceinline__ void read(uint32_t at, uint64_t (&v)[4]) {
@@ -54,6 +54,17 @@ struct Own {
 // V vectors of eight elements of a row per thread.  The sum of the next row's squares
 // goes along with this row's last sum, so x arrives a row ahead of the other inputs.  What a sum
 // separates is read again after it, rather than held.  alpha enters by the rows' factors alone.
+// A weight's gradients of a thread's elements of type T.
+template <typename T>
+__device__ __forceinline__ void store_weights(float* p, const uint64_t (&x)[4],
+                                              const bool (&mine)[kHalves<T>]) {
+  if constexpr (kHalves<T> == 1) {
+    if (mine[0]) store_pairs<float>(p, x);
+  } else {
+    store_row<float>(p, x, mine);
+  }
+}
+
 // What a call has, where the compiler knows it.
 enum Form {
   kAny,
@@ -74,25 +85,33 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
   const int rank = blockIdx.x % s.cluster;
   RowSum<SIMPLE> row_sum{buf, far, s.cluster, rank, 0};
   const uint32_t own = (uint32_t)__cvta_generic_to_shared(smem) + thread * 16;
-  // columns past the row's hold zeros throughout
   uint4* units = reinterpret_cast<uint4*>(smem) + thread;
-#pragma unroll 1
-  for (int i = 0; i < O::kUnits; ++i) units[i * THREADS] = make_uint4(0, 0, 0, 0);
+  constexpr int H = kHalves<T>;
   int c[V];
-  bool mine[V];
+  bool mine[V][H];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int at = (j * blockDim.x + threadIdx.x) * 8;
+    const int at = first_column<T>(j);
     c[j] = rank * s.cols + at;
-    mine[j] = at < s.cols && c[j] < p.W;
-    if (!mine[j]) continue;
+#pragma unroll
+    for (int i = 0; i < H; ++i)
+      mine[j][i] = at + i * kFar < s.cols && c[j] + i * kFar < p.W;
+  }
+  // columns past the row's and inputs that the call has not hold zeros throughout
+  if (!FULL || !mine[V - 1][H - 1]) {
+#pragma unroll 1
+    for (int i = 0; i < O::kUnits; ++i) units[i * THREADS] = make_uint4(0, 0, 0, 0);
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
     for (int i = 0; i < 2; ++i) {
+      if (!mine[j][i % H]) continue;
+      const int at_w = c[j] + weight_column<T>(i);
       float4* to = reinterpret_cast<float4*>(units + (2 * j + i) * THREADS);
       const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-      to[0] = p.wpost
-                  ? reinterpret_cast<const float4*>(p.wpost + (p.shared ? c[j] % p.G : c[j]))[i]
-                  : one;
-      to[2 * V * THREADS] = p.wpre ? reinterpret_cast<const float4*>(p.wpre + c[j])[i] : one;
+      to[0] = p.wpost ? *reinterpret_cast<const float4*>(p.wpost + (p.shared ? at_w % p.G : at_w))
+                      : one;
+      to[2 * V * THREADS] = p.wpre ? *reinterpret_cast<const float4*>(p.wpre + at_w) : one;
     }
   }
   const bool post_norm = FULL || p.post, pre_norm = FULL || (FORM == kAny && p.pre);
@@ -106,17 +125,15 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
     if (row >= p.T) return;
     const T* src = static_cast<const T*>(p.x) + row * p.x_stride;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (mine[j]) O::fetch(O::x(own, at, j), src + c[j]);
+    for (int j = 0; j < V; ++j) O::fetch(O::x(own, at, j), src + c[j], mine[j]);
   };
   const auto fetch = [&](int64_t row, int at) {
     if (row >= p.T) return;
     const int64_t dense = row * p.W;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (!mine[j]) continue;
       const auto copy = [&](int array, const void* src, int64_t from) {
-        O::fetch(O::input(own, at, array, j), static_cast<const T*>(src) + (from + c[j]));
+        O::fetch(O::input(own, at, array, j), static_cast<const T*>(src) + (from + c[j]), mine[j]);
       };
       if (GATE) copy(O::kGate, p.gate, row * p.gate_stride);
       if (use_res) copy(O::kRes, p.residual, dense);
@@ -133,22 +150,32 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
   fetch_x(first + step, 1);
   cp_async_commit();
   cp_async_wait<2>();
-  const auto squares = [&](int at, int j) {  // of a vector, over its group where it has one
+  // of a vector, over its groups where it has some (else all of it in the first)
+  const auto sums_of = [&](const uint64_t (&a)[4], const uint64_t (&b)[4], float (&sum)[2]) {
+    if (heads) group_sums<T>(a, b, p.G, sum);
+    else sum[0] = sum[1] = dot8(a, b);
+  };
+  const auto squares = [&](int at, int j, float (&sum)[2]) {
     uint64_t x[4];
     O::read(O::x(own, at, j), x);
-    const float sum = dot8(x, x);
-    return heads ? lanes_sum(sum, p.G / 8) : sum;
+    sums_of(x, x, sum);
   };
-  float q[V];
+  float q[V][2];  // of a vector's halves
 #pragma unroll
-  for (int j = 0; j < V; ++j) q[j] = 1.f;
+  for (int j = 0; j < V; ++j) q[j][0] = q[j][1] = 1.f;
   if (post_norm) {
-    float sum[1] = {0.f}, by[V];
+    float sum[1] = {0.f}, by[V][2];
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum[0] += by[j] = squares(0, j);
+    for (int j = 0; j < V; ++j) {
+      squares(0, j, by[j]);
+      sum[0] += by[j][0];
+    }
     if (!heads) row_sum(sum);
 #pragma unroll
-    for (int j = 0; j < V; ++j) q[j] = rsqrtf((heads ? by[j] : sum[0]) * per_group + p.eps);
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        q[j][i] = rsqrtf((heads ? by[j][i] : sum[0]) * per_group + p.eps);
   }
   int at = 0;
   for (int64_t row = first; row < p.T; row += step) {
@@ -173,9 +200,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = f2_mul(w[i], activation(p.act, t[i], sig[i]));
         }
-        const uint64_t qa = f2_dup(q[j] * p.alpha);
+        const uint64_t qa[2] = {f2_dup(q[j][0] * p.alpha), f2_dup(q[j][1] * p.alpha)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[j][i] = f2_fma(x[i], f2_mul(w[i], qa), y[j][i]);
+        for (int i = 0; i < 4; ++i) y[j][i] = f2_fma(x[i], f2_mul(w[i], qa[i / 2]), y[j][i]);
         O::read(O::input(own, at, O::kDh, j), t);
         O::template read<float>(O::weight(own, 1, j), w);
 #pragma unroll
@@ -204,59 +231,63 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
       for (int j = 0; j < V; ++j) O::read(O::input(own, at, O::kDy, j), g[j]);
     }
     cp_async_wait<1>();  // the next row's x
-    float sums[2] = {0.f, 0.f}, dot[V], next[V];
+    float sums[2] = {0.f, 0.f}, dot[V][2], next[V][2];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if ((FULL || p.dres) && mine[j]) store_pairs<T>(static_cast<T*>(p.dres) + (row * p.W + c[j]), g[j]);
+      if (FULL || p.dres)
+        store_row<T>(static_cast<T*>(p.dres) + (row * p.W + c[j]), g[j], mine[j]);
       uint64_t x[4], w[4];
       O::read(O::x(own, at, j), x);
       O::template read<float>(O::weight(own, 0, j), w);
-      const uint64_t qq = f2_dup(q[j]);
+      const uint64_t qq[2] = {f2_dup(q[j][0]), f2_dup(q[j][1])};
       if (GATE) {
         uint64_t z[4], sig[4];
         O::read(O::input(own, at, O::kGate, j), z);
         sigmoid8<T>(p.act, z, sig);
-        const uint64_t qa = f2_dup(q[j] * p.alpha);
+        const uint64_t qa[2] = {f2_dup(q[j][0] * p.alpha), f2_dup(q[j][1] * p.alpha)};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint64_t n = f2_mul(x[i], f2_mul(w[i], qa));
+          const uint64_t n = f2_mul(x[i], f2_mul(w[i], qa[i / 2]));
           const uint64_t a = activation(p.act, z[i], sig[i]);
           z[i] = f2_mul(activation_slope(p.act, z[i], sig[i]), f2_mul(g[j][i], n));
           g[j][i] = f2_mul(g[j][i], a);
         }
-        if (mine[j])
-          store_pairs<T>(static_cast<T*>(p.dgate) + (row * p.gate_stride + c[j]), z);
+        store_row<T>(static_cast<T*>(p.dgate) + (row * p.gate_stride + c[j]), z, mine[j]);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        dwpost[j][i] = f2_fma(g[j][i], f2_mul(x[i], qq), dwpost[j][i]);
+        dwpost[j][i] = f2_fma(g[j][i], f2_mul(x[i], qq[i / 2]), dwpost[j][i]);
         g[j][i] = f2_mul(g[j][i], w[i]);
       }
       if (post_norm) {
-        dot[j] = dot8(x, g[j]);
-        if (heads) dot[j] = lanes_sum(dot[j], p.G / 8);
-        next[j] = row + step < p.T ? squares(at ^ 1, j) : 0.f;
-        sums[0] += dot[j];
-        sums[1] += next[j];
+        sums_of(x, g[j], dot[j]);
+        next[j][0] = next[j][1] = 0.f;
+        if (row + step < p.T) squares(at ^ 1, j, next[j]);
+        sums[0] += dot[j][0];
+        sums[1] += next[j][0];
       }
     }
     if (post_norm && !heads) row_sum(sums);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      const float qa = q[j] * p.alpha;
-      if (post_norm) {
-        const float inner = heads ? dot[j] : sums[0];
-        const uint64_t back = f2_dup(-(inner * per_group * qa * q[j] * q[j]));
-        uint64_t x[4];
-        O::read(O::x(own, at, j), x);
+      uint64_t x[4];
+      if (post_norm) O::read(O::x(own, at, j), x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[j][i] = f2_fma(x[i], back, f2_mul(g[j][i], f2_dup(qa)));
-        q[j] = rsqrtf((heads ? next[j] : sums[1]) * per_group + p.eps);
-      } else {
+      for (int k = 0; k < 2; ++k) {
+        const float qa = q[j][k] * p.alpha;
+        if (post_norm) {
+          const float inner = heads ? dot[j][k] : sums[0];
+          const uint64_t back = f2_dup(-(inner * per_group * qa * q[j][k] * q[j][k]));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[j][i] = f2_mul(g[j][i], f2_dup(qa));
+          for (int i = 2 * k; i < 2 * k + 2; ++i)
+            g[j][i] = f2_fma(x[i], back, f2_mul(g[j][i], f2_dup(qa)));
+          q[j][k] = rsqrtf((heads ? next[j][k] : sums[1]) * per_group + p.eps);
+        } else {
+#pragma unroll
+          for (int i = 2 * k; i < 2 * k + 2; ++i) g[j][i] = f2_mul(g[j][i], f2_dup(qa));
+        }
       }
-      if (mine[j]) store_pairs<T>(static_cast<T*>(p.dx) + (row * p.x_stride + c[j]), g[j]);
+      store_row<T>(static_cast<T*>(p.dx) + (row * p.x_stride + c[j]), g[j], mine[j]);
     }
     fetch_x(row + 2 * step, at);
     cp_async_commit();
@@ -277,13 +308,14 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
   if (!p.shared && blockDim.y == 1) {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      if (mine[j]) {
-        store_pairs<float>(post + c[j], dwpost[j]);
-        store_pairs<float>(pre + c[j], dwpre[j]);
-      }
+      store_weights<T>(post + c[j], dwpost[j], mine[j]);
+      store_weights<T>(pre + c[j], dwpre[j], mine[j]);
     }
     return;
   }
+  bool all[H];
+#pragma unroll
+  for (int i = 0; i < H; ++i) all[i] = true;
   float* sums = reinterpret_cast<float*>(smem);  // [teams][columns]
   const int cols = blockDim.x * 8 * V, from = rank * s.cols;
   const int used = min(min(cols, s.cols), p.W - from);
@@ -291,8 +323,8 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      store_pairs<float>(sums + threadIdx.y * cols + (j * blockDim.x + threadIdx.x) * 8,
-                         kind ? dwpre[j] : dwpost[j]);
+      store_weights<T>(sums + threadIdx.y * cols + first_column<T>(j), kind ? dwpre[j] : dwpost[j],
+                       all);
     __syncthreads();
     const bool by_group = p.shared && !kind;
     const int n = by_group ? p.G : used;

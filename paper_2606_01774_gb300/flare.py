@@ -410,15 +410,27 @@ def _device():
     return _device()
 
 
-def _d(t, device):
-    """Data pointer of a contiguous tensor on the current device."""
-    if t is None:
-        return None
-    if t.get_device() != device:
-        raise ValueError("tensors must be on the current device")
-    if not t.is_contiguous():
+def _dense(device, *tensors):
+    """Data pointers of contiguous tensors on the current device, None for None."""
+    there = [t for t in tensors if t is not None]
+    if not all(map(_is_contiguous, there)):
         raise ValueError("only the rows of q, k, v, x, gate and their gradients may be strided")
-    return t.data_ptr()
+    for at in map(_get_device, there):
+        if at != device:
+            raise ValueError("tensors must be on the current device")
+    return [None if t is None else t.data_ptr() for t in tensors]
+
+
+def _is_contiguous(t):
+    global _is_contiguous, _get_device
+    from torch import Tensor
+
+    _is_contiguous, _get_device = Tensor.is_contiguous, Tensor.get_device
+    return t.is_contiguous()
+
+
+def _get_device(t):
+    return t.get_device()
 
 
 def _rows(t, step, inner, device):
@@ -429,8 +441,11 @@ def _rows(t, step, inner, device):
         return None
     if t.get_device() != device:
         raise ValueError("tensors must be on the current device")
-    if step and t.dim() == inner + 1 and t.stride(0) == step and (
-            t.stride(-1) == 1 and (inner == 1 or t.stride(-2) == t.shape[-1])):
+    strides = t.stride()
+    if len(strides) == inner + 1 and strides[0] == step and (
+            strides[-1] == 1 and (inner == 1 or strides[1] == t.shape[2])):
+        return t.data_ptr()
+    if not step and t.is_contiguous():
         return t.data_ptr()
     dense = 1
     for i in range(t.dim() - 1, -1, -1):
@@ -443,7 +458,12 @@ def _rows(t, step, inner, device):
 
 
 def flare_rotary_table(desc, table, stream=None) -> int:
-    return load().flare_rotary_table(ctypes.byref(desc), _d(table, _device()), _stream(stream))
+    return load().flare_rotary_table(ctypes.byref(desc), *_dense(_device(), table),
+                                     _stream(stream))
+
+
+def _in_place(out, source):
+    return out is not None and source is not None and out.data_ptr() == source.data_ptr()
 
 
 def flare_rotary(desc, q, k, table, position, prefix_len, token_len, parent, token_start, q_out,
@@ -451,18 +471,16 @@ def flare_rotary(desc, q, k, table, position, prefix_len, token_len, parent, tok
     """q, k (and the outputs written in place) have rows q_stride and k_stride apart."""
     dev = _device()
     qs, ks = desc.q_stride, desc.k_stride
-    return load().flare_rotary(
-        ctypes.byref(desc), _rows(q, qs, 2, dev), _rows(k, ks, 2, dev), _d(table, dev),
-        _d(position, dev), _d(prefix_len, dev), _d(token_len, dev), _d(parent, dev),
-        _d(token_start, dev), _out_rows(q_out, q, qs, dev), _out_rows(k_out, k, ks, dev),
-        _d(dev_status, dev), _stream(stream))
-
-
-def _out_rows(out, source, step, device):
-    """An output is dense, or its input's own rows."""
-    if out is not None and source is not None and out.data_ptr() == source.data_ptr():
-        return _rows(out, step, 2, device)
-    return _d(out, device)
+    q_at, k_at = _rows(q, qs, 2, dev), _rows(k, ks, 2, dev)
+    q_to = k_to = None
+    if _in_place(q_out, q):
+        q_to, q_out = _rows(q_out, qs, 2, dev), None
+    if _in_place(k_out, k):
+        k_to, k_out = _rows(k_out, ks, 2, dev), None
+    *ins, qo, ko, status = _dense(dev, table, position, prefix_len, token_len, parent, token_start,
+                                  q_out, k_out, dev_status)
+    return load().flare_rotary(ctypes.byref(desc), q_at, k_at, *ins, q_to or qo, k_to or ko, status,
+                               _stream(stream))
 
 
 def flare_rotary_append_kv(desc, q, k, v, table, position, prefix_len, token_len, token_start,
@@ -470,32 +488,33 @@ def flare_rotary_append_kv(desc, q, k, v, table, position, prefix_len, token_len
                            stream=None) -> int:
     dev = _device()
     qs, ks = desc.q_stride, desc.k_stride
-    return load().flare_rotary_append_kv(
-        ctypes.byref(desc), _rows(q, qs, 2, dev), _rows(k, ks, 2, dev),
-        _rows(v, desc.v_stride, 2, dev), _d(table, dev), _d(position, dev), _d(prefix_len, dev),
-        _d(token_len, dev), _d(token_start, dev), _d(page_table, dev),
-        _out_rows(q_out, q, qs, dev), _out_rows(k_out, k, ks, dev), _d(k_pool, dev),
-        _d(v_pool, dev), _d(dev_status, dev), _stream(stream))
+    q_at, k_at, v_at = _rows(q, qs, 2, dev), _rows(k, ks, 2, dev), _rows(v, desc.v_stride, 2, dev)
+    q_to = k_to = None
+    if _in_place(q_out, q):
+        q_to, q_out = _rows(q_out, qs, 2, dev), None
+    if _in_place(k_out, k):
+        k_to, k_out = _rows(k_out, ks, 2, dev), None
+    *ins, qo, ko, kp, vp, status = _dense(dev, table, position, prefix_len, token_len, token_start,
+                                          page_table, q_out, k_out, k_pool, v_pool, dev_status)
+    return load().flare_rotary_append_kv(ctypes.byref(desc), q_at, k_at, v_at, *ins, q_to or qo,
+                                         k_to or ko, kp, vp, status, _stream(stream))
 
 
 def flare_tree_logits(desc, logits, history, history_len, output_start, token, parent, node_len,
                       repetition, presence, frequency, bias_token, bias_value, bias_len, mask,
                       out, dev_status, stream=None) -> int:
-    dev = _device()
     return load().flare_tree_logits(
-        ctypes.byref(desc), _d(logits, dev), _d(history, dev), _d(history_len, dev),
-        _d(output_start, dev), _d(token, dev), _d(parent, dev), _d(node_len, dev),
-        _d(repetition, dev), _d(presence, dev), _d(frequency, dev), _d(bias_token, dev),
-        _d(bias_value, dev), _d(bias_len, dev), _d(mask, dev), _d(out, dev), _d(dev_status, dev),
-        _stream(stream))
+        ctypes.byref(desc),
+        *_dense(_device(), logits, history, history_len, output_start, token, parent, node_len,
+                repetition, presence, frequency, bias_token, bias_value, bias_len, mask, out,
+                dev_status), _stream(stream))
 
 
 def flare_block_norm(desc, x, gate, residual, post_weight, pre_weight, y, h, stream=None) -> int:
     dev = _device()
     return load().flare_block_norm(
         ctypes.byref(desc), _rows(x, desc.x_stride, 1, dev), _rows(gate, desc.gate_stride, 1, dev),
-        _d(residual, dev), _d(post_weight, dev), _d(pre_weight, dev), _d(y, dev), _d(h, dev),
-        _stream(stream))
+        *_dense(dev, residual, post_weight, pre_weight, y, h), _stream(stream))
 
 
 def flare_block_norm_bwd_workspace_size(desc) -> int:
@@ -511,12 +530,13 @@ def flare_block_norm_bwd(desc, x, gate, residual, post_weight, pre_weight, dy, d
     """dx and dgate have their inputs' strides."""
     dev = _device()
     xs, gs = desc.x_stride, desc.gate_stride
+    (res, w_post, w_pre, dy, dh, dres, dw_post, dw_pre, work) = _dense(
+        dev, residual, post_weight, pre_weight, dy, dh, dresidual, dpost_weight, dpre_weight,
+        workspace)
     return load().flare_block_norm_bwd(
-        ctypes.byref(desc), _rows(x, xs, 1, dev), _rows(gate, gs, 1, dev), _d(residual, dev),
-        _d(post_weight, dev), _d(pre_weight, dev), _d(dy, dev), _d(dh, dev),
-        _rows(dx, xs, 1, dev), _rows(dgate, gs, 1, dev), _d(dresidual, dev),
-        _d(dpost_weight, dev), _d(dpre_weight, dev), _d(workspace, dev), int(workspace_bytes),
-        _stream(stream))
+        ctypes.byref(desc), _rows(x, xs, 1, dev), _rows(gate, gs, 1, dev), res, w_post, w_pre, dy,
+        dh, _rows(dx, xs, 1, dev), _rows(dgate, gs, 1, dev), dres, dw_post, dw_pre, work,
+        int(workspace_bytes), _stream(stream))
 
 
 def flare_debug_gather_prefix(desc, k_pool, v_pool, page_table, prefix_len, request, k_out,
