@@ -782,7 +782,8 @@ flare_status flare_rotary_table(const flare_rotary_freq_desc* desc, uint64_t* ta
  *   parent         [R, B] int32, nullable
  *   token_start    [R + 1] int32, not decreasing, within [0, T]; nullable
  *   q_out, k_out   act_dtype, dense, or the input's own pointer: in place, with
- *                  its stride (any other overlap with the input is rejected)
+ *                  its stride (any other overlap with an input, or of the outputs,
+ *                  is rejected)
  *   dev_status     FLARE_DEV_BAD_PREFIX_LEN (negative), FLARE_DEV_BAD_ACCEPT_LEN
  *                  (token_len outside [0, B]), FLARE_DEV_BAD_TREE: the request is skipped;
  *                  FLARE_DEV_BAD_ACCEPT_LEN also for a wrong token_start, whose rows
@@ -806,7 +807,8 @@ flare_status flare_rotary(const flare_rotary_desc* desc, const void* q, const vo
  *   prefix_len     [R] int32
  *   page_table     [R, max_pages_per_req] int32
  *   k_out          nullable
- *   k_pool, v_pool [num_pages, Hkv, p, D] act_dtype, written in place
+ *   k_pool, v_pool [num_pages, Hkv, p, D] act_dtype, written in place, clear of each
+ *                  other and of the rows
  *   dev_status     as above; FLARE_DEV_BAD_PREFIX_LEN also for prefix_len[r] + n
  *                  beyond the table (the request is skipped); FLARE_DEV_BAD_PAGE: the
  *                  tokens of that page are skipped.
@@ -873,9 +875,10 @@ flare_status flare_tree_logits(const flare_tree_logits_desc* desc, const void* l
  *   residual     [T, W] act_dtype, dense; nullable
  *   post_weight  [W] or [G] fp32; nullable (1)
  *   pre_weight   [W] fp32; nullable (1)
- *   y            [T, W] act_dtype, dense, nullable; may be `residual` (in place) or a
- *                dense x
- *   h            [T, W] act_dtype, dense; with pre_norm only; may be a dense x
+ *   y            [T, W] act_dtype, dense, nullable
+ *   h            [T, W] act_dtype, dense; with pre_norm only
+ * An output may take a dense input's place (its pointer: y the residual's, h that of x);
+ * any other overlap with an input, or of the outputs, is rejected.
  */
 flare_status flare_block_norm(const flare_block_norm_desc* desc, const void* x, const void* gate,
                               const void* residual, const float* post_weight,
@@ -894,7 +897,9 @@ flare_status flare_block_norm_bwd_workspace_size(const flare_block_norm_desc* de
  *   dh         [T, W] act_dtype, dense; with pre_norm only
  *   dx         as x (same stride)
  *   dgate      as gate (same stride); with a gate only
- *   dresidual  [T, W] act_dtype, dense; nullable; may be dy (in place)
+ *   dresidual  [T, W] act_dtype, dense; nullable.  Of these three each may take the place of
+ *              an input of the same stride (dx that of x, dresidual that of dy; rows of the same
+ *              stride may lie between each other's); any other overlap is rejected
  *   dpost_weight, dpre_weight  fp32 as the weights; nullable; written, not added to
  *   workspace  >= flare_block_norm_bwd_workspace_size bytes, 256-byte aligned (may be
  *              NULL when neither weight gradient is asked for)

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <initializer_list>
 
 #include "flare.h"
 #include "kernels.h"
@@ -130,6 +131,48 @@ size_t span_bytes(int64_t rows, int64_t stride, int64_t width, size_t elem) {
   return rows > 0 ? (size_t)((rows - 1) * stride + width) * elem : 0;
 }
 
+// Rows of an array: `width` elements each, `stride` apart.
+struct Rows {
+  const void* at;
+  int64_t stride, width;
+};
+
+// Whether two arrays of `rows` rows share an element.  Rows of the same stride may lie between each
+// other, as slices of one projection do.
+bool rows_overlap(const Rows& a, const Rows& b, int64_t rows, size_t elem) {
+  if (!a.at || !b.at || !overlap(a.at, span_bytes(rows, a.stride, a.width, elem), b.at,
+                                 span_bytes(rows, b.stride, b.width, elem)))
+    return false;
+  if (a.stride != b.stride) return true;
+  const int64_t step = a.stride * (int64_t)elem;
+  int64_t off = (int64_t)((intptr_t)b.at - (intptr_t)a.at) % step;
+  if (off < 0) off += step;
+  return off < a.width * (int64_t)elem || off + b.width * (int64_t)elem > step;
+}
+
+// Whether every output is clear of the other outputs and of every input, unless it takes an
+// input's very place: then each element is read before it is written, by the same thread.
+// `own` (rotary): the only input whose place output i may take is the i-th.
+bool outputs_clear(const Rows* in, int n_in, const Rows* out, int n_out, bool own, int64_t rows,
+                   size_t elem) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j) {
+      const bool same = in[j].at == out[i].at && in[j].stride == out[i].stride &&
+                        in[j].width == out[i].width && (!own || i == j);
+      if (!same && rows_overlap(in[j], out[i], rows, elem)) return false;
+    }
+    for (int j = 0; j < i; ++j)
+      if (rows_overlap(out[j], out[i], rows, elem)) return false;
+  }
+  return true;
+}
+
+bool aligned4(std::initializer_list<const void*> arrays) {
+  for (const void* p : arrays)
+    if (!aligned(p, 4)) return false;
+  return true;
+}
+
 flare_status check_rotary(const flare_rotary_desc* d, bool packed, bool append) {
   if (!d) return FLARE_ERR_INVALID_ARGUMENT;
   if (d->num_requests < 0 || (packed ? d->num_tokens < 0 : d->block_len < 1) ||
@@ -194,11 +237,20 @@ flare_status rotary(const flare_rotary_desc* d, const void* q, const void* k, co
   p.q_out_stride = q_out == q ? p.q_stride : q_width;
   p.k_out_stride = k_out == k ? p.k_stride : k_width;
   const size_t e = elem_bytes(d->act_dtype);
-  if ((q && q_out != q && overlap(q, span_bytes(rows, p.q_stride, q_width, e), q_out,
-                                  span_bytes(rows, q_width, q_width, e))) ||
-      (k && k_out && k_out != k && overlap(k, span_bytes(rows, p.k_stride, k_width, e), k_out,
-                                           span_bytes(rows, k_width, k_width, e))))
+  const Rows in[3] = {{q, p.q_stride, q_width}, {k, p.k_stride, k_width}, {v, p.v_stride, k_width}};
+  const Rows out[2] = {{q_out, p.q_out_stride, q_width}, {k_out, p.k_out_stride, k_width}};
+  if (!outputs_clear(in, 3, out, 2, true, rows, e) ||
+      !aligned4({position, prefix_len, token_len, parent, token_start, page_table, dev_status}))
     return FLARE_ERR_INVALID_ARGUMENT;
+  if (k_pool) {
+    const size_t pool = (size_t)p.num_pages * p.Hkv * p.page_size * p.D * e;
+    for (const Rows& r : {in[0], in[1], in[2], out[0], out[1]}) {
+      const size_t bytes = r.at ? span_bytes(rows, r.stride, r.width, e) : 0;
+      if (overlap(r.at, bytes, k_pool, pool) || overlap(r.at, bytes, v_pool, pool))
+        return FLARE_ERR_INVALID_ARGUMENT;
+    }
+    if (overlap(k_pool, pool, v_pool, pool)) return FLARE_ERR_INVALID_ARGUMENT;
+  }
   p.q = q;
   p.k = k;
   p.v = v;
@@ -1031,7 +1083,9 @@ flare_status flare_tree_logits(const flare_tree_logits_desc* d, const void* logi
   const size_t e = elem_bytes(d->logits_dtype);
   const size_t bytes = (size_t)d->num_requests * d->num_nodes * d->vocab_size * e;
   if (!aligned(logits, e) || !aligned(out, e) ||
-      (out != logits && overlap(logits, bytes, out, bytes)))
+      (out != logits && overlap(logits, bytes, out, bytes)) ||
+      !aligned4({history, history_len, output_start, token, parent, node_len, repetition, presence,
+                 frequency, bias_token, bias_value, bias_len, mask, dev_status}))
     return FLARE_ERR_INVALID_ARGUMENT;
   TreeLogitsParams p;
   memset(&p, 0, sizeof p);
@@ -1073,7 +1127,10 @@ flare_status flare_block_norm(const flare_block_norm_desc* d, const void* x, con
       !aligned16(pre_weight) || !aligned16(y) || !aligned16(h))
     return FLARE_ERR_INVALID_ARGUMENT;
   BlockNormParams p = block_norm_params(d, x, gate, residual, post_weight, pre_weight);
-  if (y == h || ((y == x || h == x) && p.x_stride != p.W)) return FLARE_ERR_INVALID_ARGUMENT;
+  const Rows in[3] = {{x, p.x_stride, p.W}, {gate, p.gate_stride, p.W}, {residual, p.W, p.W}};
+  const Rows out[2] = {{y, p.W, p.W}, {h, p.W, p.W}};
+  if (!outputs_clear(in, 3, out, 2, false, p.T, elem_bytes(d->act_dtype)))
+    return FLARE_ERR_INVALID_ARGUMENT;
   p.y = y;
   p.h = h;
   const cudaError_t e = launch_block_norm(p, d->act_dtype == FLARE_DT_BF16, device_sms(),
@@ -1109,6 +1166,11 @@ flare_status flare_block_norm_bwd(const flare_block_norm_desc* d, const void* x,
       !aligned(dpre_weight, 4))
     return FLARE_ERR_INVALID_ARGUMENT;
   BlockNormParams p = block_norm_params(d, x, gate, residual, post_weight, pre_weight);
+  const Rows in[5] = {{x, p.x_stride, p.W}, {gate, p.gate_stride, p.W}, {residual, p.W, p.W},
+                      {dy, p.W, p.W}, {dh, p.W, p.W}};
+  const Rows out[3] = {{dx, p.x_stride, p.W}, {dgate, p.gate_stride, p.W}, {dresidual, p.W, p.W}};
+  if (!outputs_clear(in, 5, out, 3, false, p.T, elem_bytes(d->act_dtype)))
+    return FLARE_ERR_INVALID_ARGUMENT;
   const bool weights = dpost_weight || dpre_weight;
   if (weights) {
     size_t need;

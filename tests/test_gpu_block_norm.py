@@ -46,6 +46,47 @@ def test_gradients_match_the_definition(case, dtype):
     assert torch.equal(bits(bare["dx"]), bits(got["dx"]))
 
 
+MORE = [
+    dict(T=700, W=6400, group=128, gate="silu", shared=True), dict(T=500, W=7424, gate="sigmoid"),
+    dict(T=1500, W=4096), dict(T=400, W=6144), dict(T=5000, W=2048, gate="silu"),
+    dict(T=333, W=5632, group=256, post=True, residual=False),
+    dict(T=2500, W=1360, gate="silu", residual=False), dict(T=3001, W=512, group=64, pre=False),
+    dict(T=160, W=16384), dict(T=310, W=9000, gate="silu", pre=False, residual=False),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", MORE, ids=str)
+def test_several_rows_to_every_team(case, dtype):
+    s = norm_inputs(30 + case["W"], dtype=dtype, **case)
+    check_norm(s, *run_norm(s))
+    check_norm_bwd(s, run_norm_bwd(s))
+
+
+def test_gradients_in_their_inputs_place():
+    """dx, dgate and dresidual over x, gate and residual, slices of one projection; over dy and dh."""
+    s = norm_inputs(20, 900, 1024, gate="silu", group=128)
+    want = run_norm_bwd(s)
+    both = torch.cat([s.x, s.gate], 1)
+    x, gate = both.split(1024, 1)
+    d = s.desc
+    d.x_stride = d.gate_stride = 2048
+    ws = torch.empty(flare.flare_block_norm_bwd_workspace_size(d), dtype=torch.uint8, device="cuda")
+    res = s.residual.clone()
+    w = [torch.empty_like(s.post_weight), torch.empty_like(s.pre_weight)]
+    flare.check(flare.flare_block_norm_bwd(d, x, gate, res, s.post_weight, s.pre_weight, s.dy, s.dh,
+                                           x, gate, res, *w, ws, ws.numel()))
+    for a, b in ((x, "dx"), (gate, "dgate"), (res, "dresidual"), (w[0], "dpost_weight"),
+                 (w[1], "dpre_weight")):
+        assert torch.equal(bits(a), bits(want[b])), b
+    d.x_stride = d.gate_stride = 0
+    dy, dh = s.dy.clone(), s.dh.clone()
+    dgate = torch.empty_like(s.gate)
+    flare.check(flare.flare_block_norm_bwd(d, s.x, s.gate, s.residual, s.post_weight, s.pre_weight,
+                                           dy, dh, dh, dgate, dy, None, None, None, 0))
+    assert torch.equal(bits(dh), bits(want["dx"])) and torch.equal(bits(dy), bits(want["dresidual"]))
+
+
 def test_no_gradient_at_y():
     s = norm_inputs(3, 20, 512, gate="silu", dy=False)
     check_norm_bwd(s, run_norm_bwd(s))

@@ -131,6 +131,47 @@ def test_overlaps(lib):
     assert run(lib, "flare_block_norm", norm(x_stride=2048), x=AT, y=AT) == BAD
 
 
+def test_overlaps_of_rows(lib):
+    """Every pair of an output and another array that share bytes but are not the same rows."""
+    wide, rows = 1024 * 2, 8  # of norm()
+    at = lambda call, n: AT + (NAMES[call].split().index(n) << 32)  # noqa: E731
+    outs = {"flare_block_norm": ("y h", "x gate residual"),
+            "flare_block_norm_bwd": ("dx dgate dresidual", "x gate residual dy dh")}
+    for call, (outputs, inputs) in outs.items():
+        for o in outputs.split():
+            for i in inputs.split() + [n for n in outputs.split() if n != o]:
+                for off in (16, -16, wide * (rows - 1)):
+                    assert run(lib, call, **{o: at(call, i) + off}) == BAD, (call, o, i)
+            for i in outputs.split():
+                if i != o:
+                    assert run(lib, call, **{o: at(call, i)}) == BAD, (call, o, i)
+    # rows of one stride between each other: fine while none reaches into another's
+    d = norm(x_stride=2048, gate_stride=2048)
+    a = at("flare_block_norm_bwd", "dx")
+    for off in (wide - 16, 16, 2 * wide - 16):
+        assert run(lib, "flare_block_norm_bwd", d, dgate=a + off) == BAD
+    assert run(lib, "flare_block_norm_bwd", norm(x_stride=2048, gate_stride=4096),
+               dgate=a + wide) == BAD
+    assert run(lib, "flare_block_norm_bwd", d, dgate=a + wide, workspace=None) == BAD
+    for call in ("flare_rotary", "flare_rotary_append_kv"):
+        assert run(lib, call, q_out=at(call, "k")) == BAD  # another input's place
+        assert run(lib, call, k_out=at(call, "q")) == BAD
+        assert run(lib, call, k_out=at(call, "q_out") + 16) == BAD
+    call = "flare_rotary_append_kv"
+    for i in "q k v q_out k_out v_pool".split():
+        assert run(lib, call, k_pool=at(call, i)) == BAD, i
+    assert run(lib, call, v_pool=at(call, "k_pool") + 1024) == BAD
+
+
+def test_alignment_of_small_arrays(lib):
+    for call, names in (("flare_rotary", "position prefix_len token_len parent dev_status"),
+                        ("flare_rotary_append_kv", "position prefix_len page_table dev_status"),
+                        ("flare_tree_logits", NAMES["flare_tree_logits"])):
+        for n in names.split():
+            if n not in ("logits", "out"):
+                assert run(lib, call, **{n: AT + (50 << 32) + 2}) == BAD, (call, n)
+
+
 @pytest.mark.parametrize("change,status", [
     (dict(num_requests=-1), BAD), (dict(block_len=0), BAD), (dict(num_q_heads=0), BAD),
     (dict(num_kv_heads=0), BAD), (dict(act_dtype=2), BAD), (dict(layout=2), BAD),
