@@ -29,7 +29,8 @@ namespace {  // each source file its own kernels
 constexpr int kMaxWarps = 32;  // of a CTA
 constexpr int kMaxCluster = 4;
 constexpr int kSmem = 228 << 10, kSmemMost = 227 << 10;  // of an SM, and of a CTA
-constexpr int kSmemOwn = 2 * 2 * (kMaxWarps + kMaxCluster) * 4 + 1024;  // besides the rows'
+constexpr int kSmemStatic = 2 * 2 * (kMaxWarps + kMaxCluster) * 4;  // RowSum's
+constexpr int kSmemOwn = kSmemStatic + 1024;  // besides the rows', with what the system keeps
 
 __device__ __forceinline__ float exp2f_fast(float x) {
   float y;
@@ -251,8 +252,9 @@ inline void set_ctas(Shape& s, int T, int per_sm, int num_sms) {
 
 inline cudaError_t launch_shape(void (*kernel)(BlockNormParams, Shape), const BlockNormParams& p,
                                 const Shape& s, cudaStream_t stream) {
-  cudaError_t e =
-      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+  // always the same limit: another thread's call may come between this one and the launch
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       kSmemMost - kSmemStatic);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)s.ctas);

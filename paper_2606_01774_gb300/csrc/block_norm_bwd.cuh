@@ -348,7 +348,7 @@ Shape backward_shape(int T_rows, int W, int num_sms) {
   const auto consider = [&](int kind, int units, int vectors, int threads) {
     Shape s = teams_for(T_rows, W, vectors, threads, num_sms);
     s.smem = threads * 16 * units;
-    if (!s.cluster || s.smem + kSmemOwn - 1024 > kSmemMost) return;
+    if (!s.cluster || s.smem + kSmemStatic > kSmemMost) return;
     const int room = kSmem / (s.smem + kSmemOwn);
     const int per_sm = room < 512 / threads ? room : 512 / threads;
     const int used = per_sm * s.team * s.teams, warps = used / 32;

@@ -24,6 +24,7 @@ template <typename T>
 constexpr int kRowsOf = sizeof(T) == 2 ? 3 : 2;
 constexpr int kScan = 8;                 // pieces of the history in flight per thread, four tokens each
 constexpr uint32_t kPrompt = 1u << 31;   // seen in the history ahead of the output; below: count
+constexpr int kSmemMost = 220 << 10;     // of a CTA, besides the static part
 constexpr int kNarrow = 32767;           // the longest history whose counts have 16 bits each
 
 // Index of chunk token i: the eight tokens of a thread's piece, eight threads on, lie in
@@ -524,14 +525,8 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     } else {
       for (int block = tid / 32 % side * 32 * E; block < len; block += side * 32 * E) {
         const int e = block + lane * S;
-        uint32_t live = 0, t = 0;
-    #pragma unroll
-        for (int k = 0; k < E; k += S) {
-          const int x = e + k * 32;
-          if (x >= len) continue;  // V is a whole number of parts
-          live |= ((1u << S) - 1) << k;
-          t |= (touched[x >> 5] >> (x & 31) & ((1u << S) - 1)) << k;
-        }
+        uint32_t live, t;
+        bits_of(e, live, t);
         if (S == E) {
           if (!live) continue;
           live = kFull;
@@ -640,7 +635,7 @@ cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaSt
     narrow = smem_of(chunk, false) > room && p.H <= kNarrow;
     if (smem_of(chunk, narrow) <= room) break;
   }
-  while (smem_of(chunk, narrow) > (220 << 10)) chunk /= 2;
+  while (smem_of(chunk, narrow) > kSmemMost) chunk /= 2;
   chunks = (p.V + chunk - 1) / chunk;
   int parts = 1;
   while (parts * 8 <= p.N && (int64_t)p.R * chunks * parts * 2 <= slots) parts *= 2;
@@ -649,8 +644,9 @@ cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaSt
   const unsigned grid = (unsigned)p.R * parts * chunks;
   const Kernel kernel = kernel_of<T>(p);
   if (smem > (40 << 10)) {  // with the static part, more than a launch has by itself
+    // always the same limit: another thread's call may come between this one and the launch
     const cudaError_t e =
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost);
     if (e != cudaSuccess) return e;
   }
   kernel<<<grid, kThreads, smem, stream>>>(p, chunk, chunks, parts, narrow);

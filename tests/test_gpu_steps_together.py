@@ -4,6 +4,7 @@ streams and from graphs.
 
 Tolerances as in test_gpu_tree.py (the attention's) and steps_helpers.py."""
 import importlib.util
+import threading
 from pathlib import Path
 
 import numpy as np
@@ -186,6 +187,37 @@ def test_stream_argument():
                                        y, h, side))
     side.synchronize()
     assert torch.equal(bits(y), bits(want[0])) and torch.equal(bits(h), bits(want[1]))
+
+
+def test_two_threads_at_once():
+    """Calls of the same kernels at different sizes from two host threads, each on its own stream."""
+    def work(i):
+        log = logits_inputs(30 + i, 3, 2, (90000, 700)[i], "bf16", [2, 1, 2])
+        norm = norm_inputs(32 + i, 300, (7168, 512)[i], gate="silu")
+        return lambda: ([run_logits(log)] + list(run_norm(norm)) + list(run_norm_bwd(norm).values()))
+
+    calls = [work(0), work(1)]
+    want = [f() for f in calls]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(30):
+                    got = calls[i]()
+                    torch.cuda.current_stream().synchronize()
+                    # a request's unused rows are marked in both
+                    wrong.extend(not torch.equal(bits(a), bits(b)) for a, b in zip(got, want[i]))
+        except Exception as e:  # noqa: BLE001
+            wrong.append(e)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not any(wrong), [x for x in wrong if x][:3]
 
 
 def test_from_graphs_that_share_a_workspace():
