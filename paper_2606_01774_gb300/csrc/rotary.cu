@@ -41,7 +41,8 @@ __device__ __forceinline__ float2 cos_sin(uint64_t phase) {
 // Depth of node t in a request's tree; -1 when the tree is wrong.
 __device__ __forceinline__ int node_depth(const int32_t* __restrict__ parent, int n, int t) {
   bool ok = parent[0] == -1;
-  for (int i = 1; i < n; ++i) ok = ok && parent[i] >= 0 && parent[i] < i;
+#pragma unroll 8
+  for (int i = 1; i < n; ++i) ok &= (uint32_t)parent[i] < (uint32_t)i;
   if (!ok) return -1;
   int depth = 0;
   for (int i = t; i > 0; i = parent[i]) ++depth;

@@ -47,6 +47,31 @@ def test_each_part_may_be_missing(without, dtype):
         assert torch.equal(bits(out[0]), bits(s.logits[0]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("R,N,V,nodes", [
+    (64, 1, 128000, None), (3, 2, 50264, [2, 1, 2]), (3, 2, 1004, [2, 2, 0]),
+    (60, 3, 120004, [3, 0, 1, 2] + [0] * 56), (5, 7, 30004, None), (150, 1, 66000, None)])
+def test_few_rows_and_large_chunks(R, N, V, nodes, dtype):
+    check_all(logits_inputs(R + N + V, R, N, V, dtype, nodes))
+
+
+@pytest.mark.parametrize("H", [32766, 32767, 32768, 70000])
+@pytest.mark.parametrize("x", [6, 7])
+def test_counts_up_to_their_last_bit(H, x):
+    """A token all through a history that is as long as counts of 16 bits allow, and longer, over a
+    vocabulary that makes them worth while; the next token in the prompt alone."""
+    R, V = 150, 66000
+    s = logits_inputs(70, R, 1, V, "f32", [1] * R, history=1, bias=0, masked=None)
+    s.text = [[x ^ 1, x ^ 1] + [x] * (H - 2)] + [[x]] * (R - 1)
+    s.start = [2] + [0] * (R - 1)
+    s.history = torch.full((R, H), FAR, dtype=torch.int32, device="cuda")
+    s.history[:, 0] = x
+    s.history[0] = whole(s.text[0])
+    s.history_len, s.output_start = whole([H] + [1] * (R - 1)), whole(s.start)
+    s.desc.max_history = H
+    check_all(s)
+
+
 def test_no_node_lengths_no_starts():
     s = logits_inputs(51, 3, 2, 700, "f32", [2, 2, 2], tree=False)
     s.node_len = s.output_start = None
