@@ -18,13 +18,14 @@ namespace flare {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kCtas = 3;                 // of an SM
 template <typename T>
 constexpr int kRowsOf = sizeof(T) == 2 ? 3 : 2;
 constexpr int kScan = 8;                 // pieces of the history in flight per thread, four tokens each
 constexpr uint32_t kPrompt = 1u << 31;   // seen in the history ahead of the output; below: count
 constexpr int kSmemMost = 220 << 10;     // of a CTA, besides the static part
+constexpr int kAhead = 32 << 10;         // bytes of the rows that a CTA asks into L2
 constexpr int kNarrow = 32767;           // the longest history whose counts have 16 bits each
 
 // Index of chunk token i: the eight tokens of a thread's piece, eight threads on, lie in
@@ -96,19 +97,18 @@ struct Tables {
 
   __device__ __forceinline__ float bias_of(int e) const {
     const uint32_t w = biased[e >> 5], bit = 1u << (e & 31);
-    return w & bit ? bias[before[e >> 5] + __popc(w & (bit - 1))] : 0.f;
+    return w & bit ? bias[before[e >> 5] + __popc(w & (bit - 1))] : -0.f;
   }
 
-  // Of token e of the chunk.
+  // Of token e of the chunk, but for its bias.
   __device__ __forceinline__ void one(int e, float& up, float& down, float& add) const {
     const uint32_t w = counts[e], c = w & ~kPrompt;
     up = w ? rep_inv : 1.f;
     down = w ? rep : 1.f;
     add = c ? -freq * (float)c - pres : -0.f;
-    if (biased[e >> 5] >> (e & 31) & 1) add += bias_of(e);
   }
-  // Of a piece whose element k is token e + k / S * 32 S + k % S.
-  template <int E, int S>
+  // Of a piece whose element k is token e + k / S * 32 S + k % S; GRID: e is a multiple of S.
+  template <int E, int S, bool GRID>
   __device__ __forceinline__ void piece(int e, uint32_t touched, Change<E>& ch) const {
 #pragma unroll
     for (int k = 0; k < E; ++k) {
@@ -116,6 +116,18 @@ struct Tables {
       ch.add[k] = -0.f;
       if (touched >> k & 1)
         one(e + k / S * 32 * S + k % S, ch.up[k], ch.down[k], ch.add[k]);
+    }
+    uint32_t some = 0;
+#pragma unroll
+    for (int k = 0; k < E; k += S) {
+      const int x = e + k * 32;
+      const uint32_t bits = GRID ? biased[x >> 5] >> (x & 31) : bits_at(biased, x);
+      some |= (bits & ((1u << S) - 1)) << k;
+    }
+    if (some & touched) {
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (some & touched & 1u << k) ch.add[k] += bias_of(e + k / S * 32 * S + k % S);
     }
   }
 };
@@ -168,37 +180,44 @@ template <typename T, int W, int ROWS, bool MASK, bool IN_PLACE>
 struct Batch {
   static constexpr int E = Piece<T>::N, S = W / (int)sizeof(T), K = E / S;
   uint4 raw[ROWS];
-  uint32_t allowed[ROWS];
+  uint32_t word[ROWS][MASK ? K : 1];  // the mask's bytes, untouched while they are on their way
 
+  // Which of row u's tokens are allowed, `bit` the first one's place in its byte.
+  __device__ __forceinline__ uint32_t allowed(int u, int bit, uint32_t live) const {
+    if (!MASK) return live;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) bits |= (word[u][k] >> bit & ((1u << S) - 1)) << (k * S);
+    return bits;
+  }
   // src: the lane's first element, bits: the mask's byte with it, both of the first row.
   __device__ __forceinline__ void load(const T* src, size_t V, const uint8_t* bits, int bit,
                                        size_t mask_bytes, uint32_t live, bool kept) {
+    if (MASK) {
 #pragma unroll
-    for (int u = 0; u < ROWS; ++u) {
-      allowed[u] = live;
-      if (MASK) {
-        allowed[u] = 0;
+      for (int u = 0; u < ROWS; ++u)
 #pragma unroll
         for (int k = 0; k < K; ++k)
-          if (live >> (k * S) & 1)
-            allowed[u] |= (bits[u * mask_bytes + k * 4 * S] >> bit & ((1u << S) - 1)) << (k * S);
-      }
+          word[u][k] = live >> (k * S) & 1 ? bits[u * mask_bytes + k * 4 * S] : 0;
     }
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-      if (IN_PLACE && kept && allowed[u] == live) continue;  // what stays as it is, stays
+      // what stays as it is, stays
+      if (IN_PLACE && kept && (!MASK || allowed(u, bit, live) == live)) continue;
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (live >> (k * S) & 1) get_part<W>(raw[u], k, src + u * V + k * 32 * S);
     }
   }
-  __device__ __forceinline__ void store(T* dst, size_t V, const uint4* keep_of, uint32_t touched,
-                                        const Change<E>& ch, uint32_t live, bool kept) {
+  __device__ __forceinline__ void store(T* dst, size_t V, int bit, const uint4* keep_of,
+                                        uint32_t touched, const Change<E>& ch, uint32_t live,
+                                        bool kept) {
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
-      if (IN_PLACE && kept && allowed[u] == live) continue;
-      if (touched & allowed[u]) raw[u] = changed<T>(raw[u], ch);
-      if (MASK) raw[u] = ruled_out<T>(raw[u], keep_of[allowed[u]]);
+      const uint32_t ok = allowed(u, bit, live);
+      if (IN_PLACE && kept && ok == live) continue;
+      if (touched & ok) raw[u] = changed<T>(raw[u], ch);
+      if (MASK) raw[u] = ruled_out<T>(raw[u], keep_of[ok]);
 #pragma unroll
       for (int k = 0; k < K; ++k)
         if (live >> (k * S) & 1) put_part<W>(raw[u], k, dst + u * V + k * 32 * S);
@@ -232,7 +251,9 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   __shared__ uint64_t path[kMaxNodes];
   __shared__ int tok[kMaxNodes];
   __shared__ uint4 keep_of[1 << E];  // keep_words
-  __shared__ int tree_bad;
+  __shared__ int tree_bad, owns;
+  __shared__ uint64_t own_nodes[kMaxNodes];  // of the tree's own tokens in the chunk: who has them
+  __shared__ int own_token[kMaxNodes];       // and which they are, `owns` of them
 
   const int tid = threadIdx.x, lane = tid & 31;
   const int team = blockIdx.x / chunks;
@@ -280,6 +301,17 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     }
   };
   take(4 * tid);
+  // and so are the first biases, by the warp that takes them
+  const int32_t* bias_token = p.bias_token + (size_t)r * p.max_bias;
+  const float* bias_value = p.bias_value + (size_t)r * p.max_bias;
+  int pick[2] = {};
+  float pick_value[2] = {};
+  if (p.bias_token && tid >= kThreads - 32) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      if (lane + 32 * k < p.max_bias)
+        pick[k] = bias_token[lane + 32 * k], pick_value[k] = bias_value[lane + 32 * k];
+  }
   for (int i = tid; i < (count_words + 4 * bit_words + 3) / 4; i += kThreads)  // room for all of it
     reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
   if (tid < 1 << E) keep_of[tid] = keep_words<T>(tid);
@@ -302,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       ok = ok && (uint32_t)x0 < (uint32_t)p.V && (uint32_t)x1 < (uint32_t)p.V;
     }
     ok = __all_sync(0xffffffffu, ok);
-    if (lane == 0) tree_bad = !ok;
+    if (lane == 0) tree_bad = !ok, owns = 0;
   }
   __syncthreads();
   if (tree_bad) {
@@ -310,9 +342,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     return;
   }
   if (!IN_PLACE || MASK) {
-    // the rows, on their way to L2 while the history is counted (ahead of the loads above they would
-    // only hold those up)
-    for (int i = row_first + tid; i < row_last; i += kThreads) {
+    // the first rows, on their way to L2 while the history is counted (ahead of the loads above they
+    // would only hold those up)
+    const int first_rows = min(row_last - row_first, kAhead / (len * (int)sizeof(T)));
+    for (int i = row_first + tid; i < row_first + first_rows; i += kThreads) {
       const uintptr_t row = (uintptr_t)(logits + (size_t)i * p.V), from = row & ~(uintptr_t)15;
       const uint32_t bytes = (uint32_t)(row + len * sizeof(T) - from) & ~15u;
       if (bytes)
@@ -340,16 +373,24 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       if (i + 3 < H) count(i + 3, text[j].w);
     }
   }
-  if (tree && tid < n && tok[tid] >= c0 && tok[tid] < c1)
-    atomicOr(&held[(tok[tid] - c0) >> 5], 1u << ((tok[tid] - c0) & 31));
+  if (tree && tid < n && tok[tid] >= c0 && tok[tid] < c1) {
+    const int x = tok[tid], e = x - c0;
+    uint64_t same = 0;
+#pragma unroll 8
+    for (int k = 0; k < n; ++k) same |= (uint64_t)(tok[k] == x) << k;
+    if (tid == __ffsll(same) - 1) {  // once
+      const int i = atomicAdd(&owns, 1);
+      own_nodes[i] = same;
+      own_token[i] = e;
+      atomicOr(&held[e >> 5], 1u << (e & 31));
+    }
+  }
   if (tid >= kThreads - 32) {
     // biases by one warp: which tokens have one, and then the list in its order, a token's repetitions
     // one after another
-    const int32_t* bias_token = p.bias_token + (size_t)r * p.max_bias;
-    const float* bias_value = p.bias_value + (size_t)r * p.max_bias;
     bool any = false;
     for (int i = lane; i < n_bias; i += 32) {
-      const int x = bias_token[i], e = x - c0;
+      const int x = i < 32 ? pick[0] : i < 64 ? pick[1] : bias_token[i], e = x - c0;
       wrong |= (uint32_t)x >= (uint32_t)p.V;
       if ((uint32_t)e >= (uint32_t)len) continue;
       any = true;
@@ -371,9 +412,10 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       for (uint32_t i = lane; i < total; i += 32) bias[i] = 0.f;
       __syncwarp();
       for (int i0 = 0; i0 < n_bias; i0 += 32) {
-        const int e = i0 + lane < n_bias ? bias_token[i0 + lane] - c0 : -1;
+        const int i = i0 + lane;
+        const int e = i < n_bias ? (i < 32 ? pick[0] : i < 64 ? pick[1] : bias_token[i]) - c0 : -1;
         const bool mine = (uint32_t)e < (uint32_t)len;
-        const float b = mine ? bias_value[i0 + lane] : 0.f;
+        const float b = !mine ? 0.f : i < 32 ? pick_value[0] : i < 64 ? pick_value[1] : bias_value[i];
         const uint32_t w = mine ? biased[e >> 5] : 0, bit = 1u << (e & 31);
         float* const sum = bias + (mine ? before[e >> 5] + __popc(w & (bit - 1)) : 0);
         float value = mine ? *sum : 0.f;
@@ -401,19 +443,40 @@ __global__ void __launch_bounds__(kThreads, kCtas)
   const Tables tables{rep, 1.f / rep, pres, freq, counts, biased, before, bias};
   const int mask_words = (p.V + 31) / 32;
   const uint32_t* mask = p.mask ? p.mask + (size_t)r * p.N * mask_words : nullptr;
-  // Warps side by side take a row's pieces, kRows rows at a time; where a row has pieces for
-  // fewer warps, several groups of rows at once.
-  int side = kThreads / 32;  // warps of a row
-  while (side > 1 && side / 2 * 32 * E >= len) side /= 2;
-  const int group = tid / 32 / side, step = kThreads / 32 / side * kRows;
+  // Warps side by side take the chunk's blocks of 32 pieces, kRows rows at a time: all warps while
+  // there are blocks for all.  For the rest as many warps side by side as make the fewest steps,
+  // the others taking other rows.
+  const auto each_block = [&](const auto& rows_of) {
+    const int blocks = (len + 32 * E - 1) / (32 * E), full = blocks / kWarps * kWarps;
+    int from = 0, side = kWarps;
+    while (from < blocks) {
+      const int to = from < full ? full : blocks;
+      if (from == full) {
+        int fewest = INT32_MAX;
+#pragma unroll
+        for (int s = kWarps; s > 0; s /= 2) {
+          const int step = kWarps / s * kRows;
+          const int steps = ((to - from + s - 1) / s) * ((row_last - row_first + step - 1) / step);
+          if (steps < fewest) side = s, fewest = steps;
+        }
+      }
+      const int group = tid / 32 / side;
+      for (int block = from + tid / 32 % side; block < to; block += side)
+        rows_of(block * 32 * E, row_first + group * kRows, kWarps / side * kRows);
+      from = to;
+    }
+  };
   const size_t V = p.V, mask_bytes = (size_t)mask_words * 4;
   if constexpr (W == 0) {
     const bool together = ((uintptr_t)logits & 15) == ((uintptr_t)out & 15);
-    const auto allowed_at = [&](int row, int e) -> uint32_t {
-      if (!MASK) return kFull;
+    const auto words_at = [&](int row, int e, uint32_t& first, uint32_t& next) {
+      if (!MASK) return;
       const uint32_t* w = mask + (size_t)row * mask_words + ((c0 + e) >> 5);
-      const uint32_t next = ((c0 + e) >> 5) + 1 < mask_words ? w[1] : 0;
-      return __funnelshift_r(w[0], next, (c0 + e) & 31) & kFull;
+      first = w[0];
+      next = ((c0 + e) >> 5) + 1 < mask_words ? w[1] : 0;
+    };
+    const auto allowed_of = [&](int e, uint32_t first, uint32_t next) -> uint32_t {
+      return MASK ? __funnelshift_r(first, next, (c0 + e) & 31) & kFull : kFull;
     };
     // every row its own grid: the pieces start at its first 16-byte boundary
     const auto ahead = [&](int i) {
@@ -422,16 +485,18 @@ __global__ void __launch_bounds__(kThreads, kCtas)
     };
     struct {
       uint4 raw[kRows];
-      uint32_t allowed[kRows], touched[kRows];
+      uint32_t word[2][kRows], touched[kRows];  // of the mask, as they came
     } one, two;
     const auto load = [&](auto& batch, int i, int j) {
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         const int e = i + u < row_last ? ahead(i + u) + j * E : len;
         const bool live = e + E <= len;
-        batch.allowed[u] = live ? allowed_at(i + u, e) : 0;
         batch.touched[u] = live ? bits_at(touched, e) & kFull : 0;
-        if (live && !(IN_PLACE && batch.allowed[u] == kFull && !batch.touched[u]))
+        if (!live) continue;
+        uint32_t &w0 = batch.word[0][u], &w1 = batch.word[1][u];
+        words_at(i + u, e, w0, w1);
+        if (!(IN_PLACE && !batch.touched[u] && allowed_of(e, w0, w1) == kFull))
           batch.raw[u] = *reinterpret_cast<const uint4*>(logits + (size_t)(i + u) * p.V + e);
       }
     };
@@ -439,38 +504,45 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         const int e = i + u < row_last ? ahead(i + u) + j * E : len;
-        const uint32_t m = batch.allowed[u], t = batch.touched[u];
-        if (e + E > len || (IN_PLACE && m == kFull && !t)) continue;
+        if (e + E > len) continue;
+        const uint32_t m = allowed_of(e, batch.word[0][u], batch.word[1][u]), t = batch.touched[u];
+        if (IN_PLACE && m == kFull && !t) continue;
         if (t & m) {
           Change<E> ch;
-          tables.piece<E, E>(e, t & m, ch);
+          tables.piece<E, E, false>(e, t & m, ch);
           batch.raw[u] = changed<T>(batch.raw[u], ch);
         }
         if (MASK) batch.raw[u] = ruled_out<T>(batch.raw[u], keep_of[m]);
         *reinterpret_cast<uint4*>(out + (size_t)(i + u) * p.V + e) = batch.raw[u];
       }
     };
-    for (int j = tid % (32 * side); together && j * E + E <= len; j += 32 * side) {
-      int i = row_first + group * kRows;
-      if (i < row_last) load(one, i, j);
-      while (i < row_last) {
-        if (i + step < row_last) load(two, i + step, j);
-        store(one, i, j);
-        i += step;
-        if (i >= row_last) break;
-        if (i + step < row_last) load(one, i + step, j);
-        store(two, i, j);
-        i += step;
-      }
+    if (together) {
+      each_block([&](int block, int i, int step) {
+        const int j = block / E + lane;
+        if (j * E + E > len) return;
+        if (i < row_last) load(one, i, j);
+        while (i < row_last) {
+          if (i + step < row_last) load(two, i + step, j);
+          store(one, i, j);
+          i += step;
+          if (i >= row_last) break;
+          if (i + step < row_last) load(one, i + step, j);
+          store(two, i, j);
+          i += step;
+        }
+      });
     }
     const auto element = [&](int i, int e) {
       const T x_in = logits[(size_t)i * p.V + e];
-      const bool ok = allowed_at(i, e) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
+      uint32_t w0, w1;
+      words_at(i, e, w0, w1);
+      const bool ok = allowed_of(e, w0, w1) & 1, changes = touched[e >> 5] >> (e & 31) & 1;
       if (IN_PLACE && ok && !changes) return;
       float x = ok ? to_f32(x_in) : minus_inf();
       if (ok && changes) {
         float up, down, add;
         tables.one(e, up, down, add);
+        add += tables.bias_of(e);
         x = fmaf(x, x > 0.f ? up : down, add);
       }
       out[(size_t)i * p.V + e] = from_f32<T>(x);
@@ -517,32 +589,31 @@ __global__ void __launch_bounds__(kThreads, kCtas)
 #pragma unroll
           for (int u = 0; u < kBlocks; ++u) {
             Change<E> ch;
-            if (t[u]) tables.piece<E, S>(block + u * stride + lane * S, t[u], ch);
-            batch[u].store(dst + u * stride, V, keep_of, t[u], ch, live[u], !t[u]);
+            if (t[u]) tables.piece<E, S, true>(block + u * stride + lane * S, t[u], ch);
+            batch[u].store(dst + u * stride, V, lane * S & 7, keep_of, t[u], ch, live[u], !t[u]);
           }
         }
       }
     } else {
-      for (int block = tid / 32 % side * 32 * E; block < len; block += side * 32 * E) {
+      each_block([&](int block, int i, int step) {
         const int e = block + lane * S;
         uint32_t live, t;
         bits_of(e, live, t);
         if (S == E) {
-          if (!live) continue;
+          if (!live) return;
           live = kFull;
         }
         Change<E> ch;
-        if (t) tables.piece<E, S>(e, t, ch);
+        if (t) tables.piece<E, S, true>(e, t, ch);
         const bool kept = !t;
         const uint8_t* bits = reinterpret_cast<const uint8_t*>(mask) + (c0 + e) / 8;
         const auto load = [&](auto& batch, int i) {
           batch.load(logits + i * V + e, V, bits + i * mask_bytes, e & 7, mask_bytes, live, kept);
         };
         const auto store = [&](auto& batch, int i) {
-          batch.store(out + i * V + e, V, keep_of, t, ch, live, kept);
+          batch.store(out + i * V + e, V, e & 7, keep_of, t, ch, live, kept);
         };
         // the next rows are on their way while these are worked on
-        int i = row_first + group * kRows;
         Batch<T, W, kRows, MASK, IN_PLACE> one, two;
         if (i + kRows <= row_last) load(one, i);
         while (i + kRows <= row_last) {
@@ -559,28 +630,23 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           load(rest, i);
           store(rest, i);
         }
-      }
+      });
     }
   }
   if (!tree) return;
   __syncthreads();
 
   // the tree's tokens: each row by its own path's count
-  const int rows = row_last - row_first;
-  for (int j = tid; j < rows * n; j += kThreads) {
-    const int i = row_first + j / n, m = j % n, x = tok[m];
-    if (x < c0 || x >= c1) continue;
-    uint64_t same = 0;
-    for (int k = 0; k < n; ++k) same |= (uint64_t)(tok[k] == x) << k;
-    if (m != __ffsll(same) - 1) continue;  // once
-    float y = to_f32(logits[(size_t)i * p.V + x - c0]);
-    if (MASK && !(mask[(size_t)i * mask_words + (x >> 5)] >> (x & 31) & 1)) continue;
-    const uint32_t base = counts[x - c0];
-    const int mine = __popcll(same & path[i]);
+  for (int j = tid; j < (row_last - row_first) * owns; j += kThreads) {
+    const int i = row_first + j / owns, m = j % owns, e = own_token[m];
+    float y = to_f32(logits[i * V + e]);
+    if (MASK && !(mask[(size_t)i * mask_words + ((c0 + e) >> 5)] >> ((c0 + e) & 31) & 1)) continue;
+    const uint32_t base = counts[e];
+    const int mine = __popcll(own_nodes[m] & path[i]);
     const uint32_t c = (base & ~kPrompt) + mine;
     if (base != 0 || mine) y *= y > 0.f ? tables.rep_inv : rep;
     if (c) y -= freq * (float)c + pres;
-    out[(size_t)i * p.V + x - c0] = from_f32<T>(y + tables.bias_of(x - c0));
+    out[i * V + e] = from_f32<T>(y + tables.bias_of(e));
   }
 }
 
