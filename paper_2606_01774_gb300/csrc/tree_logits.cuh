@@ -1,12 +1,21 @@
-// Penalties for repeated tokens, biases and token masks on the logits of a tree's
-// nodes.
+// Penalties for repeated tokens, biases and token masks on the logits of a tree's nodes.
 //
-// A CTA takes a chunk of the vocabulary and a share of a request's nodes.  What a
-// token costs does not depend on the node, but for the few tokens that the tree
-// itself holds: so the CTA counts the history's tokens of its chunk once, in
-// shared memory, turns counts and biases into one summand per token, and streams
-// its rows through.  The tree's own tokens are put right at the end, each by its
-// count on every node's path.  Bound by bytes: logits in and out once.
+//   y = l (l > 0 ? up : down) + add      up, down: 1 / repetition and repetition where the token was
+//                                        seen, else 1; add: -frequency c - presence [c > 0] + bias
+//
+// A CTA takes a chunk of the vocabulary and a share of a request's nodes.  What a token gets does
+// not depend on the node, but for the few tokens that the tree itself holds: so the CTA counts
+// the history's tokens of its chunk once, in shared memory, and streams its rows through.  A lane
+// has the same tokens in every row and finds out once what they get.  Tokens that are neither
+// seen nor biased (a bit each) cost nothing but their copy, in place not even that.  The tree's
+// own tokens come last, each by its count on every node's path.
+//
+// Bound by bytes once there are many rows, logits in and out (64 requests x 64 nodes over 32000
+// bf16 tokens: 102 us, 5.3 TB/s); with few, by the steps before them: lengths, tree, history and
+// biases are round trips to memory one after another, some 3 us, and a history of 8192 tokens is
+// counted in 3 us more, once per chunk (64 x 16 nodes under a mask: 33 us, 4.1 TB/s; 64 x 1 over
+// 128000: 23 us).  One wave of three CTAs an SM keeps that to once; two took 1.3 to 1.5 times as
+// long.
 #pragma once
 
 #include "common.cuh"
@@ -21,7 +30,7 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kCtas = 3;                 // of an SM
 template <typename T>
-constexpr int kRowsOf = sizeof(T) == 2 ? 3 : 2;
+constexpr int kRowsOf = sizeof(T) == 2 ? 3 : 2;  // more take registers that a third CTA needs
 constexpr int kScan = 8;                 // pieces of the history in flight per thread, four tokens each
 constexpr uint32_t kPrompt = 1u << 31;   // seen in the history ahead of the output; below: count
 constexpr int kSmemMost = 220 << 10;     // of a CTA, besides the static part
@@ -67,11 +76,12 @@ struct Counts {
   uint32_t* word;
   bool narrow;
 
-  __device__ __forceinline__ uint32_t operator[](int e) const {
-    if (!narrow) return word[at(e)];
-    const uint32_t half = word[at(e >> 1)] >> (e & 1) * 16;
-    return (half & 0x7fffu) | (half & 0x8000u) << 16;
+  __device__ __forceinline__ uint32_t full(int e) const { return word[at(e)]; }
+  __device__ __forceinline__ uint32_t half(int e) const {
+    const uint32_t w = word[at(e >> 1)] >> (e & 1) * 16;
+    return (w & 0x7fffu) | (w & 0x8000u) << 16;
   }
+  __device__ __forceinline__ uint32_t operator[](int e) const { return narrow ? half(e) : full(e); }
   __device__ __forceinline__ void add(int e, bool output) const {
     uint32_t* w = &word[at(narrow ? e >> 1 : e)];
     const int shift = narrow ? (e & 1) * 16 : 0;
@@ -100,30 +110,36 @@ struct Tables {
     return w & bit ? bias[before[e >> 5] + __popc(w & (bit - 1))] : -0.f;
   }
 
-  // Of token e of the chunk, but for its bias.
-  __device__ __forceinline__ void one(int e, float& up, float& down, float& add) const {
-    const uint32_t w = counts[e], c = w & ~kPrompt;
+  // What a count does to its token.
+  __device__ __forceinline__ void one(uint32_t w, float& up, float& down, float& add) const {
+    const uint32_t c = w & ~kPrompt;
     up = w ? rep_inv : 1.f;
     down = w ? rep : 1.f;
     add = c ? -freq * (float)c - pres : -0.f;
   }
-  // Of a piece whose element k is token e + k / S * 32 S + k % S; GRID: e is a multiple of S.
+  // Of a piece whose element k is token e + k / S * 32 S + k % S (GRID: e a multiple of S).  All
+  // counts are asked for before the first is used: a warp whose piece is touched in every row
+  // holds up its CTA.
   template <int E, int S, bool GRID>
   __device__ __forceinline__ void piece(int e, uint32_t touched, Change<E>& ch) const {
+    uint32_t w[E], some = 0;
+    if (counts.narrow) {
 #pragma unroll
-    for (int k = 0; k < E; ++k) {
-      ch.up[k] = ch.down[k] = 1.f;
-      ch.add[k] = -0.f;
-      if (touched >> k & 1)
-        one(e + k / S * 32 * S + k % S, ch.up[k], ch.down[k], ch.add[k]);
+      for (int k = 0; k < E; ++k)
+        w[k] = touched >> k & 1 ? counts.half(e + k / S * 32 * S + k % S) : 0;
+    } else {
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        w[k] = touched >> k & 1 ? counts.full(e + k / S * 32 * S + k % S) : 0;
     }
-    uint32_t some = 0;
 #pragma unroll
     for (int k = 0; k < E; k += S) {
       const int x = e + k * 32;
       const uint32_t bits = GRID ? biased[x >> 5] >> (x & 31) : bits_at(biased, x);
       some |= (bits & ((1u << S) - 1)) << k;
     }
+#pragma unroll
+    for (int k = 0; k < E; ++k) one(w[k], ch.up[k], ch.down[k], ch.add[k]);
     if (some & touched) {
 #pragma unroll
       for (int k = 0; k < E; ++k)
@@ -228,15 +244,19 @@ struct Batch {
 }  // namespace
 
 // W: bytes on whose boundaries all rows start, up to 16.  A lane's piece is 16 bytes in parts of W, a
-// warp's parts next to each other: the same tokens in every row, whatever V is.  W = 0, for parts
-// that would be small: pieces start at each row's own 16-byte boundaries.  FEW: rows too few to keep
-// a batch under way.
+// warp's parts next to each other: the same tokens in every row, whatever V is.  (fp32 parts of 4
+// against W = 0, 9 trees of 13 over 50257 tokens: 11 us, 18.)  W = 0, for bf16 rows on 2 or 4
+// bytes: pieces start at each row's own 16-byte boundaries and look up their tokens in each (parts
+// of 2, 4 trees of 26 over 81625: 34 us, 25 at the time and now 14).  FEW: rows too few to keep a
+// batch under way, so several blocks of a row are (64 x 1 over 128000: 24 us, 42 without).
 template <typename T, int W, bool MASK, bool IN_PLACE, bool FEW>
 __global__ void __launch_bounds__(kThreads, kCtas)
     tree_logits_kernel(const __grid_constant__ TreeLogitsParams p, int chunk, int chunks,
                        int row_parts, bool narrow) {
   constexpr int E = Piece<T>::N;               // elements of a piece
-  constexpr int kRows = kRowsOf<T>;            // in flight per thread, twice
+  // In flight per thread, twice.  W = 0 has to remember more with each (three: 44 us, two: 35, for 16
+  // trees of 36 nodes over 52711 tokens under a mask).
+  constexpr int kRows = W ? kRowsOf<T> : 2;
   constexpr uint32_t kFull = (1u << E) - 1;
   constexpr int S = W ? W / (int)sizeof(T) : E;  // of a part
   extern __shared__ __align__(16) char smem[];
@@ -473,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       if (!MASK) return;
       const uint32_t* w = mask + (size_t)row * mask_words + ((c0 + e) >> 5);
       first = w[0];
-      next = ((c0 + e) >> 5) + 1 < mask_words ? w[1] : 0;
+      next = w[((c0 + e) >> 5) + 1 < mask_words];  // past the last: the last again, not used
     };
     const auto allowed_of = [&](int e, uint32_t first, uint32_t next) -> uint32_t {
       return MASK ? __funnelshift_r(first, next, (c0 + e) & 31) & kFull : kFull;
@@ -483,27 +503,37 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       const uintptr_t first = (uintptr_t)(logits + (size_t)i * p.V) & 15;
       return min(len, (int)((16 - first) & 15) / (int)sizeof(T));
     };
+    // A warp takes an equal share of all rows' blocks one after another, kRows of them at a time, so
+    // that blocks with many tokens to change are spread over the warps.
+    const int blocks = (len + 32 * E - 1) / (32 * E), items = (row_last - row_first) * blocks;
+    const int share = (items + kWarps - 1) / kWarps;
+    int item = tid / 32 * share, row = row_first + item / blocks, block = item % blocks;
+    const int last = together ? min(item + share, items) : 0;
     struct {
       uint4 raw[kRows];
       uint32_t word[2][kRows], touched[kRows];  // of the mask, as they came
+      int row[kRows], e[kRows];
     } one, two;
-    const auto load = [&](auto& batch, int i, int j) {
+    const auto load = [&](auto& batch) {  // the next items
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        const int e = i + u < row_last ? ahead(i + u) + j * E : len;
-        const bool live = e + E <= len;
-        batch.touched[u] = live ? bits_at(touched, e) & kFull : 0;
-        if (!live) continue;
+        const int i = row, e = item < last ? ahead(i) + (block * 32 + lane) * E : len;
+        if (++block == blocks) block = 0, ++row;
+        ++item;
+        batch.row[u] = i;
+        batch.e[u] = e;
+        if (e + E > len) continue;
+        batch.touched[u] = bits_at(touched, e) & kFull;
         uint32_t &w0 = batch.word[0][u], &w1 = batch.word[1][u];
-        words_at(i + u, e, w0, w1);
+        words_at(i, e, w0, w1);
         if (!(IN_PLACE && !batch.touched[u] && allowed_of(e, w0, w1) == kFull))
-          batch.raw[u] = *reinterpret_cast<const uint4*>(logits + (size_t)(i + u) * p.V + e);
+          batch.raw[u] = *reinterpret_cast<const uint4*>(logits + i * V + e);
       }
     };
-    const auto store = [&](auto& batch, int i, int j) {
+    const auto store = [&](auto& batch) {
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
-        const int e = i + u < row_last ? ahead(i + u) + j * E : len;
+        const int i = batch.row[u], e = batch.e[u];
         if (e + E > len) continue;
         const uint32_t m = allowed_of(e, batch.word[0][u], batch.word[1][u]), t = batch.touched[u];
         if (IN_PLACE && m == kFull && !t) continue;
@@ -513,24 +543,15 @@ __global__ void __launch_bounds__(kThreads, kCtas)
           batch.raw[u] = changed<T>(batch.raw[u], ch);
         }
         if (MASK) batch.raw[u] = ruled_out<T>(batch.raw[u], keep_of[m]);
-        *reinterpret_cast<uint4*>(out + (size_t)(i + u) * p.V + e) = batch.raw[u];
+        *reinterpret_cast<uint4*>(out + i * V + e) = batch.raw[u];
       }
     };
-    if (together) {
-      each_block([&](int block, int i, int step) {
-        const int j = block / E + lane;
-        if (j * E + E > len) return;
-        if (i < row_last) load(one, i, j);
-        while (i < row_last) {
-          if (i + step < row_last) load(two, i + step, j);
-          store(one, i, j);
-          i += step;
-          if (i >= row_last) break;
-          if (i + step < row_last) load(one, i + step, j);
-          store(two, i, j);
-          i += step;
-        }
-      });
+    for (load(one); item - kRows < last; ) {
+      load(two);
+      store(one);
+      if (item - kRows >= last) break;
+      load(one);
+      store(two);
     }
     const auto element = [&](int i, int e) {
       const T x_in = logits[(size_t)i * p.V + e];
@@ -541,7 +562,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       float x = ok ? to_f32(x_in) : minus_inf();
       if (ok && changes) {
         float up, down, add;
-        tables.one(e, up, down, add);
+        tables.one(counts[e], up, down, add);
         add += tables.bias_of(e);
         x = fmaf(x, x > 0.f ? up : down, add);
       }
@@ -682,7 +703,8 @@ Kernel kernel_of(const TreeLogitsParams& p) {
 template <typename T>
 cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaStream_t stream) {
   // One wave of CTAs, if chunks of 512 to 32768 tokens allow it: a history is counted once per chunk.
-  // Counts of 16 bits only where those of 32 need more memory than the wave leaves.
+  // Counts of 16 bits only where those of 32 need more memory than the wave leaves (64 x 1 over 128000:
+  // 24 us with three CTAs an SM, 30 with two): they cost a shift each.
   const auto smem_of = [&](int chunk, bool narrow) {
     const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
     return (at(narrow ? chunk / 2 : chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
