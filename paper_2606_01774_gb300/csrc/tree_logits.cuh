@@ -709,7 +709,7 @@ cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaSt
     const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
     return (at(narrow ? chunk / 2 : chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
   };
-  constexpr int kOwn = 6144;  // static shared memory and what the system keeps
+  constexpr int kOwn = 7168;  // static shared memory and what the system keeps
   int chunks = 0, chunk = 0, slots = 0;
   bool narrow = false;
   for (int per_sm = kCtas; per_sm > 0; --per_sm) {
