@@ -5,7 +5,11 @@
 // it finds their requests, positions and cache rows, then the cosines and sines
 // of its rows once for all heads, then streams the heads through in 32-byte
 // units (the two 16-byte pieces that rotate together).  Bound by bytes: every
-// element is read and written once.
+// element is read and written once (32768 rows of 9 KiB in bf16: 99 us, 6.1 TB/s, a
+// copy's rate being 6.8; prompts appended to pages of 16 with their queries: 61 us,
+// 5.8 TB/s).  A few tokens take 3 us, most of it the round trips to memory from
+// lengths to positions to table.  Small CTAs, six an SM, so that some stream while
+// others work out angles (CTAs of 64, 256 or 512 threads: 4 to 15% slower).
 //
 // Angles: the table holds f_j as fractions of a turn in 64-bit fixed point, so
 // m f_j modulo a turn is one wrapping integer product, exact in the table's
