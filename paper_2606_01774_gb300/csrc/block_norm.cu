@@ -90,7 +90,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 4 + s.stages * s.arrays * Slots<T>::M; ++i)
       weights.at[i * threads] = make_uint4(0, 0, 0, 0);
   }
-  weights.fill<T>(p, c, mine);
   if (s.cluster > 1) cluster_sync();  // every CTA runs before another writes to its memory
   const int64_t step = (int64_t)(gridDim.x / s.cluster) * blockDim.y;
   const int64_t first = (int64_t)(blockIdx.x / s.cluster) * blockDim.y + threadIdx.y;
@@ -104,6 +103,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     cp_async_commit();
   };
   for (int i = 0; i < s.stages - 1; ++i) fetch(first + i * step, i);
+  weights.fill<T>(p, c, mine);  // behind the first rows
   int at = 0;
   for (int64_t row = first; row < p.T; row += step) {
     const int last = at == 0 ? s.stages - 1 : at - 1;

@@ -104,18 +104,6 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
 #pragma unroll 1
     for (int i = 0; i < O::kUnits; ++i) units[i * THREADS] = make_uint4(0, 0, 0, 0);
   }
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    for (int i = 0; i < 2; ++i) {
-      if (!mine[j][i % H]) continue;
-      const int at_w = c[j] + weight_column<T>(i);
-      float4* to = reinterpret_cast<float4*>(units + (2 * j + i) * THREADS);
-      const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-      to[0] = p.wpost ? *reinterpret_cast<const float4*>(p.wpost + (p.shared ? at_w % p.G : at_w))
-                      : one;
-      to[2 * V * THREADS] = p.wpre ? *reinterpret_cast<const float4*>(p.wpre + at_w) : one;
-    }
-  }
   const bool post_norm = FULL || p.post, pre_norm = FULL || (FORM == kAny && p.pre);
   const bool heads = !FULL && p.post && p.G != p.W;
   const float per_group = 1.f / (float)p.G, per_row = 1.f / (float)p.W;
@@ -151,6 +139,29 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
   cp_async_commit();
   fetch_x(first + step, 1);
   cp_async_commit();
+  // the weights, all asked for before the first is put down, behind the first rows
+  float4 w_post[V][2], w_pre[V][2];
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      w_post[j][i] = w_pre[j][i] = make_float4(1.f, 1.f, 1.f, 1.f);
+      if (!mine[j][i % H]) continue;
+      const int at_w = c[j] + weight_column<T>(i);
+      if (p.wpost)
+        w_post[j][i] =
+            *reinterpret_cast<const float4*>(p.wpost + (p.shared ? at_w % p.G : at_w));
+      if (p.wpre) w_pre[j][i] = *reinterpret_cast<const float4*>(p.wpre + at_w);
+    }
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (!mine[j][i % H]) continue;
+      float4* to = reinterpret_cast<float4*>(units + (2 * j + i) * THREADS);
+      to[0] = w_post[j][i];
+      to[2 * V * THREADS] = w_pre[j][i];
+    }
   cp_async_wait<2>();
   // of a vector, over its groups where it has some (else all of it in the first)
   const auto sums_of = [&](const uint64_t (&a)[4], const uint64_t (&b)[4], float (&sum)[2]) {
