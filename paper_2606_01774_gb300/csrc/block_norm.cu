@@ -155,14 +155,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (s.cluster > 1) cluster_sync();  // none leaves while another may write to its memory
 }
 
-// The CTAs' weight gradients joined: 32 columns a CTA, its warps one partial sum in 32 each, 16 of
-// them in flight, added in order at the end: the same bits every time, which atomics would not
-// give.  3.4 to 5.5 us behind the rows, started while their last CTAs finish.
+// The CTAs' weight gradients joined: 32 columns a CTA, its warps one partial sum in 32 (or 16) each,
+// 16 of them in flight, added in order at the end: the same bits every time, which atomics would
+// not give.  3 to 5 us behind the rows, started while their last CTAs finish.
 __global__ void __launch_bounds__(1024)
     block_norm_weights_kernel(const __grid_constant__ BlockNormParams p, int ctas, int cluster) {
   constexpr int kInFlight = 16;
   __shared__ float buf[32][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int wide_post = p.shared ? p.G : p.W;
   const bool post = blockIdx.y == 0;
   float* out = post ? p.dwpost : p.dwpre;
@@ -173,19 +173,21 @@ __global__ void __launch_bounds__(1024)
   float sum = 0.f;
   if (c < wide) {
     const float* at = p.part + (post ? 0 : (int64_t)ctas * wide_post) + c;
-    for (int i0 = warp; i0 < n; i0 += 32 * kInFlight) {
+    for (int i0 = warp; i0 < n; i0 += warps * kInFlight) {
       float part[kInFlight];
 #pragma unroll
       for (int k = 0; k < kInFlight; ++k)
-        part[k] = i0 + 32 * k < n ? at[(int64_t)(i0 + 32 * k) * wide] : 0.f;
+        part[k] = i0 + warps * k < n ? at[(int64_t)(i0 + warps * k) * wide] : 0.f;
 #pragma unroll
       for (int k = 0; k < kInFlight; ++k) sum += part[k];
     }
   }
   buf[warp][lane] = sum;
   __syncthreads();
-  sum = warp_sum(buf[lane][warp]);
-  if (lane == 0 && blockIdx.x * 32 + warp < wide) out[blockIdx.x * 32 + warp] = sum;
+  for (int col = warp; col < 32; col += warps) {
+    sum = warp_sum(lane < warps ? buf[lane][col] : 0.f);
+    if (lane == 0 && blockIdx.x * 32 + col < wide) out[blockIdx.x * 32 + col] = sum;
+  }
 }
 
 namespace {
@@ -245,7 +247,12 @@ cudaError_t launch_block_norm_bwd(const BlockNormParams& p, bool bf16, int num_s
   }
   if (weights) {  // of no rows: zeros
     note_launches(1);
-    return pdl_launch(block_norm_weights_kernel, dim3((unsigned)(p.W + 31) / 32, 2), 1024, 0,
+    // 16 warps where they take all sums at once, or where CTAs of 32 are more than the SMs hold (300
+    // rows of 6000: 13.8 us, 14.3; 150 of 8192: 13.3, 15.0), 32 for many sums of few columns (1021
+    // fp32 rows of 16 heads: 19.4 us, 19.7)
+    const bool few = ctas / cluster <= 16 * 16 || (p.W + 31) / 32 * 2 > num_sms;
+    const int threads = few ? 512 : 1024;
+    return pdl_launch(block_norm_weights_kernel, dim3((unsigned)(p.W + 31) / 32, 2), threads, 0,
                       stream, p.T > 0, 1, p, ctas, cluster);
   }
   return cudaSuccess;
