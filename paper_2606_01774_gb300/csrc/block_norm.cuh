@@ -13,10 +13,10 @@
 // cluster of two or four.  Teams walk their rows; a thread copies its own elements
 // of the next rows to its own places in shared memory meanwhile (cp.async), so loads need no
 // barrier, and only the sums over a row meet other threads.  16384 bf16 rows of 4096 with both
-// norms and a residual: forward 89 us (6.0 TB/s, a copy's rate being 6.8), backward 135 us
-// (5.9 TB/s).  Where rows are so wide or inputs so many that two rows of all of them fill an SM's
+// norms and a residual: forward 89 us (6.0 TB/s, a copy's rate being 6.8), backward 132 us
+// (6.1 TB/s).  Where rows are so wide or inputs so many that two rows of all of them fill an SM's
 // shared memory, loads wait for sums: 8960 gated bf16 rows of 6400 with norms per head backward
-// 291 us (3.2 TB/s).
+// 286 us (3.2 TB/s).
 #pragma once
 
 #include <cuda_runtime.h>
