@@ -302,7 +302,7 @@ BlockNormParams block_norm_params(const flare_block_norm_desc* d, const void* x,
   p.T = d->num_tokens;
   p.W = d->width;
   p.G = d->group ? d->group : d->width;
-  p.shared = d->shared_weight;
+  p.shared = d->shared_weight && p.G < d->width;  // of one group the weight has W entries either way
   p.post = d->post_norm;
   p.pre = d->pre_norm;
   p.act = d->gate_act;

@@ -339,6 +339,7 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
       store_weights<T>(sums + threadIdx.y * cols + first_column<T>(j), kind ? dwpre[j] : dwpost[j],
                        all);
     __syncthreads();
+    // over the groups, of which every CTA of a cluster has whole ones: `from` is a multiple of G
     const bool by_group = p.shared && !kind;
     const int n = by_group ? p.G : used;
     for (int i = thread; i < n; i += threads) {

@@ -279,7 +279,7 @@ cudaError_t launch_tree_logits(const TreeLogitsParams& p, bool bf16, int num_sms
                                cudaStream_t stream);
 
 struct BlockNormParams {
-  int T, W, G, shared, post, pre, act;
+  int T, W, G, shared, post, pre, act;  // shared: one weight for all groups, of which there are several
   float eps, alpha;
   int64_t x_stride, gate_stride;
   const void* x;
