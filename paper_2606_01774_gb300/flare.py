@@ -441,8 +441,8 @@ def _rows(t, step, inner, device):
         return None
     if t.get_device() != device:
         raise ValueError("tensors must be on the current device")
-    strides = t.stride()
-    if len(strides) == inner + 1 and strides[0] == step and (
+    strides = t.stride()  # 0 over rows: one row repeated, not dense
+    if step and len(strides) == inner + 1 and strides[0] == step and (
             strides[-1] == 1 and (inner == 1 or strides[1] == t.shape[2])):
         return t.data_ptr()
     if not step and t.is_contiguous():
