@@ -416,6 +416,7 @@ __global__ void __launch_bounds__(kThreads, kCtas)
       any = true;
       atomicOr(&biased[e >> 5], 1u << (e & 31));
     }
+    __syncwarp();  // every lane's bits, before others read them: a vote orders no memory
     if (__any_sync(0xffffffffu, any)) {
       uint32_t total = 0;
       for (int i0 = 0; i0 < bit_words; i0 += 32) {
