@@ -250,7 +250,8 @@ inline Shape teams_for(int T, int W, int vectors, int threads, int num_sms) {
 
 // One CTA or cluster for every `teams` rows, until the SMs have `per_sm` CTAs each.
 inline void set_ctas(Shape& s, int T, int per_sm, int num_sms) {
-  const int rows = (T + s.teams - 1) / s.teams, clusters = per_sm * num_sms / s.cluster;
+  const int rows = T / s.teams + (T % s.teams != 0);  // T may be the last int
+  const int clusters = per_sm * num_sms / s.cluster;
   s.ctas = (rows < clusters ? rows : clusters) * s.cluster;
 }
 

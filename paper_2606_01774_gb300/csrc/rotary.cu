@@ -257,8 +257,9 @@ static cudaError_t launch(const RotaryParams& p, int num_sms, cudaStream_t strea
   // (32768 rows of 9 KiB: 117 us with 32 rows, 110 with 16, 105 with 8, 99 with 4, 101 with
   // 2), smaller ones work out few at a time (of 6 KiB: 63, 61, 61, 62, 67)
   int tile = 16;
+  const auto tiles = [&] { return ((int64_t)p.rows + tile - 1) / tile; };
   while (tile > 1 && ((int64_t)tile * heads * p.D * (int)sizeof(T) > kTileBytes ||
-                      (p.rows + tile - 1) / tile < 2 * num_sms))
+                      tiles() < 2 * num_sms))
     tile /= 2;
   // as many rows at a time as the tile has, or four heads in flight per thread
   int log2_slots = 0;
@@ -267,7 +268,7 @@ static cudaError_t launch(const RotaryParams& p, int num_sms, cudaStream_t strea
     ++log2_slots;
   const int smem = tile * (p.rd / 4 * (int)sizeof(float4) + 2 * (int)sizeof(int64_t) +
                            (int)sizeof(int));
-  const unsigned grid = (unsigned)((p.rows + tile - 1) / tile);
+  const unsigned grid = (unsigned)tiles();
   if (p.interleaved)
     rotary_kernel<T, true><<<grid, kThreads, smem, stream>>>(p, tile, log2_units, log2_slots);
   else

@@ -301,3 +301,14 @@ def test_the_binding_refuses_other_strides_and_devices(monkeypatch):
         flare.flare_block_norm(n, x[:, ::2], None, None, None, None, None, x, stream=0)
     assert flare.flare_block_norm(n, x[:, :1024], None, None, None, None, None, x.clone(),
                                   stream=0) == OK
+
+
+def test_row_counts_up_to_the_last_int(lib):
+    """The workspace of 2^31 - 1 rows is that of 2^30: the launch has as many CTAs as the SMs hold."""
+    for width in (8, 64, 1024, 4096, 16384):
+        for dtype in (flare.FLARE_DT_BF16, flare.FLARE_DT_F32):
+            for pre in (0, 1):
+                need = [flare.flare_block_norm_bwd_workspace_size(
+                    flare.block_norm_desc(t, width, dtype, pre_norm=pre))
+                    for t in (1 << 30, (1 << 31) - 8, (1 << 31) - 1)]
+                assert need[0] > 0 and need == need[:1] * 3, (width, dtype, pre, need)
