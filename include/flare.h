@@ -884,7 +884,8 @@ flare_status flare_block_norm(const flare_block_norm_desc* desc, const void* x, 
                               const void* residual, const float* post_weight,
                               const float* pre_weight, void* y, void* h, void* stream);
 
-/* Bytes of device workspace flare_block_norm_bwd needs (partial weight gradients).  Host-only. */
+/* Bytes of device workspace flare_block_norm_bwd needs (partial weight gradients); enough for
+ * every num_tokens up to the descriptor's, the rest of it the same.  Host-only. */
 flare_status flare_block_norm_bwd_workspace_size(const flare_block_norm_desc* desc,
                                                  size_t* bytes);
 

@@ -354,9 +354,10 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
 
 // Vectors per thread and threads per CTA: what holds most of the rows in flight on an SM, and most
 // warps.  (Rows of 4096 in bf16: two CTAs of 256 threads, 16 elements each; where inputs are so
-// many or so wide that one CTA fills the shared memory, 512 threads.)
+// many or so wide that one CTA fills the shared memory, 512 threads.)  Fewer rows may take another
+// kind, with more CTAs: most_ctas, if given, becomes what any number of rows up to T_rows takes at most.
 template <typename T, bool GATE, bool PRE>
-Shape backward_shape(int T_rows, int W, int num_sms) {
+Shape backward_shape(int T_rows, int W, int num_sms, int* most_ctas = nullptr) {
   Shape best = {};
   int best_score = 0;
   const auto consider = [&](int kind, int units, int vectors, int threads) {
@@ -365,6 +366,12 @@ Shape backward_shape(int T_rows, int W, int num_sms) {
     if (!s.cluster || s.smem + kSmemStatic > kSmemMost) return;
     const int room = kSmem / (s.smem + kSmemOwn);
     const int per_sm = room < 512 / threads ? room : 512 / threads;
+    if (most_ctas) {  // of this kind: a row to every CTA or cluster
+      Shape one = s;
+      one.teams = 1;
+      set_ctas(one, T_rows, per_sm, num_sms);
+      if (one.ctas > *most_ctas) *most_ctas = one.ctas;
+    }
     const int used = per_sm * s.team * s.teams, warps = used / 32;
     // a cluster's barriers cost as much as half of the rows in flight, sixteen vectors as a warp
     const int score = used * vectors / (s.cluster > 1 ? 2 : 1) + 16 * warps;
@@ -421,11 +428,15 @@ cudaError_t launch_block_norm_rows(const BlockNormParams& p, int num_sms, int* c
 
 template <typename T>
 int block_norm_rows_ctas(int T_rows, int W, bool pre, int num_sms) {
-  const Shape gated = pre ? backward_shape<T, true, true>(T_rows, W, num_sms)
-                          : backward_shape<T, true, false>(T_rows, W, num_sms);
-  const Shape plain = pre ? backward_shape<T, false, true>(T_rows, W, num_sms)
-                          : backward_shape<T, false, false>(T_rows, W, num_sms);
-  return gated.ctas > plain.ctas ? gated.ctas : plain.ctas;
+  int most = 0;
+  if (pre) {
+    backward_shape<T, true, true>(T_rows, W, num_sms, &most);
+    backward_shape<T, false, true>(T_rows, W, num_sms, &most);
+  } else {
+    backward_shape<T, true, false>(T_rows, W, num_sms, &most);
+    backward_shape<T, false, false>(T_rows, W, num_sms, &most);
+  }
+  return most;
 }
 
 }  // namespace flare

@@ -300,8 +300,8 @@ struct BlockNormParams {
 };
 cudaError_t launch_block_norm(const BlockNormParams& p, bool bf16, int num_sms,
                               cudaStream_t stream);
-// The backward pass over rows (T of bf16 or fp32) and how many CTAs it takes at most: each
-// leaves one partial weight gradient.
+// The backward pass over rows (T of bf16 or fp32) and how many CTAs it takes at most, on so many
+// rows or fewer: each leaves one partial weight gradient.
 template <typename T>
 cudaError_t launch_block_norm_rows(const BlockNormParams& p, int num_sms, int* ctas, int* cluster,
                                    cudaStream_t stream);

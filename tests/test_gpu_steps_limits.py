@@ -1,4 +1,5 @@
-"""Block norms at the largest number of rows that a descriptor can name."""
+"""Block norms at the largest number of rows that a descriptor can name, and what their gradients take of
+a workspace."""
 import pytest
 import torch
 
@@ -32,3 +33,26 @@ def test_as_many_rows_as_an_int_counts():
     size = (s.dy.double() * n / (n.square().mean(1, keepdim=True) + 1e-6).sqrt()).abs().sum(0)
     off = (dw.double() - grad["dpost_weight"].double()).abs()
     assert bool((off <= 2 * GRAD_REL * size).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,W,how", [
+    (1, 128, {}), (189, 128, {}), (189, 512, dict(gate="silu")), (1924, 128, dict(pre=False)),
+    (444, 1024, {}), (2000, 2048, dict(gate="silu", group=128, shared=True, pre=False)),
+    (700, 4104, {}), (90, 6400, dict(gate="silu", group=128, shared=True)), (300, 16384, {})])
+def test_a_workspace_of_more_rows(T, W, how, dtype):
+    """Calls stay within what their own number of rows needs, and take a workspace of more rows."""
+    s = norm_inputs(91 + W, T, W, dtype, **how)
+    want = run_norm_bwd(s)
+    need = flare.flare_block_norm_bwd_workspace_size(s.desc)
+    s.desc.num_tokens = 1 << 20
+    more = flare.flare_block_norm_bwd_workspace_size(s.desc)
+    s.desc.num_tokens = T
+    assert more >= need
+    ws = torch.full((more + 4096,), 0x55, dtype=torch.uint8, device="cuda")
+    new = {k: None if x is None else torch.empty_like(x) for k, x in want.items()}
+    flare.check(flare.flare_block_norm_bwd(s.desc, s.x, s.gate, s.residual, s.post_weight,
+                                           s.pre_weight, s.dy, s.dh, *new.values(), ws, more))
+    for k, x in new.items():
+        assert x is None or torch.equal(bits(x), bits(want[k])), k
+    assert bool((ws[need:] == 0x55).all())

@@ -312,3 +312,19 @@ def test_row_counts_up_to_the_last_int(lib):
                     flare.block_norm_desc(t, width, dtype, pre_norm=pre))
                     for t in (1 << 30, (1 << 31) - 8, (1 << 31) - 1)]
                 assert need[0] > 0 and need == need[:1] * 3, (width, dtype, pre, need)
+
+
+@pytest.mark.parametrize("dtype", [flare.FLARE_DT_BF16, flare.FLARE_DT_F32])
+@pytest.mark.parametrize("pre", [0, 1])
+def test_a_workspace_serves_smaller_batches(lib, pre, dtype):
+    """More rows never need less, so that one workspace is sized by a program's largest batch."""
+    counts = sorted({*range(0, 40), *range(40, 5000, 61), *(2 ** i + j for i in range(5, 31)
+                                                          for j in (-1, 0, 1)), 2 ** 31 - 1})
+    for width in (8, 64, 128, 512, 1024, 1368, 2048, 4096, 4104, 6016, 8192, 8200, 16384):
+        last = 0
+        for t in counts:
+            need = flare.flare_block_norm_bwd_workspace_size(
+                flare.block_norm_desc(t, width, dtype, pre_norm=pre))
+            assert need >= last and need % (8 * width) == 0, (width, t)
+            assert need > 0 or t == 0
+            last = need
