@@ -253,8 +253,8 @@ typedef struct flare_rotary_freq_desc {
  *   num_q_heads Hq, num_kv_heads Hkv, head_dim D (64, 128 or 256), rotary_dim
  *   (a multiple of 16, 16..D: the first elements of each head; the others are
  *   passed on), layout, inverse (1: by the negative angles, which is the
- *   gradient of the rotation), act_dtype, amplitude (finite; multiplies the
- *   rotated elements), q_stride, k_stride, v_stride (elements from one row of
+ *   gradient of the rotation), act_dtype, amplitude (below 3e38 in magnitude;
+ *   multiplies the rotated elements), q_stride, k_stride, v_stride (elements from one row of
  *   the inputs to the next, 0 = Hq D or Hkv D; multiples of 16 bytes, so that
  *   slices of a fused projection are read in place), and for the append
  *   page_size (16, 32, 64 or 128), num_pages and max_pages_per_req. */
@@ -296,9 +296,9 @@ typedef struct flare_tree_logits_desc {
  *   the block (0 = W, or 64, 128 or 256 dividing W: a norm per head),
  *   shared_weight (1: its weight has G entries for all groups, 0: W entries),
  *   post_norm and pre_norm (0 or 1: whether there is a norm after the block and
- *   before the next), gate_act, act_dtype, eps (> 0 and finite), residual_scale
- *   (finite), x_stride and gate_stride (elements from one row to the next, 0 =
- *   W; multiples of 16 bytes). */
+ *   before the next), gate_act, act_dtype, eps (> 0 and below 3e38),
+ *   residual_scale (below 3e38 in magnitude), x_stride and gate_stride (elements
+ *   from one row to the next, 0 = W; multiples of 16 bytes). */
 typedef struct flare_block_norm_desc {
   int32_t num_tokens;
   int32_t width;
@@ -831,7 +831,8 @@ flare_status flare_rotary_append_kv(const flare_rotary_desc* desc, const void* q
  *     y = seen(x) ? (l > 0 ? l / repetition : l * repetition) : l
  *     out = y - frequency c(x) - presence [c(x) > 0] + b(x)
  * and -inf where the mask rules x out, whatever the logit is.  A row whose mask
- * leaves nothing becomes -inf throughout.  fp32 arithmetic, one rounding.
+ * leaves nothing becomes -inf throughout.  fp32 arithmetic (l / repetition as a product
+ * with the reciprocal in fp32), one rounding to logits_dtype.
  * Rows of nodes from node_len[r] on are neither used nor written.  Ordinary
  * decoding is N = 1.
  *   logits       [R, N, V] logits_dtype (any V; rows need no alignment)

@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // The CTAs' weight gradients joined: 32 columns a CTA, its warps one partial sum in 32 (or 16) each,
 // 16 of them in flight, added in order at the end: the same bits every time, which atomics would
-// not give.  3 to 5 us behind the rows, started while their last CTAs finish.
+// not give.  3 to 8 us behind the rows, started while their last CTAs finish.
 __global__ void __launch_bounds__(1024)
     block_norm_weights_kernel(const __grid_constant__ BlockNormParams p, int ctas, int cluster) {
   constexpr int kInFlight = 16;

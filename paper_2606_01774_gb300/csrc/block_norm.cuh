@@ -116,7 +116,8 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
 }
 
 // 1 / (1 + e^-z) by the fast exponential and reciprocal.  For fp32 the exponent z log2 e is taken
-// in two parts (its rounding is a relative error of |z| 2^-24): 2^-22 in all.  A NaN stays one.
+// in two parts (its rounding is a relative error of |z| 2^-24): 2^-22 in all.  A NaN stays one; below
+// -87.3, where the sigmoid is less than 2^-126, it is 0.
 template <typename T>
 __device__ __forceinline__ float sigmoid(float z) {
   constexpr float kLog2e = 1.44269504089f;

@@ -73,7 +73,9 @@ enum Form {
 // goes along with this row's last sum, so x arrives a row ahead of the other inputs.  What a sum
 // separates is read again after it, rather than held: of 128 registers a thread the weights'
 // gradients take 32.  alpha enters by the rows' factors alone.  With the form known 16384 rows of
-// 4096 take 135 us, 183 without; 1021 fp32 rows of 16 heads, an output stage, 20 and 23.
+// 4096 take 132 us, 150 without; 16384 bf16 rows of 16 heads, an output stage, 90 and 99 on CTAs of one
+// kind.  Forms with a gate, but for the output stage's, pass 4 to 196 bytes a thread through local
+// memory, kAny in fp32 24 without one.
 template <typename T, bool GATE, int FORM, bool SIMPLE, int V, int THREADS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS)
     block_norm_bwd_kernel(const __grid_constant__ BlockNormParams p,
@@ -354,7 +356,9 @@ __global__ void __launch_bounds__(THREADS, 512 / THREADS)
 
 // Vectors per thread and threads per CTA: what holds most of the rows in flight on an SM, and most
 // warps.  (Rows of 4096 in bf16: two CTAs of 256 threads, 16 elements each; where inputs are so
-// many or so wide that one CTA fills the shared memory, 512 threads.)  Fewer rows may take another
+// many or so wide that one CTA fills the shared memory, 512 threads.  Output stages would do better with
+// fewer CTAs than it finds: 1021 fp32 rows of 16 heads 19.5 us, 16.3 by the kind that a call with a
+// norm before the next block gets.)  Fewer rows may take another
 // kind, with more CTAs: most_ctas, if given, becomes what any number of rows up to T_rows takes at most.
 template <typename T, bool GATE, bool PRE>
 Shape backward_shape(int T_rows, int W, int num_sms, int* most_ctas = nullptr) {

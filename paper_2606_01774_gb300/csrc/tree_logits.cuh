@@ -11,11 +11,13 @@
 // own tokens come last, each by its count on every node's path.
 //
 // Bound by bytes once there are many rows, logits in and out (64 requests x 64 nodes over 32000
-// bf16 tokens: 102 us, 5.3 TB/s); with few, by the steps before them: lengths, tree, history and
-// biases are round trips to memory one after another, some 3 us, and a history of 8192 tokens is
-// counted in 3 us more, once per chunk (64 x 16 nodes under a mask: 33 us, 4.1 TB/s; 64 x 1 over
-// 128000: 23 us).  One wave of three CTAs an SM keeps that to once; two took 1.3 to 1.5 times as
-// long.
+// bf16 tokens: 99 us, 5.3 TB/s, under a mask 102); with few, by the steps before them: lengths,
+// tree, history and biases are round trips to memory one after another, some 3 us, and a history of
+// 8192 tokens is counted once per chunk, 3 us of 34 for 64 x 16 nodes under a mask (4.1 TB/s), 9 of
+// 24 for 64 x 1 over 128000.  One wave of three CTAs an SM keeps that to once; with two these take 40
+// and 28 us.  Some masked forms and those for one or two fp32 rows pass what 80 registers a thread
+// do not hold through local memory (12 to 308 bytes); with registers for two CTAs an SM, where
+// nothing does, the two calls take 39 and 26 us.
 #pragma once
 
 #include "common.cuh"
@@ -245,16 +247,16 @@ struct Batch {
 
 // W: bytes on whose boundaries all rows start, up to 16.  A lane's piece is 16 bytes in parts of W, a
 // warp's parts next to each other: the same tokens in every row, whatever V is.  (fp32 parts of 4
-// against W = 0, 9 trees of 13 over 50257 tokens: 11 us, 18.)  W = 0, for bf16 rows on 2 or 4
+// against W = 0, 9 trees of 13 over 50257 tokens: 11 us, 12.)  W = 0, for bf16 rows on 2 or 4
 // bytes: pieces start at each row's own 16-byte boundaries and look up their tokens in each (parts
 // of 2, 4 trees of 26 over 81625: 34 us, 25 at the time and now 14).  FEW: rows too few to keep a
-// batch under way, so several blocks of a row are (64 x 1 over 128000: 24 us, 42 without).
+// batch under way, so several blocks of a row are (64 x 1 over 128000: 24 us, 29 without).
 template <typename T, int W, bool MASK, bool IN_PLACE, bool FEW>
 __global__ void __launch_bounds__(kThreads, kCtas)
     tree_logits_kernel(const __grid_constant__ TreeLogitsParams p, int chunk, int chunks,
                        int row_parts, bool narrow) {
   constexpr int E = Piece<T>::N;               // elements of a piece
-  // In flight per thread, twice.  W = 0 has to remember more with each (three: 44 us, two: 35, for 16
+  // In flight per thread, twice.  W = 0 has to remember more with each (three: 44 us, two: 36, for 16
   // trees of 36 nodes over 52711 tokens under a mask).
   constexpr int kRows = W ? kRowsOf<T> : 2;
   constexpr uint32_t kFull = (1u << E) - 1;
@@ -705,7 +707,7 @@ template <typename T>
 cudaError_t launch_tree_logits_of(const TreeLogitsParams& p, int num_sms, cudaStream_t stream) {
   // One wave of CTAs, if chunks of 512 to 32768 tokens allow it: a history is counted once per chunk.
   // Counts of 16 bits only where those of 32 need more memory than the wave leaves (64 x 1 over 128000:
-  // 24 us with three CTAs an SM, 30 with two): they cost a shift each.
+  // 24 us with three CTAs an SM, 28 with two): they cost a shift each.
   const auto smem_of = [&](int chunk, bool narrow) {
     const int biases = p.bias_token ? p.max_bias < chunk ? p.max_bias : chunk : 0;
     return (at(narrow ? chunk / 2 : chunk) + 4 * (chunk / 32 + 1) + 3 + biases + 3) / 4 * 16;
